@@ -395,6 +395,160 @@ ra_status ra_adapter_backward_noalloc(const float* g_dev, const float* h_dev, co
                                       float* dh_dev, ra_stream_t stream);
 size_t ra_adapter_backward_noalloc_capacity(void);
 
+/* ---------------------------------------------------------------------------------------
+ * Operators that answer with a tuned decoder: a paged key-value cache, attention of the newest
+ * tokens over it, its eviction, attention with a sliding window over whole sequences (forward and
+ * backward) and the verification of drafted tokens.  The paper has no counterpart: it ends with the
+ * tuned adapters.  No context: a call takes one argument block (a struct that the caller fills in,
+ * zero for what it leaves out, and may keep for as long as its buffers stay) and a stream.
+ *
+ * Conventions, beside those at the top
+ *   - Types are RA_F32 or RA_BF16, one for all of a call's queries, keys, values and outputs; sums,
+ *     softmax statistics, log-sum-exps and accumulated weights are float32 in either case.
+ *   - A stride is in elements, from one token's first head to the next token's; the heads of a token are
+ *     next to each other, head_dim values each.  16-byte aligned bases, and strides and head dims whose
+ *     rows keep that alignment (8 values of bf16, 4 of float32), or RA_ERR_ARG / RA_ERR_SHAPE.
+ *   - Grouped heads: query head h reads key-value head h / (n_heads / n_kv_heads); n_heads is a multiple
+ *     of n_kv_heads.
+ *   - Token i sees token j when j <= i and (window == 0 or i - j < window or j < sinks): the `window`
+ *     newest tokens, itself among them, and the first `sinks` ones.  A query that sees nothing has output
+ *     zero and log-sum-exp -inf.
+ *   - A workspace is caller-owned, 256-byte aligned, at least the bytes that the call's _workspace_bytes
+ *     gives for the same argument block, and zero-filled once before its first use: calls leave zero what
+ *     they need to find zero.  Calls that may run at the same time need different workspaces.  RA_ERR_NOMEM
+ *     for one that is too small.
+ *   - err_dev (nullable): a device word into which kernels or RA_DEV_BOUNDS where an index that they read on
+ *     the device is out of range (a page of the table, a length, a position), and RA_DEV_TIMEOUT where a
+ *     bounded wait ran out.  Such an index is never followed: a length is clamped to [0, capacity], tokens of
+ *     a bad page are not there.
+ *   - RA_ERR_UNSUPPORTED on a device that is not sm_103.
+ * ------------------------------------------------------------------------------------- */
+enum { RA_DEV_TIMEOUT = 1, RA_DEV_BOUNDS = 2 };
+
+/* The cache of one layer: pages of page_size tokens, [n_pages, n_kv_heads, page_size, head_dim] for keys
+ * and for values.  Slot s of sequence b (its s-th cached token) is row s % page_size of page
+ * block_table[b, s / page_size].  head_dim <= 256, a multiple of 8 (bf16) or 4 (f32). */
+typedef struct {
+  void* k_dev;
+  void* v_dev;
+  const int32_t* block_table_dev; /* [batch, max_pages] */
+  uint32_t* err_dev;              /* nullable */
+  int32_t n_pages, max_pages, page_size, n_kv_heads, head_dim, dtype;
+} ra_kv_cache;
+
+/* Puts the keys and values of the n_new newest tokens of each sequence into the cache and turns queries
+ * and keys by rotate-half RoPE: the pair (x_i, x_{i + head_dim/2}) becomes (x_i c - x_{i+} s, x_{i+} c +
+ * x_i s) with (c, s) = rope[p, i], rope[p, head_dim/2 + i].  lens counts the new tokens: token t of
+ * sequence b goes to slot lens[b] - n_new + t and has position p = pos[b] - n_new + t (pos NULL: lens; after
+ * an eviction a sequence has seen more tokens than it has cached).  Tokens of negative slot are padding:
+ * not stored, their rotated queries zero.  Positions outside [0, rope_len) are read at the nearest end and
+ * reported.  q_dev NULL: keys and values alone.  rope_dev NULL: nothing is turned.  q_out may be q. */
+typedef struct {
+  ra_kv_cache cache;
+  const int32_t* lens_dev;               /* [batch] */
+  const int32_t* pos_dev;                /* [batch] or NULL */
+  const void *q_dev, *k_dev, *v_dev;     /* [batch * n_new] tokens of n_heads / n_kv_heads heads */
+  void* q_out_dev;                       /* [batch * n_new, n_heads, head_dim] */
+  int64_t q_stride, k_stride, v_stride, q_out_stride;
+  const float* rope_dev;                 /* [rope_len, head_dim]: cosines, then sines; or NULL */
+  int32_t rope_len, batch, n_new, n_heads;
+} ra_kv_append_args;
+ra_status ra_kv_append(const ra_kv_append_args* args, ra_stream_t stream);
+
+/* Attention of the n_new newest tokens of each sequence (token t at slot lens[b] - n_new + t, already in the
+ * cache) over its cached tokens: out = softmax(scale q k^T) v over the slots that it sees.  One token a
+ * sequence is the ordinary step; several check drafted ones.
+ * weights_out (nullable): weights_out[b, e, s] = weights_in[b, e, s] + the softmax weights that slot s got
+ * from the new tokens through the query heads of key-value head e, for s < lens[b] (weights_in NULL: 0; it
+ * may be weights_out); other slots are not touched.
+ * max_len: no sequence is longer (0: the table's capacity); it sizes the workspace and clamps lens. */
+typedef struct {
+  ra_kv_cache cache;
+  const int32_t* lens_dev;               /* [batch] */
+  const void* q_dev; int64_t q_stride;   /* [batch * n_new, n_heads, head_dim] */
+  void* out_dev; int64_t out_stride;
+  float* lse_dev;                        /* [batch, n_new, n_heads] natural log, or NULL */
+  const float* weights_in_dev;           /* [batch, n_kv_heads, weights_stride] */
+  float* weights_out_dev;
+  int64_t weights_stride;
+  void* workspace_dev; size_t workspace_bytes;
+  int32_t batch, n_new, n_heads, max_len, window, sinks;
+  float scale;
+} ra_attention_decode_args;
+size_t ra_attention_decode_workspace_bytes(const ra_attention_decode_args* args);
+ra_status ra_attention_decode(const ra_attention_decode_args* args, ra_stream_t stream);
+
+/* Eviction by accumulated weight.  A sequence of at most `budget` tokens keeps them all.  A longer one keeps,
+ * for each key-value head by itself, its first `first` and its newest `recent` tokens and, of those
+ * between, the budget - first - recent of the largest weight (of equal ones the lowest slots; a NaN counts as
+ * larger than any number).  The kept tokens are copied in order to slots 0, 1, ... of the dst cache, whose
+ * pages no src page of these sequences may be; kept[b, e, i] is the slot that slot i came from (-1 beyond
+ * the new length), weights_out[b, e, i] its weight (0 up to budget), lens_out[b] = min(lens[b], budget).
+ * RA_ERR_ARG for first + recent > budget; RA_ERR_SHAPE where src and dst differ in heads, head dim or type
+ * or dst's table cannot hold budget tokens. */
+typedef struct {
+  ra_kv_cache src, dst;
+  const int32_t* lens_dev;               /* [batch] */
+  const float* weights_dev;              /* [batch, n_kv_heads, weights_stride] */
+  int64_t weights_stride;
+  int32_t* lens_out_dev;                 /* [batch] */
+  int32_t* kept_dev;                     /* [batch, n_kv_heads, budget] */
+  float* weights_out_dev;                /* [batch, n_kv_heads, weights_out_stride] or NULL */
+  int64_t weights_out_stride;
+  int32_t batch, max_len, budget, first, recent;
+} ra_kv_evict_args;
+ra_status ra_kv_evict(const ra_kv_evict_args* args, ra_stream_t stream);
+
+/* Causal attention with a window and sinks over whole sequences [batch, seq] (a prompt, a training step):
+ * out = softmax(scale q k^T) v over the tokens that each sees, and the log-sum-exp of each row.  lens
+ * (nullable): sequence b has lens[b] tokens; rows past them see nothing and are seen by nothing, and what
+ * their memory holds does not matter.  Head dims: 64 and 128 (bf16), multiples of 4 up to 128 (f32).
+ * The backward takes the same block, with out and lse as the forward left them, and writes dq, dk and dv
+ * (zero past a sequence's end), the shared heads' gradients summed over their query heads in a fixed order.
+ * The workspace is for the backward alone. */
+typedef struct {
+  const void *q_dev, *k_dev, *v_dev;     /* [batch * seq] tokens of n_heads / n_kv_heads heads */
+  int64_t q_stride, k_stride, v_stride;
+  void* out_dev; int64_t out_stride;     /* [batch * seq, n_heads, head_dim] */
+  float* lse_dev;                        /* [batch, n_heads, seq] natural log; NULL: forward alone */
+  const int32_t* lens_dev;               /* [batch] or NULL */
+  const void* dout_dev; int64_t dout_stride;
+  void *dq_dev, *dk_dev, *dv_dev;
+  int64_t dq_stride, dk_stride, dv_stride;
+  void* workspace_dev; size_t workspace_bytes;
+  uint32_t* err_dev;                     /* nullable */
+  int32_t batch, seq, n_heads, n_kv_heads, head_dim, window, sinks, dtype;
+  float scale;
+} ra_attention_window_args;
+size_t ra_attention_window_workspace_bytes(const ra_attention_window_args* args);
+ra_status ra_attention_window_forward(const ra_attention_window_args* args, ra_stream_t stream);
+ra_status ra_attention_window_backward(const ra_attention_window_args* args, ra_stream_t stream);
+
+/* Verification of drafted tokens against the target's probabilities, from given random numbers, so that
+ * what comes out is distributed as the target's own samples.  target[b, i] and draft[b, i] are the two
+ * models' probabilities over the vocabulary for the place of drafted token tokens[b, i]; target has one
+ * row more.  Drafted token i stands while uniform[b, i] * draft < target (compared without rounding) at
+ * it and at all before it.  At the first that does not stand, n, the next token is
+ * argmax_v max(target[b, n, v] - draft[b, n, v], 0) / noise[b, v], and target[b, n, v] / noise[b, v] where
+ * all stand or that difference is nowhere positive; with noise exponentially distributed, a sample of the
+ * normalised numerator.  Ties go to the lowest token; a NaN counts as 0.  accepted[b] = n; out_tokens[b] =
+ * the n drafted tokens, the next one, then -1.  n_drafted (nullable): sequence b has n_drafted[b] <= n_draft
+ * drafts.  A drafted token outside the vocabulary does not stand. */
+typedef struct {
+  const void* target_dev; int64_t target_stride; /* [batch, n_draft + 1] rows of vocab values */
+  const void* draft_dev; int64_t draft_stride;   /* [batch, n_draft] rows */
+  const int32_t* tokens_dev;                     /* [batch, n_draft] */
+  const int32_t* n_drafted_dev;                  /* [batch] or NULL */
+  const float* uniform_dev;                      /* [batch, n_draft] in [0, 1) */
+  const float* noise_dev;                        /* [batch, vocab], positive */
+  int32_t* accepted_dev;                         /* [batch] */
+  int32_t* out_tokens_dev;                       /* [batch, n_draft + 1] */
+  void* workspace_dev; size_t workspace_bytes;
+  int32_t batch, n_draft, vocab, dtype;
+} ra_verify_draft_args;
+size_t ra_verify_draft_workspace_bytes(const ra_verify_draft_args* args);
+ra_status ra_verify_draft(const ra_verify_draft_args* args, ra_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

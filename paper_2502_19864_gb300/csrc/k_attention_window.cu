@@ -1,0 +1,393 @@
+// k_attention_window.cu -- causal attention with a sliding window and first tokens that stay visible, over whole
+// sequences, in fp32 arithmetic: the forward and the backward of fp32 inputs (tf32 products would be 1e-3 off).
+//
+// Query i sees key j when j <= i and (i - j < W or j < sinks), both below the sequence's length:
+//   forward   o_i = sum_j p_ij v_j, p_ij = exp(scale q_i k_j - lse_i), by blocks of 64 keys with a running maximum
+//             and sum;
+//   backward  dV_j = sum_i p_ij dO_i;  dS_ij = p_ij (dO_i v_j - D_i), D_i = dO_i o_i;  dQ_i = scale sum_j dS_ij k_j;
+//             dK_j = scale sum_i dS_ij q_i, the sums over i over all query heads that share the key.
+// A query CTA walks the key blocks that any of its 64 queries sees: those of the window and those that hold sinks.
+// A key CTA walks, head by head of its group, the query blocks that see any of its 64 keys: dK and dV are sums of
+// one CTA in a fixed order.  Rows past the sequence's end are loaded as zeros, whatever memory holds there.
+// Bound by FFMA: a thread keeps 4 x 4 scores and 4 x DH / 16 outputs in registers.
+#include "common.cuh"
+#include "operators.h"
+
+namespace ra {
+namespace {
+
+constexpr int BT = 64, NT = 256, PP = BT + 4;
+constexpr float kLog2e = 1.4426950408889634f;
+
+template <int DH>
+struct Plan {
+  static constexpr int DP = DH + 4;  // padded rows: eight lanes' 16 bytes of eight rows fall in distinct banks
+  static constexpr int TILE = BT * DP;
+  static constexpr int FWD_BYTES = (3 * TILE + BT * PP) * 4, BWD_BYTES = (4 * TILE + BT * PP + 2 * BT) * 4;
+};
+
+// rows [r0, r0 + 64) of one head, zeros from row `len` on and past head_dim
+template <int DH>
+__device__ __forceinline__ void load_rows(float* dst, const float* src, int64_t stride, int r0, int len, int head_dim) {
+  for (int i = threadIdx.x; i < BT * DH / 4; i += NT) {
+    const int r = i / (DH / 4), c = (i - r * (DH / 4)) * 4;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (r0 + r < len && c < head_dim) x = *reinterpret_cast<const float4*>(src + (int64_t)(r0 + r) * stride + c);
+    *reinterpret_cast<float4*>(dst + r * Plan<DH>::DP + c) = x;
+  }
+}
+// acc[i][j] = A[4 ty + i] . B[tx + 16 j]
+template <int DH>
+__device__ __forceinline__ void dot_rows(float (&acc)[4][4], const float* A, const float* B, int ty, int tx) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
+#pragma unroll 4
+  for (int d = 0; d < DH; d += 4) {
+    float4 a[4], b[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const float4*>(A + (4 * ty + i) * Plan<DH>::DP + d);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) b[j] = *reinterpret_cast<const float4*>(B + (tx + 16 * j) * Plan<DH>::DP + d);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        acc[i][j] = fmaf(a[i].x, b[j].x, acc[i][j]);
+        acc[i][j] = fmaf(a[i].y, b[j].y, acc[i][j]);
+        acc[i][j] = fmaf(a[i].z, b[j].z, acc[i][j]);
+        acc[i][j] = fmaf(a[i].w, b[j].w, acc[i][j]);
+      }
+  }
+}
+// out[i][.] += sum_k X[4 ty + i][k] B[k][.], the thread's columns 2 tx + 32 c and the next
+template <int DH>
+__device__ __forceinline__ void times_rows(float (&out)[4][DH / 16], const float* X, const float* B, int ty, int tx) {
+#pragma unroll 2
+  for (int k = 0; k < BT; k += 4) {
+    float x[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(x[i]) = *reinterpret_cast<const float4*>(X + (4 * ty + i) * PP + k);
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int c = 0; c < DH / 32; ++c) {
+        const float2 b = *reinterpret_cast<const float2*>(B + (k + u) * Plan<DH>::DP + 2 * tx + 32 * c);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          out[i][2 * c] = fmaf(x[i][u], b.x, out[i][2 * c]);
+          out[i][2 * c + 1] = fmaf(x[i][u], b.y, out[i][2 * c + 1]);
+        }
+      }
+  }
+}
+template <int DH>
+__device__ __forceinline__ void store_rows(float* dst, int64_t stride, const float (&o)[4][DH / 16], const float (&f)[4],
+                                           int r0, int rows, int head_dim, int ty, int tx) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = r0 + 4 * ty + i;
+    if (r >= rows) continue;
+#pragma unroll
+    for (int c = 0; c < DH / 32; ++c) {
+      const int col = 2 * tx + 32 * c;
+      if (col < head_dim)
+        *reinterpret_cast<float2*>(dst + (int64_t)r * stride + col) = make_float2(o[i][2 * c] * f[i], o[i][2 * c + 1] * f[i]);
+    }
+  }
+}
+
+struct Geometry {  // of a CTA's (block, sequence, head)
+  int blk, b, head, len;
+};
+__device__ __forceinline__ Geometry geometry(const ra_attention_window_args& a, int heads, int n_blk) {
+  Geometry g;
+  const int64_t id = blockIdx.x;
+  g.blk = n_blk - 1 - (int)(id % n_blk);
+  const int bh = (int)(id / n_blk);
+  g.b = bh / heads;
+  g.head = bh - g.b * heads;
+  int len = a.lens_dev ? a.lens_dev[g.b] : a.seq;
+  if (len < 0 || len > a.seq) {
+    set_dev_error(a.err_dev, RA_DEVERR_BOUNDS);
+    len = len < 0 ? 0 : a.seq;
+  }
+  g.len = len;
+  return g;
+}
+// whether query i sees key j (W: at least 1; both within the sequence)
+__device__ __forceinline__ bool sees(int i, int j, int W, int sinks, int len) {
+  return j <= i && (i - j < W || j < sinks) && i < len;
+}
+
+template <int DH>
+__global__ void __launch_bounds__(NT) window_fwd_simt_kernel(const __grid_constant__ ra_attention_window_args a, int W, int n_blk) {
+  extern __shared__ __align__(16) float sm[];
+  using P = Plan<DH>;
+  float *Q = sm, *K = Q + P::TILE, *V = K + P::TILE, *X = V + P::TILE;
+  pdl_wait();
+  pdl_trigger();
+  const Geometry g = geometry(a, a.n_heads, n_blk);
+  const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15, q0 = g.blk * BT, dh = a.head_dim;
+  const int kvh = g.head / (a.n_heads / a.n_kv_heads);
+  const int64_t tok0 = (int64_t)g.b * a.seq;
+  const float* q = (const float*)a.q_dev + tok0 * a.q_stride + g.head * dh;
+  const float* k = (const float*)a.k_dev + tok0 * a.k_stride + kvh * dh;
+  const float* v = (const float*)a.v_dev + tok0 * a.v_stride + kvh * dh;
+  float o[4][DH / 16], m[4], l[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    m[i] = -INFINITY;
+    l[i] = 0.f;
+#pragma unroll
+    for (int c = 0; c < DH / 16; ++c) o[i][c] = 0.f;
+  }
+  const float sl2 = a.scale * kLog2e;
+  if (q0 < g.len) {
+    load_rows<DH>(Q, q, a.q_stride, q0, g.len, dh);
+    const int last = q0 + BT - 1 < g.len ? q0 + BT - 1 : g.len - 1, hi = last / BT;
+    const int first = q0 - W + 1, lo = first > 0 ? first / BT : 0;
+    for (int kb = 0; kb <= hi; ++kb) {
+      if (kb < lo && kb * BT >= a.sinks) kb = lo;
+      const int k0 = kb * BT;
+      __syncthreads();
+      load_rows<DH>(K, k, a.k_stride, k0, g.len, dh);
+      load_rows<DH>(V, v, a.v_stride, k0, g.len, dh);
+      __syncthreads();
+      float s[4][4];
+      dot_rows<DH>(s, Q, K, ty, tx);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int qi = q0 + 4 * ty + i;
+        float bm = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          s[i][j] = sees(qi, k0 + tx + 16 * j, W, a.sinks, g.len) ? s[i][j] * sl2 : -INFINITY;
+          bm = fmaxf(bm, s[i][j]);
+        }
+#pragma unroll
+        for (int x = 8; x > 0; x >>= 1) bm = fmaxf(bm, __shfl_xor_sync(0xffffffffu, bm, x));
+        const float mn = fmaxf(m[i], bm), ms = mn == -INFINITY ? 0.f : mn, f = exp2f(m[i] - ms);
+        m[i] = mn;
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float p = exp2f(s[i][j] - ms);
+          sum += p;
+          X[(4 * ty + i) * PP + tx + 16 * j] = p;
+        }
+        l[i] = l[i] * f + sum;  // (a lane's own share; the 16 lanes of a row are summed at the end)
+#pragma unroll
+        for (int c = 0; c < DH / 16; ++c) o[i][c] *= f;
+      }
+      __syncthreads();
+      times_rows<DH>(o, X, V, ty, tx);
+    }
+  }
+  float f[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+#pragma unroll
+    for (int x = 8; x > 0; x >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
+    f[i] = l[i] > 0.f ? 1.f / l[i] : l[i] == 0.f ? 0.f : l[i];
+    const int qi = q0 + 4 * ty + i;
+    if (a.lse_dev && tx == 0 && qi < a.seq)
+      a.lse_dev[((int64_t)g.b * a.n_heads + g.head) * a.seq + qi] = m[i] == -INFINITY ? -INFINITY : (m[i] + log2f(l[i])) * 0.69314718055994531f;
+  }
+  store_rows<DH>((float*)a.out_dev + tok0 * a.out_stride + g.head * dh, a.out_stride, o, f, q0, a.seq, dh, ty, tx);
+}
+
+// ---- backward ------------------------------------------------------------------------------
+// D_i = dO_i . o_i, a warp a row (0 past the sequence's end)
+template <typename T>
+__global__ void __launch_bounds__(256) window_bwd_d_kernel(const __grid_constant__ ra_attention_window_args a, float* D) {
+  pdl_wait();
+  pdl_trigger();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t rows = (int64_t)a.batch * a.seq * a.n_heads;
+  for (int64_t r = (int64_t)blockIdx.x * 8 + warp; r < rows; r += (int64_t)gridDim.x * 8) {
+    const int64_t tok = r / a.n_heads;
+    const int head = (int)(r - tok * a.n_heads), b = (int)(tok / a.seq), s = (int)(tok - (int64_t)b * a.seq);
+    float d = 0.f;
+    if (!a.lens_dev || s < a.lens_dev[b]) {
+      const T* o = (const T*)a.out_dev + tok * a.out_stride + head * a.head_dim;
+      const T* g = (const T*)a.dout_dev + tok * a.dout_stride + head * a.head_dim;
+      for (int c = lane; c < a.head_dim; c += 32) d = fmaf(to_f(o[c]), to_f(g[c]), d);
+    }
+    d = warp_sum(d);
+    if (lane == 0) D[((int64_t)b * a.n_heads + head) * a.seq + s] = d;
+  }
+}
+
+// P and dS of one pair of blocks by the thread's 4 x 4: rows are queries (KEYS: keys)
+template <int DH, bool KEYS>
+__global__ void __launch_bounds__(NT) window_bwd_simt_kernel(const __grid_constant__ ra_attention_window_args a, const float* Dv,
+                                                             int W, int n_blk) {
+  extern __shared__ __align__(16) float sm[];
+  using P = Plan<DH>;
+  float *T0 = sm, *T1 = T0 + P::TILE, *T2 = T1 + P::TILE, *T3 = T2 + P::TILE, *X = T3 + P::TILE, *L = X + BT * PP, *D = L + BT;
+  pdl_wait();
+  pdl_trigger();
+  const int G = a.n_heads / a.n_kv_heads;
+  const Geometry g = geometry(a, KEYS ? a.n_kv_heads : a.n_heads, n_blk);
+  const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15, r0 = g.blk * BT, dh = a.head_dim;
+  const int kvh = KEYS ? g.head : g.head / G;
+  const int64_t tok0 = (int64_t)g.b * a.seq;
+  const float* k = (const float*)a.k_dev + tok0 * a.k_stride + kvh * dh;
+  const float* v = (const float*)a.v_dev + tok0 * a.v_stride + kvh * dh;
+  float u[4][DH / 16], w[4][DH / 16];  // KEYS: dK, dV; else dQ
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int c = 0; c < DH / 16; ++c) u[i][c] = w[i][c] = 0.f;
+  const float sl2 = a.scale * kLog2e;
+  auto stats = [&](int head, int q0) {
+    if (tid < BT) {
+      const int64_t at = ((int64_t)g.b * a.n_heads + head) * a.seq + q0 + tid;
+      const bool live = q0 + tid < g.len;
+      L[tid] = live ? a.lse_dev[at] * kLog2e : 0.f;
+      D[tid] = live ? Dv[at] : 0.f;
+    }
+  };
+  // X = P (or P^T), then dS in s
+  auto probabilities = [&](float (&s)[4][4], int c0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int row = 4 * ty + i, col = tx + 16 * j;
+        const int qi = KEYS ? c0 + col : r0 + row, ki = KEYS ? r0 + row : c0 + col;
+        s[i][j] = sees(qi, ki, W, a.sinks, g.len) ? exp2f(s[i][j] * sl2 - L[KEYS ? col : row]) : 0.f;
+      }
+  };
+  auto put = [&](const float (&s)[4][4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) X[(4 * ty + i) * PP + tx + 16 * j] = s[i][j];
+  };
+  if (r0 < g.len) {
+    if (KEYS) {
+      load_rows<DH>(T0, k, a.k_stride, r0, g.len, dh);
+      load_rows<DH>(T1, v, a.v_stride, r0, g.len, dh);
+      const int last = r0 + BT - 1 < g.len ? r0 + BT - 1 : g.len - 1;  // the last key
+      const int64_t far = r0 < a.sinks ? g.len - 1 : (int64_t)last + W - 1;
+      const int hi = (int)(far < g.len ? far : g.len - 1) / BT;
+      for (int h = kvh * G; h < (kvh + 1) * G; ++h) {
+        const float* q = (const float*)a.q_dev + tok0 * a.q_stride + h * dh;
+        const float* go = (const float*)a.dout_dev + tok0 * a.dout_stride + h * dh;
+        for (int qb = g.blk; qb <= hi; ++qb) {
+          const int q0 = qb * BT;
+          __syncthreads();
+          load_rows<DH>(T2, q, a.q_stride, q0, g.len, dh);
+          load_rows<DH>(T3, go, a.dout_stride, q0, g.len, dh);
+          stats(h, q0);
+          __syncthreads();
+          float s[4][4], dp[4][4];
+          dot_rows<DH>(s, T0, T2, ty, tx);
+          probabilities(s, q0);
+          put(s);
+          dot_rows<DH>(dp, T1, T3, ty, tx);
+          __syncthreads();
+          times_rows<DH>(w, X, T3, ty, tx);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[i][j] *= dp[i][j] - D[tx + 16 * j];
+          __syncthreads();
+          put(s);
+          __syncthreads();
+          times_rows<DH>(u, X, T2, ty, tx);
+        }
+      }
+    } else {
+      load_rows<DH>(T0, (const float*)a.q_dev + tok0 * a.q_stride + g.head * dh, a.q_stride, r0, g.len, dh);
+      load_rows<DH>(T1, (const float*)a.dout_dev + tok0 * a.dout_stride + g.head * dh, a.dout_stride, r0, g.len, dh);
+      stats(g.head, r0);
+      const int last = r0 + BT - 1 < g.len ? r0 + BT - 1 : g.len - 1, hi = last / BT;
+      const int first = r0 - W + 1, lo = first > 0 ? first / BT : 0;
+      for (int kb = 0; kb <= hi; ++kb) {
+        if (kb < lo && kb * BT >= a.sinks) kb = lo;
+        const int k0 = kb * BT;
+        __syncthreads();
+        load_rows<DH>(T2, k, a.k_stride, k0, g.len, dh);
+        load_rows<DH>(T3, v, a.v_stride, k0, g.len, dh);
+        __syncthreads();
+        float s[4][4], dp[4][4];
+        dot_rows<DH>(s, T0, T2, ty, tx);
+        probabilities(s, k0);
+        dot_rows<DH>(dp, T1, T3, ty, tx);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s[i][j] *= dp[i][j] - D[4 * ty + i];
+        put(s);
+        __syncthreads();
+        times_rows<DH>(u, X, T2, ty, tx);
+      }
+    }
+  }
+  const float fs[4] = {a.scale, a.scale, a.scale, a.scale}, f1[4] = {1.f, 1.f, 1.f, 1.f};
+  if (KEYS) {
+    store_rows<DH>((float*)a.dk_dev + tok0 * a.dk_stride + kvh * dh, a.dk_stride, u, fs, r0, a.seq, dh, ty, tx);
+    store_rows<DH>((float*)a.dv_dev + tok0 * a.dv_stride + kvh * dh, a.dv_stride, w, f1, r0, a.seq, dh, ty, tx);
+  } else {
+    store_rows<DH>((float*)a.dq_dev + tok0 * a.dq_stride + g.head * dh, a.dq_stride, u, fs, r0, a.seq, dh, ty, tx);
+  }
+}
+
+int window_of(const ra_attention_window_args& a) { return a.window == 0 || a.window > a.seq ? a.seq : a.window; }
+
+template <int DH>
+cudaError_t fwd_simt(const ra_attention_window_args& a, cudaStream_t st) {
+  const int n_blk = (a.seq + BT - 1) / BT;
+  const int64_t grid = (int64_t)n_blk * a.batch * a.n_heads;
+  if (grid > INT32_MAX) return cudaErrorNotSupported;
+  cudaError_t e = allow_smem(window_fwd_simt_kernel<DH>, Plan<DH>::FWD_BYTES);
+  if (e != cudaSuccess) return e;
+  e = launch_pdl(window_fwd_simt_kernel<DH>, dim3((unsigned)grid), dim3(NT), Plan<DH>::FWD_BYTES, st, a, window_of(a), n_blk);
+  note_launch(1);
+  return e;
+}
+template <int DH>
+cudaError_t bwd_simt(const ra_attention_window_args& a, cudaStream_t st) {
+  const int n_blk = (a.seq + BT - 1) / BT;
+  const int64_t gq = (int64_t)n_blk * a.batch * a.n_heads, gk = (int64_t)n_blk * a.batch * a.n_kv_heads;
+  if (gq > INT32_MAX) return cudaErrorNotSupported;
+  float* D = (float*)a.workspace_dev;
+  cudaError_t e = allow_smem(window_bwd_simt_kernel<DH, true>, Plan<DH>::BWD_BYTES);
+  if (e == cudaSuccess) e = allow_smem(window_bwd_simt_kernel<DH, false>, Plan<DH>::BWD_BYTES);
+  if (e == cudaSuccess) e = attention_window_d(a, D, st);
+  if (e != cudaSuccess) return e;
+  const float* Dc = D;
+  e = launch_pdl(window_bwd_simt_kernel<DH, true>, dim3((unsigned)gk), dim3(NT), Plan<DH>::BWD_BYTES, st, a, Dc, window_of(a), n_blk);
+  if (e == cudaSuccess)
+    e = launch_pdl(window_bwd_simt_kernel<DH, false>, dim3((unsigned)gq), dim3(NT), Plan<DH>::BWD_BYTES, st, a, Dc, window_of(a), n_blk);
+  note_launch(2);
+  return e;
+}
+
+}  // namespace
+
+size_t attention_window_workspace(const ra_attention_window_args& a) { return (size_t)a.batch * a.seq * a.n_heads * 4; }
+
+cudaError_t attention_window_d(const ra_attention_window_args& a, float* D, cudaStream_t st) {
+  const int64_t blocks = ((int64_t)a.batch * a.seq * a.n_heads + 7) / 8, most = 64LL * device_sm_count();
+  const dim3 grid((unsigned)(blocks < most ? blocks : most));
+  cudaError_t e = a.dtype == RA_BF16 ? launch_pdl(window_bwd_d_kernel<bf16>, grid, dim3(256), 0, st, a, D)
+                                     : launch_pdl(window_bwd_d_kernel<float>, grid, dim3(256), 0, st, a, D);
+  note_launch(1);
+  return e;
+}
+
+cudaError_t attention_window_fwd_simt(const ra_attention_window_args& a, cudaStream_t st) {
+  if (a.dtype != RA_F32) return cudaErrorNotSupported;
+  return a.head_dim <= 32 ? fwd_simt<32>(a, st) : a.head_dim <= 64 ? fwd_simt<64>(a, st) : a.head_dim <= 96 ? fwd_simt<96>(a, st) : fwd_simt<128>(a, st);
+}
+cudaError_t attention_window_bwd_simt(const ra_attention_window_args& a, cudaStream_t st) {
+  if (a.dtype != RA_F32) return cudaErrorNotSupported;
+  return a.head_dim <= 32 ? bwd_simt<32>(a, st) : a.head_dim <= 64 ? bwd_simt<64>(a, st) : a.head_dim <= 96 ? bwd_simt<96>(a, st) : bwd_simt<128>(a, st);
+}
+
+}  // namespace ra

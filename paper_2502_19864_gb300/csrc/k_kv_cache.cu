@@ -1,0 +1,300 @@
+// k_kv_cache.cu -- the paged key-value cache: putting new tokens in (with RoPE) and evicting those of little
+// accumulated weight.
+#include <type_traits>
+
+#include "common.cuh"
+#include "operators.h"
+#include "paged.cuh"
+
+namespace ra {
+namespace {
+
+// ---------------------------------------------------------------------------------------
+// Append.  A thread turns VE pairs (i, i + head_dim / 2) of one row of one token: a row of q goes to q_out, one
+// of k or v to its page.  Bound by memory: every value is read once and written once, the table's row by all
+// heads of its token (from L1).
+// ---------------------------------------------------------------------------------------
+template <typename T, int VE>
+__device__ __forceinline__ void load_pack(T* dst, const T* src) {
+  typedef typename std::conditional<sizeof(T) * VE == 16, uint4, uint2>::type V;
+  *reinterpret_cast<V*>(dst) = *reinterpret_cast<const V*>(src);
+}
+template <typename T, int VE>
+__device__ __forceinline__ void store_pack(T* dst, const T* src) {
+  typedef typename std::conditional<sizeof(T) * VE == 16, uint4, uint2>::type V;
+  *reinterpret_cast<V*>(dst) = *reinterpret_cast<const V*>(src);
+}
+
+template <typename T, int VE>
+__global__ void __launch_bounds__(256) kv_append_kernel(const __grid_constant__ ra_kv_append_args a, int tokens_per_block) {
+  pdl_wait();
+  pdl_trigger();
+  const ra_kv_cache& c = a.cache;
+  const int half = c.head_dim / 2, chunks = half / VE, hq = a.q_dev ? a.n_heads : 0;
+  const int items = (hq + 2 * c.n_kv_heads) * chunks;
+  const int sub = threadIdx.x / items, item0 = sub < tokens_per_block ? threadIdx.x - sub * items : items;
+  if (tokens_per_block > 1 && sub >= tokens_per_block) return;
+  const int64_t tokens = (int64_t)a.batch * a.n_new;
+  const int cap = (int)((int64_t)c.max_pages * c.page_size);
+  const T *qp = (const T*)a.q_dev, *kp = (const T*)a.k_dev, *vp = (const T*)a.v_dev;
+  for (int64_t tok = (int64_t)blockIdx.x * tokens_per_block + (tokens_per_block > 1 ? sub : 0); tok < tokens;
+       tok += (int64_t)gridDim.x * tokens_per_block) {
+    const int b = (int)(tok / a.n_new), t = (int)(tok - (int64_t)b * a.n_new);
+    for (int item = tokens_per_block > 1 ? item0 : (int)threadIdx.x; item < items; item += blockDim.x) {
+      const int row = item / chunks, i = (item - row * chunks) * VE;
+      const bool is_q = row < hq, is_k = !is_q && row < hq + c.n_kv_heads;
+      const int head = is_q ? row : is_k ? row - hq : row - hq - c.n_kv_heads;
+      const T* src = (is_q ? qp + tok * a.q_stride : is_k ? kp + tok * a.k_stride : vp + tok * a.v_stride) +
+                     (int64_t)head * c.head_dim + i;
+      __align__(16) T lo[VE], hi[VE];
+      load_pack<T, VE>(lo, src);
+      load_pack<T, VE>(hi, src + half);
+      const int len = clamp_len(a.lens_dev[b], cap, c.err_dev);
+      const int slot = len - a.n_new + t;
+      if (a.rope_dev && (is_q || is_k)) {
+        int p = (a.pos_dev ? a.pos_dev[b] : len) - a.n_new + t;
+        if (p < 0 || p >= a.rope_len) {
+          if (slot >= 0) set_dev_error(c.err_dev, RA_DEVERR_BOUNDS);
+          p = p < 0 ? 0 : a.rope_len - 1;
+        }
+        const float* w = a.rope_dev + (int64_t)p * c.head_dim + i;
+        __align__(16) float cs[VE], sn[VE];
+#pragma unroll
+        for (int e = 0; e < VE; e += VE < 4 ? VE : 4) {
+          load_pack<float, VE < 4 ? VE : 4>(cs + e, w + e);
+          load_pack<float, VE < 4 ? VE : 4>(sn + e, w + half + e);
+        }
+#pragma unroll
+        for (int e = 0; e < VE; ++e) {
+          const float x = to_f(lo[e]), y = to_f(hi[e]);
+          lo[e] = from_f<T>(x * cs[e] - y * sn[e]);
+          hi[e] = from_f<T>(y * cs[e] + x * sn[e]);
+        }
+      }
+      T* dst;
+      if (is_q) {
+        dst = (T*)a.q_out_dev + tok * a.q_out_stride + (int64_t)head * c.head_dim + i;
+        if (slot < 0) {
+#pragma unroll
+          for (int e = 0; e < VE; ++e) lo[e] = hi[e] = from_f<T>(0.f);
+        }
+      } else {
+        if (slot < 0) continue;
+        const int64_t at = slot_row(c, b, slot, head);
+        if (at < 0) continue;
+        dst = (T*)(is_k ? c.k_dev : c.v_dev) + at * c.head_dim + i;
+      }
+      store_pack<T, VE>(dst, lo);
+      store_pack<T, VE>(dst + half, hi);
+    }
+  }
+}
+
+template <typename T, int VE>
+cudaError_t launch_append(const ra_kv_append_args& a, cudaStream_t st) {
+  const int items = ((a.q_dev ? a.n_heads : 0) + 2 * a.cache.n_kv_heads) * (a.cache.head_dim / 2 / VE);
+  const int per = items < 256 ? 256 / items : 1;
+  const int64_t blocks = ((int64_t)a.batch * a.n_new + per - 1) / per;
+  const int64_t most = 8LL * 8 * device_sm_count();  // eight blocks of 256 threads an SM, eight rounds
+  cudaError_t e = launch_pdl(kv_append_kernel<T, VE>, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, st, a, per);
+  note_launch(1);
+  return e;
+}
+
+// ---------------------------------------------------------------------------------------
+// Eviction, first kernel: which slots stay.  A CTA takes one key-value head of one sequence.  The weights
+// become 32-bit keys that rise with them (in shared memory where they fit); the budget-th largest key of the
+// middle is found by its digits, 11, 11 and 10 bits from the top, each by a histogram of the keys that share
+// the digits found so far; then every warp counts its part of the slots, and writes what stays in order behind
+// what the warps before it count.  Counts are integers: no order of atomics changes a result.
+// ---------------------------------------------------------------------------------------
+constexpr int SEL_THREADS = 1024, SEL_WARPS = SEL_THREADS / 32, SEL_BINS = 2048;
+constexpr int SEL_KEYS = 48 * 1024;  // keys held in shared memory; longer sequences read their weights again
+
+__device__ __forceinline__ uint32_t weight_key(float w) {
+  if (w != w) return 0xffffffffu;
+  const uint32_t u = __float_as_uint(w == 0.f ? 0.f : w);  // -0 and 0 are equal
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+__global__ void __launch_bounds__(SEL_THREADS) evict_select_kernel(const __grid_constant__ ra_kv_evict_args a, int max_len) {
+  extern __shared__ uint32_t keys[];
+  __shared__ uint32_t hist[SEL_BINS];
+  __shared__ uint32_t warp_sum[SEL_WARPS], warp_eq[SEL_WARPS];
+  __shared__ uint32_t found_digit, found_left;
+  pdl_wait();
+  pdl_trigger();
+  const int kv = a.src.n_kv_heads, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int64_t unit = blockIdx.x;
+  const int b = (int)(unit / kv), head = (int)(unit - (int64_t)b * kv);
+  const int n = clamp_len(a.lens_dev[b], max_len, a.src.err_dev);
+  const float* w = a.weights_dev + unit * a.weights_stride;
+  int32_t* kept = a.kept_dev + unit * a.budget;
+  float* wout = a.weights_out_dev ? a.weights_out_dev + unit * a.weights_out_stride : nullptr;
+  const int stay = n < a.budget ? n : a.budget;
+  if (head == 0 && tid == 0) a.lens_out_dev[b] = stay;
+  for (int i = stay + tid; i < a.budget; i += SEL_THREADS) {
+    kept[i] = -1;
+    if (wout) wout[i] = 0.f;
+  }
+  if (n <= a.budget) {
+    for (int i = tid; i < n; i += SEL_THREADS) {
+      kept[i] = i;
+      if (wout) wout[i] = w[i];
+    }
+    return;
+  }
+  const int m0 = a.first, m1 = n - a.recent;  // the middle
+  const bool in_smem = n <= SEL_KEYS;
+  if (in_smem)
+    for (int i = tid; i < n; i += SEL_THREADS) keys[i] = weight_key(w[i]);
+  auto key_at = [&](int i) { return in_smem ? keys[i] : weight_key(w[i]); };
+  uint32_t left = (uint32_t)(a.budget - a.first - a.recent);  // how many of the middle stay
+  uint32_t prefix = 0xffffffffu;  // (left == 0: nothing is larger)
+  if (left > 0) {
+    prefix = 0;
+    uint32_t mask = 0;
+#pragma unroll 1
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048;
+      for (int i = tid; i < SEL_BINS; i += SEL_THREADS) hist[i] = 0;
+      __syncthreads();
+      for (int i = m0 + tid; i < m1; i += SEL_THREADS) {
+        const uint32_t k = key_at(i);
+        if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1u);
+      }
+      __syncthreads();
+      // the digit at which the count from the top reaches `left`: thread t has bins 2 r and 2 r + 1, r from the top
+      const int r = SEL_THREADS - 1 - tid;
+      const uint32_t hi = hist[2 * r + 1], lo = hist[2 * r];
+      uint32_t incl = hi + lo;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t v = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += v;
+      }
+      if (lane == 31) warp_sum[warp] = incl;
+      __syncthreads();
+      uint32_t before = 0;
+      for (int i = 0; i < warp; ++i) before += warp_sum[i];
+      const uint32_t above = before + incl - hi - lo;  // keys with a larger digit than this thread's
+      if (above < left && left <= above + hi + lo) {
+        const bool in_hi = left <= above + hi;
+        found_digit = (uint32_t)(2 * r + (in_hi ? 1 : 0));
+        found_left = left - above - (in_hi ? 0 : hi);
+      }
+      __syncthreads();
+      prefix |= found_digit << shift;
+      mask |= (uint32_t)(bins - 1) << shift;
+      left = found_left;  // how many of the keys with this digit (at last: of the keys equal to it) stay
+    }
+  } else if (in_smem) {
+    __syncthreads();
+  }
+  const uint32_t edge = prefix, equal_stay = left;
+  const int seg = ((n + SEL_WARPS - 1) / SEL_WARPS + 31) / 32 * 32, s0 = warp * seg, s1 = s0 + seg < n ? s0 + seg : n;
+  uint32_t gt = 0, eq = 0;
+  for (int i = s0 + lane; i < s1; i += 32) {
+    const bool always = i < m0 || i >= m1;
+    const uint32_t k = key_at(i);
+    gt += always || k > edge;
+    eq += !always && k == edge;
+  }
+  gt = __reduce_add_sync(0xffffffffu, gt);
+  eq = __reduce_add_sync(0xffffffffu, eq);
+  if (lane == 0) {
+    warp_sum[warp] = gt;
+    warp_eq[warp] = eq;
+  }
+  __syncthreads();
+  uint32_t gt0 = 0, eq0 = 0;  // of the slots before the ones at hand
+  for (int i = 0; i < warp; ++i) {
+    gt0 += warp_sum[i];
+    eq0 += warp_eq[i];
+  }
+  for (int base = s0; base < s1; base += 32) {
+    const int i = base + lane;
+    const bool live = i < s1, always = live && (i < m0 || i >= m1);
+    const uint32_t k = live ? key_at(i) : 0;
+    const bool is_gt = always || (live && k > edge), is_eq = live && !always && k == edge;
+    const uint32_t bg = __ballot_sync(0xffffffffu, is_gt), be = __ballot_sync(0xffffffffu, is_eq);
+    const uint32_t below = (1u << lane) - 1u;
+    const uint32_t g = gt0 + __popc(bg & below), q = eq0 + __popc(be & below);
+    if (is_gt || (is_eq && q < equal_stay)) {
+      const uint32_t at = g + (q < equal_stay ? q : equal_stay);
+      kept[at] = i;
+      if (wout) wout[at] = w[i];
+    }
+    gt0 += __popc(bg);
+    eq0 += __popc(be);
+  }
+}
+
+// Second kernel: the rows that stay, K and V, 16 bytes a thread and load, MOVE rows of a thread in flight.
+constexpr int MOVE = 4;
+__global__ void __launch_bounds__(256) evict_move_kernel(const __grid_constant__ ra_kv_evict_args a, int cpr, int rows_per_block,
+                                                         int blocks_per_unit, int64_t n_blocks) {
+  pdl_wait();
+  pdl_trigger();
+  const int kv = a.src.n_kv_heads, per = 256 / cpr, r0 = threadIdx.x / cpr, col = threadIdx.x - r0 * cpr;
+  if (r0 >= per) return;
+  for (int64_t blk = blockIdx.x; blk < n_blocks; blk += gridDim.x) {
+    const int64_t unit = blk / blocks_per_unit;
+    const int b = (int)(unit / kv), head = (int)(unit - (int64_t)b * kv);
+    const int row0 = (int)(blk - unit * blocks_per_unit) * rows_per_block + r0;
+    uint4 kx[MOVE], vx[MOVE];
+    int from[MOVE];
+#pragma unroll
+    for (int i = 0; i < MOVE; ++i) {
+      const int row = row0 + i * per;
+      from[i] = row < a.budget ? a.kept_dev[unit * a.budget + row] : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < MOVE; ++i) {
+      kx[i] = vx[i] = make_uint4(0, 0, 0, 0);
+      if (from[i] >= 0) {
+        const int64_t at = slot_row(a.src, b, from[i], head);
+        if (at >= 0) {
+          kx[i] = reinterpret_cast<const uint4*>(a.src.k_dev)[at * cpr + col];
+          vx[i] = reinterpret_cast<const uint4*>(a.src.v_dev)[at * cpr + col];
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < MOVE; ++i) {
+      if (from[i] < 0) continue;
+      const int64_t at = slot_row(a.dst, b, row0 + i * per, head);
+      if (at < 0) continue;
+      reinterpret_cast<uint4*>(a.dst.k_dev)[at * cpr + col] = kx[i];
+      reinterpret_cast<uint4*>(a.dst.v_dev)[at * cpr + col] = vx[i];
+    }
+  }
+}
+
+}  // namespace
+
+cudaError_t kv_append(const ra_kv_append_args& a, cudaStream_t st) {
+  const int half = a.cache.head_dim / 2;
+  if (a.cache.dtype == RA_BF16) return half % 8 ? launch_append<bf16, 4>(a, st) : launch_append<bf16, 8>(a, st);
+  return half % 4 ? launch_append<float, 2>(a, st) : launch_append<float, 4>(a, st);
+}
+
+cudaError_t kv_evict(const ra_kv_evict_args& a, cudaStream_t st) {
+  const int max_len = call_max_len(a.src, a.max_len);
+  const int64_t units = (int64_t)a.batch * a.src.n_kv_heads;
+  cudaError_t e = allow_smem(evict_select_kernel, SEL_KEYS * 4);
+  if (e != cudaSuccess) return e;
+  // (the keys' space goes by the longest sequence that can come, so that short ones leave room for more CTAs)
+  const size_t smem = 4 * (size_t)(max_len < SEL_KEYS ? max_len : SEL_KEYS);
+  e = launch_pdl(evict_select_kernel, dim3((unsigned)units), dim3(SEL_THREADS), smem, st, a, max_len);
+  if (e != cudaSuccess) return e;
+  const int cpr = a.src.head_dim * (a.src.dtype == RA_BF16 ? 2 : 4) / 16, rows = 256 / cpr * MOVE;
+  const int per_unit = (a.budget + rows - 1) / rows;
+  const int64_t n_blocks = units * per_unit, most = 8LL * 8 * device_sm_count();
+  e = launch_pdl(evict_move_kernel, dim3((unsigned)(n_blocks < most ? n_blocks : most)), dim3(256), 0, st, a, cpr, rows, per_unit,
+                 n_blocks);
+  note_launch(2);
+  return e;
+}
+
+}  // namespace ra

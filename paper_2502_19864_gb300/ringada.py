@@ -82,6 +82,67 @@ class ra_profile_record(C.Structure):
     _fields_ = [("cat", C.c_int32), ("ms", C.c_float), ("flops", C.c_double), ("bytes", C.c_double)]
 
 
+class ra_kv_cache(C.Structure):
+    """A layer's paged key-value cache (device addresses and shape)."""
+    _fields_ = [("k_dev", C.c_void_p), ("v_dev", C.c_void_p), ("block_table_dev", C.c_void_p),
+                ("err_dev", C.c_void_p), ("n_pages", C.c_int32), ("max_pages", C.c_int32),
+                ("page_size", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int32)]
+
+
+class ra_kv_append_args(C.Structure):
+    _fields_ = [("cache", ra_kv_cache), ("lens_dev", C.c_void_p), ("pos_dev", C.c_void_p),
+                ("q_dev", C.c_void_p), ("k_dev", C.c_void_p), ("v_dev", C.c_void_p),
+                ("q_out_dev", C.c_void_p), ("q_stride", C.c_int64), ("k_stride", C.c_int64),
+                ("v_stride", C.c_int64), ("q_out_stride", C.c_int64), ("rope_dev", C.c_void_p),
+                ("rope_len", C.c_int32), ("batch", C.c_int32), ("n_new", C.c_int32),
+                ("n_heads", C.c_int32)]
+
+
+class ra_attention_decode_args(C.Structure):
+    _fields_ = [("cache", ra_kv_cache), ("lens_dev", C.c_void_p), ("q_dev", C.c_void_p),
+                ("q_stride", C.c_int64), ("out_dev", C.c_void_p), ("out_stride", C.c_int64),
+                ("lse_dev", C.c_void_p), ("weights_in_dev", C.c_void_p),
+                ("weights_out_dev", C.c_void_p), ("weights_stride", C.c_int64),
+                ("workspace_dev", C.c_void_p), ("workspace_bytes", C.c_size_t),
+                ("batch", C.c_int32), ("n_new", C.c_int32), ("n_heads", C.c_int32),
+                ("max_len", C.c_int32), ("window", C.c_int32), ("sinks", C.c_int32),
+                ("scale", C.c_float)]
+
+
+class ra_kv_evict_args(C.Structure):
+    _fields_ = [("src", ra_kv_cache), ("dst", ra_kv_cache), ("lens_dev", C.c_void_p),
+                ("weights_dev", C.c_void_p), ("weights_stride", C.c_int64),
+                ("lens_out_dev", C.c_void_p), ("kept_dev", C.c_void_p),
+                ("weights_out_dev", C.c_void_p), ("weights_out_stride", C.c_int64),
+                ("batch", C.c_int32), ("max_len", C.c_int32), ("budget", C.c_int32),
+                ("first", C.c_int32), ("recent", C.c_int32)]
+
+
+class ra_attention_window_args(C.Structure):
+    _fields_ = [("q_dev", C.c_void_p), ("k_dev", C.c_void_p), ("v_dev", C.c_void_p),
+                ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64),
+                ("out_dev", C.c_void_p), ("out_stride", C.c_int64), ("lse_dev", C.c_void_p),
+                ("lens_dev", C.c_void_p), ("dout_dev", C.c_void_p), ("dout_stride", C.c_int64),
+                ("dq_dev", C.c_void_p), ("dk_dev", C.c_void_p), ("dv_dev", C.c_void_p),
+                ("dq_stride", C.c_int64), ("dk_stride", C.c_int64), ("dv_stride", C.c_int64),
+                ("workspace_dev", C.c_void_p), ("workspace_bytes", C.c_size_t),
+                ("err_dev", C.c_void_p), ("batch", C.c_int32), ("seq", C.c_int32),
+                ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("window", C.c_int32), ("sinks", C.c_int32), ("dtype", C.c_int32),
+                ("scale", C.c_float)]
+
+
+class ra_verify_draft_args(C.Structure):
+    _fields_ = [("target_dev", C.c_void_p), ("target_stride", C.c_int64), ("draft_dev", C.c_void_p),
+                ("draft_stride", C.c_int64), ("tokens_dev", C.c_void_p),
+                ("n_drafted_dev", C.c_void_p), ("uniform_dev", C.c_void_p),
+                ("noise_dev", C.c_void_p), ("accepted_dev", C.c_void_p),
+                ("out_tokens_dev", C.c_void_p), ("workspace_dev", C.c_void_p),
+                ("workspace_bytes", C.c_size_t), ("batch", C.c_int32), ("n_draft", C.c_int32),
+                ("vocab", C.c_int32), ("dtype", C.c_int32)]
+
+
 class RingAdaError(RuntimeError):
     def __init__(self, status, msg):
         super().__init__("%s: %s" % (STATUS_NAMES.get(status, status), msg))
@@ -141,6 +202,15 @@ _SIGS = {
     "ra_profile_gemm_replay": (C.c_int, [C.c_void_p, C.POINTER(C.c_int32), C.POINTER(C.c_double),
                                          C.c_void_p]),
     "ra_profile_records": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.POINTER(C.c_int32)]),
+    "ra_kv_append": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "ra_attention_decode": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "ra_attention_decode_workspace_bytes": (C.c_size_t, [C.c_void_p]),
+    "ra_kv_evict": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "ra_attention_window_forward": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "ra_attention_window_backward": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "ra_attention_window_workspace_bytes": (C.c_size_t, [C.c_void_p]),
+    "ra_verify_draft": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "ra_verify_draft_workspace_bytes": (C.c_size_t, [C.c_void_p]),
 }
 
 
@@ -354,6 +424,47 @@ def ra_profile_gemm_replay(ctx, stream=None):
 
 def ra_kernel_launches() -> int:
     return lib().ra_kernel_launches()
+
+
+# ---- operators that answer with a tuned decoder: one argument block (a struct above) a call -----
+
+RA_DEV_TIMEOUT, RA_DEV_BOUNDS = 1, 2
+
+
+def ra_kv_append(args: ra_kv_append_args, stream=None):
+    _check(lib().ra_kv_append(C.byref(args), _stream_ptr(stream)))
+
+
+def ra_attention_decode_workspace_bytes(args: ra_attention_decode_args) -> int:
+    return lib().ra_attention_decode_workspace_bytes(C.byref(args))
+
+
+def ra_attention_decode(args: ra_attention_decode_args, stream=None):
+    _check(lib().ra_attention_decode(C.byref(args), _stream_ptr(stream)))
+
+
+def ra_kv_evict(args: ra_kv_evict_args, stream=None):
+    _check(lib().ra_kv_evict(C.byref(args), _stream_ptr(stream)))
+
+
+def ra_attention_window_workspace_bytes(args: ra_attention_window_args) -> int:
+    return lib().ra_attention_window_workspace_bytes(C.byref(args))
+
+
+def ra_attention_window_forward(args: ra_attention_window_args, stream=None):
+    _check(lib().ra_attention_window_forward(C.byref(args), _stream_ptr(stream)))
+
+
+def ra_attention_window_backward(args: ra_attention_window_args, stream=None):
+    _check(lib().ra_attention_window_backward(C.byref(args), _stream_ptr(stream)))
+
+
+def ra_verify_draft_workspace_bytes(args: ra_verify_draft_args) -> int:
+    return lib().ra_verify_draft_workspace_bytes(C.byref(args))
+
+
+def ra_verify_draft(args: ra_verify_draft_args, stream=None):
+    _check(lib().ra_verify_draft(C.byref(args), _stream_ptr(stream)))
 
 
 # ---- convenience: torch-owned buffers ------------------------------------------------------
