@@ -412,7 +412,8 @@ size_t ra_adapter_backward_noalloc_capacity(void);
  *     of n_kv_heads.
  *   - Token i sees token j when j <= i and (window == 0 or i - j < window or j < sinks): the `window`
  *     newest tokens, itself among them, and the first `sinks` ones.  A query that sees nothing has output
- *     zero and log-sum-exp -inf.
+ *     zero and log-sum-exp -inf.  scale is positive and finite (RA_ERR_ARG).  A key or value that is not finite
+ *     reaches the tokens that see it; it may also reach tokens of its own sequence that do not.
  *   - A workspace is caller-owned, 256-byte aligned, at least the bytes that the call's _workspace_bytes
  *     gives for the same argument block, and zero-filled once before its first use: calls leave zero what
  *     they need to find zero.  Calls that may run at the same time need different workspaces.  RA_ERR_NOMEM

@@ -1,4 +1,6 @@
 // operators.cu -- C ABI of the operators that answer with a tuned decoder: argument checks, then the launch.
+#include <cmath>
+
 #include "operators.h"
 
 using namespace ra;
@@ -11,6 +13,8 @@ ra_status launched(cudaError_t e) {
 }
 bool aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 int vec(int dtype) { return dtype == RA_BF16 ? 8 : 4; }  // values of 16 bytes
+// (the largest score is the largest product, scaled)
+bool good_scale(float s) { return s > 0.f && std::isfinite(s); }
 // rows of head_dim values, `heads` to a token, at a 16-byte aligned base
 ra_status check_rows(const void* p, int64_t stride, int heads, int head_dim, int dtype) {
   if (!p || !aligned(p, 16)) return RA_ERR_ARG;
@@ -55,7 +59,7 @@ ra_status check_decode(const ra_attention_decode_args& a) {
   TRY(check_cache(a.cache));
   const ra_kv_cache& c = a.cache;
   if (!a.lens_dev || a.batch < 0 || a.n_new < 1 || a.n_heads < 1 || a.n_heads % c.n_kv_heads || a.window < 0 ||
-      a.sinks < 0 || a.max_len < 0)
+      a.sinks < 0 || a.max_len < 0 || !good_scale(a.scale))
     return RA_ERR_ARG;
   TRY(check_rows(a.q_dev, a.q_stride, a.n_heads, c.head_dim, c.dtype));
   TRY(check_rows(a.out_dev, a.out_stride, a.n_heads, c.head_dim, c.dtype));
@@ -81,7 +85,7 @@ ra_status check_evict(const ra_kv_evict_args& a) {
 ra_status check_window(const ra_attention_window_args& a, bool backward) {
   if (a.dtype != RA_F32 && a.dtype != RA_BF16) return RA_ERR_ARG;
   if (a.batch < 0 || a.seq < 0 || a.n_heads < 1 || a.n_kv_heads < 1 || a.n_heads % a.n_kv_heads || a.window < 0 ||
-      a.sinks < 0)
+      a.sinks < 0 || !good_scale(a.scale))
     return RA_ERR_ARG;
   const bool dims = a.dtype == RA_BF16 ? a.head_dim == 64 || a.head_dim == 128
                                        : a.head_dim >= 4 && a.head_dim <= 128 && a.head_dim % 4 == 0;
@@ -154,7 +158,8 @@ ra_status ra_attention_window_forward(const ra_attention_window_args* args, ra_s
   TRY(check_window(*args, false));
   if (!tc_available()) return RA_ERR_UNSUPPORTED;
   if (args->batch == 0 || args->seq == 0) return RA_OK;
-  return launched(attention_window_fwd_simt(*args, (cudaStream_t)stream));
+  return launched(args->dtype == RA_BF16 ? attention_window_fwd_tc(*args, (cudaStream_t)stream)
+                                         : attention_window_fwd_simt(*args, (cudaStream_t)stream));
 }
 ra_status ra_attention_window_backward(const ra_attention_window_args* args, ra_stream_t stream) {
   if (!args) return RA_ERR_ARG;

@@ -90,7 +90,7 @@ def test_append(bad, status):
 @pytest.mark.parametrize("bad,status", [
     (dict(lens_dev=None), ARG), (dict(q_dev=None), ARG), (dict(out_dev=P + 8), ARG), (dict(q_stride=255), SHAPE),
     (dict(out_stride=128), SHAPE), (dict(n_heads=5), ARG), (dict(n_new=0), ARG), (dict(window=-1), ARG), (dict(sinks=-1), ARG),
-    (dict(max_len=-1), ARG), (dict(weights_in_dev=P), ARG), (dict(weights_out_dev=P, weights_stride=63), SHAPE),
+    (dict(max_len=-1), ARG), (dict(scale=0.0), ARG), (dict(scale=float("nan")), ARG), (dict(weights_in_dev=P), ARG), (dict(weights_out_dev=P, weights_stride=63), SHAPE),
     (dict(workspace_dev=None), ARG), (dict(workspace_dev=P + 128), ARG), (dict(workspace_bytes=100), NOMEM), (dict(batch=-2), ARG),
     (dict(batch=1 << 20, n_new=1 << 10), SHAPE)])
 def test_decode(bad, status):
@@ -111,6 +111,7 @@ def test_evict(bad, status):
     (dict(q_dev=None), ARG), (dict(k_dev=P + 8), ARG), (dict(v_stride=64), SHAPE), (dict(out_dev=None), ARG), (dict(dtype=2), ARG),
     (dict(n_kv_heads=3), ARG), (dict(n_kv_heads=0), ARG), (dict(head_dim=96), SHAPE), (dict(head_dim=6, dtype=R.RA_F32), SHAPE),
     (dict(head_dim=132, dtype=R.RA_F32), SHAPE), (dict(window=-1), ARG), (dict(sinks=-3), ARG), (dict(seq=-1), ARG),
+    (dict(scale=-1.0), ARG), (dict(scale=float("inf")), ARG),
     (dict(batch=1 << 16, seq=1 << 15), SHAPE), (dict(q_stride=258), SHAPE)])
 def test_window(bad, status):
     refused(R.ra_attention_window_forward, window(**bad), status)
