@@ -200,7 +200,6 @@ __global__ void __launch_bounds__(NT) window_fwd_simt_kernel(const __grid_consta
 
 // ---- backward ------------------------------------------------------------------------------
 // D_i = dO_i . o_i, a warp a row (0 past the sequence's end)
-template <typename T>
 __global__ void __launch_bounds__(256) window_bwd_d_kernel(const __grid_constant__ ra_attention_window_args a, float* D) {
   pdl_wait();
   pdl_trigger();
@@ -211,9 +210,9 @@ __global__ void __launch_bounds__(256) window_bwd_d_kernel(const __grid_constant
     const int head = (int)(r - tok * a.n_heads), b = (int)(tok / a.seq), s = (int)(tok - (int64_t)b * a.seq);
     float d = 0.f;
     if (!a.lens_dev || s < a.lens_dev[b]) {
-      const T* o = (const T*)a.out_dev + tok * a.out_stride + head * a.head_dim;
-      const T* g = (const T*)a.dout_dev + tok * a.dout_stride + head * a.head_dim;
-      for (int c = lane; c < a.head_dim; c += 32) d = fmaf(to_f(o[c]), to_f(g[c]), d);
+      const float* o = (const float*)a.out_dev + tok * a.out_stride + head * a.head_dim;
+      const float* g = (const float*)a.dout_dev + tok * a.dout_stride + head * a.head_dim;
+      for (int c = lane; c < a.head_dim; c += 32) d = fmaf(o[c], g[c], d);
     }
     d = warp_sum(d);
     if (lane == 0) D[((int64_t)b * a.n_heads + head) * a.seq + s] = d;
@@ -350,6 +349,12 @@ cudaError_t fwd_simt(const ra_attention_window_args& a, cudaStream_t st) {
   note_launch(1);
   return e;
 }
+cudaError_t rows_d(const ra_attention_window_args& a, float* D, cudaStream_t st) {
+  const int64_t blocks = ((int64_t)a.batch * a.seq * a.n_heads + 7) / 8, most = 64LL * device_sm_count();
+  cudaError_t e = launch_pdl(window_bwd_d_kernel, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, st, a, D);
+  note_launch(1);
+  return e;
+}
 template <int DH>
 cudaError_t bwd_simt(const ra_attention_window_args& a, cudaStream_t st) {
   const int n_blk = (a.seq + BT - 1) / BT;
@@ -358,7 +363,7 @@ cudaError_t bwd_simt(const ra_attention_window_args& a, cudaStream_t st) {
   float* D = (float*)a.workspace_dev;
   cudaError_t e = allow_smem(window_bwd_simt_kernel<DH, true>, Plan<DH>::BWD_BYTES);
   if (e == cudaSuccess) e = allow_smem(window_bwd_simt_kernel<DH, false>, Plan<DH>::BWD_BYTES);
-  if (e == cudaSuccess) e = attention_window_d(a, D, st);
+  if (e == cudaSuccess) e = rows_d(a, D, st);
   if (e != cudaSuccess) return e;
   const float* Dc = D;
   e = launch_pdl(window_bwd_simt_kernel<DH, true>, dim3((unsigned)gk), dim3(NT), Plan<DH>::BWD_BYTES, st, a, Dc, window_of(a), n_blk);
@@ -370,15 +375,8 @@ cudaError_t bwd_simt(const ra_attention_window_args& a, cudaStream_t st) {
 
 }  // namespace
 
-size_t attention_window_workspace(const ra_attention_window_args& a) { return (size_t)a.batch * a.seq * a.n_heads * 4; }
-
-cudaError_t attention_window_d(const ra_attention_window_args& a, float* D, cudaStream_t st) {
-  const int64_t blocks = ((int64_t)a.batch * a.seq * a.n_heads + 7) / 8, most = 64LL * device_sm_count();
-  const dim3 grid((unsigned)(blocks < most ? blocks : most));
-  cudaError_t e = a.dtype == RA_BF16 ? launch_pdl(window_bwd_d_kernel<bf16>, grid, dim3(256), 0, st, a, D)
-                                     : launch_pdl(window_bwd_d_kernel<float>, grid, dim3(256), 0, st, a, D);
-  note_launch(1);
-  return e;
+size_t attention_window_workspace(const ra_attention_window_args& a) {
+  return a.dtype == RA_BF16 ? attention_window_workspace_tc(a) : (size_t)a.batch * a.seq * a.n_heads * 4;
 }
 
 cudaError_t attention_window_fwd_simt(const ra_attention_window_args& a, cudaStream_t st) {

@@ -14,11 +14,9 @@
 // below 2^8 and sums in fp32 lose nothing): the first block sets the scale and almost none after it changes it.
 // Key blocks that no row of a tile sees are not loaded: a tile walks the blocks that hold sinks, then its window.  Rows past a
 // sequence's end are zero in V's last block before it is read (p = 0 there, but 0 times NaN would not be 0).
-#include <cuda.h>
-
 #include "common.cuh"
 #include "operators.h"
-#include "tcgen05.cuh"
+#include "window_tc.cuh"
 
 namespace ra {
 namespace {
@@ -46,38 +44,6 @@ struct FwdPlan {
   static constexpr uint32_t C_S = 0, C_O = 256;  // scores of tile t at 128 t; outputs at 256 + DH t
 };
 
-__device__ __forceinline__ void tma_load3(const CUtensorMap* tm, uint32_t dst, uint64_t* bar, int c0, int c1, int c2) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-      " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(c0), "r"(c1), "r"(c2),
-      "r"(smem_u32(bar)) : "memory");
-}
-__device__ __forceinline__ void tma_store3(const CUtensorMap* tm, uint32_t src, int c0, int c1, int c2) {
-  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(
-                   reinterpret_cast<uint64_t>(tm)), "r"(c0), "r"(c1), "r"(c2), "r"(src) : "memory");
-}
-// D[tmem] (+)= A[tmem, 128 x 16 bf16] B
-__device__ __forceinline__ void umma_bf16_ts(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d), "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* r) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(addr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
-      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
-}
-__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ uint32_t pk2(float a, float b) {
-  __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-  return *reinterpret_cast<uint32_t*>(&h);
-}
-__device__ __forceinline__ void named_sync(int id, int threads) {
-  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
-}
-
 // The key blocks of a CTA: those with sinks, [0, ns), then [lo, hi], ns <= lo; and each tile's part of them
 struct Blocks {
   int ns, lo, hi, n;
@@ -93,7 +59,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_fwd_tc_kernel(const __grid_
   using Pl = FwdPlan<DH>;
   constexpr int SLOTS = Pl::SLOTS, BLK = Pl::BLK;
   extern __shared__ __align__(1024) uint8_t smem[];
-  __shared__ __align__(8) uint64_t full[SLOTS], empty[SLOTS], q_full, s_full[2], p_full[2], o_full[2], drain;
+  __shared__ __align__(8) uint64_t full[SLOTS], empty[SLOTS], q_full, s_full[2], p_full[2], o_full[2], staged[2], drain;
   __shared__ uint32_t tmem_sh;
   __shared__ volatile int abort_sh;
   const uint32_t sb = smem_u32(smem);
@@ -129,6 +95,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_fwd_tc_kernel(const __grid_
         mbar_init(&s_full[t], 1);
         mbar_init(&p_full[t], 4);
         mbar_init(&o_full[t], 1);
+        mbar_init(&staged[t], 4);
       }
       abort_sh = 0;
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -213,14 +180,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_fwd_tc_kernel(const __grid_
         ok = mbar_wait_warp(&full[vs], ((2 * i - 1) / SLOTS) & 1, &abort_sh, a.err);
         if (!ok) break;
         const int dead = len - prev * BR;  // rows from here on are past the sequence's end
-        if (dead < BR) {
-          for (int e = lane; e < (BR - dead) * (DH / 8); e += 32) {
-            const int r = dead + e / (DH / 8), c = e % (DH / 8);
-            *reinterpret_cast<uint4*>(smem + Pl::RING + vs * BLK + (c >> 3) * (BR * 128) + r * 128 + ((c & 7) << 4)) = make_uint4(0, 0, 0, 0);
-          }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
-        }
+        if (dead < BR) zero_rows<DH>(smem + Pl::RING + vs * BLK, dead, lane);
       }
       if (i < kb.n) {
         ok = mbar_wait_warp(&full[ks], ((2 * i) / SLOTS) & 1, &abort_sh, a.err);
@@ -374,12 +334,12 @@ __global__ void __launch_bounds__(THREADS, 1) window_fwd_tc_kernel(const __grid_
       if (a.lse && q < a.seq)
         a.lse[((int64_t)b * a.n_heads + head[t]) * a.seq + q] = q < len && m != -INFINITY ? (m + log2f(l)) * kLn2 : -INFINITY;
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      named_sync(1 + t, 128);
-      if (row == 0) {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&staged[t]);
+      if (row == 0 && mbar_wait(&staged[t], 0, &abort_sh, a.err)) {
 #pragma unroll
         for (int n = 0; n < DH / 64; ++n) tma_store3(&tmO, smem_u32(stage) + n * (BR * 128), head[t] * DH + 64 * n, q0[t], b);
-        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-        asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        tma_store_done();
       }
     }
   }

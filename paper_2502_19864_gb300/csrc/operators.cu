@@ -166,7 +166,8 @@ ra_status ra_attention_window_backward(const ra_attention_window_args* args, ra_
   TRY(check_window(*args, true));
   if (!tc_available()) return RA_ERR_UNSUPPORTED;
   if (args->batch == 0 || args->seq == 0) return RA_OK;
-  return launched(attention_window_bwd_simt(*args, (cudaStream_t)stream));
+  return launched(args->dtype == RA_BF16 ? attention_window_bwd_tc(*args, (cudaStream_t)stream)
+                                         : attention_window_bwd_simt(*args, (cudaStream_t)stream));
 }
 
 size_t ra_verify_draft_workspace_bytes(const ra_verify_draft_args* args) {

@@ -20,10 +20,10 @@ cudaError_t kv_evict(const ra_kv_evict_args& a, cudaStream_t st);
 size_t attention_decode_workspace(const ra_attention_decode_args& a);
 cudaError_t attention_decode(const ra_attention_decode_args& a, cudaStream_t st);
 size_t attention_window_workspace(const ra_attention_window_args& a);
-// D_i = dO_i . o_i into D [batch, n_heads, seq]
-cudaError_t attention_window_d(const ra_attention_window_args& a, float* D, cudaStream_t st);
 cudaError_t attention_window_fwd_simt(const ra_attention_window_args& a, cudaStream_t st);
 cudaError_t attention_window_fwd_tc(const ra_attention_window_args& a, cudaStream_t st);
+size_t attention_window_workspace_tc(const ra_attention_window_args& a);
+cudaError_t attention_window_bwd_tc(const ra_attention_window_args& a, cudaStream_t st);
 cudaError_t attention_window_bwd_simt(const ra_attention_window_args& a, cudaStream_t st);
 size_t verify_draft_workspace(const ra_verify_draft_args& a);
 cudaError_t verify_draft(const ra_verify_draft_args& a, cudaStream_t st);
