@@ -5,13 +5,16 @@
 // The query rows of a key-value head are its group's heads times the new tokens (R rows, a few to a few dozen); K and
 // V are read once for all of them, 4 R head_dim flops for every 2 head_dim values: bound by memory.  The slots that
 // any row sees (all, or the sinks and the windows) are numbered 0, 1, ... and cut into tiles of TK; the tiles of all
-// sequences and heads, one after the other, are dealt to the CTAs in equal runs, whatever the lengths are.  A CTA
-// walks its run with a ring of tiles on their way (cp.async, so that a page may end anywhere), keeping the running
-// maximum m, sum l and outputs of the (sequence, head) at hand; where a run ends inside one, (m, l, o) go to the
-// workspace and a second kernel joins the parts in the order of their slots.
+// sequences and heads, one after the other, are dealt to the CTAs in equal runs, whatever the lengths are.  A CTA's warps
+// (or groups of 2 or 4 that split more than sixteen rows) take the tiles of its run in turn, each with a ring of its own
+// for tiles on their way (cp.async: a page may end anywhere) and its own running maximum m, sum l and outputs; nothing
+// but the end of a (sequence, head) makes warps wait for one another.  There the CTA adds up its warps; where its run
+// covers a part of the head's tiles only, (m, l, o) go to the workspace, and the last CTA to leave its part (a counter;
+// the order of the sum is the parts', not theirs) joins them.
 //   bf16: the products are mma.sync m16n8k16: sixteen rows take the tensor instruction of one, and the rate asked of
 //         it, 16 flops a byte of K and V, is a tenth of what it gives, so nothing is won by tcgen05's 128 rows.
-//   f32:  FFMA, a warp's lanes on 32 tokens for q k and a thread a column for p v.
+//   f32:  mma.sync m16n8k8 on tf32, each operand in two terms of 11 bits and their products but for the smallest: about
+//         2^-22 of a product, as good as the fp32 sums around it.
 #include "common.cuh"
 #include "operators.h"
 #include "paged.cuh"
@@ -31,12 +34,14 @@ struct DecodeArgs {
   const float* w_in;
   float* w_out;
   int64_t w_stride;
-  float* part_o;                 // [2 grid][rows of a tile][DHT]
-  float2* part_ml;               // [2 grid][rows of a tile]
+  unsigned* done;                // [batch, kv heads, groups]: CTAs that have left their part; zero between calls
+  float* part_o;                 // [2 grid][rows of a unit][head dim]
+  float2* part_ml;               // [2 grid][rows of a unit]
   float* lse2;                   // [batch, kv heads, R] (powers of two), where weights are wanted
   float* scores;                 // [batch, kv heads, R, x_stride], scaled, in powers of two
   int64_t x_stride;
   int batch, n_new, n_heads, G, R, groups, max_len, window, sinks, grid;
+  int join;                      // the last CTA of a unit joins its parts (else a kernel of its own)
   float sl2;                     // scale log2 e
 };
 
@@ -68,8 +73,8 @@ __device__ __forceinline__ int64_t warp_sum64(int64_t v) {
 }
 
 // How the tiles are dealt: unit (b, u), u = kv head * groups + row group, has tiles(b) tiles; units in order.
-// One warp computes; `total` tiles go to min(grid, total) CTAs.
-template <int TK>
+// One warp computes; `total` tiles go to as many CTAs as have a tile for each of their SHARE warps, at most the grid.
+template <int TK, int SHARE>
 struct Deal {
   int64_t total;
   int workers;
@@ -79,11 +84,12 @@ struct Deal {
     int64_t t = 0;
     for (int b = lane; b < a.batch; b += 32) t += (int64_t)tiles(a, b) * units;
     total = warp_sum64(t);
-    workers = total < a.grid ? (int)total : a.grid;
+    const int64_t w = (total + SHARE - 1) / SHARE;
+    workers = w < a.grid ? (int)w : a.grid;
   }
   __device__ __forceinline__ int64_t start(int cta) const { return total * cta / workers; }
   __device__ __forceinline__ int owner(int64_t tile) const { return (int)(((tile + 1) * workers - 1) / total); }
-  // the sequence that tile `at` belongs to, and its first tile (lane-wide, same in all lanes)
+  // the sequence that tile `at` belongs to, and its first tile (same in all lanes)
   __device__ void find(const DecodeArgs& a, int64_t at, int lane, int& b, int64_t& first) const {
     const int units = a.c.n_kv_heads * a.groups;
     int64_t acc = 0;
@@ -114,7 +120,7 @@ struct Deal {
   }
 };
 
-// Where a CTA is in its run: a tile of a unit
+// Where in its run a CTA is: a tile of a unit
 template <int TK>
 struct Cursor {
   int b, u, tile, tiles;
@@ -123,15 +129,24 @@ struct Cursor {
     s = seen_of(a, b);
     tiles = (s.n + TK - 1) / TK;
   }
-  __device__ __forceinline__ void next(const DecodeArgs& a) {
-    if (++tile < tiles) return;
-    tile = 0;
+  // on to the next unit's tile 0 (past the last sequence: b == batch)
+  __device__ __forceinline__ void next_unit(const DecodeArgs& a) {
     if (++u < a.c.n_kv_heads * a.groups) return;
     u = 0;
     do {
-      if (++b >= a.batch) return;  // (the run ends before)
+      if (++b >= a.batch) {
+        tiles = 1 << 30;
+        return;
+      }
       enter(a);
     } while (tiles == 0);
+  }
+  __device__ __forceinline__ void skip(const DecodeArgs& a, int n) {
+    tile += n;
+    while (tile >= tiles) {
+      tile -= tiles;
+      next_unit(a);
+    }
   }
 };
 
@@ -150,593 +165,516 @@ __device__ __forceinline__ uint32_t pack2(float x, float y) {
 }
 __device__ __forceinline__ void ldsm4(uint32_t* r, uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
 __device__ __forceinline__ void ldsm4t(uint32_t* r, uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
 __device__ __forceinline__ void mma16816(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma1688(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// x in two tf32 terms, the first rounded to nearest
+__device__ __forceinline__ void split_tf32(float x, uint32_t& hi, uint32_t& lo) {
+  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(hi) : "f"(x));
+  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(lo) : "f"(x - __uint_as_float(hi)));
+}
 
-// The start of a CTA's run, for all its threads; false where it has none
-template <int TK>
-__device__ bool begin_run(const DecodeArgs& a, Cursor<TK>& cur, int64_t& n_tiles) {
-  __shared__ int64_t run_n, run_first;
-  __shared__ int run_b;
-  if (threadIdx.x < 32) {
-    Deal<TK> d;
-    d.count(a, threadIdx.x);
+// ---------------------------------------------------------------------------------------
+// WM: warps of a group, each on sixteen of the unit's 16 WM rows; NG groups a CTA, one CTA an SM.  A stage holds K and V
+// of TK tokens, rows of DHT values (zeros past head_dim and past the tokens that are there) whose 16-byte chunks are
+// permuted so that the reads below meet no bank twice.
+// ---------------------------------------------------------------------------------------
+template <typename T, int DHT, int WM>
+struct Plan {
+  static constexpr bool B16 = sizeof(T) == 2;
+  static constexpr int TK = (B16 ? (DHT == 256 ? 16 : 32) : (DHT == 256 ? 8 : 16)) * (WM == 4 ? 2 : 1);
+  static constexpr int NG = WM == 4 ? 2 : 4, THREADS = 32 * WM * NG, ROWS = 16 * WM;
+  static constexpr int TILE = TK * DHT * (int)sizeof(T), STAGE = 2 * TILE, STAGES = DHT == 64 ? 6 : 3, RING = STAGES * STAGE;
+  static constexpr int Q = NG * RING, STATS = Q + ROWS * DHT * (int)sizeof(T), MASK = STATS + NG * ROWS * 8,
+                       BYTES = MASK + NG * STAGES * 8;
+  static_assert(ROWS * DHT * 4 <= STAGE, "a group's outputs are put into a stage");
+  static_assert(BYTES <= 226 * 1024, "shared memory");
+  // float `col` of row `row` of a group's outputs in its stage: eight rows' pairs fall in distinct banks
+  static __device__ __forceinline__ int at(int row, int col) { return row * DHT + (col ^ ((row & 7) << 3)); }
+  // where the 16-byte chunk of a row of K or V goes
+  static __device__ __forceinline__ int k_chunk(int row, int c) { return B16 ? c ^ (row & 7) : c ^ ((row & 1) << 2); }
+  static __device__ __forceinline__ int v_chunk(int row, int c) { return B16 ? c ^ (row & 7) : c ^ (((row >> 1) & 3) << 1); }
+};
+
+template <typename T>
+__device__ __forceinline__ void store4(T* dst, float4 v);
+template <>
+__device__ __forceinline__ void store4<bf16>(bf16* dst, float4 v) {
+  *reinterpret_cast<uint2*>(dst) = make_uint2(pack2(v.x, v.y), pack2(v.z, v.w));
+}
+template <>
+__device__ __forceinline__ void store4<float>(float* dst, float4 v) {
+  *reinterpret_cast<float4*>(dst) = v;
+}
+// f a + s
+__device__ __forceinline__ float4 fma4(float4 a, float f, float4 s) {
+  return make_float4(fmaf(a.x, f, s.x), fmaf(a.y, f, s.y), fmaf(a.z, f, s.z), fmaf(a.w, f, s.w));
+}
+// the factor of a part with statistics (m, l) under the common maximum M; what has seen nothing takes no part
+__device__ __forceinline__ bool counts(float2 ml) { return !(ml.x == -INFINITY && ml.y == 0.f); }
+// a finished row: output (four columns from d) and, with column 0, its log-sum-exp
+template <typename T>
+__device__ __forceinline__ void finish(const DecodeArgs& a, int b, int hk, int row, int d, float4 o, float M, float L, bool any) {
+  const int t = row / a.G, head = hk * a.G + row - t * a.G;
+  const float f = any ? 1.f / L : 0.f;
+  store4<T>((T*)a.out + ((int64_t)b * a.n_new + t) * a.out_stride + head * a.c.head_dim + d, make_float4(o.x * f, o.y * f, o.z * f, o.w * f));
+  if (d == 0) {
+    const float lse2 = any ? M + log2f(L) : -INFINITY;
+    if (a.lse) a.lse[((int64_t)b * a.n_new + t) * a.n_heads + head] = lse2 * kLn2;
+    if (a.scores) a.lse2[((int64_t)b * a.c.n_kv_heads + hk) * a.R + row] = lse2;
+  }
+}
+
+template <typename T, int DHT, int WM>
+__global__ void __launch_bounds__(Plan<T, DHT, WM>::THREADS, 1) decode_kernel(const __grid_constant__ DecodeArgs a) {
+  using P = Plan<T, DHT, WM>;
+  constexpr bool B16 = P::B16;
+  constexpr int TK = P::TK, S = P::STAGES, NG = P::NG, ROWS = P::ROWS, GT = 32 * WM, VE = 16 / (int)sizeof(T), CH = DHT / VE, NT = TK / 8;
+  extern __shared__ __align__(128) uint8_t sm[];
+  __shared__ int64_t run_start, run_total;
+  __shared__ int run_n, run_b, run_workers, joins;
+  __shared__ int64_t run_in;
+  pdl_wait();
+  pdl_trigger();
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, grp = warp / WM, wm = warp - grp * WM;
+  if (warp == 0) {
+    Deal<TK, NG> d;
+    d.count(a, lane);
     int b = 0;
-    int64_t first = 0, n = 0;
+    int64_t first = 0, n = 0, s = 0;
     if ((int)blockIdx.x < d.workers) {
-      const int64_t s = d.start(blockIdx.x);
+      s = d.start(blockIdx.x);
       n = d.start(blockIdx.x + 1) - s;
-      d.find(a, s, threadIdx.x, b, first);
-      first = s - first;  // of its sequence's tiles
+      d.find(a, s, lane, b, first);
     }
-    if (threadIdx.x == 0) {
-      run_n = n;
+    if (lane == 0) {
+      run_n = (int)n;
       run_b = b;
-      run_first = first;
+      run_in = s - first;  // of its sequence's tiles
+      run_start = s;
+      run_total = d.total;
+      run_workers = d.workers;
     }
   }
   __syncthreads();
-  n_tiles = run_n;
-  if (n_tiles == 0) return false;
+  // sequences without a token: zeros (dealt in turn to all CTAs)
+  for (int b = blockIdx.x; b < a.batch; b += gridDim.x)
+    if (seen_of(a, b).n == 0)
+      for (int e = tid; e < a.c.n_kv_heads * a.R * (a.c.head_dim / 4); e += P::THREADS) {
+        const int row = e / (a.c.head_dim / 4), d = (e - row * (a.c.head_dim / 4)) * 4;
+        finish<T>(a, b, row / a.R, row % a.R, d, make_float4(0.f, 0.f, 0.f, 0.f), 0.f, 0.f, false);
+      }
+  const int n_tiles = run_n;
+  if (n_tiles == 0) return;
+  const int g = lane >> 2, t4 = lane & 3, dh = a.c.head_dim;
+  const T *Kp = (const T*)a.c.k_dev, *Vp = (const T*)a.c.v_dev;
+  uint8_t* ring = sm + grp * P::RING;
+  float2* stats = reinterpret_cast<float2*>(sm + P::STATS);  // [NG][ROWS]
+  uint64_t* mask = reinterpret_cast<uint64_t*>(sm + P::MASK) + grp * S;
+  auto group_sync = [&]() {
+    if (WM == 1)
+      __syncwarp();
+    else
+      asm volatile("bar.sync %0, %1;" ::"r"(1 + grp), "r"(GT) : "memory");
+  };
+
+  Cursor<TK> cur;  // the first tile of the segment at hand
   cur.b = run_b;
   cur.enter(a);
-  cur.u = (int)(run_first / cur.tiles);
-  cur.tile = (int)(run_first - (int64_t)cur.u * cur.tiles);
-  return true;
-}
+  cur.u = (int)(run_in / cur.tiles);
+  cur.tile = (int)(run_in - (int64_t)cur.u * cur.tiles);
+  Cursor<TK> ahead = cur;  // this group's tile whose rows are looked up next
+  ahead.skip(a, grp);
 
-// A tile's rows: their places in the pools (-1: none), by the threads below TK; the pages' numbers are requested a
-// tile ahead.
-template <int TK>
-struct RowPlan {
-  int page, off;  // page number read from the table; row of the page
-  __device__ __forceinline__ void request(const DecodeArgs& a, const Cursor<TK>& c, bool live) {
-    page = -1;
-    const int x = c.tile * TK + (int)threadIdx.x;
-    if (live && x < c.s.n) {
-      const int slot = slot_of(c.s, x), p = slot / a.c.page_size;
-      off = slot - p * a.c.page_size;
-      page = a.c.block_table_dev[(int64_t)c.b * a.c.max_pages + p];
-      if ((uint32_t)page >= (uint32_t)a.c.n_pages) {
-        set_dev_error(a.c.err_dev, RA_DEVERR_BOUNDS);
-        page = -1;
+  // ---- copies.  Lanes (of every warp of the group) look up the rows of a tile, a tile before they are copied
+  int asked = grp;         // run-relative number of the tile looked up
+  int64_t my_row[(TK + 31) / 32];
+  auto look_up = [&]() {
+#pragma unroll
+    for (int h = 0; h < (TK + 31) / 32; ++h) {
+      my_row[h] = -1;
+      const int i = 32 * h + lane, x = ahead.tile * TK + i;
+      if (asked < n_tiles && i < TK && x < ahead.s.n) {
+        const int slot = slot_of(ahead.s, x), p = slot / a.c.page_size;
+        const int page = a.c.block_table_dev[(int64_t)ahead.b * a.c.max_pages + p];
+        if ((uint32_t)page < (uint32_t)a.c.n_pages)
+          my_row[h] = ((int64_t)page * a.c.n_kv_heads + ahead.u / a.groups) * a.c.page_size + (slot - p * a.c.page_size);
+        else
+          set_dev_error(a.c.err_dev, RA_DEVERR_BOUNDS);
       }
     }
-  }
-  __device__ __forceinline__ int64_t row(const DecodeArgs& a, int head) const {
-    return page < 0 ? -1 : ((int64_t)page * a.c.n_kv_heads + head) * a.c.page_size + off;
-  }
-};
-
-// ---------------------------------------------------------------------------------------
-// bf16.  Tiles of 64 tokens; 4 WM warps: warp (w, g) takes 16 of the tokens for rows 16 g .. 16 g + 15, with
-// its own m, l and outputs; the four warps of a row group are added up where the CTA leaves a unit.
-// ---------------------------------------------------------------------------------------
-constexpr int TKB = 64;
-template <int DHT, int WM>
-struct MmaPlan {
-  static constexpr int THREADS = 128 * WM, STAGES = DHT == 64 ? 6 : 3, ROWS = 16 * WM;
-  static constexpr int TILE = TKB * DHT * 2, STAGE = 2 * TILE;
-  // two sets of outputs are added up in the stage of the tile just done, which nothing is copied into before the
-  // next tile's barrier; four row groups have more than it holds and a space of their own
-  static constexpr bool IN_STAGE = 2 * ROWS * DHT * 4 <= STAGE;
-  static constexpr int STATS = STAGES * STAGE + (IN_STAGE ? 0 : 2 * ROWS * DHT * 4), ROWOFF = STATS + 4 * ROWS * 8,
-                       MASK = ROWOFF + 2 * TKB * 8, BYTES = MASK + (STAGES + 1) * 8;
-  // float `col` of a row of the sum: eight rows' pairs fall in distinct banks
-  static __device__ __forceinline__ int at(int buf, int row, int col) { return (buf * ROWS + row) * DHT + (col ^ ((row & 7) << 3)); }
-};
-
-template <int DHT, int WM>
-__global__ void __launch_bounds__(128 * WM) decode_mma_kernel(const __grid_constant__ DecodeArgs a) {
-  using P = MmaPlan<DHT, WM>;
-  constexpr int TK = TKB, S = P::STAGES, CH = DHT / 8;
-  extern __shared__ __align__(128) uint8_t sm[];
-  pdl_wait();
-  pdl_trigger();
-  Cursor<TK> cur;
-  int64_t n_tiles;
-  if (!begin_run<TK>(a, cur, n_tiles)) return;
-  Cursor<TK> ahead = cur;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, wt = warp & 3, wg = warp >> 2;
-  const int g = lane >> 2, t2 = (lane & 3) * 2, dh = a.c.head_dim;
-  float2* stats = reinterpret_cast<float2*>(sm + P::STATS);  // [4][ROWS]
-  int64_t* rowoff = reinterpret_cast<int64_t*>(sm + P::ROWOFF);
-  // [STAGES + 1][2]: one more than there are stages, as a tile's is written before the barrier that its stage waits for
-  uint32_t* mask = reinterpret_cast<uint32_t*>(sm + P::MASK);
-  const uint32_t ring = smem_addr(sm);
-  const bf16 *Kp = (const bf16*)a.c.k_dev, *Vp = (const bf16*)a.c.v_dev;
-  const int col = tid % CH, r_first = tid / CH;  // this thread's 16-byte column of the rows it copies
-
-  RowPlan<TK> plan;
-  int64_t asked = 0;  // tiles whose pages were requested
-  if (tid < TK) plan.request(a, ahead, true);
-  asked = 1;
-  // the requested tile's rows -> rowoff and mask; the next tile's pages are requested
-  auto place = [&](int64_t tile, int head) {
-    if (tid < TK) {
-      const int64_t r = plan.row(a, head);
-      rowoff[(tile & 1) * TK + tid] = r;
-      const uint32_t m = __ballot_sync(0xffffffffu, r >= 0);
-      if (lane == 0) mask[2 * (int)(tile % (S + 1)) + warp] = m;
-    }
   };
-  auto copy = [&](int64_t tile) {
-    const uint32_t st = ring + (uint32_t)(tile % S) * P::STAGE;
-    const bool in = col * 8 < dh;
+  // the looked-up tile into stage st
+  auto copy = [&](int st) {
+    const uint32_t dst = smem_addr(ring + st * P::STAGE);
+    uint64_t live = 0;
+#pragma unroll
+    for (int h = 0; h < (TK + 31) / 32; ++h) live |= (uint64_t)__ballot_sync(0xffffffffu, my_row[h] >= 0) << (32 * h);
+    if (lane == 0 && wm == 0) mask[st] = live;
+    constexpr int PER = (CH < 32 ? 32 / CH : 1), STEP = PER * WM;  // rows a warp copies at once, and the group
+    const int rsub = CH < 32 ? lane / CH : 0;
 #pragma unroll 4
-    for (int r = r_first; r < TK; r += P::THREADS / CH) {
-      const int64_t at = rowoff[(tile & 1) * TK + r];
-      const bool live = in && at >= 0;
-      const int64_t e = live ? at * dh + col * 8 : 0;
-      const uint32_t d = st + r * (DHT * 2) + ((col ^ (r & 7)) << 4);
-      cp16(d, Kp + e, live);
-      cp16(d + P::TILE, Vp + e, live);
+    for (int r0 = wm * PER; r0 < TK; r0 += STEP) {
+      const int r = r0 + rsub;
+      const int64_t row = __shfl_sync(0xffffffffu, (TK > 32 && r0 >= 32) ? my_row[(TK + 31) / 32 - 1] : my_row[0], r & 31);
+#pragma unroll
+      for (int c = CH < 32 ? lane % CH : lane; c < CH; c += 32) {
+        const bool on = row >= 0 && c * VE < dh;
+        const int64_t e = on ? row * dh + c * VE : 0;
+        cp16(dst + r * (DHT * (int)sizeof(T)) + P::k_chunk(r, c) * 16, Kp + e, on);
+        cp16(dst + P::TILE + r * (DHT * (int)sizeof(T)) + P::v_chunk(r, c) * 16, Vp + e, on);
+      }
     }
   };
-  auto step_ahead = [&]() {  // after place(): on to the next tile's pages
-    ahead.next(a);
-    if (tid < TK) plan.request(a, ahead, asked < n_tiles);
-    ++asked;
+  auto go_on = [&]() {  // to this group's next tile
+    asked += NG;
+    if (asked < n_tiles) ahead.skip(a, NG);
+    look_up();
   };
+  look_up();
 #pragma unroll 1
   for (int i = 0; i < S - 1; ++i) {
-    if (i < n_tiles) {
-      place(i, ahead.u / a.groups);
-      __syncthreads();
-      copy(i);
-      if (asked < n_tiles) step_ahead();
-    }
+    if (asked < n_tiles) copy(i);
     cp_commit();
+    go_on();
   }
 
-  uint32_t qf[DHT / 16][4];
-  float o[DHT / 8][4], m[2], l[2];
-  int qslot[2];
-  bool first_tile_of_unit = true, first_segment = true;
-  int seg_start = cur.tile;
-  for (int64_t i = 0; i < n_tiles; ++i) {
-    if (first_tile_of_unit) {
-      first_tile_of_unit = false;
-      seg_start = cur.tile;
-      const int hk = cur.u / a.groups, r0 = (cur.u - hk * a.groups) * P::ROWS + 16 * wg;
+  int st = 0;          // the stage of this group's next tile
+  int n = 0;           // run-relative number of the segment's first tile
+  int mine = grp;      // of this group's next tile
+  bool first_segment = true;
+  while (n < n_tiles) {
+    // ---- a segment: the tiles of one unit in this run
+    const int seg = cur.tiles - cur.tile < n_tiles - n ? cur.tiles - cur.tile : n_tiles - n;
+    const int hk = cur.u / a.groups, r0 = (cur.u - hk * a.groups) * ROWS;
+    T* Qs = reinterpret_cast<T*>(sm + P::Q);
+    for (int e = tid; e < ROWS * CH; e += P::THREADS) {
+      const int r = e / CH, c = e - r * CH, t = (r0 + r) / a.G;
+      uint4 x = make_uint4(0, 0, 0, 0);
+      if (r0 + r < a.R && c * VE < dh)
+        x = *reinterpret_cast<const uint4*>((const T*)a.q + ((int64_t)cur.b * a.n_new + t) * a.q_stride + (hk * a.G + r0 + r - t * a.G) * dh + c * VE);
+      *reinterpret_cast<uint4*>(Qs + r * DHT + (B16 ? c ^ (r & 7) : c ^ ((r & 1) << 2)) * VE) = x;
+    }
+    __syncthreads();
+    // the sixteen rows of this warp as A operands (f32: dims 4 t .. 4 t + 3 of every sixteen, of which a step of eight takes
+    // two; K's are taken alike, and the sum over dims does not mind)
+    constexpr bool QREG = B16 || DHT <= 128;
+    uint32_t qf[QREG ? DHT / 16 : 1][B16 ? 4 : 8];
+    auto load_q = [&](int ks, uint32_t* f) {
+      if constexpr (B16) {
+        const int row = 16 * wm + (lane & 15), c = 2 * ks + (lane >> 4);
+        ldsm4(f, smem_addr(Qs + row * DHT + ((c ^ (row & 7)) * VE)));
+      } else {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int r = r0 + g + 8 * h, t = r / a.G;
-        const bool live = r < a.R;
-        qslot[h] = live ? cur.s.len - a.n_new + t : -1;
-        const bf16* q = (const bf16*)a.q + ((int64_t)cur.b * a.n_new + t) * a.q_stride + (hk * a.G + r - t * a.G) * dh;
+        for (int h = 0; h < 2; ++h) {
+          const int row = 16 * wm + g + 8 * h;
+          *reinterpret_cast<uint4*>(f + 4 * h) = *reinterpret_cast<const uint4*>(Qs + row * DHT + ((4 * ks + t4) ^ ((row & 1) << 2)) * VE);
+        }
+      }
+    };
+    if constexpr (QREG) {
+#pragma unroll
+      for (int ks = 0; ks < DHT / 16; ++ks) load_q(ks, qf[ks]);
+    }
+    int qslot[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int r = r0 + 16 * wm + g + 8 * h;
+      qslot[h] = r < a.R ? cur.s.len - a.n_new + r / a.G : -1;
+    }
+    float o[DHT / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+#pragma unroll
+    for (int d = 0; d < DHT / 8; ++d)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[d][e] = 0.f;
+
+    for (; mine < n + seg; mine += NG) {
+      cp_wait<S - 2>();
+      group_sync();  // this tile is there for the group's lanes, and they are done with the one before
+      const int free_st = st == 0 ? S - 1 : st - 1;
+      if (asked < n_tiles) copy(free_st);
+      cp_commit();
+      go_on();
+      const uint32_t base = smem_addr(ring + st * P::STAGE);
+      const int x0 = (cur.tile + mine - n) * TK;
+
+      // ---- scores
+      float s[NT][4] = {};
+      if constexpr (B16) {
+        const int rr = ((lane >> 4) << 3) + (lane & 7), half = (lane >> 3) & 1;
 #pragma unroll
         for (int ks = 0; ks < DHT / 16; ++ks)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int k = 16 * ks + 8 * e + t2;
-            qf[ks][h + 2 * e] = live && k < dh ? *reinterpret_cast<const uint32_t*>(q + k) : 0u;
+          for (int n2 = 0; n2 < NT / 2; ++n2) {
+            uint32_t kf[4];
+            const int row = 16 * n2 + rr;
+            ldsm4(kf, base + row * (DHT * 2) + (((2 * ks + half) ^ (row & 7)) << 4));
+            mma16816(s[2 * n2], qf[ks], kf[0], kf[1]);
+            mma16816(s[2 * n2 + 1], qf[ks], kf[2], kf[3]);
           }
-        m[h] = -INFINITY;
-        l[h] = 0.f;
-      }
+      } else {
 #pragma unroll
-      for (int n = 0; n < DHT / 8; ++n)
+        for (int ks = 0; ks < DHT / 16; ++ks) {
+          uint32_t q8[8];
+          if constexpr (!QREG) load_q(ks, q8);
+          const uint32_t* qr = QREG ? qf[QREG ? ks : 0] : q8;
+          uint32_t ah[2][4], al[2][4];  // the two steps of eight dims: rows g, g + 8 of dims (4 t, 4 t + 1), then (4 t + 2, 4 t + 3)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
-    }
-    cp_wait<S - 2>();
-    const int64_t nt = i + S - 1;  // the tile whose copies start now
-    if (nt < n_tiles) place(nt, ahead.u / a.groups);
-    __syncthreads();  // tile i is there for all; all are done with tile i - 1; rowoff is written
-    if (nt < n_tiles) {
-      copy(nt);
-      if (asked < n_tiles) step_ahead();
-    }
-    cp_commit();
-
-    // ---- scores of this warp's 16 tokens
-    const uint32_t st = ring + (uint32_t)(i % S) * P::STAGE;
-    float s[2][4] = {};
-    {
-      const int row = 16 * wt + ((lane >> 4) << 3) + (lane & 7), half = (lane >> 3) & 1;
-      const uint32_t base = st + row * (DHT * 2);
+          for (int k2 = 0; k2 < 2; ++k2)
 #pragma unroll
-      for (int ks = 0; ks < DHT / 16; ++ks) {
-        uint32_t kf[4];
-        ldsm4(kf, base + (((2 * ks + half) ^ (row & 7)) << 4));
-        mma16816(s[0], qf[ks], kf[0], kf[1]);
-        mma16816(s[1], qf[ks], kf[2], kf[3]);
-      }
-    }
-    const uint32_t live = mask[2 * (int)(i % (S + 1)) + (wt >> 1)] >> (16 * (wt & 1)) & 0xffffu;
-    const int x0 = cur.tile * TK + 16 * wt;
-    // every row sees all sixteen: no test a token
-    const int j0 = slot_of(cur.s, x0), j1 = slot_of(cur.s, x0 + 15), qmin = cur.s.len - a.n_new;
-    const bool all = live == 0xffffu && j1 <= qmin && (a.window == 0 || j1 < a.sinks || (x0 >= cur.s.n_sink && cur.s.len - 1 - j0 < a.window));
+            for (int e = 0; e < 4; ++e)
+              split_tf32(__uint_as_float(qr[4 * (e & 1) + 2 * k2 + (e >> 1)]), ah[k2][e], al[k2][e]);
 #pragma unroll
-    for (int n = 0; n < 2; ++n)
+          for (int nt = 0; nt < NT; ++nt) {
+            const int row = 8 * nt + g;
+            const float4 k = *reinterpret_cast<const float4*>(ring + st * P::STAGE + row * (DHT * 4) + (((4 * ks + t4) ^ ((row & 1) << 2)) << 4));
+            uint32_t bh[4], bl[4];
+            split_tf32(k.x, bh[0], bl[0]);
+            split_tf32(k.y, bh[1], bl[1]);
+            split_tf32(k.z, bh[2], bl[2]);
+            split_tf32(k.w, bh[3], bl[3]);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        s[n][e] *= a.sl2;
-        if (!all) {
-          const int k = 8 * n + t2 + (e & 1);
-          if (!((live >> k) & 1u) || !sees(a, qslot[e >> 1], slot_of(cur.s, x0 + k))) s[n][e] = -INFINITY;
+            for (int k2 = 0; k2 < 2; ++k2) {
+              mma1688(s[nt], al[k2], bh[2 * k2], bh[2 * k2 + 1]);
+              mma1688(s[nt], ah[k2], bl[2 * k2], bl[2 * k2 + 1]);
+              mma1688(s[nt], ah[k2], bh[2 * k2], bh[2 * k2 + 1]);
+            }
+          }
         }
       }
-    if (a.scores) {
-      const int hk = cur.u / a.groups, r0 = (cur.u - hk * a.groups) * P::ROWS + 16 * wg;
+      // every row sees every token of the tile: no test a token
+      const uint64_t live = mask[st];
+      const int j0 = slot_of(cur.s, x0), j1 = slot_of(cur.s, x0 + TK - 1);
+      const bool all = live == (TK == 64 ? ~0ull : (1ull << (TK & 63)) - 1) && j1 <= cur.s.len - a.n_new &&
+                       (a.window == 0 || j1 < a.sinks || (x0 >= cur.s.n_sink && cur.s.len - 1 - j0 < a.window));
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[nt][e] *= a.sl2;
+      if (!all) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int k = 8 * nt + 2 * t4 + (e & 1);
+            if (!((live >> k) & 1ull) || !sees(a, qslot[e >> 1], slot_of(cur.s, x0 + k))) s[nt][e] = -INFINITY;
+          }
+      }
+      if (a.scores) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int r = r0 + 16 * wm + g + 8 * h;
+          if (r < a.R) {
+            float* d = a.scores + (((int64_t)cur.b * a.c.n_kv_heads + hk) * a.R + r) * a.x_stride + x0 + 2 * t4;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) *reinterpret_cast<float2*>(d + 8 * nt) = make_float2(s[nt][2 * h], s[nt][2 * h + 1]);
+          }
+        }
+      }
+      // ---- running maximum and sum
+      float ms[2], mn[2];
+      bool grew = false;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int r = r0 + g + 8 * h;
-        if (r < a.R) {
-          float* d = a.scores + (((int64_t)cur.b * a.c.n_kv_heads + hk) * a.R + r) * a.x_stride + x0 + t2;
-          *reinterpret_cast<float2*>(d) = make_float2(s[0][2 * h], s[0][2 * h + 1]);
-          *reinterpret_cast<float2*>(d + 8) = make_float2(s[1][2 * h], s[1][2 * h + 1]);
+        float bm = fmaxf(s[0][2 * h], s[0][2 * h + 1]);
+#pragma unroll
+        for (int nt = 1; nt < NT; ++nt) bm = fmaxf(bm, fmaxf(s[nt][2 * h], s[nt][2 * h + 1]));
+        bm = fmaxf(bm, __shfl_xor_sync(0xffffffffu, bm, 1));
+        bm = fmaxf(bm, __shfl_xor_sync(0xffffffffu, bm, 2));
+        mn[h] = fmaxf(m[h], bm);
+        grew = grew || mn[h] > m[h];
+        ms[h] = mn[h] == -INFINITY ? 0.f : mn[h];
+      }
+      if (__any_sync(0xffffffffu, grew)) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float f = ex2_fast(m[h] - ms[h]);
+          l[h] *= f;
+          m[h] = mn[h];
+#pragma unroll
+          for (int d = 0; d < DHT / 8; ++d) {
+            o[d][2 * h] *= f;
+            o[d][2 * h + 1] *= f;
+          }
         }
       }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          s[nt][e] = ex2_fast(s[nt][e] - ms[e >> 1]);
+          l[e >> 1] += s[nt][e];
+        }
+      // ---- outputs
+      if constexpr (B16) {
+        // P as an A operand, in two bf16 terms: rounded to one it would add as much to the error as the output's own
+        // rounding does
+        const int rr = (((lane >> 3) & 1) << 3) + (lane & 7), half = lane >> 4;
+#pragma unroll
+        for (int n2 = 0; n2 < NT / 2; ++n2) {
+          uint32_t pf[4], pl[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float p0 = s[2 * n2 + (k >> 1)][2 * (k & 1)], p1 = s[2 * n2 + (k >> 1)][2 * (k & 1) + 1];
+            pf[k] = pack2(p0, p1);
+            const float2 hi = __bfloat1622float2(*reinterpret_cast<__nv_bfloat162*>(&pf[k]));
+            pl[k] = pack2(p0 - hi.x, p1 - hi.y);
+          }
+          const int row = 16 * n2 + rr;
+#pragma unroll
+          for (int nb = 0; nb < DHT / 16; ++nb) {
+            uint32_t vf[4];
+            ldsm4t(vf, base + P::TILE + row * (DHT * 2) + (((2 * nb + half) ^ (row & 7)) << 4));
+            mma16816(o[2 * nb], pf, vf[0], vf[1]);
+            mma16816(o[2 * nb + 1], pf, vf[2], vf[3]);
+            mma16816(o[2 * nb], pl, vf[0], vf[1]);
+            mma16816(o[2 * nb + 1], pl, vf[2], vf[3]);
+          }
+        }
+      } else {
+        // a step of eight tokens takes them in the order 0, 2, 4, 6, 1, 3, 5, 7: the scores' own layout
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          uint32_t ah[4], al[4];
+          split_tf32(s[nt][0], ah[0], al[0]);
+          split_tf32(s[nt][2], ah[1], al[1]);
+          split_tf32(s[nt][1], ah[2], al[2]);
+          split_tf32(s[nt][3], ah[3], al[3]);
+          const int v0 = 8 * nt + 2 * t4;
+          const float* V0 = reinterpret_cast<const float*>(ring + st * P::STAGE + P::TILE + v0 * (DHT * 4));
+          const float* V1 = V0 + DHT;
+#pragma unroll
+          for (int d = 0; d < DHT / 8; ++d) {
+            const int c = 2 * d + (g >> 2), w = g & 3;
+            uint32_t h0, l0, h1, l1;
+            split_tf32(V0[(c ^ (t4 << 1)) * 4 + w], h0, l0);
+            split_tf32(V1[(c ^ (t4 << 1)) * 4 + w], h1, l1);
+            mma1688(o[d], al, h0, h1);
+            mma1688(o[d], ah, l0, l1);
+            mma1688(o[d], ah, h0, h1);
+          }
+        }
+      }
+      st = st + 1 == S ? 0 : st + 1;
     }
-    // ---- running maximum and sum
-    float ms[2];
-    bool grew = false;
-    float mn[2];
+
+    // ---- the groups' outputs together: each puts its own into the stage that has no tile on its way
+    group_sync();
+    float* stage = reinterpret_cast<float*>(ring + (st == 0 ? S - 1 : st - 1) * P::STAGE);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      float bm = fmaxf(fmaxf(s[0][2 * h], s[0][2 * h + 1]), fmaxf(s[1][2 * h], s[1][2 * h + 1]));
-      bm = fmaxf(bm, __shfl_xor_sync(0xffffffffu, bm, 1));
-      bm = fmaxf(bm, __shfl_xor_sync(0xffffffffu, bm, 2));
-      mn[h] = fmaxf(m[h], bm);
-      grew = grew || mn[h] > m[h];
-      ms[h] = mn[h] == -INFINITY ? 0.f : mn[h];
+      l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
+      l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
+      const int row = 16 * wm + g + 8 * h;
+      if (t4 == 0) stats[grp * ROWS + row] = make_float2(m[h], l[h]);
+#pragma unroll
+      for (int d = 0; d < DHT / 8; ++d) *reinterpret_cast<float2*>(stage + P::at(row, 8 * d + 2 * t4)) = make_float2(o[d][2 * h], o[d][2 * h + 1]);
     }
-    if (__any_sync(0xffffffffu, grew)) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const float f = ex2_fast(m[h] - ms[h]);
-        l[h] *= f;
-        m[h] = mn[h];
-#pragma unroll
-        for (int n = 0; n < DHT / 8; ++n) {
-          o[n][2 * h] *= f;
-          o[n][2 * h + 1] *= f;
-        }
-      }
-    }
-    // P as an A operand (rows g, g + 8; tokens 2 t and 8 + 2 t), in two bf16 terms: rounded to one it would add as much to
-    // the error as the output's own rounding does
-    uint32_t pf[4], pl[4];
-#pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const float p0 = ex2_fast(s[n][2 * h] - ms[h]), p1 = ex2_fast(s[n][2 * h + 1] - ms[h]);
-        l[h] += p0 + p1;
-        pf[2 * n + h] = pack2(p0, p1);
-        const float2 hi = __bfloat1622float2(*reinterpret_cast<__nv_bfloat162*>(&pf[2 * n + h]));
-        pl[2 * n + h] = pack2(p0 - hi.x, p1 - hi.y);
-      }
-    // ---- outputs
-    {
-      const int row = 16 * wt + (((lane >> 3) & 1) << 3) + (lane & 7), half = lane >> 4;
-      const uint32_t base = st + P::TILE + row * (DHT * 2);
-#pragma unroll
-      for (int nb = 0; nb < DHT / 16; ++nb) {
-        uint32_t vf[4];
-        ldsm4t(vf, base + (((2 * nb + half) ^ (row & 7)) << 4));
-        mma16816(o[2 * nb], pf, vf[0], vf[1]);
-        mma16816(o[2 * nb + 1], pf, vf[2], vf[3]);
-        mma16816(o[2 * nb], pl, vf[0], vf[1]);
-        mma16816(o[2 * nb + 1], pl, vf[2], vf[3]);
-      }
-    }
-
-    const bool unit_ends = cur.tile + 1 == cur.tiles;
-    if (unit_ends || i + 1 == n_tiles) {
-      // ---- the four warps of a row group together, in the order ((0 + 2) + (1 + 3))
-      float* merge = reinterpret_cast<float*>(sm + (P::IN_STAGE ? (int)(i % S) : S) * P::STAGE);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
-        l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
-        if ((lane & 3) == 0) stats[wt * P::ROWS + 16 * wg + g + 8 * h] = make_float2(m[h], l[h]);
-      }
-      __syncthreads();
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float M = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) M = fmaxf(M, stats[w * P::ROWS + 16 * wg + g + 8 * h].x);
-        const float f = M == -INFINITY ? 0.f : ex2_fast(m[h] - M);
-#pragma unroll
-        for (int n = 0; n < DHT / 8; ++n) {
-          o[n][2 * h] *= f;
-          o[n][2 * h + 1] *= f;
-        }
-      }
-      auto put = [&](int buf) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int n = 0; n < DHT / 8; ++n)
-            *reinterpret_cast<float2*>(merge + P::at(buf, 16 * wg + g + 8 * h, 8 * n + t2)) =
-                make_float2(o[n][2 * h], o[n][2 * h + 1]);
-      };
-      auto add = [&](int buf) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int n = 0; n < DHT / 8; ++n) {
-            const float2 x = *reinterpret_cast<const float2*>(merge + P::at(buf, 16 * wg + g + 8 * h, 8 * n + t2));
-            o[n][2 * h] += x.x;
-            o[n][2 * h + 1] += x.y;
-          }
-      };
-      if (wt >= 2) put(wt - 2);
-      __syncthreads();
-      if (wt < 2) add(wt);
-      if (wt == 1) put(1);
-      __syncthreads();
-      if (wt == 0) {
-        add(1);
-        put(0);
-      }
-      __syncthreads();
-      const int hk = cur.u / a.groups, r0 = (cur.u - hk * a.groups) * P::ROWS;
-      const bool whole = seg_start == 0 && unit_ends;
-      const int64_t slot = 2 * (int64_t)blockIdx.x + (first_segment ? 0 : 1);
-      for (int e = tid; e < P::ROWS * (DHT / 4); e += P::THREADS) {
-        const int r = e / (DHT / 4), d = (e - r * (DHT / 4)) * 4;
-        if (r0 + r >= a.R || d >= dh) continue;
-        float M = -INFINITY, L = 0.f;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) M = fmaxf(M, stats[w * P::ROWS + r].x);
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const float2 x = stats[w * P::ROWS + r];
-          if (x.x != -INFINITY) L += x.y * ex2_fast(x.x - M);
-        }
-        float4 v = *reinterpret_cast<const float4*>(merge + P::at(0, r, d));
-        if (whole) {
-          const float f = M == -INFINITY ? 0.f : 1.f / L;
-          const int t = (r0 + r) / a.G, head = hk * a.G + r0 + r - t * a.G;
-          bf16* out = (bf16*)a.out + ((int64_t)cur.b * a.n_new + t) * a.out_stride + head * dh + d;
-          *reinterpret_cast<uint2*>(out) = make_uint2(pack2(v.x * f, v.y * f), pack2(v.z * f, v.w * f));
-          if (d == 0) {
-            const float lse2 = M == -INFINITY ? -INFINITY : M + log2f(L);
-            if (a.lse) a.lse[((int64_t)cur.b * a.n_new + t) * a.n_heads + head] = lse2 * kLn2;
-            if (a.scores) a.lse2[((int64_t)cur.b * a.c.n_kv_heads + hk) * a.R + r0 + r] = lse2;
-          }
-        } else {
-          *reinterpret_cast<float4*>(a.part_o + (slot * P::ROWS + r) * DHT + d) = v;
-          if (d == 0) a.part_ml[slot * P::ROWS + r] = make_float2(M, L);
-        }
-      }
-      __syncthreads();  // the merge space and the statistics are free again
-      first_segment = false;
-      first_tile_of_unit = true;
-    }
-    cur.next(a);
-  }
-  cp_wait<0>();
-}
-
-// ---------------------------------------------------------------------------------------
-// f32.  Tiles of 32 tokens, 128 threads, RM rows.  Scores: warp w's lanes on the tokens, rows w, w + 4, ...; outputs:
-// a thread a column (two at head dims above 128, half the rows each at 64).
-// ---------------------------------------------------------------------------------------
-constexpr int TKF = 32;
-template <int DHT, int RM>
-struct SimtPlan {
-  static constexpr int STAGES = DHT == 64 ? 6 : 3, DP = DHT + 4;  // (padded rows: lanes on tokens without conflicts)
-  static constexpr int TILE = TKF * DP * 4, STAGE = 2 * TILE, Q = STAGES * STAGE, X = Q + RM * DHT * 4,
-                       XP = TKF + 4, FAC = X + RM * XP * 4, STATS = FAC + RM * 4, ROWOFF = STATS + RM * 8 + 8,
-                       MASK = ROWOFF + 2 * TKF * 8, BYTES = MASK + (STAGES + 1) * 4;
-  static constexpr int CT = DHT > 128 ? DHT / 128 : 1, RG = DHT < 128 ? 128 / DHT : 1, RT = RM / RG;
-};
-
-template <int DHT, int RM>
-__global__ void __launch_bounds__(128) decode_simt_kernel(const __grid_constant__ DecodeArgs a) {
-  using P = SimtPlan<DHT, RM>;
-  constexpr int TK = TKF, S = P::STAGES, CH = DHT / 4, RW = RM / 4;
-  extern __shared__ __align__(128) uint8_t sm[];
-  pdl_wait();
-  pdl_trigger();
-  Cursor<TK> cur;
-  int64_t n_tiles;
-  if (!begin_run<TK>(a, cur, n_tiles)) return;
-  Cursor<TK> ahead = cur;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, dh = a.c.head_dim;
-  float *Q = reinterpret_cast<float*>(sm + P::Q), *X = reinterpret_cast<float*>(sm + P::X), *fac = reinterpret_cast<float*>(sm + P::FAC);
-  float2* stats = reinterpret_cast<float2*>(sm + P::STATS);
-  int64_t* rowoff = reinterpret_cast<int64_t*>(sm + P::ROWOFF);
-  uint32_t* mask = reinterpret_cast<uint32_t*>(sm + P::MASK);
-  const uint32_t ring = smem_addr(sm);
-  const float *Kp = (const float*)a.c.k_dev, *Vp = (const float*)a.c.v_dev;
-
-  RowPlan<TK> plan;
-  int64_t asked = 1;
-  if (tid < TK) plan.request(a, ahead, true);
-  auto place = [&](int64_t tile, int head) {
-    if (tid < TK) {
-      const int64_t r = plan.row(a, head);
-      rowoff[(tile & 1) * TK + tid] = r;
-      const uint32_t m = __ballot_sync(0xffffffffu, r >= 0);
-      if (lane == 0) mask[tile % (S + 1)] = m;
-    }
-  };
-  auto copy = [&](int64_t tile) {
-    const uint32_t st = ring + (uint32_t)(tile % S) * P::STAGE;
-#pragma unroll 4
-    for (int e = tid; e < TK * CH; e += 128) {
-      const int r = e / CH, col = e - r * CH;
-      const int64_t at = rowoff[(tile & 1) * TK + r];
-      const bool live = at >= 0 && col * 4 < dh;
-      const int64_t src = live ? at * dh + col * 4 : 0;
-      const uint32_t d = st + (r * P::DP + col * 4) * 4;
-      cp16(d, Kp + src, live);
-      cp16(d + P::TILE, Vp + src, live);
-    }
-  };
-  auto step_ahead = [&]() {
-    ahead.next(a);
-    if (tid < TK) plan.request(a, ahead, asked < n_tiles);
-    ++asked;
-  };
-#pragma unroll 1
-  for (int i = 0; i < S - 1; ++i) {
-    if (i < n_tiles) {
-      place(i, ahead.u / a.groups);
-      __syncthreads();
-      copy(i);
-      if (asked < n_tiles) step_ahead();
-    }
-    cp_commit();
-  }
-  const int c0 = DHT < 128 ? tid % DHT : tid, rg = DHT < 128 ? tid / DHT : 0;  // output columns c0 (+ 128), rows rg RT ...
-  float o[P::RT][P::CT], m[RW], l[RW];
-  bool first_tile_of_unit = true, first_segment = true;
-  int seg_start = cur.tile;
-  for (int64_t i = 0; i < n_tiles; ++i) {
-    const int hk = cur.u / a.groups, r0 = (cur.u - hk * a.groups) * RM;
-    if (first_tile_of_unit) {
-      first_tile_of_unit = false;
-      seg_start = cur.tile;
-      for (int e = tid; e < RM * DHT; e += 128) {
-        const int r = e / DHT, d = e - r * DHT, t = (r0 + r) / a.G;
-        Q[e] = r0 + r < a.R && d < dh
-                   ? ((const float*)a.q)[((int64_t)cur.b * a.n_new + t) * a.q_stride + (hk * a.G + r0 + r - t * a.G) * dh + d] : 0.f;
-      }
-#pragma unroll
-      for (int r = 0; r < P::RT; ++r)
-#pragma unroll
-        for (int c = 0; c < P::CT; ++c) o[r][c] = 0.f;
-#pragma unroll
-      for (int r = 0; r < RW; ++r) {
-        m[r] = -INFINITY;
-        l[r] = 0.f;
-      }
-    }
-    cp_wait<S - 2>();
-    const int64_t nt = i + S - 1;
-    if (nt < n_tiles) place(nt, ahead.u / a.groups);
+    // (the free stage of every group, for the sum)
+    __shared__ int free_stage[NG];
+    if (lane == 0 && wm == 0) free_stage[grp] = st == 0 ? S - 1 : st - 1;
     __syncthreads();
-    if (nt < n_tiles) {
-      copy(nt);
-      if (asked < n_tiles) step_ahead();
-    }
-    cp_commit();
-    const float* K = reinterpret_cast<const float*>(sm + (i % S) * P::STAGE);
-    const float* V = reinterpret_cast<const float*>(sm + (i % S) * P::STAGE + P::TILE);
-    float s[RW] = {};
-#pragma unroll 4
-    for (int d = 0; d < DHT; d += 4) {
-      const float4 k = *reinterpret_cast<const float4*>(K + lane * P::DP + d);
+    const bool whole = seg == cur.tiles;
+    const int64_t slot = 2 * (int64_t)blockIdx.x + (first_segment ? 0 : 1);
+    for (int e = tid; e < ROWS * (DHT / 4); e += P::THREADS) {
+      const int r = e / (DHT / 4), d = (e - r * (DHT / 4)) * 4;
+      if (r0 + r >= a.R || d >= dh) continue;
+      float M = -INFINITY, L = 0.f;
+      bool any = false;
 #pragma unroll
-      for (int r = 0; r < RW; ++r) {
-        const float4 q = *reinterpret_cast<const float4*>(Q + (warp + 4 * r) * DHT + d);
-        s[r] = fmaf(q.x, k.x, s[r]);
-        s[r] = fmaf(q.y, k.y, s[r]);
-        s[r] = fmaf(q.z, k.z, s[r]);
-        s[r] = fmaf(q.w, k.w, s[r]);
-      }
-    }
-    const int x = cur.tile * TK + lane, slot = slot_of(cur.s, x);
-    const bool live = mask[i % (S + 1)] >> lane & 1u;
+      for (int k = 0; k < NG; ++k) M = fmaxf(M, stats[k * ROWS + r].x);
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-    for (int r = 0; r < RW; ++r) {
-      const int row = r0 + warp + 4 * r, qs = row < a.R ? cur.s.len - a.n_new + row / a.G : -1;
-      s[r] = live && sees(a, qs, slot) ? s[r] * a.sl2 : -INFINITY;
-      if (a.scores && row < a.R) a.scores[(((int64_t)cur.b * a.c.n_kv_heads + hk) * a.R + row) * a.x_stride + x] = s[r];
-      const float mn = fmaxf(m[r], warp_max(s[r])), ms = mn == -INFINITY ? 0.f : mn;
-      const float p = exp2f(s[r] - ms), f = exp2f(m[r] - ms);
-      m[r] = mn;
-      l[r] = l[r] * f + p;  // a lane's share
-      X[(warp + 4 * r) * P::XP + lane] = p;
-      if (lane == 0) fac[warp + 4 * r] = f;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < P::RT; ++r) {
-      const float f = fac[rg * P::RT + r];
-#pragma unroll
-      for (int c = 0; c < P::CT; ++c) o[r][c] *= f;
-    }
-#pragma unroll 2
-    for (int k = 0; k < TK; k += 4) {
-      float v[4][P::CT];
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-#pragma unroll
-        for (int c = 0; c < P::CT; ++c) v[u][c] = V[(k + u) * P::DP + c0 + 128 * c];
-#pragma unroll
-      for (int r = 0; r < P::RT; ++r) {
-        const float4 p = *reinterpret_cast<const float4*>(X + (rg * P::RT + r) * P::XP + k);
-#pragma unroll
-        for (int c = 0; c < P::CT; ++c) {
-          o[r][c] = fmaf(p.x, v[0][c], o[r][c]);
-          o[r][c] = fmaf(p.y, v[1][c], o[r][c]);
-          o[r][c] = fmaf(p.z, v[2][c], o[r][c]);
-          o[r][c] = fmaf(p.w, v[3][c], o[r][c]);
+      for (int k = 0; k < NG; ++k) {
+        const float2 ml = stats[k * ROWS + r];
+        if (counts(ml)) {
+          const float f = ex2_fast(ml.x - M);
+          any = true;
+          L = fmaf(ml.y, f, L);
+          v = fma4(*reinterpret_cast<const float4*>(reinterpret_cast<const float*>(sm + k * P::RING + free_stage[k] * P::STAGE) + P::at(r, d)), f, v);
         }
       }
+      if (whole) {
+        finish<T>(a, cur.b, hk, r0 + r, d, v, M, L, any);
+      } else {
+        *reinterpret_cast<float4*>(a.part_o + (slot * ROWS + r) * DHT + d) = v;
+        if (d == 0) a.part_ml[slot * ROWS + r] = make_float2(M, any ? L : 0.f);
+      }
     }
-    const bool unit_ends = cur.tile + 1 == cur.tiles;
-    if (unit_ends || i + 1 == n_tiles) {
-#pragma unroll
-      for (int r = 0; r < RW; ++r) {
-        const float sum = warp_sum(l[r]);
-        if (lane == 0) stats[warp + 4 * r] = make_float2(m[r], sum);
+    if (!whole && a.join) {
+      // the last CTA to come here has all parts
+      __threadfence();
+      __syncthreads();
+      const int64_t first = run_start + n - cur.tile;  // the unit's first tile
+      const int c0 = (int)(((first + 1) * run_workers - 1) / run_total);
+      if (tid == 0) {
+        const int c1 = (int)(((first + cur.tiles) * run_workers - 1) / run_total);
+        unsigned* count = a.done + (int64_t)cur.b * (a.c.n_kv_heads * a.groups) + cur.u;
+        const unsigned before = atomicAdd(count, 1u);
+        joins = before == (unsigned)(c1 - c0) ? c1 - c0 + 1 : 0;
+        if (joins) *count = 0;
+        __threadfence();
       }
       __syncthreads();
-      const bool whole = seg_start == 0 && unit_ends;
-      const int64_t slot_ = 2 * (int64_t)blockIdx.x + (first_segment ? 0 : 1);
-#pragma unroll
-      for (int r = 0; r < P::RT; ++r) {
-        const int row = rg * P::RT + r;
-        if (r0 + row >= a.R) continue;
-        const float2 ml = stats[row];
-        const int t = (r0 + row) / a.G, head = hk * a.G + r0 + row - t * a.G;
-#pragma unroll
-        for (int c = 0; c < P::CT; ++c) {
-          const int d = c0 + 128 * c;
-          if (d >= dh) continue;
-          if (whole) {
-            ((float*)a.out)[((int64_t)cur.b * a.n_new + t) * a.out_stride + head * dh + d] = ml.x == -INFINITY ? 0.f : o[r][c] / ml.y;
-            if (d == 0) {
-              const float lse2 = ml.x == -INFINITY ? -INFINITY : ml.x + log2f(ml.y);
-              if (a.lse) a.lse[((int64_t)cur.b * a.n_new + t) * a.n_heads + head] = lse2 * kLn2;
-              if (a.scores) a.lse2[((int64_t)cur.b * a.c.n_kv_heads + hk) * a.R + r0 + row] = lse2;
+      const int parts = joins;
+      if (parts) {
+        // part p's slot: the first is its CTA's last segment, unless the unit starts that CTA's run
+        const bool starts = run_total * c0 / run_workers == first;
+        auto ml_of = [&](int p, int r) { return __ldcg(&a.part_ml[(2 * (int64_t)(c0 + p) + (p == 0 && !starts ? 1 : 0)) * ROWS + r]); };
+        const int rows = a.R - r0 < ROWS ? a.R - r0 : ROWS;
+        for (int e = tid; e < rows * (dh / 4); e += P::THREADS) {
+          const int r = e / (dh / 4), d = (e - r * (dh / 4)) * 4;
+          float M = -INFINITY, L = 0.f;
+          bool any = false;
+#pragma unroll 8
+          for (int p = 0; p < parts; ++p) M = fmaxf(M, ml_of(p, r).x);
+          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+          for (int p = 0; p < parts; ++p) {
+            const float2 ml = ml_of(p, r);
+            const float4 x = __ldcg(reinterpret_cast<const float4*>(a.part_o + ((2 * (int64_t)(c0 + p) + (p == 0 && !starts ? 1 : 0)) * ROWS + r) * DHT + d));
+            if (counts(ml)) {
+              const float f = ex2_fast(ml.x - M);
+              any = true;
+              L = fmaf(ml.y, f, L);
+              v = fma4(x, f, v);
             }
-          } else {
-            a.part_o[(slot_ * RM + row) * DHT + d] = o[r][c];
-            if (d == 0) a.part_ml[slot_ * RM + row] = ml;
           }
+          finish<T>(a, cur.b, hk, r0 + r, d, v, M, L, any);
         }
       }
-      __syncthreads();
-      first_segment = false;
-      first_tile_of_unit = true;
     }
-    cur.next(a);
+    __syncthreads();  // the stages, the statistics and Q's space are free again
+    first_segment = false;
+    n += seg;
+    cur.tile = 0;
+    if (n < n_tiles) cur.next_unit(a);
   }
   cp_wait<0>();
 }
 
 // ---------------------------------------------------------------------------------------
-// Joins the parts of one query row: a CTA a row; its 256 threads take the parts in turns of 1024 / DHT, each four
-// columns, and are added in a fixed order.  Rows of one part were written by the first kernel; sequences without a
-// token get their zeros here.
+// Joins the parts of one query row where there may be many: a CTA a row; its 256 threads take the parts in turns of
+// 1024 / DHT, four columns each, and are added in a fixed order.  What one CTA finished is left alone.
 // ---------------------------------------------------------------------------------------
-template <typename T, int DHT, int TK, int ROWS>
+template <typename T, int DHT, int TK, int NG, int ROWS>
 __global__ void __launch_bounds__(256) decode_join_kernel(const __grid_constant__ DecodeArgs a) {
   constexpr int TPP = DHT / 4, TURNS = 256 / TPP;
   __shared__ float4 red[256];
   __shared__ float L_part[TURNS];
-  __shared__ int64_t sh_first;
-  __shared__ int sh_c0, sh_c1, sh_tiles;
+  __shared__ int any_part[TURNS];
+  __shared__ int sh_starts, sh_c0, sh_parts;
   pdl_wait();
   pdl_trigger();
   const int tid = threadIdx.x;
@@ -744,83 +682,62 @@ __global__ void __launch_bounds__(256) decode_join_kernel(const __grid_constant_
   const int per_b = a.c.n_kv_heads * a.R, b = (int)(id / per_b), hk = (int)(id - (int64_t)b * per_b) / a.R, row = (int)(id % a.R);
   const int grp = row / ROWS, lr = row - grp * ROWS;
   if (tid < 32) {
-    Deal<TK> d;
+    Deal<TK, NG> d;
     d.count(a, tid);
     const int tiles = d.tiles(a, b);
+    if (tid == 0) sh_parts = 0;
     if (tiles > 0) {
       const int64_t first = d.first_of(a, b, hk * a.groups + grp, tid);
       if (tid == 0) {
         sh_c0 = d.owner(first);
-        sh_c1 = d.owner(first + tiles - 1);
-        sh_first = first - d.start(sh_c0);
+        sh_parts = d.owner(first + tiles - 1) - sh_c0 + 1;
+        sh_starts = first == d.start(sh_c0);
       }
     }
-    if (tid == 0) sh_tiles = tiles;
   }
   __syncthreads();
-  const int t = row / a.G, head = hk * a.G + row - t * a.G, dh = a.c.head_dim;
-  T* out = (T*)a.out + ((int64_t)b * a.n_new + t) * a.out_stride + head * dh;
-  if (sh_tiles == 0) {
-    for (int d = tid; d < dh; d += 256) out[d] = from_f<T>(0.f);
-    if (tid == 0) {
-      if (a.lse) a.lse[((int64_t)b * a.n_new + t) * a.n_heads + head] = -INFINITY;
-      if (a.scores) a.lse2[((int64_t)b * a.c.n_kv_heads + hk) * a.R + row] = -INFINITY;
-    }
-    return;
-  }
-  const int c0 = sh_c0, parts = sh_c1 - c0 + 1;
-  if (parts == 1) return;
-  // the first part is its CTA's last segment, unless the unit starts that CTA's run
-  auto slot = [&](int p) { return 2 * (int64_t)(c0 + p) + (p == 0 && sh_first != 0 ? 1 : 0); };
+  const int c0 = sh_c0, parts = sh_parts, dh = a.c.head_dim;
+  if (parts < 2) return;
+  auto slot = [&](int p) { return 2 * (int64_t)(c0 + p) + (p == 0 && !sh_starts ? 1 : 0); };
   float M = -INFINITY;
   for (int p = tid & 31; p < parts; p += 32) M = fmaxf(M, a.part_ml[slot(p) * ROWS + lr].x);
   M = warp_max(M);
   const int turn = tid / TPP, d = (tid - turn * TPP) * 4;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
   float L = 0.f;
-  if (M != -INFINITY) {
+  int any = 0;
 #pragma unroll 4
-    for (int p = turn; p < parts; p += TURNS) {
-      const float2 ml = a.part_ml[slot(p) * ROWS + lr];
-      const float4 x = d < dh ? *reinterpret_cast<const float4*>(a.part_o + (slot(p) * ROWS + lr) * DHT + d) : s;
-      const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
-      if (f > 0.f) {
-        s.x = fmaf(x.x, f, s.x);
-        s.y = fmaf(x.y, f, s.y);
-        s.z = fmaf(x.z, f, s.z);
-        s.w = fmaf(x.w, f, s.w);
-        L = fmaf(ml.y, f, L);
-      }
+  for (int p = turn; p < parts; p += TURNS) {
+    const float2 ml = a.part_ml[slot(p) * ROWS + lr];
+    const float4 x = d < dh ? *reinterpret_cast<const float4*>(a.part_o + (slot(p) * ROWS + lr) * DHT + d) : make_float4(0.f, 0.f, 0.f, 0.f);
+    if (counts(ml)) {
+      const float f = ex2_fast(ml.x - M);
+      any = 1;
+      L = fmaf(ml.y, f, L);
+      s = fma4(x, f, s);
     }
   }
   red[tid] = s;
-  if (d == 0) L_part[turn] = L;
+  if (d == 0) {
+    L_part[turn] = L;
+    any_part[turn] = any;
+  }
   __syncthreads();
   if (tid >= TPP || d >= dh) return;
   L = 0.f;
+  any = 0;
 #pragma unroll
-  for (int i = 0; i < TURNS; ++i) L += L_part[i];
+  for (int i = 0; i < TURNS; ++i) {
+    L += L_part[i];
+    any |= any_part[i];
+  }
 #pragma unroll
-  for (int i = 1; i < TURNS; ++i) {
-    const float4 x = red[i * TPP + tid];
-    s.x += x.x;
-    s.y += x.y;
-    s.z += x.z;
-    s.w += x.w;
-  }
-  const float f = M == -INFINITY ? 0.f : 1.f / L;
-  out[d] = from_f<T>(s.x * f);
-  out[d + 1] = from_f<T>(s.y * f);
-  out[d + 2] = from_f<T>(s.z * f);
-  out[d + 3] = from_f<T>(s.w * f);
-  if (d == 0) {
-    const float lse2 = M == -INFINITY ? -INFINITY : M + log2f(L);
-    if (a.lse) a.lse[((int64_t)b * a.n_new + t) * a.n_heads + head] = lse2 * kLn2;
-    if (a.scores) a.lse2[((int64_t)b * a.c.n_kv_heads + hk) * a.R + row] = lse2;
-  }
+  for (int i = 1; i < TURNS; ++i) s = fma4(red[i * TPP + tid], 1.f, s);
+  finish<T>(a, b, hk, row, d, s, M, L, any != 0);
 }
 
-// weights_out = weights_in + the rows' softmax weights, in row order: a thread a slot
+// weights_out = weights_in + the rows' softmax weights, in row order: a thread four slots, 256 apart
+constexpr int WROWS = 8;
 __global__ void __launch_bounds__(256) decode_weights_kernel(const __grid_constant__ DecodeArgs a, int chunks) {
   pdl_wait();
   pdl_trigger();
@@ -828,28 +745,42 @@ __global__ void __launch_bounds__(256) decode_weights_kernel(const __grid_consta
   const int b = (int)(unit / a.c.n_kv_heads);
   const Seen s = seen_of(a, b);
   const float* lse2 = a.lse2 + unit * a.R;
-  const float* sc = a.scores + unit * a.R * a.x_stride;
-  const int j0 = (int)(blockIdx.x - unit * chunks) * 1024;
+  const int j0 = (int)(blockIdx.x - unit * chunks) * 1024 + (int)threadIdx.x;
+  if (j0 >= s.len) return;
+  float w[4];
+  const float* sc[4];
+  bool on[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int j = j0 + 256 * i + (int)threadIdx.x;
-    if (j >= s.len) return;
-    float w = a.w_in ? a.w_in[unit * a.w_stride + j] : 0.f;
-    const int x = j < s.n_sink ? j : j >= s.w0 ? j - s.w0 + s.n_sink : -1;
-    if (x >= 0)
-      for (int r = 0; r < a.R; ++r) {
-        const float z = lse2[r];
-        if (z != -INFINITY) w += exp2f(sc[(int64_t)r * a.x_stride + x] - z);
-      }
-    a.w_out[unit * a.w_stride + j] = w;
+    const int j = j0 + 256 * i, x = j < s.n_sink ? j : j >= s.w0 ? j - s.w0 + s.n_sink : -1;
+    on[i] = j < s.len && x >= 0;
+    w[i] = j < s.len && a.w_in ? a.w_in[unit * a.w_stride + j] : 0.f;
+    sc[i] = a.scores + unit * a.R * a.x_stride + (on[i] ? x : 0);
   }
+  for (int r0 = 0; r0 < a.R; r0 += WROWS) {
+    float z[WROWS], v[WROWS][4];
+#pragma unroll
+    for (int r = 0; r < WROWS; ++r) {
+      z[r] = r0 + r < a.R ? lse2[r0 + r] : -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[r][i] = on[i] && r0 + r < a.R ? sc[i][(int64_t)(r0 + r) * a.x_stride] : -INFINITY;
+    }
+#pragma unroll
+    for (int r = 0; r < WROWS; ++r)
+      if (z[r] != -INFINITY)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] += ex2_fast(v[r][i] - z[r]);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (j0 + 256 * i < s.len) a.w_out[unit * a.w_stride + j0 + 256 * i] = w[i];
 }
 
 // ---- host ------------------------------------------------------------------------------
 struct DecodeLayout {
-  int rows, groups, dht, tk, grid, R;
+  int rows, groups, dht, grid, R, join;
   int64_t x_stride;
-  size_t ml, o, lse2, scores, bytes;
+  size_t done, ml, o, lse2, scores, bytes;
 };
 DecodeLayout layout_of(const ra_attention_decode_args& p) {
   DecodeLayout L;
@@ -858,12 +789,15 @@ DecodeLayout layout_of(const ra_attention_decode_args& p) {
   L.R = G * p.n_new;
   L.dht = p.cache.head_dim <= 64 ? 64 : p.cache.head_dim <= 128 ? 128 : 256;
   // rows that one pass over K and V serves: 16, 32 or 64 (bf16; 16 at head dims above 128, whose outputs fill the
-  // registers), 4 or 16 (f32)
-  L.rows = b16 ? (L.R <= 16 || L.dht == 256 ? 16 : L.R <= 32 ? 32 : 64) : (L.R <= 4 ? 4 : 16);
+  // registers), 16 (f32)
+  L.rows = !b16 || L.R <= 16 || L.dht == 256 ? 16 : L.R <= 32 ? 32 : 64;
   L.groups = (L.R + L.rows - 1) / L.rows;
-  L.tk = b16 ? TKB : TKF;
-  // CTAs that the SMs hold at once: by shared memory two of a plan up to 112 KB, one of a larger
-  L.grid = (L.dht == 256 || (b16 && L.rows == 64) ? 1 : 2) * device_sm_count();
+  L.grid = device_sm_count();
+  // A unit has about grid / units parts; the last CTA reads them all, alone on its SM (about 20 us a MB), while a kernel of
+  // its own takes about 3 us and has the GPU
+  const int64_t units = (int64_t)p.batch * p.cache.n_kv_heads * L.groups;
+  const int64_t parts = units > 0 ? L.grid / units + 2 : 0;
+  L.join = parts * (L.R < L.rows ? L.R : L.rows) * p.cache.head_dim * 4 <= 128 * 1024;
   L.x_stride = ((int64_t)call_max_len(p.cache, p.max_len) + 63) / 64 * 64;
   size_t at = 0;
   auto take = [&](size_t n) {
@@ -871,6 +805,7 @@ DecodeLayout layout_of(const ra_attention_decode_args& p) {
     at += (n + 255) / 256 * 256;
     return o;
   };
+  L.done = take((size_t)units * 4);
   L.ml = take((size_t)2 * L.grid * L.rows * 8);
   L.o = take((size_t)2 * L.grid * L.rows * L.dht * 4);
   L.lse2 = L.scores = 0;
@@ -883,38 +818,15 @@ DecodeLayout layout_of(const ra_attention_decode_args& p) {
   return L;
 }
 
-template <typename K>
-cudaError_t start(K* kernel, int smem, int threads, const DecodeArgs& a, cudaStream_t st) {
-  cudaError_t e = allow_smem(kernel, smem);
-  return e == cudaSuccess ? launch_pdl(kernel, dim3(a.grid), dim3(threads), (size_t)smem, st, a) : e;
-}
-template <int DHT>
-cudaError_t run_mma(const DecodeArgs& a, int rows, cudaStream_t st) {
-  const dim3 joins((unsigned)((int64_t)a.batch * a.c.n_kv_heads * a.R));
-  cudaError_t e;
-  if constexpr (DHT < 256) {
-    if (rows == 32) {
-      e = start(decode_mma_kernel<DHT, 2>, MmaPlan<DHT, 2>::BYTES, 256, a, st);
-      return e == cudaSuccess ? launch_pdl(decode_join_kernel<bf16, DHT, TKB, 32>, joins, dim3(256), 0, st, a) : e;
-    }
-    if (rows == 64) {
-      e = start(decode_mma_kernel<DHT, 4>, MmaPlan<DHT, 4>::BYTES, 512, a, st);
-      return e == cudaSuccess ? launch_pdl(decode_join_kernel<bf16, DHT, TKB, 64>, joins, dim3(256), 0, st, a) : e;
-    }
-  }
-  e = start(decode_mma_kernel<DHT, 1>, MmaPlan<DHT, 1>::BYTES, 128, a, st);
-  return e == cudaSuccess ? launch_pdl(decode_join_kernel<bf16, DHT, TKB, 16>, joins, dim3(256), 0, st, a) : e;
-}
-template <int DHT>
-cudaError_t run_simt(const DecodeArgs& a, int rows, cudaStream_t st) {
-  const dim3 joins((unsigned)((int64_t)a.batch * a.c.n_kv_heads * a.R));
-  cudaError_t e;
-  if (rows == 4) {
-    e = start(decode_simt_kernel<DHT, 4>, SimtPlan<DHT, 4>::BYTES, 128, a, st);
-    return e == cudaSuccess ? launch_pdl(decode_join_kernel<float, DHT, TKF, 4>, joins, dim3(256), 0, st, a) : e;
-  }
-  e = start(decode_simt_kernel<DHT, 16>, SimtPlan<DHT, 16>::BYTES, 128, a, st);
-  return e == cudaSuccess ? launch_pdl(decode_join_kernel<float, DHT, TKF, 16>, joins, dim3(256), 0, st, a) : e;
+template <typename T, int DHT, int WM>
+cudaError_t launch(const DecodeArgs& a, cudaStream_t st) {
+  using P = Plan<T, DHT, WM>;
+  cudaError_t e = allow_smem(decode_kernel<T, DHT, WM>, P::BYTES);
+  if (e == cudaSuccess) e = launch_pdl(decode_kernel<T, DHT, WM>, dim3(a.grid), dim3(P::THREADS), (size_t)P::BYTES, st, a);
+  note_launch(1);
+  if (e != cudaSuccess || a.join) return e;
+  note_launch(1);
+  return launch_pdl(decode_join_kernel<T, DHT, P::TK, P::NG, P::ROWS>, dim3((unsigned)((int64_t)a.batch * a.c.n_kv_heads * a.R)), dim3(256), 0, st, a);
 }
 
 }  // namespace
@@ -935,6 +847,7 @@ cudaError_t attention_decode(const ra_attention_decode_args& p, cudaStream_t st)
   a.w_in = p.weights_in_dev;
   a.w_out = p.weights_out_dev;
   a.w_stride = p.weights_stride;
+  a.done = (unsigned*)(ws + L.done);
   a.part_ml = (float2*)(ws + L.ml);
   a.part_o = (float*)(ws + L.o);
   a.lse2 = p.weights_out_dev ? (float*)(ws + L.lse2) : nullptr;
@@ -950,13 +863,17 @@ cudaError_t attention_decode(const ra_attention_decode_args& p, cudaStream_t st)
   a.window = p.window;
   a.sinks = p.sinks;
   a.grid = L.grid;
+  a.join = L.join;
   a.sl2 = p.scale * kLog2e;
   cudaError_t e;
-  if (p.cache.dtype == RA_BF16)
-    e = L.dht == 64 ? run_mma<64>(a, L.rows, st) : L.dht == 128 ? run_mma<128>(a, L.rows, st) : run_mma<256>(a, L.rows, st);
+  if (p.cache.dtype == RA_F32)
+    e = L.dht == 64 ? launch<float, 64, 1>(a, st) : L.dht == 128 ? launch<float, 128, 1>(a, st) : launch<float, 256, 1>(a, st);
+  else if (L.dht == 64)
+    e = L.rows == 16 ? launch<bf16, 64, 1>(a, st) : L.rows == 32 ? launch<bf16, 64, 2>(a, st) : launch<bf16, 64, 4>(a, st);
+  else if (L.dht == 128)
+    e = L.rows == 16 ? launch<bf16, 128, 1>(a, st) : L.rows == 32 ? launch<bf16, 128, 2>(a, st) : launch<bf16, 128, 4>(a, st);
   else
-    e = L.dht == 64 ? run_simt<64>(a, L.rows, st) : L.dht == 128 ? run_simt<128>(a, L.rows, st) : run_simt<256>(a, L.rows, st);
-  note_launch(2);
+    e = launch<bf16, 256, 1>(a, st);
   if (e != cudaSuccess || !a.scores) return e;
   const int chunks = (a.max_len + 1023) / 1024;
   const int64_t n = (int64_t)chunks * a.batch * a.c.n_kv_heads;

@@ -10,10 +10,12 @@ namespace ra {
 namespace {
 
 // ---------------------------------------------------------------------------------------
-// Append.  A thread turns VE pairs (i, i + head_dim / 2) of one row of one token: a row of q goes to q_out, one
-// of k or v to its page.  Bound by memory: every value is read once and written once, the table's row by all
-// heads of its token (from L1).
+// Append.  A thread turns VE pairs (i, i + head_dim / 2) of one row (a head's query, key or value) of TOK tokens: a row
+// of q goes to q_out, one of k or v to its page.  Bound by memory: every value is read once and written once, the
+// table's row by all heads of its token (from L1).  The values of all TOK tokens are requested before the tokens' slots
+// are known, which one thread a token looks up.
 // ---------------------------------------------------------------------------------------
+constexpr int TOK = 4;
 template <typename T, int VE>
 __device__ __forceinline__ void load_pack(T* dst, const T* src) {
   typedef typename std::conditional<sizeof(T) * VE == 16, uint4, uint2>::type V;
@@ -26,77 +28,97 @@ __device__ __forceinline__ void store_pack(T* dst, const T* src) {
 }
 
 template <typename T, int VE>
-__global__ void __launch_bounds__(256) kv_append_kernel(const __grid_constant__ ra_kv_append_args a, int tokens_per_block) {
+__global__ void __launch_bounds__(256) kv_append_kernel(const __grid_constant__ ra_kv_append_args a) {
+  struct Token {
+    int64_t row;  // of key-value head 0 in the pools; the heads are page_size rows apart
+    int pos;
+    bool live, stored;
+  };
+  __shared__ Token info[TOK];
   pdl_wait();
   pdl_trigger();
   const ra_kv_cache& c = a.cache;
   const int half = c.head_dim / 2, chunks = half / VE, hq = a.q_dev ? a.n_heads : 0;
-  const int items = (hq + 2 * c.n_kv_heads) * chunks;
-  const int sub = threadIdx.x / items, item0 = sub < tokens_per_block ? threadIdx.x - sub * items : items;
-  if (tokens_per_block > 1 && sub >= tokens_per_block) return;
-  const int64_t tokens = (int64_t)a.batch * a.n_new;
-  const int cap = (int)((int64_t)c.max_pages * c.page_size);
-  const T *qp = (const T*)a.q_dev, *kp = (const T*)a.k_dev, *vp = (const T*)a.v_dev;
-  for (int64_t tok = (int64_t)blockIdx.x * tokens_per_block + (tokens_per_block > 1 ? sub : 0); tok < tokens;
-       tok += (int64_t)gridDim.x * tokens_per_block) {
-    const int b = (int)(tok / a.n_new), t = (int)(tok - (int64_t)b * a.n_new);
-    for (int item = tokens_per_block > 1 ? item0 : (int)threadIdx.x; item < items; item += blockDim.x) {
+  const int items = (hq + 2 * c.n_kv_heads) * chunks, t0 = blockIdx.x * TOK;
+  const int n = a.n_new - t0 < TOK ? a.n_new - t0 : TOK;
+  for (int b = blockIdx.y; b < a.batch; b += gridDim.y) {
+    const int64_t tok0 = (int64_t)b * a.n_new + t0;
+    bool known = false;
+    for (int item = threadIdx.x; item < items || !known; item += 256) {
+      const bool mine = item < items;
       const int row = item / chunks, i = (item - row * chunks) * VE;
       const bool is_q = row < hq, is_k = !is_q && row < hq + c.n_kv_heads;
       const int head = is_q ? row : is_k ? row - hq : row - hq - c.n_kv_heads;
-      const T* src = (is_q ? qp + tok * a.q_stride : is_k ? kp + tok * a.k_stride : vp + tok * a.v_stride) +
-                     (int64_t)head * c.head_dim + i;
-      __align__(16) T lo[VE], hi[VE];
-      load_pack<T, VE>(lo, src);
-      load_pack<T, VE>(hi, src + half);
-      const int len = clamp_len(a.lens_dev[b], cap, c.err_dev);
-      const int slot = len - a.n_new + t;
-      if (a.rope_dev && (is_q || is_k)) {
-        int p = (a.pos_dev ? a.pos_dev[b] : len) - a.n_new + t;
-        if (p < 0 || p >= a.rope_len) {
-          if (slot >= 0) set_dev_error(c.err_dev, RA_DEVERR_BOUNDS);
-          p = p < 0 ? 0 : a.rope_len - 1;
-        }
-        const float* w = a.rope_dev + (int64_t)p * c.head_dim + i;
-        __align__(16) float cs[VE], sn[VE];
+      const int64_t stride = is_q ? a.q_stride : is_k ? a.k_stride : a.v_stride;
+      const T* src = (const T*)(is_q ? a.q_dev : is_k ? a.k_dev : a.v_dev) + tok0 * stride + (int64_t)head * c.head_dim + i;
+      __align__(16) T lo[TOK][VE], hi[TOK][VE];
 #pragma unroll
-        for (int e = 0; e < VE; e += VE < 4 ? VE : 4) {
-          load_pack<float, VE < 4 ? VE : 4>(cs + e, w + e);
-          load_pack<float, VE < 4 ? VE : 4>(sn + e, w + half + e);
+      for (int t = 0; t < TOK; ++t)
+        if (mine && t < n) {
+          load_pack<T, VE>(lo[t], src + t * stride);
+          load_pack<T, VE>(hi[t], src + t * stride + half);
         }
-#pragma unroll
-        for (int e = 0; e < VE; ++e) {
-          const float x = to_f(lo[e]), y = to_f(hi[e]);
-          lo[e] = from_f<T>(x * cs[e] - y * sn[e]);
-          hi[e] = from_f<T>(y * cs[e] + x * sn[e]);
+      if (!known) {
+        known = true;
+        __syncthreads();  // (the sequence before is done with info)
+        if ((int)threadIdx.x < n) {
+          const int cap = (int)((int64_t)c.max_pages * c.page_size), len = clamp_len(a.lens_dev[b], cap, c.err_dev);
+          const int slot = len - a.n_new + t0 + (int)threadIdx.x;
+          Token x;
+          x.live = slot >= 0;
+          x.row = x.live ? slot_row(c, b, slot, 0) : -1;
+          x.stored = x.row >= 0;
+          x.pos = (a.pos_dev ? a.pos_dev[b] : len) - a.n_new + t0 + (int)threadIdx.x;
+          if (a.rope_dev && (x.pos < 0 || x.pos >= a.rope_len)) {
+            if (x.live) set_dev_error(c.err_dev, RA_DEVERR_BOUNDS);
+            x.pos = x.pos < 0 ? 0 : a.rope_len - 1;
+          }
+          info[threadIdx.x] = x;
         }
+        __syncthreads();
       }
-      T* dst;
-      if (is_q) {
-        dst = (T*)a.q_out_dev + tok * a.q_out_stride + (int64_t)head * c.head_dim + i;
-        if (slot < 0) {
+      if (!mine) break;
 #pragma unroll
-          for (int e = 0; e < VE; ++e) lo[e] = hi[e] = from_f<T>(0.f);
+      for (int t = 0; t < TOK; ++t) {
+        if (t >= n) break;
+        const Token x = info[t];
+        if (a.rope_dev && (is_q || is_k)) {
+          const float* w = a.rope_dev + (int64_t)x.pos * c.head_dim + i;
+          __align__(16) float cs[VE], sn[VE];
+#pragma unroll
+          for (int e = 0; e < VE; e += VE < 4 ? VE : 4) {
+            load_pack<float, VE < 4 ? VE : 4>(cs + e, w + e);
+            load_pack<float, VE < 4 ? VE : 4>(sn + e, w + half + e);
+          }
+#pragma unroll
+          for (int e = 0; e < VE; ++e) {
+            const float u = to_f(lo[t][e]), v = to_f(hi[t][e]);
+            lo[t][e] = from_f<T>(u * cs[e] - v * sn[e]);
+            hi[t][e] = from_f<T>(v * cs[e] + u * sn[e]);
+          }
         }
-      } else {
-        if (slot < 0) continue;
-        const int64_t at = slot_row(c, b, slot, head);
-        if (at < 0) continue;
-        dst = (T*)(is_k ? c.k_dev : c.v_dev) + at * c.head_dim + i;
+        T* dst;
+        if (is_q) {
+          dst = (T*)a.q_out_dev + (tok0 + t) * a.q_out_stride + (int64_t)head * c.head_dim + i;
+          if (!x.live) {
+#pragma unroll
+            for (int e = 0; e < VE; ++e) lo[t][e] = hi[t][e] = from_f<T>(0.f);
+          }
+        } else {
+          if (!x.stored) continue;
+          dst = (T*)(is_k ? c.k_dev : c.v_dev) + (x.row + (int64_t)head * c.page_size) * c.head_dim + i;
+        }
+        store_pack<T, VE>(dst, lo[t]);
+        store_pack<T, VE>(dst + half, hi[t]);
       }
-      store_pack<T, VE>(dst, lo);
-      store_pack<T, VE>(dst + half, hi);
     }
   }
 }
 
 template <typename T, int VE>
 cudaError_t launch_append(const ra_kv_append_args& a, cudaStream_t st) {
-  const int items = ((a.q_dev ? a.n_heads : 0) + 2 * a.cache.n_kv_heads) * (a.cache.head_dim / 2 / VE);
-  const int per = items < 256 ? 256 / items : 1;
-  const int64_t blocks = ((int64_t)a.batch * a.n_new + per - 1) / per;
-  const int64_t most = 8LL * 8 * device_sm_count();  // eight blocks of 256 threads an SM, eight rounds
-  cudaError_t e = launch_pdl(kv_append_kernel<T, VE>, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, st, a, per);
+  const dim3 grid((unsigned)((a.n_new + TOK - 1) / TOK), (unsigned)(a.batch < 65535 ? a.batch : 65535));
+  cudaError_t e = launch_pdl(kv_append_kernel<T, VE>, grid, dim3(256), 0, st, a);
   note_launch(1);
   return e;
 }
@@ -117,6 +139,7 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+template <bool IN_SMEM>
 __global__ void __launch_bounds__(SEL_THREADS) evict_select_kernel(const __grid_constant__ ra_kv_evict_args a, int max_len) {
   extern __shared__ uint32_t keys[];
   __shared__ uint32_t hist[SEL_BINS];
@@ -145,10 +168,11 @@ __global__ void __launch_bounds__(SEL_THREADS) evict_select_kernel(const __grid_
     return;
   }
   const int m0 = a.first, m1 = n - a.recent;  // the middle
-  const bool in_smem = n <= SEL_KEYS;
-  if (in_smem)
+  if (IN_SMEM) {
+#pragma unroll 8
     for (int i = tid; i < n; i += SEL_THREADS) keys[i] = weight_key(w[i]);
-  auto key_at = [&](int i) { return in_smem ? keys[i] : weight_key(w[i]); };
+  }
+  auto key_at = [&](int i) { return IN_SMEM ? keys[i] : weight_key(w[i]); };
   uint32_t left = (uint32_t)(a.budget - a.first - a.recent);  // how many of the middle stay
   uint32_t prefix = 0xffffffffu;  // (left == 0: nothing is larger)
   if (left > 0) {
@@ -159,6 +183,7 @@ __global__ void __launch_bounds__(SEL_THREADS) evict_select_kernel(const __grid_
       const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048;
       for (int i = tid; i < SEL_BINS; i += SEL_THREADS) hist[i] = 0;
       __syncthreads();
+#pragma unroll 4
       for (int i = m0 + tid; i < m1; i += SEL_THREADS) {
         const uint32_t k = key_at(i);
         if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1u);
@@ -188,12 +213,13 @@ __global__ void __launch_bounds__(SEL_THREADS) evict_select_kernel(const __grid_
       mask |= (uint32_t)(bins - 1) << shift;
       left = found_left;  // how many of the keys with this digit (at last: of the keys equal to it) stay
     }
-  } else if (in_smem) {
+  } else if (IN_SMEM) {
     __syncthreads();
   }
   const uint32_t edge = prefix, equal_stay = left;
   const int seg = ((n + SEL_WARPS - 1) / SEL_WARPS + 31) / 32 * 32, s0 = warp * seg, s1 = s0 + seg < n ? s0 + seg : n;
   uint32_t gt = 0, eq = 0;
+#pragma unroll 4
   for (int i = s0 + lane; i < s1; i += 32) {
     const bool always = i < m0 || i >= m1;
     const uint32_t k = key_at(i);
@@ -212,6 +238,7 @@ __global__ void __launch_bounds__(SEL_THREADS) evict_select_kernel(const __grid_
     gt0 += warp_sum[i];
     eq0 += warp_eq[i];
   }
+#pragma unroll 4
   for (int base = s0; base < s1; base += 32) {
     const int i = base + lane;
     const bool live = i < s1, always = live && (i < m0 || i >= m1);
@@ -282,11 +309,15 @@ cudaError_t kv_append(const ra_kv_append_args& a, cudaStream_t st) {
 cudaError_t kv_evict(const ra_kv_evict_args& a, cudaStream_t st) {
   const int max_len = call_max_len(a.src, a.max_len);
   const int64_t units = (int64_t)a.batch * a.src.n_kv_heads;
-  cudaError_t e = allow_smem(evict_select_kernel, SEL_KEYS * 4);
-  if (e != cudaSuccess) return e;
   // (the keys' space goes by the longest sequence that can come, so that short ones leave room for more CTAs)
-  const size_t smem = 4 * (size_t)(max_len < SEL_KEYS ? max_len : SEL_KEYS);
-  e = launch_pdl(evict_select_kernel, dim3((unsigned)units), dim3(SEL_THREADS), smem, st, a, max_len);
+  cudaError_t e;
+  if (max_len <= SEL_KEYS) {
+    e = allow_smem(evict_select_kernel<true>, SEL_KEYS * 4);
+    if (e == cudaSuccess)
+      e = launch_pdl(evict_select_kernel<true>, dim3((unsigned)units), dim3(SEL_THREADS), 4 * (size_t)max_len, st, a, max_len);
+  } else {
+    e = launch_pdl(evict_select_kernel<false>, dim3((unsigned)units), dim3(SEL_THREADS), 0, st, a, max_len);
+  }
   if (e != cudaSuccess) return e;
   const int cpr = a.src.head_dim * (a.src.dtype == RA_BF16 ? 2 : 4) / 16, rows = 256 / cpr * MOVE;
   const int per_unit = (a.budget + rows - 1) / rows;

@@ -16,7 +16,7 @@
 namespace ra {
 namespace {
 
-constexpr int VT = 512;  // threads
+constexpr int VT = 512, UN = 8;  // threads; tokens a thread has on their way
 
 // larger score first, then the lower token: a maximum of these is the answer
 __device__ __forceinline__ unsigned long long packed(float score, uint32_t v) {
@@ -24,20 +24,35 @@ __device__ __forceinline__ unsigned long long packed(float score, uint32_t v) {
 }
 __device__ __forceinline__ unsigned long long max64(unsigned long long a, unsigned long long b) { return a > b ? a : b; }
 
-// the largest r / e of tokens [v0, v1), from every thread
+// The largest r / e of tokens [v0, v1), from every thread.  Each thread has UN tokens on their way at once; `ready`: the
+// noise of the first UN is in e.  The quotient is computed where it can be the largest yet (the test before it is wide by
+// more than its own rounding).
 template <typename T, bool DIFF>
 __device__ unsigned long long race(const T* __restrict__ p, const T* __restrict__ q, const float* __restrict__ noise,
-                                   int v0, int v1) {
+                                   int v0, int v1, float (&e)[UN], bool ready) {
   unsigned long long best = packed(0.f, (uint32_t)v0);
   float top = 0.f;
-#pragma unroll 4
-  for (int v = v0 + (int)threadIdx.x; v < v1; v += VT) {
-    float r = fmaxf(to_f(p[v]), 0.f);
-    if (DIFF) r = fmaxf(r - fmaxf(to_f(q[v]), 0.f), 0.f);
-    const float s = fmaxf(__fdiv_rn(r, noise[v]), 0.f);  // (a NaN, of 0 / 0 too, counts as 0)
-    if (s > top) {  // a thread's tokens rise: of equal ones the first stays
-      top = s;
-      best = packed(s, (uint32_t)v);
+  for (int base = v0 + (int)threadIdx.x; base < v1; base += VT * UN) {
+    float r[UN], d[UN];
+#pragma unroll
+    for (int i = 0; i < UN; ++i) {
+      const int v = base + VT * i;
+      r[i] = v < v1 ? to_f(p[v]) : 0.f;
+      d[i] = DIFF && v < v1 ? to_f(q[v]) : 0.f;
+      if (!ready) e[i] = v < v1 ? noise[v] : 1.f;
+    }
+    ready = false;
+#pragma unroll
+    for (int i = 0; i < UN; ++i) {
+      float x = fmaxf(r[i], 0.f);  // (a NaN counts as 0)
+      if (DIFF) x = fmaxf(x - fmaxf(d[i], 0.f), 0.f);
+      if (x > top * e[i] * 0.999999f) {
+        const float s = fmaxf(__fdiv_rn(x, e[i]), 0.f);
+        if (s > top) {  // a thread's tokens rise: of equal ones the first stays
+          top = s;
+          best = packed(s, (uint32_t)(base + VT * i));
+        }
+      }
     }
   }
 #pragma unroll
@@ -65,6 +80,12 @@ __global__ void __launch_bounds__(VT) verify_draft_kernel(const __grid_constant_
   const int K = a.n_draft, V = a.vocab;
   int nd = a.n_drafted_dev ? a.n_drafted_dev[b] : K;
   nd = nd < 0 ? 0 : nd > K ? K : nd;
+  // the noise does not wait for n
+  const float* noise = a.noise_dev + (int64_t)b * V;
+  const int v0 = part * per_part, v1 = v0 + per_part < V ? v0 + per_part : V;
+  float e[UN];
+#pragma unroll
+  for (int i = 0; i < UN; ++i) e[i] = v0 + VT * i + tid < v1 ? noise[v0 + VT * i + tid] : 1.f;
   const T* target = (const T*)a.target_dev + (int64_t)b * (K + 1) * a.target_stride;
   const T* draft = (const T*)a.draft_dev + (int64_t)b * K * a.draft_stride;
   // every warp finds n: the first drafted token that does not stand
@@ -89,9 +110,7 @@ __global__ void __launch_bounds__(VT) verify_draft_kernel(const __grid_constant_
   }
   const T* p = target + (int64_t)n * a.target_stride;
   const T* q = draft + (int64_t)n * a.draft_stride;
-  const float* noise = a.noise_dev + (int64_t)b * V;
-  const int v0 = part * per_part, v1 = v0 + per_part < V ? v0 + per_part : V;
-  unsigned long long best = n < nd ? race<T, true>(p, q, noise, v0, v1) : race<T, false>(p, q, noise, v0, v1);
+  unsigned long long best = n < nd ? race<T, true>(p, q, noise, v0, v1, e, true) : race<T, false>(p, q, noise, v0, v1, e, true);
   if (parts > 1) {
     VerifySlot* slot = (VerifySlot*)a.workspace_dev + b;
     __shared__ bool last;
@@ -110,7 +129,7 @@ __global__ void __launch_bounds__(VT) verify_draft_kernel(const __grid_constant_
     if (!last) return;
     best = all;
   }
-  if (n < nd && (best >> 32) == 0) best = race<T, false>(p, q, noise, 0, V);  // p is nowhere above q
+  if (n < nd && (best >> 32) == 0) best = race<T, false>(p, q, noise, 0, V, e, false);  // p is nowhere above q
   const int32_t next = (int32_t)(0xffffffffu - (uint32_t)best);
   if (tid == 0) a.accepted_dev[b] = n;
   for (int i = tid; i <= K; i += VT)
