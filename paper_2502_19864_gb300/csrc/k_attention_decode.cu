@@ -5,19 +5,22 @@
 // The query rows of a key-value head are its group's heads times the new tokens (R rows, a few to a few dozen); K and
 // V are read once for all of them, 4 R head_dim flops for every 2 head_dim values: bound by memory.  The slots that
 // any row sees (all, or the sinks and the windows) are numbered 0, 1, ... and cut into tiles of TK; the tiles of all
-// sequences and heads, one after the other, are dealt to the CTAs in equal runs, whatever the lengths are.  A CTA's warps
-// (or groups of 2 or 4 that split more than sixteen rows) take the tiles of its run in turn, each with a ring of its own
-// for tiles on their way (cp.async: a page may end anywhere) and its own running maximum m, sum l and outputs; nothing
-// but the end of a (sequence, head) makes warps wait for one another.  There the CTA adds up its warps; where its run
-// covers a part of the head's tiles only, (m, l, o) go to the workspace, and the last CTA to leave its part (a counter;
-// the order of the sum is the parts', not theirs) joins them.
+// sequences and heads, one after the other, are dealt to the CTAs in equal runs, whatever the lengths are.  Two warps of a
+// CTA look up pages and copy tiles, in turn, into a ring; the others (or groups of 2 or 4 that split more than sixteen rows) take
+// the tiles in turn, each with its own running maximum m, sum l and outputs; nothing but the end of a (sequence, head)
+// makes them wait for one another.  There the CTA adds them up; where its run covers a part of the head's tiles only,
+// (m, l, o) go to the workspace, and the last CTA to leave its part (a counter; the order of the sum is the parts', not
+// theirs) joins them.
 //   bf16: the products are mma.sync m16n8k16: sixteen rows take the tensor instruction of one, and the rate asked of
 //         it, 16 flops a byte of K and V, is a tenth of what it gives, so nothing is won by tcgen05's 128 rows.
 //   f32:  mma.sync m16n8k8 on tf32, each operand in two terms of 11 bits and their products but for the smallest: about
 //         2^-22 of a product, as good as the fp32 sums around it.
+#include <cstring>
+
 #include "common.cuh"
 #include "operators.h"
 #include "paged.cuh"
+#include "window_tc.cuh"
 
 namespace ra {
 namespace {
@@ -41,27 +44,37 @@ struct DecodeArgs {
   float* scores;                 // [batch, kv heads, R, x_stride], scaled, in powers of two
   int64_t x_stride;
   int batch, n_new, n_heads, G, R, groups, max_len, window, sinks, grid;
+  int page_shift;                // pages of 2^page_shift tokens, or -1
+  int brs, whole_rows;           // the tensor maps' boxes: 2^brs rows; whole rows of the head, or 128 bytes of them
   int join;                      // the last CTA of a unit joins its parts (else a kernel of its own)
   float sl2;                     // scale log2 e
 };
 
-// The slots that a call's new tokens see of a sequence: [0, n_sink) and [w0, len), as n numbers
+// What a call's new tokens see of a sequence: slots [0, n_sink) and [w0, len), in tiles of TK slots: sink_tiles from the
+// first, the others from tile w_tile on
 struct Seen {
-  int len, w0, n_sink, n;
+  int len, w0, n_sink, sink_tiles, w_tile, tiles;
 };
+template <int TK>
 __device__ __forceinline__ Seen seen_of(const DecodeArgs& a, int b) {
   Seen s;
-  s.len = clamp_len(a.lens[b], a.max_len, a.c.err_dev);
+  s.len = clamp_len(__ldg(a.lens + b), a.max_len, a.c.err_dev);
   s.w0 = 0;
   if (a.window > 0) {
     const int64_t w0 = (int64_t)s.len - a.n_new - a.window + 1;  // the first new token's window
     s.w0 = w0 > 0 ? (int)w0 : 0;
   }
   s.n_sink = a.sinks < s.w0 ? a.sinks : s.w0;
-  s.n = s.n_sink + s.len - s.w0;
+  s.w_tile = s.w0 / TK;
+  s.sink_tiles = (s.n_sink + TK - 1) / TK;
+  if (s.sink_tiles > s.w_tile) s.sink_tiles = s.w_tile;
+  s.tiles = s.len > 0 ? s.sink_tiles + (s.len + TK - 1) / TK - s.w_tile : 0;
   return s;
 }
-__device__ __forceinline__ int slot_of(const Seen& s, int x) { return x < s.n_sink ? x : x - s.n_sink + s.w0; }
+template <int TK>
+__device__ __forceinline__ int first_slot(const Seen& s, int tile) {
+  return (tile < s.sink_tiles ? tile : tile - s.sink_tiles + s.w_tile) * TK;
+}
 // whether the query at slot i sees slot j <= its sequence's last
 __device__ __forceinline__ bool sees(const DecodeArgs& a, int i, int j) {
   return j <= i && (a.window == 0 || i - j < a.window || j < a.sinks);
@@ -73,18 +86,18 @@ __device__ __forceinline__ int64_t warp_sum64(int64_t v) {
 }
 
 // How the tiles are dealt: unit (b, u), u = kv head * groups + row group, has tiles(b) tiles; units in order.
-// One warp computes; `total` tiles go to as many CTAs as have a tile for each of their SHARE warps, at most the grid.
-template <int TK, int SHARE>
+// One warp computes; `total` tiles go to as many CTAs as have LEAST tiles each, at most the grid.
+template <int TK, int LEAST>
 struct Deal {
   int64_t total;
   int workers;
-  __device__ __forceinline__ int tiles(const DecodeArgs& a, int b) const { return (seen_of(a, b).n + TK - 1) / TK; }
+  __device__ __forceinline__ int tiles(const DecodeArgs& a, int b) const { return seen_of<TK>(a, b).tiles; }
   __device__ void count(const DecodeArgs& a, int lane) {
     const int units = a.c.n_kv_heads * a.groups;
     int64_t t = 0;
     for (int b = lane; b < a.batch; b += 32) t += (int64_t)tiles(a, b) * units;
     total = warp_sum64(t);
-    const int64_t w = (total + SHARE - 1) / SHARE;
+    const int64_t w = (total + LEAST - 1) / LEAST;
     workers = w < a.grid ? (int)w : a.grid;
   }
   __device__ __forceinline__ int64_t start(int cta) const { return total * cta / workers; }
@@ -126,8 +139,8 @@ struct Cursor {
   int b, u, tile, tiles;
   Seen s;
   __device__ __forceinline__ void enter(const DecodeArgs& a) {
-    s = seen_of(a, b);
-    tiles = (s.n + TK - 1) / TK;
+    s = seen_of<TK>(a, b);
+    tiles = s.tiles;
   }
   // on to the next unit's tile 0 (past the last sequence: b == batch)
   __device__ __forceinline__ void next_unit(const DecodeArgs& a) {
@@ -186,25 +199,32 @@ __device__ __forceinline__ void split_tf32(float x, uint32_t& hi, uint32_t& lo) 
 }
 
 // ---------------------------------------------------------------------------------------
-// WM: warps of a group, each on sixteen of the unit's 16 WM rows; NG groups a CTA, one CTA an SM.  A stage holds K and V
-// of TK tokens, rows of DHT values (zeros past head_dim and past the tokens that are there) whose 16-byte chunks are
-// permuted so that the reads below meet no bank twice.
+// WM: warps of a group, each on sixteen of the unit's 16 WM rows; NG groups and two copying warps a CTA, one CTA an SM.  A
+// stage holds K and V of TK tokens, rows of DHT values (zeros past head_dim) whose 16-byte chunks are permuted so that the
+// reads below meet no bank twice (f32 keys: twice).
+//   TMA   pages of a multiple of 8 tokens: boxes of BR slots of a page, BR the largest of 32, 16 and 8 that divides a page and
+//         a tile: 8 instructions a tile of 32 tokens in pages of 16;
+//   else  cp.async, 16 bytes a lane.
 // ---------------------------------------------------------------------------------------
 template <typename T, int DHT, int WM>
 struct Plan {
   static constexpr bool B16 = sizeof(T) == 2;
-  static constexpr int TK = (B16 ? (DHT == 256 ? 16 : 32) : (DHT == 256 ? 8 : 16)) * (WM == 4 ? 2 : 1);
-  static constexpr int NG = WM == 4 ? 2 : 4, THREADS = 32 * WM * NG, ROWS = 16 * WM;
-  static constexpr int TILE = TK * DHT * (int)sizeof(T), STAGE = 2 * TILE, STAGES = DHT == 64 ? 6 : 3, RING = STAGES * STAGE;
-  static constexpr int Q = NG * RING, STATS = Q + ROWS * DHT * (int)sizeof(T), MASK = STATS + NG * ROWS * 8,
-                       BYTES = MASK + NG * STAGES * 8;
-  static_assert(ROWS * DHT * 4 <= STAGE, "a group's outputs are put into a stage");
-  static_assert(BYTES <= 226 * 1024, "shared memory");
+  static constexpr int TK = (DHT == 256 ? 16 : WM == 4 || DHT == 64 ? 64 : 32) / (B16 ? 1 : 2);
+  // six warps and the two that copy may have 255 registers each (four row groups: eight and two, 168)
+  static constexpr int NG = WM == 1 ? 6 : WM == 2 ? 3 : 2, WORKERS = 32 * WM * NG, THREADS = WORKERS + 64, ROWS = 16 * WM;
+  static constexpr int TILE = TK * DHT * (int)sizeof(T), STAGE = 2 * TILE, STAGES = 192 * 1024 / STAGE < 16 ? 192 * 1024 / STAGE : 16;
+  static constexpr int Q = STAGES * STAGE, QB = ROWS * DHT * (int)sizeof(T), STATS = Q + 2 * QB, MASK = STATS + NG * ROWS * 8;
+  static_assert(ROWS * DHT * 4 <= STAGE, "a group's outputs are put into the stage of its last tile");
   // float `col` of row `row` of a group's outputs in its stage: eight rows' pairs fall in distinct banks
-  static __device__ __forceinline__ int at(int row, int col) { return row * DHT + (col ^ ((row & 7) << 3)); }
-  // where the 16-byte chunk of a row of K or V goes
-  static __device__ __forceinline__ int k_chunk(int row, int c) { return B16 ? c ^ (row & 7) : c ^ ((row & 1) << 2); }
-  static __device__ __forceinline__ int v_chunk(int row, int c) { return B16 ? c ^ (row & 7) : c ^ (((row >> 1) & 3) << 1); }
+  static __device__ __forceinline__ int sum_at(int row, int col) { return row * DHT + (col ^ ((row & 7) << 3)); }
+  // K or V of a stage: boxes of 2^brs rows, of each box the atoms of 128 bytes of every row, whose chunks the 128-byte
+  // swizzle of TMA permutes.  A row's place, an atom's distance, and a 16-byte chunk's place in a row of its atom:
+  static __device__ __forceinline__ int row_at(int r, int brs) { return ((r >> brs) * ATOMS << (brs + 7)) + ((r & ((1 << brs) - 1)) << 7); }
+  static __device__ __forceinline__ int chunk_at(int r, int c) { return ((c & 7) ^ (r & 7)) << 4; }
+  static __device__ __forceinline__ int at(int r, int c, int brs) { return row_at(r, brs) + ((c >> 3) << (brs + 7)) + chunk_at(r, c); }
+  static constexpr int ATOMS = DHT * (int)sizeof(T) / 128, MBAR = MASK + STAGES * 8, PLACES = MBAR + 2 * STAGES * 8,
+                       BYTES = PLACES + 2 * 32 * 8;
+  static_assert(BYTES <= 226 * 1024, "shared memory");
 };
 
 template <typename T>
@@ -236,20 +256,40 @@ __device__ __forceinline__ void finish(const DecodeArgs& a, int b, int hk, int r
   }
 }
 
-template <typename T, int DHT, int WM>
-__global__ void __launch_bounds__(Plan<T, DHT, WM>::THREADS, 1) decode_kernel(const __grid_constant__ DecodeArgs a) {
+// shares of a call with few tiles: a CTA has at least this many (fewer CTAs would leave SMs without copies, more make joins)
+constexpr int SHARE = 4;
+
+template <typename T, int DHT, int WM, bool TMA>
+__global__ void __launch_bounds__(Plan<T, DHT, WM>::THREADS, 1) decode_kernel(const __grid_constant__ CUtensorMap tmK,
+    const __grid_constant__ CUtensorMap tmV, const __grid_constant__ DecodeArgs a) {
   using P = Plan<T, DHT, WM>;
   constexpr bool B16 = P::B16;
-  constexpr int TK = P::TK, S = P::STAGES, NG = P::NG, ROWS = P::ROWS, GT = 32 * WM, VE = 16 / (int)sizeof(T), CH = DHT / VE, NT = TK / 8;
-  extern __shared__ __align__(128) uint8_t sm[];
-  __shared__ int64_t run_start, run_total;
+  constexpr int TK = P::TK, S = P::STAGES, NG = P::NG, ROWS = P::ROWS, VE = 16 / (int)sizeof(T), CH = DHT / VE, NT = TK / 8;
+  constexpr uint64_t FULL = TK == 64 ? ~0ull : (1ull << (TK & 63)) - 1;
+  extern __shared__ __align__(1024) uint8_t sm[];
+  __shared__ int64_t run_start, run_total, run_in;
   __shared__ int run_n, run_b, run_workers, joins;
-  __shared__ int64_t run_in;
+  __shared__ int last_stage[NG];
+  __shared__ volatile int abort_sh;
+  uint64_t* full = reinterpret_cast<uint64_t*>(sm + P::MBAR);  // [S]: a stage's copies have landed
+  uint64_t* empty = full + S;                                  // [S]: its group has read it
+  uint64_t* mask = reinterpret_cast<uint64_t*>(sm + P::MASK);  // [S]: tokens of the tile that are there and seen by a row
+  if (smem_addr(sm) & 1023u) {  // the swizzle goes by the address
+    if (threadIdx.x == 0) set_dev_error(a.c.err_dev, RA_DEVERR_BOUNDS);
+    return;
+  }
+  const int tid = threadIdx.x, warp = tc::warp_index(), lane = tid & 31, grp = warp / WM, wm = warp - grp * WM;
+  if (tid < S) {
+    tc::mbar_init(&full[tid], TMA ? 1 : 33);
+    tc::mbar_init(&empty[tid], WM);
+  }
+  if (tid == 0) abort_sh = 0;
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   pdl_wait();
   pdl_trigger();
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, grp = warp / WM, wm = warp - grp * WM;
   if (warp == 0) {
-    Deal<TK, NG> d;
+    Deal<TK, SHARE> d;
     d.count(a, lane);
     int b = 0;
     int64_t first = 0, n = 0, s = 0;
@@ -270,7 +310,7 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM>::THREADS, 1) decode_kernel(co
   __syncthreads();
   // sequences without a token: zeros (dealt in turn to all CTAs)
   for (int b = blockIdx.x; b < a.batch; b += gridDim.x)
-    if (seen_of(a, b).n == 0)
+    if (seen_of<TK>(a, b).tiles == 0)
       for (int e = tid; e < a.c.n_kv_heads * a.R * (a.c.head_dim / 4); e += P::THREADS) {
         const int row = e / (a.c.head_dim / 4), d = (e - row * (a.c.head_dim / 4)) * 4;
         finish<T>(a, b, row / a.R, row % a.R, d, make_float4(0.f, 0.f, 0.f, 0.f), 0.f, 0.f, false);
@@ -278,95 +318,182 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM>::THREADS, 1) decode_kernel(co
   const int n_tiles = run_n;
   if (n_tiles == 0) return;
   const int g = lane >> 2, t4 = lane & 3, dh = a.c.head_dim;
-  const T *Kp = (const T*)a.c.k_dev, *Vp = (const T*)a.c.v_dev;
-  uint8_t* ring = sm + grp * P::RING;
-  float2* stats = reinterpret_cast<float2*>(sm + P::STATS);  // [NG][ROWS]
-  uint64_t* mask = reinterpret_cast<uint64_t*>(sm + P::MASK) + grp * S;
-  auto group_sync = [&]() {
-    if (WM == 1)
-      __syncwarp();
-    else
-      asm volatile("bar.sync %0, %1;" ::"r"(1 + grp), "r"(GT) : "memory");
-  };
-
-  Cursor<TK> cur;  // the first tile of the segment at hand
+  Cursor<TK> cur;
   cur.b = run_b;
   cur.enter(a);
   cur.u = (int)(run_in / cur.tiles);
   cur.tile = (int)(run_in - (int64_t)cur.u * cur.tiles);
-  Cursor<TK> ahead = cur;  // this group's tile whose rows are looked up next
-  ahead.skip(a, grp);
 
-  // ---- copies.  Lanes (of every warp of the group) look up the rows of a tile, a tile before they are copied
-  int asked = grp;         // run-relative number of the tile looked up
-  int64_t my_row[(TK + 31) / 32];
-  auto look_up = [&]() {
+  if (warp >= P::WORKERS / 32) {
+    // ------------------------------------------------------------ copies: the two warps take the tiles in turn
+    const int odd = warp - P::WORKERS / 32;
+    const T *Kp = (const T*)a.c.k_dev, *Vp = (const T*)a.c.v_dev;
+    int2* boxes_at = reinterpret_cast<int2*>(sm + P::PLACES) + 32 * odd;  // of the batch: page and kv head, row of the page
+    const int box = TMA ? 1 << a.brs : 1, nb = TK / box;  // slots a box, boxes a tile
+    constexpr int HALVES = TMA ? 1 : (TK + 31) / 32;      // boxes a lane looks up
+    const int batch = TMA ? 32 / nb : 1;                  // tiles looked up at once, of one unit
+    int64_t place[HALVES], next_place[HALVES];            // TMA: page and kv head; else the row of the pools; -1: not there
+    int off = 0, next_off = 0;                            // TMA: row of the page
+    auto look_up = [&](const Cursor<TK>& c, int tiles, int64_t (&pl)[HALVES], int& po) {
 #pragma unroll
-    for (int h = 0; h < (TK + 31) / 32; ++h) {
-      my_row[h] = -1;
-      const int i = 32 * h + lane, x = ahead.tile * TK + i;
-      if (asked < n_tiles && i < TK && x < ahead.s.n) {
-        const int slot = slot_of(ahead.s, x), p = slot / a.c.page_size;
-        const int page = a.c.block_table_dev[(int64_t)ahead.b * a.c.max_pages + p];
-        if ((uint32_t)page < (uint32_t)a.c.n_pages)
-          my_row[h] = ((int64_t)page * a.c.n_kv_heads + ahead.u / a.groups) * a.c.page_size + (slot - p * a.c.page_size);
-        else
-          set_dev_error(a.c.err_dev, RA_DEVERR_BOUNDS);
+      for (int h = 0; h < HALVES; ++h) {
+        const int i = 32 * h + lane, t = i / nb, slot = first_slot<TK>(c.s, c.tile + t) + (i - t * nb) * box;
+        pl[h] = -1;
+        if (t < tiles && slot < c.s.len && (TMA || slot < c.s.n_sink || slot >= c.s.w0)) {
+          const int p = a.page_shift >= 0 ? slot >> a.page_shift : slot / a.c.page_size;
+          const int page = a.c.block_table_dev[(int64_t)c.b * a.c.max_pages + p];
+          if ((uint32_t)page < (uint32_t)a.c.n_pages) {
+            const int64_t ph = (int64_t)page * a.c.n_kv_heads + c.u / a.groups;
+            po = slot - p * a.c.page_size;
+            pl[h] = TMA ? ph : ph * a.c.page_size + po;
+          } else {
+            set_dev_error(a.c.err_dev, RA_DEVERR_BOUNDS);
+          }
+        }
       }
-    }
-  };
-  // the looked-up tile into stage st
-  auto copy = [&](int st) {
-    const uint32_t dst = smem_addr(ring + st * P::STAGE);
-    uint64_t live = 0;
+    };
+    auto batch_of = [&](const Cursor<TK>& c, int left) {
+      const int n = c.tiles - c.tile < left ? c.tiles - c.tile : left;
+      return n < batch ? n : batch;
+    };
+    int done = 0, st = -1, round = 0, tile = -1, many = batch_of(cur, n_tiles);
+    bool ok = true;
+    look_up(cur, many, next_place, next_off);
+    while (done < n_tiles && ok) {
+      // this batch's places; the next one's are requested
+      const Cursor<TK> at = cur;
+      const int now = many;
 #pragma unroll
-    for (int h = 0; h < (TK + 31) / 32; ++h) live |= (uint64_t)__ballot_sync(0xffffffffu, my_row[h] >= 0) << (32 * h);
-    if (lane == 0 && wm == 0) mask[st] = live;
-    constexpr int PER = (CH < 32 ? 32 / CH : 1), STEP = PER * WM;  // rows a warp copies at once, and the group
-    const int rsub = CH < 32 ? lane / CH : 0;
+      for (int h = 0; h < HALVES; ++h) place[h] = next_place[h];
+      off = next_off;
+      const uint32_t there = TMA ? __ballot_sync(0xffffffffu, place[0] >= 0) : 0;
+      if (TMA) {
+        __syncwarp();
+        boxes_at[lane] = make_int2((int)place[0], off);
+        __syncwarp();
+      }
+      done += now;
+      if (done < n_tiles) {
+        cur.skip(a, now);
+        many = batch_of(cur, n_tiles - done);
+        look_up(cur, many, next_place, next_off);
+      }
+      for (int t = 0; t < now; ++t) {
+        ++tile;
+        if (++st == S) {
+          st = 0;
+          ++round;
+        }
+        if ((tile & 1) != odd) continue;
+        const int slot0 = first_slot<TK>(at.s, at.tile + t);
+        const uint32_t boxes = TMA ? (there >> (t * nb)) & (uint32_t)((1ull << nb) - 1) : 0;
+        uint64_t live = FULL;
+        if (!TMA || boxes != (uint32_t)((1ull << nb) - 1) || slot0 + TK > at.s.len || (slot0 < at.s.w0 && slot0 + TK > at.s.n_sink)) {
+          live = 0;
+#pragma unroll
+          for (int h = 0; h < (TK + 31) / 32; ++h) {
+            const int i = 32 * h + lane, slot = slot0 + i;
+            const bool on = TMA ? i < TK && slot < at.s.len && (slot < at.s.n_sink || slot >= at.s.w0) && ((boxes >> (i / box)) & 1u)
+                                : place[TMA ? 0 : h] >= 0;
+            live |= (uint64_t)__ballot_sync(0xffffffffu, on) << (32 * h);
+          }
+        }
+        if (round > 0) ok = __all_sync(0xffffffffu, tc::mbar_wait(&empty[st], (round - 1) & 1, &abort_sh, a.c.err_dev)) != 0;
+        if (!ok) break;
+        const uint32_t dst = smem_addr(sm + st * P::STAGE);
+        if constexpr (TMA) {
+          if (tc::elect_one()) {
+            mask[st] = live;
+            tc::mbar_expect_tx(&full[st], (uint32_t)__popc(boxes) * (uint32_t)box * (2 * 128 * P::ATOMS));
+#pragma unroll
+            for (int i = 0; i < TK / 8; ++i)
+              if ((boxes >> i) & 1u) {
+                const int2 at_ = boxes_at[t * nb + i];
+                const uint32_t d = dst + i * box * (128 * P::ATOMS);
+                if (a.whole_rows) {
+                  tc::tma_load4(&tmK, d, &full[st], 0, at_.y, 0, at_.x);
+                  tc::tma_load4(&tmV, d + P::TILE, &full[st], 0, at_.y, 0, at_.x);
+                } else {
+#pragma unroll
+                  for (int n = 0; n < P::ATOMS; ++n) {
+                    tc::tma_load3(&tmK, d + n * box * 128, &full[st], n * (128 / (int)sizeof(T)), at_.y, at_.x);
+                    tc::tma_load3(&tmV, d + P::TILE + n * box * 128, &full[st], n * (128 / (int)sizeof(T)), at_.y, at_.x);
+                  }
+                }
+              }
+          }
+          __syncwarp();
+        } else {
+          if (lane == 0) mask[st] = live;
+          constexpr int PER = CH < 32 ? 32 / CH : 1;  // rows copied at once
+          const int rsub = CH < 32 ? lane / CH : 0;
 #pragma unroll 4
-    for (int r0 = wm * PER; r0 < TK; r0 += STEP) {
-      const int r = r0 + rsub;
-      const int64_t row = __shfl_sync(0xffffffffu, (TK > 32 && r0 >= 32) ? my_row[(TK + 31) / 32 - 1] : my_row[0], r & 31);
+          for (int r0 = 0; r0 < TK; r0 += PER) {
+            const int r = r0 + rsub;
+            const int64_t row = __shfl_sync(0xffffffffu, (TK > 32 && r0 >= 32) ? place[HALVES - 1] : place[0], r & 31);
 #pragma unroll
-      for (int c = CH < 32 ? lane % CH : lane; c < CH; c += 32) {
-        const bool on = row >= 0 && c * VE < dh;
-        const int64_t e = on ? row * dh + c * VE : 0;
-        cp16(dst + r * (DHT * (int)sizeof(T)) + P::k_chunk(r, c) * 16, Kp + e, on);
-        cp16(dst + P::TILE + r * (DHT * (int)sizeof(T)) + P::v_chunk(r, c) * 16, Vp + e, on);
+            for (int c = CH < 32 ? lane % CH : lane; c < CH; c += 32) {
+              const bool on = row >= 0 && c * VE < dh;
+              const int64_t e = on ? row * dh + c * VE : 0;
+              cp16(dst + P::at(r, c, a.brs), Kp + e, on);
+              cp16(dst + P::TILE + P::at(r, c, a.brs), Vp + e, on);
+            }
+          }
+          asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_addr(&full[st])) : "memory");
+          if (lane == 0) tc::mbar_arrive(&full[st]);
+        }
       }
     }
-  };
-  auto go_on = [&]() {  // to this group's next tile
-    asked += NG;
-    if (asked < n_tiles) ahead.skip(a, NG);
-    look_up();
-  };
-  look_up();
-#pragma unroll 1
-  for (int i = 0; i < S - 1; ++i) {
-    if (asked < n_tiles) copy(i);
-    cp_commit();
-    go_on();
+    if (!TMA) cp_wait<0>();
+    if (TMA && !ok) {
+      // a wait gave up: let the copies on their way land before shared memory is released (those of tiles below `tile`)
+      volatile int no_abort = 0;
+      for (int i = tile > S ? tile - S : 0; i < tile; ++i)
+        if ((i & 1) == odd) tc::mbar_wait(&full[i % S], (i / S) & 1, &no_abort, nullptr);
+    }
+    return;
   }
 
-  int st = 0;          // the stage of this group's next tile
-  int n = 0;           // run-relative number of the segment's first tile
-  int mine = grp;      // of this group's next tile
+  // ------------------------------------------------------------ arithmetic
+  float2* stats = reinterpret_cast<float2*>(sm + P::STATS);  // [NG][ROWS]
+  auto group_sync = [&]() {
+    if (WM == 1)
+      __syncwarp();
+    else
+      tc::named_sync(2 + grp, 32 * WM);
+  };
+  int n = 0;                     // run-relative number of the segment's first tile
+  int mine = grp;                // of this group's next tile
+  int st = grp % S, round = 0;   // its stage
   bool first_segment = true;
+  // a unit's queries into one of two buffers, the next unit's while this one's tiles are done
+  auto load_queries = [&](const Cursor<TK>& c, int buf) {
+    const int hk = c.u / a.groups, r0 = (c.u - hk * a.groups) * ROWS;
+    for (int e = tid; e < ROWS * CH; e += P::WORKERS) {
+      const int r = e / CH, k = e - r * CH, t = (r0 + r) / a.G;
+      const bool live = r0 + r < a.R && k * VE < dh;
+      const T* src = live ? (const T*)a.q + ((int64_t)c.b * a.n_new + t) * a.q_stride + (hk * a.G + r0 + r - t * a.G) * dh + k * VE : (const T*)a.q;
+      cp16(smem_addr(sm + P::Q + buf * P::QB) + r * (DHT * (int)sizeof(T)) + ((B16 ? k ^ (r & 7) : k ^ ((r & 1) << 2)) << 4), src, live);
+    }
+    cp_commit();
+  };
+  Cursor<TK> nxt = cur;
+  int qbuf = 0;
+  load_queries(cur, 0);
   while (n < n_tiles) {
     // ---- a segment: the tiles of one unit in this run
     const int seg = cur.tiles - cur.tile < n_tiles - n ? cur.tiles - cur.tile : n_tiles - n;
     const int hk = cur.u / a.groups, r0 = (cur.u - hk * a.groups) * ROWS;
-    T* Qs = reinterpret_cast<T*>(sm + P::Q);
-    for (int e = tid; e < ROWS * CH; e += P::THREADS) {
-      const int r = e / CH, c = e - r * CH, t = (r0 + r) / a.G;
-      uint4 x = make_uint4(0, 0, 0, 0);
-      if (r0 + r < a.R && c * VE < dh)
-        x = *reinterpret_cast<const uint4*>((const T*)a.q + ((int64_t)cur.b * a.n_new + t) * a.q_stride + (hk * a.G + r0 + r - t * a.G) * dh + c * VE);
-      *reinterpret_cast<uint4*>(Qs + r * DHT + (B16 ? c ^ (r & 7) : c ^ ((r & 1) << 2)) * VE) = x;
+    cp_wait<0>();
+    tc::named_sync(1, P::WORKERS);  // this unit's queries are there
+    T* Qs = reinterpret_cast<T*>(sm + P::Q + qbuf * P::QB);
+    qbuf ^= 1;
+    if (n + seg < n_tiles) {
+      nxt = cur;
+      nxt.tile = 0;
+      nxt.next_unit(a);
+      load_queries(nxt, qbuf);
     }
-    __syncthreads();
     // the sixteen rows of this warp as A operands (f32: dims 4 t .. 4 t + 3 of every sixteen, of which a step of eight takes
     // two; K's are taken alike, and the sum over dims does not mind)
     constexpr bool QREG = B16 || DHT <= 128;
@@ -399,27 +526,37 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM>::THREADS, 1) decode_kernel(co
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[d][e] = 0.f;
 
+    int held = -1;  // the stage of this group's last tile, kept until its outputs have been in it
     for (; mine < n + seg; mine += NG) {
-      cp_wait<S - 2>();
-      group_sync();  // this tile is there for the group's lanes, and they are done with the one before
-      const int free_st = st == 0 ? S - 1 : st - 1;
-      if (asked < n_tiles) copy(free_st);
-      cp_commit();
-      go_on();
-      const uint32_t base = smem_addr(ring + st * P::STAGE);
-      const int x0 = (cur.tile + mine - n) * TK;
+      const uint32_t base = smem_addr(sm + st * P::STAGE);
+      const uint8_t* stage = sm + st * P::STAGE;
+      const int x0 = (cur.tile + mine - n) * TK, j0 = first_slot<TK>(cur.s, cur.tile + mine - n);
+      tc::mbar_wait(&full[st], round & 1, &abort_sh, a.c.err_dev);
+      __syncwarp();
+      const uint64_t live = mask[st];
+      if (TMA && live != FULL) {
+        // what was copied beside the tokens (or was not: a bad page's place) may be anything, and 0 times NaN is not 0
+        for (int r = wm; r < TK; r += WM)
+          if (!((live >> r) & 1ull))
+            for (int c = lane; c < CH; c += 32) *reinterpret_cast<uint4*>(sm + st * P::STAGE + P::TILE + P::at(r, c, a.brs)) = make_uint4(0, 0, 0, 0);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        group_sync();
+      }
 
-      // ---- scores
+  // ---- scores
       float s[NT][4] = {};
       if constexpr (B16) {
         const int rr = ((lane >> 4) << 3) + (lane & 7), half = (lane >> 3) & 1;
+        int krow[NT / 2];
+#pragma unroll
+        for (int n2 = 0; n2 < NT / 2; ++n2) krow[n2] = P::row_at(16 * n2 + rr, a.brs);
 #pragma unroll
         for (int ks = 0; ks < DHT / 16; ++ks)
 #pragma unroll
           for (int n2 = 0; n2 < NT / 2; ++n2) {
             uint32_t kf[4];
             const int row = 16 * n2 + rr;
-            ldsm4(kf, base + row * (DHT * 2) + (((2 * ks + half) ^ (row & 7)) << 4));
+            ldsm4(kf, base + krow[n2] + ((ks >> 2) << (a.brs + 7)) + P::chunk_at(row, 2 * ks + half));
             mma16816(s[2 * n2], qf[ks], kf[0], kf[1]);
             mma16816(s[2 * n2 + 1], qf[ks], kf[2], kf[3]);
           }
@@ -438,7 +575,7 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM>::THREADS, 1) decode_kernel(co
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
             const int row = 8 * nt + g;
-            const float4 k = *reinterpret_cast<const float4*>(ring + st * P::STAGE + row * (DHT * 4) + (((4 * ks + t4) ^ ((row & 1) << 2)) << 4));
+            const float4 k = *reinterpret_cast<const float4*>(stage + P::at(row, 4 * ks + t4, a.brs));
             uint32_t bh[4], bl[4];
             split_tf32(k.x, bh[0], bl[0]);
             split_tf32(k.y, bh[1], bl[1]);
@@ -454,10 +591,8 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM>::THREADS, 1) decode_kernel(co
         }
       }
       // every row sees every token of the tile: no test a token
-      const uint64_t live = mask[st];
-      const int j0 = slot_of(cur.s, x0), j1 = slot_of(cur.s, x0 + TK - 1);
-      const bool all = live == (TK == 64 ? ~0ull : (1ull << (TK & 63)) - 1) && j1 <= cur.s.len - a.n_new &&
-                       (a.window == 0 || j1 < a.sinks || (x0 >= cur.s.n_sink && cur.s.len - 1 - j0 < a.window));
+      const bool all = live == FULL && j0 + TK - 1 <= cur.s.len - a.n_new &&
+                       (a.window == 0 || j0 + TK <= a.sinks || cur.s.len - 1 - j0 < a.window);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -468,7 +603,7 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM>::THREADS, 1) decode_kernel(co
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int k = 8 * nt + 2 * t4 + (e & 1);
-            if (!((live >> k) & 1ull) || !sees(a, qslot[e >> 1], slot_of(cur.s, x0 + k))) s[nt][e] = -INFINITY;
+            if (!((live >> k) & 1ull) || !sees(a, qslot[e >> 1], j0 + k)) s[nt][e] = -INFINITY;
           }
       }
       if (a.scores) {
@@ -531,11 +666,11 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM>::THREADS, 1) decode_kernel(co
             const float2 hi = __bfloat1622float2(*reinterpret_cast<__nv_bfloat162*>(&pf[k]));
             pl[k] = pack2(p0 - hi.x, p1 - hi.y);
           }
-          const int row = 16 * n2 + rr;
+          const int row = 16 * n2 + rr, vrow = P::row_at(row, a.brs);
 #pragma unroll
           for (int nb = 0; nb < DHT / 16; ++nb) {
             uint32_t vf[4];
-            ldsm4t(vf, base + P::TILE + row * (DHT * 2) + (((2 * nb + half) ^ (row & 7)) << 4));
+            ldsm4t(vf, base + P::TILE + vrow + ((nb >> 2) << (a.brs + 7)) + P::chunk_at(row, 2 * nb + half));
             mma16816(o[2 * nb], pf, vf[0], vf[1]);
             mma16816(o[2 * nb + 1], pf, vf[2], vf[3]);
             mma16816(o[2 * nb], pl, vf[0], vf[1]);
@@ -552,42 +687,53 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM>::THREADS, 1) decode_kernel(co
           split_tf32(s[nt][1], ah[2], al[2]);
           split_tf32(s[nt][3], ah[3], al[3]);
           const int v0 = 8 * nt + 2 * t4;
-          const float* V0 = reinterpret_cast<const float*>(ring + st * P::STAGE + P::TILE + v0 * (DHT * 4));
-          const float* V1 = V0 + DHT;
+          const float* V = reinterpret_cast<const float*>(stage + P::TILE);
 #pragma unroll
           for (int d = 0; d < DHT / 8; ++d) {
             const int c = 2 * d + (g >> 2), w = g & 3;
             uint32_t h0, l0, h1, l1;
-            split_tf32(V0[(c ^ (t4 << 1)) * 4 + w], h0, l0);
-            split_tf32(V1[(c ^ (t4 << 1)) * 4 + w], h1, l1);
+            split_tf32(V[P::at(v0, c, a.brs) / 4 + w], h0, l0);
+            split_tf32(V[P::at(v0 + 1, c, a.brs) / 4 + w], h1, l1);
             mma1688(o[d], al, h0, h1);
             mma1688(o[d], ah, l0, l1);
             mma1688(o[d], ah, h0, h1);
           }
         }
       }
-      st = st + 1 == S ? 0 : st + 1;
+      // the stage is free again, but for the last one's
+      if (mine + NG < n + seg) {
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&empty[st]);
+      } else {
+        held = st;
+      }
+      st += NG;
+      if (st >= S) {
+        st -= S;
+        ++round;
+      }
     }
 
-    // ---- the groups' outputs together: each puts its own into the stage that has no tile on its way
+    // ---- the groups' outputs together: each puts its own into its last tile's stage
     group_sync();
-    float* stage = reinterpret_cast<float*>(ring + (st == 0 ? S - 1 : st - 1) * P::STAGE);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
       l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
       const int row = 16 * wm + g + 8 * h;
       if (t4 == 0) stats[grp * ROWS + row] = make_float2(m[h], l[h]);
+      if (held >= 0) {
+        float* to = reinterpret_cast<float*>(sm + held * P::STAGE);
 #pragma unroll
-      for (int d = 0; d < DHT / 8; ++d) *reinterpret_cast<float2*>(stage + P::at(row, 8 * d + 2 * t4)) = make_float2(o[d][2 * h], o[d][2 * h + 1]);
+        for (int d = 0; d < DHT / 8; ++d) *reinterpret_cast<float2*>(to + P::sum_at(row, 8 * d + 2 * t4)) = make_float2(o[d][2 * h], o[d][2 * h + 1]);
+      }
     }
-    // (the free stage of every group, for the sum)
-    __shared__ int free_stage[NG];
-    if (lane == 0 && wm == 0) free_stage[grp] = st == 0 ? S - 1 : st - 1;
-    __syncthreads();
+    if (lane == 0 && wm == 0) last_stage[grp] = held;
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    tc::named_sync(1, P::WORKERS);
     const bool whole = seg == cur.tiles;
     const int64_t slot = 2 * (int64_t)blockIdx.x + (first_segment ? 0 : 1);
-    for (int e = tid; e < ROWS * (DHT / 4); e += P::THREADS) {
+    for (int e = tid; e < ROWS * (DHT / 4); e += P::WORKERS) {
       const int r = e / (DHT / 4), d = (e - r * (DHT / 4)) * 4;
       if (r0 + r >= a.R || d >= dh) continue;
       float M = -INFINITY, L = 0.f;
@@ -602,7 +748,7 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM>::THREADS, 1) decode_kernel(co
           const float f = ex2_fast(ml.x - M);
           any = true;
           L = fmaf(ml.y, f, L);
-          v = fma4(*reinterpret_cast<const float4*>(reinterpret_cast<const float*>(sm + k * P::RING + free_stage[k] * P::STAGE) + P::at(r, d)), f, v);
+          v = fma4(*reinterpret_cast<const float4*>(reinterpret_cast<const float*>(sm + last_stage[k] * P::STAGE) + P::sum_at(r, d)), f, v);
         }
       }
       if (whole) {
@@ -615,7 +761,7 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM>::THREADS, 1) decode_kernel(co
     if (!whole && a.join) {
       // the last CTA to come here has all parts
       __threadfence();
-      __syncthreads();
+      tc::named_sync(1, P::WORKERS);
       const int64_t first = run_start + n - cur.tile;  // the unit's first tile
       const int c0 = (int)(((first + 1) * run_workers - 1) / run_total);
       if (tid == 0) {
@@ -626,14 +772,14 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM>::THREADS, 1) decode_kernel(co
         if (joins) *count = 0;
         __threadfence();
       }
-      __syncthreads();
+      tc::named_sync(1, P::WORKERS);
       const int parts = joins;
       if (parts) {
         // part p's slot: the first is its CTA's last segment, unless the unit starts that CTA's run
         const bool starts = run_total * c0 / run_workers == first;
         auto ml_of = [&](int p, int r) { return __ldcg(&a.part_ml[(2 * (int64_t)(c0 + p) + (p == 0 && !starts ? 1 : 0)) * ROWS + r]); };
         const int rows = a.R - r0 < ROWS ? a.R - r0 : ROWS;
-        for (int e = tid; e < rows * (dh / 4); e += P::THREADS) {
+        for (int e = tid; e < rows * (dh / 4); e += P::WORKERS) {
           const int r = e / (dh / 4), d = (e - r * (dh / 4)) * 4;
           float M = -INFINITY, L = 0.f;
           bool any = false;
@@ -655,20 +801,19 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM>::THREADS, 1) decode_kernel(co
         }
       }
     }
-    __syncthreads();  // the stages, the statistics and Q's space are free again
+    tc::named_sync(1, P::WORKERS);  // the held stages, the statistics and Q's space are free again
+    if (held >= 0 && lane == 0) tc::mbar_arrive(&empty[held]);
     first_segment = false;
     n += seg;
-    cur.tile = 0;
-    if (n < n_tiles) cur.next_unit(a);
+    cur = nxt;
   }
-  cp_wait<0>();
 }
 
 // ---------------------------------------------------------------------------------------
 // Joins the parts of one query row where there may be many: a CTA a row; its 256 threads take the parts in turns of
 // 1024 / DHT, four columns each, and are added in a fixed order.  What one CTA finished is left alone.
 // ---------------------------------------------------------------------------------------
-template <typename T, int DHT, int TK, int NG, int ROWS>
+template <typename T, int DHT, int TK, int ROWS>
 __global__ void __launch_bounds__(256) decode_join_kernel(const __grid_constant__ DecodeArgs a) {
   constexpr int TPP = DHT / 4, TURNS = 256 / TPP;
   __shared__ float4 red[256];
@@ -682,7 +827,7 @@ __global__ void __launch_bounds__(256) decode_join_kernel(const __grid_constant_
   const int per_b = a.c.n_kv_heads * a.R, b = (int)(id / per_b), hk = (int)(id - (int64_t)b * per_b) / a.R, row = (int)(id % a.R);
   const int grp = row / ROWS, lr = row - grp * ROWS;
   if (tid < 32) {
-    Deal<TK, NG> d;
+    Deal<TK, SHARE> d;
     d.count(a, tid);
     const int tiles = d.tiles(a, b);
     if (tid == 0) sh_parts = 0;
@@ -738,12 +883,13 @@ __global__ void __launch_bounds__(256) decode_join_kernel(const __grid_constant_
 
 // weights_out = weights_in + the rows' softmax weights, in row order: a thread four slots, 256 apart
 constexpr int WROWS = 8;
+template <int TK>
 __global__ void __launch_bounds__(256) decode_weights_kernel(const __grid_constant__ DecodeArgs a, int chunks) {
   pdl_wait();
   pdl_trigger();
   const int64_t unit = blockIdx.x / chunks;  // b * kv heads + head
   const int b = (int)(unit / a.c.n_kv_heads);
-  const Seen s = seen_of(a, b);
+  const Seen s = seen_of<TK>(a, b);
   const float* lse2 = a.lse2 + unit * a.R;
   const int j0 = (int)(blockIdx.x - unit * chunks) * 1024 + (int)threadIdx.x;
   if (j0 >= s.len) return;
@@ -752,7 +898,8 @@ __global__ void __launch_bounds__(256) decode_weights_kernel(const __grid_consta
   bool on[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int j = j0 + 256 * i, x = j < s.n_sink ? j : j >= s.w0 ? j - s.w0 + s.n_sink : -1;
+    const int j = j0 + 256 * i, tile = j / TK;
+    const int x = tile < s.sink_tiles ? j : tile >= s.w_tile ? j + (s.sink_tiles - s.w_tile) * TK : -1;
     on[i] = j < s.len && x >= 0;
     w[i] = j < s.len && a.w_in ? a.w_in[unit * a.w_stride + j] : 0.f;
     sc[i] = a.scores + unit * a.R * a.x_stride + (on[i] ? x : 0);
@@ -818,15 +965,40 @@ DecodeLayout layout_of(const ra_attention_decode_args& p) {
   return L;
 }
 
-template <typename T, int DHT, int WM>
-cudaError_t launch(const DecodeArgs& a, cudaStream_t st) {
+template <typename T, int DHT, int WM, bool TMA>
+cudaError_t launch_kernel(const CUtensorMap& k, const CUtensorMap& v, const DecodeArgs& a, cudaStream_t st) {
   using P = Plan<T, DHT, WM>;
-  cudaError_t e = allow_smem(decode_kernel<T, DHT, WM>, P::BYTES);
-  if (e == cudaSuccess) e = launch_pdl(decode_kernel<T, DHT, WM>, dim3(a.grid), dim3(P::THREADS), (size_t)P::BYTES, st, a);
+  cudaError_t e = allow_smem(decode_kernel<T, DHT, WM, TMA>, P::BYTES);
+  return e == cudaSuccess ? launch_pdl(decode_kernel<T, DHT, WM, TMA>, dim3(a.grid), dim3(P::THREADS), (size_t)P::BYTES, st, k, v, a) : e;
+}
+template <typename T, int DHT, int WM>
+cudaError_t launch(DecodeArgs& a, cudaStream_t st) {
+  using P = Plan<T, DHT, WM>;
+  const ra_kv_cache& c = a.c;
+  // boxes of 2^brs slots of a page: a pool is [pages x kv heads][page_size][head_dim]
+  a.brs = c.page_size % 32 == 0 && P::TK >= 32 ? 5 : c.page_size % 16 == 0 && P::TK >= 16 ? 4 : 3;
+  a.whole_rows = c.head_dim == DHT;
+  CUtensorMap k, v;
+  memset(&k, 0, sizeof k);
+  memset(&v, 0, sizeof v);
+  const int64_t planes = (int64_t)c.n_pages * c.n_kv_heads;
+  auto map = [&](CUtensorMap* m, const void* p) {
+    return tma_map_planes(m, p, sizeof(T) == 2 ? DT_BF16 : DT_F32, (int)planes, c.page_size, c.head_dim, 128 / (int)sizeof(T), 1 << a.brs,
+                          a.whole_rows != 0);
+  };
+  const bool tma = c.page_size % 8 == 0 && planes <= INT32_MAX && map(&k, c.k_dev) && map(&v, c.v_dev);
+  cudaError_t e = tma ? launch_kernel<T, DHT, WM, true>(k, v, a, st) : launch_kernel<T, DHT, WM, false>(k, v, a, st);
   note_launch(1);
-  if (e != cudaSuccess || a.join) return e;
+  if (e == cudaSuccess && !a.join) {
+    e = launch_pdl(decode_join_kernel<T, DHT, P::TK, P::ROWS>, dim3((unsigned)((int64_t)a.batch * c.n_kv_heads * a.R)), dim3(256), 0, st, a);
+    note_launch(1);
+  }
+  if (e != cudaSuccess || !a.scores) return e;
+  const int chunks = (a.max_len + 1023) / 1024;
+  const int64_t n = (int64_t)chunks * a.batch * c.n_kv_heads;
+  if (n > INT32_MAX) return cudaErrorNotSupported;
   note_launch(1);
-  return launch_pdl(decode_join_kernel<T, DHT, P::TK, P::NG, P::ROWS>, dim3((unsigned)((int64_t)a.batch * a.c.n_kv_heads * a.R)), dim3(256), 0, st, a);
+  return launch_pdl(decode_weights_kernel<P::TK>, dim3((unsigned)n), dim3(256), 0, st, a, chunks);
 }
 
 }  // namespace
@@ -864,6 +1036,9 @@ cudaError_t attention_decode(const ra_attention_decode_args& p, cudaStream_t st)
   a.sinks = p.sinks;
   a.grid = L.grid;
   a.join = L.join;
+  a.page_shift = -1;
+  for (int i = 0; i < 31; ++i)
+    if (p.cache.page_size == 1 << i) a.page_shift = i;
   a.sl2 = p.scale * kLog2e;
   cudaError_t e;
   if (p.cache.dtype == RA_F32)
@@ -874,12 +1049,6 @@ cudaError_t attention_decode(const ra_attention_decode_args& p, cudaStream_t st)
     e = L.rows == 16 ? launch<bf16, 128, 1>(a, st) : L.rows == 32 ? launch<bf16, 128, 2>(a, st) : launch<bf16, 128, 4>(a, st);
   else
     e = launch<bf16, 256, 1>(a, st);
-  if (e != cudaSuccess || !a.scores) return e;
-  const int chunks = (a.max_len + 1023) / 1024;
-  const int64_t n = (int64_t)chunks * a.batch * a.c.n_kv_heads;
-  if (n > INT32_MAX) return cudaErrorNotSupported;
-  e = launch_pdl(decode_weights_kernel, dim3((unsigned)n), dim3(256), 0, st, a, chunks);
-  note_launch(1);
   return e;
 }
 

@@ -990,14 +990,16 @@ bool make_map(CUtensorMap* out, const void* ptr, int64_t rows, int64_t cols, int
                                            : CU_TENSOR_MAP_SWIZZLE_NONE;
   const bool b3 = blocks > 0;
   if (b3 && cols % box_cols) return false;
-  cuuint64_t gdim[3] = {(cuuint64_t)(b3 ? box_cols : cols), (cuuint64_t)rows,
-                        (cuuint64_t)(b3 ? cols / box_cols : batch ? batch : 1)};
-  cuuint64_t gstride[2] = {(cuuint64_t)ld * es, (cuuint64_t)(batch ? rows * ld : box_cols) * es};
-  cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, (cuuint32_t)(b3 ? blocks : 1)};
-  cuuint32_t estride[3] = {1, 1, 1};
+  // (blocks and batch: 4-D, columns of a block, rows, blocks, matrices)
+  cuuint64_t gdim[4] = {(cuuint64_t)(b3 ? box_cols : cols), (cuuint64_t)rows,
+                        (cuuint64_t)(b3 ? cols / box_cols : batch ? batch : 1), (cuuint64_t)batch};
+  cuuint64_t gstride[3] = {(cuuint64_t)ld * es, (cuuint64_t)(b3 ? box_cols : batch ? rows * ld : box_cols) * es,
+                           (cuuint64_t)rows * ld * es};
+  cuuint32_t box[4] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, (cuuint32_t)(b3 ? blocks : 1), 1};
+  cuuint32_t estride[4] = {1, 1, 1, 1};
   auto encode = [&] {
     return fn(out, dtype == DT_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32,
-              b3 || batch ? 3 : 2, const_cast<void*>(ptr), gdim, gstride, box, estride,
+              b3 && batch ? 4 : b3 || batch ? 3 : 2, const_cast<void*>(ptr), gdim, gstride, box, estride,
               CU_TENSOR_MAP_INTERLEAVE_NONE, sw, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   };
@@ -1075,6 +1077,11 @@ bool tma_map_bf16(CUtensorMap* out, const void* ptr, int64_t rows, int64_t cols,
 bool tma_map_bf16_batch(CUtensorMap* out, const void* ptr, int batch, int64_t rows, int64_t cols, int64_t ld,
                         int box_cols, int box_rows) {
   return make_map(out, ptr, rows, cols, ld, box_cols, box_rows, DT_BF16, 0, batch);
+}
+
+bool tma_map_planes(CUtensorMap* out, const void* ptr, int dtype, int planes, int64_t rows, int64_t cols, int box_cols,
+                    int box_rows, bool whole_rows) {
+  return make_map(out, ptr, rows, cols, cols, box_cols, box_rows, dtype, whole_rows ? (int)(cols / box_cols) : 0, planes);
 }
 
 bool tma_map_f32(CUtensorMap* out, const void* ptr, int64_t rows, int64_t cols, int64_t ld, int box_cols,

@@ -104,6 +104,10 @@ bool tma_map_bf16(CUtensorMap* out, const void* ptr, int64_t rows, int64_t cols,
 // the last of its own matrix arrive as zeros, not as the next one's (batch 0: the 2-D map)
 bool tma_map_bf16_batch(CUtensorMap* out, const void* ptr, int batch, int64_t rows, int64_t cols, int64_t ld,
                         int box_cols, int box_rows);
+// Map of `planes` contiguous [rows, cols] matrices: (columns, rows, planes) in boxes of box_cols x box_rows; whole_rows:
+// 4-D (box_cols, rows, cols / box_cols, planes), a box all column blocks of its rows, one after the other
+bool tma_map_planes(CUtensorMap* out, const void* ptr, int dtype, int planes, int64_t rows, int64_t cols, int box_cols,
+                    int box_rows, bool whole_rows);
 // the 2-D map for float32
 bool tma_map_f32(CUtensorMap* out, const void* ptr, int64_t rows, int64_t cols, int64_t ld, int box_cols,
                  int box_rows);
