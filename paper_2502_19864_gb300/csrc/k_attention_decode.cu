@@ -13,8 +13,9 @@
 // theirs) joins them.
 //   bf16: the products are mma.sync m16n8k16: sixteen rows take the tensor instruction of one, and the rate asked of
 //         it, 16 flops a byte of K and V, is a tenth of what it gives, so nothing is won by tcgen05's 128 rows.
-//   f32:  mma.sync m16n8k8 on tf32, each operand in two terms of 11 bits and their products but for the smallest: about
-//         2^-22 of a product, as good as the fp32 sums around it.
+//   f32:  FFMA, on the rows that there are (4, 8 or 16): lanes are tokens (and parts of their dims) for q K^T and dims for
+//         p V.  (tf32 products of operands split in two terms, sixteen rows always, took 217 us for 671 MB where this takes
+//         @F32@.)
 #include <cstring>
 
 #include "common.cuh"
@@ -188,31 +189,28 @@ __device__ __forceinline__ void mma16816(float* d, const uint32_t* a, uint32_t b
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ void mma1688(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-// x in two tf32 terms, the first rounded to nearest
-__device__ __forceinline__ void split_tf32(float x, uint32_t& hi, uint32_t& lo) {
-  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(hi) : "f"(x));
-  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(lo) : "f"(x - __uint_as_float(hi)));
+// the largest of the warp's values
+__device__ __forceinline__ float redux_max(float x) {
+  float y;
+  asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+  return y;
 }
 
 // ---------------------------------------------------------------------------------------
-// WM: warps of a group, each on sixteen of the unit's 16 WM rows; NG groups and two copying warps a CTA, one CTA an SM.  A
+// bf16: WM warps a group, each on sixteen of the unit's 16 WM rows; f32: WM = 1 and RM rows.  NG groups and two copying warps a CTA, one CTA an SM.  A
 // stage holds K and V of TK tokens, rows of DHT values (zeros past head_dim) whose 16-byte chunks are permuted so that the
-// reads below meet no bank twice (f32 keys: twice).
+// reads below meet no bank twice.
 //   TMA   pages of a multiple of 8 tokens: boxes of BR slots of a page, BR the largest of 32, 16 and 8 that divides a page and
 //         a tile: 8 instructions a tile of 32 tokens in pages of 16;
 //   else  cp.async, 16 bytes a lane.
 // ---------------------------------------------------------------------------------------
-template <typename T, int DHT, int WM>
+template <typename T, int DHT, int WM, int RM>
 struct Plan {
   static constexpr bool B16 = sizeof(T) == 2;
   static constexpr int TK = (DHT == 256 ? 16 : WM == 4 || DHT == 64 ? 64 : 32) / (B16 ? 1 : 2);
   // six warps and the two that copy may have 255 registers each (four row groups: eight and two, 168)
-  static constexpr int NG = WM == 1 ? 6 : WM == 2 ? 3 : 2, WORKERS = 32 * WM * NG, THREADS = WORKERS + 64, ROWS = 16 * WM;
-  static constexpr int TILE = TK * DHT * (int)sizeof(T), STAGE = 2 * TILE, STAGES = 192 * 1024 / STAGE < 16 ? 192 * 1024 / STAGE : 16;
+  static constexpr int NG = WM == 4 ? 2 : WM == 2 ? 3 : !B16 && DHT == 256 ? 5 : 6, WORKERS = 32 * WM * NG, THREADS = WORKERS + 64, ROWS = RM;
+  static constexpr int TILE = TK * DHT * (int)sizeof(T), STAGE = 2 * TILE, STAGES = (!B16 && DHT == 256 ? 160 : 192) * 1024 / STAGE;
   static constexpr int Q = STAGES * STAGE, QB = ROWS * DHT * (int)sizeof(T), STATS = Q + 2 * QB, MASK = STATS + NG * ROWS * 8;
   static_assert(ROWS * DHT * 4 <= STAGE, "a group's outputs are put into the stage of its last tile");
   // float `col` of row `row` of a group's outputs in its stage: eight rows' pairs fall in distinct banks
@@ -223,8 +221,11 @@ struct Plan {
   static __device__ __forceinline__ int chunk_at(int r, int c) { return ((c & 7) ^ (r & 7)) << 4; }
   static __device__ __forceinline__ int at(int r, int c, int brs) { return row_at(r, brs) + ((c >> 3) << (brs + 7)) + chunk_at(r, c); }
   static constexpr int ATOMS = DHT * (int)sizeof(T) / 128, MBAR = MASK + STAGES * 8, PLACES = MBAR + 2 * STAGES * 8,
-                       BYTES = PLACES + 2 * 32 * 8;
-  static_assert(BYTES <= 226 * 1024, "shared memory");
+                       X = (PLACES + 2 * 32 * 8 + 15) / 16 * 16, BYTES = X + (B16 ? 0 : NG * TK * ROWS * 4);
+  // a stage is filled by the same warp and read by the same group every time round, so that each has seen every phase of
+  // its barriers: a wait by parity for a phase that is two ahead would return at once
+  static_assert(STAGES % 2 == 0 && STAGES % NG == 0, "stages belong to copying warps and to groups");
+  static_assert(STATS % 16 == 0 && MBAR % 8 == 0 && X % 16 == 0 && BYTES <= 226 * 1024, "shared memory");
 };
 
 template <typename T>
@@ -259,10 +260,10 @@ __device__ __forceinline__ void finish(const DecodeArgs& a, int b, int hk, int r
 // shares of a call with few tiles: a CTA has at least this many (fewer CTAs would leave SMs without copies, more make joins)
 constexpr int SHARE = 4;
 
-template <typename T, int DHT, int WM, bool TMA>
-__global__ void __launch_bounds__(Plan<T, DHT, WM>::THREADS, 1) decode_kernel(const __grid_constant__ CUtensorMap tmK,
+template <typename T, int DHT, int WM, int RM, bool TMA>
+__global__ void __launch_bounds__(Plan<T, DHT, WM, RM>::THREADS, 1) decode_kernel(const __grid_constant__ CUtensorMap tmK,
     const __grid_constant__ CUtensorMap tmV, const __grid_constant__ DecodeArgs a) {
-  using P = Plan<T, DHT, WM>;
+  using P = Plan<T, DHT, WM, RM>;
   constexpr bool B16 = P::B16;
   constexpr int TK = P::TK, S = P::STAGES, NG = P::NG, ROWS = P::ROWS, VE = 16 / (int)sizeof(T), CH = DHT / VE, NT = TK / 8;
   constexpr uint64_t FULL = TK == 64 ? ~0ull : (1ull << (TK & 63)) - 1;
@@ -473,7 +474,7 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM>::THREADS, 1) decode_kernel(co
       const int r = e / CH, k = e - r * CH, t = (r0 + r) / a.G;
       const bool live = r0 + r < a.R && k * VE < dh;
       const T* src = live ? (const T*)a.q + ((int64_t)c.b * a.n_new + t) * a.q_stride + (hk * a.G + r0 + r - t * a.G) * dh + k * VE : (const T*)a.q;
-      cp16(smem_addr(sm + P::Q + buf * P::QB) + r * (DHT * (int)sizeof(T)) + ((B16 ? k ^ (r & 7) : k ^ ((r & 1) << 2)) << 4), src, live);
+      cp16(smem_addr(sm + P::Q + buf * P::QB) + r * (DHT * (int)sizeof(T)) + ((B16 ? k ^ (r & 7) : k) << 4), src, live);
     }
     cp_commit();
   };
@@ -494,25 +495,15 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM>::THREADS, 1) decode_kernel(co
       nxt.next_unit(a);
       load_queries(nxt, qbuf);
     }
-    // the sixteen rows of this warp as A operands (f32: dims 4 t .. 4 t + 3 of every sixteen, of which a step of eight takes
-    // two; K's are taken alike, and the sum over dims does not mind)
-    constexpr bool QREG = B16 || DHT <= 128;
-    uint32_t qf[QREG ? DHT / 16 : 1][B16 ? 4 : 8];
-    auto load_q = [&](int ks, uint32_t* f) {
-      if constexpr (B16) {
+    // bf16: the sixteen rows of this warp as A operands, outputs and statistics in the layout of the products: rows g and
+    // g + 8; f32: every lane has all rows' statistics and, of the outputs, its dims
+    uint32_t qf[B16 ? DHT / 16 : 1][4];
+    if constexpr (B16) {
+#pragma unroll
+      for (int ks = 0; ks < DHT / 16; ++ks) {
         const int row = 16 * wm + (lane & 15), c = 2 * ks + (lane >> 4);
-        ldsm4(f, smem_addr(Qs + row * DHT + ((c ^ (row & 7)) * VE)));
-      } else {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int row = 16 * wm + g + 8 * h;
-          *reinterpret_cast<uint4*>(f + 4 * h) = *reinterpret_cast<const uint4*>(Qs + row * DHT + ((4 * ks + t4) ^ ((row & 1) << 2)) * VE);
-        }
+        ldsm4(qf[ks], smem_addr(Qs + row * DHT + ((c ^ (row & 7)) * VE)));
       }
-    };
-    if constexpr (QREG) {
-#pragma unroll
-      for (int ks = 0; ks < DHT / 16; ++ks) load_q(ks, qf[ks]);
     }
     int qslot[2];
 #pragma unroll
@@ -520,12 +511,17 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM>::THREADS, 1) decode_kernel(co
       const int r = r0 + 16 * wm + g + 8 * h;
       qslot[h] = r < a.R ? cur.s.len - a.n_new + r / a.G : -1;
     }
-    float o[DHT / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    constexpr int OD = B16 ? DHT / 8 : RM, OE = B16 ? 4 : DHT / 32, MR = B16 ? 2 : RM;
+    float o[OD][OE], m[MR], l[MR];
 #pragma unroll
-    for (int d = 0; d < DHT / 8; ++d)
+    for (int r = 0; r < MR; ++r) {
+      m[r] = -INFINITY;
+      l[r] = 0.f;
+    }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[d][e] = 0.f;
-
+    for (int d = 0; d < OD; ++d)
+#pragma unroll
+      for (int e = 0; e < OE; ++e) o[d][e] = 0.f;
     int held = -1;  // the stage of this group's last tile, kept until its outputs have been in it
     for (; mine < n + seg; mine += NG) {
       const uint32_t base = smem_addr(sm + st * P::STAGE);
@@ -543,9 +539,13 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM>::THREADS, 1) decode_kernel(co
         group_sync();
       }
 
-  // ---- scores
-      float s[NT][4] = {};
+      // every row sees every token of the tile: no test a token
+      const bool all = live == FULL && j0 + TK - 1 <= cur.s.len - a.n_new &&
+                       (a.window == 0 || j0 + TK <= a.sinks || cur.s.len - 1 - j0 < a.window);
       if constexpr (B16) {
+      // ---- scores
+      float s[NT][4] = {};
+      {
         const int rr = ((lane >> 4) << 3) + (lane & 7), half = (lane >> 3) & 1;
         int krow[NT / 2];
 #pragma unroll
@@ -560,39 +560,7 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM>::THREADS, 1) decode_kernel(co
             mma16816(s[2 * n2], qf[ks], kf[0], kf[1]);
             mma16816(s[2 * n2 + 1], qf[ks], kf[2], kf[3]);
           }
-      } else {
-#pragma unroll
-        for (int ks = 0; ks < DHT / 16; ++ks) {
-          uint32_t q8[8];
-          if constexpr (!QREG) load_q(ks, q8);
-          const uint32_t* qr = QREG ? qf[QREG ? ks : 0] : q8;
-          uint32_t ah[2][4], al[2][4];  // the two steps of eight dims: rows g, g + 8 of dims (4 t, 4 t + 1), then (4 t + 2, 4 t + 3)
-#pragma unroll
-          for (int k2 = 0; k2 < 2; ++k2)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              split_tf32(__uint_as_float(qr[4 * (e & 1) + 2 * k2 + (e >> 1)]), ah[k2][e], al[k2][e]);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            const int row = 8 * nt + g;
-            const float4 k = *reinterpret_cast<const float4*>(stage + P::at(row, 4 * ks + t4, a.brs));
-            uint32_t bh[4], bl[4];
-            split_tf32(k.x, bh[0], bl[0]);
-            split_tf32(k.y, bh[1], bl[1]);
-            split_tf32(k.z, bh[2], bl[2]);
-            split_tf32(k.w, bh[3], bl[3]);
-#pragma unroll
-            for (int k2 = 0; k2 < 2; ++k2) {
-              mma1688(s[nt], al[k2], bh[2 * k2], bh[2 * k2 + 1]);
-              mma1688(s[nt], ah[k2], bl[2 * k2], bl[2 * k2 + 1]);
-              mma1688(s[nt], ah[k2], bh[2 * k2], bh[2 * k2 + 1]);
-            }
-          }
-        }
       }
-      // every row sees every token of the tile: no test a token
-      const bool all = live == FULL && j0 + TK - 1 <= cur.s.len - a.n_new &&
-                       (a.window == 0 || j0 + TK <= a.sinks || cur.s.len - 1 - j0 < a.window);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -652,7 +620,7 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM>::THREADS, 1) decode_kernel(co
           l[e >> 1] += s[nt][e];
         }
       // ---- outputs
-      if constexpr (B16) {
+      {
         // P as an A operand, in two bf16 terms: rounded to one it would add as much to the error as the output's own
         // rounding does
         const int rr = (((lane >> 3) & 1) << 3) + (lane & 7), half = lane >> 4;
@@ -677,28 +645,77 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM>::THREADS, 1) decode_kernel(co
             mma16816(o[2 * nb + 1], pl, vf[2], vf[3]);
           }
         }
+      }
       } else {
-        // a step of eight tokens takes them in the order 0, 2, 4, 6, 1, 3, 5, 7: the scores' own layout
+      // ---- scores: a lane a token, or a part of its dims (16-byte chunks, in turn)
+      constexpr int LPT = 32 / TK;
+      const int tok = lane % TK, part = lane / TK;
+      float s[RM];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          uint32_t ah[4], al[4];
-          split_tf32(s[nt][0], ah[0], al[0]);
-          split_tf32(s[nt][2], ah[1], al[1]);
-          split_tf32(s[nt][1], ah[2], al[2]);
-          split_tf32(s[nt][3], ah[3], al[3]);
-          const int v0 = 8 * nt + 2 * t4;
-          const float* V = reinterpret_cast<const float*>(stage + P::TILE);
+      for (int r = 0; r < RM; ++r) s[r] = 0.f;
+#pragma unroll 4
+      for (int i = 0; i < 16; ++i) {
+        const int c = i * LPT + part;
+        const float4 k = *reinterpret_cast<const float4*>(stage + P::at(tok, c, a.brs));
 #pragma unroll
-          for (int d = 0; d < DHT / 8; ++d) {
-            const int c = 2 * d + (g >> 2), w = g & 3;
-            uint32_t h0, l0, h1, l1;
-            split_tf32(V[P::at(v0, c, a.brs) / 4 + w], h0, l0);
-            split_tf32(V[P::at(v0 + 1, c, a.brs) / 4 + w], h1, l1);
-            mma1688(o[d], al, h0, h1);
-            mma1688(o[d], ah, l0, l1);
-            mma1688(o[d], ah, h0, h1);
+        for (int r = 0; r < RM; ++r) {
+          const float4 q = *reinterpret_cast<const float4*>(Qs + r * DHT + 4 * c);
+          s[r] = fmaf(q.x, k.x, s[r]);
+          s[r] = fmaf(q.y, k.y, s[r]);
+          s[r] = fmaf(q.z, k.z, s[r]);
+          s[r] = fmaf(q.w, k.w, s[r]);
+        }
+      }
+      const bool here = (live >> tok) & 1ull;
+      float* X = reinterpret_cast<float*>(sm + P::X) + grp * (TK * RM);  // p, [token][row]
+#pragma unroll
+      for (int r = 0; r < RM; ++r) {
+#pragma unroll
+        for (int x = TK; x < 32; x <<= 1) s[r] += __shfl_xor_sync(0xffffffffu, s[r], x);
+        const int row = r0 + r;
+        s[r] = here && row < a.R && (all || sees(a, cur.s.len - a.n_new + row / a.G, j0 + tok)) ? s[r] * a.sl2 : -INFINITY;
+        if (a.scores && row < a.R && part == 0)
+          a.scores[(((int64_t)cur.b * a.c.n_kv_heads + hk) * a.R + row) * a.x_stride + x0 + tok] = s[r];
+        const float mn = fmaxf(m[r], redux_max(s[r])), ms = mn == -INFINITY ? 0.f : mn;
+        if (mn > m[r]) {
+          const float f = exp2f(m[r] - ms);
+          l[r] *= f;
+          m[r] = mn;
+#pragma unroll
+          for (int e = 0; e < OE; ++e) o[r][e] *= f;
+        }
+        s[r] = exp2f(s[r] - ms);
+        l[r] += s[r];  // a lane's share
+      }
+      if (part == 0) {
+#pragma unroll
+        for (int r = 0; r < RM; r += 4) *reinterpret_cast<float4*>(X + tok * RM + r) = make_float4(s[r], s[r + 1], s[r + 2], s[r + 3]);
+      }
+      __syncwarp();
+      // ---- outputs: a lane DHT / 32 dims
+#pragma unroll 2
+      for (int k = 0; k < TK; ++k) {
+        float v[OE];
+        const uint8_t* row = stage + P::TILE;
+        if constexpr (OE == 2) {
+          *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(row + P::at(k, lane >> 1, a.brs) + 8 * (lane & 1));
+        } else {
+#pragma unroll
+          for (int e = 0; e < OE; e += 4) *reinterpret_cast<float4*>(v + e) = *reinterpret_cast<const float4*>(row + P::at(k, lane + 8 * e, a.brs));
+        }
+#pragma unroll
+        for (int r = 0; r < RM; r += 4) {
+          const float4 p = *reinterpret_cast<const float4*>(X + k * RM + r);
+#pragma unroll
+          for (int e = 0; e < OE; ++e) {
+            o[r][e] = fmaf(p.x, v[e], o[r][e]);
+            o[r + 1][e] = fmaf(p.y, v[e], o[r + 1][e]);
+            o[r + 2][e] = fmaf(p.z, v[e], o[r + 2][e]);
+            o[r + 3][e] = fmaf(p.w, v[e], o[r + 3][e]);
           }
         }
+      }
+      __syncwarp();
       }
       // the stage is free again, but for the last one's
       if (mine + NG < n + seg) {
@@ -716,16 +733,32 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM>::THREADS, 1) decode_kernel(co
 
     // ---- the groups' outputs together: each puts its own into its last tile's stage
     group_sync();
+    float* to = reinterpret_cast<float*>(sm + (held >= 0 ? held : 0) * P::STAGE);
+    if constexpr (B16) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
-      l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
-      const int row = 16 * wm + g + 8 * h;
-      if (t4 == 0) stats[grp * ROWS + row] = make_float2(m[h], l[h]);
-      if (held >= 0) {
-        float* to = reinterpret_cast<float*>(sm + held * P::STAGE);
+      for (int h = 0; h < 2; ++h) {
+        l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
+        l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
+        const int row = 16 * wm + g + 8 * h;
+        if (t4 == 0) stats[grp * ROWS + row] = make_float2(m[h], l[h]);
+        if (held >= 0) {
 #pragma unroll
-        for (int d = 0; d < DHT / 8; ++d) *reinterpret_cast<float2*>(to + P::sum_at(row, 8 * d + 2 * t4)) = make_float2(o[d][2 * h], o[d][2 * h + 1]);
+          for (int d = 0; d < DHT / 8; ++d) *reinterpret_cast<float2*>(to + P::sum_at(row, 8 * d + 2 * t4)) = make_float2(o[d][2 * h], o[d][2 * h + 1]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int r = 0; r < RM; ++r) {
+        const float sum = warp_sum(lane < TK ? l[r] : 0.f);
+        if (lane == 0) stats[grp * ROWS + r] = make_float2(m[r], sum);
+        if (held >= 0) {
+          if constexpr (OE == 2) {
+            *reinterpret_cast<float2*>(to + P::sum_at(r, 2 * lane)) = make_float2(o[r][0], o[r][1]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < OE; e += 4) *reinterpret_cast<float4*>(to + P::sum_at(r, 4 * lane + 32 * e)) = make_float4(o[r][e], o[r][e + 1], o[r][e + 2], o[r][e + 3]);
+          }
+        }
       }
     }
     if (lane == 0 && wm == 0) last_stage[grp] = held;
@@ -881,8 +914,7 @@ __global__ void __launch_bounds__(256) decode_join_kernel(const __grid_constant_
   finish<T>(a, b, hk, row, d, s, M, L, any != 0);
 }
 
-// weights_out = weights_in + the rows' softmax weights, in row order: a thread four slots, 256 apart
-constexpr int WROWS = 8;
+// weights_out = weights_in + the rows' softmax weights, in row order: a thread four slots, four rows on their way at once
 template <int TK>
 __global__ void __launch_bounds__(256) decode_weights_kernel(const __grid_constant__ DecodeArgs a, int chunks) {
   pdl_wait();
@@ -890,37 +922,31 @@ __global__ void __launch_bounds__(256) decode_weights_kernel(const __grid_consta
   const int64_t unit = blockIdx.x / chunks;  // b * kv heads + head
   const int b = (int)(unit / a.c.n_kv_heads);
   const Seen s = seen_of<TK>(a, b);
+  const int j = (int)(blockIdx.x - unit * chunks) * 1024 + 4 * (int)threadIdx.x, n = s.len - j < 4 ? s.len - j : 4;
+  if (n <= 0) return;
   const float* lse2 = a.lse2 + unit * a.R;
-  const int j0 = (int)(blockIdx.x - unit * chunks) * 1024 + (int)threadIdx.x;
-  if (j0 >= s.len) return;
+  const int tile = j / TK;
+  const int x = tile < s.sink_tiles ? j : tile >= s.w_tile ? j + (s.sink_tiles - s.w_tile) * TK : -1;
   float w[4];
-  const float* sc[4];
-  bool on[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int j = j0 + 256 * i, tile = j / TK;
-    const int x = tile < s.sink_tiles ? j : tile >= s.w_tile ? j + (s.sink_tiles - s.w_tile) * TK : -1;
-    on[i] = j < s.len && x >= 0;
-    w[i] = j < s.len && a.w_in ? a.w_in[unit * a.w_stride + j] : 0.f;
-    sc[i] = a.scores + unit * a.R * a.x_stride + (on[i] ? x : 0);
-  }
-  for (int r0 = 0; r0 < a.R; r0 += WROWS) {
-    float z[WROWS], v[WROWS][4];
-#pragma unroll
-    for (int r = 0; r < WROWS; ++r) {
-      z[r] = r0 + r < a.R ? lse2[r0 + r] : -INFINITY;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[r][i] = on[i] && r0 + r < a.R ? sc[i][(int64_t)(r0 + r) * a.x_stride] : -INFINITY;
+  for (int i = 0; i < 4; ++i) w[i] = i < n && a.w_in ? a.w_in[unit * a.w_stride + j + i] : 0.f;
+  if (x >= 0) {
+    const float* sc = a.scores + unit * a.R * a.x_stride + x;
+#pragma unroll 4
+    for (int r = 0; r < a.R; ++r) {
+      const float4 v = *reinterpret_cast<const float4*>(sc + (int64_t)r * a.x_stride);
+      const float z = lse2[r];
+      if (z != -INFINITY) {
+        w[0] += ex2_fast(v.x - z);
+        w[1] += ex2_fast(v.y - z);
+        w[2] += ex2_fast(v.z - z);
+        w[3] += ex2_fast(v.w - z);
+      }
     }
-#pragma unroll
-    for (int r = 0; r < WROWS; ++r)
-      if (z[r] != -INFINITY)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] += ex2_fast(v[r][i] - z[r]);
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    if (j0 + 256 * i < s.len) a.w_out[unit * a.w_stride + j0 + 256 * i] = w[i];
+    if (i < n) a.w_out[unit * a.w_stride + j + i] = w[i];
 }
 
 // ---- host ------------------------------------------------------------------------------
@@ -936,8 +962,8 @@ DecodeLayout layout_of(const ra_attention_decode_args& p) {
   L.R = G * p.n_new;
   L.dht = p.cache.head_dim <= 64 ? 64 : p.cache.head_dim <= 128 ? 128 : 256;
   // rows that one pass over K and V serves: 16, 32 or 64 (bf16; 16 at head dims above 128, whose outputs fill the
-  // registers), 16 (f32)
-  L.rows = !b16 || L.R <= 16 || L.dht == 256 ? 16 : L.R <= 32 ? 32 : 64;
+  // registers), 4, 8 or 16 (f32)
+  L.rows = !b16 ? (L.R <= 4 ? 4 : L.R <= 8 ? 8 : 16) : L.R <= 16 || L.dht == 256 ? 16 : L.R <= 32 ? 32 : 64;
   L.groups = (L.R + L.rows - 1) / L.rows;
   L.grid = device_sm_count();
   // A unit has about grid / units parts; the last CTA reads them all, alone on its SM (about 20 us a MB), while a kernel of
@@ -965,15 +991,15 @@ DecodeLayout layout_of(const ra_attention_decode_args& p) {
   return L;
 }
 
-template <typename T, int DHT, int WM, bool TMA>
+template <typename T, int DHT, int WM, int RM, bool TMA>
 cudaError_t launch_kernel(const CUtensorMap& k, const CUtensorMap& v, const DecodeArgs& a, cudaStream_t st) {
-  using P = Plan<T, DHT, WM>;
-  cudaError_t e = allow_smem(decode_kernel<T, DHT, WM, TMA>, P::BYTES);
-  return e == cudaSuccess ? launch_pdl(decode_kernel<T, DHT, WM, TMA>, dim3(a.grid), dim3(P::THREADS), (size_t)P::BYTES, st, k, v, a) : e;
+  using P = Plan<T, DHT, WM, RM>;
+  cudaError_t e = allow_smem(decode_kernel<T, DHT, WM, RM, TMA>, P::BYTES);
+  return e == cudaSuccess ? launch_pdl(decode_kernel<T, DHT, WM, RM, TMA>, dim3(a.grid), dim3(P::THREADS), (size_t)P::BYTES, st, k, v, a) : e;
 }
-template <typename T, int DHT, int WM>
+template <typename T, int DHT, int WM, int RM>
 cudaError_t launch(DecodeArgs& a, cudaStream_t st) {
-  using P = Plan<T, DHT, WM>;
+  using P = Plan<T, DHT, WM, RM>;
   const ra_kv_cache& c = a.c;
   // boxes of 2^brs slots of a page: a pool is [pages x kv heads][page_size][head_dim]
   a.brs = c.page_size % 32 == 0 && P::TK >= 32 ? 5 : c.page_size % 16 == 0 && P::TK >= 16 ? 4 : 3;
@@ -987,7 +1013,7 @@ cudaError_t launch(DecodeArgs& a, cudaStream_t st) {
                           a.whole_rows != 0);
   };
   const bool tma = c.page_size % 8 == 0 && planes <= INT32_MAX && map(&k, c.k_dev) && map(&v, c.v_dev);
-  cudaError_t e = tma ? launch_kernel<T, DHT, WM, true>(k, v, a, st) : launch_kernel<T, DHT, WM, false>(k, v, a, st);
+  cudaError_t e = tma ? launch_kernel<T, DHT, WM, RM, true>(k, v, a, st) : launch_kernel<T, DHT, WM, RM, false>(k, v, a, st);
   note_launch(1);
   if (e == cudaSuccess && !a.join) {
     e = launch_pdl(decode_join_kernel<T, DHT, P::TK, P::ROWS>, dim3((unsigned)((int64_t)a.batch * c.n_kv_heads * a.R)), dim3(256), 0, st, a);
@@ -999,6 +1025,15 @@ cudaError_t launch(DecodeArgs& a, cudaStream_t st) {
   if (n > INT32_MAX) return cudaErrorNotSupported;
   note_launch(1);
   return launch_pdl(decode_weights_kernel<P::TK>, dim3((unsigned)n), dim3(256), 0, st, a, chunks);
+}
+
+template <int DHT>
+cudaError_t launch_f32(DecodeArgs& a, int rows, cudaStream_t st) {
+  return rows == 4 ? launch<float, DHT, 1, 4>(a, st) : rows == 8 ? launch<float, DHT, 1, 8>(a, st) : launch<float, DHT, 1, 16>(a, st);
+}
+template <int DHT>
+cudaError_t launch_bf16(DecodeArgs& a, int rows, cudaStream_t st) {
+  return rows == 16 ? launch<bf16, DHT, 1, 16>(a, st) : rows == 32 ? launch<bf16, DHT, 2, 32>(a, st) : launch<bf16, DHT, 4, 64>(a, st);
 }
 
 }  // namespace
@@ -1040,16 +1075,8 @@ cudaError_t attention_decode(const ra_attention_decode_args& p, cudaStream_t st)
   for (int i = 0; i < 31; ++i)
     if (p.cache.page_size == 1 << i) a.page_shift = i;
   a.sl2 = p.scale * kLog2e;
-  cudaError_t e;
-  if (p.cache.dtype == RA_F32)
-    e = L.dht == 64 ? launch<float, 64, 1>(a, st) : L.dht == 128 ? launch<float, 128, 1>(a, st) : launch<float, 256, 1>(a, st);
-  else if (L.dht == 64)
-    e = L.rows == 16 ? launch<bf16, 64, 1>(a, st) : L.rows == 32 ? launch<bf16, 64, 2>(a, st) : launch<bf16, 64, 4>(a, st);
-  else if (L.dht == 128)
-    e = L.rows == 16 ? launch<bf16, 128, 1>(a, st) : L.rows == 32 ? launch<bf16, 128, 2>(a, st) : launch<bf16, 128, 4>(a, st);
-  else
-    e = launch<bf16, 256, 1>(a, st);
-  return e;
+  if (p.cache.dtype == RA_F32) return L.dht == 64 ? launch_f32<64>(a, L.rows, st) : L.dht == 128 ? launch_f32<128>(a, L.rows, st) : launch_f32<256>(a, L.rows, st);
+  return L.dht == 64 ? launch_bf16<64>(a, L.rows, st) : L.dht == 128 ? launch_bf16<128>(a, L.rows, st) : launch<bf16, 256, 1, 16>(a, st);
 }
 
 }  // namespace ra
