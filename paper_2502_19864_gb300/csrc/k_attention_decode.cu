@@ -80,45 +80,51 @@ __device__ __forceinline__ int first_slot(const Seen& s, int tile) {
 __device__ __forceinline__ bool sees(const DecodeArgs& a, int i, int j) {
   return j <= i && (a.window == 0 || i - j < a.window || j < a.sinks);
 }
-__device__ __forceinline__ int64_t warp_sum64(int64_t v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
-
 // How the tiles are dealt: unit (b, u), u = kv head * groups + row group, has tiles(b) tiles; units in order.
-// One warp computes; `total` tiles go to as many CTAs as have LEAST tiles each, at most the grid.
+// One warp computes; `total` tiles go to as many CTAs as have LEAST tiles each, or one a unit, at most the grid: the
+// first `extra` of them take base + 1 tiles, the others base.  (The host has checked that 32 bits hold the total.)
+__device__ __forceinline__ int warp_sum_int(int v) { return (int)__reduce_add_sync(0xffffffffu, (unsigned)v); }
 template <int TK, int LEAST>
 struct Deal {
-  int64_t total;
-  int workers;
+  int total, workers, base, extra;
   __device__ __forceinline__ int tiles(const DecodeArgs& a, int b) const { return seen_of<TK>(a, b).tiles; }
   __device__ void count(const DecodeArgs& a, int lane) {
     const int units = a.c.n_kv_heads * a.groups;
-    int64_t t = 0;
-    for (int b = lane; b < a.batch; b += 32) t += (int64_t)tiles(a, b) * units;
-    total = warp_sum64(t);
-    const int64_t w = (total + LEAST - 1) / LEAST;
-    workers = w < a.grid ? (int)w : a.grid;
+    int t = 0, live = 0;
+    for (int b = lane; b < a.batch; b += 32) {
+      const int n = tiles(a, b);
+      t += n * units;
+      live += n > 0 ? units : 0;
+    }
+    total = warp_sum_int(t);
+    live = warp_sum_int(live);
+    int w = (total + LEAST - 1) / LEAST;
+    if (w < live) w = live;  // (short sequences: a CTA a unit)
+    workers = w < a.grid ? w : a.grid;
+    base = workers ? (int)((unsigned)total / (unsigned)workers) : 0;
+    extra = total - base * workers;
   }
-  __device__ __forceinline__ int64_t start(int cta) const { return total * cta / workers; }
-  __device__ __forceinline__ int owner(int64_t tile) const { return (int)(((tile + 1) * workers - 1) / total); }
+  __device__ __forceinline__ int start(int cta) const { return cta * base + (cta < extra ? cta : extra); }
+  __device__ __forceinline__ int owner(int tile) const {
+    const int more = extra * (base + 1);
+    return tile < more ? (int)((unsigned)tile / (unsigned)(base + 1)) : extra + (int)((unsigned)(tile - more) / (unsigned)base);
+  }
   // the sequence that tile `at` belongs to, and its first tile (same in all lanes)
-  __device__ void find(const DecodeArgs& a, int64_t at, int lane, int& b, int64_t& first) const {
+  __device__ void find(const DecodeArgs& a, int at, int lane, int& b, int& first) const {
     const int units = a.c.n_kv_heads * a.groups;
-    int64_t acc = 0;
-    for (int base = 0;; base += 32) {
-      const int64_t t = base + lane < a.batch ? (int64_t)tiles(a, base + lane) * units : 0;
-      int64_t incl = t;
+    int acc = 0;
+    for (int base_b = 0;; base_b += 32) {
+      const int t = base_b + lane < a.batch ? tiles(a, base_b + lane) * units : 0;
+      int incl = t;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const int64_t v = __shfl_up_sync(0xffffffffu, incl, o);
+        const int v = __shfl_up_sync(0xffffffffu, incl, o);
         if (lane >= o) incl += v;
       }
       const uint32_t past = __ballot_sync(0xffffffffu, acc + incl > at);
       if (past) {
         const int l = __ffs(past) - 1;
-        b = base + l;
+        b = base_b + l;
         first = acc + __shfl_sync(0xffffffffu, incl - t, l);
         return;
       }
@@ -126,11 +132,11 @@ struct Deal {
     }
   }
   // the first tile of sequence b's unit u
-  __device__ int64_t first_of(const DecodeArgs& a, int b, int u, int lane) const {
+  __device__ int first_of(const DecodeArgs& a, int b, int u, int lane) const {
     const int units = a.c.n_kv_heads * a.groups;
-    int64_t t = 0;
-    for (int i = lane; i < b; i += 32) t += (int64_t)tiles(a, i) * units;
-    return warp_sum64(t) + (int64_t)u * tiles(a, b);
+    int t = 0;
+    for (int i = lane; i < b; i += 32) t += tiles(a, i) * units;
+    return warp_sum_int(t) + u * tiles(a, b);
   }
 };
 
@@ -197,7 +203,7 @@ __device__ __forceinline__ float redux_max(float x) {
 }
 
 // ---------------------------------------------------------------------------------------
-// bf16: WM warps a group, each on sixteen of the unit's 16 WM rows; f32: WM = 1 and RM rows.  NG groups and two copying warps a CTA, one CTA an SM.  A
+// WM warps a group, each on RM of the unit's rows (bf16: sixteen).  NG groups and two copying warps a CTA, one CTA an SM.  A
 // stage holds K and V of TK tokens, rows of DHT values (zeros past head_dim) whose 16-byte chunks are permuted so that the
 // reads below meet no bank twice.
 //   TMA   pages of a multiple of 8 tokens: boxes of BR slots of a page, BR the largest of 32, 16 and 8 that divides a page and
@@ -208,8 +214,9 @@ template <typename T, int DHT, int WM, int RM>
 struct Plan {
   static constexpr bool B16 = sizeof(T) == 2;
   static constexpr int TK = (DHT == 256 ? 16 : WM == 4 || DHT == 64 ? 64 : 32) / (B16 ? 1 : 2);
-  // six warps and the two that copy may have 255 registers each (four row groups: eight and two, 168)
-  static constexpr int NG = WM == 4 ? 2 : WM == 2 ? 3 : !B16 && DHT == 256 ? 5 : 6, WORKERS = 32 * WM * NG, THREADS = WORKERS + 64, ROWS = RM;
+  // bf16: six warps and the two that copy may have 255 registers each (four row groups: eight and two, 168); f32: twelve and
+  // two with 128, as the arithmetic is latency (head dims above 128: ten and two with 168)
+  static constexpr int NG = B16 ? (WM == 4 ? 2 : 6 / WM) : (DHT == 256 ? 10 : 12) / WM, WORKERS = 32 * WM * NG, THREADS = WORKERS + 64, ROWS = RM * WM;
   static constexpr int TILE = TK * DHT * (int)sizeof(T), STAGE = 2 * TILE, STAGES = (!B16 && DHT == 256 ? 160 : 192) * 1024 / STAGE;
   static constexpr int Q = STAGES * STAGE, QB = ROWS * DHT * (int)sizeof(T), STATS = Q + 2 * QB, MASK = STATS + NG * ROWS * 8;
   static_assert(ROWS * DHT * 4 <= STAGE, "a group's outputs are put into the stage of its last tile");
@@ -221,11 +228,11 @@ struct Plan {
   static __device__ __forceinline__ int chunk_at(int r, int c) { return ((c & 7) ^ (r & 7)) << 4; }
   static __device__ __forceinline__ int at(int r, int c, int brs) { return row_at(r, brs) + ((c >> 3) << (brs + 7)) + chunk_at(r, c); }
   static constexpr int ATOMS = DHT * (int)sizeof(T) / 128, MBAR = MASK + STAGES * 8, PLACES = MBAR + 2 * STAGES * 8,
-                       X = (PLACES + 2 * 32 * 8 + 15) / 16 * 16, BYTES = X + (B16 ? 0 : NG * TK * ROWS * 4);
+                       X = (PLACES + 2 * 32 * 8 + 15) / 16 * 16, QSLOT = X + (B16 ? 0 : NG * TK * ROWS * 4), BYTES = QSLOT + ROWS * 4;
   // a stage is filled by the same warp and read by the same group every time round, so that each has seen every phase of
   // its barriers: a wait by parity for a phase that is two ahead would return at once
   static_assert(STAGES % 2 == 0 && STAGES % NG == 0, "stages belong to copying warps and to groups");
-  static_assert(STATS % 16 == 0 && MBAR % 8 == 0 && X % 16 == 0 && BYTES <= 226 * 1024, "shared memory");
+  static_assert(STATS % 16 == 0 && MBAR % 8 == 0 && X % 16 == 0 && QSLOT % 4 == 0 && BYTES <= 226 * 1024, "shared memory");
 };
 
 template <typename T>
@@ -268,8 +275,8 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM, RM>::THREADS, 1) decode_kerne
   constexpr int TK = P::TK, S = P::STAGES, NG = P::NG, ROWS = P::ROWS, VE = 16 / (int)sizeof(T), CH = DHT / VE, NT = TK / 8;
   constexpr uint64_t FULL = TK == 64 ? ~0ull : (1ull << (TK & 63)) - 1;
   extern __shared__ __align__(1024) uint8_t sm[];
-  __shared__ int64_t run_start, run_total, run_in;
-  __shared__ int run_n, run_b, run_workers, joins;
+  __shared__ Deal<TK, SHARE> deal;
+  __shared__ int run_start, run_in, run_n, run_b, joins;
   __shared__ int last_stage[NG];
   __shared__ volatile int abort_sh;
   uint64_t* full = reinterpret_cast<uint64_t*>(sm + P::MBAR);  // [S]: a stage's copies have landed
@@ -284,7 +291,13 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM, RM>::THREADS, 1) decode_kerne
     tc::mbar_init(&full[tid], TMA ? 1 : 33);
     tc::mbar_init(&empty[tid], WM);
   }
-  if (tid == 0) abort_sh = 0;
+  if (tid == 0) {
+    abort_sh = 0;
+    if (TMA) {
+      asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmK)) : "memory");
+      asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmV)) : "memory");
+    }
+  }
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   pdl_wait();
@@ -292,20 +305,18 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM, RM>::THREADS, 1) decode_kerne
   if (warp == 0) {
     Deal<TK, SHARE> d;
     d.count(a, lane);
-    int b = 0;
-    int64_t first = 0, n = 0, s = 0;
+    int b = 0, first = 0, n = 0, s = 0;
     if ((int)blockIdx.x < d.workers) {
       s = d.start(blockIdx.x);
       n = d.start(blockIdx.x + 1) - s;
       d.find(a, s, lane, b, first);
     }
     if (lane == 0) {
-      run_n = (int)n;
+      run_n = n;
       run_b = b;
       run_in = s - first;  // of its sequence's tiles
       run_start = s;
-      run_total = d.total;
-      run_workers = d.workers;
+      deal = d;
     }
   }
   __syncthreads();
@@ -322,8 +333,8 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM, RM>::THREADS, 1) decode_kerne
   Cursor<TK> cur;
   cur.b = run_b;
   cur.enter(a);
-  cur.u = (int)(run_in / cur.tiles);
-  cur.tile = (int)(run_in - (int64_t)cur.u * cur.tiles);
+  cur.u = run_in / cur.tiles;
+  cur.tile = run_in - cur.u * cur.tiles;
 
   if (warp >= P::WORKERS / 32) {
     // ------------------------------------------------------------ copies: the two warps take the tiles in turn
@@ -357,6 +368,7 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM, RM>::THREADS, 1) decode_kerne
       const int n = c.tiles - c.tile < left ? c.tiles - c.tile : left;
       return n < batch ? n : batch;
     };
+    const uint32_t all_boxes = TMA ? (uint32_t)((1ull << (nb & 63)) - 1) : 0;
     int done = 0, st = -1, round = 0, tile = -1, many = batch_of(cur, n_tiles);
     bool ok = true;
     look_up(cur, many, next_place, next_off);
@@ -387,9 +399,9 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM, RM>::THREADS, 1) decode_kerne
         }
         if ((tile & 1) != odd) continue;
         const int slot0 = first_slot<TK>(at.s, at.tile + t);
-        const uint32_t boxes = TMA ? (there >> (t * nb)) & (uint32_t)((1ull << nb) - 1) : 0;
+        const uint32_t boxes = TMA ? (there >> (t * nb)) & all_boxes : 0;
         uint64_t live = FULL;
-        if (!TMA || boxes != (uint32_t)((1ull << nb) - 1) || slot0 + TK > at.s.len || (slot0 < at.s.w0 && slot0 + TK > at.s.n_sink)) {
+        if (!TMA || boxes != all_boxes || slot0 + TK > at.s.len || (slot0 < at.s.w0 && slot0 + TK > at.s.n_sink)) {
           live = 0;
 #pragma unroll
           for (int h = 0; h < (TK + 31) / 32; ++h) {
@@ -505,14 +517,25 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM, RM>::THREADS, 1) decode_kerne
         ldsm4(qf[ks], smem_addr(Qs + row * DHT + ((c ^ (row & 7)) * VE)));
       }
     }
+    // the rows' own slots
+    int* qslots = reinterpret_cast<int*>(sm + P::QSLOT);
     int qslot[2];
+    if (!B16) {
+      for (int r = tid; r < ROWS; r += P::WORKERS) qslots[r] = r0 + r < a.R ? cur.s.len - a.n_new + (r0 + r) / a.G : -1;
+      tc::named_sync(1, P::WORKERS);
+    }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int r = r0 + 16 * wm + g + 8 * h;
-      qslot[h] = r < a.R ? cur.s.len - a.n_new + r / a.G : -1;
+      qslot[h] = B16 && r < a.R ? cur.s.len - a.n_new + r / a.G : -1;
     }
-    constexpr int OD = B16 ? DHT / 8 : RM, OE = B16 ? 4 : DHT / 32, MR = B16 ? 2 : RM;
+    constexpr int OD = B16 ? DHT / 8 : 1, OE = B16 ? 4 : DHT / 32, MR = B16 ? 2 : RM;
     float o[OD][OE], m[MR], l[MR];
+    float2 o2[B16 ? 1 : RM / 2][OE];  // (f32: pairs of rows, for packed products)
+#pragma unroll
+    for (int r = 0; r < (B16 ? 1 : RM / 2); ++r)
+#pragma unroll
+      for (int e = 0; e < OE; ++e) o2[r][e] = f2(0.f);
 #pragma unroll
     for (int r = 0; r < MR; ++r) {
       m[r] = -INFINITY;
@@ -651,29 +674,32 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM, RM>::THREADS, 1) decode_kerne
       constexpr int LPT = 32 / TK;
       const int tok = lane % TK, part = lane / TK;
       float s[RM];
+      {
+        float2 s2[RM];
 #pragma unroll
-      for (int r = 0; r < RM; ++r) s[r] = 0.f;
+        for (int r = 0; r < RM; ++r) s2[r] = f2(0.f);
 #pragma unroll 4
-      for (int i = 0; i < 16; ++i) {
-        const int c = i * LPT + part;
-        const float4 k = *reinterpret_cast<const float4*>(stage + P::at(tok, c, a.brs));
+        for (int i = 0; i < 16; ++i) {
+          const int c = i * LPT + part;
+          const float4 k = *reinterpret_cast<const float4*>(stage + P::at(tok, c, a.brs));
 #pragma unroll
-        for (int r = 0; r < RM; ++r) {
-          const float4 q = *reinterpret_cast<const float4*>(Qs + r * DHT + 4 * c);
-          s[r] = fmaf(q.x, k.x, s[r]);
-          s[r] = fmaf(q.y, k.y, s[r]);
-          s[r] = fmaf(q.z, k.z, s[r]);
-          s[r] = fmaf(q.w, k.w, s[r]);
+          for (int r = 0; r < RM; ++r) {
+            const float4 q = *reinterpret_cast<const float4*>(Qs + (RM * wm + r) * DHT + 4 * c);
+            s2[r] = __ffma2_rn(make_float2(q.x, q.y), make_float2(k.x, k.y), s2[r]);
+            s2[r] = __ffma2_rn(make_float2(q.z, q.w), make_float2(k.z, k.w), s2[r]);
+          }
         }
+#pragma unroll
+        for (int r = 0; r < RM; ++r) s[r] = s2[r].x + s2[r].y;
       }
       const bool here = (live >> tok) & 1ull;
-      float* X = reinterpret_cast<float*>(sm + P::X) + grp * (TK * RM);  // p, [token][row]
+      float* X = reinterpret_cast<float*>(sm + P::X) + warp * (TK * RM);  // p, [token][row]
 #pragma unroll
       for (int r = 0; r < RM; ++r) {
 #pragma unroll
         for (int x = TK; x < 32; x <<= 1) s[r] += __shfl_xor_sync(0xffffffffu, s[r], x);
-        const int row = r0 + r;
-        s[r] = here && row < a.R && (all || sees(a, cur.s.len - a.n_new + row / a.G, j0 + tok)) ? s[r] * a.sl2 : -INFINITY;
+        const int row = r0 + RM * wm + r;
+        s[r] = here && row < a.R && (all || sees(a, qslots[RM * wm + r], j0 + tok)) ? s[r] * a.sl2 : -INFINITY;
         if (a.scores && row < a.R && part == 0)
           a.scores[(((int64_t)cur.b * a.c.n_kv_heads + hk) * a.R + row) * a.x_stride + x0 + tok] = s[r];
         const float mn = fmaxf(m[r], redux_max(s[r])), ms = mn == -INFINITY ? 0.f : mn;
@@ -682,7 +708,7 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM, RM>::THREADS, 1) decode_kerne
           l[r] *= f;
           m[r] = mn;
 #pragma unroll
-          for (int e = 0; e < OE; ++e) o[r][e] *= f;
+          for (int e = 0; e < OE; ++e) (r & 1 ? o2[r / 2][e].y : o2[r / 2][e].x) *= f;
         }
         s[r] = exp2f(s[r] - ms);
         l[r] += s[r];  // a lane's share
@@ -708,10 +734,8 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM, RM>::THREADS, 1) decode_kerne
           const float4 p = *reinterpret_cast<const float4*>(X + k * RM + r);
 #pragma unroll
           for (int e = 0; e < OE; ++e) {
-            o[r][e] = fmaf(p.x, v[e], o[r][e]);
-            o[r + 1][e] = fmaf(p.y, v[e], o[r + 1][e]);
-            o[r + 2][e] = fmaf(p.z, v[e], o[r + 2][e]);
-            o[r + 3][e] = fmaf(p.w, v[e], o[r + 3][e]);
+            o2[r / 2][e] = __ffma2_rn(make_float2(p.x, p.y), f2(v[e]), o2[r / 2][e]);
+            o2[r / 2 + 1][e] = __ffma2_rn(make_float2(p.z, p.w), f2(v[e]), o2[r / 2 + 1][e]);
           }
         }
       }
@@ -750,13 +774,15 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM, RM>::THREADS, 1) decode_kerne
 #pragma unroll
       for (int r = 0; r < RM; ++r) {
         const float sum = warp_sum(lane < TK ? l[r] : 0.f);
-        if (lane == 0) stats[grp * ROWS + r] = make_float2(m[r], sum);
+        const int row = RM * wm + r;
+        if (lane == 0) stats[grp * ROWS + row] = make_float2(m[r], sum);
         if (held >= 0) {
+          auto of = [&](int e) { return r & 1 ? o2[r / 2][e].y : o2[r / 2][e].x; };
           if constexpr (OE == 2) {
-            *reinterpret_cast<float2*>(to + P::sum_at(r, 2 * lane)) = make_float2(o[r][0], o[r][1]);
+            *reinterpret_cast<float2*>(to + P::sum_at(row, 2 * lane)) = make_float2(of(0), of(1));
           } else {
 #pragma unroll
-            for (int e = 0; e < OE; e += 4) *reinterpret_cast<float4*>(to + P::sum_at(r, 4 * lane + 32 * e)) = make_float4(o[r][e], o[r][e + 1], o[r][e + 2], o[r][e + 3]);
+            for (int e = 0; e < OE; e += 4) *reinterpret_cast<float4*>(to + P::sum_at(row, 4 * lane + 32 * e)) = make_float4(of(e), of(e + 1), of(e + 2), of(e + 3));
           }
         }
       }
@@ -793,13 +819,13 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM, RM>::THREADS, 1) decode_kerne
     }
     if (!whole && a.join) {
       // the last CTA to come here has all parts
-      __threadfence();
       tc::named_sync(1, P::WORKERS);
-      const int64_t first = run_start + n - cur.tile;  // the unit's first tile
-      const int c0 = (int)(((first + 1) * run_workers - 1) / run_total);
+      const int first = run_start + n - cur.tile;  // the unit's first tile
+      const int c0 = deal.owner(first);
       if (tid == 0) {
-        const int c1 = (int)(((first + cur.tiles) * run_workers - 1) / run_total);
+        const int c1 = deal.owner(first + cur.tiles - 1);
         unsigned* count = a.done + (int64_t)cur.b * (a.c.n_kv_heads * a.groups) + cur.u;
+        __threadfence();  // (of all threads' parts: the barrier came before)
         const unsigned before = atomicAdd(count, 1u);
         joins = before == (unsigned)(c1 - c0) ? c1 - c0 + 1 : 0;
         if (joins) *count = 0;
@@ -809,26 +835,42 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM, RM>::THREADS, 1) decode_kerne
       const int parts = joins;
       if (parts) {
         // part p's slot: the first is its CTA's last segment, unless the unit starts that CTA's run
-        const bool starts = run_total * c0 / run_workers == first;
-        auto ml_of = [&](int p, int r) { return __ldcg(&a.part_ml[(2 * (int64_t)(c0 + p) + (p == 0 && !starts ? 1 : 0)) * ROWS + r]); };
-        const int rows = a.R - r0 < ROWS ? a.R - r0 : ROWS;
-        for (int e = tid; e < rows * (dh / 4); e += P::WORKERS) {
-          const int r = e / (dh / 4), d = (e - r * (dh / 4)) * 4;
+        const bool starts = deal.start(c0) == first;
+        const int rows = a.R - r0 < ROWS ? a.R - r0 : ROWS, per = dh / 4;
+        for (int e = tid; e < rows * per; e += P::WORKERS) {
+          const int r = e / per, d = (e - r * per) * 4;
           float M = -INFINITY, L = 0.f;
           bool any = false;
-#pragma unroll 8
-          for (int p = 0; p < parts; ++p) M = fmaxf(M, ml_of(p, r).x);
           float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-          for (int p = 0; p < parts; ++p) {
-            const float2 ml = ml_of(p, r);
-            const float4 x = __ldcg(reinterpret_cast<const float4*>(a.part_o + ((2 * (int64_t)(c0 + p) + (p == 0 && !starts ? 1 : 0)) * ROWS + r) * DHT + d));
-            if (counts(ml)) {
-              const float f = ex2_fast(ml.x - M);
-              any = true;
-              L = fmaf(ml.y, f, L);
-              v = fma4(x, f, v);
+          for (int p0 = 0; p0 < parts; p0 += 8) {  // eight parts on their way at once
+            float2 ml[8];
+            float4 x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int p = p0 + i, at = (2 * (c0 + p) + (p == 0 && !starts ? 1 : 0)) * ROWS + r;
+              ml[i] = make_float2(-INFINITY, 0.f);
+              if (p < parts) {
+                ml[i] = __ldcg(&a.part_ml[at]);
+                x[i] = __ldcg(reinterpret_cast<const float4*>(a.part_o + (int64_t)at * DHT + d));
+              }
             }
+            float Mn = M;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) Mn = fmaxf(Mn, ml[i].x);
+            if (any) {
+              const float f = ex2_fast(M - Mn);
+              L *= f;
+              v = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
+            }
+            M = Mn;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              if (counts(ml[i])) {
+                const float f = ex2_fast(ml[i].x - M);
+                any = true;
+                L = fmaf(ml[i].y, f, L);
+                v = fma4(x[i], f, v);
+              }
           }
           finish<T>(a, cur.b, hk, r0 + r, d, v, M, L, any);
         }
@@ -865,7 +907,7 @@ __global__ void __launch_bounds__(256) decode_join_kernel(const __grid_constant_
     const int tiles = d.tiles(a, b);
     if (tid == 0) sh_parts = 0;
     if (tiles > 0) {
-      const int64_t first = d.first_of(a, b, hk * a.groups + grp, tid);
+      const int first = d.first_of(a, b, hk * a.groups + grp, tid);
       if (tid == 0) {
         sh_c0 = d.owner(first);
         sh_parts = d.owner(first + tiles - 1) - sh_c0 + 1;
@@ -1012,6 +1054,8 @@ cudaError_t launch(DecodeArgs& a, cudaStream_t st) {
     return tma_map_planes(m, p, sizeof(T) == 2 ? DT_BF16 : DT_F32, (int)planes, c.page_size, c.head_dim, 128 / (int)sizeof(T), 1 << a.brs,
                           a.whole_rows != 0);
   };
+  // tiles are counted in 32 bits
+  if ((int64_t)a.batch * c.n_kv_heads * a.groups * ((a.max_len + P::TK - 1) / P::TK) > INT32_MAX) return cudaErrorNotSupported;
   const bool tma = c.page_size % 8 == 0 && planes <= INT32_MAX && map(&k, c.k_dev) && map(&v, c.v_dev);
   cudaError_t e = tma ? launch_kernel<T, DHT, WM, RM, true>(k, v, a, st) : launch_kernel<T, DHT, WM, RM, false>(k, v, a, st);
   note_launch(1);
@@ -1029,11 +1073,11 @@ cudaError_t launch(DecodeArgs& a, cudaStream_t st) {
 
 template <int DHT>
 cudaError_t launch_f32(DecodeArgs& a, int rows, cudaStream_t st) {
-  return rows == 4 ? launch<float, DHT, 1, 4>(a, st) : rows == 8 ? launch<float, DHT, 1, 8>(a, st) : launch<float, DHT, 1, 16>(a, st);
+  return rows == 4 ? launch<float, DHT, 1, 4>(a, st) : rows == 8 ? launch<float, DHT, 1, 8>(a, st) : launch<float, DHT, 2, 8>(a, st);
 }
 template <int DHT>
 cudaError_t launch_bf16(DecodeArgs& a, int rows, cudaStream_t st) {
-  return rows == 16 ? launch<bf16, DHT, 1, 16>(a, st) : rows == 32 ? launch<bf16, DHT, 2, 32>(a, st) : launch<bf16, DHT, 4, 64>(a, st);
+  return rows == 16 ? launch<bf16, DHT, 1, 16>(a, st) : rows == 32 ? launch<bf16, DHT, 2, 16>(a, st) : launch<bf16, DHT, 4, 16>(a, st);
 }
 
 }  // namespace
