@@ -13,9 +13,11 @@
 // theirs) joins them.
 //   bf16: the products are mma.sync m16n8k16: sixteen rows take the tensor instruction of one, and the rate asked of
 //         it, 16 flops a byte of K and V, is a tenth of what it gives, so nothing is won by tcgen05's 128 rows.
-//   f32:  FFMA, on the rows that there are (4, 8 or 16): lanes are tokens (and parts of their dims) for q K^T and dims for
-//         p V.  (tf32 products of operands split in two terms, sixteen rows always, took 217 us for 671 MB where this takes
-//         @F32@.)
+//   f32:  FFMA on packed pairs of rows, for the rows that there are (4, 8 or 16).  Shared memory paces it: 128 bytes a cycle
+//         reach the registers, whether lanes read different values or the same one.  So a lane takes four tokens by an eighth
+//         of the dims for q K^T (a key is read once, a query once for four tokens), and 16 lanes all dims of every other token
+//         for p V.  (With a lane a token, queries read by every lane: 2.4 times the reads, 224 us where this takes 175 for
+//         10 rows of 453 MB; tf32 products of operands split in two terms, sixteen rows always: 217 us for 671 MB.)
 #include <cstring>
 
 #include "common.cuh"
@@ -173,6 +175,9 @@ struct Cursor {
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool live) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void cp4(uint32_t dst, const void* src, bool live) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(live ? 4 : 0) : "memory");
+}
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_wait() {
@@ -195,13 +200,6 @@ __device__ __forceinline__ void mma16816(float* d, const uint32_t* a, uint32_t b
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// the largest of the warp's values
-__device__ __forceinline__ float redux_max(float x) {
-  float y;
-  asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
-  return y;
-}
-
 // ---------------------------------------------------------------------------------------
 // WM warps a group, each on RM of the unit's rows (bf16: sixteen).  NG groups and two copying warps a CTA, one CTA an SM.  A
 // stage holds K and V of TK tokens, rows of DHT values (zeros past head_dim) whose 16-byte chunks are permuted so that the
@@ -214,10 +212,10 @@ template <typename T, int DHT, int WM, int RM>
 struct Plan {
   static constexpr bool B16 = sizeof(T) == 2;
   static constexpr int TK = (DHT == 256 ? 16 : WM == 4 || DHT == 64 ? 64 : 32) / (B16 ? 1 : 2);
-  // bf16: six warps and the two that copy may have 255 registers each (four row groups: eight and two, 168); f32: twelve and
-  // two with 128, as the arithmetic is latency (head dims above 128: ten and two with 168)
-  static constexpr int NG = B16 ? (WM == 4 ? 2 : 6 / WM) : (DHT == 256 ? 10 : 12) / WM, WORKERS = 32 * WM * NG, THREADS = WORKERS + 64, ROWS = RM * WM;
-  static constexpr int TILE = TK * DHT * (int)sizeof(T), STAGE = 2 * TILE, STAGES = (!B16 && DHT == 256 ? 160 : 192) * 1024 / STAGE;
+  // bf16: six warps and the two that copy may have 255 registers each (four row groups: eight and two, 168); f32: eight
+  // (eight rows) with 168, twelve (four rows) with 128
+  static constexpr int F32_WARPS = RM == 8 ? 8 : DHT == 256 ? 10 : 12, NG = B16 ? (WM == 4 ? 2 : 6 / WM) : F32_WARPS / WM, WORKERS = 32 * WM * NG, THREADS = WORKERS + 64, ROWS = RM * WM;
+  static constexpr int TILE = TK * DHT * (int)sizeof(T), STAGE = 2 * TILE, STAGES = B16 ? 192 * 1024 / STAGE : F32_WARPS;
   static constexpr int Q = STAGES * STAGE, QB = ROWS * DHT * (int)sizeof(T), STATS = Q + 2 * QB, MASK = STATS + NG * ROWS * 8;
   static_assert(ROWS * DHT * 4 <= STAGE, "a group's outputs are put into the stage of its last tile");
   // float `col` of row `row` of a group's outputs in its stage: eight rows' pairs fall in distinct banks
@@ -228,11 +226,11 @@ struct Plan {
   static __device__ __forceinline__ int chunk_at(int r, int c) { return ((c & 7) ^ (r & 7)) << 4; }
   static __device__ __forceinline__ int at(int r, int c, int brs) { return row_at(r, brs) + ((c >> 3) << (brs + 7)) + chunk_at(r, c); }
   static constexpr int ATOMS = DHT * (int)sizeof(T) / 128, MBAR = MASK + STAGES * 8, PLACES = MBAR + 2 * STAGES * 8,
-                       X = (PLACES + 2 * 32 * 8 + 15) / 16 * 16, QSLOT = X + (B16 ? 0 : NG * TK * ROWS * 4), BYTES = QSLOT + ROWS * 4;
+                       X = (PLACES + 2 * 32 * 8 + 15) / 16 * 16, BYTES = X + (B16 ? 0 : NG * TK * ROWS * 4);
   // a stage is filled by the same warp and read by the same group every time round, so that each has seen every phase of
   // its barriers: a wait by parity for a phase that is two ahead would return at once
   static_assert(STAGES % 2 == 0 && STAGES % NG == 0, "stages belong to copying warps and to groups");
-  static_assert(STATS % 16 == 0 && MBAR % 8 == 0 && X % 16 == 0 && QSLOT % 4 == 0 && BYTES <= 226 * 1024, "shared memory");
+  static_assert(STATS % 16 == 0 && MBAR % 8 == 0 && X % 16 == 0 && BYTES <= 226 * 1024, "shared memory");
 };
 
 template <typename T>
@@ -482,11 +480,16 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM, RM>::THREADS, 1) decode_kerne
   // a unit's queries into one of two buffers, the next unit's while this one's tiles are done
   auto load_queries = [&](const Cursor<TK>& c, int buf) {
     const int hk = c.u / a.groups, r0 = (c.u - hk * a.groups) * ROWS;
-    for (int e = tid; e < ROWS * CH; e += P::WORKERS) {
-      const int r = e / CH, k = e - r * CH, t = (r0 + r) / a.G;
-      const bool live = r0 + r < a.R && k * VE < dh;
-      const T* src = live ? (const T*)a.q + ((int64_t)c.b * a.n_new + t) * a.q_stride + (hk * a.G + r0 + r - t * a.G) * dh + k * VE : (const T*)a.q;
-      cp16(smem_addr(sm + P::Q + buf * P::QB) + r * (DHT * (int)sizeof(T)) + ((B16 ? k ^ (r & 7) : k) << 4), src, live);
+    for (int e = tid; e < ROWS * (B16 ? CH : DHT); e += P::WORKERS) {
+      constexpr int PER = B16 ? CH : DHT, V = B16 ? VE : 1;
+      const int r = e / PER, k = e - r * PER, t = (r0 + r) / a.G;
+      const bool live = r0 + r < a.R && k * V < dh;
+      const T* src = live ? (const T*)a.q + ((int64_t)c.b * a.n_new + t) * a.q_stride + (hk * a.G + r0 + r - t * a.G) * dh + k * V : (const T*)a.q;
+      const uint32_t to = smem_addr(sm + P::Q + buf * P::QB);
+      if (B16)
+        cp16(to + r * (DHT * 2) + ((k ^ (r & 7)) << 4), src, live);
+      else  // pairs of rows side by side: [pair][half of a chunk of four dims][chunk][two dims of two rows]
+        cp4(to + ((((r >> 1) * 2 + ((k >> 1) & 1)) * CH + (k >> 2)) * 4 + (k & 1) * 2 + (r & 1)) * 4, src, live);
     }
     cp_commit();
   };
@@ -508,7 +511,7 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM, RM>::THREADS, 1) decode_kerne
       load_queries(nxt, qbuf);
     }
     // bf16: the sixteen rows of this warp as A operands, outputs and statistics in the layout of the products: rows g and
-    // g + 8; f32: every lane has all rows' statistics and, of the outputs, its dims
+    // g + 8.  f32: a lane has the statistics of row lane % RM and, of the outputs of all rows (in pairs), its dims
     uint32_t qf[B16 ? DHT / 16 : 1][4];
     if constexpr (B16) {
 #pragma unroll
@@ -517,34 +520,27 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM, RM>::THREADS, 1) decode_kerne
         ldsm4(qf[ks], smem_addr(Qs + row * DHT + ((c ^ (row & 7)) * VE)));
       }
     }
-    // the rows' own slots
-    int* qslots = reinterpret_cast<int*>(sm + P::QSLOT);
-    int qslot[2];
-    if (!B16) {
-      for (int r = tid; r < ROWS; r += P::WORKERS) qslots[r] = r0 + r < a.R ? cur.s.len - a.n_new + (r0 + r) / a.G : -1;
-      tc::named_sync(1, P::WORKERS);
-    }
+    constexpr int MR = B16 ? 2 : 1;
+    int qslot[MR];
+    float m[MR], l[MR];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int r = r0 + 16 * wm + g + 8 * h;
-      qslot[h] = B16 && r < a.R ? cur.s.len - a.n_new + r / a.G : -1;
+    for (int h = 0; h < MR; ++h) {
+      const int r = r0 + RM * wm + (B16 ? g + 8 * h : lane % RM);
+      qslot[h] = r < a.R ? cur.s.len - a.n_new + r / a.G : -1;
+      m[h] = -INFINITY;
+      l[h] = 0.f;
     }
-    constexpr int OD = B16 ? DHT / 8 : 1, OE = B16 ? 4 : DHT / 32, MR = B16 ? 2 : RM;
-    float o[OD][OE], m[MR], l[MR];
-    float2 o2[B16 ? 1 : RM / 2][OE];  // (f32: pairs of rows, for packed products)
+    constexpr int HS = !B16 && DHT <= 128 ? 2 : 1, OC = DHT * HS / 128 > 0 ? DHT * HS / 128 : 1;  // f32: token halves; chunks a lane
+    float o[B16 ? DHT / 8 : 1][4];
+    float2 o2[B16 ? 1 : RM / 2][4 * OC];
+#pragma unroll
+    for (int d = 0; d < (B16 ? DHT / 8 : 1); ++d)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[d][e] = 0.f;
 #pragma unroll
     for (int r = 0; r < (B16 ? 1 : RM / 2); ++r)
 #pragma unroll
-      for (int e = 0; e < OE; ++e) o2[r][e] = f2(0.f);
-#pragma unroll
-    for (int r = 0; r < MR; ++r) {
-      m[r] = -INFINITY;
-      l[r] = 0.f;
-    }
-#pragma unroll
-    for (int d = 0; d < OD; ++d)
-#pragma unroll
-      for (int e = 0; e < OE; ++e) o[d][e] = 0.f;
+      for (int e = 0; e < 4 * OC; ++e) o2[r][e] = f2(0.f);
     int held = -1;  // the stage of this group's last tile, kept until its outputs have been in it
     for (; mine < n + seg; mine += NG) {
       const uint32_t base = smem_addr(sm + st * P::STAGE);
@@ -670,73 +666,105 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM, RM>::THREADS, 1) decode_kerne
         }
       }
       } else {
-      // ---- scores: a lane a token, or a part of its dims (16-byte chunks, in turn)
-      constexpr int LPT = 32 / TK;
-      const int tok = lane % TK, part = lane / TK;
-      float s[RM];
-      {
-        float2 s2[RM];
+      // ---- scores: lane (tg, part) takes four tokens (TK 8: two) by every eighth chunk of their dims, then the eight parts are
+      // added so that each lane is left with a part of the sums: row lane % RM and, of its tokens, all (RM 8) or half (RM 4)
+      constexpr int TPL = TK < 16 ? TK / 4 : 4, PASS = TK / (4 * TPL), NV = TPL * RM / 8;
+      const int tg = lane >> 3, part = lane & 7;
+      float s[PASS * NV];
 #pragma unroll
-        for (int r = 0; r < RM; ++r) s2[r] = f2(0.f);
-#pragma unroll 4
-        for (int i = 0; i < 16; ++i) {
-          const int c = i * LPT + part;
-          const float4 k = *reinterpret_cast<const float4*>(stage + P::at(tok, c, a.brs));
+      for (int ps = 0; ps < PASS; ++ps) {
+        float2 acc[RM / 2][TPL];
 #pragma unroll
-          for (int r = 0; r < RM; ++r) {
-            const float4 q = *reinterpret_cast<const float4*>(Qs + (RM * wm + r) * DHT + 4 * c);
-            s2[r] = __ffma2_rn(make_float2(q.x, q.y), make_float2(k.x, k.y), s2[r]);
-            s2[r] = __ffma2_rn(make_float2(q.z, q.w), make_float2(k.z, k.w), s2[r]);
+        for (int r = 0; r < RM / 2; ++r)
+#pragma unroll
+          for (int i = 0; i < TPL; ++i) acc[r][i] = f2(0.f);
+#pragma unroll 2
+        for (int c8 = 0; c8 < CH; c8 += 8) {
+          const int c = c8 + part;
+          float4 k[TPL];
+#pragma unroll
+          for (int i = 0; i < TPL; ++i) k[i] = *reinterpret_cast<const float4*>(stage + P::at((ps * 4 + tg) * TPL + i, c, a.brs));
+#pragma unroll
+          for (int r = 0; r < RM / 2; ++r) {
+            const float* q = reinterpret_cast<const float*>(Qs) + ((RM / 2 * wm + r) * 2 * CH + c) * 4;
+            const float4 q0 = *reinterpret_cast<const float4*>(q), q1 = *reinterpret_cast<const float4*>(q + CH * 4);
+#pragma unroll
+            for (int i = 0; i < TPL; ++i) {
+              acc[r][i] = __ffma2_rn(make_float2(q0.x, q0.y), f2(k[i].x), acc[r][i]);
+              acc[r][i] = __ffma2_rn(make_float2(q0.z, q0.w), f2(k[i].y), acc[r][i]);
+              acc[r][i] = __ffma2_rn(make_float2(q1.x, q1.y), f2(k[i].z), acc[r][i]);
+              acc[r][i] = __ffma2_rn(make_float2(q1.z, q1.w), f2(k[i].w), acc[r][i]);
+            }
           }
         }
+        const bool b2 = lane & 4, b1 = lane & 2, b0 = lane & 1;
+        float2 h4[RM / 2 * TPL / 2];  // after lanes 4 apart: RM 8: pairs of rows 0, 1 or 2, 3; RM 4: half of the tokens
 #pragma unroll
-        for (int r = 0; r < RM; ++r) s[r] = s2[r].x + s2[r].y;
+        for (int i = 0; i < RM / 2 * TPL / 2; ++i) {
+          const float2 lo = RM == 8 ? acc[i / TPL][i % TPL] : acc[i / (TPL / 2)][i % (TPL / 2)];
+          const float2 hi = RM == 8 ? acc[(i / TPL + 2) % (RM / 2)][i % TPL] : acc[i / (TPL / 2)][i % (TPL / 2) + TPL / 2];
+          const float2 give = b2 ? lo : hi, keep = b2 ? hi : lo;
+          h4[i] = make_float2(keep.x + __shfl_xor_sync(0xffffffffu, give.x, 4), keep.y + __shfl_xor_sync(0xffffffffu, give.y, 4));
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          const float2 give = b1 ? h4[i] : h4[i + NV], keep = b1 ? h4[i + NV] : h4[i];
+          const float2 h2 = make_float2(keep.x + __shfl_xor_sync(0xffffffffu, give.x, 2), keep.y + __shfl_xor_sync(0xffffffffu, give.y, 2));
+          s[ps * NV + i] = (b0 ? h2.y : h2.x) + __shfl_xor_sync(0xffffffffu, b0 ? h2.x : h2.y, 1);
+        }
       }
-      const bool here = (live >> tok) & 1ull;
+      auto token = [&](int i) { return ((i / NV) * 4 + tg) * TPL + (RM == 8 ? 0 : ((lane >> 2) & 1) * (TPL / 2)) + i % NV; };
+      const int row = r0 + RM * wm + lane % RM;
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < PASS * NV; ++i) {
+        const int k = token(i);
+        s[i] = ((live >> k) & 1ull) && (all || sees(a, qslot[0], j0 + k)) ? s[i] * a.sl2 : -INFINITY;
+        if (a.scores && row < a.R) a.scores[(((int64_t)cur.b * a.c.n_kv_heads + hk) * a.R + row) * a.x_stride + x0 + k] = s[i];
+        top = fmaxf(top, s[i]);
+      }
+#pragma unroll
+      for (int x = RM; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+      const float mn = fmaxf(m[0], top), ms = mn == -INFINITY ? 0.f : mn;
+      if (__any_sync(0xffffffffu, mn > m[0])) {
+        const float f = exp2f(m[0] - ms);
+        l[0] *= f;
+        m[0] = mn;
+#pragma unroll
+        for (int r = 0; r < RM / 2; ++r) {
+          const float2 fr = make_float2(__shfl_sync(0xffffffffu, f, 2 * r), __shfl_sync(0xffffffffu, f, 2 * r + 1));
+#pragma unroll
+          for (int e = 0; e < 4 * OC; ++e) o2[r][e] = __fmul2_rn(o2[r][e], fr);
+        }
+      }
       float* X = reinterpret_cast<float*>(sm + P::X) + warp * (TK * RM);  // p, [token][row]
 #pragma unroll
-      for (int r = 0; r < RM; ++r) {
-#pragma unroll
-        for (int x = TK; x < 32; x <<= 1) s[r] += __shfl_xor_sync(0xffffffffu, s[r], x);
-        const int row = r0 + RM * wm + r;
-        s[r] = here && row < a.R && (all || sees(a, qslots[RM * wm + r], j0 + tok)) ? s[r] * a.sl2 : -INFINITY;
-        if (a.scores && row < a.R && part == 0)
-          a.scores[(((int64_t)cur.b * a.c.n_kv_heads + hk) * a.R + row) * a.x_stride + x0 + tok] = s[r];
-        const float mn = fmaxf(m[r], redux_max(s[r])), ms = mn == -INFINITY ? 0.f : mn;
-        if (mn > m[r]) {
-          const float f = exp2f(m[r] - ms);
-          l[r] *= f;
-          m[r] = mn;
-#pragma unroll
-          for (int e = 0; e < OE; ++e) (r & 1 ? o2[r / 2][e].y : o2[r / 2][e].x) *= f;
-        }
-        s[r] = exp2f(s[r] - ms);
-        l[r] += s[r];  // a lane's share
-      }
-      if (part == 0) {
-#pragma unroll
-        for (int r = 0; r < RM; r += 4) *reinterpret_cast<float4*>(X + tok * RM + r) = make_float4(s[r], s[r + 1], s[r + 2], s[r + 3]);
+      for (int i = 0; i < PASS * NV; ++i) {
+        const float x = exp2f(s[i] - ms);
+        l[0] += x;  // a lane's share
+        X[token(i) * RM + lane % RM] = x;
       }
       __syncwarp();
-      // ---- outputs: a lane DHT / 32 dims
+      // ---- outputs: a half of the lanes every other token (head dims above 128: all lanes every token), a lane chunks
+      // li + 16 j (32 j) of the dims
+      const int hw = HS == 2 ? lane >> 4 : 0, li = HS == 2 ? lane & 15 : lane;
 #pragma unroll 2
-      for (int k = 0; k < TK; ++k) {
-        float v[OE];
-        const uint8_t* row = stage + P::TILE;
-        if constexpr (OE == 2) {
-          *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(row + P::at(k, lane >> 1, a.brs) + 8 * (lane & 1));
-        } else {
+      for (int k = hw; k < TK; k += HS) {
+        float2 pp[RM / 2];
 #pragma unroll
-          for (int e = 0; e < OE; e += 4) *reinterpret_cast<float4*>(v + e) = *reinterpret_cast<const float4*>(row + P::at(k, lane + 8 * e, a.brs));
+        for (int r = 0; r < RM / 2; r += 2) {
+          const float4 x = *reinterpret_cast<const float4*>(X + k * RM + 2 * r);
+          pp[r] = make_float2(x.x, x.y);
+          pp[r + 1] = make_float2(x.z, x.w);
         }
 #pragma unroll
-        for (int r = 0; r < RM; r += 4) {
-          const float4 p = *reinterpret_cast<const float4*>(X + k * RM + r);
+        for (int j = 0; j < OC; ++j) {
+          const float4 v = *reinterpret_cast<const float4*>(stage + P::TILE + P::at(k, li + 32 / HS * j, a.brs));
+          const float vs[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-          for (int e = 0; e < OE; ++e) {
-            o2[r / 2][e] = __ffma2_rn(make_float2(p.x, p.y), f2(v[e]), o2[r / 2][e]);
-            o2[r / 2 + 1][e] = __ffma2_rn(make_float2(p.z, p.w), f2(v[e]), o2[r / 2 + 1][e]);
-          }
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int r = 0; r < RM / 2; ++r) o2[r][4 * j + e] = __ffma2_rn(pp[r], f2(vs[e]), o2[r][4 * j + e]);
         }
       }
       __syncwarp();
@@ -772,17 +800,24 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM, RM>::THREADS, 1) decode_kerne
       }
     } else {
 #pragma unroll
-      for (int r = 0; r < RM; ++r) {
-        const float sum = warp_sum(lane < TK ? l[r] : 0.f);
-        const int row = RM * wm + r;
-        if (lane == 0) stats[grp * ROWS + row] = make_float2(m[r], sum);
-        if (held >= 0) {
-          auto of = [&](int e) { return r & 1 ? o2[r / 2][e].y : o2[r / 2][e].x; };
-          if constexpr (OE == 2) {
-            *reinterpret_cast<float2*>(to + P::sum_at(row, 2 * lane)) = make_float2(of(0), of(1));
-          } else {
+      for (int x = RM; x < 32; x <<= 1) l[0] += __shfl_xor_sync(0xffffffffu, l[0], x);
+      if (lane < RM) stats[grp * ROWS + RM * wm + lane] = make_float2(m[0], l[0]);
+      if (held >= 0) {
 #pragma unroll
-            for (int e = 0; e < OE; e += 4) *reinterpret_cast<float4*>(to + P::sum_at(row, 4 * lane + 32 * e)) = make_float4(of(e), of(e + 1), of(e + 2), of(e + 3));
+        for (int r = 0; r < RM / 2; ++r) {
+          if (HS == 2) {
+#pragma unroll
+            for (int e = 0; e < 4 * OC; ++e)
+              o2[r][e] = make_float2(o2[r][e].x + __shfl_xor_sync(0xffffffffu, o2[r][e].x, 16), o2[r][e].y + __shfl_xor_sync(0xffffffffu, o2[r][e].y, 16));
+          }
+          const int row = RM * wm + 2 * r, li = HS == 2 ? lane & 15 : lane;
+          if (HS == 1 || lane < 16) {
+#pragma unroll
+            for (int j = 0; j < OC; ++j) {
+              const int d = 4 * (li + 32 / HS * j);
+              *reinterpret_cast<float4*>(to + P::sum_at(row, d)) = make_float4(o2[r][4 * j].x, o2[r][4 * j + 1].x, o2[r][4 * j + 2].x, o2[r][4 * j + 3].x);
+              *reinterpret_cast<float4*>(to + P::sum_at(row + 1, d)) = make_float4(o2[r][4 * j].y, o2[r][4 * j + 1].y, o2[r][4 * j + 2].y, o2[r][4 * j + 3].y);
+            }
           }
         }
       }
