@@ -73,7 +73,7 @@ struct VerifySlot {  // of a sequence, zero between calls
 };
 
 template <typename T>
-__global__ void __launch_bounds__(VT) verify_draft_kernel(const __grid_constant__ ra_verify_draft_args a, int parts, int per_part) {
+__global__ void __launch_bounds__(VT, 3) verify_draft_kernel(const __grid_constant__ ra_verify_draft_args a, int parts, int per_part) {
   pdl_wait();
   pdl_trigger();
   const int part = blockIdx.x % parts, b = blockIdx.x / parts, tid = threadIdx.x, lane = tid & 31;
@@ -141,9 +141,10 @@ __global__ void __launch_bounds__(VT) verify_draft_kernel(const __grid_constant_
 size_t verify_draft_workspace(const ra_verify_draft_args& a) { return (size_t)a.batch * sizeof(VerifySlot); }
 
 cudaError_t verify_draft(const ra_verify_draft_args& a, cudaStream_t st) {
-  // two CTAs an SM, none with fewer than four tokens a thread
-  const int want = (2 * device_sm_count() + a.batch - 1) / a.batch, most = (a.vocab + 4 * VT - 1) / (4 * VT);
-  int parts = want < most ? want : most;
+  // the SMs filled once, with three CTAs each (64 rows of 50001: four and a half a row and a second round of a few CTAs took
+  // 15.5 us), none with fewer than four tokens a thread
+  const int want = 3 * device_sm_count() / a.batch, most = (a.vocab + 4 * VT - 1) / (4 * VT);
+  int parts = want < 1 ? 1 : want < most ? want : most;
   const int per = (a.vocab + parts - 1) / parts;
   parts = (a.vocab + per - 1) / per;
   const dim3 grid((unsigned)parts * (unsigned)a.batch);

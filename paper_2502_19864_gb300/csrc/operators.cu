@@ -52,7 +52,7 @@ ra_status check_append(const ra_kv_append_args& a) {
     TRY(check_rows(a.q_out_dev, a.q_out_stride, a.n_heads, c.head_dim, c.dtype));
   }
   if (a.rope_dev && (a.rope_len < 1 || !aligned(a.rope_dev, 16))) return RA_ERR_ARG;
-  if (a.rope_dev && c.head_dim % 2) return RA_ERR_SHAPE;
+  if ((int64_t)a.batch * a.n_new > INT32_MAX) return RA_ERR_SHAPE;  // (tokens are counted in 32 bits)
   return RA_OK;
 }
 ra_status check_decode(const ra_attention_decode_args& a) {
