@@ -6,30 +6,35 @@
 //             and sum;
 //   backward  dV_j = sum_i p_ij dO_i;  dS_ij = p_ij (dO_i v_j - D_i), D_i = dO_i o_i;  dQ_i = scale sum_j dS_ij k_j;
 //             dK_j = scale sum_i dS_ij q_i, the sums over i over all query heads that share the key.
-// A query CTA walks the key blocks that any of its 64 queries sees: those of the window and those that hold sinks.
-// A key CTA walks, head by head of its group, the query blocks that see any of its 64 keys: dK and dV are sums of
-// one CTA in a fixed order.  Rows past the sequence's end are loaded as zeros, whatever memory holds there.
-// Bound by FFMA: a thread keeps 4 x 4 scores and 4 x DH / 16 outputs in registers.
+// A query CTA holds 32 queries and walks the blocks of 64 keys that any of them sees: those of the window and those that
+// hold sinks.  A key CTA holds 32 keys and walks, head by head of its group, the blocks of 64 queries that see any of them:
+// dK and dV are sums in a fixed order.  Keys that are sinks are seen by every later query; where that makes their blocks
+// much longer than a window, several CTAs share a block's queries and a last kernel adds their parts in order.  The query
+// pass of the backward computes D on its way and leaves it for the key pass.  Rows past the sequence's end are loaded as
+// zeros, whatever memory holds there.
+// A thread keeps 4 x 4 scores and 4 x DH / 16 outputs in registers.  Paced by shared memory: 8 reads of 16 bytes a lane for
+// 64 multiply-adds (32 packed ones).  32 held rows make a CTA a step half as long as 64 did and twice as many: 3 sequences of
+// 333 tokens, 4 heads of 64 on 2, window 100, forward and backward 102 us (228 us).
 #include "common.cuh"
 #include "operators.h"
 
 namespace ra {
 namespace {
 
-constexpr int BT = 64, NT = 256, PP = BT + 4;
+constexpr int BH = 32, BT = 64, NT = 128, PP = BT + 4;  // rows held and streamed, threads, floats of a row of X
 constexpr float kLog2e = 1.4426950408889634f;
 
 template <int DH>
 struct Plan {
   static constexpr int DP = DH + 4;  // padded rows: eight lanes' 16 bytes of eight rows fall in distinct banks
-  static constexpr int TILE = BT * DP;
-  static constexpr int FWD_BYTES = (3 * TILE + BT * PP) * 4, BWD_BYTES = (4 * TILE + BT * PP + 2 * BT) * 4;
+  static constexpr int HELD = BH * DP, TILE = BT * DP;
+  static constexpr int FWD_BYTES = (HELD + 2 * TILE + BH * PP) * 4, BWD_BYTES = (2 * HELD + 2 * TILE + BH * PP + 2 * BT) * 4;
 };
 
-// rows [r0, r0 + 64) of one head, zeros from row `len` on and past head_dim
-template <int DH>
+// ROWS rows from r0 on of one head, zeros from row `len` on and past head_dim
+template <int DH, int ROWS>
 __device__ __forceinline__ void load_rows(float* dst, const float* src, int64_t stride, int r0, int len, int head_dim) {
-  for (int i = threadIdx.x; i < BT * DH / 4; i += NT) {
+  for (int i = threadIdx.x; i < ROWS * DH / 4; i += NT) {
     const int r = i / (DH / 4), c = (i - r * (DH / 4)) * 4;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
     if (r0 + r < len && c < head_dim) x = *reinterpret_cast<const float4*>(src + (int64_t)(r0 + r) * stride + c);
@@ -39,10 +44,11 @@ __device__ __forceinline__ void load_rows(float* dst, const float* src, int64_t 
 // acc[i][j] = A[4 ty + i] . B[tx + 16 j]
 template <int DH>
 __device__ __forceinline__ void dot_rows(float (&acc)[4][4], const float* A, const float* B, int ty, int tx) {
+  float2 s[4][4];  // even and odd dims
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
+    for (int j = 0; j < 4; ++j) s[i][j] = f2(0.f);
 #pragma unroll 4
   for (int d = 0; d < DH; d += 4) {
     float4 a[4], b[4];
@@ -54,12 +60,14 @@ __device__ __forceinline__ void dot_rows(float (&acc)[4][4], const float* A, con
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        acc[i][j] = fmaf(a[i].x, b[j].x, acc[i][j]);
-        acc[i][j] = fmaf(a[i].y, b[j].y, acc[i][j]);
-        acc[i][j] = fmaf(a[i].z, b[j].z, acc[i][j]);
-        acc[i][j] = fmaf(a[i].w, b[j].w, acc[i][j]);
+        s[i][j] = __ffma2_rn(make_float2(a[i].x, a[i].y), make_float2(b[j].x, b[j].y), s[i][j]);
+        s[i][j] = __ffma2_rn(make_float2(a[i].z, a[i].w), make_float2(b[j].z, b[j].w), s[i][j]);
       }
   }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = s[i][j].x + s[i][j].y;
 }
 // out[i][.] += sum_k X[4 ty + i][k] B[k][.], the thread's columns 2 tx + 32 c and the next
 template <int DH>
@@ -125,11 +133,11 @@ template <int DH>
 __global__ void __launch_bounds__(NT) window_fwd_simt_kernel(const __grid_constant__ ra_attention_window_args a, int W, int n_blk) {
   extern __shared__ __align__(16) float sm[];
   using P = Plan<DH>;
-  float *Q = sm, *K = Q + P::TILE, *V = K + P::TILE, *X = V + P::TILE;
+  float *Q = sm, *K = Q + P::HELD, *V = K + P::TILE, *X = V + P::TILE;
   pdl_wait();
   pdl_trigger();
   const Geometry g = geometry(a, a.n_heads, n_blk);
-  const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15, q0 = g.blk * BT, dh = a.head_dim;
+  const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15, q0 = g.blk * BH, dh = a.head_dim;
   const int kvh = g.head / (a.n_heads / a.n_kv_heads);
   const int64_t tok0 = (int64_t)g.b * a.seq;
   const float* q = (const float*)a.q_dev + tok0 * a.q_stride + g.head * dh;
@@ -145,15 +153,15 @@ __global__ void __launch_bounds__(NT) window_fwd_simt_kernel(const __grid_consta
   }
   const float sl2 = a.scale * kLog2e;
   if (q0 < g.len) {
-    load_rows<DH>(Q, q, a.q_stride, q0, g.len, dh);
-    const int last = q0 + BT - 1 < g.len ? q0 + BT - 1 : g.len - 1, hi = last / BT;
+    load_rows<DH, BH>(Q, q, a.q_stride, q0, g.len, dh);
+    const int last = q0 + BH - 1 < g.len ? q0 + BH - 1 : g.len - 1, hi = last / BT;
     const int first = q0 - W + 1, lo = first > 0 ? first / BT : 0;
     for (int kb = 0; kb <= hi; ++kb) {
       if (kb < lo && kb * BT >= a.sinks) kb = lo;
       const int k0 = kb * BT;
       __syncthreads();
-      load_rows<DH>(K, k, a.k_stride, k0, g.len, dh);
-      load_rows<DH>(V, v, a.v_stride, k0, g.len, dh);
+      load_rows<DH, BT>(K, k, a.k_stride, k0, g.len, dh);
+      load_rows<DH, BT>(V, v, a.v_stride, k0, g.len, dh);
       __syncthreads();
       float s[4][4];
       dot_rows<DH>(s, Q, K, ty, tx);
@@ -199,38 +207,26 @@ __global__ void __launch_bounds__(NT) window_fwd_simt_kernel(const __grid_consta
 }
 
 // ---- backward ------------------------------------------------------------------------------
-// D_i = dO_i . o_i, a warp a row (0 past the sequence's end)
-__global__ void __launch_bounds__(256) window_bwd_d_kernel(const __grid_constant__ ra_attention_window_args a, float* D) {
-  pdl_wait();
-  pdl_trigger();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t rows = (int64_t)a.batch * a.seq * a.n_heads;
-  for (int64_t r = (int64_t)blockIdx.x * 8 + warp; r < rows; r += (int64_t)gridDim.x * 8) {
-    const int64_t tok = r / a.n_heads;
-    const int head = (int)(r - tok * a.n_heads), b = (int)(tok / a.seq), s = (int)(tok - (int64_t)b * a.seq);
-    float d = 0.f;
-    if (!a.lens_dev || s < a.lens_dev[b]) {
-      const float* o = (const float*)a.out_dev + tok * a.out_stride + head * a.head_dim;
-      const float* g = (const float*)a.dout_dev + tok * a.dout_stride + head * a.head_dim;
-      for (int c = lane; c < a.head_dim; c += 32) d = fmaf(o[c], g[c], d);
-    }
-    d = warp_sum(d);
-    if (lane == 0) D[((int64_t)b * a.n_heads + head) * a.seq + s] = d;
-  }
-}
-
-// P and dS of one pair of blocks by the thread's 4 x 4: rows are queries (KEYS: keys)
+// KEYS: the held rows are keys (dK, dV), the streamed ones queries; else queries (dQ, D) and keys
 template <int DH, bool KEYS>
-__global__ void __launch_bounds__(NT) window_bwd_simt_kernel(const __grid_constant__ ra_attention_window_args a, const float* Dv,
-                                                             int W, int n_blk) {
+__global__ void __launch_bounds__(NT) window_bwd_simt_kernel(const __grid_constant__ ra_attention_window_args a, float* Dv,
+                                                             float* parts, int W, int n_blk, int split, int chunks) {
   extern __shared__ __align__(16) float sm[];
   using P = Plan<DH>;
-  float *T0 = sm, *T1 = T0 + P::TILE, *T2 = T1 + P::TILE, *T3 = T2 + P::TILE, *X = T3 + P::TILE, *L = X + BT * PP, *D = L + BT;
+  float *T0 = sm, *T1 = T0 + P::HELD, *T2 = T1 + P::HELD, *T3 = T2 + P::TILE, *X = T3 + P::TILE, *L = X + BH * PP, *D = L + BT;
   pdl_wait();
   pdl_trigger();
-  const int G = a.n_heads / a.n_kv_heads;
-  const Geometry g = geometry(a, KEYS ? a.n_kv_heads : a.n_heads, n_blk);
-  const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15, r0 = g.blk * BT, dh = a.head_dim;
+  const int G = a.n_heads / a.n_kv_heads, items = n_blk - split + split * chunks;
+  Geometry g = geometry(a, KEYS ? a.n_kv_heads : a.n_heads, items);
+  int chunk = 0, n_chunks = 1;
+  if (KEYS) {  // (g.blk counts down: the first blocks, which most queries see, come first)
+    const int it = items - 1 - g.blk;
+    const bool shared = it < split * chunks;
+    g.blk = shared ? it / chunks : it - split * chunks + split;
+    chunk = shared ? it - g.blk * chunks : 0;
+    n_chunks = shared ? chunks : 1;
+  }
+  const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15, r0 = g.blk * BH, dh = a.head_dim;
   const int kvh = KEYS ? g.head : g.head / G;
   const int64_t tok0 = (int64_t)g.b * a.seq;
   const float* k = (const float*)a.k_dev + tok0 * a.k_stride + kvh * dh;
@@ -241,14 +237,6 @@ __global__ void __launch_bounds__(NT) window_bwd_simt_kernel(const __grid_consta
 #pragma unroll
     for (int c = 0; c < DH / 16; ++c) u[i][c] = w[i][c] = 0.f;
   const float sl2 = a.scale * kLog2e;
-  auto stats = [&](int head, int q0) {
-    if (tid < BT) {
-      const int64_t at = ((int64_t)g.b * a.n_heads + head) * a.seq + q0 + tid;
-      const bool live = q0 + tid < g.len;
-      L[tid] = live ? a.lse_dev[at] * kLog2e : 0.f;
-      D[tid] = live ? Dv[at] : 0.f;
-    }
-  };
   // X = P (or P^T), then dS in s
   auto probabilities = [&](float (&s)[4][4], int c0) {
 #pragma unroll
@@ -267,51 +255,75 @@ __global__ void __launch_bounds__(NT) window_bwd_simt_kernel(const __grid_consta
       for (int j = 0; j < 4; ++j) X[(4 * ty + i) * PP + tx + 16 * j] = s[i][j];
   };
   if (r0 < g.len) {
+    const int last = r0 + BH - 1 < g.len ? r0 + BH - 1 : g.len - 1;
     if (KEYS) {
-      load_rows<DH>(T0, k, a.k_stride, r0, g.len, dh);
-      load_rows<DH>(T1, v, a.v_stride, r0, g.len, dh);
-      const int last = r0 + BT - 1 < g.len ? r0 + BT - 1 : g.len - 1;  // the last key
+      load_rows<DH, BH>(T0, k, a.k_stride, r0, g.len, dh);
+      load_rows<DH, BH>(T1, v, a.v_stride, r0, g.len, dh);
       const int64_t far = r0 < a.sinks ? g.len - 1 : (int64_t)last + W - 1;
-      const int hi = (int)(far < g.len ? far : g.len - 1) / BT;
-      for (int h = kvh * G; h < (kvh + 1) * G; ++h) {
+      const int first = r0 / BT, per_head = (int)(far < g.len ? far : g.len - 1) / BT - first + 1;
+      const int64_t total = (int64_t)per_head * G;
+      const int n1 = (int)(total * (chunk + 1) / n_chunks);
+      for (int n = (int)(total * chunk / n_chunks); n < n1; ++n) {
+        const int h = kvh * G + n / per_head, q0 = (first + n % per_head) * BT;
         const float* q = (const float*)a.q_dev + tok0 * a.q_stride + h * dh;
         const float* go = (const float*)a.dout_dev + tok0 * a.dout_stride + h * dh;
-        for (int qb = g.blk; qb <= hi; ++qb) {
-          const int q0 = qb * BT;
-          __syncthreads();
-          load_rows<DH>(T2, q, a.q_stride, q0, g.len, dh);
-          load_rows<DH>(T3, go, a.dout_stride, q0, g.len, dh);
-          stats(h, q0);
-          __syncthreads();
-          float s[4][4], dp[4][4];
-          dot_rows<DH>(s, T0, T2, ty, tx);
-          probabilities(s, q0);
-          put(s);
-          dot_rows<DH>(dp, T1, T3, ty, tx);
-          __syncthreads();
-          times_rows<DH>(w, X, T3, ty, tx);
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) s[i][j] *= dp[i][j] - D[tx + 16 * j];
-          __syncthreads();
-          put(s);
-          __syncthreads();
-          times_rows<DH>(u, X, T2, ty, tx);
+        __syncthreads();
+        load_rows<DH, BT>(T2, q, a.q_stride, q0, g.len, dh);
+        load_rows<DH, BT>(T3, go, a.dout_stride, q0, g.len, dh);
+        if (tid < BT) {
+          const int64_t at = ((int64_t)g.b * a.n_heads + h) * a.seq + q0 + tid;
+          const bool live = q0 + tid < g.len;
+          L[tid] = live ? a.lse_dev[at] * kLog2e : 0.f;
+          D[tid] = live ? Dv[at] : 0.f;
         }
+        __syncthreads();
+        float s[4][4], dp[4][4];
+        dot_rows<DH>(s, T0, T2, ty, tx);
+        probabilities(s, q0);
+        put(s);
+        dot_rows<DH>(dp, T1, T3, ty, tx);
+        __syncthreads();
+        times_rows<DH>(w, X, T3, ty, tx);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s[i][j] *= dp[i][j] - D[tx + 16 * j];
+        __syncthreads();
+        put(s);
+        __syncthreads();
+        times_rows<DH>(u, X, T2, ty, tx);
       }
     } else {
-      load_rows<DH>(T0, (const float*)a.q_dev + tok0 * a.q_stride + g.head * dh, a.q_stride, r0, g.len, dh);
-      load_rows<DH>(T1, (const float*)a.dout_dev + tok0 * a.dout_stride + g.head * dh, a.dout_stride, r0, g.len, dh);
-      stats(g.head, r0);
-      const int last = r0 + BT - 1 < g.len ? r0 + BT - 1 : g.len - 1, hi = last / BT;
-      const int first = r0 - W + 1, lo = first > 0 ? first / BT : 0;
+      load_rows<DH, BH>(T0, (const float*)a.q_dev + tok0 * a.q_stride + g.head * dh, a.q_stride, r0, g.len, dh);
+      load_rows<DH, BH>(T1, (const float*)a.dout_dev + tok0 * a.dout_stride + g.head * dh, a.dout_stride, r0, g.len, dh);
+      const int64_t at = ((int64_t)g.b * a.n_heads + g.head) * a.seq + r0;
+      if (tid < BH) L[tid] = r0 + tid < g.len ? a.lse_dev[at + tid] * kLog2e : 0.f;
+      __syncthreads();
+      // D = dO . o, four threads a row
+      {
+        const int row = tid >> 2;
+        float d = 0.f;
+        if (r0 + row < g.len) {
+          const float* o = (const float*)a.out_dev + (tok0 + r0 + row) * a.out_stride + g.head * dh;
+          for (int c = 4 * (tid & 3); c < dh; c += 16) {
+            const float4 x = *reinterpret_cast<const float4*>(o + c), y = *reinterpret_cast<const float4*>(T1 + row * P::DP + c);
+            d = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, d))));
+          }
+        }
+        d += __shfl_xor_sync(0xffffffffu, d, 1);
+        d += __shfl_xor_sync(0xffffffffu, d, 2);
+        if ((tid & 3) == 0) {
+          D[row] = d;
+          if (r0 + row < a.seq) Dv[at + row] = d;
+        }
+      }
+      const int hi = last / BT, first = r0 - W + 1, lo = first > 0 ? first / BT : 0;
       for (int kb = 0; kb <= hi; ++kb) {
         if (kb < lo && kb * BT >= a.sinks) kb = lo;
         const int k0 = kb * BT;
         __syncthreads();
-        load_rows<DH>(T2, k, a.k_stride, k0, g.len, dh);
-        load_rows<DH>(T3, v, a.v_stride, k0, g.len, dh);
+        load_rows<DH, BT>(T2, k, a.k_stride, k0, g.len, dh);
+        load_rows<DH, BT>(T3, v, a.v_stride, k0, g.len, dh);
         __syncthreads();
         float s[4][4], dp[4][4];
         dot_rows<DH>(s, T0, T2, ty, tx);
@@ -328,7 +340,11 @@ __global__ void __launch_bounds__(NT) window_bwd_simt_kernel(const __grid_consta
     }
   }
   const float fs[4] = {a.scale, a.scale, a.scale, a.scale}, f1[4] = {1.f, 1.f, 1.f, 1.f};
-  if (KEYS) {
+  if (KEYS && n_chunks > 1) {
+    float* part = parts + (((int64_t)(g.b * a.n_kv_heads + g.head) * split + g.blk) * chunks + chunk) * (2 * BH * DH);
+    store_rows<DH>(part, DH, u, fs, 0, BH, DH, ty, tx);
+    store_rows<DH>(part + BH * DH, DH, w, f1, 0, BH, DH, ty, tx);
+  } else if (KEYS) {
     store_rows<DH>((float*)a.dk_dev + tok0 * a.dk_stride + kvh * dh, a.dk_stride, u, fs, r0, a.seq, dh, ty, tx);
     store_rows<DH>((float*)a.dv_dev + tok0 * a.dv_stride + kvh * dh, a.dv_stride, w, f1, r0, a.seq, dh, ty, tx);
   } else {
@@ -336,11 +352,53 @@ __global__ void __launch_bounds__(NT) window_bwd_simt_kernel(const __grid_consta
   }
 }
 
+// dK and dV of the shared key blocks: the parts in order, four values a thread
+template <int DH>
+__global__ void __launch_bounds__(256) window_bwd_simt_parts_kernel(const __grid_constant__ ra_attention_window_args a, const float* parts,
+                                                                    int split, int chunks) {
+  pdl_wait();
+  pdl_trigger();
+  constexpr int PER = BH * DH / 4;
+  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x, blk = e / (2 * PER);
+  if (blk >= (int64_t)a.batch * a.n_kv_heads * split) return;
+  const int x = (int)(e - blk * (2 * PER)), o = x / PER, y = x - o * PER, row = y / (DH / 4), c = (y - row * (DH / 4)) * 4;
+  const int64_t unit = blk / split;
+  const int r = (int)(blk - unit * split) * BH + row, head = (int)(unit % a.n_kv_heads), b = (int)(unit / a.n_kv_heads);
+  if (r >= a.seq || c >= a.head_dim) return;
+  const float* p = parts + blk * chunks * (2 * BH * DH) + (o * BH + row) * DH + c;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i = 0; i < chunks; ++i) {
+    const float4 v = *reinterpret_cast<const float4*>(p + (int64_t)i * (2 * BH * DH));
+    s.x += v.x;
+    s.y += v.y;
+    s.z += v.z;
+    s.w += v.w;
+  }
+  float* d = o == 0 ? (float*)a.dk_dev + ((int64_t)b * a.seq + r) * a.dk_stride : (float*)a.dv_dev + ((int64_t)b * a.seq + r) * a.dv_stride;
+  *reinterpret_cast<float4*>(d + head * a.head_dim + c) = s;
+}
+
 int window_of(const ra_attention_window_args& a) { return a.window == 0 || a.window > a.seq ? a.seq : a.window; }
+
+int dims_of(const ra_attention_window_args& a) { return a.head_dim <= 32 ? 32 : a.head_dim <= 64 ? 64 : a.head_dim <= 96 ? 96 : 128; }
+
+// How many CTAs share each of the first key blocks: an ordinary block is seen from W + 32 queries, one with sinks from all.
+// Up to 128 sinks and where that is twice as long, as many CTAs as bring them back to an ordinary one's length, at most 32.
+void split_of(const ra_attention_window_args& a, int& split, int& chunks) {
+  const int64_t ordinary = (int64_t)window_of(a) + BH;
+  split = 0;
+  chunks = 1;
+  if (a.sinks < 1 || a.sinks > 128 || a.seq < 2 * ordinary) return;
+  const int n_blk = (a.seq + BH - 1) / BH, blocks = (a.sinks + BH - 1) / BH;
+  split = blocks < n_blk ? blocks : n_blk;
+  const int64_t n = (a.seq + ordinary - 1) / ordinary;
+  chunks = n < 32 ? (int)n : 32;
+}
+size_t d_bytes(const ra_attention_window_args& a) { return ((size_t)a.batch * a.seq * a.n_heads * 4 + 255) / 256 * 256; }
 
 template <int DH>
 cudaError_t fwd_simt(const ra_attention_window_args& a, cudaStream_t st) {
-  const int n_blk = (a.seq + BT - 1) / BT;
+  const int n_blk = (a.seq + BH - 1) / BH;
   const int64_t grid = (int64_t)n_blk * a.batch * a.n_heads;
   if (grid > INT32_MAX) return cudaErrorNotSupported;
   cudaError_t e = allow_smem(window_fwd_simt_kernel<DH>, Plan<DH>::FWD_BYTES);
@@ -349,43 +407,48 @@ cudaError_t fwd_simt(const ra_attention_window_args& a, cudaStream_t st) {
   note_launch(1);
   return e;
 }
-cudaError_t rows_d(const ra_attention_window_args& a, float* D, cudaStream_t st) {
-  const int64_t blocks = ((int64_t)a.batch * a.seq * a.n_heads + 7) / 8, most = 64LL * device_sm_count();
-  cudaError_t e = launch_pdl(window_bwd_d_kernel, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, st, a, D);
-  note_launch(1);
-  return e;
-}
 template <int DH>
 cudaError_t bwd_simt(const ra_attention_window_args& a, cudaStream_t st) {
-  const int n_blk = (a.seq + BT - 1) / BT;
-  const int64_t gq = (int64_t)n_blk * a.batch * a.n_heads, gk = (int64_t)n_blk * a.batch * a.n_kv_heads;
-  if (gq > INT32_MAX) return cudaErrorNotSupported;
+  int split, chunks;
+  split_of(a, split, chunks);
+  const int n_blk = (a.seq + BH - 1) / BH;
+  const int64_t gq = (int64_t)n_blk * a.batch * a.n_heads, gk = (int64_t)(n_blk - split + split * chunks) * a.batch * a.n_kv_heads;
+  if (gq > INT32_MAX || gk > INT32_MAX) return cudaErrorNotSupported;
   float* D = (float*)a.workspace_dev;
+  float* parts = (float*)((char*)a.workspace_dev + d_bytes(a));
   cudaError_t e = allow_smem(window_bwd_simt_kernel<DH, true>, Plan<DH>::BWD_BYTES);
   if (e == cudaSuccess) e = allow_smem(window_bwd_simt_kernel<DH, false>, Plan<DH>::BWD_BYTES);
-  if (e == cudaSuccess) e = rows_d(a, D, st);
-  if (e != cudaSuccess) return e;
-  const float* Dc = D;
-  e = launch_pdl(window_bwd_simt_kernel<DH, true>, dim3((unsigned)gk), dim3(NT), Plan<DH>::BWD_BYTES, st, a, Dc, window_of(a), n_blk);
   if (e == cudaSuccess)
-    e = launch_pdl(window_bwd_simt_kernel<DH, false>, dim3((unsigned)gq), dim3(NT), Plan<DH>::BWD_BYTES, st, a, Dc, window_of(a), n_blk);
+    e = launch_pdl(window_bwd_simt_kernel<DH, false>, dim3((unsigned)gq), dim3(NT), Plan<DH>::BWD_BYTES, st, a, D, parts, window_of(a), n_blk, 0, 1);
+  if (e == cudaSuccess)
+    e = launch_pdl(window_bwd_simt_kernel<DH, true>, dim3((unsigned)gk), dim3(NT), Plan<DH>::BWD_BYTES, st, a, D, parts, window_of(a), n_blk, split, chunks);
   note_launch(2);
+  if (e == cudaSuccess && split > 0) {
+    const int64_t threads = (int64_t)a.batch * a.n_kv_heads * split * 2 * BH * DH / 4;
+    e = launch_pdl(window_bwd_simt_parts_kernel<DH>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, a, (const float*)parts, split, chunks);
+    note_launch(1);
+  }
   return e;
 }
 
 }  // namespace
 
 size_t attention_window_workspace(const ra_attention_window_args& a) {
-  return a.dtype == RA_BF16 ? attention_window_workspace_tc(a) : (size_t)a.batch * a.seq * a.n_heads * 4;
+  if (a.dtype == RA_BF16) return attention_window_workspace_tc(a);
+  int split, chunks;
+  split_of(a, split, chunks);
+  return d_bytes(a) + (size_t)a.batch * a.n_kv_heads * split * chunks * 2 * BH * dims_of(a) * 4;
 }
 
 cudaError_t attention_window_fwd_simt(const ra_attention_window_args& a, cudaStream_t st) {
   if (a.dtype != RA_F32) return cudaErrorNotSupported;
-  return a.head_dim <= 32 ? fwd_simt<32>(a, st) : a.head_dim <= 64 ? fwd_simt<64>(a, st) : a.head_dim <= 96 ? fwd_simt<96>(a, st) : fwd_simt<128>(a, st);
+  const int d = dims_of(a);
+  return d == 32 ? fwd_simt<32>(a, st) : d == 64 ? fwd_simt<64>(a, st) : d == 96 ? fwd_simt<96>(a, st) : fwd_simt<128>(a, st);
 }
 cudaError_t attention_window_bwd_simt(const ra_attention_window_args& a, cudaStream_t st) {
   if (a.dtype != RA_F32) return cudaErrorNotSupported;
-  return a.head_dim <= 32 ? bwd_simt<32>(a, st) : a.head_dim <= 64 ? bwd_simt<64>(a, st) : a.head_dim <= 96 ? bwd_simt<96>(a, st) : bwd_simt<128>(a, st);
+  const int d = dims_of(a);
+  return d == 32 ? bwd_simt<32>(a, st) : d == 64 ? bwd_simt<64>(a, st) : d == 96 ? bwd_simt<96>(a, st) : bwd_simt<128>(a, st);
 }
 
 }  // namespace ra
