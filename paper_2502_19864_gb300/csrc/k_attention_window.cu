@@ -12,54 +12,70 @@
 // much longer than a window, several CTAs share a block's queries and a last kernel adds their parts in order.  The query
 // pass of the backward computes D on its way and leaves it for the key pass.  Rows past the sequence's end are loaded as
 // zeros, whatever memory holds there.
-// A thread keeps 4 x 4 scores and 4 x DH / 16 outputs in registers.  Paced by shared memory: 8 reads of 16 bytes a lane for
-// 64 multiply-adds (32 packed ones).  32 held rows make a CTA a step half as long as 64 did and twice as many: 3 sequences of
-// 333 tokens, 4 heads of 64 on 2, window 100, forward and backward 102 us (228 us).
+// A warp has four held rows: a thread keeps their scores with 2 of the 64 streamed rows and their outputs in DH / 32
+// columns.  What bounds it is the latency of a step at the sizes that fp32 models have, not a pipe: 32 held rows and eight
+// warps (64 rows and as many warps: 228 us for 3 sequences of 333 tokens, 4 heads of 64 on 2, window 100, forward and
+// backward; four warps of 4 x 4 scores a thread: 102 us; this: 75 us), and the next step's rows on their way.
 #include "common.cuh"
 #include "operators.h"
 
 namespace ra {
 namespace {
 
-constexpr int BH = 32, BT = 64, NT = 128, PP = BT + 4;  // rows held and streamed, threads, floats of a row of X
+constexpr int BH = 32, BT = 64, NT = 256, PP = BT + 4;  // rows held and streamed, threads, floats of a row of X
 constexpr float kLog2e = 1.4426950408889634f;
 
 template <int DH>
 struct Plan {
   static constexpr int DP = DH + 4;  // padded rows: eight lanes' 16 bytes of eight rows fall in distinct banks
   static constexpr int HELD = BH * DP, TILE = BT * DP;
-  static constexpr int FWD_BYTES = (HELD + 2 * TILE + BH * PP) * 4, BWD_BYTES = (2 * HELD + 2 * TILE + BH * PP + 2 * BT) * 4;
+  static constexpr int FWD_BYTES = (HELD + 4 * TILE + BH * PP) * 4, BWD_BYTES = (2 * HELD + 4 * TILE + BH * PP + 4 * BT) * 4;
 };
 
-// ROWS rows from r0 on of one head, zeros from row `len` on and past head_dim
+// ROWS rows from r0 on of one head, zeros from row `len` on and past head_dim, on their way (cp.async)
 template <int DH, int ROWS>
 __device__ __forceinline__ void load_rows(float* dst, const float* src, int64_t stride, int r0, int len, int head_dim) {
+  const uint32_t to = (uint32_t)__cvta_generic_to_shared(dst);
   for (int i = threadIdx.x; i < ROWS * DH / 4; i += NT) {
     const int r = i / (DH / 4), c = (i - r * (DH / 4)) * 4;
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (r0 + r < len && c < head_dim) x = *reinterpret_cast<const float4*>(src + (int64_t)(r0 + r) * stride + c);
-    *reinterpret_cast<float4*>(dst + r * Plan<DH>::DP + c) = x;
+    const bool live = r0 + r < len && c < head_dim;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + (r * Plan<DH>::DP + c) * 4),
+                 "l"(live ? src + (int64_t)(r0 + r) * stride + c : src), "r"(live ? 16 : 0) : "memory");
   }
 }
-// acc[i][j] = A[4 ty + i] . B[tx + 16 j]
+// 64 floats from r0 on, zeros from `len` on
+__device__ __forceinline__ void load_stats(float* dst, const float* src, int r0, int len) {
+  const int i = threadIdx.x;
+  if (i < BT) {
+    const bool live = r0 + i < len;
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst + i)),
+                 "l"(live ? src + r0 + i : src), "r"(live ? 4 : 0) : "memory");
+  }
+}
+__device__ __forceinline__ void loads_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void loads_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+// all but the newest group of this thread's loads have landed
+__device__ __forceinline__ void loads_before_newest() { asm volatile("cp.async.wait_group 1;" ::: "memory"); }
+
+// acc[i][j] = A[4 ty + i] . B[tx + 32 j]
 template <int DH>
-__device__ __forceinline__ void dot_rows(float (&acc)[4][4], const float* A, const float* B, int ty, int tx) {
-  float2 s[4][4];  // even and odd dims
+__device__ __forceinline__ void dot_rows(float (&acc)[4][2], const float* A, const float* B, int ty, int tx) {
+  float2 s[4][2];  // even and odd dims
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) s[i][j] = f2(0.f);
-#pragma unroll 4
+    for (int j = 0; j < 2; ++j) s[i][j] = f2(0.f);
+#pragma unroll 8
   for (int d = 0; d < DH; d += 4) {
-    float4 a[4], b[4];
+    float4 a[4], b[2];
 #pragma unroll
     for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const float4*>(A + (4 * ty + i) * Plan<DH>::DP + d);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) b[j] = *reinterpret_cast<const float4*>(B + (tx + 16 * j) * Plan<DH>::DP + d);
+    for (int j = 0; j < 2; ++j) b[j] = *reinterpret_cast<const float4*>(B + (tx + 32 * j) * Plan<DH>::DP + d);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < 2; ++j) {
         s[i][j] = __ffma2_rn(make_float2(a[i].x, a[i].y), make_float2(b[j].x, b[j].y), s[i][j]);
         s[i][j] = __ffma2_rn(make_float2(a[i].z, a[i].w), make_float2(b[j].z, b[j].w), s[i][j]);
       }
@@ -67,12 +83,12 @@ __device__ __forceinline__ void dot_rows(float (&acc)[4][4], const float* A, con
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = s[i][j].x + s[i][j].y;
+    for (int j = 0; j < 2; ++j) acc[i][j] = s[i][j].x + s[i][j].y;
 }
-// out[i][.] += sum_k X[4 ty + i][k] B[k][.], the thread's columns 2 tx + 32 c and the next
+// out[i][c] += sum_k X[4 ty + i][k] B[k][tx + 32 c]
 template <int DH>
-__device__ __forceinline__ void times_rows(float (&out)[4][DH / 16], const float* X, const float* B, int ty, int tx) {
-#pragma unroll 2
+__device__ __forceinline__ void times_rows(float (&out)[4][DH / 32], const float* X, const float* B, int ty, int tx) {
+#pragma unroll 4
   for (int k = 0; k < BT; k += 4) {
     float x[4][4];
 #pragma unroll
@@ -81,28 +97,22 @@ __device__ __forceinline__ void times_rows(float (&out)[4][DH / 16], const float
     for (int u = 0; u < 4; ++u)
 #pragma unroll
       for (int c = 0; c < DH / 32; ++c) {
-        const float2 b = *reinterpret_cast<const float2*>(B + (k + u) * Plan<DH>::DP + 2 * tx + 32 * c);
+        const float b = B[(k + u) * Plan<DH>::DP + tx + 32 * c];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          out[i][2 * c] = fmaf(x[i][u], b.x, out[i][2 * c]);
-          out[i][2 * c + 1] = fmaf(x[i][u], b.y, out[i][2 * c + 1]);
-        }
+        for (int i = 0; i < 4; ++i) out[i][c] = fmaf(x[i][u], b, out[i][c]);
       }
   }
 }
 template <int DH>
-__device__ __forceinline__ void store_rows(float* dst, int64_t stride, const float (&o)[4][DH / 16], const float (&f)[4],
+__device__ __forceinline__ void store_rows(float* dst, int64_t stride, const float (&o)[4][DH / 32], const float (&f)[4],
                                            int r0, int rows, int head_dim, int ty, int tx) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int r = r0 + 4 * ty + i;
     if (r >= rows) continue;
 #pragma unroll
-    for (int c = 0; c < DH / 32; ++c) {
-      const int col = 2 * tx + 32 * c;
-      if (col < head_dim)
-        *reinterpret_cast<float2*>(dst + (int64_t)r * stride + col) = make_float2(o[i][2 * c] * f[i], o[i][2 * c + 1] * f[i]);
-    }
+    for (int c = 0; c < DH / 32; ++c)
+      if (tx + 32 * c < head_dim) dst[(int64_t)r * stride + tx + 32 * c] = o[i][c] * f[i];
   }
 }
 
@@ -129,75 +139,97 @@ __device__ __forceinline__ bool sees(int i, int j, int W, int sinks, int len) {
   return j <= i && (i - j < W || j < sinks) && i < len;
 }
 
+// The key blocks that the queries r0 .. last see: those with sinks, [0, ns), then [lo, hi]
+struct KeyBlocks {
+  int ns, lo, n;
+  __device__ __forceinline__ int at(int i) const { return i < ns ? i : i - ns + lo; }
+};
+__device__ __forceinline__ KeyBlocks key_blocks(int r0, int last, int W, int sinks) {
+  KeyBlocks k;
+  const int hi = last / BT, first = r0 - W + 1, sink_blocks = sinks / BT + (sinks % BT != 0);
+  k.lo = first > 0 ? first / BT : 0;
+  k.ns = sink_blocks < hi + 1 ? sink_blocks : hi + 1;
+  if (k.lo < k.ns) k.lo = k.ns;
+  k.n = k.ns + (hi >= k.lo ? hi - k.lo + 1 : 0);
+  return k;
+}
+
 template <int DH>
 __global__ void __launch_bounds__(NT) window_fwd_simt_kernel(const __grid_constant__ ra_attention_window_args a, int W, int n_blk) {
   extern __shared__ __align__(16) float sm[];
   using P = Plan<DH>;
-  float *Q = sm, *K = Q + P::HELD, *V = K + P::TILE, *X = V + P::TILE;
+  float *Q = sm, *KV = Q + P::HELD, *X = KV + 4 * P::TILE;  // (two buffers of K and V)
   pdl_wait();
   pdl_trigger();
   const Geometry g = geometry(a, a.n_heads, n_blk);
-  const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15, q0 = g.blk * BH, dh = a.head_dim;
+  const int tid = threadIdx.x, ty = tid >> 5, tx = tid & 31, q0 = g.blk * BH, dh = a.head_dim;
   const int kvh = g.head / (a.n_heads / a.n_kv_heads);
   const int64_t tok0 = (int64_t)g.b * a.seq;
   const float* q = (const float*)a.q_dev + tok0 * a.q_stride + g.head * dh;
   const float* k = (const float*)a.k_dev + tok0 * a.k_stride + kvh * dh;
   const float* v = (const float*)a.v_dev + tok0 * a.v_stride + kvh * dh;
-  float o[4][DH / 16], m[4], l[4];
+  float o[4][DH / 32], m[4], l[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     m[i] = -INFINITY;
     l[i] = 0.f;
 #pragma unroll
-    for (int c = 0; c < DH / 16; ++c) o[i][c] = 0.f;
+    for (int c = 0; c < DH / 32; ++c) o[i][c] = 0.f;
   }
   const float sl2 = a.scale * kLog2e;
   if (q0 < g.len) {
     load_rows<DH, BH>(Q, q, a.q_stride, q0, g.len, dh);
-    const int last = q0 + BH - 1 < g.len ? q0 + BH - 1 : g.len - 1, hi = last / BT;
-    const int first = q0 - W + 1, lo = first > 0 ? first / BT : 0;
-    for (int kb = 0; kb <= hi; ++kb) {
-      if (kb < lo && kb * BT >= a.sinks) kb = lo;
-      const int k0 = kb * BT;
+    const KeyBlocks kb = key_blocks(q0, q0 + BH - 1 < g.len ? q0 + BH - 1 : g.len - 1, W, a.sinks);
+    auto fetch = [&](int n) {
+      if (n < kb.n) {
+        float* to = KV + (n & 1) * 2 * P::TILE;
+        load_rows<DH, BT>(to, k, a.k_stride, kb.at(n) * BT, g.len, dh);
+        load_rows<DH, BT>(to + P::TILE, v, a.v_stride, kb.at(n) * BT, g.len, dh);
+      }
+      loads_commit();
+    };
+    fetch(0);
+    for (int n = 0; n < kb.n; ++n) {
+      const int k0 = kb.at(n) * BT;
+      const float *K = KV + (n & 1) * 2 * P::TILE, *V = K + P::TILE;
+      fetch(n + 1);
+      loads_before_newest();
       __syncthreads();
-      load_rows<DH, BT>(K, k, a.k_stride, k0, g.len, dh);
-      load_rows<DH, BT>(V, v, a.v_stride, k0, g.len, dh);
-      __syncthreads();
-      float s[4][4];
+      float s[4][2];
       dot_rows<DH>(s, Q, K, ty, tx);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int qi = q0 + 4 * ty + i;
         float bm = -INFINITY;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          s[i][j] = sees(qi, k0 + tx + 16 * j, W, a.sinks, g.len) ? s[i][j] * sl2 : -INFINITY;
+        for (int j = 0; j < 2; ++j) {
+          s[i][j] = sees(qi, k0 + tx + 32 * j, W, a.sinks, g.len) ? s[i][j] * sl2 : -INFINITY;
           bm = fmaxf(bm, s[i][j]);
         }
-#pragma unroll
-        for (int x = 8; x > 0; x >>= 1) bm = fmaxf(bm, __shfl_xor_sync(0xffffffffu, bm, x));
+        bm = warp_max(bm);
         const float mn = fmaxf(m[i], bm), ms = mn == -INFINITY ? 0.f : mn, f = exp2f(m[i] - ms);
         m[i] = mn;
         float sum = 0.f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < 2; ++j) {
           const float p = exp2f(s[i][j] - ms);
           sum += p;
-          X[(4 * ty + i) * PP + tx + 16 * j] = p;
+          X[(4 * ty + i) * PP + tx + 32 * j] = p;
         }
-        l[i] = l[i] * f + sum;  // (a lane's own share; the 16 lanes of a row are summed at the end)
+        l[i] = l[i] * f + sum;  // (a lane's own share; the lanes are summed at the end)
 #pragma unroll
-        for (int c = 0; c < DH / 16; ++c) o[i][c] *= f;
+        for (int c = 0; c < DH / 32; ++c) o[i][c] *= f;
       }
       __syncthreads();
       times_rows<DH>(o, X, V, ty, tx);
+      __syncthreads();  // the buffer and X are free again
     }
   }
+  loads_done();
   float f[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-#pragma unroll
-    for (int x = 8; x > 0; x >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
+    l[i] = warp_sum(l[i]);
     f[i] = l[i] > 0.f ? 1.f / l[i] : l[i] == 0.f ? 0.f : l[i];
     const int qi = q0 + 4 * ty + i;
     if (a.lse_dev && tx == 0 && qi < a.seq)
@@ -213,7 +245,7 @@ __global__ void __launch_bounds__(NT) window_bwd_simt_kernel(const __grid_consta
                                                              float* parts, int W, int n_blk, int split, int chunks) {
   extern __shared__ __align__(16) float sm[];
   using P = Plan<DH>;
-  float *T0 = sm, *T1 = T0 + P::HELD, *T2 = T1 + P::HELD, *T3 = T2 + P::TILE, *X = T3 + P::TILE, *L = X + BH * PP, *D = L + BT;
+  float *T0 = sm, *T1 = T0 + P::HELD, *BUF = T1 + P::HELD, *X = BUF + 4 * P::TILE, *STAT = X + BH * PP;  // (two buffers of the streamed pair, and of lse and D)
   pdl_wait();
   pdl_trigger();
   const int G = a.n_heads / a.n_kv_heads, items = n_blk - split + split * chunks;
@@ -226,33 +258,33 @@ __global__ void __launch_bounds__(NT) window_bwd_simt_kernel(const __grid_consta
     chunk = shared ? it - g.blk * chunks : 0;
     n_chunks = shared ? chunks : 1;
   }
-  const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15, r0 = g.blk * BH, dh = a.head_dim;
+  const int tid = threadIdx.x, ty = tid >> 5, tx = tid & 31, r0 = g.blk * BH, dh = a.head_dim;
   const int kvh = KEYS ? g.head : g.head / G;
   const int64_t tok0 = (int64_t)g.b * a.seq;
   const float* k = (const float*)a.k_dev + tok0 * a.k_stride + kvh * dh;
   const float* v = (const float*)a.v_dev + tok0 * a.v_stride + kvh * dh;
-  float u[4][DH / 16], w[4][DH / 16];  // KEYS: dK, dV; else dQ
+  float u[4][DH / 32], w[4][DH / 32];  // KEYS: dK, dV; else dQ
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int c = 0; c < DH / 16; ++c) u[i][c] = w[i][c] = 0.f;
+    for (int c = 0; c < DH / 32; ++c) u[i][c] = w[i][c] = 0.f;
   const float sl2 = a.scale * kLog2e;
   // X = P (or P^T), then dS in s
-  auto probabilities = [&](float (&s)[4][4], int c0) {
+  auto probabilities = [&](float (&s)[4][2], int c0, const float* L) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int row = 4 * ty + i, col = tx + 16 * j;
+      for (int j = 0; j < 2; ++j) {
+        const int row = 4 * ty + i, col = tx + 32 * j;
         const int qi = KEYS ? c0 + col : r0 + row, ki = KEYS ? r0 + row : c0 + col;
-        s[i][j] = sees(qi, ki, W, a.sinks, g.len) ? exp2f(s[i][j] * sl2 - L[KEYS ? col : row]) : 0.f;
+        s[i][j] = sees(qi, ki, W, a.sinks, g.len) ? exp2f(s[i][j] * sl2 - L[KEYS ? col : row] * kLog2e) : 0.f;
       }
   };
-  auto put = [&](const float (&s)[4][4]) {
+  auto put = [&](const float (&s)[4][2]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) X[(4 * ty + i) * PP + tx + 16 * j] = s[i][j];
+      for (int j = 0; j < 2; ++j) X[(4 * ty + i) * PP + tx + 32 * j] = s[i][j];
   };
   if (r0 < g.len) {
     const int last = r0 + BH - 1 < g.len ? r0 + BH - 1 : g.len - 1;
@@ -263,23 +295,29 @@ __global__ void __launch_bounds__(NT) window_bwd_simt_kernel(const __grid_consta
       const int first = r0 / BT, per_head = (int)(far < g.len ? far : g.len - 1) / BT - first + 1;
       const int64_t total = (int64_t)per_head * G;
       const int n1 = (int)(total * (chunk + 1) / n_chunks);
-      for (int n = (int)(total * chunk / n_chunks); n < n1; ++n) {
-        const int h = kvh * G + n / per_head, q0 = (first + n % per_head) * BT;
-        const float* q = (const float*)a.q_dev + tok0 * a.q_stride + h * dh;
-        const float* go = (const float*)a.dout_dev + tok0 * a.dout_stride + h * dh;
-        __syncthreads();
-        load_rows<DH, BT>(T2, q, a.q_stride, q0, g.len, dh);
-        load_rows<DH, BT>(T3, go, a.dout_stride, q0, g.len, dh);
-        if (tid < BT) {
-          const int64_t at = ((int64_t)g.b * a.n_heads + h) * a.seq + q0 + tid;
-          const bool live = q0 + tid < g.len;
-          L[tid] = live ? a.lse_dev[at] * kLog2e : 0.f;
-          D[tid] = live ? Dv[at] : 0.f;
+      const int n0 = (int)(total * chunk / n_chunks);
+      auto fetch = [&](int n) {
+        if (n < n1) {
+          const int h = kvh * G + n / per_head, q0 = (first + n % per_head) * BT, buf = (n - n0) & 1;
+          float* to = BUF + buf * 2 * P::TILE;
+          load_rows<DH, BT>(to, (const float*)a.q_dev + tok0 * a.q_stride + h * dh, a.q_stride, q0, g.len, dh);
+          load_rows<DH, BT>(to + P::TILE, (const float*)a.dout_dev + tok0 * a.dout_stride + h * dh, a.dout_stride, q0, g.len, dh);
+          const int64_t at = ((int64_t)g.b * a.n_heads + h) * a.seq;
+          load_stats(STAT + buf * 2 * BT, a.lse_dev + at, q0, g.len);
+          load_stats(STAT + buf * 2 * BT + BT, Dv + at, q0, g.len);
         }
+        loads_commit();
+      };
+      fetch(n0);
+      for (int n = n0; n < n1; ++n) {
+        const int q0 = (first + n % per_head) * BT, buf = (n - n0) & 1;
+        const float *T2 = BUF + buf * 2 * P::TILE, *T3 = T2 + P::TILE, *L = STAT + buf * 2 * BT, *D = L + BT;
+        fetch(n + 1);
+        loads_before_newest();
         __syncthreads();
-        float s[4][4], dp[4][4];
+        float s[4][2], dp[4][2];
         dot_rows<DH>(s, T0, T2, ty, tx);
-        probabilities(s, q0);
+        probabilities(s, q0, L);
         put(s);
         dot_rows<DH>(dp, T1, T3, ty, tx);
         __syncthreads();
@@ -287,58 +325,73 @@ __global__ void __launch_bounds__(NT) window_bwd_simt_kernel(const __grid_consta
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) s[i][j] *= dp[i][j] - D[tx + 16 * j];
+          for (int j = 0; j < 2; ++j) s[i][j] *= dp[i][j] - D[tx + 32 * j];
         __syncthreads();
         put(s);
         __syncthreads();
         times_rows<DH>(u, X, T2, ty, tx);
+        __syncthreads();  // the buffer and X are free again
       }
     } else {
       load_rows<DH, BH>(T0, (const float*)a.q_dev + tok0 * a.q_stride + g.head * dh, a.q_stride, r0, g.len, dh);
       load_rows<DH, BH>(T1, (const float*)a.dout_dev + tok0 * a.dout_stride + g.head * dh, a.dout_stride, r0, g.len, dh);
       const int64_t at = ((int64_t)g.b * a.n_heads + g.head) * a.seq + r0;
-      if (tid < BH) L[tid] = r0 + tid < g.len ? a.lse_dev[at + tid] * kLog2e : 0.f;
+      float *L = STAT, *D = L + BT;
+      if (tid < BH) L[tid] = r0 + tid < g.len ? a.lse_dev[at + tid] : 0.f;
+      const KeyBlocks kb = key_blocks(r0, last, W, a.sinks);
+      auto fetch = [&](int n) {
+        if (n < kb.n) {
+          float* to = BUF + (n & 1) * 2 * P::TILE;
+          load_rows<DH, BT>(to, k, a.k_stride, kb.at(n) * BT, g.len, dh);
+          load_rows<DH, BT>(to + P::TILE, v, a.v_stride, kb.at(n) * BT, g.len, dh);
+        }
+        loads_commit();
+      };
+      loads_commit();
+      fetch(0);
+      loads_before_newest();  // the held rows
       __syncthreads();
-      // D = dO . o, four threads a row
+      // D = dO . o, eight threads a row
       {
-        const int row = tid >> 2;
+        const int row = tid >> 3;
         float d = 0.f;
         if (r0 + row < g.len) {
           const float* o = (const float*)a.out_dev + (tok0 + r0 + row) * a.out_stride + g.head * dh;
-          for (int c = 4 * (tid & 3); c < dh; c += 16) {
+          for (int c = 4 * (tid & 7); c < dh; c += 32) {
             const float4 x = *reinterpret_cast<const float4*>(o + c), y = *reinterpret_cast<const float4*>(T1 + row * P::DP + c);
             d = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, d))));
           }
         }
         d += __shfl_xor_sync(0xffffffffu, d, 1);
         d += __shfl_xor_sync(0xffffffffu, d, 2);
-        if ((tid & 3) == 0) {
+        d += __shfl_xor_sync(0xffffffffu, d, 4);
+        if ((tid & 7) == 0) {
           D[row] = d;
           if (r0 + row < a.seq) Dv[at + row] = d;
         }
       }
-      const int hi = last / BT, first = r0 - W + 1, lo = first > 0 ? first / BT : 0;
-      for (int kb = 0; kb <= hi; ++kb) {
-        if (kb < lo && kb * BT >= a.sinks) kb = lo;
-        const int k0 = kb * BT;
+      for (int n = 0; n < kb.n; ++n) {
+        const int k0 = kb.at(n) * BT;
+        const float *T2 = BUF + (n & 1) * 2 * P::TILE, *T3 = T2 + P::TILE;
+        fetch(n + 1);
+        loads_before_newest();
         __syncthreads();
-        load_rows<DH, BT>(T2, k, a.k_stride, k0, g.len, dh);
-        load_rows<DH, BT>(T3, v, a.v_stride, k0, g.len, dh);
-        __syncthreads();
-        float s[4][4], dp[4][4];
+        float s[4][2], dp[4][2];
         dot_rows<DH>(s, T0, T2, ty, tx);
-        probabilities(s, k0);
+        probabilities(s, k0, L);
         dot_rows<DH>(dp, T1, T3, ty, tx);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) s[i][j] *= dp[i][j] - D[4 * ty + i];
+          for (int j = 0; j < 2; ++j) s[i][j] *= dp[i][j] - D[4 * ty + i];
         put(s);
         __syncthreads();
         times_rows<DH>(u, X, T2, ty, tx);
+        __syncthreads();  // the buffer and X are free again
       }
     }
   }
+  loads_done();
   const float fs[4] = {a.scale, a.scale, a.scale, a.scale}, f1[4] = {1.f, 1.f, 1.f, 1.f};
   if (KEYS && n_chunks > 1) {
     float* part = parts + (((int64_t)(g.b * a.n_kv_heads + g.head) * split + g.blk) * chunks + chunk) * (2 * BH * DH);
@@ -382,14 +435,25 @@ int window_of(const ra_attention_window_args& a) { return a.window == 0 || a.win
 
 int dims_of(const ra_attention_window_args& a) { return a.head_dim <= 32 ? 32 : a.head_dim <= 64 ? 64 : a.head_dim <= 96 ? 96 : 128; }
 
-// How many CTAs share each of the first key blocks: an ordinary block is seen from W + 32 queries, one with sinks from all.
-// Up to 128 sinks and where that is twice as long, as many CTAs as bring them back to an ordinary one's length, at most 32.
+// How many CTAs share each of the first `split` key blocks.  An ordinary block is seen from W + 32 queries, one with sinks
+// from all: up to 128 sinks and where that is twice as long, as many CTAs as bring those blocks back to an ordinary one's
+// length, at most 32.  Where the key blocks are fewer than 152 (the SMs, as a constant: the order of the sums is the shape's),
+// all are shared, so that the SMs have a CTA each, at most 8 a block (66 blocks of the case above: 45 -> 35 us).
 void split_of(const ra_attention_window_args& a, int& split, int& chunks) {
   const int64_t ordinary = (int64_t)window_of(a) + BH;
   split = 0;
   chunks = 1;
+  const int n_blk = (a.seq + BH - 1) / BH;
+  const int64_t all = (int64_t)n_blk * a.batch * a.n_kv_heads;
+  if (all == 0) return;
+  if (all < 152) {
+    split = n_blk;
+    chunks = (int)((152 + all - 1) / all);
+    if (chunks > 8) chunks = 8;
+    return;
+  }
   if (a.sinks < 1 || a.sinks > 128 || a.seq < 2 * ordinary) return;
-  const int n_blk = (a.seq + BH - 1) / BH, blocks = (a.sinks + BH - 1) / BH;
+  const int blocks = (a.sinks + BH - 1) / BH;
   split = blocks < n_blk ? blocks : n_blk;
   const int64_t n = (a.seq + ordinary - 1) / ordinary;
   chunks = n < 32 ? (int)n : 32;
