@@ -10,6 +10,9 @@
 //   warp 8              issues the products: O0 += P0 V, S0 = Q0 K', O1 += P1 V, S1 = Q1 K', ...: while one tile's softmax
 //                       runs the tensor cores have the other's products;
 //   warp 9              loads Q, then K and V blocks by TMA into a ring.
+// The CTAs are persistent: the copies and first products of a CTA's next pair of tiles run while the last outputs of this one
+// leave (one pair of tiles a CTA: 60 us for 8 x 1024 tokens of 16 heads and window 256, this: @T@ us; a pair takes as
+// little as three blocks, and its start and end as long).
 // O stays in TMEM.  It is rescaled only when a row's maximum has grown by more than 2^8 since the scale in use (p then stays
 // below 2^8 and sums in fp32 lose nothing): the first block sets the scale and almost none after it changes it.
 // Key blocks that no row of a tile sees are not loaded: a tile walks the blocks that hold sinks, then its window.  Rows past a
@@ -34,6 +37,9 @@ struct WindowFwdArgs {
   int batch, seq, n_heads, n_kv_heads, W, sinks;
   int pair_heads;  // the two tiles are two heads of a group; else two row blocks
   int n_work;      // row blocks (or pairs of them) a (sequence, head or pair of heads)
+  int units, items;  // (sequence, head or pair of heads)s; pairs of tiles
+  bf16* out;
+  int64_t out_stride;
   float sl2;
 };
 
@@ -52,35 +58,68 @@ struct Blocks {
   __device__ __forceinline__ bool active(int t, int j) const { return j <= thi[t] && (j >= tlo[t] || j < ns); }
 };
 
+// bits 0 .. n - 1
+__device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
+
+// A pair of tiles, and what its rows see; the row blocks with the most keys come first
+struct Item {
+  int b, len, head[2], q0[2], kvh;
+  Blocks kb;
+};
+__device__ __forceinline__ Item item_of(const WindowFwdArgs& a, int id) {
+  Item x;
+  const int work = a.n_work - 1 - id / a.units, u = id % a.units;
+  const int per = a.pair_heads ? a.n_heads / 2 : a.n_heads;
+  x.b = u / per;
+  const int unit = u - x.b * per;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    x.head[t] = a.pair_heads ? 2 * unit + t : unit;
+    x.q0[t] = a.pair_heads ? work * BR : (2 * work + t) * BR;
+  }
+  x.kvh = x.head[0] / (a.n_heads / a.n_kv_heads);
+  int len = a.lens ? __ldg(a.lens + x.b) : a.seq;
+  if (len < 0 || len > a.seq) {
+    set_dev_error(a.err, RA_DEVERR_BOUNDS);
+    len = len < 0 ? 0 : a.seq;
+  }
+  x.len = len;
+  Blocks& kb = x.kb;
+  kb.lo = 1 << 30;
+  kb.hi = -1;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const bool any = x.q0[t] < len;
+    const int last = x.q0[t] + BR - 1 < len ? x.q0[t] + BR - 1 : len - 1, first = x.q0[t] - a.W + 1;
+    kb.thi[t] = any ? last / BR : -1;
+    kb.tlo[t] = any && first > 0 ? first / BR : 0;
+    if (any && kb.tlo[t] < kb.lo) kb.lo = kb.tlo[t];
+    if (kb.thi[t] > kb.hi) kb.hi = kb.thi[t];
+  }
+  const int sink_blocks = a.sinks / BR + (a.sinks % BR != 0);
+  kb.ns = sink_blocks < kb.hi + 1 ? sink_blocks : kb.hi + 1;
+  if (kb.lo < kb.ns) kb.lo = kb.ns;
+  kb.n = kb.hi < 0 ? 0 : kb.ns + (kb.hi >= kb.lo ? kb.hi - kb.lo + 1 : 0);
+  return x;
+}
+
 template <int DH>
 __global__ void __launch_bounds__(THREADS, 1) window_fwd_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
-    const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmO,
-    const __grid_constant__ WindowFwdArgs a) {
+    const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ WindowFwdArgs a) {
   using Pl = FwdPlan<DH>;
   constexpr int SLOTS = Pl::SLOTS, BLK = Pl::BLK;
   extern __shared__ __align__(1024) uint8_t smem[];
-  __shared__ __align__(8) uint64_t full[SLOTS], empty[SLOTS], q_full, s_full[2], p_full[2], o_full[2], staged[2], drain;
+  // q_read: the last product with this pair's queries is done; o_full: a tile's outputs are complete; o_read: they have left TMEM
+  __shared__ __align__(8) uint64_t full[SLOTS], empty[SLOTS], q_full, q_read, s_full[2], p_full[2], o_full[2], o_read[2], drain;
   __shared__ uint32_t tmem_sh;
   __shared__ volatile int abort_sh;
+  __shared__ int info[8][8];
   const uint32_t sb = smem_u32(smem);
   if (sb & 1023u) {  // the swizzled operand tiles need 1024-byte alignment
     if (threadIdx.x == 0) set_dev_error(a.err, RA_DEVERR_BOUNDS);
     return;
   }
   const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
-
-  // ---- this CTA's tiles; the row blocks with the most keys first
-  const int G = a.n_heads / a.n_kv_heads, units = a.pair_heads ? a.n_heads / 2 : a.n_heads;
-  const int work = a.n_work - 1 - (int)(blockIdx.x % a.n_work), bu = (int)(blockIdx.x / a.n_work);
-  const int b = bu / units, unit = bu - b * units;
-  int head[2], q0[2];
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    head[t] = a.pair_heads ? 2 * unit + t : unit;
-    q0[t] = a.pair_heads ? work * BR : (2 * work + t) * BR;
-  }
-  const int kvh = head[0] / G;
-
   if (warp == 9) {
     if (elect_one()) {
 #pragma unroll
@@ -89,13 +128,14 @@ __global__ void __launch_bounds__(THREADS, 1) window_fwd_tc_kernel(const __grid_
         mbar_init(&empty[i], 1);
       }
       mbar_init(&q_full, 1);
+      mbar_init(&q_read, 1);
       mbar_init(&drain, 1);
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         mbar_init(&s_full[t], 1);
         mbar_init(&p_full[t], 4);
         mbar_init(&o_full[t], 1);
-        mbar_init(&staged[t], 4);
+        mbar_init(&o_read[t], 4);
       }
       abort_sh = 0;
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -109,27 +149,6 @@ __global__ void __launch_bounds__(THREADS, 1) window_fwd_tc_kernel(const __grid_
   }
   pdl_wait();
   pdl_trigger();
-  int len = a.lens ? a.lens[b] : a.seq;
-  if (len < 0 || len > a.seq) {
-    if (tid == 0) set_dev_error(a.err, RA_DEVERR_BOUNDS);
-    len = len < 0 ? 0 : a.seq;
-  }
-  Blocks kb;
-  kb.lo = 1 << 30;
-  kb.hi = -1;
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const bool any = q0[t] < len;
-    const int last = q0[t] + BR - 1 < len ? q0[t] + BR - 1 : len - 1, first = q0[t] - a.W + 1;
-    kb.thi[t] = any ? last / BR : -1;
-    kb.tlo[t] = any && first > 0 ? first / BR : 0;
-    if (any && kb.tlo[t] < kb.lo) kb.lo = kb.tlo[t];
-    if (kb.thi[t] > kb.hi) kb.hi = kb.thi[t];
-  }
-  const int sink_blocks = a.sinks / BR + (a.sinks % BR != 0);
-  kb.ns = sink_blocks < kb.hi + 1 ? sink_blocks : kb.hi + 1;
-  if (kb.lo < kb.ns) kb.lo = kb.ns;
-  kb.n = kb.hi < 0 ? 0 : kb.ns + (kb.hi >= kb.lo ? kb.hi - kb.lo + 1 : 0);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -137,95 +156,113 @@ __global__ void __launch_bounds__(THREADS, 1) window_fwd_tc_kernel(const __grid_
 
   if (warp == 9) {
     // ------------------------------------------------------------ copies
-    if (kb.n > 0 && elect_one()) {
-      auto load = [&](const CUtensorMap* tm, uint32_t dst, uint64_t* bar, int col, int row) {
-        mbar_expect_tx(bar, BLK);
+    if (elect_one()) {
+      auto load = [&](const CUtensorMap* tm, uint32_t dst, uint64_t* bar, int col, int row, int b) {
 #pragma unroll
         for (int n = 0; n < DH / 64; ++n) tma_load3(tm, dst + n * (BR * 128), bar, col + 64 * n, row, b);
       };
-      mbar_expect_tx(&q_full, 2 * BLK);
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int n = 0; n < DH / 64; ++n)
-          tma_load3(&tmQ, sb + Pl::Q + t * BLK + n * (BR * 128), &q_full, head[t] * DH + 64 * n, q0[t], b);
-      int i = 0;  // block of the ring: keys and values in turn
+      int i = 0, nq = 0;  // blocks of the ring (keys and values in turn) and pairs of query tiles that were started
       bool ok = true;
-      for (; i < 2 * kb.n && ok; ++i) {
-        const int s = i % SLOTS;
-        if (i >= SLOTS) ok = mbar_wait(&empty[s], ((i / SLOTS) - 1) & 1, &abort_sh, a.err);
-        if (ok) load(i & 1 ? &tmV : &tmK, sb + Pl::RING + s * BLK, &full[s], kvh * DH, kb.at(i >> 1) * BR);
+      for (int id = blockIdx.x; id < a.items && ok; id += gridDim.x) {
+        const Item x = item_of(a, id);
+        if (x.kb.n == 0) continue;
+        if (nq > 0) ok = mbar_wait(&q_read, (nq - 1) & 1, &abort_sh, a.err);
+        if (!ok) break;
+        mbar_expect_tx(&q_full, 2 * BLK);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) load(&tmQ, sb + Pl::Q + t * BLK, &q_full, x.head[t] * DH, x.q0[t], x.b);
+        ++nq;
+        for (int k = 0; k < 2 * x.kb.n; ++k) {
+          const int s = i % SLOTS;
+          if (i >= SLOTS) ok = mbar_wait(&empty[s], ((i / SLOTS) - 1) & 1, &abort_sh, a.err);
+          if (!ok) break;
+          mbar_expect_tx(&full[s], BLK);
+          load(k & 1 ? &tmV : &tmK, sb + Pl::RING + s * BLK, &full[s], x.kvh * DH, x.kb.at(k >> 1) * BR, x.b);
+          ++i;
+        }
       }
       if (!ok) {
         // a wait gave up: let the copies on their way land before shared memory is released
         volatile int no_abort = 0;
-        const int issued = i - 1;  // (the block whose slot did not come free was not)
-        mbar_wait(&q_full, 0, &no_abort, nullptr);
-        for (int k = issued > SLOTS ? issued - SLOTS : 0; k < issued; ++k)
-          mbar_wait(&full[k % SLOTS], (k / SLOTS) & 1, &no_abort, nullptr);
+        if (nq > 0) mbar_wait(&q_full, (nq - 1) & 1, &no_abort, nullptr);
+        for (int k = i > SLOTS ? i - SLOTS : 0; k < i; ++k) mbar_wait(&full[k % SLOTS], (k / SLOTS) & 1, &no_abort, nullptr);
       }
     }
     __syncwarp();
   } else if (warp == 8) {
     // ------------------------------------------------------------ products
     constexpr uint32_t IDS = idesc_bf16(BR, BR), IDO = idesc_bf16_bmn(BR, DH);
-    bool ok = kb.n == 0 || mbar_wait_warp(&q_full, 0, &abort_sh, a.err);
+    bool ok = true;
     uint32_t p_phase[2] = {0, 0};
-    bool started[2] = {false, false}, pend[2] = {false, false};
-    int prev = 0;
-    for (int i = 0; i <= kb.n && ok; ++i) {
-      const int j = i < kb.n ? kb.at(i) : -1;
-      const int ks = (2 * i) % SLOTS, vs = (2 * i - 1 + SLOTS) % SLOTS;  // this block's keys, the last one's values
-      if (i > 0) {
-        ok = mbar_wait_warp(&full[vs], ((2 * i - 1) / SLOTS) & 1, &abort_sh, a.err);
-        if (!ok) break;
-        const int dead = len - prev * BR;  // rows from here on are past the sequence's end
-        if (dead < BR) zero_rows<DH>(smem + Pl::RING + vs * BLK, dead, lane);
-      }
-      if (i < kb.n) {
-        ok = mbar_wait_warp(&full[ks], ((2 * i) / SLOTS) & 1, &abort_sh, a.err);
-        if (!ok) break;
-      }
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        if (pend[t]) {
-          ok = mbar_wait_warp(&p_full[t], p_phase[t], &abort_sh, a.err);
+    int nq = 0, no[2] = {0, 0}, ring = 0;  // pairs of tiles; tiles with outputs; blocks of the ring before this pair's
+    for (int id = blockIdx.x; id < a.items && ok; id += gridDim.x) {
+      const Item x = item_of(a, id);
+      const Blocks& kb = x.kb;
+      if (kb.n == 0) continue;
+      ok = mbar_wait_warp(&q_full, nq & 1, &abort_sh, a.err);
+      ++nq;
+      bool started[2] = {false, false}, pend[2] = {false, false};
+      int prev = 0;
+      for (int i = 0; i <= kb.n && ok; ++i) {
+        const int j = i < kb.n ? kb.at(i) : -1;
+        const int kn = ring + 2 * i, vn = kn - 1, ks = kn % SLOTS, vs = (vn + SLOTS) % SLOTS;  // this block's keys, the last one's values
+        if (i > 0) {
+          ok = mbar_wait_warp(&full[vs], (vn / SLOTS) & 1, &abort_sh, a.err);
           if (!ok) break;
-          p_phase[t] ^= 1u;
-          tc_fence_after();
-          if (elect_one()) {
-            const uint32_t v = sb + Pl::RING + vs * BLK;
-#pragma unroll
-            for (int kk = 0; kk < BR / 16; ++kk)
-              umma_bf16_ts(tmem + Pl::C_O + t * DH, tmem + Pl::C_S + t * BR + kk * 8, sdesc_mn_sw128_lbo(v + kk * 2048, BR * 128), IDO,
-                           started[t] || kk > 0 ? 1u : 0u);
-            if (prev == kb.thi[t]) umma_commit(&o_full[t]);
-          }
-          __syncwarp();
-          started[t] = true;
-          pend[t] = false;
+          const int dead = x.len - prev * BR;  // rows from here on are past the sequence's end
+          if (dead < BR) zero_rows<DH>(smem + Pl::RING + vs * BLK, dead, lane);
         }
-        if (i < kb.n && kb.active(t, j)) {
-          if (elect_one()) {
-            const uint32_t q = sb + Pl::Q + t * BLK, k = sb + Pl::RING + ks * BLK;
+        if (i < kb.n) {
+          ok = mbar_wait_warp(&full[ks], (kn / SLOTS) & 1, &abort_sh, a.err);
+          if (!ok) break;
+        }
 #pragma unroll
-            for (int kk = 0; kk < DH / 16; ++kk) {
-              const uint32_t o = (kk >> 2) * (BR * 128) + (kk & 3) * 32;
-              umma_bf16(tmem + Pl::C_S + t * BR, sdesc_sw128(q + o), sdesc_sw128(k + o), IDS, kk > 0 ? 1u : 0u);
+        for (int t = 0; t < 2; ++t) {
+          if (pend[t]) {
+            ok = mbar_wait_warp(&p_full[t], p_phase[t], &abort_sh, a.err);
+            if (ok && !started[t]) {  // the outputs of this tile's last pair have left TMEM
+              if (no[t] > 0) ok = mbar_wait_warp(&o_read[t], (no[t] - 1) & 1, &abort_sh, a.err);
+              ++no[t];
             }
-            umma_commit(&s_full[t]);
+            if (!ok) break;
+            p_phase[t] ^= 1u;
+            tc_fence_after();
+            if (elect_one()) {
+              const uint32_t v = sb + Pl::RING + vs * BLK;
+#pragma unroll
+              for (int kk = 0; kk < BR / 16; ++kk)
+                umma_bf16_ts(tmem + Pl::C_O + t * DH, tmem + Pl::C_S + t * BR + kk * 8, sdesc_mn_sw128_lbo(v + kk * 2048, BR * 128), IDO,
+                             started[t] || kk > 0 ? 1u : 0u);
+              if (prev == kb.thi[t]) umma_commit(&o_full[t]);
+            }
+            __syncwarp();
+            started[t] = true;
+            pend[t] = false;
           }
-          __syncwarp();
-          pend[t] = true;
+          if (i < kb.n && kb.active(t, j)) {
+            if (elect_one()) {
+              const uint32_t q = sb + Pl::Q + t * BLK, k = sb + Pl::RING + ks * BLK;
+#pragma unroll
+              for (int kk = 0; kk < DH / 16; ++kk) {
+                const uint32_t o = (kk >> 2) * (BR * 128) + (kk & 3) * 32;
+                umma_bf16(tmem + Pl::C_S + t * BR, sdesc_sw128(q + o), sdesc_sw128(k + o), IDS, kk > 0 ? 1u : 0u);
+              }
+              umma_commit(&s_full[t]);
+            }
+            __syncwarp();
+            pend[t] = true;
+          }
         }
+        if (!ok) break;
+        if (elect_one()) {
+          if (i > 0) umma_commit(&empty[vs]);
+          if (i < kb.n) umma_commit(&empty[ks]);
+          if (i == kb.n - 1) umma_commit(&q_read);
+        }
+        __syncwarp();
+        prev = j;
       }
-      if (!ok) break;
-      if (elect_one()) {
-        if (i > 0) umma_commit(&empty[vs]);
-        if (i < kb.n) umma_commit(&empty[ks]);
-      }
-      __syncwarp();
-      prev = j;
+      ring += 2 * kb.n;
     }
     // what was issued ends before shared memory and TMEM are released
     if (elect_one()) {
@@ -236,111 +273,147 @@ __global__ void __launch_bounds__(THREADS, 1) window_fwd_tc_kernel(const __grid_
     __syncwarp();
   } else {
     // ------------------------------------------------------------ softmax: warps 4 t .. 4 t + 3, thread = row
-    const int t = warp >> 2, row = tid & 127, q = q0[t] + row;
+    const int t = warp >> 2, row = tid & 127;
     const uint32_t tS = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + Pl::C_S + t * BR;
     const uint32_t tO = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + Pl::C_O + t * DH;
-    float m = -INFINITY, l = 0.f;  // m: the scale in use (powers of two); l: this row's sum under it
-    uint32_t s_phase = 0;
-    bool ok = true, first = true;
-    for (int i = 0; i < kb.n && ok; ++i) {
-      const int j = kb.at(i);
-      if (!kb.active(t, j)) continue;
-      ok = mbar_wait_warp(&s_full[t], s_phase, &abort_sh, a.err);
-      if (!ok) break;
-      s_phase ^= 1u;
-      tc_fence_after();
-      float s[128];
-      uint32_t* su = reinterpret_cast<uint32_t*>(s);
-#pragma unroll
-      for (int c = 0; c < 4; ++c) tmem_ld32_issue(tS + 32 * c, su + 32 * c);
-#pragma unroll
-      for (int c = 0; c < 4; ++c) tmem_wait32(su + 32 * c);
-      const int j0 = j * BR;
-      // a block that all rows of the tile see whole has no test a key
-      const bool whole = j0 + BR - 1 <= q0[t] && (q0[t] + BR - 1 - j0 < a.W || j0 + BR <= a.sinks);
-      if (!whole) {
-        const int hi = q < len ? q - j0 : -1, lo = hi - a.W + 1, sk = a.sinks - j0;
-#pragma unroll
-        for (int c = 0; c < 128; ++c)
-          if (!(c <= hi && (c >= lo || c < sk))) s[c] = -INFINITY;
+    uint32_t s_phase = 0, o_phase = 0;
+    bool ok = true;
+    for (int id = blockIdx.x; id < a.items && ok; id += gridDim.x) {
+      // (what a pair is, is kept in shared memory: the scores of a row take most of a thread's registers)
+      {
+        const Item x = item_of(a, id);
+        __syncwarp();
+        if (lane == 0) {
+          info[warp][0] = x.kb.ns;
+          info[warp][1] = x.kb.lo;
+          info[warp][2] = t ? x.kb.tlo[1] : x.kb.tlo[0];
+          info[warp][3] = t ? x.kb.thi[1] : x.kb.thi[0];
+          info[warp][4] = x.len;
+          info[warp][5] = t ? x.q0[1] : x.q0[0];
+          info[warp][6] = x.b;
+          info[warp][7] = t ? x.head[1] : x.head[0];
+        }
+        __syncwarp();
       }
-      float bm[4] = {s[0], s[1], s[2], s[3]};
+      const volatile int* I = info[warp];
+      float m = -INFINITY, l = 0.f;  // m: the scale in use (powers of two); l: this row's sum under it
+      bool first = true;
+      for (int i = 0;; ++i) {
+        int j = i;
+        if (i >= I[0]) j = i - I[0] + I[1];
+        if (j > I[3]) break;  // (the other tile may have a block more)
+        if (j < I[2] && j >= I[0]) continue;
+        ok = mbar_wait_warp(&s_full[t], s_phase, &abort_sh, a.err);
+        if (!ok) break;
+        s_phase ^= 1u;
+        tc_fence_after();
+        const int j0 = j * BR, q0 = I[5];
+        // a block that all rows of the tile see whole has no test a key; else a bit a key
+        const bool whole = j0 + BR - 1 <= q0 && (q0 + BR - 1 - j0 < a.W || j0 + BR <= a.sinks);
+        uint32_t live[4] = {~0u, ~0u, ~0u, ~0u};
+        if (!whole) {
+          const int q = q0 + row, hi = q < I[4] ? q - j0 + 1 : 0, lo = q - a.W + 1 - j0, sk = a.sinks - j0;
 #pragma unroll
-      for (int c = 4; c < 128; c += 4)
+          for (int c = 0; c < 4; ++c) live[c] = below(hi - 32 * c) & (~below(lo - 32 * c) | below(sk - 32 * c));
+        }
+        // the scores are read twice, 32 at a time, for the maximum and for the exponentials: held in registers all along they
+        // leave too few for the rest
+        float s[2][32];
+        float bm[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        tmem_ld32_issue(tS, reinterpret_cast<uint32_t*>(s[0]));
 #pragma unroll
-        for (int u = 0; u < 4; ++u) bm[u] = fmaxf(bm[u], s[c + u]);
-      const float top = fmaxf(fmaxf(bm[0], bm[1]), fmaxf(bm[2], bm[3])) * a.sl2;  // (scale is positive)
-      const bool grew = top > m + RESCALE;  // (-inf: nothing seen before)
-      if (__any_sync(0xffffffffu, grew)) {
-        const float mn = fmaxf(m, top), ms = mn == -INFINITY ? 0.f : mn, f = ex2_fast(m - ms);
-        l *= f;
-        m = mn;
-        if (!first) {
-          float o[32];
-          uint32_t* ou = reinterpret_cast<uint32_t*>(o);
-#pragma unroll 1
-          for (int c = 0; c < DH; c += 32) {
-            tmem_ld32(tO + c, o);
+        for (int c = 0; c < 4; ++c) {
+          float* x = s[c & 1];
+          tmem_wait32(reinterpret_cast<uint32_t*>(x));
+          if (c < 3) tmem_ld32_issue(tS + 32 * (c + 1), reinterpret_cast<uint32_t*>(s[(c + 1) & 1]));
+          if (whole) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] *= f;
-            tmem_st16(tO + c, ou);
-            tmem_st16(tO + c + 16, ou + 16);
+            for (int e = 0; e < 32; ++e) bm[e & 3] = fmaxf(bm[e & 3], x[e]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) bm[e & 3] = fmaxf(bm[e & 3], (live[c] >> e) & 1u ? x[e] : -INFINITY);
           }
         }
-      }
-      first = false;
-      const float ms = m == -INFINITY ? 0.f : m;
-      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        const float top = fmaxf(fmaxf(bm[0], bm[1]), fmaxf(bm[2], bm[3])) * a.sl2;  // (scale is positive)
+        const bool grew = top > m + RESCALE;  // (-inf: nothing seen before)
+        if (__any_sync(0xffffffffu, grew)) {
+          const float mn = fmaxf(m, top), ms = mn == -INFINITY ? 0.f : mn, f = ex2_fast(m - ms);
+          l *= f;
+          m = mn;
+          if (!first) {
+            float o[32];
+            uint32_t* ou = reinterpret_cast<uint32_t*>(o);
+#pragma unroll 1
+            for (int c = 0; c < DH; c += 32) {
+              tmem_ld32(tO + c, o);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        uint32_t w[16];
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float p0 = ex2_fast(fmaf(s[32 * c + 2 * e], a.sl2, -ms)), p1 = ex2_fast(fmaf(s[32 * c + 2 * e + 1], a.sl2, -ms));
-          sum[(2 * e) & 3] += p0;
-          sum[(2 * e + 1) & 3] += p1;
-          w[e] = pk2(p0, p1);
+              for (int e = 0; e < 32; ++e) o[e] *= f;
+              tmem_st16(tO + c, ou);
+              tmem_st16(tO + c + 16, ou + 16);
+            }
+          }
         }
-        tmem_st16(tS + 16 * c, w);
+        first = false;
+        const float ms = m == -INFINITY ? 0.f : m;
+        float2 sum[2] = {f2(0.f), f2(0.f)};
+        tmem_ld32_issue(tS, reinterpret_cast<uint32_t*>(s[0]));
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          float* x = s[c & 1];
+          tmem_wait32(reinterpret_cast<uint32_t*>(x));
+          if (c < 3) tmem_ld32_issue(tS + 32 * (c + 1), reinterpret_cast<uint32_t*>(s[(c + 1) & 1]));
+          if (!whole) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) x[e] = (live[c] >> e) & 1u ? x[e] : -INFINITY;
+          }
+          uint32_t w[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float2 z = __ffma2_rn(make_float2(x[2 * e], x[2 * e + 1]), f2(a.sl2), f2(-ms));
+            const float2 p = make_float2(ex2_fast(z.x), ex2_fast(z.y));
+            sum[e & 1] = __fadd2_rn(sum[e & 1], p);
+            w[e] = pk2(p.x, p.y);
+          }
+          tmem_st16(tS + 16 * c, w);  // over scores that have been read
+        }
+        l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&p_full[t]);
       }
-      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-      tmem_st_wait();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&p_full[t]);
-    }
-    // ---- outputs: staged over this tile's queries (whose last product is done), stored by TMA, which leaves out rows past seq
-    const bool any = kb.thi[t] >= 0;
-    if (ok && kb.n > 0) {
-      // (a tile without a key still has its queries on their way to where zeros go now)
-      ok = mbar_wait_warp(any ? &o_full[t] : &q_full, 0, &abort_sh, a.err);
-      tc_fence_after();
-    }
-    if (ok && q0[t] < a.seq) {
-      const float f = q < len && m != -INFINITY ? 1.f / l : 0.f;
-      uint8_t* stage = smem + Pl::Q + t * BLK;
+      // ---- outputs
+      const bool any = I[3] >= 0;
+      if (ok && any) {
+        ok = mbar_wait_warp(&o_full[t], o_phase, &abort_sh, a.err);
+        o_phase ^= 1u;
+        tc_fence_after();
+      }
+      if (!ok) break;
+      const int len = I[4], q = I[5] + row, head = I[7], b = I[6];
+      const bool seen = q < len && m != -INFINITY;
+      const float f = seen ? 1.f / l : 0.f;
+      bf16* out = a.out + ((int64_t)b * a.seq + (q < a.seq ? q : 0)) * a.out_stride + head * DH;
 #pragma unroll 1
       for (int c = 0; c < DH; c += 32) {
         float o[32];
         if (any) tmem_ld32(tO + c, o);
+        if (any && c + 32 == DH) {  // the accumulator is free for the next pair's products
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&o_read[t]);
+        }
+        if (q < a.seq) {
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          uint32_t w[4];
+          for (int g = 0; g < 4; ++g) {
+            uint32_t w[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) w[e] = q < len ? pk2(o[8 * g + 2 * e] * f, o[8 * g + 2 * e + 1] * f) : 0u;
-          *reinterpret_cast<uint4*>(stage + (c >> 6) * (BR * 128) + swz(row, ((c & 63) >> 3) + g)) = make_uint4(w[0], w[1], w[2], w[3]);
+            for (int e = 0; e < 4; ++e) w[e] = q < len ? pk2(o[8 * g + 2 * e] * f, o[8 * g + 2 * e + 1] * f) : 0u;
+            *reinterpret_cast<uint4*>(out + c + 8 * g) = make_uint4(w[0], w[1], w[2], w[3]);
+          }
         }
       }
-      if (a.lse && q < a.seq)
-        a.lse[((int64_t)b * a.n_heads + head[t]) * a.seq + q] = q < len && m != -INFINITY ? (m + log2f(l)) * kLn2 : -INFINITY;
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&staged[t]);
-      if (row == 0 && mbar_wait(&staged[t], 0, &abort_sh, a.err)) {
-#pragma unroll
-        for (int n = 0; n < DH / 64; ++n) tma_store3(&tmO, smem_u32(stage) + n * (BR * 128), head[t] * DH + 64 * n, q0[t], b);
-        tma_store_done();
-      }
+      if (a.lse && q < a.seq) a.lse[((int64_t)b * a.n_heads + head) * a.seq + q] = seen ? (m + log2f(l)) * kLn2 : -INFINITY;
     }
   }
   tc_fence_before();
@@ -367,16 +440,21 @@ cudaError_t launch(const ra_attention_window_args& p, cudaStream_t st) {
   const int n_blk = (p.seq + BR - 1) / BR;
   a.n_work = a.pair_heads ? n_blk : (n_blk + 1) / 2;
   a.sl2 = p.scale * kLog2e;
-  const int64_t grid = (int64_t)a.n_work * p.batch * (a.pair_heads ? p.n_heads / 2 : p.n_heads);
-  if (grid > INT32_MAX) return cudaErrorNotSupported;
-  CUtensorMap q, k, v, o;
+  const int64_t units = (int64_t)p.batch * (a.pair_heads ? p.n_heads / 2 : p.n_heads), items = units * a.n_work;
+  if (items > INT32_MAX - 1024) return cudaErrorNotSupported;
+  a.units = (int)units;
+  a.items = (int)items;
+  a.out = (bf16*)p.out_dev;
+  a.out_stride = p.out_stride;
+  CUtensorMap q, k, v;
   if (!tma_map_bf16_batch(&q, p.q_dev, p.batch, p.seq, (int64_t)p.n_heads * DH, p.q_stride, 64, BR) ||
       !tma_map_bf16_batch(&k, p.k_dev, p.batch, p.seq, (int64_t)p.n_kv_heads * DH, p.k_stride, 64, BR) ||
-      !tma_map_bf16_batch(&v, p.v_dev, p.batch, p.seq, (int64_t)p.n_kv_heads * DH, p.v_stride, 64, BR) ||
-      !tma_map_bf16_batch(&o, p.out_dev, p.batch, p.seq, (int64_t)p.n_heads * DH, p.out_stride, 64, BR))
+      !tma_map_bf16_batch(&v, p.v_dev, p.batch, p.seq, (int64_t)p.n_kv_heads * DH, p.v_stride, 64, BR))
     return cudaErrorNotSupported;
+  const int sms = device_sm_count();
   cudaError_t e = allow_smem(window_fwd_tc_kernel<DH>, FwdPlan<DH>::BYTES);
-  if (e == cudaSuccess) e = launch_pdl(window_fwd_tc_kernel<DH>, dim3((unsigned)grid), dim3(THREADS), (size_t)FwdPlan<DH>::BYTES, st, q, k, v, o, a);
+  if (e == cudaSuccess)
+    e = launch_pdl(window_fwd_tc_kernel<DH>, dim3(a.items < sms ? a.items : sms), dim3(THREADS), (size_t)FwdPlan<DH>::BYTES, st, q, k, v, a);
   note_launch(1);
   return e;
 }
