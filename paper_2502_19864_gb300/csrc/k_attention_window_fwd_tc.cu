@@ -50,12 +50,19 @@ struct FwdPlan {
   static constexpr uint32_t C_S = 0, C_O = 256;  // scores of tile t at 128 t; outputs at 256 + DH t
 };
 
+// the columns of a key block that products and softmax go through, where its sinks alone are seen: in sixteens
+__device__ __forceinline__ int sink_columns(bool alone, int j, int sinks) {
+  const int n = sinks - j * BR;
+  return alone && n < BR ? (n + 15) & ~15 : BR;
+}
 // The key blocks of a CTA: those with sinks, [0, ns), then [lo, hi], ns <= lo; and each tile's part of them
 struct Blocks {
   int ns, lo, hi, n;
   int tlo[2], thi[2];
   __device__ __forceinline__ int at(int i) const { return i < ns ? i : i - ns + lo; }
   __device__ __forceinline__ bool active(int t, int j) const { return j <= thi[t] && (j >= tlo[t] || j < ns); }
+  // the keys of block j that a row of tile t can see, from its first one, in sixteens: all, or its sinks alone
+  __device__ __forceinline__ int columns(int t, int j, int sinks) const { return sink_columns(j < tlo[t], j, sinks); }
 };
 
 // bits 0 .. n - 1
@@ -191,7 +198,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_fwd_tc_kernel(const __grid_
     __syncwarp();
   } else if (warp == 8) {
     // ------------------------------------------------------------ products
-    constexpr uint32_t IDS = idesc_bf16(BR, BR), IDO = idesc_bf16_bmn(BR, DH);
+    constexpr uint32_t IDS = idesc_bf16(BR, 0), IDO = idesc_bf16_bmn(BR, DH);  // (the scores' columns come with the block)
     bool ok = true;
     uint32_t p_phase[2] = {0, 0};
     int nq = 0, no[2] = {0, 0}, ring = 0;  // pairs of tiles; tiles with outputs; blocks of the ring before this pair's
@@ -228,11 +235,13 @@ __global__ void __launch_bounds__(THREADS, 1) window_fwd_tc_kernel(const __grid_
             p_phase[t] ^= 1u;
             tc_fence_after();
             if (elect_one()) {
-              const uint32_t v = sb + Pl::RING + vs * BLK;
+              // (descriptors by adding to one: the address is their lowest field)
+              const uint64_t v = sdesc_mn_sw128_lbo(sb + Pl::RING + vs * BLK, BR * 128);
+              const int n = kb.columns(t, prev, a.sinks);
 #pragma unroll
               for (int kk = 0; kk < BR / 16; ++kk)
-                umma_bf16_ts(tmem + Pl::C_O + t * DH, tmem + Pl::C_S + t * BR + kk * 8, sdesc_mn_sw128_lbo(v + kk * 2048, BR * 128), IDO,
-                             started[t] || kk > 0 ? 1u : 0u);
+                if (16 * kk < n)
+                  umma_bf16_ts(tmem + Pl::C_O + t * DH, tmem + Pl::C_S + t * BR + kk * 8, v + kk * (2048 >> 4), IDO, started[t] || kk > 0 ? 1u : 0u);
               if (prev == kb.thi[t]) umma_commit(&o_full[t]);
             }
             __syncwarp();
@@ -241,11 +250,12 @@ __global__ void __launch_bounds__(THREADS, 1) window_fwd_tc_kernel(const __grid_
           }
           if (i < kb.n && kb.active(t, j)) {
             if (elect_one()) {
-              const uint32_t q = sb + Pl::Q + t * BLK, k = sb + Pl::RING + ks * BLK;
+              const uint64_t q = sdesc_sw128(sb + Pl::Q + t * BLK), k = sdesc_sw128(sb + Pl::RING + ks * BLK);
+              const uint32_t ids = IDS | ((uint32_t)(kb.columns(t, j, a.sinks) >> 3) << 17);
 #pragma unroll
               for (int kk = 0; kk < DH / 16; ++kk) {
-                const uint32_t o = (kk >> 2) * (BR * 128) + (kk & 3) * 32;
-                umma_bf16(tmem + Pl::C_S + t * BR, sdesc_sw128(q + o), sdesc_sw128(k + o), IDS, kk > 0 ? 1u : 0u);
+                const uint32_t o = ((kk >> 2) * (BR * 128) + (kk & 3) * 32) >> 4;
+                umma_bf16(tmem + Pl::C_S + t * BR, q + o, k + o, ids, kk > 0 ? 1u : 0u);
               }
               umma_commit(&s_full[t]);
             }
@@ -310,29 +320,39 @@ __global__ void __launch_bounds__(THREADS, 1) window_fwd_tc_kernel(const __grid_
         const int j0 = j * BR, q0 = I[5];
         // a block that all rows of the tile see whole has no test a key; else a bit a key
         const bool whole = j0 + BR - 1 <= q0 && (q0 + BR - 1 - j0 < a.W || j0 + BR <= a.sinks);
+        const int chunks = (sink_columns(j < I[2], j, a.sinks) + 31) >> 5;  // of 32 columns
         uint32_t live[4] = {~0u, ~0u, ~0u, ~0u};
+        uint32_t some = 0xfu;  // chunks that a row of this warp sees something of
         if (!whole) {
           const int q = q0 + row, hi = q < I[4] ? q - j0 + 1 : 0, lo = q - a.W + 1 - j0, sk = a.sinks - j0;
 #pragma unroll
-          for (int c = 0; c < 4; ++c) live[c] = below(hi - 32 * c) & (~below(lo - 32 * c) | below(sk - 32 * c));
+          for (int c = 0; c < 4; ++c) {
+            live[c] = below(hi - 32 * c) & (~below(lo - 32 * c) | below(sk - 32 * c));
+            if (!__any_sync(0xffffffffu, live[c] != 0)) some &= ~(1u << c);
+          }
         }
         // the scores are read twice, 32 at a time, for the maximum and for the exponentials: held in registers all along they
         // leave too few for the rest
         float s[2][32];
         float bm[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        tmem_ld32_issue(tS, reinterpret_cast<uint32_t*>(s[0]));
+        if (whole) {
+          tmem_ld32_issue(tS, reinterpret_cast<uint32_t*>(s[0]));
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          float* x = s[c & 1];
-          tmem_wait32(reinterpret_cast<uint32_t*>(x));
-          if (c < 3) tmem_ld32_issue(tS + 32 * (c + 1), reinterpret_cast<uint32_t*>(s[(c + 1) & 1]));
-          if (whole) {
+          for (int c = 0; c < 4; ++c) {
+            float* x = s[c & 1];
+            tmem_wait32(reinterpret_cast<uint32_t*>(x));
+            if (c < 3) tmem_ld32_issue(tS + 32 * (c + 1), reinterpret_cast<uint32_t*>(s[(c + 1) & 1]));
 #pragma unroll
             for (int e = 0; e < 32; ++e) bm[e & 3] = fmaxf(bm[e & 3], x[e]);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 32; ++e) bm[e & 3] = fmaxf(bm[e & 3], (live[c] >> e) & 1u ? x[e] : -INFINITY);
           }
+        } else {
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            if ((some >> c) & 1u) {
+              tmem_ld32(tS + 32 * c, s[0]);
+#pragma unroll
+              for (int e = 0; e < 32; ++e) bm[e & 3] = fmaxf(bm[e & 3], (live[c] >> e) & 1u ? s[0][e] : -INFINITY);
+            }
         }
         const float top = fmaxf(fmaxf(bm[0], bm[1]), fmaxf(bm[2], bm[3])) * a.sl2;  // (scale is positive)
         const bool grew = top > m + RESCALE;  // (-inf: nothing seen before)
@@ -356,16 +376,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_fwd_tc_kernel(const __grid_
         first = false;
         const float ms = m == -INFINITY ? 0.f : m;
         float2 sum[2] = {f2(0.f), f2(0.f)};
-        tmem_ld32_issue(tS, reinterpret_cast<uint32_t*>(s[0]));
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          float* x = s[c & 1];
-          tmem_wait32(reinterpret_cast<uint32_t*>(x));
-          if (c < 3) tmem_ld32_issue(tS + 32 * (c + 1), reinterpret_cast<uint32_t*>(s[(c + 1) & 1]));
-          if (!whole) {
-#pragma unroll
-            for (int e = 0; e < 32; ++e) x[e] = (live[c] >> e) & 1u ? x[e] : -INFINITY;
-          }
+        auto exponentials = [&](int c, const float* x) {
           uint32_t w[16];
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
@@ -375,6 +386,30 @@ __global__ void __launch_bounds__(THREADS, 1) window_fwd_tc_kernel(const __grid_
             w[e] = pk2(p.x, p.y);
           }
           tmem_st16(tS + 16 * c, w);  // over scores that have been read
+        };
+        if (whole) {
+          tmem_ld32_issue(tS, reinterpret_cast<uint32_t*>(s[0]));
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            float* x = s[c & 1];
+            tmem_wait32(reinterpret_cast<uint32_t*>(x));
+            if (c < 3) tmem_ld32_issue(tS + 32 * (c + 1), reinterpret_cast<uint32_t*>(s[(c + 1) & 1]));
+            exponentials(c, x);
+          }
+        } else {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            if (c >= chunks) break;
+            if ((some >> c) & 1u) {
+              tmem_ld32(tS + 32 * c, s[0]);
+#pragma unroll
+              for (int e = 0; e < 32; ++e) s[0][e] = (live[c] >> e) & 1u ? s[0][e] : -INFINITY;
+              exponentials(c, s[0]);
+            } else {
+              const uint32_t none[16] = {};
+              tmem_st16(tS + 16 * c, none);
+            }
+          }
         }
         l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
         tmem_st_wait();
