@@ -4,14 +4,18 @@
 // One pass over the keys with a running maximum m and sum l per row:
 //   S = q K_j^T;  p = 2^(S scale log2 e - m);  O += p V_j;  l += sum p;   at the end o = O / l, lse = m + log l.
 // A CTA takes two tiles of 128 queries that walk the same key blocks of 128: the same rows of two heads that share their
-// keys, or (heads of their own) two consecutive row blocks of one head.  Ten warps:
-//   warps 0-3 and 4-7   the softmax of tile 0 and 1, a thread a row: its 128 scores come from TMEM in one load, its p go back
-//                       to TMEM as bf16 over the scores, where the next product reads them as its A operand;
-//   warp 8              issues the products: O0 += P0 V, S0 = Q0 K', O1 += P1 V, S1 = Q1 K', ...: while one tile's softmax
-//                       runs the tensor cores have the other's products;
-//   warp 9              loads Q, then K and V blocks by TMA into a ring.
+// keys, or (heads of their own) two consecutive row blocks of one head.  Eleven warps:
+//   warps 0-3 and 4-7   the softmax of tile 0 and 1, a thread a row: its scores come from TMEM 32 at a time, its p go back to
+//                       TMEM as bf16 over the scores, where the next product reads them as its A operand;
+//   warps 8 and 9       issue the products of tile 0 and 1, in turns: O0 += P0 V, S0 = Q0 K', O1 += P1 V, S1 = Q1 K', ...:
+//                       while one tile's softmax runs the tensor cores have the other's products;
+//   warp 10             loads Q, then K and V blocks by TMA into a ring.
+// What bounds it is each tile's round of softmax (1900 cycles a block of 128 keys: 500 for the maximum, 1000 for the
+// exponentials, 400 until its p are seen) and products (1230).  One warp for both tiles' products had its waits and
+// commits in that round: 406 us for 16384 tokens of 16 heads over 4, window 4096, against 360 (1338 TFLOP/s).  Two warps without
+// turns interleave their products, so that each tile waits for both: 488 us.
 // The CTAs are persistent: the copies and first products of a CTA's next pair of tiles run while the last outputs of this one
-// leave (one pair of tiles a CTA: 60 us for 8 x 1024 tokens of 16 heads and window 256, this: @T@ us; a pair takes as
+// leave (one pair of tiles a CTA: 60 us for 8 x 1024 tokens of 16 heads and window 256, this: 50 us; a pair takes as
 // little as three blocks, and its start and end as long).
 // O stays in TMEM.  It is rescaled only when a row's maximum has grown by more than 2^8 since the scale in use (p then stays
 // below 2^8 and sums in fp32 lose nothing): the first block sets the scale and almost none after it changes it.
@@ -27,7 +31,7 @@ namespace {
 using namespace tc;
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
-constexpr int BR = 128, THREADS = 320;
+constexpr int BR = 128, THREADS = 352;
 constexpr float RESCALE = 8.f;  // powers of two
 
 struct WindowFwdArgs {
@@ -60,9 +64,6 @@ struct Blocks {
   int ns, lo, hi, n;
   int tlo[2], thi[2];
   __device__ __forceinline__ int at(int i) const { return i < ns ? i : i - ns + lo; }
-  __device__ __forceinline__ bool active(int t, int j) const { return j <= thi[t] && (j >= tlo[t] || j < ns); }
-  // the keys of block j that a row of tile t can see, from its first one, in sixteens: all, or its sinks alone
-  __device__ __forceinline__ int columns(int t, int j, int sinks) const { return sink_columns(j < tlo[t], j, sinks); }
 };
 
 // bits 0 .. n - 1
@@ -117,7 +118,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_fwd_tc_kernel(const __grid_
   constexpr int SLOTS = Pl::SLOTS, BLK = Pl::BLK;
   extern __shared__ __align__(1024) uint8_t smem[];
   // q_read: the last product with this pair's queries is done; o_full: a tile's outputs are complete; o_read: they have left TMEM
-  __shared__ __align__(8) uint64_t full[SLOTS], empty[SLOTS], q_full, q_read, s_full[2], p_full[2], o_full[2], o_read[2], drain;
+  __shared__ __align__(8) uint64_t full[SLOTS], empty[SLOTS], zeroed[SLOTS], q_full, q_read, s_full[2], p_full[2], o_full[2], o_read[2], turn[2], drain[2];
   __shared__ uint32_t tmem_sh;
   __shared__ volatile int abort_sh;
   __shared__ int info[8][8];
@@ -127,22 +128,24 @@ __global__ void __launch_bounds__(THREADS, 1) window_fwd_tc_kernel(const __grid_
     return;
   }
   const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
-  if (warp == 9) {
+  if (warp == 10) {
     if (elect_one()) {
 #pragma unroll
       for (int i = 0; i < SLOTS; ++i) {
         mbar_init(&full[i], 1);
-        mbar_init(&empty[i], 1);
+        mbar_init(&empty[i], 2);
+        mbar_init(&zeroed[i], 1);
       }
       mbar_init(&q_full, 1);
-      mbar_init(&q_read, 1);
-      mbar_init(&drain, 1);
+      mbar_init(&q_read, 2);
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         mbar_init(&s_full[t], 1);
         mbar_init(&p_full[t], 4);
         mbar_init(&o_full[t], 1);
         mbar_init(&o_read[t], 4);
+        mbar_init(&turn[t], 1);
+        mbar_init(&drain[t], 1);
       }
       abort_sh = 0;
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -161,7 +164,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_fwd_tc_kernel(const __grid_
   tc_fence_after();
   const uint32_t tmem = tmem_sh;
 
-  if (warp == 9) {
+  if (warp == 10) {
     // ------------------------------------------------------------ copies
     if (elect_one()) {
       auto load = [&](const CUtensorMap* tm, uint32_t dst, uint64_t* bar, int col, int row, int b) {
@@ -196,89 +199,110 @@ __global__ void __launch_bounds__(THREADS, 1) window_fwd_tc_kernel(const __grid_
       }
     }
     __syncwarp();
-  } else if (warp == 8) {
-    // ------------------------------------------------------------ products
+  } else if (warp >= 8) {
+    // ------------------------------------------------------------ products, of tile 0 and of tile 1
+    // A block of the ring is free, and the queries are, when both tiles are done with them; a tile that does not see a block
+    // says so as soon as that has landed (not before: its word would count for what the slot held earlier).
     constexpr uint32_t IDS = idesc_bf16(BR, 0), IDO = idesc_bf16_bmn(BR, DH);  // (the scores' columns come with the block)
+    const int t = warp - 8;
+    const uint32_t tS = uniform(tmem + Pl::C_S + t * BR), tO = uniform(tmem + Pl::C_O + t * DH);
+    const uint32_t q = desc_lo_k(sb + Pl::Q + t * BLK);
     bool ok = true;
-    uint32_t p_phase[2] = {0, 0};
-    int nq = 0, no[2] = {0, 0}, ring = 0;  // pairs of tiles; tiles with outputs; blocks of the ring before this pair's
+    uint32_t turns = 0;  // each warp has one a block and one after the last, with or without products
+    uint32_t p_phase = 0, z_phase = 0;  // (z_phase: a bit a slot, which tile 0 zeroes again only when tile 1 has let it go)
+    int nq = 0, no = 0, ring = 0;  // pairs of tiles; tiles with outputs; blocks of the ring before this pair's
     for (int id = blockIdx.x; id < a.items && ok; id += gridDim.x) {
       const Item x = item_of(a, id);
       const Blocks& kb = x.kb;
       if (kb.n == 0) continue;
       ok = mbar_wait_warp(&q_full, nq & 1, &abort_sh, a.err);
       ++nq;
-      bool started[2] = {false, false}, pend[2] = {false, false};
-      int prev = 0;
+      const int thi = t ? kb.thi[1] : kb.thi[0], tlo = t ? kb.tlo[1] : kb.tlo[0];
+      bool started = false, pend = false;
+      int prev = 0, prev_n = 0;
       for (int i = 0; i <= kb.n && ok; ++i) {
-        const int j = i < kb.n ? kb.at(i) : -1;
         const int kn = ring + 2 * i, vn = kn - 1, ks = kn % SLOTS, vs = (vn + SLOTS) % SLOTS;  // this block's keys, the last one's values
         if (i > 0) {
           ok = mbar_wait_warp(&full[vs], (vn / SLOTS) & 1, &abort_sh, a.err);
           if (!ok) break;
           const int dead = x.len - prev * BR;  // rows from here on are past the sequence's end
-          if (dead < BR) zero_rows<DH>(smem + Pl::RING + vs * BLK, dead, lane);
+          if (dead < BR) {
+            if (t == 0) {
+              zero_rows<DH>(smem + Pl::RING + vs * BLK, dead, lane);
+              if (lane == 0) mbar_arrive(&zeroed[vs]);
+            } else {
+              ok = mbar_wait_warp(&zeroed[vs], (z_phase >> vs) & 1u, &abort_sh, a.err);
+              if (!ok) break;
+              z_phase ^= 1u << vs;
+            }
+          }
+          if (pend && !started) {  // the outputs of this tile's last pair have left TMEM
+            if (no > 0) ok = mbar_wait_warp(&o_read[t], (no - 1) & 1, &abort_sh, a.err);
+            ++no;
+            if (!ok) break;
+          }
         }
+        const int j = i < kb.n ? kb.at(i) : 0;
+        bool next = false;
+        int next_n = 0;
         if (i < kb.n) {
           ok = mbar_wait_warp(&full[ks], (kn / SLOTS) & 1, &abort_sh, a.err);
           if (!ok) break;
+          next = j <= thi && (j >= tlo || j < kb.ns);
+          next_n = sink_columns(j < tlo, j, a.sinks);
         }
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          if (pend[t]) {
-            ok = mbar_wait_warp(&p_full[t], p_phase[t], &abort_sh, a.err);
-            if (ok && !started[t]) {  // the outputs of this tile's last pair have left TMEM
-              if (no[t] > 0) ok = mbar_wait_warp(&o_read[t], (no[t] - 1) & 1, &abort_sh, a.err);
-              ++no[t];
-            }
-            if (!ok) break;
-            p_phase[t] ^= 1u;
-            tc_fence_after();
-            if (elect_one()) {
-              // (descriptors by adding to one: the address is their lowest field)
-              const uint64_t v = sdesc_mn_sw128_lbo(sb + Pl::RING + vs * BLK, BR * 128);
-              const int n = kb.columns(t, prev, a.sinks);
-#pragma unroll
-              for (int kk = 0; kk < BR / 16; ++kk)
-                if (16 * kk < n)
-                  umma_bf16_ts(tmem + Pl::C_O + t * DH, tmem + Pl::C_S + t * BR + kk * 8, v + kk * (2048 >> 4), IDO, started[t] || kk > 0 ? 1u : 0u);
-              if (prev == kb.thi[t]) umma_commit(&o_full[t]);
-            }
-            __syncwarp();
-            started[t] = true;
-            pend[t] = false;
-          }
-          if (i < kb.n && kb.active(t, j)) {
-            if (elect_one()) {
-              const uint64_t q = sdesc_sw128(sb + Pl::Q + t * BLK), k = sdesc_sw128(sb + Pl::RING + ks * BLK);
-              const uint32_t ids = IDS | ((uint32_t)(kb.columns(t, j, a.sinks) >> 3) << 17);
-#pragma unroll
-              for (int kk = 0; kk < DH / 16; ++kk) {
-                const uint32_t o = ((kk >> 2) * (BR * 128) + (kk & 3) * 32) >> 4;
-                umma_bf16(tmem + Pl::C_S + t * BR, q + o, k + o, ids, kk > 0 ? 1u : 0u);
-              }
-              umma_commit(&s_full[t]);
-            }
-            __syncwarp();
-            pend[t] = true;
-          }
-        }
+        const uint32_t v = desc_lo_mn(sb + Pl::RING + vs * BLK, BR * 128), acc = uniform(started ? 1u : 0u);
+        const uint32_t k = desc_lo_k(sb + Pl::RING + ks * BLK);
+        const uint32_t ids = uniform(IDS | ((uint32_t)(next_n >> 3) << 17));
+        const int n = (int)uniform(prev_n);
+        if (t == 1 || turns > 0) ok = mbar_wait_warp(&turn[t], (turns - (t == 0)) & 1, &abort_sh, a.err);
         if (!ok) break;
+        ++turns;
+        if (pend) {
+          ok = mbar_wait_warp(&p_full[t], p_phase, &abort_sh, a.err);
+          if (!ok) break;
+          p_phase ^= 1u;
+        }
+        tc_fence_after();
         if (elect_one()) {
-          if (i > 0) umma_commit(&empty[vs]);
-          if (i < kb.n) umma_commit(&empty[ks]);
-          if (i == kb.n - 1) umma_commit(&q_read);
+          if (pend) {
+#pragma unroll
+            for (int kk = 0; kk < BR / 16; ++kk)
+              if (16 * kk < n) umma_bf16_ts(tO, tS + kk * 8, desc_of(v + kk * (2048 >> 4)), IDO, kk > 0 ? 1u : acc);
+          }
+          if (next) {
+#pragma unroll
+            for (int kk = 0; kk < DH / 16; ++kk) {
+              const uint32_t o = ((kk >> 2) * (BR * 128) + (kk & 3) * 32) >> 4;
+              umma_bf16(tS, desc_of(q + o), desc_of(k + o), ids, kk > 0 ? 1u : 0u);
+            }
+            umma_commit(&s_full[t]);
+          }
+          mbar_arrive(&turn[t ^ 1]);
+          if (pend && prev == thi) umma_commit(&o_full[t]);
+          if (i > 0) {
+            if (pend) umma_commit(&empty[vs]);
+            else mbar_arrive(&empty[vs]);
+          }
+          if (i < kb.n) {
+            if (next) umma_commit(&empty[ks]);
+            else mbar_arrive(&empty[ks]);
+            if (i == kb.n - 1) umma_commit(&q_read);
+          }
         }
         __syncwarp();
+        if (pend) started = true;
+        pend = next;
         prev = j;
+        prev_n = next_n;
       }
       ring += 2 * kb.n;
     }
     // what was issued ends before shared memory and TMEM are released
     if (elect_one()) {
       volatile int no_abort = 0;
-      umma_commit(&drain);
-      mbar_wait(&drain, 0, &no_abort, nullptr);
+      umma_commit(&drain[t]);
+      mbar_wait(&drain[t], 0, &no_abort, nullptr);
     }
     __syncwarp();
   } else {

@@ -30,6 +30,13 @@ __device__ __forceinline__ void tma_store_done() {
   asm volatile("cp.async.bulk.commit_group;" ::: "memory");
   asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
 }
+// The low words of the operands' descriptors (address and leading byte offset), in a uniform register, and the whole: what
+// a product's issue costs is the moves of its operands into uniform registers, so that a base goes there once and steps
+// are added to it (the address is the lowest field; 16 bytes count one)
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
+__device__ __forceinline__ uint32_t desc_lo_k(uint32_t saddr) { return uniform(((saddr & 0x3FFFFu) >> 4) | (1u << 16)); }
+__device__ __forceinline__ uint32_t desc_lo_mn(uint32_t saddr, uint32_t lbo) { return uniform(((saddr & 0x3FFFFu) >> 4) | (((lbo >> 4) & 0x3FFFu) << 16)); }
+__device__ __forceinline__ uint64_t desc_of(uint32_t lo) { return ((uint64_t)((1024u >> 4) | (1u << 14) | (2u << 29)) << 32) | lo; }
 // D[tmem] (+)= A[tmem, 128 x 16 bf16] B
 __device__ __forceinline__ void umma_bf16_ts(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
