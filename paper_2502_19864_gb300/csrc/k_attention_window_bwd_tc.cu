@@ -48,23 +48,23 @@ struct BwdPlan {
   static constexpr uint32_t C_S = 0, C_DP = 128, C_A0 = 256, C_A1 = 256 + DH, C_S1 = 384;
 };
 
-// D[128 x 128] = A B^T over DH, both K-major blocks
+// D[128 x 128] = A B^T over DH, both K-major blocks (a, b: the low words of their descriptors)
 template <int DH>
 __device__ __forceinline__ void mma_nt(uint32_t d, uint32_t a, uint32_t b) {
   constexpr uint32_t ID = idesc_bf16(BR, BR);
 #pragma unroll
   for (int kk = 0; kk < DH / 16; ++kk) {
-    const uint32_t o = (kk >> 2) * (BR * 128) + (kk & 3) * 32;
-    umma_bf16(d, sdesc_sw128(a + o), sdesc_sw128(b + o), ID, kk > 0 ? 1u : 0u);
+    const uint32_t o = ((kk >> 2) * (BR * 128) + (kk & 3) * 32) >> 4;
+    umma_bf16(d, desc_of(a + o), desc_of(b + o), ID, kk > 0 ? 1u : 0u);
   }
 }
 // D[128 x DH] (+)= X[128 x 128, bf16 in TMEM: columns 0-63 packed at x, 64-127 at x + 64] B[128 x DH]
 template <int DH>
-__device__ __forceinline__ void mma_tn(uint32_t d, uint32_t x, uint32_t b, bool acc) {
+__device__ __forceinline__ void mma_tn(uint32_t d, uint32_t x, uint32_t b, uint32_t acc) {
   constexpr uint32_t ID = idesc_bf16_bmn(BR, DH);
 #pragma unroll
   for (int kk = 0; kk < BR / 16; ++kk)
-    umma_bf16_ts(d, x + 64 * (kk >> 2) + 8 * (kk & 3), sdesc_mn_sw128_lbo(b + kk * 2048, BR * 128), ID, acc || kk > 0 ? 1u : 0u);
+    umma_bf16_ts(d, x + 64 * (kk >> 2) + 8 * (kk & 3), desc_of(b + kk * (2048 >> 4)), ID, kk > 0 ? 1u : acc);
 }
 
 template <int DH, bool KEYS>
@@ -209,6 +209,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_bwd_tc_kernel(const __grid_
   } else if (warp == 8) {
     // ------------------------------------------------------------ products
     bool ok = n_steps == 0 || mbar_wait_warp(&fixed_full, 0, &abort_sh, a.err);
+    const uint32_t utmem = uniform(tmem), f0 = desc_lo_k(sb + Pl::F0), f1 = desc_lo_k(sb + Pl::F1);
     // S(n), into buffer n & 1 (queries)
     auto scores = [&](int n) {
       const int s = n % NA;
@@ -216,8 +217,9 @@ __global__ void __launch_bounds__(THREADS, 1) window_bwd_tc_kernel(const __grid_
       if (!ok) return;
       const int dead = len - step_blk(n) * BR;
       if (dead < BR) zero_rows<DH>(smem + Pl::A + s * BLK, dead, lane);
+      const uint32_t d = uniform(tmem + (!KEYS && (n & 1) ? Pl::C_S1 : Pl::C_S)), x = desc_lo_k(sb + Pl::A + s * BLK);
       if (elect_one()) {
-        mma_nt<DH>(tmem + (!KEYS && (n & 1) ? Pl::C_S1 : Pl::C_S), sb + Pl::F0, sb + Pl::A + s * BLK);
+        mma_nt<DH>(d, f0, x);
         umma_commit(&s_full[KEYS ? 0 : n & 1]);
       }
       __syncwarp();
@@ -228,8 +230,9 @@ __global__ void __launch_bounds__(THREADS, 1) window_bwd_tc_kernel(const __grid_
       if (!ok) return;
       const int dead = len - step_blk(n) * BR;
       if (KEYS && dead < BR) zero_rows<DH>(smem + Pl::B + s * BLK, dead, lane);
+      const uint32_t x = desc_lo_k(sb + Pl::B + s * BLK);
       if (elect_one()) {
-        mma_nt<DH>(tmem + Pl::C_DP, sb + Pl::F1, sb + Pl::B + s * BLK);
+        mma_nt<DH>(utmem + Pl::C_DP, f1, x);
         umma_commit(&dp_full);
         if (!KEYS) umma_commit(&b_empty[s]);
       }
@@ -245,8 +248,10 @@ __global__ void __launch_bounds__(THREADS, 1) window_bwd_tc_kernel(const __grid_
         ok = mbar_wait_warp(&p_full, n & 1, &abort_sh, a.err);
         if (!ok) break;
         tc_fence_after();
+        const uint32_t acc = uniform(n > 0), g = desc_lo_mn(sb + Pl::B + (n % NB) * BLK, BR * 128);
+        const uint32_t q = desc_lo_mn(sb + Pl::A + (n % NA) * BLK, BR * 128);
         if (elect_one()) {  // dV += P^T dO
-          mma_tn<DH>(tmem + Pl::C_A1, tmem + Pl::C_S, sb + Pl::B + (n % NB) * BLK, n > 0);
+          mma_tn<DH>(utmem + Pl::C_A1, utmem + Pl::C_S, g, acc);
           umma_commit(&b_empty[n % NB]);
         }
         __syncwarp();
@@ -255,7 +260,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_bwd_tc_kernel(const __grid_
         if (!ok) break;
         tc_fence_after();
         if (elect_one()) {  // dK += dS^T Q
-          mma_tn<DH>(tmem + Pl::C_A0, tmem + Pl::C_DP, sb + Pl::A + (n % NA) * BLK, n > 0);
+          mma_tn<DH>(utmem + Pl::C_A0, utmem + Pl::C_DP, q, acc);
           umma_commit(&a_empty[n % NA]);
           if (n + 1 == n_steps) umma_commit(&done);
         }
@@ -267,8 +272,9 @@ __global__ void __launch_bounds__(THREADS, 1) window_bwd_tc_kernel(const __grid_
         tc_fence_after();
         if (n + 1 < n_steps) dprobs(n + 1);
         if (!ok) break;
+        const uint32_t acc = uniform(n > 0), x = uniform(tmem + (n & 1 ? Pl::C_S1 : Pl::C_S)), k = desc_lo_mn(sb + Pl::A + (n % NA) * BLK, BR * 128);
         if (elect_one()) {  // dQ += dS K
-          mma_tn<DH>(tmem + Pl::C_A0, tmem + (n & 1 ? Pl::C_S1 : Pl::C_S), sb + Pl::A + (n % NA) * BLK, n > 0);
+          mma_tn<DH>(utmem + Pl::C_A0, x, k, acc);
           umma_commit(&a_empty[n % NA]);
           if (n + 1 == n_steps) umma_commit(&done);
         }
