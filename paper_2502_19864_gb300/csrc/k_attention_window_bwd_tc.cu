@@ -26,19 +26,20 @@ namespace {
 using namespace tc;
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int BR = 128, THREADS = 320, NA = 3, NB = 2;  // ring slots of the two streams
+constexpr int BR = 128, THREADS = 352, NA = 3, NB = 2;  // ring slots of the two streams
 
 struct WindowBwdArgs {
   const int32_t* lens;
   const float* lse;
-  const bf16* out;
-  int64_t out_stride;
   float* D;        // [batch, n_heads, seq]
   float* part;     // [batch, n_kv_heads, split blocks, chunks][dK | dV][128][DH], in order
   uint32_t* err;
   int batch, seq, n_heads, n_kv_heads, W, sinks, n_blk;
   int split, chunks;  // the first `split` key blocks are shared by `chunks` CTAs each
   float scale, sl2;
+  int items;
+  bf16* grad[2];  // queries: dQ; keys: dK, dV
+  int64_t grad_stride[2];
 };
 
 template <int DH>
@@ -67,49 +68,113 @@ __device__ __forceinline__ void mma_tn(uint32_t d, uint32_t x, uint32_t b, uint3
     umma_bf16_ts(d, x + 64 * (kk >> 2) + 8 * (kk & 3), desc_of(b + kk * (2048 >> 4)), ID, kk > 0 ? 1u : acc);
 }
 
+// A CTA's block and its steps.  keys: (head of the group, query block); queries: key blocks [0, ns), then [lo, blk]
+struct Item {
+  int blk, b, head, chunk, chunks;  // head: keys: key-value head
+  int len, n_steps, s0, per_head, ns, lo;
+};
+// the ones with the most steps first
+template <bool KEYS>
+__device__ __forceinline__ Item item_of(const WindowBwdArgs& a, int id) {
+  Item x;
+  x.chunk = 0;
+  x.chunks = 1;
+  if (KEYS) {
+    const int units = a.batch * a.n_kv_heads, it = id / units, u = id % units;
+    if (it < a.split * a.chunks) {
+      x.blk = it / a.chunks;
+      x.chunk = it - x.blk * a.chunks;
+      x.chunks = a.chunks;
+    } else {
+      x.blk = a.split + it - a.split * a.chunks;
+    }
+    x.b = u / a.n_kv_heads;
+    x.head = u - x.b * a.n_kv_heads;
+  } else {
+    const int units = a.batch * a.n_heads, u = id % units;
+    x.blk = a.n_blk - 1 - id / units;
+    x.b = u / a.n_heads;
+    x.head = u - x.b * a.n_heads;
+  }
+  int len = a.lens ? __ldg(a.lens + x.b) : a.seq;
+  if (len < 0 || len > a.seq) {
+    set_dev_error(a.err, RA_DEVERR_BOUNDS);
+    len = len < 0 ? 0 : a.seq;
+  }
+  x.len = len;
+  x.n_steps = x.s0 = x.ns = x.lo = 0;
+  x.per_head = 1;
+  const int r0 = x.blk * BR, last = r0 + BR - 1 < len ? r0 + BR - 1 : len - 1;  // the last live row
+  if (r0 < len) {
+    if (KEYS) {
+      const int64_t far = r0 < a.sinks ? len - 1 : (int64_t)last + a.W - 1;
+      x.per_head = (int)(far < len ? far : len - 1) / BR - x.blk + 1;
+      const int64_t total = (int64_t)x.per_head * (a.n_heads / a.n_kv_heads);
+      x.s0 = (int)(total * x.chunk / x.chunks);
+      x.n_steps = (int)(total * (x.chunk + 1) / x.chunks) - x.s0;
+    } else {
+      const int first = r0 - a.W + 1, sink_blocks = a.sinks / BR + (a.sinks % BR != 0);
+      x.lo = first > 0 ? first / BR : 0;
+      x.ns = sink_blocks < x.blk + 1 ? sink_blocks : x.blk + 1;
+      if (x.lo < x.ns) x.lo = x.ns;
+      x.n_steps = x.ns + (x.blk >= x.lo ? x.blk - x.lo + 1 : 0);
+    }
+  }
+  return x;
+}
+// A step of an item: the streamed block and its head (stepped from one to the next: a division costs as much as a handshake)
+template <bool KEYS>
+struct Step {
+  int head, blk;
+  __device__ __forceinline__ Step(const WindowBwdArgs& a, const volatile Item& x) {
+    if (KEYS) {
+      const int h = x.s0 / x.per_head;
+      head = x.head * (a.n_heads / a.n_kv_heads) + h;
+      blk = x.blk + x.s0 - h * x.per_head;
+    } else {
+      head = x.head / (a.n_heads / a.n_kv_heads);
+      blk = x.ns > 0 ? 0 : x.lo;
+    }
+  }
+  __device__ __forceinline__ void next(const volatile Item& x) {
+    ++blk;
+    if (KEYS) {
+      if (blk == x.blk + x.per_head) {
+        blk = x.blk;
+        ++head;
+      }
+    } else if (blk == x.ns) {
+      blk = x.lo;
+    }
+  }
+};
+
 template <int DH, bool KEYS>
 __global__ void __launch_bounds__(THREADS, 1) window_bwd_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
     const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmDO,
-    const __grid_constant__ CUtensorMap tmG0, const __grid_constant__ CUtensorMap tmG1, const __grid_constant__ WindowBwdArgs a) {
+    const __grid_constant__ CUtensorMap tmO, const __grid_constant__ WindowBwdArgs a) {
   using Pl = BwdPlan<DH>;
   constexpr int BLK = Pl::BLK;
   extern __shared__ __align__(1024) uint8_t smem[];
-  __shared__ __align__(8) uint64_t fixed_full, a_full[NA], a_empty[NA], b_full[NB], b_empty[NB], s_full[2], dp_full, p_full, ds_full, stat_full, staged, done, drain;
+  // f_free: the held blocks were read for the last time; zeroed: (keys) rows past the end in a dO slot; done: an item's gradients
+  // are complete; o_read: they have left TMEM
+  __shared__ __align__(8) uint64_t fixed_full, f_free, a_full[NA], a_empty[NA], b_full[NB], b_empty[NB], zeroed[NB];
+  __shared__ __align__(8) uint64_t s_full[2], dp_full, p_full, ds_full[2], stat_full, done, o_read, drain[2];
   __shared__ uint32_t tmem_sh;
+  __shared__ Item info[8][2];
   __shared__ volatile int abort_sh;
-  __shared__ __align__(16) float stat[2][2][BR];  // keys: log-sum-exps and D of the query block, two steps; queries: [0][0]: D's halves
+  __shared__ __align__(16) float stat[2][2][BR];  // keys: log-sum-exps and D of the query block, two steps; queries: D's halves, two items
   const uint32_t sb = smem_u32(smem);
   if (sb & 1023u) {  // the swizzled operand tiles need 1024-byte alignment
     if (threadIdx.x == 0) set_dev_error(a.err, RA_DEVERR_BOUNDS);
     return;
   }
   const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
-  const int G = a.n_heads / a.n_kv_heads;
 
-  // ---- this CTA's block: the ones with the most steps first
-  int blk, b, head, chunk = 0, chunks = 1;  // head: keys: key-value head
-  if (KEYS) {
-    const int units = a.batch * a.n_kv_heads, it = (int)(blockIdx.x / units), u = (int)(blockIdx.x % units);
-    if (it < a.split * a.chunks) {
-      blk = it / a.chunks;
-      chunk = it - blk * a.chunks;
-      chunks = a.chunks;
-    } else {
-      blk = a.split + it - a.split * a.chunks;
-    }
-    b = u / a.n_kv_heads;
-    head = u - b * a.n_kv_heads;
-  } else {
-    const int units = a.batch * a.n_heads, u = (int)(blockIdx.x % units);
-    blk = a.n_blk - 1 - (int)(blockIdx.x / units);
-    b = u / a.n_heads;
-    head = u - b * a.n_heads;
-  }
-  const int kvh = KEYS ? head : head / G, r0 = blk * BR;
-
-  if (warp == 9) {
+  if (warp == 10) {
     if (elect_one()) {
       mbar_init(&fixed_full, 1);
+      mbar_init(&f_free, KEYS ? 2 : 10);
 #pragma unroll
       for (int i = 0; i < NA; ++i) {
         mbar_init(&a_full[i], 1);
@@ -118,17 +183,20 @@ __global__ void __launch_bounds__(THREADS, 1) window_bwd_tc_kernel(const __grid_
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
         mbar_init(&b_full[i], 1);
-        mbar_init(&b_empty[i], 1);
+        mbar_init(&b_empty[i], KEYS ? 2 : 1);
+        mbar_init(&zeroed[i], 1);
       }
-      mbar_init(&s_full[0], 1);
-      mbar_init(&s_full[1], 1);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        mbar_init(&s_full[i], 1);
+        mbar_init(&ds_full[i], 8);
+        mbar_init(&drain[i], 1);
+      }
       mbar_init(&dp_full, 1);
       mbar_init(&p_full, 8);
-      mbar_init(&ds_full, 8);
       mbar_init(&stat_full, 8);
-      mbar_init(&staged, 8);
-      mbar_init(&done, 1);
-      mbar_init(&drain, 1);
+      mbar_init(&done, KEYS ? 2 : 1);
+      mbar_init(&o_read, 8);
       abort_sh = 0;
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -141,334 +209,427 @@ __global__ void __launch_bounds__(THREADS, 1) window_bwd_tc_kernel(const __grid_
   }
   pdl_wait();
   pdl_trigger();
-  int len = a.lens ? a.lens[b] : a.seq;
-  if (len < 0 || len > a.seq) {
-    if (tid == 0) set_dev_error(a.err, RA_DEVERR_BOUNDS);
-    len = len < 0 ? 0 : a.seq;
-  }
-  // ---- the steps: keys: (head of the group, query block); queries: key blocks [0, ns), then [lo, hi]
-  int n_steps = 0, s0 = 0, per_head = 1, ns = 0, lo = 0;
-  const int last = r0 + BR - 1 < len ? r0 + BR - 1 : len - 1;  // the last live row
-  if (r0 < len) {
-    if (KEYS) {
-      const int64_t far = r0 < a.sinks ? len - 1 : (int64_t)last + a.W - 1;
-      per_head = (int)(far < len ? far : len - 1) / BR - blk + 1;
-      const int64_t total = (int64_t)per_head * G;
-      s0 = (int)(total * chunk / chunks);
-      n_steps = (int)(total * (chunk + 1) / chunks) - s0;
-    } else {
-      const int first = r0 - a.W + 1, sink_blocks = a.sinks / BR + (a.sinks % BR != 0);
-      lo = first > 0 ? first / BR : 0;
-      ns = sink_blocks < blk + 1 ? sink_blocks : blk + 1;
-      if (lo < ns) lo = ns;
-      n_steps = ns + (blk >= lo ? blk - lo + 1 : 0);
-    }
-  }
-  // the streamed block of step n, and (keys) its head
-  auto step_head = [&](int n) { return KEYS ? kvh * G + (s0 + n) / per_head : kvh; };
-  auto step_blk = [&](int n) { return KEYS ? blk + (s0 + n) % per_head : n < ns ? n : n - ns + lo; };
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_sh;
+  // Every role counts its steps over all items (g): ring slots, buffers and the barriers' phases go by that.
 
-  if (warp == 9) {
+  if (warp == 10) {
     // ------------------------------------------------------------ copies
-    if (n_steps > 0 && elect_one()) {
-      auto load = [&](const CUtensorMap* tm, uint32_t dst, uint64_t* bar, int h, int row) {
-#pragma unroll
-        for (int n = 0; n < DH / 64; ++n) tma_load3(tm, dst + n * (BR * 128), bar, h * DH + 64 * n, row, b);
-      };
-      mbar_expect_tx(&fixed_full, 2 * BLK);
-      load(KEYS ? &tmK : &tmQ, sb + Pl::F0, &fixed_full, head, r0);
-      load(KEYS ? &tmV : &tmDO, sb + Pl::F1, &fixed_full, head, r0);
+    if (elect_one()) {
       bool ok = true;
-      int na = 0, nb = 0;
-      for (int n = 0; n < n_steps && ok; ++n) {
-        const int sa = n % NA, sl = n % NB, h = step_head(n), row = step_blk(n) * BR;
-        if (n >= NA) ok = mbar_wait(&a_empty[sa], ((n / NA) - 1) & 1, &abort_sh, a.err);
+      int na = 0, nb = 0, ni = 0;  // blocks of the two rings and items that were started
+      for (int id = blockIdx.x; id < a.items && ok; id += gridDim.x) {
+        const Item x = item_of<KEYS>(a, id);
+        if (x.n_steps == 0) continue;
+        auto load = [&](const CUtensorMap* tm, uint32_t dst, uint64_t* bar, int h, int row) {
+#pragma unroll
+          for (int n = 0; n < DH / 64; ++n) tma_load3(tm, dst + n * (BR * 128), bar, h * DH + 64 * n, row, x.b);
+        };
+        if (ni > 0) ok = mbar_wait(&f_free, (ni - 1) & 1, &abort_sh, a.err);
         if (!ok) break;
-        mbar_expect_tx(&a_full[sa], BLK);
-        load(KEYS ? &tmQ : &tmK, sb + Pl::A + sa * BLK, &a_full[sa], h, row);
-        na = n + 1;
-        if (n >= NB) ok = mbar_wait(&b_empty[sl], ((n / NB) - 1) & 1, &abort_sh, a.err);
-        if (!ok) break;
-        mbar_expect_tx(&b_full[sl], BLK);
-        load(KEYS ? &tmDO : &tmV, sb + Pl::B + sl * BLK, &b_full[sl], h, row);
-        nb = n + 1;
+        mbar_expect_tx(&fixed_full, 2 * BLK);
+        load(KEYS ? &tmK : &tmQ, sb + Pl::F0, &fixed_full, x.head, x.blk * BR);
+        load(KEYS ? &tmV : &tmDO, sb + Pl::F1, &fixed_full, x.head, x.blk * BR);
+        ++ni;
+        if (!KEYS) {  // o, for D, in a slot of the keys' ring
+          const int s = na % NA;
+          if (na >= NA) ok = mbar_wait(&a_empty[s], ((na / NA) - 1) & 1, &abort_sh, a.err);
+          if (!ok) break;
+          mbar_expect_tx(&a_full[s], BLK);
+          load(&tmO, sb + Pl::A + s * BLK, &a_full[s], x.head, x.blk * BR);
+          ++na;
+        }
+        Step<KEYS> at(a, x);
+        for (int n = 0; n < x.n_steps; ++n, at.next(x)) {
+          const int sa = na % NA, sl = nb % NB, h = at.head, row = at.blk * BR;
+          if (na >= NA) ok = mbar_wait(&a_empty[sa], ((na / NA) - 1) & 1, &abort_sh, a.err);
+          if (!ok) break;
+          mbar_expect_tx(&a_full[sa], BLK);
+          load(KEYS ? &tmQ : &tmK, sb + Pl::A + sa * BLK, &a_full[sa], h, row);
+          ++na;
+          if (nb >= NB) ok = mbar_wait(&b_empty[sl], ((nb / NB) - 1) & 1, &abort_sh, a.err);
+          if (!ok) break;
+          mbar_expect_tx(&b_full[sl], BLK);
+          load(KEYS ? &tmDO : &tmV, sb + Pl::B + sl * BLK, &b_full[sl], h, row);
+          ++nb;
+        }
       }
       if (!ok) {
         // a wait gave up: let the copies on their way land before shared memory is released
         volatile int no_abort = 0;
-        mbar_wait(&fixed_full, 0, &no_abort, nullptr);
+        if (ni > 0) mbar_wait(&fixed_full, (ni - 1) & 1, &no_abort, nullptr);
         for (int n = na > NA ? na - NA : 0; n < na; ++n) mbar_wait(&a_full[n % NA], (n / NA) & 1, &no_abort, nullptr);
         for (int n = nb > NB ? nb - NB : 0; n < nb; ++n) mbar_wait(&b_full[n % NB], (n / NB) & 1, &no_abort, nullptr);
       }
     }
     __syncwarp();
   } else if (warp == 8) {
-    // ------------------------------------------------------------ products
-    bool ok = n_steps == 0 || mbar_wait_warp(&fixed_full, 0, &abort_sh, a.err);
-    const uint32_t utmem = uniform(tmem), f0 = desc_lo_k(sb + Pl::F0), f1 = desc_lo_k(sb + Pl::F1);
-    // S(n), into buffer n & 1 (queries)
-    auto scores = [&](int n) {
-      const int s = n % NA;
-      ok = ok && mbar_wait_warp(&a_full[s], (n / NA) & 1, &abort_sh, a.err);
-      if (!ok) return;
-      const int dead = len - step_blk(n) * BR;
-      if (dead < BR) zero_rows<DH>(smem + Pl::A + s * BLK, dead, lane);
-      const uint32_t d = uniform(tmem + (!KEYS && (n & 1) ? Pl::C_S1 : Pl::C_S)), x = desc_lo_k(sb + Pl::A + s * BLK);
-      if (elect_one()) {
-        mma_nt<DH>(d, f0, x);
-        umma_commit(&s_full[KEYS ? 0 : n & 1]);
-      }
-      __syncwarp();
-    };
-    auto dprobs = [&](int n) {
-      const int s = n % NB;
-      ok = ok && mbar_wait_warp(&b_full[s], (n / NB) & 1, &abort_sh, a.err);
-      if (!ok) return;
-      const int dead = len - step_blk(n) * BR;
-      if (KEYS && dead < BR) zero_rows<DH>(smem + Pl::B + s * BLK, dead, lane);
-      const uint32_t x = desc_lo_k(sb + Pl::B + s * BLK);
-      if (elect_one()) {
-        mma_nt<DH>(utmem + Pl::C_DP, f1, x);
-        umma_commit(&dp_full);
-        if (!KEYS) umma_commit(&b_empty[s]);
-      }
-      __syncwarp();
-    };
-    if (n_steps > 0) {
-      scores(0);
-      dprobs(0);
-      if (!KEYS && n_steps > 1) scores(1);
-    }
-    for (int n = 0; n < n_steps && ok; ++n) {
-      if (KEYS) {
-        ok = mbar_wait_warp(&p_full, n & 1, &abort_sh, a.err);
-        if (!ok) break;
-        tc_fence_after();
-        const uint32_t acc = uniform(n > 0), g = desc_lo_mn(sb + Pl::B + (n % NB) * BLK, BR * 128);
-        const uint32_t q = desc_lo_mn(sb + Pl::A + (n % NA) * BLK, BR * 128);
-        if (elect_one()) {  // dV += P^T dO
-          mma_tn<DH>(utmem + Pl::C_A1, utmem + Pl::C_S, g, acc);
-          umma_commit(&b_empty[n % NB]);
+    // ------------------------------------------------------------ products: scores, and what follows from them in their place
+    const uint32_t utmem = uniform(tmem), f0 = desc_lo_k(sb + Pl::F0);
+    bool ok = true;
+    uint32_t z_phase = 0;  // a bit a slot, which is zeroed again only when this warp has let it go
+    int g0 = 0, ni = 0;
+    for (int id = blockIdx.x; id < a.items && ok; id += gridDim.x) {
+      const Item x = item_of<KEYS>(a, id);
+      if (x.n_steps == 0) continue;
+      ok = mbar_wait_warp(&fixed_full, ni & 1, &abort_sh, a.err);
+      // S(n); queries: into buffer g & 1
+      Step<KEYS> at(a, x), to(a, x);  // of S and of what follows from it
+      auto scores = [&](int n) {
+        const int g = g0 + n, ga = KEYS ? g : g + ni + 1, s = ga % NA;
+        ok = ok && mbar_wait_warp(&a_full[s], (ga / NA) & 1, &abort_sh, a.err);
+        if (!ok) return;
+        const int dead = x.len - at.blk * BR;
+        at.next(x);
+        if (dead < BR) zero_rows<DH>(smem + Pl::A + s * BLK, dead, lane);
+        const uint32_t d = uniform(tmem + (!KEYS && (g & 1) ? Pl::C_S1 : Pl::C_S)), k = desc_lo_k(sb + Pl::A + s * BLK);
+        if (elect_one()) {
+          mma_nt<DH>(d, f0, k);
+          umma_commit(&s_full[KEYS ? 0 : g & 1]);
+          if (n + 1 == x.n_steps) umma_commit(&f_free);
         }
         __syncwarp();
-        if (n + 1 < n_steps) scores(n + 1);
-        ok = ok && mbar_wait_warp(&ds_full, n & 1, &abort_sh, a.err);
-        if (!ok) break;
-        tc_fence_after();
-        if (elect_one()) {  // dK += dS^T Q
-          mma_tn<DH>(utmem + Pl::C_A0, utmem + Pl::C_DP, q, acc);
-          umma_commit(&a_empty[n % NA]);
-          if (n + 1 == n_steps) umma_commit(&done);
-        }
-        __syncwarp();
-        if (n + 1 < n_steps) dprobs(n + 1);
-      } else {
-        ok = mbar_wait_warp(&ds_full, n & 1, &abort_sh, a.err);
-        if (!ok) break;
-        tc_fence_after();
-        if (n + 1 < n_steps) dprobs(n + 1);
-        if (!ok) break;
-        const uint32_t acc = uniform(n > 0), x = uniform(tmem + (n & 1 ? Pl::C_S1 : Pl::C_S)), k = desc_lo_mn(sb + Pl::A + (n % NA) * BLK, BR * 128);
-        if (elect_one()) {  // dQ += dS K
-          mma_tn<DH>(utmem + Pl::C_A0, x, k, acc);
-          umma_commit(&a_empty[n % NA]);
-          if (n + 1 == n_steps) umma_commit(&done);
-        }
-        __syncwarp();
-        if (n + 2 < n_steps) scores(n + 2);
+      };
+      if (ok) scores(0);
+      if (ok && !KEYS && x.n_steps > 1) scores(1);
+      if (ok && !KEYS) {  // o has been read: the slot before this item's first keys is free
+        ok = mbar_wait_warp(&stat_full, ni & 1, &abort_sh, a.err);
+        if (ok && lane == 0) mbar_arrive(&a_empty[(g0 + ni) % NA]);
       }
+      for (int n = 0; n < x.n_steps && ok; ++n, to.next(x)) {
+        const int g = g0 + n;
+        const uint32_t acc = uniform(n > 0);
+        if (n == 0 && ni > 0) ok = mbar_wait_warp(&o_read, (ni - 1) & 1, &abort_sh, a.err);
+        if (!ok) break;
+        if (KEYS) {
+          const int s = g % NB;
+          const uint32_t y = desc_lo_mn(sb + Pl::B + s * BLK, BR * 128);
+          ok = mbar_wait_warp(&b_full[s], (g / NB) & 1, &abort_sh, a.err);
+          if (ok && x.len - to.blk * BR < BR) {
+            ok = mbar_wait_warp(&zeroed[s], (z_phase >> s) & 1u, &abort_sh, a.err);
+            z_phase ^= 1u << s;
+          }
+          ok = ok && mbar_wait_warp(&p_full, g & 1, &abort_sh, a.err);
+          if (!ok) break;
+          tc_fence_after();
+          if (elect_one()) {  // dV += P^T dO
+            mma_tn<DH>(utmem + Pl::C_A1, utmem + Pl::C_S, y, acc);
+            umma_commit(&b_empty[s]);
+            if (n + 1 == x.n_steps) umma_commit(&done);
+          }
+          __syncwarp();
+          if (n + 1 < x.n_steps) scores(n + 1);
+        } else {
+          const int s = (g + ni + 1) % NA;
+          const uint32_t d = uniform(tmem + (g & 1 ? Pl::C_S1 : Pl::C_S)), k = desc_lo_mn(sb + Pl::A + s * BLK, BR * 128);
+          ok = mbar_wait_warp(&ds_full[g & 1], (g >> 1) & 1, &abort_sh, a.err);
+          if (!ok) break;
+          tc_fence_after();
+          if (elect_one()) {  // dQ += dS K
+            mma_tn<DH>(utmem + Pl::C_A0, d, k, acc);
+            umma_commit(&a_empty[s]);
+            if (n + 1 == x.n_steps) umma_commit(&done);
+          }
+          __syncwarp();
+          if (n + 2 < x.n_steps) scores(n + 2);
+        }
+      }
+      g0 += x.n_steps;
+      ++ni;
     }
     // what was issued ends before shared memory and TMEM are released
     if (elect_one()) {
       volatile int no_abort = 0;
-      umma_commit(&drain);
-      mbar_wait(&drain, 0, &no_abort, nullptr);
+      umma_commit(&drain[0]);
+      mbar_wait(&drain[0], 0, &no_abort, nullptr);
+    }
+    __syncwarp();
+  } else if (warp == 9) {
+    // ------------------------------------------------------------ products: dP, and (keys) dK from dS in its place
+    const uint32_t utmem = uniform(tmem), f1 = desc_lo_k(sb + Pl::F1);
+    bool ok = true;
+    int g0 = 0, ni = 0;
+    for (int id = blockIdx.x; id < a.items && ok; id += gridDim.x) {
+      const Item x = item_of<KEYS>(a, id);
+      if (x.n_steps == 0) continue;
+      ok = mbar_wait_warp(&fixed_full, ni & 1, &abort_sh, a.err);
+      Step<KEYS> at(a, x);
+      for (int n = 0; n <= x.n_steps && ok; ++n, at.next(x)) {
+        const int g = g0 + n, s = g % NB;
+        const uint32_t v = desc_lo_k(sb + Pl::B + s * BLK), q = desc_lo_mn(sb + Pl::A + ((g + NA - 1) % NA) * BLK, BR * 128);
+        const uint32_t acc = uniform(n > 1);
+        if (n < x.n_steps) {
+          ok = mbar_wait_warp(&b_full[s], (g / NB) & 1, &abort_sh, a.err);
+          if (!ok) break;
+          const int dead = x.len - at.blk * BR;
+          if (KEYS && dead < BR) {
+            zero_rows<DH>(smem + Pl::B + s * BLK, dead, lane);
+            if (lane == 0) mbar_arrive(&zeroed[s]);
+          }
+        } else if (!KEYS) {
+          break;
+        }
+        if (KEYS && n == 1 && ni > 0) ok = mbar_wait_warp(&o_read, (ni - 1) & 1, &abort_sh, a.err);
+        // the last step's dP has been read; (keys) its dS is there
+        if (KEYS ? n > 0 : g > 0) ok = ok && mbar_wait_warp(&ds_full[(g - 1) & 1], ((g - 1) >> 1) & 1, &abort_sh, a.err);
+        if (!ok) break;
+        tc_fence_after();
+        if (elect_one()) {
+          if (KEYS && n > 0) {  // dK += dS^T Q
+            mma_tn<DH>(utmem + Pl::C_A0, utmem + Pl::C_DP, q, acc);
+            umma_commit(&a_empty[(g + NA - 1) % NA]);
+            if (n == x.n_steps) umma_commit(&done);
+          }
+          if (n < x.n_steps) {
+            mma_nt<DH>(utmem + Pl::C_DP, f1, v);
+            umma_commit(&dp_full);
+            umma_commit(&b_empty[s]);
+            if (n + 1 == x.n_steps) umma_commit(&f_free);
+          }
+        }
+        __syncwarp();
+      }
+      g0 += x.n_steps;
+      ++ni;
+    }
+    if (elect_one()) {
+      volatile int no_abort = 0;
+      umma_commit(&drain[1]);
+      mbar_wait(&drain[1], 0, &no_abort, nullptr);
     }
     __syncwarp();
   } else {
     // ------------------------------------------------------------ P and dS: thread = row, half of the columns
-    const int half = warp >> 2, row = 32 * (warp & 3) + lane, r = r0 + row, c0 = 64 * half;
+    const int half = warp >> 2, row = 32 * (warp & 3) + lane, c0 = 64 * half;
     const uint32_t trow = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
     bool ok = true;
-    float my_lse = 0.f, my_d = 0.f;  // queries: of this row, in powers of two
-    float next_stat = 0.f;           // keys: this thread's value of the next step's statistics
-    auto fetch = [&](int n) {
-      const int q = step_blk(n) * BR + (tid & 127);
-      const int64_t at = ((int64_t)b * a.n_heads + step_head(n)) * a.seq + q;
-      next_stat = q >= len ? 0.f : tid < BR ? a.lse[at] * kLog2e : a.D[at];
+    // the next item and what of it comes by plain loads are on their way before this one's end: keys: this thread's value of the
+    // next step's statistics; queries: its row's log-sum-exp
+    // (what an item is, is kept in shared memory: P and dP take most of a thread's registers)
+    float next = 0.f;
+    auto fetch = [&](const volatile Item& x, const Step<KEYS>& s) {
+      const int q = s.blk * BR + (tid & 127);
+      const float* from = tid < BR ? a.lse : a.D;
+      next = 0.f;
+      if (q < x.len) next = from[((int64_t)x.b * a.n_heads + s.head) * a.seq + q];
     };
-    if (KEYS) {
-      if (n_steps > 0) fetch(0);
-    } else {
-      // D = dO . o: each thread half a row
-      const int64_t at = ((int64_t)b * a.n_heads + head) * a.seq + r;
-      if (n_steps > 0) {
-        float d = 0.f;
-        ok = mbar_wait_warp(&fixed_full, 0, &abort_sh, a.err);
-        if (ok && r < len) {
-          my_lse = a.lse[at] * kLog2e;
-          const bf16* o = a.out + ((int64_t)b * a.seq + r) * a.out_stride + head * DH + (DH / 2) * half;
+    auto ahead = [&](int id, int slot) {
+      if (id >= a.items) return;
+      const Item x = item_of<KEYS>(a, id);
+      __syncwarp();
+      if (lane == 0) info[warp][slot] = x;
+      if (x.n_steps > 0) {
+        if (KEYS) {
+          fetch(x, Step<KEYS>(a, x));
+        } else {
+          const int r = x.blk * BR + row;
+          next = 0.f;
+          if (r < x.len) next = a.lse[((int64_t)x.b * a.n_heads + x.head) * a.seq + r];
+        }
+      }
+      __syncwarp();
+    };
+    ahead(blockIdx.x, 0);
+    int g0 = 0, ni = 0, slot = 0;
+    for (int id = blockIdx.x; id < a.items && ok; id += gridDim.x, slot ^= 1) {
+      const volatile Item& x = info[warp][slot];
+      const int r0 = x.blk * BR, r = r0 + row, len = x.len;
+      float my_lse = 0.f, my_d = 0.f;  // queries: of this row, in powers of two
+      if (!KEYS) {
+        if (x.n_steps > 0) {
+          // D = dO . o: each thread half a row
+          float d = 0.f;
+          my_lse = next * kLog2e;
+          const int ga = g0 + ni, s = ga % NA;
+          ok = mbar_wait_warp(&fixed_full, ni & 1, &abort_sh, a.err) && mbar_wait_warp(&a_full[s], (ga / NA) & 1, &abort_sh, a.err);
+          if (!ok) break;
+          if (r < len) {
 #pragma unroll
-          for (int g = 0; g < DH / 16; ++g) {
-            const int c = (DH / 16) * half + g;  // 16-byte chunk of the row
-            const uint4 x = *reinterpret_cast<const uint4*>(o + 8 * g);
-            const uint4 y = *reinterpret_cast<const uint4*>(smem + Pl::F1 + (c >> 3) * (BR * 128) + swz(row, c & 7));
-            const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+            for (int i = 0; i < DH / 16; ++i) {
+              const int c = (DH / 16) * half + i, at = (c >> 3) * (BR * 128) + swz(row, c & 7);  // 16-byte chunk of the row
+              const uint4 o = *reinterpret_cast<const uint4*>(smem + Pl::A + s * BLK + at);
+              const uint4 y = *reinterpret_cast<const uint4*>(smem + Pl::F1 + at);
+              const uint32_t xs[4] = {o.x, o.y, o.z, o.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float2 u = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&xs[e]));
-              const float2 v = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&ys[e]));
-              d = fmaf(u.x, v.x, fmaf(u.y, v.y, d));
+              for (int e = 0; e < 4; ++e) {
+                const float2 u = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&xs[e]));
+                const float2 v = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&ys[e]));
+                d = fmaf(u.x, v.x, fmaf(u.y, v.y, d));
+              }
             }
           }
+          stat[ni & 1][half][row] = d;
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(&f_free);
+            mbar_arrive(&stat_full);
+          }
+          ok = mbar_wait_warp(&stat_full, ni & 1, &abort_sh, a.err);
+          if (!ok) break;
+          my_d = stat[ni & 1][0][row] + stat[ni & 1][1][row];
         }
-        stat[0][half][row] = d;
-        named_sync(1, 256);
-        my_d = stat[0][0][row] + stat[0][1][row];
+        if (half == 0 && r < a.seq) a.D[((int64_t)x.b * a.n_heads + x.head) * a.seq + r] = my_d;
       }
-      if (half == 0 && r < a.seq) a.D[at] = my_d;
-    }
-    for (int n = 0; n < n_steps && ok; ++n) {
-      const int st0 = step_blk(n) * BR;
-      if (KEYS) {
-        stat[n & 1][tid >> 7][tid & 127] = next_stat;
-        if (n + 1 < n_steps) fetch(n + 1);
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&stat_full);
-        ok = mbar_wait_warp(&stat_full, n & 1, &abort_sh, a.err);
+      Step<KEYS> at(a, x);
+      for (int n = 0; n < x.n_steps; ++n) {
+        const int st0 = at.blk * BR, g = g0 + n;
+        at.next(x);
+        if (KEYS) {
+          stat[g & 1][tid >> 7][tid & 127] = tid < BR ? next * kLog2e : next;
+          if (n + 1 < x.n_steps) fetch(x, at);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&stat_full);
+          ok = mbar_wait_warp(&stat_full, g & 1, &abort_sh, a.err);
+          if (!ok) break;
+        }
+        ok = mbar_wait_warp(&s_full[KEYS ? 0 : g & 1], (KEYS ? g : g >> 1) & 1, &abort_sh, a.err);
         if (!ok) break;
-      }
-      ok = mbar_wait_warp(&s_full[KEYS ? 0 : n & 1], (KEYS ? n : n >> 1) & 1, &abort_sh, a.err);
-      if (!ok) break;
-      tc_fence_after();
-      const uint32_t tS = trow + (!KEYS && (n & 1) ? Pl::C_S1 : Pl::C_S) + c0, tDP = trow + Pl::C_DP + c0;
-      const float* L = &stat[n & 1][0][c0];
-      const float* Dc = &stat[n & 1][1][c0];
-      float p[64];
-      uint32_t* pu = reinterpret_cast<uint32_t*>(p);
-      tmem_ld32_issue(tS, pu);
-      tmem_ld32_issue(tS + 32, pu + 32);
-      tmem_wait32(pu);
-      tmem_wait32(pu + 32);
+        tc_fence_after();
+        const uint32_t tS = trow + (!KEYS && (g & 1) ? Pl::C_S1 : Pl::C_S) + c0, tDP = trow + Pl::C_DP + c0;
+        const float* L = &stat[g & 1][0][c0];
+        const float* Dc = &stat[g & 1][1][c0];
+        // the columns that this row's pairs are, a bit each: [from, to), and (queries) those below `sk`
+        uint32_t live[2] = {~0u, ~0u};
+        bool some[2] = {true, true};  // a row of this warp has pairs among these 32 columns
+        const int k_first = KEYS ? r0 : st0, q_first = KEYS ? st0 : r0;
+        const bool whole = k_first + BR - 1 <= q_first && (q_first + BR - 1 - k_first < a.W || k_first + BR <= a.sinks) &&
+                           q_first + BR <= len;
+        if (!whole) {
+          int from, to, sk = 0;
+          if (KEYS) {  // queries from the key itself to its window's end, or the sequence's
+            const int64_t end = r < a.sinks ? len : (int64_t)r + a.W;
+            from = r - st0;
+            to = r < len ? (int)(end < len ? end : len) - st0 : 0;
+          } else {     // keys to the query itself, inside the window or among the sinks
+            to = r < len ? r + 1 - st0 : 0;
+            from = r + 1 - a.W - st0;
+            sk = a.sinks - st0;
+          }
 #pragma unroll
-      for (int c = 0; c < 64; c += 4) {
-        float4 x = make_float4(my_lse, my_lse, my_lse, my_lse);
-        if (KEYS) x = *reinterpret_cast<const float4*>(L + c);
-        p[c] = ex2_fast(fmaf(p[c], a.sl2, -x.x));
-        p[c + 1] = ex2_fast(fmaf(p[c + 1], a.sl2, -x.y));
-        p[c + 2] = ex2_fast(fmaf(p[c + 2], a.sl2, -x.z));
-        p[c + 3] = ex2_fast(fmaf(p[c + 3], a.sl2, -x.w));
-      }
-      // the columns that this row's pairs are: [from, to), and (queries) those below `sk`
-      const int k_first = KEYS ? r0 : st0, q_first = KEYS ? st0 : r0;
-      const bool whole = k_first + BR - 1 <= q_first && (q_first + BR - 1 - k_first < a.W || k_first + BR <= a.sinks) &&
-                         q_first + BR <= len;
-      if (!whole) {
-        int from, to, sk = 0;
-        if (KEYS) {  // queries from the key itself to its window's end, or the sequence's
-          from = r - st0;
-          const int64_t end = r < a.sinks ? len : (int64_t)r + a.W;
-          to = (int)(end < len ? end : len) - st0;
-          if (r >= len) to = from = 0;
-        } else {     // keys to the query itself, inside the window or among the sinks
-          to = r < len ? r + 1 - st0 : 0;
-          from = r + 1 - a.W - st0;
-          sk = r < len ? a.sinks - st0 : 0;
+          for (int c = 0; c < 2; ++c) {
+            const int at = c0 + 32 * c;
+            live[c] = below(to - at) & (~below(from - at) | below(sk - at));
+            some[c] = __any_sync(0xffffffffu, live[c] != 0);
+          }
         }
+        float p[64];
 #pragma unroll
-        for (int c = 0; c < 64; ++c)
-          if (!(c0 + c < to && (c0 + c >= from || c0 + c < sk))) p[c] = 0.f;
-      }
-      if (KEYS) {
+        for (int c = 0; c < 2; ++c) {
+          float* pc = p + 32 * c;
+          if (some[c]) {
+            tmem_ld32(tS + 32 * c, pc);
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+              float4 x = make_float4(my_lse, my_lse, my_lse, my_lse);
+              if (KEYS) x = *reinterpret_cast<const float4*>(L + 32 * c + e);
+              pc[e] = (live[c] >> e) & 1u ? ex2_fast(fmaf(pc[e], a.sl2, -x.x)) : 0.f;
+              pc[e + 1] = (live[c] >> (e + 1)) & 1u ? ex2_fast(fmaf(pc[e + 1], a.sl2, -x.y)) : 0.f;
+              pc[e + 2] = (live[c] >> (e + 2)) & 1u ? ex2_fast(fmaf(pc[e + 2], a.sl2, -x.z)) : 0.f;
+              pc[e + 3] = (live[c] >> (e + 3)) & 1u ? ex2_fast(fmaf(pc[e + 3], a.sl2, -x.w)) : 0.f;
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) pc[e] = 0.f;
+          }
+          if (KEYS) {
+            uint32_t w[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) w[e] = pk2(pc[2 * e], pc[2 * e + 1]);
+            tmem_st16(tS + 16 * c, w);  // over columns that have been read
+          }
+        }
+        if (KEYS) {
+          tmem_st_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&p_full);
+        }
+        ok = mbar_wait_warp(&dp_full, g & 1, &abort_sh, a.err);
+        if (!ok) break;
+        tc_fence_after();
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           uint32_t w[16];
+          if (some[c]) {
+            float dp[32];
+            tmem_ld32(tDP + 32 * c, dp);
 #pragma unroll
-          for (int e = 0; e < 16; ++e) w[e] = pk2(p[32 * c + 2 * e], p[32 * c + 2 * e + 1]);
-          tmem_st16(tS + 16 * c, w);
+            for (int e = 0; e < 32; e += 4) {
+              float4 y = make_float4(my_d, my_d, my_d, my_d);
+              if (KEYS) y = *reinterpret_cast<const float4*>(Dc + 32 * c + e);
+              // (a pair that is not one stays zero, whatever its dP is)
+              const float* pe = p + 32 * c + e;
+              w[e >> 1] = pk2(pe[0] == 0.f ? 0.f : pe[0] * (dp[e] - y.x), pe[1] == 0.f ? 0.f : pe[1] * (dp[e + 1] - y.y));
+              w[(e >> 1) + 1] = pk2(pe[2] == 0.f ? 0.f : pe[2] * (dp[e + 2] - y.z), pe[3] == 0.f ? 0.f : pe[3] * (dp[e + 3] - y.w));
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) w[e] = 0u;
+          }
+          tmem_st16((KEYS ? tDP : tS) + 16 * c, w);  // (keys: over columns that have been read)
         }
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&p_full);
+        if (lane == 0) mbar_arrive(&ds_full[g & 1]);
       }
-      ok = mbar_wait_warp(&dp_full, n & 1, &abort_sh, a.err);
       if (!ok) break;
-      tc_fence_after();
-      float dp[64];
-      uint32_t* du = reinterpret_cast<uint32_t*>(dp);
-      tmem_ld32_issue(tDP, du);
-      tmem_ld32_issue(tDP + 32, du + 32);
-      tmem_wait32(du);
-      tmem_wait32(du + 32);
-#pragma unroll
-      for (int c = 0; c < 64; c += 4) {
-        float4 x = make_float4(my_d, my_d, my_d, my_d);
-        if (KEYS) x = *reinterpret_cast<const float4*>(Dc + c);
-        // (a pair that is not one stays zero, whatever its dP is)
-        p[c] = p[c] == 0.f ? 0.f : p[c] * (dp[c] - x.x);
-        p[c + 1] = p[c + 1] == 0.f ? 0.f : p[c + 1] * (dp[c + 1] - x.y);
-        p[c + 2] = p[c + 2] == 0.f ? 0.f : p[c + 2] * (dp[c + 2] - x.z);
-        p[c + 3] = p[c + 3] == 0.f ? 0.f : p[c + 3] * (dp[c + 3] - x.w);
+      // ---- gradients
+      ahead(id + gridDim.x, slot ^ 1);
+      if (x.n_steps > 0) {
+        ok = mbar_wait_warp(&done, ni & 1, &abort_sh, a.err);
+        if (!ok) break;
+        tc_fence_after();
       }
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        uint32_t w[16];
-#pragma unroll
-        for (int e = 0; e < 16; ++e) w[e] = pk2(p[32 * c + 2 * e], p[32 * c + 2 * e + 1]);
-        tmem_st16((KEYS ? tDP : tS) + 16 * c, w);
-      }
-      tmem_st_wait();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&ds_full);
-    }
-    // ---- gradients: staged over the held blocks (the last product is done), stored by TMA, which leaves out rows past seq
-    if (ok && n_steps > 0) {
-      ok = mbar_wait_warp(&done, 0, &abort_sh, a.err);
-      tc_fence_after();
-    }
-    if (ok) {
-      const bool live = r < len;
-#pragma unroll
-      for (int o = 0; o < (KEYS ? 2 : 1); ++o) {
-        const float f = o == 0 ? a.scale : 1.f;
-        float* part = nullptr;
-        if (KEYS && chunks > 1)
-          part = a.part + ((((int64_t)(b * a.n_kv_heads + head) * a.split + blk) * a.chunks + chunk) * 2 + o) * (BR * DH) + row * DH;
+      const bool any = x.n_steps > 0, split = KEYS && x.chunks > 1;
+      const int quad = r & ~3;
+      const int64_t quad_row = (int64_t)x.b * a.seq + quad, col = x.head * DH + 8 * (lane & 3);
+      float* part = nullptr;
+      if (split)
+        part = a.part + (((int64_t)(x.b * a.n_kv_heads + x.head) * a.split + x.blk) * a.chunks + x.chunk) * (2 * BR * DH) +
+               (row & ~3) * DH + 4 * (lane & 3);
+      constexpr int PIECES = DH / 64, ALL = (KEYS ? 2 : 1) * PIECES;  // 32 columns each
 #pragma unroll 1
-        for (int c = (DH / 2) * half; c < (DH / 2) * (half + 1); c += 32) {
-          float x[32];
-          if (n_steps > 0) tmem_ld32(trow + (o == 0 ? Pl::C_A0 : Pl::C_A1) + c, x);
-#pragma unroll
-          for (int e = 0; e < 32; ++e) x[e] = live && n_steps > 0 ? x[e] * f : 0.f;
-          if (part) {
-#pragma unroll
-            for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(part + c + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
-          } else {
-#pragma unroll
-            for (int g = 0; g < 4; ++g)
-              *reinterpret_cast<uint4*>(smem + (o == 0 ? Pl::F0 : Pl::F1) + (c >> 6) * (BR * 128) + swz(row, ((c & 63) >> 3) + g)) =
-                  make_uint4(pk2(x[8 * g], x[8 * g + 1]), pk2(x[8 * g + 2], x[8 * g + 3]), pk2(x[8 * g + 4], x[8 * g + 5]),
-                             pk2(x[8 * g + 6], x[8 * g + 7]));
+      for (int it = 0; it < ALL; ++it) {
+        const int o = it / PIECES, c = (DH / 2) * half + 32 * (it % PIECES);
+        const float f = r >= len ? 0.f : o == 0 ? a.scale : 1.f;
+        float v[32];
+        if (any) {
+          tmem_ld32(trow + (o == 0 ? Pl::C_A0 : Pl::C_A1) + c, v);
+          if (it + 1 == ALL) {  // the accumulators are free for the next item's products
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&o_read);
           }
         }
-      }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&staged);
-      if (tid == 0 && !(KEYS && chunks > 1) && mbar_wait(&staged, 0, &abort_sh, a.err)) {
 #pragma unroll
-        for (int o = 0; o < (KEYS ? 2 : 1); ++o)
+        for (int e = 0; e < 32; ++e) v[e] = any && r < len ? v[e] * f : 0.f;
+        uint32_t w[16];
+        if (split) {
 #pragma unroll
-          for (int n = 0; n < DH / 64; ++n)
-            tma_store3(o == 0 ? &tmG0 : &tmG1, sb + (o == 0 ? Pl::F0 : Pl::F1) + n * (BR * 128), head * DH + 64 * n, r0, b);
-        tma_store_done();
+          for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) w[e] = __float_as_uint(v[16 * h + e]);
+            transpose4(w, lane);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              *reinterpret_cast<uint4*>(part + o * (BR * DH) + i * DH + c + 16 * h) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+          }
+        } else {
+          bf16* out = a.grad[o] + quad_row * a.grad_stride[o] + col + c;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) w[e] = pk2(v[2 * e], v[2 * e + 1]);
+          transpose4(w, lane);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (quad + i < a.seq)
+              *reinterpret_cast<uint4*>(out + i * a.grad_stride[o]) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+        }
       }
+      g0 += x.n_steps;
+      if (x.n_steps > 0) ++ni;
     }
   }
   tc_fence_before();
@@ -509,18 +670,23 @@ __global__ void __launch_bounds__(256) window_bwd_parts_kernel(const __grid_cons
 }
 
 // How many CTAs share each of the key blocks that hold sinks.  An ordinary key block has (W / 128 + 2) G steps at most and
-// one with sinks up to n_blk G: with up to two such blocks, as many CTAs as bring them back to an ordinary one's length, at
-// most 32.  (With more sinks than that most blocks are long, and the CTAs have even work without it.)
+// one with sinks up to n_blk G: with up to two such blocks, as many CTAs as bring them back to an ordinary one's length, or to
+// half of what each of the 152 SMs has to do in all, at most 32.  (With more sinks than that most blocks are long, and the CTAs
+// have even work without it.  1 x 8192 tokens, 16 heads over 4, window 1024: 9 CTAs each, @A@ us, without @B@; 8 x 1024
+// tokens of 16 heads, window 256, where an SM has 24 steps and the longest block 8: two each 242 us, without @C@.)
 void split_of(const ra_attention_window_args& p, int& split, int& chunks) {
-  const int n_blk = (p.seq + BR - 1) / BR;
+  const int64_t n_blk = (p.seq + BR - 1) / BR, G = p.n_heads / p.n_kv_heads, units = (int64_t)p.batch * p.n_kv_heads;
   const int64_t W = p.window == 0 || p.window > p.seq ? p.seq : p.window;
-  const int64_t ordinary = W / BR + 2;
+  const int64_t ordinary = (W / BR + 2) * G;
   split = 0;
   chunks = 1;
   const int sink_blocks = p.sinks / BR + (p.sinks % BR != 0);
-  if (p.dtype != RA_BF16 || sink_blocks < 1 || sink_blocks > 2 || n_blk < 2 * ordinary) return;
-  split = sink_blocks < n_blk ? sink_blocks : n_blk;
-  chunks = (int)((n_blk + ordinary - 1) / ordinary);
+  if (p.dtype != RA_BF16 || sink_blocks < 1 || sink_blocks > 2 || sink_blocks >= n_blk) return;
+  const int64_t total = units * (sink_blocks * n_blk * G + (n_blk - sink_blocks) * ordinary), half = total / (2 * 152);
+  const int64_t most = ordinary > half ? ordinary : half;
+  if (n_blk * G < 2 * most) return;
+  split = sink_blocks;
+  chunks = (int)((n_blk * G + most - 1) / most);
   if (chunks > 32) chunks = 32;
 }
 size_t d_bytes(const ra_attention_window_args& p) { return ((size_t)p.batch * p.seq * p.n_heads * 4 + 255) / 256 * 256; }
@@ -530,8 +696,6 @@ cudaError_t launch(const ra_attention_window_args& p, cudaStream_t st) {
   WindowBwdArgs a;
   a.lens = p.lens_dev;
   a.lse = p.lse_dev;
-  a.out = (const bf16*)p.out_dev;
-  a.out_stride = p.out_stride;
   a.D = (float*)p.workspace_dev;
   a.part = (float*)((char*)p.workspace_dev + d_bytes(p));
   a.err = p.err_dev;
@@ -547,23 +711,32 @@ cudaError_t launch(const ra_attention_window_args& p, cudaStream_t st) {
   a.sl2 = p.scale * kLog2e;
   const int64_t gq = (int64_t)a.n_blk * p.batch * p.n_heads;
   const int64_t gk = (int64_t)(a.n_blk - a.split + a.split * a.chunks) * p.batch * p.n_kv_heads;
-  if (gq > INT32_MAX || gk > INT32_MAX) return cudaErrorNotSupported;
-  CUtensorMap q, k, v, g, dq, dk, dv;
+  if (gq > INT32_MAX - 1024 || gk > INT32_MAX - 1024) return cudaErrorNotSupported;
+  CUtensorMap q, k, v, g, o;
   const int64_t hq = (int64_t)p.n_heads * DH, hk = (int64_t)p.n_kv_heads * DH;
   if (!tma_map_bf16_batch(&q, p.q_dev, p.batch, p.seq, hq, p.q_stride, 64, BR) ||
       !tma_map_bf16_batch(&k, p.k_dev, p.batch, p.seq, hk, p.k_stride, 64, BR) ||
       !tma_map_bf16_batch(&v, p.v_dev, p.batch, p.seq, hk, p.v_stride, 64, BR) ||
       !tma_map_bf16_batch(&g, p.dout_dev, p.batch, p.seq, hq, p.dout_stride, 64, BR) ||
-      !tma_map_bf16_batch(&dq, p.dq_dev, p.batch, p.seq, hq, p.dq_stride, 64, BR) ||
-      !tma_map_bf16_batch(&dk, p.dk_dev, p.batch, p.seq, hk, p.dk_stride, 64, BR) ||
-      !tma_map_bf16_batch(&dv, p.dv_dev, p.batch, p.seq, hk, p.dv_stride, 64, BR))
+      !tma_map_bf16_batch(&o, p.out_dev, p.batch, p.seq, hq, p.out_stride, 64, BR))
     return cudaErrorNotSupported;
   cudaError_t e = allow_smem(window_bwd_tc_kernel<DH, false>, BwdPlan<DH>::BYTES);
   if (e == cudaSuccess) e = allow_smem(window_bwd_tc_kernel<DH, true>, BwdPlan<DH>::BYTES);
+  const int sms = device_sm_count();
+  a.items = (int)gq;
+  a.grad[0] = (bf16*)p.dq_dev;
+  a.grad_stride[0] = p.dq_stride;
+  a.grad[1] = nullptr;
+  a.grad_stride[1] = 0;
   if (e == cudaSuccess)
-    e = launch_pdl(window_bwd_tc_kernel<DH, false>, dim3((unsigned)gq), dim3(THREADS), (size_t)BwdPlan<DH>::BYTES, st, q, k, v, g, dq, dq, a);
+    e = launch_pdl(window_bwd_tc_kernel<DH, false>, dim3(a.items < sms ? a.items : sms), dim3(THREADS), (size_t)BwdPlan<DH>::BYTES, st, q, k, v, g, o, a);
+  a.items = (int)gk;
+  a.grad[0] = (bf16*)p.dk_dev;
+  a.grad_stride[0] = p.dk_stride;
+  a.grad[1] = (bf16*)p.dv_dev;
+  a.grad_stride[1] = p.dv_stride;
   if (e == cudaSuccess)
-    e = launch_pdl(window_bwd_tc_kernel<DH, true>, dim3((unsigned)gk), dim3(THREADS), (size_t)BwdPlan<DH>::BYTES, st, q, k, v, g, dk, dv, a);
+    e = launch_pdl(window_bwd_tc_kernel<DH, true>, dim3(a.items < sms ? a.items : sms), dim3(THREADS), (size_t)BwdPlan<DH>::BYTES, st, q, k, v, g, o, a);
   note_launch(2);
   if (e == cudaSuccess && a.split > 0) {
     const int64_t threads = (int64_t)p.batch * p.n_kv_heads * a.split * 2 * BR * DH / 4;

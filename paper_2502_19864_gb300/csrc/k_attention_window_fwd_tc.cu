@@ -66,9 +66,6 @@ struct Blocks {
   __device__ __forceinline__ int at(int i) const { return i < ns ? i : i - ns + lo; }
 };
 
-// bits 0 .. n - 1
-__device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
-
 // A pair of tiles, and what its rows see; the row blocks with the most keys come first
 struct Item {
   int b, len, head[2], q0[2], kvh;

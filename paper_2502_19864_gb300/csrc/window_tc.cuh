@@ -55,9 +55,27 @@ __device__ __forceinline__ uint32_t pk2(float a, float b) {
   __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<uint32_t*>(&h);
 }
+// Four 16-byte pieces a lane, of four lanes' rows in turn: afterwards piece i is row (lane & ~3) + i's, its (lane & 3)-th.  A
+// store of a piece a lane then writes 64 bytes of each of eight rows, where a row a lane it would touch 32 lines
+__device__ __forceinline__ void transpose4(uint32_t* w, int lane) {
+#pragma unroll
+  for (int b = 1; b < 4; b <<= 1)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (!(i & b))
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          uint32_t &lo = w[4 * i + e], &hi = w[4 * (i | b) + e];
+          const uint32_t got = __shfl_xor_sync(0xffffffffu, lane & b ? lo : hi, b);
+          if (lane & b) lo = got;
+          else hi = got;
+        }
+}
 __device__ __forceinline__ void named_sync(int id, int threads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
+// bits 0 .. n - 1
+__device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
 // The rows from `dead` on of a [128][DH] operand block (64-wide swizzle atoms of [128][128 bytes]) become zero, by one warp:
 // memory past a sequence's end may hold anything, and 0 times NaN is not 0
 template <int DH>
