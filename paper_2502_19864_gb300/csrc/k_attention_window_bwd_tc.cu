@@ -515,19 +515,26 @@ __global__ void __launch_bounds__(THREADS, 1) window_bwd_tc_kernel(const __grid_
           }
         }
         float p[64];
+        tmem_ld32_issue(tS, reinterpret_cast<uint32_t*>(p));
+        tmem_ld32_issue(tS + 32, reinterpret_cast<uint32_t*>(p + 32));
+        tmem_wait32(reinterpret_cast<uint32_t*>(p));
+        tmem_wait32(reinterpret_cast<uint32_t*>(p + 32));
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           float* pc = p + 32 * c;
           if (some[c]) {
-            tmem_ld32(tS + 32 * c, pc);
 #pragma unroll
             for (int e = 0; e < 32; e += 4) {
               float4 x = make_float4(my_lse, my_lse, my_lse, my_lse);
               if (KEYS) x = *reinterpret_cast<const float4*>(L + 32 * c + e);
-              pc[e] = (live[c] >> e) & 1u ? ex2_fast(fmaf(pc[e], a.sl2, -x.x)) : 0.f;
-              pc[e + 1] = (live[c] >> (e + 1)) & 1u ? ex2_fast(fmaf(pc[e + 1], a.sl2, -x.y)) : 0.f;
-              pc[e + 2] = (live[c] >> (e + 2)) & 1u ? ex2_fast(fmaf(pc[e + 2], a.sl2, -x.z)) : 0.f;
-              pc[e + 3] = (live[c] >> (e + 3)) & 1u ? ex2_fast(fmaf(pc[e + 3], a.sl2, -x.w)) : 0.f;
+              pc[e] = ex2_fast(fmaf(pc[e], a.sl2, -x.x));
+              pc[e + 1] = ex2_fast(fmaf(pc[e + 1], a.sl2, -x.y));
+              pc[e + 2] = ex2_fast(fmaf(pc[e + 2], a.sl2, -x.z));
+              pc[e + 3] = ex2_fast(fmaf(pc[e + 3], a.sl2, -x.w));
+            }
+            if (!whole) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e) pc[e] = (live[c] >> e) & 1u ? pc[e] : 0.f;
             }
           } else {
 #pragma unroll
