@@ -8,11 +8,20 @@
 //   keys     a CTA holds K_j, V_j and streams the query blocks that see the rows, head by head of the group: S^T, dP^T,
 //            dV += P^T dO_i, dK += dS^T Q_i.
 // The scores are computed in both: seven products a pair of blocks where atomics would do with five.
-// Ten warps: eight of arithmetic (a thread a row of the held block and half of the columns), one that issues the products,
-// one that loads by TMA.  P (in fp32, in registers) and dS are the owner's of the row; as bf16 they go back to TMEM, over the
-// scores they came from, and are the A operand of the next product there.
-//   keys:    dV(n), S(n+1) run while the warps turn dP(n) into dS(n); dK(n), dP(n+1) while they turn S(n+1) into P(n+1).
-//   queries: the scores have two buffers: dP(n+1), dQ(n), S(n+2) run while the warps turn S(n+1) into P(n+1).
+// Eleven warps: eight of arithmetic (a thread a row of the held block and half of the columns), two that issue products, one
+// that loads by TMA.  P (in fp32, in registers) and dS are the owner's of the row; as bf16 they go back to TMEM, over the
+// values they came from, and are the A operand of the next product there.  A warp that issues has a place in TMEM and all that
+// goes through it, so that its products are in order by themselves:
+//   keys:    dV(n), S(n+1) while the warps turn dP(n) into dS(n); dK(n), dP(n+1) while they turn S(n+1) into P(n+1).
+//   queries: dQ(n), S(n+2) in two buffers of scores; dP(n+1).
+// (One warp for all of a pass's products: 3000 and 4150 cycles a step of long sequences, of which it issued 2700 and 3900;
+// two: 2500 and 3500, which the warps of arithmetic take, 1100 for P (64 exponentials a thread on a pipe that two warps
+// share) and 1000 for dS, and their waits.)
+// The CTAs are persistent: a CTA's next block is loaded when the last products with this one are done, and its first scores
+// are computed while gradients leave.  Steps are masked by bits, and 32 columns that no row of a warp sees are left out: of a
+// window of 256 two blocks of three are masked.  8 x 1024 tokens, 16 heads of 128, window 256, 4 sinks: 57 us the queries,
+// 78 the keys (a CTA a block, one warp of products, a compare a column: 94 and 109); what it
+// reads and writes takes 30 us each.  2 x 4096 tokens without a window: 446 us, 1079 TFLOP/s over the seven products.
 // The first key blocks may hold sinks, which every later query sees: where that makes them much longer than a block of the
 // window, several CTAs share such a block's queries and a last kernel adds their fp32 parts in order.
 // Rows past a sequence's end are set to zero in operands that a product sums over.
@@ -679,8 +688,8 @@ __global__ void __launch_bounds__(256) window_bwd_parts_kernel(const __grid_cons
 // How many CTAs share each of the key blocks that hold sinks.  An ordinary key block has (W / 128 + 2) G steps at most and
 // one with sinks up to n_blk G: with up to two such blocks, as many CTAs as bring them back to an ordinary one's length, or to
 // half of what each of the 152 SMs has to do in all, at most 32.  (With more sinks than that most blocks are long, and the CTAs
-// have even work without it.  1 x 8192 tokens, 16 heads over 4, window 1024: 9 CTAs each, @A@ us, without @B@; 8 x 1024
-// tokens of 16 heads, window 256, where an SM has 24 steps and the longest block 8: two each 242 us, without @C@.)
+// have even work without it.  1 x 8192 tokens, 16 heads over 4, window 1024, forward and backward: shared
+// 336 us, else 748; 8 x 1024 tokens of 16 heads, window 256, where an SM has 24 steps and the longest block 8: 217 us, else 203.)
 void split_of(const ra_attention_window_args& p, int& split, int& chunks) {
   const int64_t n_blk = (p.seq + BR - 1) / BR, G = p.n_heads / p.n_kv_heads, units = (int64_t)p.batch * p.n_kv_heads;
   const int64_t W = p.window == 0 || p.window > p.seq ? p.seq : p.window;

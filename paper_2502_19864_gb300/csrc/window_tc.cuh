@@ -21,15 +21,6 @@ __device__ __forceinline__ void tma_load4(const CUtensorMap* tm, uint32_t dst, u
       " [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(c0), "r"(c1), "r"(c2), "r"(c3),
       "r"(smem_u32(bar)) : "memory");
 }
-__device__ __forceinline__ void tma_store3(const CUtensorMap* tm, uint32_t src, int c0, int c1, int c2) {
-  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(
-                   reinterpret_cast<uint64_t>(tm)), "r"(c0), "r"(c1), "r"(c2), "r"(src) : "memory");
-}
-// every store of this thread has left shared memory and reached global memory
-__device__ __forceinline__ void tma_store_done() {
-  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-  asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-}
 // The low words of the operands' descriptors (address and leading byte offset), in a uniform register, and the whole: what
 // a product's issue costs is the moves of its operands into uniform registers, so that a base goes there once and steps
 // are added to it (the address is the lowest field; 16 bytes count one)
