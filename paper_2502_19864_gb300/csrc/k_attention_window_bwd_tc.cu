@@ -25,6 +25,8 @@
 // The first key blocks may hold sinks, which every later query sees: where that makes them much longer than a block of the
 // window, several CTAs share such a block's queries and a last kernel adds their fp32 parts in order.
 // Rows past a sequence's end are set to zero in operands that a product sums over.
+// dS enters its products as bf16, one rounding a pair as the inputs of the formula have, and D is of the rounded output: dQ and dK are
+// 0.0027 from 64 bits where their own rounding is 0.0017.
 #include "common.cuh"
 #include "operators.h"
 #include "window_tc.cuh"
