@@ -9,15 +9,17 @@
 // A query CTA holds 32 queries and walks the blocks of 64 keys that any of them sees: those of the window and those that
 // hold sinks.  A key CTA holds 32 keys and walks, head by head of its group, the blocks of 64 queries that see any of them:
 // dK and dV are sums in a fixed order.  Keys that are sinks are seen by every later query; where that makes their blocks
-// much longer than a window, several CTAs share a block's queries and a last kernel adds their parts in order.  The query
-// pass of the backward computes D on its way and leaves it for the key pass.  Rows past the sequence's end are loaded as
+// much longer than a window, several CTAs share a block's queries and a last kernel adds their parts in order.  A kernel
+// before them computes D, so that both passes of the backward run in one launch.  Rows past the sequence's end are loaded as
 // zeros, whatever memory holds there.
 // A warp has four held rows: a thread keeps their scores with 2 of the 64 streamed rows and their outputs in DH / 32
 // columns.  What bounds it is the latency of a step at the sizes that fp32 models have, not a pipe: 32 held rows and eight
 // warps (64 rows and as many warps: 228 us for 3 sequences of 333 tokens, 4 heads of 64 on 2, window 100, forward and
-// backward; four warps of 4 x 4 scores a thread: 102 us; this: 75 us), and the next step's rows on their way.
+// backward; four warps of 4 x 4 scores a thread: 102 us; this, the passes one after the other: 77 us), the next step's rows on
+// their way, and both passes at once: 55 us.
 #include "common.cuh"
 #include "operators.h"
+#include "paged.cuh"
 
 namespace ra {
 namespace {
@@ -119,9 +121,8 @@ __device__ __forceinline__ void store_rows(float* dst, int64_t stride, const flo
 struct Geometry {  // of a CTA's (block, sequence, head)
   int blk, b, head, len;
 };
-__device__ __forceinline__ Geometry geometry(const ra_attention_window_args& a, int heads, int n_blk) {
+__device__ __forceinline__ Geometry geometry(const ra_attention_window_args& a, int heads, int n_blk, int64_t id) {
   Geometry g;
-  const int64_t id = blockIdx.x;
   g.blk = n_blk - 1 - (int)(id % n_blk);
   const int bh = (int)(id / n_blk);
   g.b = bh / heads;
@@ -161,7 +162,7 @@ __global__ void __launch_bounds__(NT) window_fwd_simt_kernel(const __grid_consta
   float *Q = sm, *KV = Q + P::HELD, *X = KV + 4 * P::TILE;  // (two buffers of K and V)
   pdl_wait();
   pdl_trigger();
-  const Geometry g = geometry(a, a.n_heads, n_blk);
+  const Geometry g = geometry(a, a.n_heads, n_blk, blockIdx.x);
   const int tid = threadIdx.x, ty = tid >> 5, tx = tid & 31, q0 = g.blk * BH, dh = a.head_dim;
   const int kvh = g.head / (a.n_heads / a.n_kv_heads);
   const int64_t tok0 = (int64_t)g.b * a.seq;
@@ -239,17 +240,39 @@ __global__ void __launch_bounds__(NT) window_fwd_simt_kernel(const __grid_consta
 }
 
 // ---- backward ------------------------------------------------------------------------------
-// KEYS: the held rows are keys (dK, dV), the streamed ones queries; else queries (dQ, D) and keys
+// D = dO . o of every row and head, eight threads each
+__global__ void __launch_bounds__(256) window_d_simt_kernel(const __grid_constant__ ra_attention_window_args a, float* Dv) {
+  pdl_wait();
+  pdl_trigger();
+  const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 3;  // (token of the batch, head)
+  const int64_t tok = row / a.n_heads;
+  const int h = (int)(row - tok * a.n_heads), part = threadIdx.x & 7;
+  const int64_t b = tok / a.seq;
+  if (b >= a.batch) return;  // (the eight of a row together)
+  const int q = (int)(tok - b * a.seq), len = clamp_len(a.lens_dev ? a.lens_dev[b] : a.seq, a.seq, a.err_dev);
+  float d = 0.f;
+  if (q < len) {
+    const float* o = (const float*)a.out_dev + tok * a.out_stride + h * a.head_dim;
+    const float* g = (const float*)a.dout_dev + tok * a.dout_stride + h * a.head_dim;
+    for (int c = 4 * part; c < a.head_dim; c += 32) {
+      const float4 x = *reinterpret_cast<const float4*>(o + c), y = *reinterpret_cast<const float4*>(g + c);
+      d = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, d))));
+    }
+  }
+#pragma unroll
+  for (int m = 1; m < 8; m <<= 1) d += __shfl_xor_sync(0xffu << (threadIdx.x & 24), d, m);
+  if (part == 0) Dv[(b * a.n_heads + h) * a.seq + q] = d;
+}
+
+// KEYS: the held rows are keys (dK, dV), the streamed ones queries; else queries (dQ) and keys
 template <int DH, bool KEYS>
-__global__ void __launch_bounds__(NT) window_bwd_simt_kernel(const __grid_constant__ ra_attention_window_args a, float* Dv,
-                                                             float* parts, int W, int n_blk, int split, int chunks) {
+__device__ __forceinline__ void bwd_pass(const ra_attention_window_args& a, const float* Dv, float* parts, int W, int n_blk, int split, int chunks,
+                                         int64_t cta) {
   extern __shared__ __align__(16) float sm[];
   using P = Plan<DH>;
   float *T0 = sm, *T1 = T0 + P::HELD, *BUF = T1 + P::HELD, *X = BUF + 4 * P::TILE, *STAT = X + BH * PP;  // (two buffers of the streamed pair, and of lse and D)
-  pdl_wait();
-  pdl_trigger();
   const int G = a.n_heads / a.n_kv_heads, items = n_blk - split + split * chunks;
-  Geometry g = geometry(a, KEYS ? a.n_kv_heads : a.n_heads, items);
+  Geometry g = geometry(a, KEYS ? a.n_kv_heads : a.n_heads, items, cta);
   int chunk = 0, n_chunks = 1;
   if (KEYS) {  // (g.blk counts down: the first blocks, which most queries see, come first)
     const int it = items - 1 - g.blk;
@@ -337,7 +360,10 @@ __global__ void __launch_bounds__(NT) window_bwd_simt_kernel(const __grid_consta
       load_rows<DH, BH>(T1, (const float*)a.dout_dev + tok0 * a.dout_stride + g.head * dh, a.dout_stride, r0, g.len, dh);
       const int64_t at = ((int64_t)g.b * a.n_heads + g.head) * a.seq + r0;
       float *L = STAT, *D = L + BT;
-      if (tid < BH) L[tid] = r0 + tid < g.len ? a.lse_dev[at + tid] : 0.f;
+      if (tid < BH) {
+        L[tid] = r0 + tid < g.len ? a.lse_dev[at + tid] : 0.f;
+        D[tid] = r0 + tid < g.len ? Dv[at + tid] : 0.f;
+      }
       const KeyBlocks kb = key_blocks(r0, last, W, a.sinks);
       auto fetch = [&](int n) {
         if (n < kb.n) {
@@ -347,29 +373,7 @@ __global__ void __launch_bounds__(NT) window_bwd_simt_kernel(const __grid_consta
         }
         loads_commit();
       };
-      loads_commit();
       fetch(0);
-      loads_before_newest();  // the held rows
-      __syncthreads();
-      // D = dO . o, eight threads a row
-      {
-        const int row = tid >> 3;
-        float d = 0.f;
-        if (r0 + row < g.len) {
-          const float* o = (const float*)a.out_dev + (tok0 + r0 + row) * a.out_stride + g.head * dh;
-          for (int c = 4 * (tid & 7); c < dh; c += 32) {
-            const float4 x = *reinterpret_cast<const float4*>(o + c), y = *reinterpret_cast<const float4*>(T1 + row * P::DP + c);
-            d = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, d))));
-          }
-        }
-        d += __shfl_xor_sync(0xffffffffu, d, 1);
-        d += __shfl_xor_sync(0xffffffffu, d, 2);
-        d += __shfl_xor_sync(0xffffffffu, d, 4);
-        if ((tid & 7) == 0) {
-          D[row] = d;
-          if (r0 + row < a.seq) Dv[at + row] = d;
-        }
-      }
       for (int n = 0; n < kb.n; ++n) {
         const int k0 = kb.at(n) * BT;
         const float *T2 = BUF + (n & 1) * 2 * P::TILE, *T3 = T2 + P::TILE;
@@ -405,6 +409,18 @@ __global__ void __launch_bounds__(NT) window_bwd_simt_kernel(const __grid_consta
   }
 }
 
+// Both passes in one launch, the keys' CTAs (the longer ones) first: where there are few of either they run at once
+template <int DH>
+__global__ void __launch_bounds__(NT) window_bwd_simt_kernel(const __grid_constant__ ra_attention_window_args a, const float* Dv, float* parts, int W,
+                                                             int n_blk, int split, int chunks, int64_t key_ctas) {
+  pdl_wait();
+  pdl_trigger();
+  if (blockIdx.x < key_ctas)
+    bwd_pass<DH, true>(a, Dv, parts, W, n_blk, split, chunks, blockIdx.x);
+  else
+    bwd_pass<DH, false>(a, Dv, parts, W, n_blk, 0, 1, blockIdx.x - key_ctas);
+}
+
 // dK and dV of the shared key blocks: the parts in order, four values a thread
 template <int DH>
 __global__ void __launch_bounds__(256) window_bwd_simt_parts_kernel(const __grid_constant__ ra_attention_window_args a, const float* parts,
@@ -438,7 +454,8 @@ int dims_of(const ra_attention_window_args& a) { return a.head_dim <= 32 ? 32 : 
 // How many CTAs share each of the first `split` key blocks.  An ordinary block is seen from W + 32 queries, one with sinks
 // from all: up to 128 sinks and where that is twice as long, as many CTAs as bring those blocks back to an ordinary one's
 // length, at most 32.  Where the key blocks are fewer than 152 (the SMs, as a constant: the order of the sums is the shape's),
-// all are shared, so that the SMs have a CTA each, at most 8 a block (66 blocks of the case above: 45 -> 35 us).
+// all are shared, so that the SMs have two CTAs each beside those of the queries, at most 8 a block (63 blocks of 2000 tokens,
+// 2 heads of 32 over 1: one CTA an SM 136 us, two 88; 66 blocks of the case above: 57 and 55 us; 176 blocks: 62 us, shared 66).
 void split_of(const ra_attention_window_args& a, int& split, int& chunks) {
   const int64_t ordinary = (int64_t)window_of(a) + BH;
   split = 0;
@@ -448,7 +465,7 @@ void split_of(const ra_attention_window_args& a, int& split, int& chunks) {
   if (all == 0) return;
   if (all < 152) {
     split = n_blk;
-    chunks = (int)((152 + all - 1) / all);
+    chunks = (int)((2 * 152 + all - 1) / all);
     if (chunks > 8) chunks = 8;
     return;
   }
@@ -477,15 +494,15 @@ cudaError_t bwd_simt(const ra_attention_window_args& a, cudaStream_t st) {
   split_of(a, split, chunks);
   const int n_blk = (a.seq + BH - 1) / BH;
   const int64_t gq = (int64_t)n_blk * a.batch * a.n_heads, gk = (int64_t)(n_blk - split + split * chunks) * a.batch * a.n_kv_heads;
-  if (gq > INT32_MAX || gk > INT32_MAX) return cudaErrorNotSupported;
+  const int64_t d_ctas = ((int64_t)a.batch * a.seq * a.n_heads + 31) / 32;
+  if (gq + gk > INT32_MAX || d_ctas > INT32_MAX) return cudaErrorNotSupported;
   float* D = (float*)a.workspace_dev;
   float* parts = (float*)((char*)a.workspace_dev + d_bytes(a));
-  cudaError_t e = allow_smem(window_bwd_simt_kernel<DH, true>, Plan<DH>::BWD_BYTES);
-  if (e == cudaSuccess) e = allow_smem(window_bwd_simt_kernel<DH, false>, Plan<DH>::BWD_BYTES);
+  cudaError_t e = allow_smem(window_bwd_simt_kernel<DH>, Plan<DH>::BWD_BYTES);
+  if (e == cudaSuccess) e = launch_pdl(window_d_simt_kernel, dim3((unsigned)d_ctas), dim3(256), 0, st, a, D);
   if (e == cudaSuccess)
-    e = launch_pdl(window_bwd_simt_kernel<DH, false>, dim3((unsigned)gq), dim3(NT), Plan<DH>::BWD_BYTES, st, a, D, parts, window_of(a), n_blk, 0, 1);
-  if (e == cudaSuccess)
-    e = launch_pdl(window_bwd_simt_kernel<DH, true>, dim3((unsigned)gk), dim3(NT), Plan<DH>::BWD_BYTES, st, a, D, parts, window_of(a), n_blk, split, chunks);
+    e = launch_pdl(window_bwd_simt_kernel<DH>, dim3((unsigned)(gq + gk)), dim3(NT), Plan<DH>::BWD_BYTES, st, a, (const float*)D, parts, window_of(a),
+                   n_blk, split, chunks, gk);
   note_launch(2);
   if (e == cudaSuccess && split > 0) {
     const int64_t threads = (int64_t)a.batch * a.n_kv_heads * split * 2 * BH * DH / 4;
