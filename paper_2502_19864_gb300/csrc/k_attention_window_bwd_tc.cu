@@ -13,20 +13,22 @@
 // values they came from, and are the A operand of the next product there.  A warp that issues has a place in TMEM and all that
 // goes through it, so that its products are in order by themselves:
 //   keys:    dV(n), S(n+1) while the warps turn dP(n) into dS(n); dK(n), dP(n+1) while they turn S(n+1) into P(n+1).
-//   queries: dQ(n), S(n+2) in two buffers of scores; dP(n+1).
+//   queries: dQ(n) in two terms, S(n+2) in two buffers of scores; dP(n+1).
 // (One warp for all of a pass's products: 3000 and 4150 cycles a step of long sequences, of which it issued 2700 and 3900;
 // two: 2500 and 3500, which the warps of arithmetic take, 1100 for P (64 exponentials a thread on a pipe that two warps
 // share) and 1000 for dS, and their waits.)
 // The CTAs are persistent: a CTA's next block is loaded when the last products with this one are done, and its first scores
 // are computed while gradients leave.  Steps are masked by bits, and 32 columns that no row of a warp sees are left out: of a
-// window of 256 two blocks of three are masked.  8 x 1024 tokens, 16 heads of 128, window 256, 4 sinks: 57 us the queries,
-// 78 the keys (a CTA a block, one warp of products, a compare a column: 94 and 109); what it
-// reads and writes takes 30 us each.  2 x 4096 tokens without a window: 446 us, 1079 TFLOP/s over the seven products.
+// window of 256 two blocks of three are masked.  8 x 1024 tokens, 16 heads of 128, window 256, 4 sinks: 65 us the queries, 76 the
+// keys (a CTA a block, one warp of products, a compare a column, dS in one term: 94 and 109); what it reads and writes takes 30
+// us each.  2 x 4096 tokens without a window: 503 us, 957 TFLOP/s over seven products.
 // The first key blocks may hold sinks, which every later query sees: where that makes them much longer than a block of the
 // window, several CTAs share such a block's queries and a last kernel adds their fp32 parts in order.
 // Rows past a sequence's end are set to zero in operands that a product sums over.
-// dS enters its products as bf16, one rounding a pair as the inputs of the formula have, and D is of the rounded output: dQ and dK are
-// 0.0027 from 64 bits where their own rounding is 0.0017.
+// What is rounded: P to bf16 before dV.  dS goes into dQ in two bf16 terms (its first product is followed by one with what the
+// first left over) and into dK in one; D, of the rounded output, is good enough for dQ then, and leaves the query pass as
+// sum_j P_ij dP_ij for dK.  dQ and dK are 0.0023 from 64 bits, where their own rounding is 0.0017; with dS in one term and D of
+// the rounded output in both, 0.0027 to 0.0029 (and 203 us where this takes 211: 8 x 1024 tokens below, both directions).
 #include "common.cuh"
 #include "operators.h"
 #include "window_tc.cuh"
@@ -170,11 +172,11 @@ __global__ void __launch_bounds__(THREADS, 1) window_bwd_tc_kernel(const __grid_
   // f_free: the held blocks were read for the last time; zeroed: (keys) rows past the end in a dO slot; done: an item's gradients
   // are complete; o_read: they have left TMEM
   __shared__ __align__(8) uint64_t fixed_full, f_free, a_full[NA], a_empty[NA], b_full[NB], b_empty[NB], zeroed[NB];
-  __shared__ __align__(8) uint64_t s_full[2], dp_full, p_full, ds_full[2], stat_full, done, o_read, drain[2];
+  __shared__ __align__(8) uint64_t s_full[2], dp_full, p_full, ds_full[2], stat_full, sum_full, done, o_read, drain[2];
   __shared__ uint32_t tmem_sh;
   __shared__ Item info[8][2];
   __shared__ volatile int abort_sh;
-  __shared__ __align__(16) float stat[2][2][BR];  // keys: log-sum-exps and D of the query block, two steps; queries: D's halves, two items
+  __shared__ __align__(16) float stat[2][2][BR];  // keys: log-sum-exps and D of the query block, two steps; queries: halves of D, of the sums of dS
   const uint32_t sb = smem_u32(smem);
   if (sb & 1023u) {  // the swizzled operand tiles need 1024-byte alignment
     if (threadIdx.x == 0) set_dev_error(a.err, RA_DEVERR_BOUNDS);
@@ -206,6 +208,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_bwd_tc_kernel(const __grid_
       mbar_init(&dp_full, 1);
       mbar_init(&p_full, 8);
       mbar_init(&stat_full, 8);
+      mbar_init(&sum_full, 8);
       mbar_init(&done, KEYS ? 2 : 1);
       mbar_init(&o_read, 8);
       abort_sh = 0;
@@ -340,6 +343,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_bwd_tc_kernel(const __grid_
           tc_fence_after();
           if (elect_one()) {  // dQ += dS K
             mma_tn<DH>(utmem + Pl::C_A0, d, k, acc);
+            mma_tn<DH>(utmem + Pl::C_A0, d + 32, k, 1u);
             umma_commit(&a_empty[s]);
             if (n + 1 == x.n_steps) umma_commit(&done);
           }
@@ -471,7 +475,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_bwd_tc_kernel(const __grid_
               }
             }
           }
-          stat[ni & 1][half][row] = d;
+          stat[0][half][row] = d;
           __syncwarp();
           if (lane == 0) {
             mbar_arrive(&f_free);
@@ -479,10 +483,10 @@ __global__ void __launch_bounds__(THREADS, 1) window_bwd_tc_kernel(const __grid_
           }
           ok = mbar_wait_warp(&stat_full, ni & 1, &abort_sh, a.err);
           if (!ok) break;
-          my_d = stat[ni & 1][0][row] + stat[ni & 1][1][row];
+          my_d = stat[0][0][row] + stat[0][1][row];
         }
-        if (half == 0 && r < a.seq) a.D[((int64_t)x.b * a.n_heads + x.head) * a.seq + r] = my_d;
       }
+      float sum = 0.f;  // queries: of the row's dS
       Step<KEYS> at(a, x);
       for (int n = 0; n < x.n_steps; ++n) {
         const int st0 = at.blk * BR, g = g0 + n;
@@ -568,25 +572,36 @@ __global__ void __launch_bounds__(THREADS, 1) window_bwd_tc_kernel(const __grid_
         if (!ok) break;
         tc_fence_after();
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          uint32_t w[16];
-          if (some[c]) {
-            float dp[32];
-            tmem_ld32(tDP + 32 * c, dp);
+        for (int c = 0; c < 4; ++c) {  // (16 columns at a time: more would leave too few registers)
+          uint32_t w[8], rest[8];
+          if (some[c >> 1]) {
+            float dp[16];
+            tmem_ld16(tDP + 16 * c, dp);
 #pragma unroll
-            for (int e = 0; e < 32; e += 4) {
+            for (int e = 0; e < 16; e += 4) {
               float4 y = make_float4(my_d, my_d, my_d, my_d);
-              if (KEYS) y = *reinterpret_cast<const float4*>(Dc + 32 * c + e);
+              if (KEYS) y = *reinterpret_cast<const float4*>(Dc + 16 * c + e);
               // (a pair that is not one stays zero, whatever its dP is)
-              const float* pe = p + 32 * c + e;
-              w[e >> 1] = pk2(pe[0] == 0.f ? 0.f : pe[0] * (dp[e] - y.x), pe[1] == 0.f ? 0.f : pe[1] * (dp[e + 1] - y.y));
-              w[(e >> 1) + 1] = pk2(pe[2] == 0.f ? 0.f : pe[2] * (dp[e + 2] - y.z), pe[3] == 0.f ? 0.f : pe[3] * (dp[e + 3] - y.w));
+              const float* pe = p + 16 * c + e;
+              const float ds[4] = {pe[0] == 0.f ? 0.f : pe[0] * (dp[e] - y.x), pe[1] == 0.f ? 0.f : pe[1] * (dp[e + 1] - y.y),
+                                   pe[2] == 0.f ? 0.f : pe[2] * (dp[e + 2] - y.z), pe[3] == 0.f ? 0.f : pe[3] * (dp[e + 3] - y.w)};
+              if (!KEYS) sum += (ds[0] + ds[1]) + (ds[2] + ds[3]);
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                const uint32_t x2 = pk2(ds[2 * h], ds[2 * h + 1]);
+                w[(e >> 1) + h] = x2;
+                if (!KEYS) {
+                  const float2 hi = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x2));
+                  rest[(e >> 1) + h] = pk2(ds[2 * h] - hi.x, ds[2 * h + 1] - hi.y);
+                }
+              }
             }
           } else {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) w[e] = 0u;
+            for (int e = 0; e < 8; ++e) w[e] = rest[e] = 0u;
           }
-          tmem_st16((KEYS ? tDP : tS) + 16 * c, w);  // (keys: over columns that have been read)
+          tmem_st8((KEYS ? tDP : tS) + 8 * c, w);  // (keys: over columns that have been read)
+          if (!KEYS) tmem_st8(tS + 32 + 8 * c, rest);
         }
         tmem_st_wait();
         tc_fence_before();
@@ -594,6 +609,18 @@ __global__ void __launch_bounds__(THREADS, 1) window_bwd_tc_kernel(const __grid_
         if (lane == 0) mbar_arrive(&ds_full[g & 1]);
       }
       if (!ok) break;
+      if (!KEYS) {
+        // D of the rounded output is off by what the row's dS add up to (with sum P dP for D they add up to 0)
+        if (x.n_steps > 0) {
+          stat[1][half][row] = sum;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sum_full);
+          ok = mbar_wait_warp(&sum_full, ni & 1, &abort_sh, a.err);
+          if (!ok) break;
+          my_d += stat[1][0][row] + stat[1][1][row];
+        }
+        if (half == 0 && r < a.seq) a.D[((int64_t)x.b * a.n_heads + x.head) * a.seq + r] = my_d;
+      }
       // ---- gradients
       ahead(id + gridDim.x, slot ^ 1);
       if (x.n_steps > 0) {
