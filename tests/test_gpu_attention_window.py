@@ -210,3 +210,30 @@ def test_lengths_out_of_range_are_reported():
     R.ra_attention_window_forward(case.a)
     torch.cuda.synchronize()
     assert case.err.item() == R.RA_DEV_BOUNDS and (case.out[0] == 0).all()
+
+
+@pytest.mark.parametrize("dtype,dh", DIMS)
+@pytest.mark.parametrize("kv", [4, 2, 1])
+def test_more_blocks_than_the_gpu_holds(dtype, dh, kv):
+    """Several blocks a CTA, one after the other, among them blocks of sequences that have ended."""
+    lens = [(7 * i * i + 13 * i) % 301 for i in range(36)] + [0, 0, 300, 1]
+    Case(dtype, 300, lens, 4, kv, dh, 70, 2).check()
+
+
+@pytest.mark.parametrize("dtype,dh", DIMS)
+@pytest.mark.parametrize("sinks", [3, 200])
+def test_long_with_few_sinks(dtype, dh, sinks):
+    """The first keys are seen from 40 blocks of queries, the others from two or three."""
+    Case(dtype, 5000, [5000], 2, 1, dh, 100, sinks).check()
+
+
+@pytest.mark.parametrize("dtype,dh", DIMS)
+def test_lengths_out_of_range_in_the_backward(dtype, dh):
+    case = Case(dtype, 200, [200, 60], 2, 2, dh, 30, 1, poison=False)
+    case.lens.copy_(torch.tensor([-4, 1000], dtype=torch.int32))
+    R.ra_attention_window_forward(case.a)
+    R.ra_attention_window_backward(case.a)
+    torch.cuda.synchronize()
+    assert case.err.item() == R.RA_DEV_BOUNDS
+    for t in (case.out, case.dq, case.dk, case.dv):
+        assert (t[0] == 0).all() and torch.isfinite(t[1].float()).all() and (t[1] != 7).any()
