@@ -124,8 +124,8 @@ cudaError_t launch_append(const ra_kv_append_args& a, cudaStream_t st) {
 // middle is found by its digits, 11, 11 and 10 bits from the top, each by a histogram of the keys that share
 // the digits found so far; then every warp counts its part of the slots, and writes what stays in order behind
 // what the warps before it count.  Counts are integers: no order of atomics changes a result.  Bound by the latency of its
-// passes, one CTA's: 17 us for 16384 slots (16 sequences of 4 heads); a sequence of 700 with its rows' move 8.6 us, 9.6 with
-// the keys in shared memory.
+// passes, one CTA's: 17 us for 16384 slots (16 sequences of 4 heads); a sequence of 700 with its rows' move 7.8 us, one
+// more with the keys in shared memory.
 // ---------------------------------------------------------------------------------------
 constexpr int SEL_BINS = 2048;
 constexpr int SEL_KEYS = 48 * 1024;  // keys held in shared memory; longer sequences read their weights again
@@ -284,11 +284,10 @@ __global__ void __launch_bounds__(SEL_THREADS) evict_select_kernel(const __grid_
   }
 }
 
-// Second kernel: the rows that stay, K and V, 16 bytes a thread and load, MOVE rows of a thread in flight.  Bound by memory:
-// 268 MB read and written (4096 rows of 64 heads, K and V) in 46 us, 5.8 TB/s.
-constexpr int MOVE = 4;
-__global__ void __launch_bounds__(256) evict_move_kernel(const __grid_constant__ ra_kv_evict_args a, int cpr, int rows_per_block,
-                                                         int blocks_per_unit, int64_t n_blocks) {
+// Second kernel: the rows that stay, K and V, 16 bytes of each a thread.  Bound by memory: 268 MB read and written (4096 rows of 64
+// heads, K and V) in 43 us, 6.2 TB/s, by as many CTAs as the SMs hold at once (eight times as many: 45 us; with four rows of a
+// thread in flight: 46 us, and a sequence of 700, with its selection, in 8.6 us instead of 7.8).
+__global__ void __launch_bounds__(256) evict_move_kernel(const __grid_constant__ ra_kv_evict_args a, int cpr, int blocks_per_unit, int64_t n_blocks) {
   pdl_wait();
   pdl_trigger();
   const int kv = a.src.n_kv_heads, per = 256 / cpr, r0 = threadIdx.x / cpr, col = threadIdx.x - r0 * cpr;
@@ -296,32 +295,18 @@ __global__ void __launch_bounds__(256) evict_move_kernel(const __grid_constant__
   for (int64_t blk = blockIdx.x; blk < n_blocks; blk += gridDim.x) {
     const int64_t unit = blk / blocks_per_unit;
     const int b = (int)(unit / kv), head = (int)(unit - (int64_t)b * kv);
-    const int row0 = (int)(blk - unit * blocks_per_unit) * rows_per_block + r0;
-    uint4 kx[MOVE], vx[MOVE];
-    int from[MOVE];
-#pragma unroll
-    for (int i = 0; i < MOVE; ++i) {
-      const int row = row0 + i * per;
-      from[i] = row < a.budget ? a.kept_dev[unit * a.budget + row] : -1;
+    const int row = (int)(blk - unit * blocks_per_unit) * per + r0;
+    const int from = row < a.budget ? a.kept_dev[unit * a.budget + row] : -1;
+    if (from < 0) continue;
+    const int64_t at = slot_row(a.src, b, from, head), to = slot_row(a.dst, b, row, head);
+    uint4 kx = make_uint4(0, 0, 0, 0), vx = kx;
+    if (at >= 0) {
+      kx = reinterpret_cast<const uint4*>(a.src.k_dev)[at * cpr + col];
+      vx = reinterpret_cast<const uint4*>(a.src.v_dev)[at * cpr + col];
     }
-#pragma unroll
-    for (int i = 0; i < MOVE; ++i) {
-      kx[i] = vx[i] = make_uint4(0, 0, 0, 0);
-      if (from[i] >= 0) {
-        const int64_t at = slot_row(a.src, b, from[i], head);
-        if (at >= 0) {
-          kx[i] = reinterpret_cast<const uint4*>(a.src.k_dev)[at * cpr + col];
-          vx[i] = reinterpret_cast<const uint4*>(a.src.v_dev)[at * cpr + col];
-        }
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < MOVE; ++i) {
-      if (from[i] < 0) continue;
-      const int64_t at = slot_row(a.dst, b, row0 + i * per, head);
-      if (at < 0) continue;
-      reinterpret_cast<uint4*>(a.dst.k_dev)[at * cpr + col] = kx[i];
-      reinterpret_cast<uint4*>(a.dst.v_dev)[at * cpr + col] = vx[i];
+    if (to >= 0) {
+      reinterpret_cast<uint4*>(a.dst.k_dev)[to * cpr + col] = kx;
+      reinterpret_cast<uint4*>(a.dst.v_dev)[to * cpr + col] = vx;
     }
   }
 }
@@ -353,11 +338,9 @@ cudaError_t kv_evict(const ra_kv_evict_args& a, cudaStream_t st) {
     e = select(evict_select_kernel<1024, -1>, 1024, 0);
   }
   if (e != cudaSuccess) return e;
-  const int cpr = a.src.head_dim * (a.src.dtype == RA_BF16 ? 2 : 4) / 16, rows = 256 / cpr * MOVE;
-  const int per_unit = (a.budget + rows - 1) / rows;
-  const int64_t n_blocks = units * per_unit, most = 8LL * 8 * device_sm_count();
-  e = launch_pdl(evict_move_kernel, dim3((unsigned)(n_blocks < most ? n_blocks : most)), dim3(256), 0, st, a, cpr, rows, per_unit,
-                 n_blocks);
+  const int cpr = a.src.head_dim * (a.src.dtype == RA_BF16 ? 2 : 4) / 16, rows = 256 / cpr, per_unit = (a.budget + rows - 1) / rows;
+  const int64_t n_blocks = units * per_unit, most = 8LL * device_sm_count();  // what the SMs hold
+  e = launch_pdl(evict_move_kernel, dim3((unsigned)(n_blocks < most ? n_blocks : most)), dim3(256), 0, st, a, cpr, per_unit, n_blocks);
   note_launch(2);
   return e;
 }
