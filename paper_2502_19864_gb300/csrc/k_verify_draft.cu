@@ -9,7 +9,7 @@
 // Of all the probabilities one row of p, one of q and the noise are read, and two values of every drafted place.
 // Bound by these reads where the batch is large and by latency where it is small: a sequence's row is cut over
 // several CTAs so that the batch fills the SMs once; each finds n for itself, and the last of them to finish (a
-// counter) writes the answer and leaves the workspace zero.  64 bf16 sequences of 50001 words and 8 drafts: 9.7 us;
+// counter) writes the answer and leaves the workspace zero.  64 bf16 sequences of 50001 words and 8 drafts: 9.9 us;
 // one fp32 sequence of 32000 and 4 drafts: 4.2 us.
 #include "common.cuh"
 #include "operators.h"
@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(VT, 8) verify_draft_kernel(const __grid_consta
 size_t verify_draft_workspace(const ra_verify_draft_args& a) { return (size_t)a.batch * sizeof(VerifySlot); }
 
 cudaError_t verify_draft(const ra_verify_draft_args& a, cudaStream_t st) {
-  // the SMs filled once, with eight small CTAs each (64 rows of 50001: three of 512 threads 10.7 us, four of 256 10.0, these 9.7; a
+  // the SMs filled once, with eight small CTAs each (64 rows of 50001: three of 512 threads 10.7 us, four of 256 10.0, these 9.9; a
   // second round of a few CTAs 13.6), none with fewer than four tokens a thread
   const int want = 8 * device_sm_count() / a.batch, most = (a.vocab + 4 * VT - 1) / (4 * VT);
   int parts = want < 1 ? 1 : want < most ? want : most;
