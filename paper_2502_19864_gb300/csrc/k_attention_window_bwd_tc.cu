@@ -7,7 +7,8 @@
 //            and leaves it for
 //   keys     a CTA holds K_j, V_j and streams the query blocks that see the rows, head by head of the group: S^T, dP^T,
 //            dV += P^T dO_i, dK += dS^T Q_i.
-// The scores are computed in both: seven products a pair of blocks where atomics would do with five.
+// The scores are computed in both, and dQ in two terms: eight products a pair of blocks where atomics and one term would do with
+// five.
 // Eleven warps: eight of arithmetic (a thread a row of the held block and half of the columns), two that issue products, one
 // that loads by TMA.  P (in fp32, in registers) and dS are the owner's of the row; as bf16 they go back to TMEM, over the
 // values they came from, and are the A operand of the next product there.  A warp that issues has a place in TMEM and all that
@@ -21,7 +22,7 @@
 // are computed while gradients leave.  Steps are masked by bits, and 32 columns that no row of a warp sees are left out: of a
 // window of 256 two blocks of three are masked.  8 x 1024 tokens, 16 heads of 128, window 256, 4 sinks: 65 us the queries, 76 the
 // keys (a CTA a block, one warp of products, a compare a column, dS in one term: 94 and 109); what it reads and writes takes 30
-// us each.  2 x 4096 tokens without a window: 503 us, 957 TFLOP/s over seven products.
+// us each.  2 x 4096 tokens without a window: 503 us, 1093 TFLOP/s over eight products.
 // The first key blocks may hold sinks, which every later query sees: where that makes them much longer than a block of the
 // window, several CTAs share such a block's queries and a last kernel adds their fp32 parts in order.
 // Rows past a sequence's end are set to zero in operands that a product sums over.
