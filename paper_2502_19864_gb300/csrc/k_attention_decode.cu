@@ -10,7 +10,9 @@
 // the tiles in turn, each with its own running maximum m, sum l and outputs; nothing but the end of a (sequence, head)
 // makes them wait for one another.  There the CTA adds them up; where its run covers a part of the head's tiles only,
 // (m, l, o) go to the workspace, and the last CTA to leave its part (a counter; the order of the sum is the parts', not
-// theirs) joins them.
+// theirs) joins them.  The counter is that of the CTA with the head's first tile: a head that is cut ends the run it starts
+// in, so that a CTA starts one at most, and the counters, all that has to be zero between calls, have their place whatever
+// the call's shape is.
 //   bf16: the products are mma.sync m16n8k16: sixteen rows take the tensor instruction of one, and the rate asked of
 //         it, 16 flops a byte of K and V, is a tenth of what it gives, so nothing is won by tcgen05's 128 rows.
 //   f32:  FFMA on packed pairs of rows, for the rows that there are (4, 8 or 16).  Shared memory paces it: 128 bytes a cycle
@@ -43,7 +45,7 @@ struct DecodeArgs {
   const float* w_in;
   float* w_out;
   int64_t w_stride;
-  unsigned* done;                // [batch, kv heads, groups]: CTAs that have left their part; zero between calls
+  unsigned* done;                // [grid]: CTAs that have left their part of the unit that starts in CTA i; zero between calls
   float* part_o;                 // [2 grid][rows of a unit][head dim]
   float2* part_ml;               // [2 grid][rows of a unit]
   float* lse2;                   // [batch, kv heads, R] (powers of two), where weights are wanted
@@ -862,7 +864,7 @@ __global__ void __launch_bounds__(Plan<T, DHT, WM, RM>::THREADS, 1) decode_kerne
       const int c0 = deal.owner(first);
       if (tid == 0) {
         const int c1 = deal.owner(first + cur.tiles - 1);
-        unsigned* count = a.done + (int64_t)cur.b * (a.c.n_kv_heads * a.groups) + cur.u;
+        unsigned* count = a.done + c0;
         __threadfence();  // (of all threads' parts: the barrier came before)
         const unsigned before = atomicAdd(count, 1u);
         joins = before == (unsigned)(c1 - c0) ? c1 - c0 + 1 : 0;
@@ -1058,7 +1060,7 @@ DecodeLayout layout_of(const ra_attention_decode_args& p) {
     at += (n + 255) / 256 * 256;
     return o;
   };
-  L.done = take((size_t)units * 4);
+  L.done = take((size_t)L.grid * 4);
   L.ml = take((size_t)2 * L.grid * L.rows * 8);
   L.o = take((size_t)2 * L.grid * L.rows * L.dht * 4);
   L.lse2 = L.scores = 0;
