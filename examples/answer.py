@@ -22,6 +22,9 @@ BF16 = torch.bfloat16
 
 
 def _workspace(n):
+    """`n` bytes, as a size function gave them for the whole argument block; it gives 0 for one that the call would refuse."""
+    if n == 0:
+        raise ValueError("the argument block is refused")
     return torch.zeros(max(n, 256), dtype=torch.uint8, device="cuda")
 
 
@@ -216,7 +219,7 @@ def answer(model, draft, prompt, tokens, n_draft=4, budget=128, limit=192, seed=
     last = big.step(prompt, prompt=True)[:, -1].softmax(-1).multinomial(1, generator=g)
     small.step(prompt, prompt=True)
     answers = [[int(t)] for t in last[:, 0]]
-    ws = _workspace(R.ra_verify_draft_workspace_bytes(R.ra_verify_draft_args(batch=B, n_draft=n_draft, vocab=V, dtype=R.RA_F32)))
+    ws = None
     accepted = torch.empty(B, dtype=torch.int32, device="cuda")
     out = torch.empty(B, n_draft + 1, dtype=torch.int32, device="cuda")
     stood = rounds = evictions = 0
@@ -237,11 +240,14 @@ def answer(model, draft, prompt, tokens, n_draft=4, budget=128, limit=192, seed=
         drafted = proposed.to(torch.int32).contiguous()
         uniform = torch.rand(B, n_draft, device="cuda", generator=g)
         noise = torch.empty(B, V, device="cuda").exponential_(generator=g).clamp_min_(1e-30)
-        R.ra_verify_draft(R.ra_verify_draft_args(
+        args = R.ra_verify_draft_args(
             target_dev=p.data_ptr(), target_stride=V, draft_dev=q.data_ptr(), draft_stride=V, tokens_dev=drafted.data_ptr(),
             uniform_dev=uniform.data_ptr(), noise_dev=noise.data_ptr(), accepted_dev=accepted.data_ptr(),
-            out_tokens_dev=out.data_ptr(), workspace_dev=ws.data_ptr(), workspace_bytes=ws.numel(), batch=B,
-            n_draft=n_draft, vocab=V, dtype=R.RA_F32), stream)
+            out_tokens_dev=out.data_ptr(), batch=B, n_draft=n_draft, vocab=V, dtype=R.RA_F32)
+        if ws is None:  # (the batch is the same every round)
+            ws = _workspace(R.ra_verify_draft_workspace_bytes(args))
+        args.workspace_dev, args.workspace_bytes = ws.data_ptr(), ws.numel()
+        R.ra_verify_draft(args, stream)
         big.back(n_draft - accepted)
         small.back(n_draft - accepted)
         last = out.gather(1, accepted[:, None].long()).long()

@@ -415,9 +415,10 @@ size_t ra_adapter_backward_noalloc_capacity(void);
  *     zero and log-sum-exp -inf.  scale is positive and finite (RA_ERR_ARG).  A key or value that is not finite
  *     reaches the tokens that see it; it may also reach tokens of its own sequence that do not.
  *   - A workspace is caller-owned, 256-byte aligned, at least the bytes that the call's _workspace_bytes
- *     gives for the same argument block, and zero-filled once before its first use: calls leave zero what
- *     they need to find zero.  Calls that may run at the same time need different workspaces.  RA_ERR_NOMEM
- *     for one that is too small.
+ *     gives for the same argument block (all of it but the workspace filled in: for a block that the call would
+ *     refuse it gives 0), and zero-filled once before its first use: calls leave zero what they need to find
+ *     zero.  Calls that may run at the same time need different workspaces.  RA_ERR_NOMEM for one that is too
+ *     small.
  *   - err_dev (nullable): a device word into which kernels or RA_DEV_BOUNDS where an index that they read on
  *     the device is out of range (a page of the table, a length, a position), and RA_DEV_TIMEOUT where a
  *     bounded wait ran out.  Such an index is never followed: a length is clamped to [0, capacity], tokens of

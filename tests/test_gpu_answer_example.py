@@ -47,3 +47,10 @@ def test_tuning_learns_and_answers(ex):
     right = sum(a == b for row, w in zip(answers, want) for a, b in zip(row, w)) / 450
     assert all(len(a) == 150 and all(0 <= t < m.V for t in a) for a in answers)
     assert right > 0.5
+
+
+def test_many_prompts(ex):
+    """More sequences than the least workspace of the verification has room for."""
+    m = ex.Decoder(1, seed=4)
+    answers, _, _ = ex.answer(m, m, ex.text(18, 40, m.V, seed=6), 8)
+    assert len(answers) == 18 and all(len(a) == 8 and all(0 <= t < m.V for t in a) for a in answers)
