@@ -210,7 +210,8 @@ class Session:
 @torch.no_grad()
 def answer(model, draft, prompt, tokens, n_draft=4, budget=128, limit=192, seed=0):
     """`tokens` more tokens of each sequence, sampled as `model` would, with `draft`'s proposals; how many of those stood,
-    and the number of evictions."""
+    and the number of evictions.  A sequence that has all of its tokens waits for the others: what a round puts into its
+    caches is taken back, so that they hold no more than its own answer."""
     B, V, stream = prompt.shape[0], model.V, torch.cuda.current_stream()
     g = torch.Generator("cuda").manual_seed(seed)
     length = prompt.shape[1] + tokens + n_draft + 1
@@ -222,11 +223,12 @@ def answer(model, draft, prompt, tokens, n_draft=4, budget=128, limit=192, seed=
     ws = None
     accepted = torch.empty(B, dtype=torch.int32, device="cuda")
     out = torch.empty(B, n_draft + 1, dtype=torch.int32, device="cuda")
-    stood = rounds = evictions = 0
+    stood = drafts = evictions = 0
     while min(map(len, answers)) < tokens:
         if int(big.lens.max()) > limit:
             big.evict(budget, recent=budget // 4)
             evictions += 1
+        live = [len(a) < tokens for a in answers]
         # the draft's tokens; its last step puts the last of them into its cache
         t, proposed, q = last, [], []
         for i in range(n_draft + 1):
@@ -248,17 +250,20 @@ def answer(model, draft, prompt, tokens, n_draft=4, budget=128, limit=192, seed=
             ws = _workspace(R.ra_verify_draft_workspace_bytes(args))
         args.workspace_dev, args.workspace_bytes = ws.data_ptr(), ws.numel()
         R.ra_verify_draft(args, stream)
-        big.back(n_draft - accepted)
-        small.back(n_draft - accepted)
-        last = out.gather(1, accepted[:, None].long()).long()
+        on = torch.tensor(live, device="cuda")
+        gone = torch.where(on, n_draft - accepted, n_draft + 1)
+        big.back(gone)
+        small.back(gone)
+        last = torch.where(on[:, None], out.gather(1, accepted[:, None].long()).long(), last)
         for b, (row, n) in enumerate(zip(out.tolist(), accepted.tolist())):
-            answers[b] += row[:n + 1]
-            stood += n
-        rounds += 1
+            if live[b]:
+                answers[b] += row[:n + 1]
+                stood += n
+                drafts += n_draft
     for m in (model, draft):
         if int(m.err):
             raise RuntimeError("device error word %d" % int(m.err))
-    return [a[:tokens] for a in answers], stood / (rounds * B * n_draft), evictions
+    return [a[:tokens] for a in answers], stood / max(drafts, 1), evictions
 
 
 def tune(model, tokens, steps, lr=2e-3):

@@ -54,3 +54,11 @@ def test_many_prompts(ex):
     m = ex.Decoder(1, seed=4)
     answers, _, _ = ex.answer(m, m, ex.text(18, 40, m.V, seed=6), 8)
     assert len(answers) == 18 and all(len(a) == 8 and all(0 <= t < m.V for t in a) for a in answers)
+
+
+def test_sequences_that_end_early(ex):
+    """Drafts that often fall: some sequences have all their tokens many rounds before others, and wait."""
+    m, draft = ex.Decoder(1, seed=4), ex.Decoder(1, seed=9)
+    answers, stood, _ = ex.answer(m, draft, ex.text(12, 40, m.V, seed=6), 207)
+    assert all(len(a) == 207 and all(0 <= t < m.V for t in a) for a in answers)
+    assert 0 < stood < 1
