@@ -417,8 +417,9 @@ size_t ra_adapter_backward_noalloc_capacity(void);
  *   - A workspace is caller-owned, 256-byte aligned, at least the bytes that the call's _workspace_bytes
  *     gives for the same argument block (all of it but the workspace filled in: for a block that the call would
  *     refuse it gives 0), and zero-filled once before its first use: calls leave zero what they need to find
- *     zero.  Calls that may run at the same time need different workspaces.  RA_ERR_NOMEM for one that is too
- *     small.
+ *     zero, so that one may serve any of these operators, in any shapes, one call after the other.  Calls that
+ *     may run at the same time need different workspaces, and after RA_DEV_TIMEOUT one has to be zero-filled
+ *     again.  RA_ERR_NOMEM for one that is too small.
  *   - err_dev (nullable): a device word into which kernels or RA_DEV_BOUNDS where an index that they read on
  *     the device is out of range (a page of the table, a length, a position), and RA_DEV_TIMEOUT where a
  *     bounded wait ran out.  Such an index is never followed: a length is clamped to [0, capacity], tokens of

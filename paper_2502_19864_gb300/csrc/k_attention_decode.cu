@@ -1035,7 +1035,7 @@ __global__ void __launch_bounds__(256) decode_weights_kernel(const __grid_consta
 struct DecodeLayout {
   int rows, groups, dht, grid, R, join;
   int64_t x_stride;
-  size_t done, ml, o, lse2, scores, bytes;
+  size_t ml, o, lse2, scores, bytes;
 };
 DecodeLayout layout_of(const ra_attention_decode_args& p) {
   DecodeLayout L;
@@ -1048,19 +1048,19 @@ DecodeLayout layout_of(const ra_attention_decode_args& p) {
   L.rows = !b16 ? (L.R <= 4 ? 4 : L.R <= 8 ? 8 : 16) : L.R <= 16 || L.dht == 256 ? 16 : L.R <= 32 ? 32 : 64;
   L.groups = (L.R + L.rows - 1) / L.rows;
   L.grid = device_sm_count();
+  if (L.grid > WS_COUNTERS) L.grid = WS_COUNTERS;
   // A unit has about grid / units parts; the last CTA reads them all, alone on its SM (about 20 us a MB), while a kernel of
   // its own takes about 3 us and has the GPU
   const int64_t units = (int64_t)p.batch * p.cache.n_kv_heads * L.groups;
   const int64_t parts = units > 0 ? L.grid / units + 2 : 0;
   L.join = parts * (L.R < L.rows ? L.R : L.rows) * p.cache.head_dim * 4 <= 128 * 1024;
   L.x_stride = ((int64_t)call_max_len(p.cache, p.max_len) + 63) / 64 * 64;
-  size_t at = 0;
+  size_t at = WS_ZERO;
   auto take = [&](size_t n) {
     const size_t o = at;
     at += (n + 255) / 256 * 256;
     return o;
   };
-  L.done = take((size_t)L.grid * 4);
   L.ml = take((size_t)2 * L.grid * L.rows * 8);
   L.o = take((size_t)2 * L.grid * L.rows * L.dht * 4);
   L.lse2 = L.scores = 0;
@@ -1138,7 +1138,7 @@ cudaError_t attention_decode(const ra_attention_decode_args& p, cudaStream_t st)
   a.w_in = p.weights_in_dev;
   a.w_out = p.weights_out_dev;
   a.w_stride = p.weights_stride;
-  a.done = (unsigned*)(ws + L.done);
+  a.done = (unsigned*)ws;
   a.part_ml = (float2*)(ws + L.ml);
   a.part_o = (float*)(ws + L.o);
   a.lse2 = p.weights_out_dev ? (float*)(ws + L.lse2) : nullptr;

@@ -496,8 +496,8 @@ cudaError_t bwd_simt(const ra_attention_window_args& a, cudaStream_t st) {
   const int64_t gq = (int64_t)n_blk * a.batch * a.n_heads, gk = (int64_t)(n_blk - split + split * chunks) * a.batch * a.n_kv_heads;
   const int64_t d_ctas = ((int64_t)a.batch * a.seq * a.n_heads + 31) / 32;
   if (gq + gk > INT32_MAX || d_ctas > INT32_MAX) return cudaErrorNotSupported;
-  float* D = (float*)a.workspace_dev;
-  float* parts = (float*)((char*)a.workspace_dev + d_bytes(a));
+  float* D = (float*)((char*)a.workspace_dev + WS_ZERO);
+  float* parts = (float*)((char*)D + d_bytes(a));
   cudaError_t e = allow_smem(window_bwd_simt_kernel<DH>, Plan<DH>::BWD_BYTES);
   if (e == cudaSuccess) e = launch_pdl(window_d_simt_kernel, dim3((unsigned)d_ctas), dim3(256), 0, st, a, D);
   if (e == cudaSuccess)
@@ -518,7 +518,7 @@ size_t attention_window_workspace(const ra_attention_window_args& a) {
   if (a.dtype == RA_BF16) return attention_window_workspace_tc(a);
   int split, chunks;
   split_of(a, split, chunks);
-  return d_bytes(a) + (size_t)a.batch * a.n_kv_heads * split * chunks * 2 * BH * dims_of(a) * 4;
+  return WS_ZERO + d_bytes(a) + (size_t)a.batch * a.n_kv_heads * split * chunks * 2 * BH * dims_of(a) * 4;
 }
 
 cudaError_t attention_window_fwd_simt(const ra_attention_window_args& a, cudaStream_t st) {

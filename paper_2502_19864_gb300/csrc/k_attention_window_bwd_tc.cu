@@ -742,8 +742,8 @@ cudaError_t launch(const ra_attention_window_args& p, cudaStream_t st) {
   WindowBwdArgs a;
   a.lens = p.lens_dev;
   a.lse = p.lse_dev;
-  a.D = (float*)p.workspace_dev;
-  a.part = (float*)((char*)p.workspace_dev + d_bytes(p));
+  a.D = (float*)((char*)p.workspace_dev + WS_ZERO);
+  a.part = (float*)((char*)a.D + d_bytes(p));
   a.err = p.err_dev;
   a.batch = p.batch;
   a.seq = p.seq;
@@ -798,7 +798,7 @@ cudaError_t launch(const ra_attention_window_args& p, cudaStream_t st) {
 size_t attention_window_workspace_tc(const ra_attention_window_args& p) {
   int split, chunks;
   split_of(p, split, chunks);
-  return d_bytes(p) + (size_t)p.batch * p.n_kv_heads * split * chunks * 2 * BR * p.head_dim * 4;
+  return WS_ZERO + d_bytes(p) + (size_t)p.batch * p.n_kv_heads * split * chunks * 2 * BR * p.head_dim * 4;
 }
 
 cudaError_t attention_window_bwd_tc(const ra_attention_window_args& a, cudaStream_t st) {

@@ -68,10 +68,11 @@ __device__ unsigned long long race(const T* __restrict__ p, const T* __restrict_
   return best;
 }
 
-struct VerifySlot {  // of a sequence, zero between calls
+struct VerifySlot {  // of a sequence that is cut, zero between calls
   unsigned long long best;
   unsigned done, pad;
 };
+static_assert(sizeof(VerifySlot) * WS_SLOTS == WS_ZERO - WS_SLOTS_AT, "the slots' place in a workspace");
 
 template <typename T>
 __global__ void __launch_bounds__(VT, 8) verify_draft_kernel(const __grid_constant__ ra_verify_draft_args a, int parts, int per_part) {
@@ -113,7 +114,7 @@ __global__ void __launch_bounds__(VT, 8) verify_draft_kernel(const __grid_consta
   const T* q = draft + (int64_t)n * a.draft_stride;
   unsigned long long best = n < nd ? race<T, true>(p, q, noise, v0, v1, e, true) : race<T, false>(p, q, noise, v0, v1, e, true);
   if (parts > 1) {
-    VerifySlot* slot = (VerifySlot*)a.workspace_dev + b;
+    VerifySlot* slot = (VerifySlot*)((char*)a.workspace_dev + WS_SLOTS_AT) + b;
     __shared__ bool last;
     __shared__ unsigned long long all;
     if (tid == 0) {
@@ -139,13 +140,14 @@ __global__ void __launch_bounds__(VT, 8) verify_draft_kernel(const __grid_consta
 
 }  // namespace
 
-size_t verify_draft_workspace(const ra_verify_draft_args& a) { return (size_t)a.batch * sizeof(VerifySlot); }
+size_t verify_draft_workspace(const ra_verify_draft_args&) { return WS_ZERO; }
 
 cudaError_t verify_draft(const ra_verify_draft_args& a, cudaStream_t st) {
   // the SMs filled once, with eight small CTAs each (64 rows of 50001: three of 512 threads 10.7 us, four of 256 10.0, these 9.9; a
-  // second round of a few CTAs 13.6), none with fewer than four tokens a thread
+  // second round of a few CTAs 13.6), none with fewer than four tokens a thread.  From 609 sequences on, with 152 SMs, none is
+  // cut; none may be beyond the slots
   const int want = 8 * device_sm_count() / a.batch, most = (a.vocab + 4 * VT - 1) / (4 * VT);
-  int parts = want < 1 ? 1 : want < most ? want : most;
+  int parts = want < 1 || a.batch > WS_SLOTS ? 1 : want < most ? want : most;
   const int per = (a.vocab + parts - 1) / parts;
   parts = (a.vocab + per - 1) / per;
   const dim3 grid((unsigned)parts * (unsigned)a.batch);

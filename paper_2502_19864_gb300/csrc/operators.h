@@ -15,6 +15,12 @@ inline int call_max_len(const ra_kv_cache& c, int max_len) {
   return (int)(max_len > 0 && max_len < cap ? max_len : cap);
 }
 
+// What calls need to find zero in a workspace, and leave zero, lies at its start, at a place and of a size that no shape and
+// no operator moves: the decode's join counters, one a CTA, then the verification's slots, one for each sequence that
+// is cut over several CTAs.  Everything else comes behind, and may hold anything.
+constexpr int WS_COUNTERS = 1024, WS_SLOTS = 768;
+constexpr size_t WS_SLOTS_AT = WS_COUNTERS * 4, WS_ZERO = WS_SLOTS_AT + WS_SLOTS * 16;  // 16 KB
+
 cudaError_t kv_append(const ra_kv_append_args& a, cudaStream_t st);
 cudaError_t kv_evict(const ra_kv_evict_args& a, cudaStream_t st);
 size_t attention_decode_workspace(const ra_attention_decode_args& a);
