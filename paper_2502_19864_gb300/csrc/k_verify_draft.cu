@@ -101,7 +101,10 @@ __global__ void __launch_bounds__(VT, 8) verify_draft_kernel(const __grid_consta
       if ((uint32_t)x < (uint32_t)V) {
         const float p = fmaxf(to_f(target[(int64_t)i * a.target_stride + x]), 0.f);
         const float q = fmaxf(to_f(draft[(int64_t)i * a.draft_stride + x]), 0.f);
-        falls = !(fmaf(a.uniform_dev[(int64_t)b * K + i], q, -p) < 0.f);  // the sign of the exact u q - p
+        // The sign of the exact u q - p.  Where that is not 0, u q is a multiple of 2^-197 if it is near a p (of 2^-149 at
+        // least): times 2^64 the difference is not lost below the least float
+        const float s = 0x1p64f;
+        falls = !(fmaf(a.uniform_dev[(int64_t)b * K + i] * s, q, -p * s) < 0.f);
       }
     }
     const uint32_t f = __ballot_sync(0xffffffffu, falls);

@@ -151,3 +151,25 @@ def test_the_samples_follow_the_target():
     R.ra_verify_draft(a)
     counts = torch.bincount(out[:, 0].long(), minlength=V).double()
     assert ((counts - B * p.double()).abs() <= 6 * (B * p.double()).sqrt()).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("uniform", [0.5, 0.9, 1 - 2.0 ** -24])
+def test_acceptance_of_the_smallest_probabilities(dtype, uniform):
+    """u q < p where u q - p is far below what 32 bits hold: equal probabilities stand for every u < 1."""
+    target, draft, tokens, u, e = model_like(5, 3, 200, 9)
+    least = 2.0 ** -149 if dtype == "f32" else 2.0 ** -133
+    for b, k in enumerate([1, 2, 3, 7, 100]):
+        target[b, :3].scatter_(1, tokens[b, :, None], k * least)
+        draft[b].scatter_(1, tokens[b, :, None], k * least)
+    u.fill_(uniform)
+    assert set(check(dtype, target, draft, tokens, u, e)) == {3}
+
+
+def test_acceptance_with_small_random_numbers():
+    """u q of two ordinary numbers just below and just above a p that 32 bits barely hold."""
+    target, draft, tokens, u, e = model_like(2, 1, 200, 10)
+    target[:, :1].scatter_(2, tokens[..., None], 2.0 ** -149)
+    draft.scatter_(2, tokens[..., None], 2.0 ** -10)
+    u[0], u[1] = 2.0 ** -140, 2.0 ** -139 * (1 + 2.0 ** -20)
+    assert check("f32", target, draft, tokens, u, e)[:2] == [1, 0]
