@@ -26,8 +26,8 @@ __device__ __forceinline__ unsigned long long packed(float score, uint32_t v) {
 __device__ __forceinline__ unsigned long long max64(unsigned long long a, unsigned long long b) { return a > b ? a : b; }
 
 // The largest r / e of tokens [v0, v1), from every thread.  Each thread has UN tokens on their way at once; `ready`: the
-// noise of the first UN is in e.  The quotient is computed where it can be the largest yet (the test before it is wide by
-// more than its own rounding).
+// noise of the first UN is in e.  The quotient is computed where it can be the largest yet: x / e rounds to more than
+// top only if x > top e, and then x is no less than the rounded top e, as rounding keeps the order and x is a float.
 template <typename T, bool DIFF>
 __device__ unsigned long long race(const T* __restrict__ p, const T* __restrict__ q, const float* __restrict__ noise,
                                    int v0, int v1, float (&e)[UN], bool ready) {
@@ -47,7 +47,7 @@ __device__ unsigned long long race(const T* __restrict__ p, const T* __restrict_
     for (int i = 0; i < UN; ++i) {
       float x = fmaxf(r[i], 0.f);  // (a NaN counts as 0)
       if (DIFF) x = fmaxf(x - fmaxf(d[i], 0.f), 0.f);
-      if (x > top * e[i] * 0.999999f) {
+      if (x > 0.f && x >= top * e[i]) {
         const float s = fmaxf(__fdiv_rn(x, e[i]), 0.f);
         if (s > top) {  // a thread's tokens rise: of equal ones the first stays
           top = s;

@@ -173,3 +173,21 @@ def test_acceptance_with_small_random_numbers():
     draft.scatter_(2, tokens[..., None], 2.0 ** -10)
     u[0], u[1] = 2.0 ** -140, 2.0 ** -139 * (1 + 2.0 ** -20)
     assert check("f32", target, draft, tokens, u, e)[:2] == [1, 0]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("drafted", [0, 1])
+def test_race_of_the_smallest_probabilities(dtype, drafted):
+    """Rows whose probabilities are all below what 32 bits hold to full precision, with noise that makes their quotients
+    ordinary numbers: later tokens win by 1 % to 80 % over earlier ones, at many distances."""
+    least = 2.0 ** -149 if dtype == "f32" else 2.0 ** -133
+    behind = [1, 32, 64, 128, 128, 128, 256, 512, 640, 1024, 2048]
+    B, V = len(behind), 3000
+    target, noise = torch.zeros(B, drafted + 1, V), torch.full((B, V), 1.0)
+    for b, far in enumerate(behind):
+        for i, share in enumerate((1.0, 0.99, 0.9, 0.55)[:4 - b % 3]):
+            v = 7 + b + i * far if i * far < 2900 else 2950 + b + i
+            target[b, :, v] = least
+            noise[b, v] = share * 2.0 ** -30
+    draft, tokens, u = torch.zeros(B, drafted, V), torch.zeros(B, drafted), torch.full((B, drafted), 0.5)
+    assert set(check(dtype, target, draft, tokens, u, noise)) == {0}
