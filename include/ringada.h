@@ -413,7 +413,8 @@ size_t ra_adapter_backward_noalloc_capacity(void);
  *   - Token i sees token j when j <= i and (window == 0 or i - j < window or j < sinks): the `window`
  *     newest tokens, itself among them, and the first `sinks` ones.  A query that sees nothing has output
  *     zero and log-sum-exp -inf.  scale is positive and finite (RA_ERR_ARG).  A key or value that is not finite
- *     reaches the tokens that see it; it may also reach tokens of its own sequence that do not.
+ *     reaches the tokens that see it; it may also reach tokens of its own sequence that do not.  Where a token's
+ *     scores are NaN, its output and its log-sum-exp are NaN.
  *   - A workspace is caller-owned, 256-byte aligned, at least the bytes that the call's _workspace_bytes
  *     gives for the same argument block (all of it but the workspace filled in: for a block that the call would
  *     refuse it gives 0), and zero-filled once before its first use: calls leave zero what they need to find

@@ -233,8 +233,9 @@ __global__ void __launch_bounds__(NT) window_fwd_simt_kernel(const __grid_consta
     l[i] = warp_sum(l[i]);
     f[i] = l[i] > 0.f ? 1.f / l[i] : l[i] == 0.f ? 0.f : l[i];
     const int qi = q0 + 4 * ty + i;
-    if (a.lse_dev && tx == 0 && qi < a.seq)
-      a.lse_dev[((int64_t)g.b * a.n_heads + g.head) * a.seq + qi] = m[i] == -INFINITY ? -INFINITY : (m[i] + log2f(l[i])) * 0.69314718055994531f;
+    if (a.lse_dev && tx == 0 && qi < a.seq)  // (the maximum of NaN scores stays -inf, their sum does not stay 0)
+      a.lse_dev[((int64_t)g.b * a.n_heads + g.head) * a.seq + qi] =
+          m[i] == -INFINITY && l[i] == 0.f ? -INFINITY : (m[i] + log2f(l[i])) * 0.69314718055994531f;
   }
   store_rows<DH>((float*)a.out_dev + tok0 * a.out_stride + g.head * dh, a.out_stride, o, f, q0, a.seq, dh, ty, tx);
 }

@@ -447,7 +447,7 @@ __global__ void __launch_bounds__(THREADS, 1) window_fwd_tc_kernel(const __grid_
       }
       if (!ok) break;
       const int len = I[4], q = I[5] + row, head = I[7], b = I[6];
-      const bool seen = q < len && m != -INFINITY;
+      const bool seen = q < len && !(m == -INFINITY && l == 0.f);  // (the maximum of NaN scores stays -inf, their sum does not stay 0)
       const float f = seen ? 1.f / l : 0.f;
       bf16* out = a.out + ((int64_t)b * a.seq + (q < a.seq ? q : 0)) * a.out_stride + head * DH;
 #pragma unroll 1

@@ -233,3 +233,36 @@ def test_infinite_scores_and_lowest_values():
     out = case.run()
     want = H.slots(case.v, case.table, 0, 40).double().mean(1)
     assert torch.allclose(out[0, 0].double(), want, rtol=0, atol=1e-5)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens", [[700, 90], [40, 20000]])
+def test_not_finite(dtype, lens):
+    """A NaN query, key or value: NaN in what sees it, output and log-sum-exp (a value: the output alone), through the parts
+    of long sequences too; other heads and sequences are as they are without it."""
+    for what in ("q", "k", "v"):
+        case, clean = (Case(dtype, lens, 1, 4, 2, 64, 16, weights=True) for _ in "ab")
+        clean.run()
+        for c in (case, clean):
+            c.w_out[:] = 0
+        clean.run()
+        if what == "q":
+            case.q[0, 0, 3, 5] = math.nan
+            hit = (3,)
+        else:
+            slot = lens[0] // 2
+            getattr(case, what)[case.table[0].long()[slot // 16], 1, slot % 16, 5] = math.nan
+            hit = (2, 3)
+        out = case.run()
+        want = clean.out[:, :256].reshape(out.shape)
+        for h in range(4):
+            if h not in hit:
+                assert torch.equal(out[0, :, h], want[0, :, h]) and torch.equal(case.lse[0, :, h], clean.lse[0, :, h])
+            elif what == "v":
+                assert out[0, :, h, 5].isnan().all() and torch.equal(case.lse[0, :, h], clean.lse[0, :, h])
+            else:
+                assert out[0, :, h].isnan().all() and case.lse[0, :, h].isnan().all()
+        assert torch.equal(out[1], want[1]) and torch.equal(case.lse[1], clean.lse[1]) and torch.equal(case.w_out[1], clean.w_out[1])
+        if what != "v":
+            assert case.w_out[0, 1, :lens[0]].isnan().all()
+        assert torch.equal(case.w_out[0, 0], clean.w_out[0, 0])

@@ -237,3 +237,46 @@ def test_lengths_out_of_range_in_the_backward(dtype, dh):
     assert case.err.item() == R.RA_DEV_BOUNDS
     for t in (case.out, case.dq, case.dk, case.dv):
         assert (t[0] == 0).all() and torch.isfinite(t[1].float()).all() and (t[1] != 7).any()
+
+
+@pytest.mark.parametrize("dtype,dh", DIMS + [("f32", 20)])
+@pytest.mark.parametrize("what", ["query", "key", "value", "infinite query", "infinite value"])
+def test_not_finite(dtype, dh, what):
+    """A query, or a key or value that is seen, that is not finite: NaN in the rows that see it (infinite where the formula
+    says so), in the log-sum-exp as in the output, and never the log-sum-exp of a row that sees nothing.  Rows of other
+    sequences, and what came before, are as they are without it."""
+    S, at = 300, 140
+    case, clean = (Case(dtype, S, [S, 200], 2, 2, dh, 100, 3, poison=False) for _ in "ab")
+    clean.run(backward=False)
+    x = {"query": case.q, "infinite query": case.q, "key": case.k, "value": case.v, "infinite value": case.v}[what]
+    bad = math.inf if "infinite" in what else math.nan
+    x[0, at, dh + 3] = bad  # of head 1
+    case.run(backward=False)
+    rows = [at] if "query" in what else list(range(at, at + 100))  # that see it
+    out, lse = case.out[0, :, dh:2 * dh].float(), case.lse[0, 1]
+    if "value" in what:
+        assert (out[rows, 3].isnan() | out[rows, 3].isinf()).all()
+        assert torch.equal(lse, clean.lse[0, 1])
+    elif what == "infinite query":  # products of either sign: +-inf, and inf - inf
+        assert out[rows].isnan().all() and not lse[rows].isneginf().any() and not lse[rows].isfinite().any()
+    else:
+        assert out[rows].isnan().all() and lse[rows].isnan().all()
+    before = slice(0, at - at % 128)  # (blocks of keys that it is not in)
+    for t, c in ((case.out, clean.out), (case.lse[:, :, None, :], clean.lse[:, :, None, :])):
+        assert torch.equal(t[1], c[1])
+    assert torch.equal(case.out[0, before], clean.out[0, before]) and torch.equal(case.out[0, :, :dh], clean.out[0, :, :dh])
+    assert torch.equal(case.lse[0, 0], clean.lse[0, 0]) and torch.equal(case.lse[0, 1, before], clean.lse[0, 1, before])
+
+
+@pytest.mark.parametrize("dtype,dh", DIMS)
+def test_every_key_not_finite(dtype, dh):
+    """All scores NaN from the first block on: NaN, not the zero and -inf of a row that sees nothing; gradients are NaN too."""
+    case = Case(dtype, 200, [200, 150], 2, 1, dh, 0, 0, poison=False)
+    case.k[0] = math.nan
+    case.run()
+    assert case.out[0].isnan().all() and case.lse[0].isnan().all()
+    for t in (case.dq, case.dk):
+        assert t[0].isnan().all()
+    assert case.out[1, :150].isfinite().all() and case.lse[1, :, :150].isfinite().all()
+    for t in (case.dq, case.dk, case.dv):
+        assert t[1].isfinite().all()
