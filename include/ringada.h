@@ -408,6 +408,8 @@ size_t ra_adapter_backward_noalloc_capacity(void);
  *   - A stride is in elements, from one token's first head to the next token's; the heads of a token are
  *     next to each other, head_dim values each.  16-byte aligned bases, and strides and head dims whose
  *     rows keep that alignment (8 values of bf16, 4 of float32), or RA_ERR_ARG / RA_ERR_SHAPE.
+ *   - RA_ERR_SHAPE, too, for sizes that the kernels' 32-bit counts do not hold: a cache of more than 2^31 - 4097
+ *     slots a sequence, a token of 2^31 values, more than 2^28 drafts or 2^30 words, 2^31 tokens a call.
  *   - Grouped heads: query head h reads key-value head h / (n_heads / n_kv_heads); n_heads is a multiple
  *     of n_kv_heads.
  *   - Token i sees token j when j <= i and (window == 0 or i - j < window or j < sinks): the `window`

@@ -7,7 +7,7 @@ using namespace ra;
 
 namespace {
 
-// the device check of the stand-alone calls: sm_103 alone has the kernels
+// what a launcher returns: cudaErrorNotSupported for a size that its kernels do not take
 ra_status launched(cudaError_t e) {
   return e == cudaSuccess ? RA_OK : e == cudaErrorNotSupported ? RA_ERR_SHAPE : RA_ERR_CUDA;
 }
@@ -19,6 +19,7 @@ bool good_scale(float s) { return s > 0.f && std::isfinite(s); }
 ra_status check_rows(const void* p, int64_t stride, int heads, int head_dim, int dtype) {
   if (!p || !aligned(p, 16)) return RA_ERR_ARG;
   if (stride < (int64_t)heads * head_dim || stride % vec(dtype)) return RA_ERR_SHAPE;
+  if ((int64_t)heads * head_dim > INT32_MAX) return RA_ERR_SHAPE;  // (a head's place in its token is counted in 32 bits)
   return RA_OK;
 }
 ra_status check_cache(const ra_kv_cache& c) {
@@ -26,7 +27,8 @@ ra_status check_cache(const ra_kv_cache& c) {
   if (c.dtype != RA_F32 && c.dtype != RA_BF16) return RA_ERR_ARG;
   if (c.n_pages < 1 || c.max_pages < 1 || c.page_size < 1 || c.n_kv_heads < 1) return RA_ERR_ARG;
   if (c.head_dim < 1 || c.head_dim > 256 || c.head_dim % vec(c.dtype)) return RA_ERR_SHAPE;
-  if (cache_capacity(c) > INT32_MAX) return RA_ERR_SHAPE;
+  // slots are counted in 32 bits, and shares of them run past a sequence's end (in the selection by up to 2016)
+  if (cache_capacity(c) > INT32_MAX - 4096) return RA_ERR_SHAPE;
   return RA_OK;
 }
 ra_status check_workspace(const void* p, size_t bytes, size_t need) {
@@ -67,6 +69,7 @@ ra_status check_decode(const ra_attention_decode_args& a) {
   if (a.weights_out_dev && a.weights_stride < call_max_len(c, a.max_len)) return RA_ERR_SHAPE;
   // rows of queries, and the tiles that they are cut into, are counted in 32 bits
   if ((int64_t)a.batch * a.n_new * a.n_heads > (1 << 28)) return RA_ERR_SHAPE;
+  if ((int64_t)a.n_new * a.n_heads * (c.head_dim / 4) > INT32_MAX - 1024) return RA_ERR_SHAPE;  // ... and a sequence's outputs, in fours
   return RA_OK;
 }
 ra_status check_evict(const ra_kv_evict_args& a) {
@@ -112,6 +115,7 @@ ra_status check_verify(const ra_verify_draft_args& a) {
       !a.out_tokens_dev)
     return RA_ERR_ARG;
   if (a.n_draft > 0 && (!a.draft_dev || !a.tokens_dev || !a.uniform_dev)) return RA_ERR_ARG;
+  if (a.n_draft > (1 << 28) || a.vocab > (1 << 30)) return RA_ERR_SHAPE;  // (both are walked in strides, in 32 bits)
   const size_t es = a.dtype == RA_BF16 ? 2 : 4;
   if (!aligned(a.target_dev, es) || !aligned(a.draft_dev, es)) return RA_ERR_ARG;
   if (a.target_stride < a.vocab || (a.n_draft > 0 && a.draft_stride < a.vocab)) return RA_ERR_SHAPE;

@@ -145,3 +145,23 @@ def test_null_blocks_and_workspaces_of_refused_ones():
     assert R.ra_attention_decode_workspace_bytes(decode()) > 0
     assert R.ra_attention_window_workspace_bytes(window(head_dim=96)) == 0
     assert R.ra_verify_draft_workspace_bytes(verify(vocab=0)) == 0
+
+
+BIG = (1 << 31) - 1
+WIDE = dict(head_dim=128, n_kv_heads=1 << 25)  # 2^32 values a token
+
+
+@pytest.mark.parametrize("call,args", [
+    (R.ra_kv_append, append(cache(max_pages=(1 << 27) - 1))),      # slots up to the last 32-bit one: blocks of them end behind it
+    (R.ra_attention_decode, decode(cache(max_pages=(1 << 27) - 1))),
+    (R.ra_kv_evict, evict(dst=cache(max_pages=(1 << 27) - 1), budget=BIG - 15, weights_out_stride=BIG)),
+    (R.ra_kv_evict, evict(src=cache(max_pages=(1 << 27) - 1), weights_stride=BIG)),
+    (R.ra_kv_append, append(cache(**WIDE), q_dev=None, q_out_dev=None, k_stride=1 << 32, v_stride=1 << 32)),
+    (R.ra_attention_decode, decode(cache(**WIDE), n_heads=1 << 25, q_stride=1 << 32, out_stride=1 << 32)),
+    (R.ra_attention_decode, decode(cache(head_dim=256), q_stride=1024, out_stride=1024, n_new=1 << 25)),  # 2^33 values to zero
+    (R.ra_attention_window_forward, window(n_heads=1 << 25, **WIDE, seq=1, q_stride=1 << 32, k_stride=1 << 32, v_stride=1 << 32,
+                                           out_stride=1 << 32)),
+    (R.ra_verify_draft, verify(n_draft=BIG)),
+    (R.ra_verify_draft, verify(vocab=BIG, target_stride=BIG, draft_stride=BIG))])
+def test_counts_that_32_bits_do_not_hold(call, args):
+    refused(call, args, SHAPE)
