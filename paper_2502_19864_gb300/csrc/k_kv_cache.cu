@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(256, 3) kv_append_kernel(const __grid_constant
 
 template <typename T, int VE>
 cudaError_t launch_append(const ra_kv_append_args& a, cudaStream_t st) {
-  const int rows = (a.q_dev ? a.n_heads : 0) + 2 * a.cache.n_kv_heads, chunks = a.cache.head_dim / 2 / VE;  // (at most 32 chunks)
+  const int rows = (a.q_dev ? a.n_heads : 0) + 2 * a.cache.n_kv_heads, chunks = a.cache.head_dim / 2 / VE;  // (at most 63 chunks: f32, head dim 252)
   int lanes = (rows + 3) / 4;  // four rows a thread, more where a token would not fit a block
   if (lanes * chunks > 256) lanes = 256 / chunks;
   const int per = 256 / (lanes * chunks);

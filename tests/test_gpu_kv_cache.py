@@ -223,3 +223,11 @@ def test_evict_reports_bad_pages():
     assert kept.tolist() == [3, 20, 40, 41] and err.item() == R.RA_DEV_BOUNDS
     assert torch.equal(dst[0][0, 0, 0], src[0][0, 0, 3]) and (dst[0][0, 0, 1] == 0).all()
     assert torch.equal(dst[1][0, 0, 2], src[1][2, 0, 8])
+
+
+@pytest.mark.parametrize("dtype,dh", [("f32", 4), ("f32", 12), ("f32", 20), ("f32", 252), ("bf16", 24), ("bf16", 248)])
+@pytest.mark.parametrize("heads,kv", [(1, 1), (40, 8)])
+def test_append_of_halves_that_no_wide_load_divides(dtype, dh, heads, kv):
+    """Head dims whose halves are cut into 2 (f32) or 4 (bf16) values a thread, up to 63 a row."""
+    for fused in (False, True):
+        test_append(dtype, 3, 5, heads, kv, dh, 16, True, fused)
