@@ -195,10 +195,10 @@ __global__ void __launch_bounds__(NTHR, DH == 64 ? 2 : 1) attn_bwd_tc_kernel(con
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   pdl_wait();
-  pdl_trigger();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  pdl_trigger();  // (TMEM is allocated: the next kernel's CTAs cannot come before this one)
   const uint32_t tmem = tmem_sh;
   const uint32_t trow = tmem + ((uint32_t)(32 * quad) << 16);  // this warp's TMEM lanes
   const int row = 32 * quad + lane;                             // block row of this thread
@@ -617,10 +617,10 @@ __global__ void __launch_bounds__(NTHR, 2) attn_fwd_blocks_tc_kernel(
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   pdl_wait();
-  pdl_trigger();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  pdl_trigger();  // (TMEM is allocated: the next kernel's CTAs cannot come before this one)
   const uint32_t tmem = tmem_sh;
   const uint32_t trow = tmem + ((uint32_t)(32 * quad) << 16);
   const int row = 32 * quad + lane, q = i * BR + row;

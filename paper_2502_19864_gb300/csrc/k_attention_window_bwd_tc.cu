@@ -223,10 +223,10 @@ __global__ void __launch_bounds__(THREADS, 1) window_bwd_tc_kernel(const __grid_
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   pdl_wait();
-  pdl_trigger();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  pdl_trigger();  // (TMEM is allocated: the next kernel's CTAs cannot come before this one)
   const uint32_t tmem = tmem_sh;
   // Every role counts its steps over all items (g): ring slots, buffers and the barriers' phases go by that.
 

@@ -155,10 +155,10 @@ __global__ void __launch_bounds__(THREADS, 1) window_fwd_tc_kernel(const __grid_
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   pdl_wait();
-  pdl_trigger();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  pdl_trigger();  // (TMEM is allocated: the next kernel's CTAs cannot come before this one)
   const uint32_t tmem = tmem_sh;
 
   if (warp == 10) {
