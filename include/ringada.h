@@ -417,6 +417,7 @@ size_t ra_adapter_backward_noalloc_capacity(void);
  *     zero and log-sum-exp -inf.  scale is positive and finite (RA_ERR_ARG).  A key or value that is not finite
  *     reaches the tokens that see it; it may also reach tokens of its own sequence that do not.  Where a token's
  *     scores are NaN, its output and its log-sum-exp are NaN.
+ *   - Outputs share no memory with inputs, but where a call says that they may.
  *   - A workspace is caller-owned, 256-byte aligned, at least the bytes that the call's _workspace_bytes
  *     gives for the same argument block (all of it but the workspace filled in: for a block that the call would
  *     refuse it gives 0), and zero-filled once before its first use: calls leave zero what they need to find
@@ -489,7 +490,8 @@ ra_status ra_attention_decode(const ra_attention_decode_args* args, ra_stream_t 
  * between, the budget - first - recent of the largest weight (of equal ones the lowest slots; a NaN counts as
  * larger than any number).  The kept tokens are copied in order to slots 0, 1, ... of the dst cache, whose
  * pages no src page of these sequences may be; kept[b, e, i] is the slot that slot i came from (-1 beyond
- * the new length), weights_out[b, e, i] its weight (0 up to budget), lens_out[b] = min(lens[b], budget).
+ * the new length), weights_out[b, e, i] its weight (0 up to budget), lens_out[b] = min(lens[b], budget)
+ * (lens_out may be lens).
  * RA_ERR_ARG for first + recent > budget; RA_ERR_SHAPE where src and dst differ in heads, head dim or type
  * or dst's table cannot hold budget tokens. */
 typedef struct {

@@ -148,13 +148,12 @@ __global__ void __launch_bounds__(SEL_THREADS) evict_select_kernel(const __grid_
   pdl_trigger();
   const int kv = a.src.n_kv_heads, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int64_t unit = blockIdx.x;
-  const int b = (int)(unit / kv), head = (int)(unit - (int64_t)b * kv);
+  const int b = (int)(unit / kv);
   const int n = clamp_len(a.lens_dev[b], max_len, a.src.err_dev);
   const float* w = a.weights_dev + unit * a.weights_stride;
   int32_t* kept = a.kept_dev + unit * a.budget;
   float* wout = a.weights_out_dev ? a.weights_out_dev + unit * a.weights_out_stride : nullptr;
   const int stay = n < a.budget ? n : a.budget;
-  if (head == 0 && tid == 0) a.lens_out_dev[b] = stay;
   for (int i = stay + tid; i < a.budget; i += SEL_THREADS) {
     kept[i] = -1;
     if (wout) wout[i] = 0.f;
@@ -286,13 +285,22 @@ __global__ void __launch_bounds__(SEL_THREADS) evict_select_kernel(const __grid_
 
 // Second kernel: the rows that stay, K and V, 16 bytes of each a thread.  Bound by memory: 268 MB read and written (4096 rows of 64
 // heads, K and V) in 43 us, 6.2 TB/s, by as many CTAs as the SMs hold at once (eight times as many: 45 us; with four rows of a
-// thread in flight: 46 us, and a sequence of 700, with its selection, in 8.6 us instead of 7.8).
-__global__ void __launch_bounds__(256) evict_move_kernel(const __grid_constant__ ra_kv_evict_args a, int cpr, int blocks_per_unit, int64_t n_blocks) {
+// thread in flight: 46 us, and a sequence of 700, with its selection, in 8.6 us instead of 7.8).  The last CTA writes the new
+// lengths, which may lie where the old ones do: all of the first kernel's threads have read those (in a CTA of the rows: 60.4 us
+// for the call above where this takes 59.2).
+__global__ void __launch_bounds__(256) evict_move_kernel(const __grid_constant__ ra_kv_evict_args a, int max_len, int cpr, int blocks_per_unit, int64_t n_blocks) {
   pdl_wait();
   pdl_trigger();
+  if (blockIdx.x == gridDim.x - 1) {
+    for (int b = threadIdx.x; b < a.batch; b += 256) {
+      const int n = clamp_len(a.lens_dev[b], max_len, a.src.err_dev);
+      a.lens_out_dev[b] = n < a.budget ? n : a.budget;
+    }
+    return;
+  }
   const int kv = a.src.n_kv_heads, per = 256 / cpr, r0 = threadIdx.x / cpr, col = threadIdx.x - r0 * cpr;
   if (r0 >= per) return;
-  for (int64_t blk = blockIdx.x; blk < n_blocks; blk += gridDim.x) {
+  for (int64_t blk = blockIdx.x; blk < n_blocks; blk += gridDim.x - 1) {
     const int64_t unit = blk / blocks_per_unit;
     const int b = (int)(unit / kv), head = (int)(unit - (int64_t)b * kv);
     const int row = (int)(blk - unit * blocks_per_unit) * per + r0;
@@ -340,7 +348,7 @@ cudaError_t kv_evict(const ra_kv_evict_args& a, cudaStream_t st) {
   if (e != cudaSuccess) return e;
   const int cpr = a.src.head_dim * (a.src.dtype == RA_BF16 ? 2 : 4) / 16, rows = 256 / cpr, per_unit = (a.budget + rows - 1) / rows;
   const int64_t n_blocks = units * per_unit, most = 8LL * device_sm_count();  // what the SMs hold
-  e = launch_pdl(evict_move_kernel, dim3((unsigned)(n_blocks < most ? n_blocks : most)), dim3(256), 0, st, a, cpr, per_unit, n_blocks);
+  e = launch_pdl(evict_move_kernel, dim3((unsigned)(n_blocks + 1 < most ? n_blocks + 1 : most)), dim3(256), 0, st, a, max_len, cpr, per_unit, n_blocks);
   note_launch(2);
   return e;
 }

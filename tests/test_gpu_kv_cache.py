@@ -231,3 +231,29 @@ def test_append_of_halves_that_no_wide_load_divides(dtype, dh, heads, kv):
     """Head dims whose halves are cut into 2 (f32) or 4 (bf16) values a thread, up to 63 a row."""
     for fused in (False, True):
         test_append(dtype, 3, 5, heads, kv, dh, 16, True, fused)
+
+
+def test_evict_with_lengths_in_place():
+    """lens_out may be lens: heads of a sequence whose turn comes after another head's still find its old length."""
+    B, kv, page, budget, n = 96, 48, 16, 64, 160
+    g = torch.Generator(device="cuda").manual_seed(3)
+    src = [torch.randn((10 * B, kv, page, 8), generator=g, device="cuda") for _ in "kv"]
+    dst = [torch.zeros((4 * B, kv, page, 8), device="cuda") for _ in "kv"]
+    table = torch.randperm(10 * B, generator=g, device="cuda").to(torch.int32).view(B, 10)
+    out_table = torch.randperm(4 * B, generator=g, device="cuda").to(torch.int32).view(B, 4)
+    w = heavy((B, kv, 8192), g)  # (a long stride, for the kernel of the most threads a CTA)
+    lens = torch.full((B,), n, dtype=torch.int32, device="cuda")
+    lens[5], lens[6] = 30, 64
+    kept = torch.full((B, kv, budget), 99, dtype=torch.int32, device="cuda")
+    other = torch.full_like(kept, 99)
+    new = torch.zeros_like(lens)
+    a = R.ra_kv_evict_args(src=H.cache(*src, table), dst=H.cache(*dst, out_table), lens_dev=lens.data_ptr(), weights_dev=w.data_ptr(),
+                           weights_stride=w.shape[2], lens_out_dev=new.data_ptr(), kept_dev=other.data_ptr(), batch=B, budget=budget,
+                           first=4, recent=20)
+    R.ra_kv_evict(a)
+    rows = [d.clone() for d in dst]
+    a.lens_out_dev, a.kept_dev = lens.data_ptr(), kept.data_ptr()
+    R.ra_kv_evict(a)
+    torch.cuda.synchronize()
+    assert torch.equal(lens, new) and lens.tolist() == [30 if b == 5 else 64 for b in range(B)]
+    assert torch.equal(kept, other) and torch.equal(dst[0], rows[0]) and torch.equal(dst[1], rows[1])
