@@ -418,6 +418,7 @@ size_t ra_adapter_backward_noalloc_capacity(void);
  *     reaches the tokens that see it; it may also reach tokens of its own sequence that do not.  Where a token's
  *     scores are NaN, its output and its log-sum-exp are NaN.
  *   - Outputs share no memory with inputs, but where a call says that they may.
+ *   - A batch of 0, or sequences of seq = 0 tokens, are RA_OK without work; their pointers may be null.
  *   - A workspace is caller-owned, 256-byte aligned, at least the bytes that the call's _workspace_bytes
  *     gives for the same argument block (all of it but the workspace filled in: for a block that the call would
  *     refuse it gives 0), and zero-filled once before its first use: calls leave zero what they need to find

@@ -109,6 +109,8 @@ ra_status check_window(const ra_attention_window_args& a, bool backward) {
   }
   return RA_OK;
 }
+// (of a negative size the check says what is wrong)
+bool no_tokens(const ra_attention_window_args& a) { return a.batch >= 0 && a.seq >= 0 && (a.batch == 0 || a.seq == 0); }
 ra_status check_verify(const ra_verify_draft_args& a) {
   if (a.dtype != RA_F32 && a.dtype != RA_BF16) return RA_ERR_ARG;
   if (a.batch < 0 || a.n_draft < 0 || a.vocab < 1 || !a.target_dev || !a.noise_dev || !a.accepted_dev ||
@@ -128,61 +130,64 @@ extern "C" {
 
 ra_status ra_kv_append(const ra_kv_append_args* args, ra_stream_t stream) {
   if (!args) return RA_ERR_ARG;
+  if (args->batch == 0) return RA_OK;
   TRY(check_append(*args));
   if (!tc_available()) return RA_ERR_UNSUPPORTED;
-  if (args->batch == 0) return RA_OK;
   return launched(kv_append(*args, (cudaStream_t)stream));
 }
 
 size_t ra_attention_decode_workspace_bytes(const ra_attention_decode_args* args) {
+  if (args && args->batch == 0) return WS_ZERO;
   return args && check_decode(*args) == RA_OK ? attention_decode_workspace(*args) : 0;
 }
 ra_status ra_attention_decode(const ra_attention_decode_args* args, ra_stream_t stream) {
   if (!args) return RA_ERR_ARG;
+  if (args->batch == 0) return RA_OK;
   TRY(check_decode(*args));
   TRY(check_workspace(args->workspace_dev, args->workspace_bytes, attention_decode_workspace(*args)));
   if (!tc_available()) return RA_ERR_UNSUPPORTED;
-  if (args->batch == 0) return RA_OK;
   return launched(attention_decode(*args, (cudaStream_t)stream));
 }
 
 ra_status ra_kv_evict(const ra_kv_evict_args* args, ra_stream_t stream) {
   if (!args) return RA_ERR_ARG;
+  if (args->batch == 0) return RA_OK;
   TRY(check_evict(*args));
   if (!tc_available()) return RA_ERR_UNSUPPORTED;
-  if (args->batch == 0) return RA_OK;
   return launched(kv_evict(*args, (cudaStream_t)stream));
 }
 
 size_t ra_attention_window_workspace_bytes(const ra_attention_window_args* args) {
+  if (args && no_tokens(*args)) return WS_ZERO;
   return args && check_window(*args, false) == RA_OK ? attention_window_workspace(*args) : 0;
 }
 ra_status ra_attention_window_forward(const ra_attention_window_args* args, ra_stream_t stream) {
   if (!args) return RA_ERR_ARG;
+  if (no_tokens(*args)) return RA_OK;
   TRY(check_window(*args, false));
   if (!tc_available()) return RA_ERR_UNSUPPORTED;
-  if (args->batch == 0 || args->seq == 0) return RA_OK;
   return launched(args->dtype == RA_BF16 ? attention_window_fwd_tc(*args, (cudaStream_t)stream)
                                          : attention_window_fwd_simt(*args, (cudaStream_t)stream));
 }
 ra_status ra_attention_window_backward(const ra_attention_window_args* args, ra_stream_t stream) {
   if (!args) return RA_ERR_ARG;
+  if (no_tokens(*args)) return RA_OK;
   TRY(check_window(*args, true));
   if (!tc_available()) return RA_ERR_UNSUPPORTED;
-  if (args->batch == 0 || args->seq == 0) return RA_OK;
   return launched(args->dtype == RA_BF16 ? attention_window_bwd_tc(*args, (cudaStream_t)stream)
                                          : attention_window_bwd_simt(*args, (cudaStream_t)stream));
 }
 
 size_t ra_verify_draft_workspace_bytes(const ra_verify_draft_args* args) {
+  if (args && args->batch == 0) return WS_ZERO;
   return args && check_verify(*args) == RA_OK ? verify_draft_workspace(*args) : 0;
 }
 ra_status ra_verify_draft(const ra_verify_draft_args* args, ra_stream_t stream) {
   if (!args) return RA_ERR_ARG;
+  if (args->batch == 0) return RA_OK;
   TRY(check_verify(*args));
   TRY(check_workspace(args->workspace_dev, args->workspace_bytes, verify_draft_workspace(*args)));
   if (!tc_available()) return RA_ERR_UNSUPPORTED;
-  if (args->batch == 0) return RA_OK;
   return launched(verify_draft(*args, (cudaStream_t)stream));
 }
 

@@ -165,3 +165,23 @@ WIDE = dict(head_dim=128, n_kv_heads=1 << 25)  # 2^32 values a token
     (R.ra_verify_draft, verify(vocab=BIG, target_stride=BIG, draft_stride=BIG))])
 def test_counts_that_32_bits_do_not_hold(call, args):
     refused(call, args, SHAPE)
+
+
+def test_no_sequences():
+    """A batch of none (or of sequences without tokens), whose tensors have no memory: nothing to do, and no error."""
+    cache0 = cache(k_dev=None, v_dev=None, block_table_dev=None)
+    nothing = dict(batch=0, lens_dev=None)
+    R.ra_kv_append(append(cache0, q_dev=None, k_dev=None, v_dev=None, q_out_dev=None, **nothing))
+    calls = [(R.ra_attention_decode, R.ra_attention_decode_workspace_bytes, decode(cache0, q_dev=None, out_dev=None, **nothing)),
+             (R.ra_kv_evict, None, evict(cache0, cache0, weights_dev=None, lens_out_dev=None, kept_dev=None, **nothing)),
+             (R.ra_verify_draft, R.ra_verify_draft_workspace_bytes, verify(batch=0, target_dev=None, draft_dev=None, tokens_dev=None,
+                                                                          uniform_dev=None, noise_dev=None, accepted_dev=None,
+                                                                          out_tokens_dev=None))]
+    empty = dict(q_dev=None, k_dev=None, v_dev=None, out_dev=None, lse_dev=None, dout_dev=None, dq_dev=None, dk_dev=None, dv_dev=None)
+    for a in (window(batch=0, **empty), window(seq=0, **empty)):
+        calls += [(R.ra_attention_window_forward, R.ra_attention_window_workspace_bytes, a),
+                  (R.ra_attention_window_backward, R.ra_attention_window_workspace_bytes, a)]
+    for call, size, a in calls:
+        call(a)
+        if size:
+            assert size(a) > 0  # (0 is that of a refused block)
