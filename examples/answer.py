@@ -193,6 +193,9 @@ class Session:
                 w.masked_fill_(gone, 0)
 
     def evict(self, budget, recent):
+        """Down to `budget` tokens a sequence.  (A prompt's windowed attention leaves no weights: its tokens have those that
+        the tokens after it gave them, and a prompt that is evicted at once keeps its first and newest tokens and, all
+        being equal, the lowest slots.)"""
         stream, lens = torch.cuda.current_stream(), torch.empty_like(self.lens)
         for i, pools in enumerate(self.pools):
             w = torch.zeros_like(self.weights[i])

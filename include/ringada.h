@@ -465,7 +465,8 @@ ra_status ra_kv_append(const ra_kv_append_args* args, ra_stream_t stream);
 
 /* Attention of the n_new newest tokens of each sequence (token t at slot lens[b] - n_new + t, already in the
  * cache) over its cached tokens: out = softmax(scale q k^T) v over the slots that it sees.  One token a
- * sequence is the ordinary step; several check drafted ones.
+ * sequence is the ordinary step; several check drafted ones.  The window counts slots: after an eviction, tokens
+ * that were kept, not those that the sequence has seen.
  * weights_out (nullable): weights_out[b, e, s] = weights_in[b, e, s] + the softmax weights that slot s got
  * from the new tokens through the query heads of key-value head e, for s < lens[b] (weights_in NULL: 0; it
  * may be weights_out); other slots are not touched.
@@ -493,6 +494,8 @@ ra_status ra_attention_decode(const ra_attention_decode_args* args, ra_stream_t 
  * pages no src page of these sequences may be; kept[b, e, i] is the slot that slot i came from (-1 beyond
  * the new length), weights_out[b, e, i] its weight (0 up to budget), lens_out[b] = min(lens[b], budget)
  * (lens_out may be lens).
+ * The weights are what ra_attention_decode has added up.  ra_attention_window_forward gives none: a prompt's tokens
+ * have the weights that the tokens decoded after it gave them, and none where none has been.
  * RA_ERR_ARG for first + recent > budget; RA_ERR_SHAPE where src and dst differ in heads, head dim or type
  * or dst's table cannot hold budget tokens. */
 typedef struct {
@@ -540,9 +543,9 @@ ra_status ra_attention_window_backward(const ra_attention_window_args* args, ra_
  * it and at all before it.  At the first that does not stand, n, the next token is
  * argmax_v max(target[b, n, v] - draft[b, n, v], 0) / noise[b, v], and target[b, n, v] / noise[b, v] where
  * all stand or that difference is nowhere positive; with noise exponentially distributed, a sample of the
- * normalised numerator.  Ties go to the lowest token; a NaN counts as 0.  accepted[b] = n; out_tokens[b] =
- * the n drafted tokens, the next one, then -1.  n_drafted (nullable): sequence b has n_drafted[b] <= n_draft
- * drafts.  A drafted token outside the vocabulary does not stand. */
+ * normalised numerator.  Ties go to the lowest token; a probability or a quotient that is NaN counts as 0.
+ * accepted[b] = n; out_tokens[b] = the n drafted tokens, the next one, then -1.  n_drafted (nullable): sequence
+ * b has n_drafted[b] <= n_draft drafts.  A drafted token outside the vocabulary does not stand. */
 typedef struct {
   const void* target_dev; int64_t target_stride; /* [batch, n_draft + 1] rows of vocab values */
   const void* draft_dev; int64_t draft_stride;   /* [batch, n_draft] rows */

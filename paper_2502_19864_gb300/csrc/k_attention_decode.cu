@@ -3,7 +3,8 @@
 //   o = sum_j p_j v_j, p = softmax(scale q K^T) over the slots that the token sees.
 //
 // The query rows of a key-value head are its group's heads times the new tokens (R rows, a few to a few dozen); K and
-// V are read once for all of them, 4 R head_dim flops for every 2 head_dim values: bound by memory.  The slots that
+// V are read once for up to 64 of them (bf16; 16 at head dims above 128) or 16 (f32), and again for the next as many, 4 R
+// head_dim flops for every 2 head_dim values: bound by memory where the rows are few.  The slots that
 // any row sees (all, or the sinks and the windows) are numbered 0, 1, ... and cut into tiles of TK; the tiles of all
 // sequences and heads, one after the other, are dealt to the CTAs in equal runs, whatever the lengths are.  Two warps of a
 // CTA look up pages and copy tiles, in turn, into a ring; the others (or groups of 2 or 4 that split more than sixteen rows) take
@@ -21,7 +22,8 @@
 //         for p V.  (With a lane a token, queries read by every lane: 2.4 times the reads, 224 us where this takes 175 for
 //         10 rows of 453 MB; tf32 products of operands split in two terms, sixteen rows always: 217 us for 671 MB.)
 // 16 bf16 sequences of up to 32768 tokens, 16 heads of 128 over 4: 107 us, 6.3 TB/s of the 6.8 that a copy has (125 us with
-// the weights for an eviction, which read the scores again); fp32, 10 rows: 6.1 TB/s.  One sequence of 1000 tokens: 10 us, the
+// the weights for an eviction, which read the scores again); fp32, 16 sequences of 16384 tokens, 4 heads of 128: 161 us with up to
+// four rows a head, 6.7 TB/s, 197 with eight, 5.5 TB/s.  One sequence of 1000 tokens: 10 us, the
 // latency of a launch, a page, a tile, the joining of parts.
 #include <cstring>
 
@@ -1049,8 +1051,9 @@ DecodeLayout layout_of(const ra_attention_decode_args& p) {
   L.groups = (L.R + L.rows - 1) / L.rows;
   L.grid = device_sm_count();
   if (L.grid > WS_COUNTERS) L.grid = WS_COUNTERS;
-  // A unit has about grid / units parts; the last CTA reads them all, alone on its SM (about 20 us a MB), while a kernel of
-  // its own takes about 3 us and has the GPU
+  // A unit has about grid / units parts if the lengths are near to one another, which the host does not know; the last CTA
+  // reads them all, alone on its SM (about 20 us a MB), while a kernel of its own takes about 3 us and has the GPU.  (Of
+  // one sequence of 65536 tokens beside 31 of 200, with 16 heads over one, it reads some 150 where this counts on 6: 44 us.)
   const int64_t units = (int64_t)p.batch * p.cache.n_kv_heads * L.groups;
   const int64_t parts = units > 0 ? L.grid / units + 2 : 0;
   L.join = parts * (L.R < L.rows ? L.R : L.rows) * p.cache.head_dim * 4 <= 128 * 1024;

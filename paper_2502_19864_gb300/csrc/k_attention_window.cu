@@ -1,5 +1,5 @@
 // k_attention_window.cu -- causal attention with a sliding window and first tokens that stay visible, over whole
-// sequences, in fp32 arithmetic: the forward and the backward of fp32 inputs (tf32 products would be 1e-3 off).
+// sequences, in fp32 arithmetic: the forward and the backward of fp32 inputs (products of operands rounded to tf32 would be 1e-3 off).
 //
 // Query i sees key j when j <= i and (i - j < W or j < sinks), both below the sequence's length:
 //   forward   o_i = sum_j p_ij v_j, p_ij = exp(scale q_i k_j - lse_i), by blocks of 64 keys with a running maximum

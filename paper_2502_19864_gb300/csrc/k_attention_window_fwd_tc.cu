@@ -12,8 +12,9 @@
 //   warp 10             loads Q, then K and V blocks by TMA into a ring.
 // What bounds it is each tile's round of softmax (1900 cycles a block of 128 keys: 500 for the maximum, 1000 for the
 // exponentials, 400 until its p are seen) and products (1230).  One warp for both tiles' products had its waits and
-// commits in that round: 406 us for 16384 tokens of 16 heads over 4, window 4096, against 360 (1338 TFLOP/s).  Two warps without
-// turns interleave their products, so that each tile waits for both: 488 us.
+// commits in that round: 406 us for 16384 tokens of 16 heads over 4, window 4096, against 360 on the same GPU.  Two warps without
+// turns interleave their products, so that each tile waits for both: 488 us.  On other GPUs of the kind this takes 374 to 380 us,
+// 1290 to 1270 TFLOP/s.
 // The CTAs are persistent: the copies and first products of a CTA's next pair of tiles run while the last outputs of this one
 // leave (one pair of tiles a CTA: 60 us for 8 x 1024 tokens of 16 heads and window 256, this: 50 us; a pair takes as
 // little as three blocks, and its start and end as long).

@@ -9,8 +9,8 @@
 // Of all the probabilities one row of p, one of q and the noise are read, and two values of every drafted place.
 // Bound by these reads where the batch is large and by latency where it is small: a sequence's row is cut over
 // several CTAs so that the batch fills the SMs once; each finds n for itself, and the last of them to finish (a
-// counter) writes the answer and leaves the workspace zero.  64 bf16 sequences of 50001 words and 8 drafts: 9.9 us;
-// one fp32 sequence of 32000 and 4 drafts: 4.2 us.
+// counter) writes the answer and leaves its slot zero.  64 bf16 sequences of 50001 words and 8 drafts: 10.0 us, of it
+// three rounds of a thread's 21 tokens, eight at once; one fp32 sequence of 32000 and 4 drafts: 4.2 us.
 #include "common.cuh"
 #include "operators.h"
 
