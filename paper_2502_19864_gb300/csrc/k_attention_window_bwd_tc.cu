@@ -719,7 +719,8 @@ __global__ void __launch_bounds__(256) window_bwd_parts_kernel(const __grid_cons
 // one with sinks up to n_blk G: with up to two such blocks, as many CTAs as bring them back to an ordinary one's length, or to
 // half of what each of the 152 SMs has to do in all, at most 32.  (With more sinks than that most blocks are long, and the CTAs
 // have even work without it.  1 x 8192 tokens, 16 heads over 4, window 1024, forward and backward: shared
-// 336 us, else 748; 8 x 1024 tokens of 16 heads, window 256, where an SM has 24 steps and the longest block 8: 217 us, else 203.)
+// 336 us, else 748; 8 x 1024 tokens of 16 heads, window 256, where an SM has 24 steps and the longest block 8: 217 us, else 203.
+// With dS in two terms, which came later, the first takes 359 us as it is, shared, and the second 212, not shared.)
 void split_of(const ra_attention_window_args& p, int& split, int& chunks) {
   const int64_t n_blk = (p.seq + BR - 1) / BR, G = p.n_heads / p.n_kv_heads, units = (int64_t)p.batch * p.n_kv_heads;
   const int64_t W = p.window == 0 || p.window > p.seq ? p.seq : p.window;
