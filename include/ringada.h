@@ -561,6 +561,88 @@ typedef struct {
 size_t ra_verify_draft_workspace_bytes(const ra_verify_draft_args* args);
 ra_status ra_verify_draft(const ra_verify_draft_args* args, ra_stream_t stream);
 
+/* ---------------------------------------------------------------------------------------
+ * Operators that train all of a decoder's weights: the norm of a stack's activations with the gradients of its
+ * weights, the cross-entropy over a vocabulary straight from hidden states, and the orthogonalisation of an update.
+ * The paper trains adapters beside frozen weights and has no counterpart.  The conventions of the operators above hold:
+ * one argument block a call, the same workspaces (one may serve these operators and those), the same errors.
+ * ------------------------------------------------------------------------------------- */
+
+/* LayerNorm or RMSNorm of rows [rows, hidden]: with z = x + residual (residual NULL: z = x),
+ *   y = (z - mean) rstd gamma + beta, rstd = 1 / sqrt(mean((z - mean)^2) + eps); RA_NORM_RMS: mean = 0
+ * and, where residual is given and sum_dev is not NULL, sum = z rounded to the type (y is of the unrounded z).
+ * gamma, beta (nullable) are of type w_dtype: that of the rows, or RA_F32.
+ * The backward takes the same block with mean (RA_NORM_LAYER) and rstd as the forward left them and reads z from sum where
+ * residual is given, else from x: with u = (z - mean) rstd and g = dy gamma,
+ *   dx = rstd (g - mean(g) - u mean(g u)) + dsum (RA_NORM_RMS: without mean(g)), the gradient of x and of residual,
+ *   dgamma = sum over rows of dy u, dbeta = sum over rows of dy, summed in a fixed order;
+ * dsum (nullable) is the gradient that comes back on the sum.  Gradients that are NULL are left out.
+ * Any hidden up to 32768, any strides of at least it (rows at 16-byte boundaries are read fastest).
+ * y may be x or residual (where the other outputs and the backward do not need it), sum may be x or residual, dx may be dy
+ * or dsum, with equal strides.  No rows: the backward's dgamma and dbeta are zero. */
+enum { RA_NORM_LAYER = 0, RA_NORM_RMS = 1 };
+typedef struct {
+  const void* x_dev; int64_t x_stride;
+  const void* residual_dev; int64_t residual_stride; /* or NULL */
+  void* sum_dev; int64_t sum_stride;                 /* or NULL */
+  const void *gamma_dev, *beta_dev;                  /* [hidden] or NULL */
+  void* y_dev; int64_t y_stride;
+  float *mean_dev, *rstd_dev;                        /* [rows]; NULL: forward alone (mean: RA_NORM_RMS too) */
+  const void* dy_dev; int64_t dy_stride;
+  const void* dsum_dev; int64_t dsum_stride;         /* or NULL */
+  void* dx_dev; int64_t dx_stride;                   /* or NULL */
+  void *dgamma_dev, *dbeta_dev;                      /* [hidden] or NULL */
+  void* workspace_dev; size_t workspace_bytes;       /* the backward's */
+  int32_t rows, hidden, kind, dtype, w_dtype;
+  float eps;                                         /* >= 0, finite */
+} ra_norm_args;
+size_t ra_norm_workspace_bytes(const ra_norm_args* args);
+ra_status ra_norm_forward(const ra_norm_args* args, ra_stream_t stream);
+ra_status ra_norm_backward(const ra_norm_args* args, ra_stream_t stream);
+
+/* Cross-entropy over a vocabulary: loss[t] = log(sum_v exp(z[t, v])) - z[t, labels[t]] with the logits z = x W^T, x
+ * [tokens, hidden], W [vocab, hidden], which are never kept: the workspace holds pieces of them.  lse[t] is that
+ * logarithm.  A token of negative label is not counted: its loss and lse are 0, its gradients nothing, and what its x
+ * holds does not matter.  One of a label >= vocab is not counted either and reported (RA_DEV_BOUNDS).
+ * The backward takes the same block with lse as the forward left it and dloss[t], the gradient of each token's loss (1 / n for
+ * the mean over n counted ones), and writes dx [tokens, hidden] (zero for those not counted) and dw [vocab, hidden],
+ * either of them where it is not NULL, in fixed orders.
+ * bf16: products of bf16 values summed in float32; dz = dloss (softmax - onehot) enters its two products rounded to bf16.
+ * hidden is a multiple of 8 (bf16) or 4 (f32), rows at 16-byte boundaries. */
+typedef struct {
+  const void* x_dev; int64_t x_stride;
+  const void* w_dev; int64_t w_stride;
+  const int32_t* labels_dev;                         /* [tokens] */
+  float* loss_dev;                                   /* [tokens] */
+  float* lse_dev;                                    /* [tokens]; NULL: forward alone */
+  const float* dloss_dev;                            /* [tokens] */
+  void* dx_dev; int64_t dx_stride;
+  void* dw_dev; int64_t dw_stride;
+  void* workspace_dev; size_t workspace_bytes;
+  uint32_t* err_dev;                                 /* nullable */
+  int32_t tokens, vocab, hidden, dtype;
+} ra_vocab_loss_args;
+size_t ra_vocab_loss_workspace_bytes(const ra_vocab_loss_args* args);
+ra_status ra_vocab_loss_forward(const ra_vocab_loss_args* args, ra_stream_t stream);
+ra_status ra_vocab_loss_backward(const ra_vocab_loss_args* args, ra_stream_t stream);
+
+/* Orthogonalisation of updates by Newton-Schulz products, for n_matrices matrices x [rows, cols] of their own, matrix_stride
+ * elements apart: X = x / (|x| + eps) (the root of the sum of squares), then `steps` times
+ *   X <- a X + (b X X^T + c (X X^T)^2) X
+ * and out = X in the type.  With a = 3.4445, b = -4.775, c = 2.0315 five steps bring singular values that are not too
+ * small to between about 0.7 and 1.2 (what is subtracted from a weight in place of its momentum).  A matrix with an
+ * element that is not finite gives no finite value.  rows and cols of 1 to 32768, any strides; out may be x. */
+typedef struct {
+  const void* x_dev; int64_t x_stride, x_matrix_stride;
+  void* out_dev; int64_t out_stride, out_matrix_stride;
+  void* workspace_dev; size_t workspace_bytes;
+  uint32_t* err_dev;                                 /* nullable */
+  int32_t n_matrices, rows, cols, steps, dtype;      /* steps 0 to 64 */
+  float a, b, c, eps;                                /* eps >= 0 */
+} ra_orthogonalize_args;
+size_t ra_orthogonalize_workspace_bytes(const ra_orthogonalize_args* args);
+ra_status ra_orthogonalize(const ra_orthogonalize_args* args, ra_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,4 +1,5 @@
-// operators.cu -- C ABI of the operators that answer with a tuned decoder: argument checks, then the launch.
+// operators.cu -- C ABI of the operators that answer with a tuned decoder and that train all of its weights: argument
+// checks, then the launch.
 #include <cmath>
 
 #include "operators.h"
@@ -124,6 +125,68 @@ ra_status check_verify(const ra_verify_draft_args& a) {
   return RA_OK;
 }
 
+// rows of `cols` values at any boundary that their type allows
+ra_status check_loose(const void* p, int64_t stride, int64_t cols, int dtype) {
+  if (!p || !aligned(p, dtype == RA_BF16 ? 2 : 4)) return RA_ERR_ARG;
+  return stride < cols ? RA_ERR_SHAPE : RA_OK;
+}
+bool no_less_than_zero(float v) { return v >= 0.f && std::isfinite(v); }
+ra_status check_norm(const ra_norm_args& a, bool backward) {
+  if (a.dtype != RA_F32 && a.dtype != RA_BF16) return RA_ERR_ARG;
+  if (a.w_dtype != a.dtype && a.w_dtype != RA_F32) return RA_ERR_ARG;
+  if (a.kind != RA_NORM_LAYER && a.kind != RA_NORM_RMS) return RA_ERR_ARG;
+  if (a.rows < 0 || a.hidden < 1 || !no_less_than_zero(a.eps)) return RA_ERR_ARG;
+  if (a.hidden > 32768) return RA_ERR_SHAPE;
+  const size_t wes = a.w_dtype == RA_BF16 ? 2 : 4;
+  if (!aligned(a.gamma_dev, wes) || !aligned(a.beta_dev, wes) || !aligned(a.mean_dev, 4) || !aligned(a.rstd_dev, 4))
+    return RA_ERR_ARG;
+  if (a.rows == 0) return RA_OK;
+  if (!backward || !a.residual_dev) TRY(check_loose(a.x_dev, a.x_stride, a.hidden, a.dtype));
+  if (a.sum_dev) TRY(check_loose(a.sum_dev, a.sum_stride, a.hidden, a.dtype));
+  if (!backward) {
+    if (a.residual_dev) TRY(check_loose(a.residual_dev, a.residual_stride, a.hidden, a.dtype));
+    return check_loose(a.y_dev, a.y_stride, a.hidden, a.dtype);
+  }
+  if (a.residual_dev && !a.sum_dev) return RA_ERR_ARG;  // (what was normalised was not kept)
+  if (!a.rstd_dev || (a.kind == RA_NORM_LAYER && !a.mean_dev)) return RA_ERR_ARG;
+  TRY(check_loose(a.dy_dev, a.dy_stride, a.hidden, a.dtype));
+  if (a.dsum_dev) TRY(check_loose(a.dsum_dev, a.dsum_stride, a.hidden, a.dtype));
+  if (a.dx_dev) TRY(check_loose(a.dx_dev, a.dx_stride, a.hidden, a.dtype));
+  if (!aligned(a.dgamma_dev, wes) || !aligned(a.dbeta_dev, wes)) return RA_ERR_ARG;
+  return check_workspace(a.workspace_dev, a.workspace_bytes, norm_workspace(a));
+}
+ra_status check_vocab(const ra_vocab_loss_args& a, bool backward) {
+  if (a.dtype != RA_F32 && a.dtype != RA_BF16) return RA_ERR_ARG;
+  if (a.tokens < 0 || a.vocab < 1 || a.hidden < 1) return RA_ERR_ARG;
+  // tokens, words and values are counted in 32 bits, with room for whole tiles
+  if (a.hidden % vec(a.dtype) || a.hidden > (1 << 20) || a.tokens > (1 << 24) || a.vocab > (1 << 24)) return RA_ERR_SHAPE;
+  if (backward && a.dw_dev) TRY(check_rows(a.dw_dev, a.dw_stride, 1, a.hidden, a.dtype));
+  if (a.tokens == 0) return RA_OK;
+  TRY(check_rows(a.x_dev, a.x_stride, 1, a.hidden, a.dtype));
+  TRY(check_rows(a.w_dev, a.w_stride, 1, a.hidden, a.dtype));
+  if (!a.labels_dev || !aligned(a.labels_dev, 4) || !aligned(a.lse_dev, 4)) return RA_ERR_ARG;
+  if (!backward && (!a.loss_dev || !aligned(a.loss_dev, 4))) return RA_ERR_ARG;
+  if (backward) {
+    if (!a.lse_dev || !a.dloss_dev || !aligned(a.dloss_dev, 4)) return RA_ERR_ARG;
+    if (a.dx_dev) TRY(check_rows(a.dx_dev, a.dx_stride, 1, a.hidden, a.dtype));
+  }
+  return RA_OK;
+}
+ra_status check_orthogonalize(const ra_orthogonalize_args& a) {
+  if (a.dtype != RA_F32 && a.dtype != RA_BF16) return RA_ERR_ARG;
+  if (a.n_matrices < 0 || a.rows < 1 || a.cols < 1 || a.steps < 0 || !no_less_than_zero(a.eps) || !std::isfinite(a.a) ||
+      !std::isfinite(a.b) || !std::isfinite(a.c))
+    return RA_ERR_ARG;
+  if (a.rows > 32768 || a.cols > 32768 || a.steps > 64 || a.n_matrices > 65535) return RA_ERR_SHAPE;
+  TRY(check_loose(a.x_dev, a.x_stride, a.cols, a.dtype));
+  TRY(check_loose(a.out_dev, a.out_stride, a.cols, a.dtype));
+  // matrices of their own (the last row of one ends before the next begins)
+  if (a.n_matrices > 1 && (a.x_matrix_stride < (a.rows - 1) * a.x_stride + a.cols ||
+                           a.out_matrix_stride < (a.rows - 1) * a.out_stride + a.cols))
+    return RA_ERR_SHAPE;
+  return RA_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -189,6 +252,60 @@ ra_status ra_verify_draft(const ra_verify_draft_args* args, ra_stream_t stream) 
   TRY(check_workspace(args->workspace_dev, args->workspace_bytes, verify_draft_workspace(*args)));
   if (!tc_available()) return RA_ERR_UNSUPPORTED;
   return launched(verify_draft(*args, (cudaStream_t)stream));
+}
+
+size_t ra_norm_workspace_bytes(const ra_norm_args* args) {
+  if (!args) return 0;
+  ra_norm_args a = *args;  // a block for the forward alone has what this needs too
+  return check_norm(a, false) == RA_OK ? norm_workspace(a) : 0;
+}
+ra_status ra_norm_forward(const ra_norm_args* args, ra_stream_t stream) {
+  if (!args) return RA_ERR_ARG;
+  if (args->rows == 0) return RA_OK;
+  TRY(check_norm(*args, false));
+  if (!tc_available()) return RA_ERR_UNSUPPORTED;
+  return launched(norm_fwd(*args, (cudaStream_t)stream));
+}
+ra_status ra_norm_backward(const ra_norm_args* args, ra_stream_t stream) {
+  if (!args) return RA_ERR_ARG;
+  TRY(check_norm(*args, true));
+  if (!args->dx_dev && !args->dgamma_dev && !args->dbeta_dev) return RA_OK;
+  if (!tc_available()) return RA_ERR_UNSUPPORTED;
+  return launched(norm_bwd(*args, (cudaStream_t)stream));
+}
+
+size_t ra_vocab_loss_workspace_bytes(const ra_vocab_loss_args* args) {
+  return args && check_vocab(*args, false) == RA_OK ? vocab_loss_workspace(*args) : 0;
+}
+ra_status ra_vocab_loss_forward(const ra_vocab_loss_args* args, ra_stream_t stream) {
+  if (!args) return RA_ERR_ARG;
+  if (args->tokens == 0) return RA_OK;
+  TRY(check_vocab(*args, false));
+  TRY(check_workspace(args->workspace_dev, args->workspace_bytes, vocab_loss_workspace(*args)));
+  if (!tc_available()) return RA_ERR_UNSUPPORTED;
+  return launched(vocab_loss_fwd(*args, (cudaStream_t)stream));
+}
+ra_status ra_vocab_loss_backward(const ra_vocab_loss_args* args, ra_stream_t stream) {
+  if (!args) return RA_ERR_ARG;
+  TRY(check_vocab(*args, true));
+  if (args->tokens > 0) TRY(check_workspace(args->workspace_dev, args->workspace_bytes, vocab_loss_workspace(*args)));
+  if (!args->dx_dev && !args->dw_dev) return RA_OK;
+  if (args->tokens == 0 && !args->dw_dev) return RA_OK;
+  if (!tc_available()) return RA_ERR_UNSUPPORTED;
+  return launched(vocab_loss_bwd(*args, (cudaStream_t)stream));
+}
+
+size_t ra_orthogonalize_workspace_bytes(const ra_orthogonalize_args* args) {
+  if (args && args->n_matrices == 0) return WS_ZERO;
+  return args && check_orthogonalize(*args) == RA_OK ? orthogonalize_workspace(*args) : 0;
+}
+ra_status ra_orthogonalize(const ra_orthogonalize_args* args, ra_stream_t stream) {
+  if (!args) return RA_ERR_ARG;
+  if (args->n_matrices == 0) return RA_OK;
+  TRY(check_orthogonalize(*args));
+  TRY(check_workspace(args->workspace_dev, args->workspace_bytes, orthogonalize_workspace(*args)));
+  if (!tc_available()) return RA_ERR_UNSUPPORTED;
+  return launched(orthogonalize(*args, (cudaStream_t)stream));
 }
 
 }  // extern "C"

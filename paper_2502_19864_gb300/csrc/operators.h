@@ -1,4 +1,4 @@
-// operators.h -- launchers of the operators that answer with a tuned decoder (internal, not ABI).  They take
+// operators.h -- launchers of the operators that answer with a tuned decoder and train its weights (internal, not ABI).  They take
 // the ABI's argument blocks, checked by operators.cu.
 #pragma once
 
@@ -33,5 +33,14 @@ cudaError_t attention_window_bwd_tc(const ra_attention_window_args& a, cudaStrea
 cudaError_t attention_window_bwd_simt(const ra_attention_window_args& a, cudaStream_t st);
 size_t verify_draft_workspace(const ra_verify_draft_args& a);
 cudaError_t verify_draft(const ra_verify_draft_args& a, cudaStream_t st);
+
+size_t norm_workspace(const ra_norm_args& a);
+cudaError_t norm_fwd(const ra_norm_args& a, cudaStream_t st);
+cudaError_t norm_bwd(const ra_norm_args& a, cudaStream_t st);
+size_t vocab_loss_workspace(const ra_vocab_loss_args& a);
+cudaError_t vocab_loss_fwd(const ra_vocab_loss_args& a, cudaStream_t st);
+cudaError_t vocab_loss_bwd(const ra_vocab_loss_args& a, cudaStream_t st);
+size_t orthogonalize_workspace(const ra_orthogonalize_args& a);
+cudaError_t orthogonalize(const ra_orthogonalize_args& a, cudaStream_t st);
 
 }  // namespace ra

@@ -143,6 +143,39 @@ class ra_verify_draft_args(C.Structure):
                 ("vocab", C.c_int32), ("dtype", C.c_int32)]
 
 
+class ra_norm_args(C.Structure):
+    _fields_ = [("x_dev", C.c_void_p), ("x_stride", C.c_int64), ("residual_dev", C.c_void_p),
+                ("residual_stride", C.c_int64), ("sum_dev", C.c_void_p), ("sum_stride", C.c_int64),
+                ("gamma_dev", C.c_void_p), ("beta_dev", C.c_void_p), ("y_dev", C.c_void_p),
+                ("y_stride", C.c_int64), ("mean_dev", C.c_void_p), ("rstd_dev", C.c_void_p),
+                ("dy_dev", C.c_void_p), ("dy_stride", C.c_int64), ("dsum_dev", C.c_void_p),
+                ("dsum_stride", C.c_int64), ("dx_dev", C.c_void_p), ("dx_stride", C.c_int64),
+                ("dgamma_dev", C.c_void_p), ("dbeta_dev", C.c_void_p),
+                ("workspace_dev", C.c_void_p), ("workspace_bytes", C.c_size_t),
+                ("rows", C.c_int32), ("hidden", C.c_int32), ("kind", C.c_int32),
+                ("dtype", C.c_int32), ("w_dtype", C.c_int32), ("eps", C.c_float)]
+
+
+class ra_vocab_loss_args(C.Structure):
+    _fields_ = [("x_dev", C.c_void_p), ("x_stride", C.c_int64), ("w_dev", C.c_void_p),
+                ("w_stride", C.c_int64), ("labels_dev", C.c_void_p), ("loss_dev", C.c_void_p),
+                ("lse_dev", C.c_void_p), ("dloss_dev", C.c_void_p), ("dx_dev", C.c_void_p),
+                ("dx_stride", C.c_int64), ("dw_dev", C.c_void_p), ("dw_stride", C.c_int64),
+                ("workspace_dev", C.c_void_p), ("workspace_bytes", C.c_size_t),
+                ("err_dev", C.c_void_p), ("tokens", C.c_int32), ("vocab", C.c_int32),
+                ("hidden", C.c_int32), ("dtype", C.c_int32)]
+
+
+class ra_orthogonalize_args(C.Structure):
+    _fields_ = [("x_dev", C.c_void_p), ("x_stride", C.c_int64), ("x_matrix_stride", C.c_int64),
+                ("out_dev", C.c_void_p), ("out_stride", C.c_int64),
+                ("out_matrix_stride", C.c_int64), ("workspace_dev", C.c_void_p),
+                ("workspace_bytes", C.c_size_t), ("err_dev", C.c_void_p),
+                ("n_matrices", C.c_int32), ("rows", C.c_int32), ("cols", C.c_int32),
+                ("steps", C.c_int32), ("dtype", C.c_int32), ("a", C.c_float), ("b", C.c_float),
+                ("c", C.c_float), ("eps", C.c_float)]
+
+
 class RingAdaError(RuntimeError):
     def __init__(self, status, msg):
         super().__init__("%s: %s" % (STATUS_NAMES.get(status, status), msg))
@@ -211,6 +244,14 @@ _SIGS = {
     "ra_attention_window_workspace_bytes": (C.c_size_t, [C.c_void_p]),
     "ra_verify_draft": (C.c_int, [C.c_void_p, C.c_void_p]),
     "ra_verify_draft_workspace_bytes": (C.c_size_t, [C.c_void_p]),
+    "ra_norm_forward": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "ra_norm_backward": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "ra_norm_workspace_bytes": (C.c_size_t, [C.c_void_p]),
+    "ra_vocab_loss_forward": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "ra_vocab_loss_backward": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "ra_vocab_loss_workspace_bytes": (C.c_size_t, [C.c_void_p]),
+    "ra_orthogonalize": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "ra_orthogonalize_workspace_bytes": (C.c_size_t, [C.c_void_p]),
 }
 
 
@@ -465,6 +506,43 @@ def ra_verify_draft_workspace_bytes(args: ra_verify_draft_args) -> int:
 
 def ra_verify_draft(args: ra_verify_draft_args, stream=None):
     _check(lib().ra_verify_draft(C.byref(args), _stream_ptr(stream)))
+
+
+# ---- operators that train all of a decoder's weights ---------------------------------------
+
+RA_NORM_LAYER, RA_NORM_RMS = 0, 1
+
+
+def ra_norm_workspace_bytes(args: ra_norm_args) -> int:
+    return lib().ra_norm_workspace_bytes(C.byref(args))
+
+
+def ra_norm_forward(args: ra_norm_args, stream=None):
+    _check(lib().ra_norm_forward(C.byref(args), _stream_ptr(stream)))
+
+
+def ra_norm_backward(args: ra_norm_args, stream=None):
+    _check(lib().ra_norm_backward(C.byref(args), _stream_ptr(stream)))
+
+
+def ra_vocab_loss_workspace_bytes(args: ra_vocab_loss_args) -> int:
+    return lib().ra_vocab_loss_workspace_bytes(C.byref(args))
+
+
+def ra_vocab_loss_forward(args: ra_vocab_loss_args, stream=None):
+    _check(lib().ra_vocab_loss_forward(C.byref(args), _stream_ptr(stream)))
+
+
+def ra_vocab_loss_backward(args: ra_vocab_loss_args, stream=None):
+    _check(lib().ra_vocab_loss_backward(C.byref(args), _stream_ptr(stream)))
+
+
+def ra_orthogonalize_workspace_bytes(args: ra_orthogonalize_args) -> int:
+    return lib().ra_orthogonalize_workspace_bytes(C.byref(args))
+
+
+def ra_orthogonalize(args: ra_orthogonalize_args, stream=None):
+    _check(lib().ra_orthogonalize(C.byref(args), _stream_ptr(stream)))
 
 
 # ---- convenience: torch-owned buffers ------------------------------------------------------

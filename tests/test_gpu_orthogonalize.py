@@ -1,0 +1,184 @@
+"""Orthogonalisation by Newton-Schulz products against 64 bits.
+
+The bound is normwise, from the same steps in 64 bits with every product's elements moved at random by up to rho of
+the products' magnitudes (and a normalised input by u): what the roundings of each step may be, carried by the steps that
+follow, which raise what lies along small singular values by up to 3.4445 each.  fp32: a sum of K products is off by less than
+(sqrt(K) + 2) 2^-23 of their magnitudes; bf16 (operands of 16 bits in two terms): 2^-16.  Four such runs; the largest distance from the undisturbed
+result, four times, and the output's rounding."""
+import math
+
+import pytest
+import torch
+
+from paper_2502_19864_gb300 import ringada as R
+from tests.operator_helpers import DT, E, RA, U, workspace
+
+pytestmark = pytest.mark.gpu
+COEF = (3.4445, -4.775, 2.0315)
+
+
+def make(n, rows, cols, dtype, steps=5, coef=COEF, eps=1e-7, seed=0, pad=0, gap=0, scale=1e-3, fall=-2.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    low, row = min(rows, cols), cols + pad
+    each = rows * row + gap
+    f = torch.logspace(0, fall, low, device="cuda")
+    v = (torch.randn(n, rows, low, generator=g, device="cuda") * f) @ torch.randn(n, low, cols, generator=g, device="cuda").mul_(low ** -0.5)
+    buf = torch.full((n * each,), 7.0, device="cuda", dtype=DT[dtype])
+    s = {"x": torch.as_strided(buf, (n, rows, cols), (each, row, 1))}
+    s["x"].copy_(v * scale)
+    out = torch.full((n * each,), 7.0, device="cuda", dtype=DT[dtype])
+    s["out"], s["whole"] = torch.as_strided(out, (n, rows, cols), (each, row, 1)), out
+    s["err"] = torch.zeros(1, dtype=torch.int32, device="cuda")
+    a = R.ra_orthogonalize_args(x_dev=buf.data_ptr(), x_stride=row, x_matrix_stride=each, out_dev=out.data_ptr(), out_stride=row,
+                                out_matrix_stride=each, n_matrices=n, rows=rows, cols=cols, steps=steps, dtype=RA[dtype],
+                                err_dev=s["err"].data_ptr(), a=coef[0], b=coef[1], c=coef[2], eps=eps)
+    need = R.ra_orthogonalize_workspace_bytes(a)
+    assert need > 0
+    s["workspace"] = workspace(need)
+    a.workspace_dev, a.workspace_bytes = s["workspace"].data_ptr(), need
+    s["buf"] = buf
+    return a, s
+
+
+def steps64(x, steps, coef, eps, rho=0.0, gen=None):
+    def mul(p, q):
+        r = p @ q
+        if rho:
+            r = r + rho(p.shape[-1]) * (p.abs() @ q.abs()) * (torch.rand(r.shape, generator=gen, device="cuda", dtype=torch.float64) * 2 - 1)
+        return r
+    x = x.double()
+    x = x / (x.square().sum((1, 2), keepdim=True).sqrt() + eps)
+    if rho:
+        x = x * (1 + 2 * U * (torch.rand(x.shape, generator=gen, device="cuda", dtype=torch.float64) * 2 - 1))
+    tall = x.shape[1] > x.shape[2]
+    x = x.transpose(1, 2) if tall else x
+    a, b, c = (float(torch.tensor(v, dtype=torch.float32)) for v in coef)
+    for _ in range(steps):
+        S = mul(x, x.transpose(1, 2))
+        x = a * x + mul(b * S + c * mul(S, S), x)
+    return x.transpose(1, 2) if tall else x
+
+
+def check(s, dtype, steps=5, coef=COEF, eps=1e-7):
+    assert int(s["err"]) == 0
+    eps = float(torch.tensor(eps, dtype=torch.float32))
+    want = steps64(s["x"] if "kept" not in s else s["kept"], steps, coef, eps)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    rho = (lambda k: (math.sqrt(k) + 2) * 2.0 ** -23) if dtype == "f32" else (lambda k: 2.0 ** -16)
+    src = s["x"] if "kept" not in s else s["kept"]
+    e = E if dtype == "bf16" else U
+    norm = lambda t: t.square().sum((1, 2)).sqrt()  # noqa: E731
+    off = torch.stack([norm(steps64(src, steps, coef, eps, rho, gen) - want) for _ in range(4)]).amax(0)
+    got = norm(s["out"].double() - want)
+    bound = 4 * off + e * norm(want)
+    assert bool((got <= bound).all()), float((got / bound).max())
+
+
+SHAPES = [(1, 1, 1), (2, 1, 9), (3, 9, 1), (1, 5, 7), (4, 16, 128), (4, 128, 16), (2, 64, 64), (3, 65, 127), (2, 200, 130), (48, 96, 40),
+          (1, 300, 1000), (1, 513, 257), (2, 128, 128), (1, 777, 640), (1, 31, 4099)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,rows,cols", SHAPES)
+def test_against_64_bits(n, rows, cols, dtype):
+    a, s = make(n, rows, cols, dtype, seed=rows)
+    R.ra_orthogonalize(a)
+    torch.cuda.synchronize()
+    check(s, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("steps", [0, 1, 2, 6])
+def test_steps(dtype, steps):
+    a, s = make(2, 100, 72, dtype, steps=steps)
+    R.ra_orthogonalize(a)
+    torch.cuda.synchronize()
+    check(s, dtype, steps=steps)
+
+
+def test_other_coefficients():
+    """The cubic (3 X - X X^T X) / 2, which leaves an orthogonal matrix where it is."""
+    coef = (1.5, -0.5, 0.0)
+    a, s = make(1, 96, 160, "f32", steps=12, coef=coef, fall=-0.5)
+    R.ra_orthogonalize(a)
+    torch.cuda.synchronize()
+    check(s, "f32", steps=12, coef=coef)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("pad,gap", [(3, 0), (8, 5), (0, 1)])
+def test_strides(dtype, pad, gap):
+    a, s = make(3, 70, 90, dtype, pad=pad, gap=gap)
+    R.ra_orthogonalize(a)
+    torch.cuda.synchronize()
+    check(s, dtype)
+    s["out"].fill_(7.0)
+    assert bool((s["whole"] == 7.0).all())  # what lies between rows and matrices is left as it was
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(100, 72), (40, 300)])
+def test_in_place(dtype, rows, cols):
+    a, s = make(2, rows, cols, dtype)
+    s["kept"] = s["x"].clone()
+    a.out_dev = a.x_dev
+    s["out"] = s["x"]
+    R.ra_orthogonalize(a)
+    torch.cuda.synchronize()
+    check(s, dtype)
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-18, 1e18, 1e34])
+def test_values_whose_squares_do_not_fit(scale):
+    a, s = make(2, 90, 60, "f32", scale=scale, eps=0.0)
+    R.ra_orthogonalize(a)
+    torch.cuda.synchronize()
+    check(s, "f32", eps=0.0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("eps", [0.0, 1e-7])
+def test_zeros_and_values_that_are_not_finite_stay_in_their_matrix(dtype, eps):
+    for steps in (0, 5):
+        a, s = make(5, 70, 50, dtype, steps=steps, eps=eps)
+        s["x"][1] = 0.0
+        s["x"][2, 3, 4] = float("nan")
+        s["x"][4, 69, 49] = float("-inf")
+        R.ra_orthogonalize(a)
+        torch.cuda.synchronize()
+        assert bool((s["out"][1] == 0).all())
+        assert not bool(s["out"][[2, 4]].isfinite().any())
+        s["x"], s["out"] = s["x"][[0, 3]], s["out"][[0, 3]]
+        check(s, dtype, steps=steps, eps=eps)
+
+
+def test_the_same_twice_captured_and_on_two_streams():
+    a, s = make(6, 128, 64, "bf16")
+    b, t = make(1, 300, 500, "f32")
+    for x in (a, b):
+        R.ra_orthogonalize(x)
+    torch.cuda.synchronize()
+    want = [q["out"].clone() for q in (s, t)]
+    for q in (s, t):
+        q["out"].fill_(7.0)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        R.ra_orthogonalize(a, torch.cuda.current_stream())
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):
+        graph.replay()
+        R.ra_orthogonalize(b, other)
+    torch.cuda.synchronize()
+    for q, w in zip((s, t), want):
+        assert torch.equal(q["out"], w)
+
+
+def test_a_workspace_of_anything_behind_its_zeros():
+    a, s = make(3, 90, 200, "bf16")
+    s["workspace"][16384:] = 255
+    for _ in range(2):
+        R.ra_orthogonalize(a)
+    torch.cuda.synchronize()
+    check(s, "bf16")
+    assert bool((s["workspace"][:16384] == 0).all())
