@@ -1,206 +1,644 @@
 // k_vocab_loss.cu -- cross-entropy over a vocabulary from hidden states, without keeping logits.
 //
-// Forward: tiles of logits z = x W^T; of each tile's rows the maximum and the sum of exp(z - maximum) go to the
-// workspace, with the label's logit, and a second kernel joins them: lse = m + log(sum), loss = lse - z[label].
-// Backward, piece by piece of the vocabulary: the piece's logits again, dz = dloss (exp(z - lse) - onehot) into the
-// workspace, then dw of the piece = dz^T x and dx += dz W.
+// First the tokens that are counted are found and numbered (a CTA counts those before its own), and where not all are, their
+// hidden states are gathered, so that what is not counted costs nothing and is never read.
+// Forward: tiles of logits z = x W^T; of each tile's rows the maximum and the sum of exp(z - maximum) go to the workspace,
+// with the label's logit; a second kernel joins them: lse = m + log(sum), loss = lse - z[label].
+// Backward, piece by piece of the vocabulary: the piece's logits again and dz = dloss (exp(z - lse) - onehot) into the
+// workspace; then, in one launch, dw of the piece = dz^T x and the sums of dx += dz W, the latter in fp32 and, where its tiles are
+// few, in parts of the vocabulary, which a last kernel adds up and puts where the tokens were.
+// fp32 operands are cut into three planes of bf16 (products.cuh), dz too; bf16 ones are read where they are.
+#include <algorithm>
+
 #include "common.cuh"
 #include "operators.h"
-#include "simt_tile.cuh"
+#include "products.cuh"
 
 namespace ra {
 namespace {
 
-constexpr int TILE = 64;
+using prod::Shape;
+using prod::Store;
+using prod::Tile;
+using prod::Unit;
+
+constexpr float LOG2E = 1.44269504088896341f;
+constexpr int ROWS = 256;  // rows of tokens in the workspace: whole tiles of a pair
+
+// ---- which tokens are counted -------------------------------------------------------------
+struct Prep {
+  int *count, *index, *label;  // of the counted tokens: how many; each one's place among all, its label,
+  float *scale, *lse;          // ... dloss and lse (backward)
+  void* x;                     // ... and hidden states: [planes][rows][pitch]
+  int rows, pitch, planes;
+};
+__device__ __forceinline__ bool counted(const ra_vocab_loss_args& a, int label) { return (uint32_t)label < (uint32_t)a.vocab; }
+
+// sums of two counts over the CTA's 256 threads
+__device__ __forceinline__ int2 sum2(int2 v, int2* sh) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
+    v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+  }
+  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
+  __syncthreads();
+  int2 r = make_int2(0, 0);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r.x += sh[i].x, r.y += sh[i].y;
+  return r;
+}
+// A row of hidden states (src NULL: zeros) into row r of the gathered ones, by a warp
+__device__ __forceinline__ void put_row(const Prep& p, const bf16* src, int r, int H, int lane) {
+  bf16* d = static_cast<bf16*>(p.x) + (int64_t)r * p.pitch;
+  for (int c = lane * 8; c < H; c += 256)
+    *reinterpret_cast<uint4*>(d + c) = src ? *reinterpret_cast<const uint4*>(src + c) : make_uint4(0, 0, 0, 0);
+}
+__device__ __forceinline__ void split4(float4 v, bf16* d, int64_t plane) {
+  float x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    __nv_bfloat162 h[2];
+    float y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = prod::plane_trunc(x[i]);
+    h[0] = __floats2bfloat162_rn(y[0], y[1]);
+    h[1] = __floats2bfloat162_rn(y[2], y[3]);
+    *reinterpret_cast<uint2*>(d + k * plane) = *reinterpret_cast<uint2*>(h);
+  }
+}
+__device__ __forceinline__ void put_row(const Prep& p, const float* src, int r, int H, int lane) {
+  bf16* d = static_cast<bf16*>(p.x) + (int64_t)r * p.pitch;
+  for (int c = lane * 4; c < p.pitch; c += 128)
+    split4(src && c < H ? *reinterpret_cast<const float4*>(src + c) : make_float4(0.f, 0.f, 0.f, 0.f), d + c, (int64_t)p.rows * p.pitch);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) vocab_prep_kernel(const ra_vocab_loss_args a, const Prep p, int backward) {
+  __shared__ int2 sh[8];
+  __shared__ int list[256], warp_n[8];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, T_ = a.tokens;
+  pdl_wait();
+  pdl_trigger();
+  const int per = (T_ + gridDim.x - 1) / gridDim.x;
+  const int start = min(T_, (int)blockIdx.x * per), end = min(T_, start + per);
+  int2 n = make_int2(0, 0);
+  for (int t = tid; t < T_; t += 256) {
+    const bool c = counted(a, a.labels_dev[t]);
+    n.x += c && t < start;
+    n.y += c;
+  }
+  n = sum2(n, sh);
+  int base = n.x;
+  const int total = n.y;
+  const bool gather = p.planes > 1 || total < T_;
+  const T* x = static_cast<const T*>(a.x_dev);
+  for (int s = start; s < end; s += 256) {
+    const int t = s + tid;
+    const int l = t < end ? a.labels_dev[t] : -1;
+    const bool c = counted(a, l);
+    const uint32_t ballot = __ballot_sync(0xffffffffu, c);
+    if (lane == 0) warp_n[warp] = __popc(ballot);
+    __syncthreads();
+    int at = __popc(ballot & ((1u << lane) - 1u)), here = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      at += i < warp ? warp_n[i] : 0;
+      here += warp_n[i];
+    }
+    if (t < end) {
+      if (c) {
+        list[at] = t;
+        p.index[base + at] = t;
+        p.label[base + at] = l;
+        p.scale[base + at] = backward ? a.dloss_dev[t] : 0.f;
+        p.lse[base + at] = backward ? a.lse_dev[t] : 0.f;
+      } else {
+        if (l >= a.vocab) set_dev_error(a.err_dev, RA_DEVERR_BOUNDS);
+        if (!backward) {
+          a.loss_dev[t] = 0.f;
+          if (a.lse_dev) a.lse_dev[t] = 0.f;
+        }
+        list[255 - (tid - at)] = t;  // those that are not, from the other end
+      }
+    }
+    __syncthreads();
+    if (gather)
+      for (int i = warp; i < here; i += 8) put_row(p, x + list[i] * a.x_stride, base + i, a.hidden, lane);
+    if (backward && a.dx_dev)
+      for (int i = warp; i < min(256, end - s) - here; i += 8) {
+        T* d = static_cast<T*>(a.dx_dev) + list[255 - i] * a.dx_stride;
+        for (int k = lane * (16 / (int)sizeof(T)); k < a.hidden; k += 512 / (int)sizeof(T))
+          *reinterpret_cast<uint4*>(d + k) = make_uint4(0, 0, 0, 0);
+      }
+    base += here;
+    __syncthreads();
+  }
+  // the rows up to whole tiles
+  const int up = (total + ROWS - 1) / ROWS * ROWS;
+  for (int r = total + blockIdx.x; r < up; r += gridDim.x) {
+    if (gather && warp == 0) put_row(p, (const T*)nullptr, r, a.hidden, lane);
+    if (tid == 32) {
+      p.label[r] = -1;
+      p.scale[r] = p.lse[r] = 0.f;
+    }
+  }
+  if (blockIdx.x == 0 && tid == 0) *p.count = total;
+}
+
+// rows [row0, row0 + rows) of W into planes
+__global__ void __launch_bounds__(256) vocab_split_kernel(const float* w, int64_t stride, bf16* out, int rows, int H, int pitch) {
+  pdl_wait();
+  pdl_trigger();
+  const int per = pitch / 4;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)rows * per; i += (int64_t)gridDim.x * 256) {
+    const int r = (int)(i / per), c = (int)(i % per) * 4;
+    split4(c < H ? *reinterpret_cast<const float4*>(w + r * stride + c) : make_float4(0.f, 0.f, 0.f, 0.f), out + (int64_t)r * pitch + c, (int64_t)rows * pitch);
+  }
+}
+
+// ---- products -----------------------------------------------------------------------------
+struct VocabArgs {
+  CUtensorMap x, xc, w;         // logits: K-major operands (x as given, gathered)
+  CUtensorMap dzk, dzm, wm, xm, xcm;  // gradients: dz K-major and MN-major, W and x MN-major
+  CUtensorMap dz, dw, dxs;      // stores
+  Shape shape;
+  unsigned* err;
+  const int *count, *label;
+  const float *scale, *lse;
+  float2* stats;
+  float* zlab;
+  int tokens, hidden, rows, planes;
+  int v0, width;                // the piece: words v0 .. v0 + width
+  int wrow;                     // where it begins in the map of W
+  int stat0;                    // its first part of the statistics
+  int cg, splits_x, splits_w, want_x, want_w;
+  int dtype;
+};
+
+__device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
+__device__ __forceinline__ const CUtensorMap* hidden_map(const VocabArgs& p, int count, const CUtensorMap* given, const CUtensorMap* gathered) {
+  return p.planes == 1 && count == p.tokens ? given : gathered;
+}
+
+// tiles of logits; BACK: into dz, else into statistics
+template <bool BACK>
+struct Logits {
+  using Args = VocabArgs;
+  static __device__ __forceinline__ int count(const Args& p) {
+    return ceil_div(*p.count, prod::BM * p.cg) * ceil_div(p.width, p.shape.bn);
+  }
+  static __device__ __forceinline__ void unit(const Args& p, int u, Unit& w) {
+    const int n = *p.count, mt_n = ceil_div(n, prod::BM * p.cg), nt_n = ceil_div(p.width, p.shape.bn);
+    int mt, nt;
+    prod::tile_of(u, mt_n, nt_n, mt, nt);
+    w.a = hidden_map(p, n, &p.x, &p.xc);
+    w.b = &p.w;
+    w.m0 = w.ar = mt * prod::BM * p.cg;
+    w.n0 = nt * p.shape.bn;
+    w.br = p.wrow + w.n0;
+    w.ak = w.bk = w.az = w.bz = w.kb0 = 0;
+    w.kb1 = ceil_div(p.hidden, prod::BK);
+    w.a_mn = w.b_mn = false;
+    w.job = 0;
+    w.z = nt;
+  }
+  static __device__ __forceinline__ void finish(const Args& p, const Unit& w, const Tile& t, Store& st, float (&v)[4][32]) {
+    const int row0 = w.m0 + t.rank * prod::BM + t.quad * 32, row = row0 + t.lane;
+    const int label = p.label[row] - p.v0 - w.n0;  // its column in this tile
+    if (BACK) {
+      const float scale = p.scale[row], lse = p.lse[row];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int c = 32 * (t.half + 2 * i), left = p.width - w.n0 - c;  // (zeros up to a whole k-block of the sums that follow)
+        if (i >= t.chunks || w.n0 + c >= (p.width + 63) / 64 * 64) break;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+          const float e = ex2_fast(__fmul_rn(__fsub_rn(v[i][j], lse), LOG2E));
+          v[i][j] = j < left ? __fmul_rn(scale, c + j == label ? __fsub_rn(e, 1.f) : e) : 0.f;
+        }
+        if (p.planes == 1) {
+          st.bf16_row(&p.dz, v[i], w.n0 + c, row0, 0);
+        } else {
+#pragma unroll 1
+          for (int k = 0; k < 3; ++k) {
+            float h[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) h[j] = prod::plane_trunc(v[i][j]);
+            st.bf16_row(&p.dz, h, w.n0 + c, row0, k);
+          }
+        }
+      }
+    } else {
+      float m = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int c = 32 * (t.half + 2 * i);
+        if (i >= t.chunks) break;
+        if (w.n0 + c + 32 > p.width)
+#pragma unroll
+          for (int j = 0; j < 32; ++j)
+            if (w.n0 + c + j >= p.width) v[i][j] = -INFINITY;
+        if ((uint32_t)(label - c) < 32u)
+#pragma unroll
+          for (int j = 0; j < 32; ++j)
+            if (c + j == label) p.zlab[row] = v[i][j];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) m = fmaxf(m, v[i][j]);
+      }
+      float l = 0.f;
+      const float from = m > -INFINITY ? m : 0.f;  // (nothing but NaN, or no words at all)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i < t.chunks)
+#pragma unroll
+          for (int j = 0; j < 32; ++j) l += ex2_fast(__fmul_rn(__fsub_rn(v[i][j], from), LOG2E));
+      p.stats[(int64_t)(p.stat0 + 2 * w.z + t.half) * p.rows + row] = make_float2(m, l);
+    }
+  }
+};
+
+// dx sums (job 0) and dw (job 1) of a piece, the longer ones first
+struct Grads {
+  using Args = VocabArgs;
+  struct Count {
+    int n, mx, mw, nt, kx, kw, ux, uw;
+    bool x_first;
+    __device__ __forceinline__ explicit Count(const Args& p) {
+      n = *p.count;
+      mx = ceil_div(n, prod::BM * p.cg);
+      mw = ceil_div(p.width, prod::BM * p.cg);
+      nt = ceil_div(p.hidden, p.shape.bn);
+      kx = ceil_div(ceil_div(p.width, prod::BK), p.splits_x);
+      kw = ceil_div(ceil_div(n, prod::BK), p.splits_w);
+      ux = p.want_x ? mx * nt * p.splits_x : 0;
+      uw = p.want_w ? mw * nt * p.splits_w : 0;
+      x_first = kx >= kw;
+    }
+  };
+  static __device__ __forceinline__ int count(const Args& p) {
+    const Count c(p);
+    return c.ux + c.uw;
+  }
+  static __device__ __forceinline__ void unit(const Args& p, int u, Unit& w) {
+    const Count c(p);
+    bool x = u < (c.x_first ? c.ux : c.uw);
+    if (!x) u -= c.x_first ? c.ux : c.uw;
+    x = x == c.x_first;
+    const int m_n = x ? c.mx : c.mw, tiles = m_n * c.nt;
+    int mt, nt;
+    prod::tile_of(u % tiles, m_n, c.nt, mt, nt);
+    w.z = u / tiles;
+    w.job = x ? 0 : 1;
+    w.m0 = w.ar = mt * prod::BM * p.cg;
+    w.n0 = w.br = nt * p.shape.bn;
+    w.ak = 0;
+    w.az = w.bz = 0;
+    w.b_mn = true;
+    if (x) {
+      w.a = &p.dzk;
+      w.b = &p.wm;
+      w.bk = p.wrow;
+      w.a_mn = false;
+      w.kb0 = w.z * c.kx;
+      w.kb1 = min(w.kb0 + c.kx, ceil_div(p.width, prod::BK));
+    } else {
+      w.a = &p.dzm;
+      w.b = hidden_map(p, c.n, &p.xm, &p.xcm);
+      w.bk = 0;
+      w.a_mn = true;
+      w.kb0 = w.z * c.kw;
+      w.kb1 = min(w.kb0 + c.kw, ceil_div(c.n, prod::BK));
+    }
+  }
+  static __device__ __forceinline__ void finish(const Args& p, const Unit& w, const Tile& t, Store& st, float (&v)[4][32]) {
+    const int row0 = w.m0 + t.rank * prod::BM + t.quad * 32;
+    if (w.job == 1 && row0 >= p.width) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int c = w.n0 + 32 * (t.half + 2 * i);
+      if (i >= t.chunks || c >= p.hidden) break;
+      if (w.job == 0) st.f32_row(&p.dxs, v[i], c, row0, w.z, p.v0 > 0, p.hidden);
+      else if (p.splits_w > 1) st.f32_row(&p.dw, v[i], c, row0, w.z, false, p.hidden);
+      else if (p.dtype == RA_BF16) st.bf16_row(&p.dw, v[i], c, p.v0 + row0, 0);
+      else st.f32_row(&p.dw, v[i], c, p.v0 + row0, 0, false, p.hidden);
+    }
+  }
+};
+
+// ---- what is joined at the end ------------------------------------------------------------
+// 32 tokens a CTA, its 16 warps on a sixteenth of the parts each
+__global__ void __launch_bounds__(512) vocab_join_kernel(const ra_vocab_loss_args a, const Prep p, const float2* stats, const float* zlab, int parts) {
+  __shared__ float2 sh[16][33];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = blockIdx.x * 32 + lane;
+  pdl_wait();
+  pdl_trigger();
+  const int n = *p.count;
+  if ((int)blockIdx.x * 32 >= n) return;
+  float m = -INFINITY, l = 0.f;
+  if (r < n)
+#pragma unroll 4
+    for (int i = warp; i < parts; i += 16) {
+      const float2 s = stats[(int64_t)i * p.rows + r];
+      const float top = fmaxf(m, s.x);
+      if (top > -INFINITY) l = l * ex2_fast((m - top) * LOG2E) + s.y * ex2_fast((s.x - top) * LOG2E);
+      else l += s.y;  // (a part of NaN logits alone)
+      m = top;
+    }
+  sh[warp][lane] = make_float2(m, l);
+  __syncthreads();
+  if (warp || r >= n) return;
+  float top = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) top = fmaxf(top, sh[i][lane].x);
+  l = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    if (sh[i][lane].x > -INFINITY || sh[i][lane].y != 0.f) l += sh[i][lane].y * (sh[i][lane].x > -INFINITY ? ex2_fast((sh[i][lane].x - top) * LOG2E) : 1.f);
+  const float lse = top + logf(l);
+  const int t = p.index[r];
+  a.loss_dev[t] = lse - zlab[r];
+  if (a.lse_dev) a.lse_dev[t] = lse;
+}
+
+// rows of sums, added up over their parts and rounded, to where they belong
+template <typename T>
+__global__ void __launch_bounds__(128) vocab_sum_kernel(const float* sums, int splits, int64_t part, int pitch, int H, const int* count,
+                                                        int rows, const int* index, T* out, int64_t stride) {
+  pdl_wait();
+  pdl_trigger();
+  const int n = count ? *count : rows;
+  for (int r = blockIdx.x; r < n; r += gridDim.x) {
+    T* o = out + (index ? index[r] : r) * stride;
+    for (int c = threadIdx.x * 4; c < H; c += 512) {
+      float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int i = 0; i < splits; ++i) {
+        const float4 v = *reinterpret_cast<const float4*>(sums + i * part + (int64_t)r * pitch + c);
+        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+      }
+      if (sizeof(T) == 4) {
+        *reinterpret_cast<float4*>(o + c) = s;
+      } else {
+        __nv_bfloat162 h[2] = {__floats2bfloat162_rn(s.x, s.y), __floats2bfloat162_rn(s.z, s.w)};
+        *reinterpret_cast<uint2*>(o + c) = *reinterpret_cast<uint2*>(h);
+      }
+    }
+  }
+}
+
+// ---- the plan -----------------------------------------------------------------------------
+struct Pick {
+  int cg, bn;
+};
+int up(int64_t a, int b) { return (int)((a + b - 1) / b * b); }
+int parts_of(int64_t a, int b) { return (int)((a + b - 1) / b); }
 
 struct Plan {
-  int tiles;         // of the vocabulary
-  int piece;         // words of a piece
-  size_t stats, label, dz, dx, bytes;
+  int planes, rows, pitch, chunk;
+  int pieces, width;              // of the vocabulary, backward (and fp32 forward)
+  Pick forward, logits, grads;    // (forward: of its logits)
+  int splits_x, splits_w, stats;  // parts of the statistics
+  size_t count, index, label, scale, lse, zlab, xc, wc, st, dz, dxs, dws, bytes;
 };
+
+constexpr int SMS = 152;  // a plan is the same on every device
+// microseconds of a k-block of a tile: the issue of products and copies paces the narrow ones
+double block_time(Pick k) {
+  if (k.cg == 2) return k.bn == 256 ? 0.345 : 0.25;
+  return k.bn <= 64 ? 0.2 : k.bn <= 128 ? 0.222 : k.bn <= 192 ? 0.31 : 0.365;
+}
+
+// (the same whether both gradients are wanted or one)
 Plan plan(const ra_vocab_loss_args& a) {
-  Plan p;
-  p.tiles = (a.vocab + TILE - 1) / TILE;
-  int64_t piece = (64ll << 20) / 4 / (a.tokens > 0 ? a.tokens : 1) / TILE * TILE;
-  if (piece < TILE) piece = TILE;
-  if (piece > (int64_t)p.tiles * TILE) piece = (int64_t)p.tiles * TILE;
-  p.piece = (int)piece;
+  Plan p = {};
+  const bool f32 = a.dtype == RA_F32;
+  p.planes = f32 ? 3 : 1;
+  p.chunk = f32 ? 8 : 128;
+  p.rows = up(a.tokens > 0 ? a.tokens : 1, ROWS);
+  p.pitch = up(a.hidden, 8);
+  // pieces of at most 128 MB of dz
+  int64_t most = (128ll << 20) / (2ll * p.planes * p.rows) / 256 * 256;
+  most = std::max<int64_t>(most, 256);
+  p.pieces = parts_of(a.vocab, (int)std::min<int64_t>(most, 1 << 24));
+  p.width = up(parts_of(a.vocab, p.pieces), 256);
+  p.pieces = parts_of(a.vocab, p.width);
+
+  const int hb = parts_of(a.hidden, prod::BK), terms = prod::terms_of(p.planes).n;
+  auto logits_time = [&](Pick k) {
+    const int64_t tiles = (int64_t)parts_of(a.tokens, prod::BM * k.cg) * parts_of(p.pieces == 1 || !f32 ? a.vocab : p.width, k.bn);
+    return (double)parts_of(tiles, SMS / k.cg) * (hb * terms * block_time(k) + 1.) + (k.cg == 2 ? 1. : 0.);
+  };
+  p.logits = {1, 128};
+  for (Pick k : {Pick{1, 256}, Pick{2, 256}})
+    if ((k.cg == 1 || a.tokens > prod::BM) && logits_time(k) < logits_time(p.logits)) p.logits = k;
+  p.forward = p.logits;
+  if (a.tokens <= prod::BM && !f32) {
+    // few tokens: W's bytes bound, so that the tiles had best be as wide as leaves each SM with equal shares of them
+    const int waves = parts_of(parts_of(a.vocab, 256), SMS);
+    p.forward = {1, std::max(64, std::min(256, up(parts_of(a.vocab, waves * SMS), 32)))};
+  }
+  p.stats = f32 ? p.pieces * 2 * parts_of(p.width, p.forward.bn) : 2 * parts_of(a.vocab, p.forward.bn);
+
+  const int kx = parts_of(p.width, prod::BK), kw = parts_of(a.tokens > 0 ? a.tokens : 1, prod::BK);
+  double best = 1e30;
+  for (Pick k : {Pick{1, 64}, Pick{1, 128}, Pick{1, 256}, Pick{2, 256}}) {
+    if (k.cg == 2 && (a.tokens <= prod::BM || a.hidden <= 128)) continue;
+    if (k.bn > 64 && a.hidden <= k.bn / 2) continue;
+    const int64_t nt = parts_of(a.hidden, k.bn);
+    const int64_t ux = parts_of(a.tokens, prod::BM * k.cg) * nt, uw = parts_of(p.width, prod::BM * k.cg) * nt;
+    const double all = (double)ux * kx + (double)uw * kw, workers = SMS / k.cg;
+    // a tile's k-blocks are cut so that none has more than about a third of a worker's share of all of them
+    auto cut = [&](int kb) { return std::max(1, std::min(std::min(16, kb / 16), (int)(3. * kb * workers / std::max(all, 1.)))); };
+    const int sx = cut(kx), sw = p.pieces == 1 && (int64_t)p.width * a.hidden * 4 * cut(kw) <= (128ll << 20) ? cut(kw) : 1;
+    const double longest = std::max(parts_of(kx, sx), parts_of(kw, sw));
+    const double time = (std::max(all / workers, longest) + 0.3 * longest) * terms * block_time(k) + (double)(ux * sx + uw * sw) / workers * 1.;
+    if (time < best) {
+      best = time;
+      p.grads = k;
+      p.splits_x = sx;
+      p.splits_w = sw;
+    }
+  }
+
   size_t at = WS_ZERO;
   auto take = [&](size_t n) {
     const size_t r = at;
     at += (n + 255) / 256 * 256;
     return r;
   };
-  p.stats = take((size_t)p.tiles * a.tokens * sizeof(float2));
-  p.label = take((size_t)a.tokens * sizeof(float));
-  p.dz = take((size_t)a.tokens * p.piece * sizeof(float));
-  p.dx = take((size_t)a.tokens * a.hidden * sizeof(float));
-  p.bytes = at;
+  p.count = take(4);
+  p.index = take((size_t)p.rows * 4);
+  p.label = take((size_t)p.rows * 4);
+  p.scale = take((size_t)p.rows * 4);
+  p.lse = take((size_t)p.rows * 4);
+  p.zlab = take((size_t)p.rows * 4);
+  p.xc = take((size_t)p.planes * p.rows * p.pitch * 2);
+  p.wc = take(f32 ? (size_t)3 * p.width * p.pitch * 2 : 0);
+  const size_t shared = at;  // what follows is the forward's, or the backward's
+  p.st = take((size_t)p.stats * p.rows * sizeof(float2));
+  const size_t forward = at;
+  at = shared;
+  p.dz = take((size_t)p.planes * p.rows * p.width * 2);
+  p.dxs = take((size_t)p.splits_x * p.rows * p.pitch * 4);
+  p.dws = take(p.splits_w > 1 ? (size_t)p.splits_w * p.width * p.pitch * 4 : 0);
+  p.bytes = a.dx_dev || a.dw_dev ? std::max(at, forward) : forward;
   return p;
 }
 
-// the label of a token that is counted, else -1
-__device__ __forceinline__ int label_of(const ra_vocab_loss_args& a, int t) {
-  const int l = a.labels_dev[t];
-  if (l >= a.vocab) set_dev_error(a.err_dev, RA_DEVERR_BOUNDS);
-  return l < 0 || l >= a.vocab ? -1 : l;
+Prep prep_of(const Plan& p, char* ws) {
+  Prep r;
+  r.count = reinterpret_cast<int*>(ws + p.count);
+  r.index = reinterpret_cast<int*>(ws + p.index);
+  r.label = reinterpret_cast<int*>(ws + p.label);
+  r.scale = reinterpret_cast<float*>(ws + p.scale);
+  r.lse = reinterpret_cast<float*>(ws + p.lse);
+  r.x = ws + p.xc;
+  r.rows = p.rows;
+  r.pitch = p.pitch;
+  r.planes = p.planes;
+  return r;
+}
+cudaError_t prepare(const ra_vocab_loss_args& a, const Prep& r, bool backward, cudaStream_t st) {
+  const int ctas = std::min(parts_of(a.tokens, 32), 2 * SMS);
+  note_launch(1);
+  return a.dtype == RA_BF16 ? launch_pdl(vocab_prep_kernel<bf16>, dim3(ctas), dim3(256), 0, st, a, r, (int)backward)
+                            : launch_pdl(vocab_prep_kernel<float>, dim3(ctas), dim3(256), 0, st, a, r, (int)backward);
 }
 
-template <typename T>
-__device__ __forceinline__ void logits(const ra_vocab_loss_args& a, SimtTile& sh, float (&acc)[4][4], int m0, int n0) {
-  const T* x = static_cast<const T*>(a.x_dev);
-  const T* w = static_cast<const T*>(a.w_dev);
-  simt_tile<true, true>(
-      sh, acc, m0, n0, 0, a.hidden,
-      [&](int m, int k) { return m < a.tokens && (uint32_t)a.labels_dev[m] < (uint32_t)a.vocab ? to_f(x[m * a.x_stride + k]) : 0.f; },
-      [&](int n, int k) { return n < a.vocab ? to_f(w[n * a.w_stride + k]) : 0.f; });
+VocabArgs args_of(const ra_vocab_loss_args& a, const Plan& p, char* ws) {
+  VocabArgs g = {};
+  const Prep r = prep_of(p, ws);
+  g.err = a.err_dev;
+  g.count = r.count;
+  g.label = r.label;
+  g.scale = r.scale;
+  g.lse = r.lse;
+  g.stats = reinterpret_cast<float2*>(ws + p.st);
+  g.zlab = reinterpret_cast<float*>(ws + p.zlab);
+  g.tokens = a.tokens;
+  g.hidden = a.hidden;
+  g.rows = p.rows;
+  g.planes = p.planes;
+  g.dtype = a.dtype;
+  return g;
+}
+#define MAP(m, ...)                                                        \
+  do {                                                                     \
+    if (!tma_map_3d(&(m), __VA_ARGS__)) return cudaErrorInvalidValue;      \
+  } while (0)
+
+// the piece's W, K-major boxes of bn rows or MN-major ones of 64; fp32: its planes, made first
+cudaError_t piece(const ra_vocab_loss_args& a, const Plan& p, char* ws, VocabArgs& g, int v0, int width, cudaStream_t st) {
+  g.v0 = v0;
+  g.width = width;
+  g.wrow = p.planes == 1 ? v0 : 0;
+  if (p.planes == 1) return cudaSuccess;
+  note_launch(1);
+  return launch_pdl(vocab_split_kernel, dim3((unsigned)std::min<int64_t>(((int64_t)width * p.pitch / 4 + 255) / 256, 8 * SMS)), dim3(256), 0, st,
+                    static_cast<const float*>(a.w_dev) + v0 * a.w_stride, a.w_stride, reinterpret_cast<bf16*>(ws + p.wc), width, (int)a.hidden, p.pitch);
+}
+cudaError_t w_map(const ra_vocab_loss_args& a, const Plan& p, char* ws, CUtensorMap& m, int width, int box_rows) {
+  if (p.planes == 1) MAP(m, a.w_dev, DT_BF16, 1, a.vocab, a.hidden, a.w_stride, 64, box_rows);
+  else MAP(m, ws + p.wc, DT_BF16, 3, width, p.pitch, p.pitch, 64, box_rows);
+  return cudaSuccess;
+}
+#define DO(x)                                \
+  do {                                       \
+    const cudaError_t _e = (x);              \
+    if (_e != cudaSuccess) return _e;        \
+  } while (0)
+
+template <class P>
+cudaError_t products(const VocabArgs& g, int64_t units, cudaStream_t st) {
+  const int n = (int)std::min<int64_t>(units, 1 << 20);
+  return g.cg == 2 ? prod::launch<P, 2>(g, n, st) : prod::launch<P, 1>(g, n, st);
+}
+// hidden states as given (bf16) and gathered, in boxes of box_rows rows
+cudaError_t x_maps(const ra_vocab_loss_args& a, const Plan& p, char* ws, CUtensorMap& given, CUtensorMap& gathered, int box_rows) {
+  if (p.planes == 1) MAP(given, a.x_dev, DT_BF16, 1, a.tokens, a.hidden, a.x_stride, 64, box_rows);
+  MAP(gathered, ws + p.xc, DT_BF16, p.planes, p.rows, p.pitch, p.pitch, 64, box_rows);
+  return cudaSuccess;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(ST_THREADS) vocab_stats_kernel(const ra_vocab_loss_args a, float2* stats, float* label) {
-  __shared__ SimtTile sh;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, m0 = blockIdx.y * TILE, n0 = blockIdx.x * TILE;
-  float acc[4][4] = {};
-  logits<T>(a, sh, acc, m0, n0);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int t = m0 + 4 * ty + i;
-    float m = -INFINITY;
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (n0 + 4 * tx + j < a.vocab) m = fmaxf(m, acc[i][j]);
-#pragma unroll
-    for (int o = 8; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    float l = 0.f;
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (n0 + 4 * tx + j < a.vocab) l += expf(acc[i][j] - m);
-#pragma unroll
-    for (int o = 8; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-    if (t >= a.tokens) continue;
-    if (tx == 0) stats[(int64_t)blockIdx.x * a.tokens + t] = make_float2(m, l);
-    const int c = label_of(a, t) - n0 - 4 * tx;
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (c == j) label[t] = acc[i][j];
-  }
-}
-
-__global__ void __launch_bounds__(128) vocab_join_kernel(const ra_vocab_loss_args a, const float2* stats, const float* label, int tiles) {
-  const int t = blockIdx.x * 128 + threadIdx.x;
-  if (t >= a.tokens) return;
-  float lse = 0.f, loss = 0.f;
-  if (label_of(a, t) >= 0) {
-    float m = -INFINITY, l = 0.f;
-    for (int i = 0; i < tiles; ++i) m = fmaxf(m, stats[(int64_t)i * a.tokens + t].x);
-    for (int i = 0; i < tiles; ++i) {
-      const float2 s = stats[(int64_t)i * a.tokens + t];
-      l += s.y * expf(s.x - m);
-    }
-    lse = m + logf(l);
-    loss = lse - label[t];
-  }
-  a.loss_dev[t] = loss;
-  if (a.lse_dev) a.lse_dev[t] = lse;
-}
-
-template <typename T>
-__global__ void __launch_bounds__(ST_THREADS) vocab_dz_kernel(const ra_vocab_loss_args a, float* dz, int v0, int width, int pitch) {
-  __shared__ SimtTile sh;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, m0 = blockIdx.y * TILE, n0 = blockIdx.x * TILE;
-  float acc[4][4] = {};
-  logits<T>(a, sh, acc, m0, v0 + n0);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int t = m0 + 4 * ty + i;
-    if (t >= a.tokens) continue;
-    const int label = label_of(a, t);
-    const float lse = a.lse_dev[t], scale = a.dloss_dev[t];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int c = n0 + 4 * tx + j;
-      if (c < width)
-        dz[(int64_t)t * pitch + c] = label < 0 ? 0.f : scale * (expf(acc[i][j] - lse) - (v0 + c == label ? 1.f : 0.f));
-    }
-  }
-}
-
-template <typename T>
-__global__ void __launch_bounds__(ST_THREADS) vocab_dw_kernel(const ra_vocab_loss_args a, const float* dz, int v0, int width, int pitch) {
-  __shared__ SimtTile sh;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, m0 = blockIdx.y * TILE, n0 = blockIdx.x * TILE;
-  const T* x = static_cast<const T*>(a.x_dev);
-  float acc[4][4] = {};
-  simt_tile<false, false>(
-      sh, acc, m0, n0, 0, a.tokens, [&](int m, int k) { return m < width ? dz[(int64_t)k * pitch + m] : 0.f; },
-      [&](int n, int k) { return n < a.hidden && (uint32_t)a.labels_dev[k] < (uint32_t)a.vocab ? to_f(x[k * a.x_stride + n]) : 0.f; });
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int v = m0 + 4 * ty + i, c = n0 + 4 * tx + j;
-      if (v < width && c < a.hidden) static_cast<T*>(a.dw_dev)[(v0 + v) * a.dw_stride + c] = from_f<T>(acc[i][j]);
-    }
-}
-
-template <typename T>
-__global__ void __launch_bounds__(ST_THREADS) vocab_dx_kernel(const ra_vocab_loss_args a, const float* dz, float* sum, int v0, int width, int pitch) {
-  __shared__ SimtTile sh;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, m0 = blockIdx.y * TILE, n0 = blockIdx.x * TILE;
-  const T* w = static_cast<const T*>(a.w_dev);
-  float acc[4][4] = {};
-  simt_tile<true, false>(
-      sh, acc, m0, n0, 0, width, [&](int m, int k) { return m < a.tokens ? dz[(int64_t)m * pitch + k] : 0.f; },
-      [&](int n, int k) { return n < a.hidden ? to_f(w[(v0 + k) * a.w_stride + n]) : 0.f; });
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int t = m0 + 4 * ty + i, c = n0 + 4 * tx + j;
-      if (t >= a.tokens || c >= a.hidden) continue;
-      float s = acc[i][j];
-      if (v0 > 0) s += sum[(int64_t)t * a.hidden + c];
-      if (v0 + width < a.vocab) sum[(int64_t)t * a.hidden + c] = s;
-      else static_cast<T*>(a.dx_dev)[t * a.dx_stride + c] = label_of(a, t) < 0 ? from_f<T>(0.f) : from_f<T>(s);
-    }
-}
-
-int tiles_of(int n) { return (n + TILE - 1) / TILE; }
-
-template <typename T>
 cudaError_t forward(const ra_vocab_loss_args& a, cudaStream_t st) {
   const Plan p = plan(a);
   char* ws = static_cast<char*>(a.workspace_dev);
-  float2* stats = reinterpret_cast<float2*>(ws + p.stats);
-  float* label = reinterpret_cast<float*>(ws + p.label);
-  vocab_stats_kernel<T><<<dim3(p.tiles, tiles_of(a.tokens)), ST_THREADS, 0, st>>>(a, stats, label);
-  vocab_join_kernel<<<(a.tokens + 127) / 128, 128, 0, st>>>(a, stats, label, p.tiles);
-  note_launch(2);
-  return cudaGetLastError();
+  const Prep r = prep_of(p, ws);
+  DO(prepare(a, r, false, st));
+  VocabArgs g = args_of(a, p, ws);
+  g.cg = p.forward.cg;
+  g.shape = prod::shape_of(p.forward.bn, p.forward.cg, p.planes, p.chunk);
+  DO(x_maps(a, p, ws, g.x, g.xc, prod::BM));
+  const int step = p.planes == 1 ? a.vocab : p.width;
+  for (int v0 = 0; v0 < a.vocab; v0 += step) {
+    const int width = std::min(step, a.vocab - v0);
+    DO(piece(a, p, ws, g, v0, width, st));
+    DO(w_map(a, p, ws, g.w, width, p.forward.bn / p.forward.cg));
+    DO(products<Logits<false>>(g, (int64_t)parts_of(a.tokens, prod::BM * g.cg) * parts_of(width, g.shape.bn), st));
+    g.stat0 += 2 * parts_of(width, g.shape.bn);
+  }
+  note_launch(1);
+  return launch_pdl(vocab_join_kernel, dim3(parts_of(a.tokens, 32)), dim3(512), 0, st, a, r, (const float2*)g.stats, (const float*)g.zlab, (int)g.stat0);
 }
+
 template <typename T>
 cudaError_t backward(const ra_vocab_loss_args& a, cudaStream_t st) {
   const Plan p = plan(a);
   char* ws = static_cast<char*>(a.workspace_dev);
-  float* dz = reinterpret_cast<float*>(ws + p.dz);
-  for (int v0 = 0; v0 < a.vocab; v0 += p.piece) {
-    const int width = a.vocab - v0 < p.piece ? a.vocab - v0 : p.piece;
-    vocab_dz_kernel<T><<<dim3(tiles_of(width), tiles_of(a.tokens)), ST_THREADS, 0, st>>>(a, dz, v0, width, p.piece);
-    if (a.dw_dev) vocab_dw_kernel<T><<<dim3(tiles_of(a.hidden), tiles_of(width)), ST_THREADS, 0, st>>>(a, dz, v0, width, p.piece);
-    if (a.dx_dev)
-      vocab_dx_kernel<T><<<dim3(tiles_of(a.hidden), tiles_of(a.tokens)), ST_THREADS, 0, st>>>(
-          a, dz, reinterpret_cast<float*>(ws + p.dx), v0, width, p.piece);
-    note_launch(3);
+  const Prep r = prep_of(p, ws);
+  DO(prepare(a, r, true, st));
+  VocabArgs g = args_of(a, p, ws), h;
+  g.want_x = a.dx_dev != nullptr;
+  g.want_w = a.dw_dev != nullptr;
+  g.splits_x = p.splits_x;
+  g.splits_w = p.splits_w;
+  DO(x_maps(a, p, ws, g.x, g.xc, prod::BM));
+  DO(x_maps(a, p, ws, g.xm, g.xcm, 64));
+  MAP(g.dxs, ws + p.dxs, DT_F32, p.splits_x, p.rows, a.hidden, p.pitch, 16, 32);
+  if (a.dw_dev) {
+    if (p.splits_w > 1) MAP(g.dw, ws + p.dws, DT_F32, p.splits_w, p.width, a.hidden, p.pitch, 16, 32);
+    else MAP(g.dw, a.dw_dev, a.dtype, 1, a.vocab, a.hidden, a.dw_stride, a.dtype == RA_BF16 ? 32 : 16, 32);
   }
-  return cudaGetLastError();
+  h = g;
+  g.cg = p.logits.cg;
+  g.shape = prod::shape_of(p.logits.bn, p.logits.cg, p.planes, p.chunk);
+  h.cg = p.grads.cg;
+  h.shape = prod::shape_of(p.grads.bn, p.grads.cg, p.planes, p.chunk);
+  for (int v0 = 0; v0 < a.vocab; v0 += p.width) {
+    const int width = std::min(p.width, a.vocab - v0);
+    DO(piece(a, p, ws, g, v0, width, st));
+    DO(w_map(a, p, ws, g.w, width, p.logits.bn / p.logits.cg));
+    MAP(g.dz, ws + p.dz, DT_BF16, p.planes, p.rows, p.width, p.width, 32, 32);
+    DO(products<Logits<true>>(g, (int64_t)parts_of(a.tokens, prod::BM * g.cg) * parts_of(width, g.shape.bn), st));
+    h.v0 = v0;
+    h.width = width;
+    h.wrow = g.wrow;
+    DO(w_map(a, p, ws, h.wm, width, 64));
+    MAP(h.dzk, ws + p.dz, DT_BF16, p.planes, p.rows, p.width, p.width, 64, prod::BM);
+    MAP(h.dzm, ws + p.dz, DT_BF16, p.planes, p.rows, p.width, p.width, 64, 64);
+    const int64_t nt = parts_of(a.hidden, h.shape.bn);
+    DO(products<Grads>(h, nt * ((h.want_x ? (int64_t)parts_of(a.tokens, prod::BM * h.cg) * h.splits_x : 0) +
+                                (h.want_w ? (int64_t)parts_of(width, prod::BM * h.cg) * h.splits_w : 0)), st));
+  }
+  if (a.dw_dev && p.splits_w > 1) {
+    note_launch(1);
+    DO(launch_pdl(vocab_sum_kernel<T>, dim3(std::min(a.vocab, 8 * SMS)), dim3(128), 0, st, (const float*)(ws + p.dws), p.splits_w,
+                  (int64_t)p.width * p.pitch, p.pitch, (int)a.hidden, (const int*)nullptr, (int)a.vocab, (const int*)nullptr,
+                  static_cast<T*>(a.dw_dev), a.dw_stride));
+  }
+  if (a.dx_dev) {
+    note_launch(1);
+    DO(launch_pdl(vocab_sum_kernel<T>, dim3(std::min(a.tokens, 8 * SMS)), dim3(128), 0, st, (const float*)(ws + p.dxs), p.splits_x,
+                  (int64_t)p.rows * p.pitch, p.pitch, (int)a.hidden, (const int*)r.count, 0, (const int*)r.index,
+                  static_cast<T*>(a.dx_dev), a.dx_stride));
+  }
+  return cudaSuccess;
 }
 
 }  // namespace
 
 size_t vocab_loss_workspace(const ra_vocab_loss_args& a) { return plan(a).bytes; }
-cudaError_t vocab_loss_fwd(const ra_vocab_loss_args& a, cudaStream_t st) {
-  return a.dtype == RA_BF16 ? forward<bf16>(a, st) : forward<float>(a, st);
-}
+cudaError_t vocab_loss_fwd(const ra_vocab_loss_args& a, cudaStream_t st) { return forward(a, st); }
 cudaError_t vocab_loss_bwd(const ra_vocab_loss_args& a, cudaStream_t st) {
   if (a.tokens == 0) {
     const size_t es = a.dtype == RA_BF16 ? 2 : 4;

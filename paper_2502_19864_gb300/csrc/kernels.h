@@ -108,6 +108,10 @@ bool tma_map_bf16_batch(CUtensorMap* out, const void* ptr, int batch, int64_t ro
 // 4-D (box_cols, rows, cols / box_cols, planes), a box all column blocks of its rows, one after the other
 bool tma_map_planes(CUtensorMap* out, const void* ptr, int dtype, int planes, int64_t rows, int64_t cols, int box_cols,
                     int box_rows, bool whole_rows);
+// Map of z matrices [rows, cols] of leading dimension ld, rows * ld values apart: (columns, rows, z) in boxes of box_cols x
+// box_rows (rows of 128 bytes under the 128-byte swizzle, of 64 under the 64-byte one)
+bool tma_map_3d(CUtensorMap* out, const void* ptr, int dtype, int z, int64_t rows, int64_t cols, int64_t ld, int box_cols,
+                int box_rows);
 // the 2-D map for float32
 bool tma_map_f32(CUtensorMap* out, const void* ptr, int64_t rows, int64_t cols, int64_t ld, int box_cols,
                  int box_rows);

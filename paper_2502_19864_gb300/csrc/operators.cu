@@ -1,5 +1,6 @@
 // operators.cu -- C ABI of the operators that answer with a tuned decoder and that train all of its weights: argument
 // checks, then the launch.
+#include <algorithm>
 #include <cmath>
 
 #include "operators.h"
@@ -160,6 +161,8 @@ ra_status check_vocab(const ra_vocab_loss_args& a, bool backward) {
   if (a.tokens < 0 || a.vocab < 1 || a.hidden < 1) return RA_ERR_ARG;
   // tokens, words and values are counted in 32 bits, with room for whole tiles
   if (a.hidden % vec(a.dtype) || a.hidden > (1 << 20) || a.tokens > (1 << 24) || a.vocab > (1 << 24)) return RA_ERR_SHAPE;
+  // ... and so are the tiles of the products
+  if ((int64_t)a.tokens * a.vocab > (1ll << 40) || (int64_t)std::max(a.tokens, a.vocab) * a.hidden > (1ll << 37)) return RA_ERR_SHAPE;
   if (backward && a.dw_dev) TRY(check_rows(a.dw_dev, a.dw_stride, 1, a.hidden, a.dtype));
   if (a.tokens == 0) return RA_OK;
   TRY(check_rows(a.x_dev, a.x_stride, 1, a.hidden, a.dtype));

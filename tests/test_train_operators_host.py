@@ -56,7 +56,9 @@ CASES = [
     (BOTH[1:], norm, dict(workspace_dev=P + 16), ARG), (BOTH[1:], norm, dict(workspace_bytes=100), NOMEM),
     (LOSS, loss, dict(dtype=2), ARG), (LOSS, loss, dict(tokens=-1), ARG), (LOSS, loss, dict(vocab=0), ARG), (LOSS, loss, dict(hidden=0), ARG),
     (LOSS, loss, dict(hidden=60), SHAPE), (LOSS, loss, dict(hidden=1 << 21, x_stride=1 << 21), SHAPE), (LOSS, loss, dict(tokens=1 << 25), SHAPE),
-    (LOSS, loss, dict(vocab=1 << 25), SHAPE), (LOSS, loss, dict(x_dev=None), ARG), (LOSS, loss, dict(x_dev=P + 2), ARG),
+    (LOSS, loss, dict(vocab=1 << 25), SHAPE), (LOSS, loss, dict(tokens=1 << 24, vocab=1 << 17), SHAPE),
+    (LOSS, loss, dict(vocab=1 << 20, hidden=1 << 18, x_stride=1 << 18, w_stride=1 << 18, dx_stride=1 << 18, dw_stride=1 << 18), SHAPE),
+    (LOSS, loss, dict(x_dev=None), ARG), (LOSS, loss, dict(x_dev=P + 2), ARG),
     (LOSS, loss, dict(x_stride=68), SHAPE), (LOSS, loss, dict(w_dev=None), ARG), (LOSS, loss, dict(w_stride=56), SHAPE),
     (LOSS, loss, dict(labels_dev=None), ARG), (LOSS, loss, dict(workspace_dev=None), ARG), (LOSS, loss, dict(workspace_bytes=1000), NOMEM),
     (LOSS[:1], loss, dict(loss_dev=None), ARG), (LOSS[1:], loss, dict(lse_dev=None), ARG), (LOSS[1:], loss, dict(dloss_dev=None), ARG),
