@@ -5,7 +5,7 @@
 // Forward: tiles of logits z = x W^T; of each tile's rows the maximum and the sum of exp(z - maximum) go to the workspace,
 // with the label's logit; a second kernel joins them: lse = m + log(sum), loss = lse - z[label].
 // Backward, piece by piece of the vocabulary: the piece's logits again and dz = dloss (exp(z - lse) - onehot) into the
-// workspace; then, in one launch, dw of the piece = dz^T x and the sums of dx += dz W, the latter in fp32 and, where its tiles are
+// workspace (rounded, in bf16, relative to the largest |dloss|); then, in one launch, dw of the piece = dz^T x and the sums of dx += dz W, the latter in fp32 and, where its tiles are
 // few, in parts of the vocabulary, which a last kernel adds up and puts where the tokens were.
 // fp32 operands are cut into three planes of bf16 (products.cuh), dz too; bf16 ones are read where they are.
 #include <algorithm>
@@ -17,10 +17,14 @@
 namespace ra {
 namespace {
 
+using prod::parts_of;
+using prod::Pick;
 using prod::Shape;
+using prod::SMS;
 using prod::Store;
 using prod::Tile;
 using prod::Unit;
+using prod::up;
 
 constexpr float LOG2E = 1.44269504088896341f;
 constexpr int ROWS = 256;  // rows of tokens in the workspace: whole tiles of a pair
@@ -28,7 +32,7 @@ constexpr int ROWS = 256;  // rows of tokens in the workspace: whole tiles of a 
 // ---- which tokens are counted -------------------------------------------------------------
 struct Prep {
   int *count, *index, *label;  // of the counted tokens: how many; each one's place among all, its label,
-  float *scale, *lse;          // ... dloss and lse (backward)
+  float *scale, *lse, *ref;    // ... dloss over the largest of them, lse, and that largest (backward)
   void* x;                     // ... and hidden states: [planes][rows][pitch]
   int rows, pitch, planes;
 };
@@ -83,12 +87,35 @@ __global__ void __launch_bounds__(256) vocab_prep_kernel(const ra_vocab_loss_arg
   const int per = (T_ + gridDim.x - 1) / gridDim.x;
   const int start = min(T_, (int)blockIdx.x * per), end = min(T_, start + per);
   int2 n = make_int2(0, 0);
-  for (int t = tid; t < T_; t += 256) {
-    const bool c = counted(a, a.labels_dev[t]);
-    n.x += c && t < start;
-    n.y += c;
+  float top = 0.f;
+  const bool want_top = backward && p.planes == 1;
+  for (int t0 = tid; t0 < T_; t0 += 2048) {  // eight at once on their way
+    int l[8];
+    float d[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int t = t0 + 256 * i;
+      l[i] = t < T_ ? a.labels_dev[t] : -1;
+      d[i] = want_top && t < T_ ? a.dloss_dev[t] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const bool c = counted(a, l[i]);
+      n.x += c && t0 + 256 * i < start;
+      n.y += c;
+      if (c) top = fmaxf(top, fabsf(d[i]));
+    }
   }
   n = sum2(n, sh);
+  // dz is rounded to bf16 relative to the largest |dloss|: where all are equal, as in a mean, -onehot stays exact, whose
+  // rounding, the same in every row, would be that of the whole gradient (2^-9 at worst)
+  __shared__ float sh_top[8];
+  top = warp_max(top);
+  if (lane == 0) sh_top[warp] = top;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = fmaxf(top, sh_top[i]);
+  if (!(top > 0.f) || !isfinite(top)) top = 1.f;
   int base = n.x;
   const int total = n.y;
   const bool gather = p.planes > 1 || total < T_;
@@ -111,7 +138,7 @@ __global__ void __launch_bounds__(256) vocab_prep_kernel(const ra_vocab_loss_arg
         list[at] = t;
         p.index[base + at] = t;
         p.label[base + at] = l;
-        p.scale[base + at] = backward ? a.dloss_dev[t] : 0.f;
+        p.scale[base + at] = backward ? a.dloss_dev[t] / top : 0.f;
         p.lse[base + at] = backward ? a.lse_dev[t] : 0.f;
       } else {
         if (l >= a.vocab) set_dev_error(a.err_dev, RA_DEVERR_BOUNDS);
@@ -136,14 +163,16 @@ __global__ void __launch_bounds__(256) vocab_prep_kernel(const ra_vocab_loss_arg
   }
   // the rows up to whole tiles
   const int up = (total + ROWS - 1) / ROWS * ROWS;
-  for (int r = total + blockIdx.x; r < up; r += gridDim.x) {
-    if (gather && warp == 0) put_row(p, (const T*)nullptr, r, a.hidden, lane);
-    if (tid == 32) {
-      p.label[r] = -1;
-      p.scale[r] = p.lse[r] = 0.f;
-    }
+  if (gather)
+    for (int r = total + blockIdx.x * 8 + warp; r < up; r += gridDim.x * 8) put_row(p, (const T*)nullptr, r, a.hidden, lane);
+  for (int r = total + blockIdx.x * 256 + tid; r < up; r += gridDim.x * 256) {
+    p.label[r] = -1;
+    p.scale[r] = p.lse[r] = 0.f;
   }
-  if (blockIdx.x == 0 && tid == 0) *p.count = total;
+  if (blockIdx.x == 0 && tid == 0) {
+    *p.count = total;
+    *p.ref = top;
+  }
 }
 
 // rows [row0, row0 + rows) of W into planes
@@ -165,7 +194,7 @@ struct VocabArgs {
   Shape shape;
   unsigned* err;
   const int *count, *label;
-  const float *scale, *lse;
+  const float *scale, *lse, *ref;
   float2* stats;
   float* zlab;
   int tokens, hidden, rows, planes;
@@ -217,17 +246,9 @@ struct Logits {
           const float e = ex2_fast(__fmul_rn(__fsub_rn(v[i][j], lse), LOG2E));
           v[i][j] = j < left ? __fmul_rn(scale, c + j == label ? __fsub_rn(e, 1.f) : e) : 0.f;
         }
-        if (p.planes == 1) {
-          st.bf16_row(&p.dz, v[i], w.n0 + c, row0, 0);
-        } else {
-#pragma unroll 1
-          for (int k = 0; k < 3; ++k) {
-            float h[32];
-#pragma unroll
-            for (int j = 0; j < 32; ++j) h[j] = prod::plane_trunc(v[i][j]);
-            st.bf16_row(&p.dz, h, w.n0 + c, row0, k);
-          }
-        }
+        auto at = [&](int j) { return v[i][j]; };
+        if (p.planes == 1) st.bf16_row(&p.dz, at, w.n0 + c, row0, 0);
+        else st.planes_row(&p.dz, at, w.n0 + c, row0, 0, 3);
       }
     } else {
       float m = -INFINITY;
@@ -314,48 +335,57 @@ struct Grads {
   static __device__ __forceinline__ void finish(const Args& p, const Unit& w, const Tile& t, Store& st, float (&v)[4][32]) {
     const int row0 = w.m0 + t.rank * prod::BM + t.quad * 32;
     if (w.job == 1 && row0 >= p.width) return;
+    const float ref = *p.ref;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int c = w.n0 + 32 * (t.half + 2 * i);
       if (i >= t.chunks || c >= p.hidden) break;
+#pragma unroll
+      for (int j = 0; j < 32; ++j) v[i][j] *= ref;
       if (w.job == 0) st.f32_row(&p.dxs, v[i], c, row0, w.z, p.v0 > 0, p.hidden);
       else if (p.splits_w > 1) st.f32_row(&p.dw, v[i], c, row0, w.z, false, p.hidden);
-      else if (p.dtype == RA_BF16) st.bf16_row(&p.dw, v[i], c, p.v0 + row0, 0);
+      else if (p.dtype == RA_BF16) st.bf16_row(&p.dw, [&](int j) { return v[i][j]; }, c, p.v0 + row0, 0);
       else st.f32_row(&p.dw, v[i], c, p.v0 + row0, 0, false, p.hidden);
     }
   }
 };
 
 // ---- what is joined at the end ------------------------------------------------------------
-// 32 tokens a CTA, its 16 warps on a sixteenth of the parts each
+// eight tokens a CTA, 64 threads on each one's parts
 __global__ void __launch_bounds__(512) vocab_join_kernel(const ra_vocab_loss_args a, const Prep p, const float2* stats, const float* zlab, int parts) {
-  __shared__ float2 sh[16][33];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = blockIdx.x * 32 + lane;
+  __shared__ float2 sh[16][8];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, k = tid & 7, r = blockIdx.x * 8 + k;
   pdl_wait();
   pdl_trigger();
   const int n = *p.count;
-  if ((int)blockIdx.x * 32 >= n) return;
-  float m = -INFINITY, l = 0.f;
+  if ((int)blockIdx.x * 8 >= n) return;
+  // maximum and sum of two parts (-inf and 0, or NaN, where there is nothing, or nothing but NaN)
+  auto join = [](float2 x, float2 y) {
+    const float top = fmaxf(x.x, y.x);
+    if (!(top > -INFINITY)) return make_float2(top, x.y + y.y);
+    return make_float2(top, x.y * ex2_fast((x.x - top) * LOG2E) + y.y * ex2_fast((y.x - top) * LOG2E));
+  };
+  float2 s = make_float2(-INFINITY, 0.f);
   if (r < n)
-#pragma unroll 4
-    for (int i = warp; i < parts; i += 16) {
-      const float2 s = stats[(int64_t)i * p.rows + r];
-      const float top = fmaxf(m, s.x);
-      if (top > -INFINITY) l = l * ex2_fast((m - top) * LOG2E) + s.y * ex2_fast((s.x - top) * LOG2E);
-      else l += s.y;  // (a part of NaN logits alone)
-      m = top;
+    for (int i0 = tid >> 3; i0 < parts; i0 += 256) {  // four at once on their way
+      float2 v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int part = i0 + 64 * i;
+        v[i] = part < parts ? stats[(int64_t)part * p.rows + r] : make_float2(-INFINITY, 0.f);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s = join(s, v[i]);
     }
-  sh[warp][lane] = make_float2(m, l);
+#pragma unroll
+  for (int o = 8; o < 32; o <<= 1) s = join(s, make_float2(__shfl_xor_sync(0xffffffffu, s.x, o), __shfl_xor_sync(0xffffffffu, s.y, o)));
+  if (lane < 8) sh[warp][lane] = s;
   __syncthreads();
-  if (warp || r >= n) return;
-  float top = -INFINITY;
+  if (tid >= 8 || r >= n) return;
+  s = sh[0][k];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) top = fmaxf(top, sh[i][lane].x);
-  l = 0.f;
-#pragma unroll
-  for (int i = 0; i < 16; ++i)
-    if (sh[i][lane].x > -INFINITY || sh[i][lane].y != 0.f) l += sh[i][lane].y * (sh[i][lane].x > -INFINITY ? ex2_fast((sh[i][lane].x - top) * LOG2E) : 1.f);
-  const float lse = top + logf(l);
+  for (int i = 1; i < 16; ++i) s = join(s, sh[i][k]);
+  const float lse = s.x + logf(s.y);
   const int t = p.index[r];
   a.loss_dev[t] = lse - zlab[r];
   if (a.lse_dev) a.lse_dev[t] = lse;
@@ -387,33 +417,22 @@ __global__ void __launch_bounds__(128) vocab_sum_kernel(const float* sums, int s
 }
 
 // ---- the plan -----------------------------------------------------------------------------
-struct Pick {
-  int cg, bn;
-};
-int up(int64_t a, int b) { return (int)((a + b - 1) / b * b); }
-int parts_of(int64_t a, int b) { return (int)((a + b - 1) / b); }
-
 struct Plan {
   int planes, rows, pitch, chunk;
   int pieces, width;              // of the vocabulary, backward (and fp32 forward)
   Pick forward, logits, grads;    // (forward: of its logits)
   int splits_x, splits_w, stats;  // parts of the statistics
-  size_t count, index, label, scale, lse, zlab, xc, wc, st, dz, dxs, dws, bytes;
+  size_t count, index, label, scale, lse, ref, zlab, xc, wc, st, dz, dxs, dws, bytes;
 };
 
-constexpr int SMS = 152;  // a plan is the same on every device
-// microseconds of a k-block of a tile: the issue of products and copies paces the narrow ones
-double block_time(Pick k) {
-  if (k.cg == 2) return k.bn == 256 ? 0.345 : 0.25;
-  return k.bn <= 64 ? 0.2 : k.bn <= 128 ? 0.222 : k.bn <= 192 ? 0.31 : 0.365;
-}
+constexpr int LOGITS_CHUNK = 16;  // k-blocks of an accumulator of logits, whose error is the loss's: 4e-7 of it
 
 // (the same whether both gradients are wanted or one)
 Plan plan(const ra_vocab_loss_args& a) {
   Plan p = {};
   const bool f32 = a.dtype == RA_F32;
   p.planes = f32 ? 3 : 1;
-  p.chunk = f32 ? 8 : 128;
+  p.chunk = f32 ? 4 : 128;
   p.rows = up(a.tokens > 0 ? a.tokens : 1, ROWS);
   p.pitch = up(a.hidden, 8);
   // pieces of at most 128 MB of dz
@@ -424,13 +443,8 @@ Plan plan(const ra_vocab_loss_args& a) {
   p.pieces = parts_of(a.vocab, p.width);
 
   const int hb = parts_of(a.hidden, prod::BK), terms = prod::terms_of(p.planes).n;
-  auto logits_time = [&](Pick k) {
-    const int64_t tiles = (int64_t)parts_of(a.tokens, prod::BM * k.cg) * parts_of(p.pieces == 1 || !f32 ? a.vocab : p.width, k.bn);
-    return (double)parts_of(tiles, SMS / k.cg) * (hb * terms * block_time(k) + 1.) + (k.cg == 2 ? 1. : 0.);
-  };
-  p.logits = {1, 128};
-  for (Pick k : {Pick{1, 256}, Pick{2, 256}})
-    if ((k.cg == 1 || a.tokens > prod::BM) && logits_time(k) < logits_time(p.logits)) p.logits = k;
+  p.logits = prod::pick(a.tokens, p.pieces == 1 || !f32 ? a.vocab : p.width, 1, hb * terms);
+  if (p.logits.bn < 128) p.logits.bn = 128;
   p.forward = p.logits;
   if (a.tokens <= prod::BM && !f32) {
     // few tokens: W's bytes bound, so that the tiles had best be as wide as leaves each SM with equal shares of them
@@ -451,7 +465,7 @@ Plan plan(const ra_vocab_loss_args& a) {
     auto cut = [&](int kb) { return std::max(1, std::min(std::min(16, kb / 16), (int)(3. * kb * workers / std::max(all, 1.)))); };
     const int sx = cut(kx), sw = p.pieces == 1 && (int64_t)p.width * a.hidden * 4 * cut(kw) <= (128ll << 20) ? cut(kw) : 1;
     const double longest = std::max(parts_of(kx, sx), parts_of(kw, sw));
-    const double time = (std::max(all / workers, longest) + 0.3 * longest) * terms * block_time(k) + (double)(ux * sx + uw * sw) / workers * 1.;
+    const double time = (std::max(all / workers, longest) + 0.3 * longest) * terms * prod::block_time(k) + (double)(ux * sx + uw * sw) / workers * 1.;
     if (time < best) {
       best = time;
       p.grads = k;
@@ -471,6 +485,7 @@ Plan plan(const ra_vocab_loss_args& a) {
   p.label = take((size_t)p.rows * 4);
   p.scale = take((size_t)p.rows * 4);
   p.lse = take((size_t)p.rows * 4);
+  p.ref = take(4);
   p.zlab = take((size_t)p.rows * 4);
   p.xc = take((size_t)p.planes * p.rows * p.pitch * 2);
   p.wc = take(f32 ? (size_t)3 * p.width * p.pitch * 2 : 0);
@@ -492,6 +507,7 @@ Prep prep_of(const Plan& p, char* ws) {
   r.label = reinterpret_cast<int*>(ws + p.label);
   r.scale = reinterpret_cast<float*>(ws + p.scale);
   r.lse = reinterpret_cast<float*>(ws + p.lse);
+  r.ref = reinterpret_cast<float*>(ws + p.ref);
   r.x = ws + p.xc;
   r.rows = p.rows;
   r.pitch = p.pitch;
@@ -513,6 +529,7 @@ VocabArgs args_of(const ra_vocab_loss_args& a, const Plan& p, char* ws) {
   g.label = r.label;
   g.scale = r.scale;
   g.lse = r.lse;
+  g.ref = r.ref;
   g.stats = reinterpret_cast<float2*>(ws + p.st);
   g.zlab = reinterpret_cast<float*>(ws + p.zlab);
   g.tokens = a.tokens;
@@ -567,7 +584,7 @@ cudaError_t forward(const ra_vocab_loss_args& a, cudaStream_t st) {
   DO(prepare(a, r, false, st));
   VocabArgs g = args_of(a, p, ws);
   g.cg = p.forward.cg;
-  g.shape = prod::shape_of(p.forward.bn, p.forward.cg, p.planes, p.chunk);
+  g.shape = prod::shape_of(p.forward.bn, p.forward.cg, p.planes, std::min(p.chunk, LOGITS_CHUNK));
   DO(x_maps(a, p, ws, g.x, g.xc, prod::BM));
   const int step = p.planes == 1 ? a.vocab : p.width;
   for (int v0 = 0; v0 < a.vocab; v0 += step) {
@@ -578,7 +595,7 @@ cudaError_t forward(const ra_vocab_loss_args& a, cudaStream_t st) {
     g.stat0 += 2 * parts_of(width, g.shape.bn);
   }
   note_launch(1);
-  return launch_pdl(vocab_join_kernel, dim3(parts_of(a.tokens, 32)), dim3(512), 0, st, a, r, (const float2*)g.stats, (const float*)g.zlab, (int)g.stat0);
+  return launch_pdl(vocab_join_kernel, dim3(parts_of(a.tokens, 8)), dim3(512), 0, st, a, r, (const float2*)g.stats, (const float*)g.zlab, (int)g.stat0);
 }
 
 template <typename T>
@@ -601,7 +618,7 @@ cudaError_t backward(const ra_vocab_loss_args& a, cudaStream_t st) {
   }
   h = g;
   g.cg = p.logits.cg;
-  g.shape = prod::shape_of(p.logits.bn, p.logits.cg, p.planes, p.chunk);
+  g.shape = prod::shape_of(p.logits.bn, p.logits.cg, p.planes, std::min(p.chunk, LOGITS_CHUNK));
   h.cg = p.grads.cg;
   h.shape = prod::shape_of(p.grads.bn, p.grads.cg, p.planes, p.chunk);
   for (int v0 = 0; v0 < a.vocab; v0 += p.width) {

@@ -60,6 +60,30 @@ inline Shape shape_of(int bn, int cg, int planes, int chunk) {
   return s;
 }
 
+// Which tiles: CTAs to a tile, and its columns
+struct Pick {
+  int cg, bn;
+};
+constexpr int SMS = 152;  // a plan is the same on every device
+inline int parts_of(int64_t a, int b) { return (int)((a + b - 1) / b); }
+inline int up(int64_t a, int b) { return (int)((a + b - 1) / b * b); }
+// microseconds of a k-block of a tile (measured on long products; the issue of products and copies paces the narrow ones)
+inline double block_time(Pick k) {
+  if (k.cg == 2) return k.bn == 256 ? 0.345 : 0.25;
+  return k.bn <= 64 ? 0.2 : k.bn <= 128 ? 0.222 : k.bn <= 192 ? 0.31 : 0.365;
+}
+// ... of `batch` products m x n of `blocks` k-blocks: rounds of tiles, each with about 1 us for its start and end
+inline double time_of(Pick k, int64_t m, int64_t n, int64_t batch, int blocks) {
+  const int64_t tiles = batch * parts_of(m, BM * k.cg) * parts_of(n, k.bn);
+  return (double)parts_of(tiles, SMS / k.cg) * (blocks * block_time(k) + 1.) + (k.cg == 2 ? 1. : 0.);
+}
+inline Pick pick(int64_t m, int64_t n, int64_t batch, int blocks) {
+  Pick best = {1, n <= 64 ? 64 : 128};
+  for (Pick k : {Pick{1, 64}, Pick{1, 256}, Pick{2, 256}})
+    if ((k.cg == 1 || m > BM) && n > k.bn / 2 && time_of(k, m, n, batch, blocks) < time_of(best, m, n, batch, blocks)) best = k;
+  return best;
+}
+
 struct Unit {
   const CUtensorMap *a, *b;
   int ar, br;        // the tile's first row of A and of B (of C's columns)
@@ -93,6 +117,25 @@ __device__ __forceinline__ void load(const CUtensorMap* tm, uint32_t dst, uint32
         : "memory");
 }
 
+// The next 8 bits of x's significand and what is left, exactly (truncated, so that no plane overflows and all have x's sign).
+// What is not finite goes into the first plane whole.
+__device__ __forceinline__ float plane_trunc(float& x) {
+  const float h = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+  if (!isfinite(x)) {
+    const float y = x;
+    x = 0.f;
+    return y;
+  }
+  x = __fsub_rn(x, h);
+  return h;
+}
+// The same, rounded: of two planes, 17 bits together.  What is not finite is in none of them
+__device__ __forceinline__ float plane_round(float& x) {
+  const float h = __bfloat162float(__float2bfloat16_rn(x));
+  x = __fsub_rn(x, h);
+  return h;
+}
+
 // What an epilogue warp stores through: boxes of 32 rows x 64 bytes (32 bf16 or 16 fp32 columns), 64-byte swizzled, by TMA
 struct Store {
   uint8_t* staging;
@@ -119,8 +162,9 @@ struct Store {
       asm volatile("cp.async.bulk.commit_group;" ::: "memory");
     }
   }
-  // this thread's row of 32 columns, rounded to bf16
-  __device__ __forceinline__ void bf16_row(const CUtensorMap* tm, const float* v, int col, int row, int z) {
+  // this thread's row of 32 columns f(0), f(1), .., rounded to bf16
+  template <typename F>
+  __device__ __forceinline__ void bf16_row(const CUtensorMap* tm, F f, int col, int row, int z) {
     uint8_t* s = slot();
     const int sw = (lane >> 1) & 3;
 #pragma unroll
@@ -128,10 +172,31 @@ struct Store {
       uint4 x;
       __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&x);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(v[8 * q + 2 * i], v[8 * q + 2 * i + 1]);
+      for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(f(8 * q + 2 * i), f(8 * q + 2 * i + 1));
       *reinterpret_cast<uint4*>(s + lane * 64 + ((q ^ sw) << 4)) = x;
     }
     send(tm, s, col, row, z, false);
+  }
+  // ... in planes at z, z + 1, ..
+  template <typename F>
+  __device__ __forceinline__ void planes_row(const CUtensorMap* tm, F f, int col, int row, int z, int planes) {
+    if (planes == 2) {
+#pragma unroll 1
+      for (int k = 0; k < 2; ++k)
+        bf16_row(tm, [&](int j) {
+          float x = f(j);
+          const float h = plane_round(x);
+          return k == 0 ? h : x;
+        }, col, row, z + k);
+    } else {
+#pragma unroll 1
+      for (int k = 0; k < 3; ++k)
+        bf16_row(tm, [&](int j) {
+          float x = f(j);
+          const float h = plane_trunc(x), m = plane_trunc(x);
+          return k == 0 ? h : k == 1 ? m : x;
+        }, col, row, z + k);
+    }
   }
   // ... in fp32, stored or added to what is there; columns from `cols` on are not the map's
   __device__ __forceinline__ void f32_row(const CUtensorMap* tm, const float* v, int col, int row, int z, bool add, int cols) {
@@ -148,19 +213,6 @@ struct Store {
     }
   }
 };
-
-// The next 8 bits of x's significand and what is left, exactly (truncated, so that no plane overflows and all have x's sign).
-// What is not finite goes into the first plane whole.
-__device__ __forceinline__ float plane_trunc(float& x) {
-  const float h = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
-  if (!isfinite(x)) {
-    const float y = x;
-    x = 0.f;
-    return y;
-  }
-  x = __fsub_rn(x, h);
-  return h;
-}
 
 struct Tile {
   int quad, lane, half;  // TMEM lanes 32 quad.. ; columns 32 (half + 2 i)..
@@ -228,7 +280,7 @@ __global__ void __launch_bounds__(THREADS, 1) products_kernel(const __grid_const
       uint32_t phase = 0;
       bool ok = true;
       const int boxes = (bnc + 63) / 64;
-      const uint32_t bytes = CG * (uint32_t)(A_BYTES) ;
+      const uint32_t bytes = CG * (uint32_t)A_BYTES;
       for (int u = worker; ok && u < units; u += workers) {
         Unit w;
         P::unit(p, u, w);
