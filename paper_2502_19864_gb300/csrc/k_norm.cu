@@ -7,7 +7,11 @@
 // dgamma = sum dy u, dbeta = sum dy, which each CTA keeps in registers over its rows; the CTAs' partial sums are added in
 // a second kernel, in a fixed order.
 //
-// Bound: bytes.  A row is read once, held in registers through both reductions and written once.
+// Bound: bytes.  A row is read once, held in registers through the reductions and written once.  A CTA's threads share a
+// row, eight (16, 32) values each, and take ROWS rows at a time, so that enough loads are on their way and a barrier
+// serves them all.
+#include <algorithm>
+
 #include "common.cuh"
 #include "operators.h"
 
@@ -16,75 +20,105 @@ namespace {
 
 constexpr int NORM_MAX_CTAS = 608;  // four an SM of 152: the backward's partial sums
 
-// VEC values at a VEC-aligned place (VEC 1: anywhere)
-template <typename T, int VEC> struct Pack;
-template <> struct Pack<float, 4> {
-  static __device__ __forceinline__ void load(const float* p, float* v) {
-    const float4 x = *reinterpret_cast<const float4*>(p);
-    v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
-  }
-  static __device__ __forceinline__ void store(float* p, const float* v) {
-    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-  }
+// VEC values at a 16-byte aligned place (VEC 1: anywhere), as they come from memory.  keep(): what was computed of them before is
+// computed again after, and not held in registers of its own in between
+template <typename T, int VEC> struct Raw;
+template <> struct Raw<float, 4> {
+  float4 v;
+  __device__ __forceinline__ void load(const float* p) { v = *reinterpret_cast<const float4*>(p); }
+  __device__ __forceinline__ void get(float* f) const { f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w; }
+  __device__ __forceinline__ void keep() { asm volatile("" : "+f"(v.x), "+f"(v.y), "+f"(v.z), "+f"(v.w)); }
 };
-template <> struct Pack<float, 8> {
-  static __device__ __forceinline__ void load(const float* p, float* v) {
-    Pack<float, 4>::load(p, v);
-    Pack<float, 4>::load(p + 4, v + 4);
-  }
-  static __device__ __forceinline__ void store(float* p, const float* v) {
-    Pack<float, 4>::store(p, v);
-    Pack<float, 4>::store(p + 4, v + 4);
-  }
-};
-template <> struct Pack<bf16, 8> {
-  static __device__ __forceinline__ void load(const bf16* p, float* v) {
-    const uint4 x = *reinterpret_cast<const uint4*>(p);
-    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&x);
+template <> struct Raw<bf16, 8> {
+  uint4 v;
+  __device__ __forceinline__ void load(const bf16* p) { v = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void get(float* f) const {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float2 f = __bfloat1622float2(h[i]);
-      v[2 * i] = f.x;
-      v[2 * i + 1] = f.y;
+      f[2 * i] = __uint_as_float(w[i] << 16);
+      f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
     }
   }
-  static __device__ __forceinline__ void store(bf16* p, const float* v) {
+  __device__ __forceinline__ void keep() { asm volatile("" : "+r"(v.x), "+r"(v.y), "+r"(v.z), "+r"(v.w)); }
+};
+template <> struct Raw<float, 8> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p) {
+    a = reinterpret_cast<const float4*>(p)[0];
+    b = reinterpret_cast<const float4*>(p)[1];
+  }
+  __device__ __forceinline__ void get(float* f) const {
+    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
+    f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+  }
+};
+template <typename T> struct Raw<T, 1> {
+  T v;
+  __device__ __forceinline__ void load(const T* p) { v = *p; }
+  __device__ __forceinline__ void get(float* f) const { f[0] = to_f(v); }
+  __device__ __forceinline__ void keep() {}
+};
+template <int VEC> __device__ __forceinline__ void put(float* p, const float* v) {
+  if (VEC == 1) *p = v[0];
+  else *reinterpret_cast<float4*>(p) = make_float4(v[0], v[VEC > 1 ? 1 : 0], v[VEC > 1 ? 2 : 0], v[VEC > 1 ? 3 : 0]);
+}
+template <int VEC> __device__ __forceinline__ void put(bf16* p, const float* v) {
+  if (VEC == 1) {
+    *p = __float2bfloat16_rn(v[0]);
+  } else {
     uint4 x;
     __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&x);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+    for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(v[VEC > 1 ? 2 * i : 0], v[VEC > 1 ? 2 * i + 1 : 0]);
     *reinterpret_cast<uint4*>(p) = x;
   }
-};
-template <typename T> struct Pack<T, 1> {
-  static __device__ __forceinline__ void load(const T* p, float* v) { v[0] = to_f(p[0]); }
-  static __device__ __forceinline__ void store(T* p, const float* v) { p[0] = from_f<T>(v[0]); }
-};
-
-// Sums of K values over the CTA, for every thread, in a fixed order.  `sh` holds 2 x 32 x K floats, used in turn by
-// successive calls (`turn`), so that one barrier a call is enough.
-template <int K>
-__device__ __forceinline__ void block_sum(float (&v)[K], float* sh, int turn) {
-#pragma unroll
-  for (int k = 0; k < K; ++k) v[k] = warp_sum(v[k]);
-  const int warps = (int)blockDim.x >> 5;
-  if (warps == 1) return;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  float* at = sh + (turn & 1) * 32 * K;
-  if (lane == 0)
-#pragma unroll
-    for (int k = 0; k < K; ++k) at[warp * K + k] = v[k];
-  __syncthreads();
-#pragma unroll
-  for (int k = 0; k < K; ++k) v[k] = warp_sum(lane < warps ? at[lane * K + k] : 0.f);
 }
 
-// the most threads of a CTA: those of 8 and 32 values a thread take the longest rows of their kind
-constexpr int max_threads(int n) { return n == 16 ? 512 : 1024; }
+// Sums of K (a power of two) values over the CTA, for every thread, in a fixed order.  A warp halves the values it carries
+// with the lanes that share them, so that K values cost K + 4 - log2(K) exchanges.  sh holds two parts of 32 K floats,
+// used in turn by successive calls (`turn`), so that one barrier a call is enough.
+template <int K>
+__device__ __forceinline__ void block_sum(float (&v)[K], float* sh, int turn) {
+  const int lane = threadIdx.x & 31, warps = (int)blockDim.x >> 5;
+  int o = 16, idx = 0;
+#pragma unroll
+  for (int k = K / 2; k >= 1; k >>= 1, o >>= 1) {
+    const bool high = lane & o;
+#pragma unroll
+    for (int i = 0; i < k; ++i) {
+      const float give = high ? v[i] : v[i + k], keep = high ? v[i + k] : v[i];
+      v[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+    }
+    idx += high ? k : 0;
+  }
+#pragma unroll
+  for (int p = 16 / K; p >= 1; p >>= 1) v[0] += __shfl_xor_sync(0xffffffffu, v[0], p);
+  if (warps == 1) {
+    const float mine = v[0];
+    // value i is with the lanes whose high bits are i
+#pragma unroll
+    for (int i = 0; i < K; ++i) v[i] = __shfl_sync(0xffffffffu, mine, i * (32 / K));
+    return;
+  }
+  float* at = sh + (turn & 1) * 32 * K;
+  if ((lane & (32 / K - 1)) == 0) at[(threadIdx.x >> 5) * K + idx] = v[0];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < K; ++i) v[i] = at[i];
+  for (int w = 1; w < warps; ++w)
+#pragma unroll
+    for (int i = 0; i < K; ++i) v[i] += at[w * K + i];
+}
 
-template <typename T, typename W, int VEC, int NV>
-__global__ void __launch_bounds__(max_threads(VEC * NV)) norm_fwd_kernel(const ra_norm_args a) {
-  __shared__ float sh[64];
+// the most threads of a CTA by its values a thread: 8 take rows up to 8192 values one by one, up to 2048 four at a time;
+// 16 rows up to 8192; 32 the longest
+constexpr int max_threads(int n, int rows) { return n == 8 && rows == 1 ? 1024 : n == 8 ? 256 : n == 16 ? 512 : 1024; }
+constexpr int min_ctas(int n, int rows) { return n == 8 && rows > 1 ? 2 : 1; }
+
+template <typename T, typename W, int VEC, int NV, int ROWS>
+__global__ void __launch_bounds__(max_threads(VEC * NV, ROWS), min_ctas(VEC * NV, ROWS)) norm_fwd_kernel(const __grid_constant__ ra_norm_args a) {
+  __shared__ __align__(16) float sh1[2 * 32 * ROWS], sh2[2 * 32 * 2 * ROWS];
   constexpr int N = VEC * NV;
   const int t = threadIdx.x, G = blockDim.x, H = a.hidden;
   const bool layer = a.kind == RA_NORM_LAYER;
@@ -94,105 +128,128 @@ __global__ void __launch_bounds__(max_threads(VEC * NV)) norm_fwd_kernel(const r
   pdl_wait();
   pdl_trigger();
   int turn = 0;
-  for (int row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    const T* x = static_cast<const T*>(a.x_dev) + row * a.x_stride;
-    float z[N];
+  for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < a.rows; row0 += (int64_t)gridDim.x * ROWS, ++turn) {
+    float z[ROWS][N];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (i * G + t) * VEC;
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) z[i * VEC + j] = 0.f;
-      if (c < H) Pack<T, VEC>::load(x + c, z + i * VEC);
-    }
-    if (a.residual_dev) {
-      const T* r = static_cast<const T*>(a.residual_dev) + row * a.residual_stride;
+    for (int r = 0; r < ROWS; ++r) {
+      const T* x = static_cast<const T*>(a.x_dev) + (row0 + r) * a.x_stride;
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const int c = (i * G + t) * VEC;
-        if (c < H) {
-          float v[VEC];
-          Pack<T, VEC>::load(r + c, v);
 #pragma unroll
-          for (int j = 0; j < VEC; ++j) z[i * VEC + j] += v[j];
+        for (int j = 0; j < VEC; ++j) z[r][i * VEC + j] = 0.f;
+        if (c < H && row0 + r < a.rows) {
+          Raw<T, VEC> v;
+          v.load(x + c);
+          v.get(z[r] + i * VEC);
         }
       }
-      if (a.sum_dev) {
-        T* s = static_cast<T*>(a.sum_dev) + row * a.sum_stride;
+    }
+    if (a.residual_dev) {
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) {
+        const T* p = static_cast<const T*>(a.residual_dev) + (row0 + r) * a.residual_stride;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
           const int c = (i * G + t) * VEC;
-          if (c < H) Pack<T, VEC>::store(s + c, z + i * VEC);
+          if (c < H && row0 + r < a.rows) {
+            float f[VEC];
+            Raw<T, VEC> v;
+            v.load(p + c);
+            v.get(f);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) z[r][i * VEC + j] += f[j];
+          }
         }
       }
+      if (a.sum_dev)
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+          for (int i = 0; i < NV; ++i) {
+            const int c = (i * G + t) * VEC;
+            if (c < H && row0 + r < a.rows) put<VEC>(static_cast<T*>(a.sum_dev) + (row0 + r) * a.sum_stride + c, z[r] + i * VEC);
+          }
     }
-    float mean = 0.f;
+    float mean[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) mean[r] = 0.f;
     if (layer) {
-      float s[1] = {0.f};
 #pragma unroll
-      for (int i = 0; i < N; ++i) s[0] += z[i];
-      block_sum(s, sh, turn++);
-      mean = s[0] * inv;
+      for (int r = 0; r < ROWS; ++r)
 #pragma unroll
-      for (int i = 0; i < NV; ++i)
-        if ((i * G + t) * VEC < H)
+        for (int i = 0; i < N; ++i) mean[r] += z[r][i];
+      block_sum(mean, sh1, turn);
 #pragma unroll
-          for (int j = 0; j < VEC; ++j) z[i * VEC + j] -= mean;
+      for (int r = 0; r < ROWS; ++r) {
+        mean[r] *= inv;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+          if ((i * G + t) * VEC < H)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) z[r][i * VEC + j] -= mean[r];
+      }
     }
-    float s[2] = {0.f, 0.f};
+    float s[2 * ROWS];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      s[0] = fmaf(z[i], z[i], s[0]);
-      s[1] += z[i];
+    for (int r = 0; r < ROWS; ++r) {
+      s[2 * r] = s[2 * r + 1] = 0.f;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        s[2 * r] = fmaf(z[r][i], z[r][i], s[2 * r]);
+        s[2 * r + 1] += z[r][i];
+      }
     }
-    __shared__ float sh2[128];
     block_sum(s, sh2, turn);
-    float off = 0.f;
-    if (layer) {
-      off = s[1] * inv;
-      mean += off;
+    float off[ROWS], rstd[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      off[r] = layer ? s[2 * r + 1] * inv : 0.f;
+      mean[r] += off[r];
+      rstd[r] = 1.f / sqrtf(fmaxf(s[2 * r] * inv - off[r] * off[r], 0.f) + a.eps);
+      if (s[2 * r] != s[2 * r]) rstd[r] = s[2 * r];  // (fmaxf would lose a NaN)
+      if (t == 0 && row0 + r < a.rows) {
+        if (a.mean_dev && layer) a.mean_dev[row0 + r] = mean[r];
+        if (a.rstd_dev) a.rstd_dev[row0 + r] = rstd[r];
+      }
     }
-    const float rstd = 1.f / sqrtf(fmaxf(s[0] * inv - off * off, 0.f) + a.eps);
-    if (t == 0) {
-      if (a.mean_dev && layer) a.mean_dev[row] = mean;
-      if (a.rstd_dev) a.rstd_dev[row] = rstd;
-    }
-    T* y = static_cast<T*>(a.y_dev) + row * a.y_stride;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (i * G + t) * VEC;
-      if (c < H) {
-        float v[VEC];
+      if (c >= H) continue;
+      float w[VEC], b[VEC];
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) v[j] = (z[i * VEC + j] - off) * rstd;
-        if (gamma) {
-          float w[VEC];
-          Pack<W, VEC>::load(gamma + c, w);
+      for (int j = 0; j < VEC; ++j) w[j] = 1.f, b[j] = 0.f;
+      Raw<W, VEC> v;
+      if (gamma) {
+        v.load(gamma + c);
+        v.get(w);
+      }
+      if (beta) {
+        v.load(beta + c);
+        v.get(b);
+      }
 #pragma unroll
-          for (int j = 0; j < VEC; ++j) v[j] *= w[j];
-        }
-        if (beta) {
-          float w[VEC];
-          Pack<W, VEC>::load(beta + c, w);
+      for (int r = 0; r < ROWS; ++r) {
+        float f[VEC];
 #pragma unroll
-          for (int j = 0; j < VEC; ++j) v[j] += w[j];
-        }
-        Pack<T, VEC>::store(y + c, v);
+        for (int j = 0; j < VEC; ++j) f[j] = fmaf((z[r][i * VEC + j] - off[r]) * rstd[r], w[j], b[j]);
+        if (row0 + r < a.rows) put<VEC>(static_cast<T*>(a.y_dev) + (row0 + r) * a.y_stride + c, f);
       }
     }
-    if (!layer) ++turn;
   }
 }
 
 // sums [2][ctas][hidden]: each CTA's part of dgamma, then of dbeta
-template <typename T, typename W, int VEC, int NV>
-__global__ void __launch_bounds__(max_threads(VEC * NV)) norm_bwd_kernel(const ra_norm_args a, float* sums) {
-  __shared__ float sh[128];
+template <typename T, typename W, int VEC, int NV, int ROWS>
+__global__ void __launch_bounds__(max_threads(VEC * NV, ROWS), min_ctas(VEC * NV, ROWS)) norm_bwd_kernel(const __grid_constant__ ra_norm_args a, float* sums) {
+  __shared__ __align__(16) float sh[2 * 32 * 2 * ROWS];
   constexpr int N = VEC * NV;
   const int t = threadIdx.x, G = blockDim.x, H = a.hidden;
   const bool layer = a.kind == RA_NORM_LAYER;
   const float inv = 1.f / (float)H;
   const W* gamma = static_cast<const W*>(a.gamma_dev);
-  const char* zsrc = static_cast<const char*>(a.residual_dev ? a.sum_dev : a.x_dev);
+  const T* zsrc = static_cast<const T*>(a.residual_dev ? a.sum_dev : a.x_dev);
   const int64_t zstride = a.residual_dev ? a.sum_stride : a.x_stride;
   pdl_wait();
   pdl_trigger();
@@ -203,51 +260,83 @@ __global__ void __launch_bounds__(max_threads(VEC * NV)) norm_bwd_kernel(const r
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (i * G + t) * VEC;
-      if (c < H) Pack<W, VEC>::load(gamma + c, w + i * VEC);
-    }
-  int turn = 0;
-  for (int row = blockIdx.x; row < a.rows; row += gridDim.x, ++turn) {
-    const T* x = reinterpret_cast<const T*>(zsrc) + row * zstride;
-    const T* dy = static_cast<const T*>(a.dy_dev) + row * a.dy_stride;
-    const float mean = layer ? a.mean_dev[row] : 0.f, rstd = a.rstd_dev[row];
-    float u[N], g[N];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (i * G + t) * VEC;
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) u[i * VEC + j] = mean, g[i * VEC + j] = 0.f;
+      Raw<W, VEC> v;
       if (c < H) {
-        Pack<T, VEC>::load(x + c, u + i * VEC);
-        Pack<T, VEC>::load(dy + c, g + i * VEC);
+        v.load(gamma + c);
+        v.get(w + i * VEC);
       }
     }
-    float s[2] = {0.f, 0.f};
+  int turn = 0;
+  for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < a.rows; row0 += (int64_t)gridDim.x * ROWS, ++turn) {
+    Raw<T, VEC> x[ROWS][NV], y[ROWS][NV], d[ROWS][NV];
+    float mean[ROWS], rstd[ROWS];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      u[i] = (u[i] - mean) * rstd;
-      dg[i] = fmaf(g[i], u[i], dg[i]);
-      db[i] += g[i];
-      g[i] *= w[i];
-      s[0] += g[i];
-      s[1] = fmaf(g[i], u[i], s[1]);
+    for (int r = 0; r < ROWS; ++r) {
+      const int64_t row = row0 + r;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int c = (i * G + t) * VEC;
+        if (c < H && row < a.rows) {
+          x[r][i].load(zsrc + row * zstride + c);
+          y[r][i].load(static_cast<const T*>(a.dy_dev) + row * a.dy_stride + c);
+        }
+      }
+      mean[r] = layer && row < a.rows ? a.mean_dev[row] : 0.f;
+      rstd[r] = row < a.rows ? a.rstd_dev[row] : 0.f;
+    }
+    if (a.dsum_dev && a.dx_dev)  // (on their way through the reductions)
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          const int c = (i * G + t) * VEC;
+          if (c < H && row0 + r < a.rows) d[r][i].load(static_cast<const T*>(a.dsum_dev) + (row0 + r) * a.dsum_stride + c);
+        }
+    float s[2 * ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      s[2 * r] = s[2 * r + 1] = 0.f;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if ((i * G + t) * VEC < H && row0 + r < a.rows) {
+          float u[VEC], g[VEC];
+          x[r][i].get(u);
+          y[r][i].get(g);
+#pragma unroll
+          for (int j = 0; j < VEC; ++j) {
+            const int k = i * VEC + j;
+            u[j] = (u[j] - mean[r]) * rstd[r];
+            dg[k] = fmaf(g[j], u[j], dg[k]);
+            db[k] += g[j];
+            g[j] *= w[k];
+            s[2 * r] += g[j];
+            s[2 * r + 1] = fmaf(g[j], u[j], s[2 * r + 1]);
+          }
+        }
     }
     if (!a.dx_dev) continue;
     block_sum(s, sh, turn);
-    const float mg = layer ? s[0] * inv : 0.f, mgu = s[1] * inv;
-    const T* ds = a.dsum_dev ? static_cast<const T*>(a.dsum_dev) + row * a.dsum_stride : nullptr;
-    T* dx = static_cast<T*>(a.dx_dev) + row * a.dx_stride;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (i * G + t) * VEC;
-      if (c < H) {
-        float v[VEC], d[VEC];
-        if (ds) Pack<T, VEC>::load(ds + c, d);
+    for (int r = 0; r < ROWS; ++r) {
+      const float mg = layer ? s[2 * r] * inv : 0.f, mgu = s[2 * r + 1] * inv;
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-          v[j] = (g[i * VEC + j] - mg - u[i * VEC + j] * mgu) * rstd;
-          if (ds) v[j] += d[j];
+      for (int i = 0; i < NV; ++i) {
+        const int c = (i * G + t) * VEC;
+        if (c < H && row0 + r < a.rows) {
+          float u[VEC], g[VEC], e[VEC];
+          x[r][i].keep();
+          y[r][i].keep();
+          x[r][i].get(u);
+          y[r][i].get(g);
+          if (a.dsum_dev) d[r][i].get(e);
+#pragma unroll
+          for (int j = 0; j < VEC; ++j) {
+            u[j] = (u[j] - mean[r]) * rstd[r];
+            g[j] = (g[j] * w[i * VEC + j] - mg - u[j] * mgu) * rstd[r];
+            if (a.dsum_dev) g[j] += e[j];
+          }
+          put<VEC>(static_cast<T*>(a.dx_dev) + (row0 + r) * a.dx_stride + c, g);
         }
-        Pack<T, VEC>::store(dx + c, v);
       }
     }
   }
@@ -287,20 +376,21 @@ __global__ void __launch_bounds__(512) norm_weights_kernel(const float* sums, W*
   }
 }
 
-int bwd_ctas(const ra_norm_args& a) { return a.rows < NORM_MAX_CTAS ? a.rows : NORM_MAX_CTAS; }
+int bwd_ctas(const ra_norm_args& a) { return std::min(a.rows, NORM_MAX_CTAS); }
 
-template <typename T, typename W, int VEC, int NV>
+template <typename T, typename W, int VEC, int NV, int ROWS>
 cudaError_t launch(const ra_norm_args& a, bool backward, cudaStream_t st) {
   const int vecs = (a.hidden + VEC - 1) / VEC;
   const int threads = ((vecs + NV - 1) / NV + 31) / 32 * 32;
+  const int groups = (a.rows + ROWS - 1) / ROWS;
   note_launch(1);
   if (!backward) {
-    const int most = 8 * device_sm_count();
-    return launch_pdl(norm_fwd_kernel<T, W, VEC, NV>, dim3(a.rows < most ? a.rows : most), dim3(threads), 0, st, a);
+    const int most = device_sm_count() * std::max(1, std::min(32, 2048 / threads));
+    return launch_pdl(norm_fwd_kernel<T, W, VEC, NV, ROWS>, dim3(std::min(groups, most)), dim3(threads), 0, st, a);
   }
-  const int ctas = bwd_ctas(a);
+  const int ctas = std::min(groups, NORM_MAX_CTAS);
   float* sums = reinterpret_cast<float*>(static_cast<char*>(a.workspace_dev) + WS_ZERO);
-  cudaError_t e = launch_pdl(norm_bwd_kernel<T, W, VEC, NV>, dim3(ctas), dim3(threads), 0, st, a, sums);
+  cudaError_t e = launch_pdl(norm_bwd_kernel<T, W, VEC, NV, ROWS>, dim3(ctas), dim3(threads), 0, st, a, sums);
   if (e != cudaSuccess || (!a.dgamma_dev && !a.dbeta_dev)) return e;
   note_launch(1);
   return launch_pdl(norm_weights_kernel<W>, dim3((a.hidden + 31) / 32, a.dbeta_dev ? 2 : 1), dim3(512), 0, st,
@@ -319,14 +409,15 @@ cudaError_t dispatch(const ra_norm_args& a, bool backward, cudaStream_t st) {
     wide = wide && at16(a.dy_dev, a.dy_stride, es) && at16(a.dsum_dev, a.dsum_stride, es) && at16(a.dx_dev, a.dx_stride, es);
   else
     wide = wide && at16(a.residual_dev, a.residual_stride, es) && at16(a.y_dev, a.y_stride, es);
+  // several rows at a time where there are enough of them for every SM
+  const bool many = a.rows >= 4 * 608;
   if (wide) {
-    const int vecs = a.hidden / V;
-    if (vecs <= 64) return launch<T, W, V, 1>(a, backward, st);
-    if (a.hidden <= 8192) return launch<T, W, V, 16 / V>(a, backward, st);
-    return launch<T, W, V, 32 / V>(a, backward, st);
+    if (a.hidden <= 2048) return many ? launch<T, W, V, 8 / V, 16 / es / 2>(a, backward, st) : launch<T, W, V, 8 / V, 1>(a, backward, st);
+    if (a.hidden <= 8192) return many ? launch<T, W, V, 16 / V, 4 / es>(a, backward, st) : launch<T, W, V, 8 / V, 1>(a, backward, st);
+    return launch<T, W, V, 32 / V, 1>(a, backward, st);
   }
-  if (a.hidden <= 8192) return launch<T, W, 1, 8>(a, backward, st);
-  return launch<T, W, 1, 32>(a, backward, st);
+  if (a.hidden <= 8192) return a.hidden <= 2048 && many ? launch<T, W, 1, 8, 16 / es / 2>(a, backward, st) : launch<T, W, 1, 8, 1>(a, backward, st);
+  return launch<T, W, 1, 32, 1>(a, backward, st);
 }
 
 cudaError_t any(const ra_norm_args& a, bool backward, cudaStream_t st) {

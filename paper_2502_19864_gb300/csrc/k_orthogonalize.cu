@@ -241,7 +241,7 @@ cudaError_t run(const ra_orthogonalize_args& a, cudaStream_t st) {
                 reinterpret_cast<bf16*>(ws + p.x[0]), a.steps ? p.planes : 0, p.pitch));
   if (a.steps == 0) return cudaSuccess;
 
-  const int terms = prod::terms_of(p.planes).n, chunk = p.planes == 3 ? 8 : 32;
+  const int terms = prod::terms_of(p.planes).n, chunk = p.planes == 3 ? 4 : 32;
   OrthArgs g = {};
   g.err = a.err_dev;
   g.n = n;

@@ -210,8 +210,8 @@ __device__ __forceinline__ const CUtensorMap* hidden_map(const VocabArgs& p, int
   return p.planes == 1 && count == p.tokens ? given : gathered;
 }
 
-// tiles of logits; BACK: into dz, else into statistics
-template <bool BACK>
+// tiles of logits; BACK: into dz, else into statistics; PLANES: of dz
+template <bool BACK, int PLANES = 1>
 struct Logits {
   using Args = VocabArgs;
   static __device__ __forceinline__ int count(const Args& p) {
@@ -247,7 +247,7 @@ struct Logits {
           v[i][j] = j < left ? __fmul_rn(scale, c + j == label ? __fsub_rn(e, 1.f) : e) : 0.f;
         }
         auto at = [&](int j) { return v[i][j]; };
-        if (p.planes == 1) st.bf16_row(&p.dz, at, w.n0 + c, row0, 0);
+        if (PLANES == 1) st.bf16_row(&p.dz, at, w.n0 + c, row0, 0);
         else st.planes_row(&p.dz, at, w.n0 + c, row0, 0, 3);
       }
     } else {
@@ -626,7 +626,9 @@ cudaError_t backward(const ra_vocab_loss_args& a, cudaStream_t st) {
     DO(piece(a, p, ws, g, v0, width, st));
     DO(w_map(a, p, ws, g.w, width, p.logits.bn / p.logits.cg));
     MAP(g.dz, ws + p.dz, DT_BF16, p.planes, p.rows, p.width, p.width, 32, 32);
-    DO(products<Logits<true>>(g, (int64_t)parts_of(a.tokens, prod::BM * g.cg) * parts_of(width, g.shape.bn), st));
+    const int64_t tiles = (int64_t)parts_of(a.tokens, prod::BM * g.cg) * parts_of(width, g.shape.bn);
+    if (p.planes == 1) DO((products<Logits<true, 1>>(g, tiles, st)));
+    else DO((products<Logits<true, 3>>(g, tiles, st)));
     h.v0 = v0;
     h.width = width;
     h.wrow = g.wrow;
