@@ -75,6 +75,72 @@ template <int VEC> __device__ __forceinline__ void put(bf16* p, const float* v) 
   }
 }
 
+// d = a b + c, d = a + b, d = a b of VEC values, two to an instruction; operands that are one value for all as such
+template <int VEC> __device__ __forceinline__ void vfma(float* d, const float* a, const float* b, const float* c) {
+  if constexpr (VEC == 1) d[0] = fmaf(a[0], b[0], c[0]);
+  else
+#pragma unroll
+    for (int j = 0; j < VEC; j += 2) {
+      const float2 r = __ffma2_rn(make_float2(a[j], a[j + 1]), make_float2(b[j], b[j + 1]), make_float2(c[j], c[j + 1]));
+      d[j] = r.x;
+      d[j + 1] = r.y;
+    }
+}
+template <int VEC> __device__ __forceinline__ void vfma1(float* d, const float* a, float b, float c) {
+  if constexpr (VEC == 1) d[0] = fmaf(a[0], b, c);
+  else
+#pragma unroll
+    for (int j = 0; j < VEC; j += 2) {
+      const float2 r = __ffma2_rn(make_float2(a[j], a[j + 1]), make_float2(b, b), make_float2(c, c));
+      d[j] = r.x;
+      d[j + 1] = r.y;
+    }
+}
+template <int VEC> __device__ __forceinline__ void vfmas(float* d, const float* a, float b, const float* c) {
+  if constexpr (VEC == 1) d[0] = fmaf(a[0], b, c[0]);
+  else
+#pragma unroll
+    for (int j = 0; j < VEC; j += 2) {
+      const float2 r = __ffma2_rn(make_float2(a[j], a[j + 1]), make_float2(b, b), make_float2(c[j], c[j + 1]));
+      d[j] = r.x;
+      d[j + 1] = r.y;
+    }
+}
+template <int VEC> __device__ __forceinline__ void vadd(float* d, const float* a, const float* b) {
+  if constexpr (VEC == 1) d[0] = a[0] + b[0];
+  else
+#pragma unroll
+    for (int j = 0; j < VEC; j += 2) {
+      const float2 r = __fadd2_rn(make_float2(a[j], a[j + 1]), make_float2(b[j], b[j + 1]));
+      d[j] = r.x;
+      d[j + 1] = r.y;
+    }
+}
+template <int VEC> __device__ __forceinline__ void vmul(float* d, const float* a, const float* b) {
+  if constexpr (VEC == 1) d[0] = a[0] * b[0];
+  else
+#pragma unroll
+    for (int j = 0; j < VEC; j += 2) {
+      const float2 r = __fmul2_rn(make_float2(a[j], a[j + 1]), make_float2(b[j], b[j + 1]));
+      d[j] = r.x;
+      d[j + 1] = r.y;
+    }
+}
+// 1 / sqrt(v): the special function unit's (2 ulp) and a step of Newton's method
+__device__ __forceinline__ float inv_sqrt(float v) {
+  const float y = rsqrtf(v);
+  const float r = y * fmaf(-0.5f * v * y, y, 1.5f);
+  return y > 0.f && y < INFINITY ? r : y;  // (of 0, infinity and NaN the unit's answer)
+}
+
+// DEPTH groups of ROWS rows in shared memory on their way from `N_IN` inputs, 16 bytes (VEC values) a thread at a place of its own,
+// so that no thread waits for another's copies
+__device__ __forceinline__ void copy16(void* smem, const void* p) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(p) : "memory");
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 // Sums of K (a power of two) values over the CTA, for every thread, in a fixed order.  A warp halves the values it carries
 // with the lanes that share them, so that K values cost K + 4 - log2(K) exchanges.  sh holds two parts of 32 K floats,
 // used in turn by successive calls (`turn`), so that one barrier a call is enough.
@@ -114,10 +180,10 @@ __device__ __forceinline__ void block_sum(float (&v)[K], float* sh, int turn) {
 // the most threads of a CTA by its values a thread: 8 take rows up to 8192 values one by one, up to 2048 four at a time;
 // 16 rows up to 8192; 32 the longest
 constexpr int max_threads(int n, int rows) { return n == 8 && rows == 1 ? 1024 : n == 8 ? 256 : n == 16 ? 512 : 1024; }
-constexpr int min_ctas(int n, int rows) { return n == 8 && rows > 1 ? 2 : 1; }
+constexpr int min_ctas(int n, int rows, bool backward) { return n == 8 && rows > 1 ? (backward ? 2 : 3) : 1; }
 
-template <typename T, typename W, int VEC, int NV, int ROWS>
-__global__ void __launch_bounds__(max_threads(VEC * NV, ROWS), min_ctas(VEC * NV, ROWS)) norm_fwd_kernel(const __grid_constant__ ra_norm_args a) {
+template <typename T, typename W, int VEC, int NV, int ROWS, int DEPTH>
+__global__ void __launch_bounds__(max_threads(VEC * NV, ROWS), min_ctas(VEC * NV, ROWS, false)) norm_fwd_kernel(const __grid_constant__ ra_norm_args a) {
   __shared__ __align__(16) float sh1[2 * 32 * ROWS], sh2[2 * 32 * 2 * ROWS];
   constexpr int N = VEC * NV;
   const int t = threadIdx.x, G = blockDim.x, H = a.hidden;
@@ -127,8 +193,39 @@ __global__ void __launch_bounds__(max_threads(VEC * NV, ROWS), min_ctas(VEC * NV
   const W* beta = static_cast<const W*>(a.beta_dev);
   pdl_wait();
   pdl_trigger();
-  int turn = 0;
-  for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < a.rows; row0 += (int64_t)gridDim.x * ROWS, ++turn) {
+  extern __shared__ __align__(16) uint8_t ring[];  // [DEPTH][inputs][ROWS][NV][G] pieces of 16 bytes
+  const int inputs = a.residual_dev ? 2 : 1;
+  const int64_t step = (int64_t)gridDim.x * ROWS;
+  auto place = [&](int slot, int in, int r, int i) { return ring + ((((slot * inputs + in) * ROWS + r) * NV + i) * G + t) * 16; };
+  auto fetch = [&](int64_t row0, int slot) {
+    if constexpr (DEPTH > 0) {
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          const int c = (i * G + t) * VEC;
+          if (c < H && row0 + r < a.rows) {
+            copy16(place(slot, 0, r, i), static_cast<const T*>(a.x_dev) + (row0 + r) * a.x_stride + c);
+            if (inputs > 1) copy16(place(slot, 1, r, i), static_cast<const T*>(a.residual_dev) + (row0 + r) * a.residual_stride + c);
+          }
+        }
+      copies_end();
+    }
+  };
+  auto from = [&](const T* p, int slot, int in, int r, int i) {
+    Raw<T, VEC> v;
+    if constexpr (DEPTH > 0) v.load(reinterpret_cast<const T*>(place(slot, in, r, i)));
+    else v.load(p);
+    return v;
+  };
+  int turn = 0, slot = 0;
+  if constexpr (DEPTH > 0)
+    for (int d = 0; d + 1 < DEPTH; ++d) fetch((int64_t)blockIdx.x * ROWS + d * step, d);
+  for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < a.rows; row0 += step, ++turn) {
+    if constexpr (DEPTH > 0) {
+      fetch(row0 + (DEPTH - 1) * step, slot == 0 ? DEPTH - 1 : slot - 1);
+      copies_wait<DEPTH - 1>();
+    }
     float z[ROWS][N];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
@@ -138,11 +235,7 @@ __global__ void __launch_bounds__(max_threads(VEC * NV, ROWS), min_ctas(VEC * NV
         const int c = (i * G + t) * VEC;
 #pragma unroll
         for (int j = 0; j < VEC; ++j) z[r][i * VEC + j] = 0.f;
-        if (c < H && row0 + r < a.rows) {
-          Raw<T, VEC> v;
-          v.load(x + c);
-          v.get(z[r] + i * VEC);
-        }
+        if (c < H && row0 + r < a.rows) from(x + c, slot, 0, r, i).get(z[r] + i * VEC);
       }
     }
     if (a.residual_dev) {
@@ -154,11 +247,8 @@ __global__ void __launch_bounds__(max_threads(VEC * NV, ROWS), min_ctas(VEC * NV
           const int c = (i * G + t) * VEC;
           if (c < H && row0 + r < a.rows) {
             float f[VEC];
-            Raw<T, VEC> v;
-            v.load(p + c);
-            v.get(f);
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) z[r][i * VEC + j] += f[j];
+            from(p + c, slot, 1, r, i).get(f);
+            vadd<VEC>(z[r] + i * VEC, z[r] + i * VEC, f);
           }
         }
       }
@@ -171,34 +261,38 @@ __global__ void __launch_bounds__(max_threads(VEC * NV, ROWS), min_ctas(VEC * NV
             if (c < H && row0 + r < a.rows) put<VEC>(static_cast<T*>(a.sum_dev) + (row0 + r) * a.sum_stride + c, z[r] + i * VEC);
           }
     }
+    constexpr int P = N > 1 ? 2 : 1;  // sums in pairs
     float mean[ROWS];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) mean[r] = 0.f;
     if (layer) {
 #pragma unroll
-      for (int r = 0; r < ROWS; ++r)
+      for (int r = 0; r < ROWS; ++r) {
+        float m[P] = {};
 #pragma unroll
-        for (int i = 0; i < N; ++i) mean[r] += z[r][i];
+        for (int i = 0; i < N; i += P) vadd<P>(m, m, z[r] + i);
+        mean[r] = m[0] + (P > 1 ? m[P - 1] : 0.f);
+      }
       block_sum(mean, sh1, turn);
 #pragma unroll
       for (int r = 0; r < ROWS; ++r) {
         mean[r] *= inv;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-          if ((i * G + t) * VEC < H)
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) z[r][i * VEC + j] -= mean[r];
+          if ((i * G + t) * VEC < H) vfma1<VEC>(z[r] + i * VEC, z[r] + i * VEC, 1.f, -mean[r]);
       }
     }
     float s[2 * ROWS];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      s[2 * r] = s[2 * r + 1] = 0.f;
+      float q[P] = {}, m[P] = {};
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        s[2 * r] = fmaf(z[r][i], z[r][i], s[2 * r]);
-        s[2 * r + 1] += z[r][i];
+      for (int i = 0; i < N; i += P) {
+        vfma<P>(q, z[r] + i, z[r] + i, q);
+        if (layer) vadd<P>(m, m, z[r] + i);
       }
+      s[2 * r] = q[0] + (P > 1 ? q[P - 1] : 0.f);
+      s[2 * r + 1] = m[0] + (P > 1 ? m[P - 1] : 0.f);
     }
     block_sum(s, sh2, turn);
     float off[ROWS], rstd[ROWS];
@@ -206,12 +300,13 @@ __global__ void __launch_bounds__(max_threads(VEC * NV, ROWS), min_ctas(VEC * NV
     for (int r = 0; r < ROWS; ++r) {
       off[r] = layer ? s[2 * r + 1] * inv : 0.f;
       mean[r] += off[r];
-      rstd[r] = 1.f / sqrtf(fmaxf(s[2 * r] * inv - off[r] * off[r], 0.f) + a.eps);
-      if (s[2 * r] != s[2 * r]) rstd[r] = s[2 * r];  // (fmaxf would lose a NaN)
+      const float var = fmaf(-off[r], off[r], s[2 * r] * inv);
+      rstd[r] = inv_sqrt((var < 0.f ? 0.f : var) + a.eps);  // (a NaN stays)
       if (t == 0 && row0 + r < a.rows) {
         if (a.mean_dev && layer) a.mean_dev[row0 + r] = mean[r];
         if (a.rstd_dev) a.rstd_dev[row0 + r] = rstd[r];
       }
+      off[r] *= -rstd[r];
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -232,17 +327,18 @@ __global__ void __launch_bounds__(max_threads(VEC * NV, ROWS), min_ctas(VEC * NV
 #pragma unroll
       for (int r = 0; r < ROWS; ++r) {
         float f[VEC];
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) f[j] = fmaf((z[r][i * VEC + j] - off[r]) * rstd[r], w[j], b[j]);
+        vfma1<VEC>(f, z[r] + i * VEC, rstd[r], off[r]);
+        vfma<VEC>(f, f, w, b);
         if (row0 + r < a.rows) put<VEC>(static_cast<T*>(a.y_dev) + (row0 + r) * a.y_stride + c, f);
       }
     }
+    if (DEPTH > 0) slot = slot + 1 == DEPTH ? 0 : slot + 1;
   }
 }
 
 // sums [2][ctas][hidden]: each CTA's part of dgamma, then of dbeta
-template <typename T, typename W, int VEC, int NV, int ROWS>
-__global__ void __launch_bounds__(max_threads(VEC * NV, ROWS), min_ctas(VEC * NV, ROWS)) norm_bwd_kernel(const __grid_constant__ ra_norm_args a, float* sums) {
+template <typename T, typename W, int VEC, int NV, int ROWS, int DEPTH>
+__global__ void __launch_bounds__(max_threads(VEC * NV, ROWS), min_ctas(VEC * NV, ROWS, true)) norm_bwd_kernel(const __grid_constant__ ra_norm_args a, float* sums) {
   __shared__ __align__(16) float sh[2 * 32 * 2 * ROWS];
   constexpr int N = VEC * NV;
   const int t = threadIdx.x, G = blockDim.x, H = a.hidden;
@@ -266,74 +362,114 @@ __global__ void __launch_bounds__(max_threads(VEC * NV, ROWS), min_ctas(VEC * NV
         v.get(w + i * VEC);
       }
     }
-  int turn = 0;
-  for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < a.rows; row0 += (int64_t)gridDim.x * ROWS, ++turn) {
-    Raw<T, VEC> x[ROWS][NV], y[ROWS][NV], d[ROWS][NV];
-    float mean[ROWS], rstd[ROWS];
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-      const int64_t row = row0 + r;
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int c = (i * G + t) * VEC;
-        if (c < H && row < a.rows) {
-          x[r][i].load(zsrc + row * zstride + c);
-          y[r][i].load(static_cast<const T*>(a.dy_dev) + row * a.dy_stride + c);
-        }
-      }
-      mean[r] = layer && row < a.rows ? a.mean_dev[row] : 0.f;
-      rstd[r] = row < a.rows ? a.rstd_dev[row] : 0.f;
-    }
-    if (a.dsum_dev && a.dx_dev)  // (on their way through the reductions)
+  extern __shared__ __align__(16) uint8_t ring[];  // [DEPTH][inputs][ROWS][NV][G] pieces of 16 bytes
+  const bool more = a.dsum_dev && a.dx_dev;
+  const int inputs = more ? 3 : 2;
+  const int64_t step = (int64_t)gridDim.x * ROWS;
+  auto source = [&](int in, int64_t row, int c) {
+    return in == 0 ? zsrc + row * zstride + c
+                   : in == 1 ? static_cast<const T*>(a.dy_dev) + row * a.dy_stride + c : static_cast<const T*>(a.dsum_dev) + row * a.dsum_stride + c;
+  };
+  auto place = [&](int slot, int in, int r, int i) { return ring + ((((slot * inputs + in) * ROWS + r) * NV + i) * G + t) * 16; };
+  auto fetch = [&](int64_t row0, int slot) {
+    if constexpr (DEPTH > 0) {
 #pragma unroll
       for (int r = 0; r < ROWS; ++r)
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
           const int c = (i * G + t) * VEC;
-          if (c < H && row0 + r < a.rows) d[r][i].load(static_cast<const T*>(a.dsum_dev) + (row0 + r) * a.dsum_stride + c);
+          if (c < H && row0 + r < a.rows) {
+            copy16(place(slot, 0, r, i), source(0, row0 + r, c));
+            copy16(place(slot, 1, r, i), source(1, row0 + r, c));
+            if (more) copy16(place(slot, 2, r, i), source(2, row0 + r, c));
+          }
         }
+      copies_end();
+    }
+  };
+  int turn = 0, slot = 0;
+  if constexpr (DEPTH > 0)
+    for (int d = 0; d + 1 < DEPTH; ++d) fetch((int64_t)blockIdx.x * ROWS + d * step, d);
+  for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < a.rows; row0 += step, ++turn) {
+    // (without a ring the rows are held as they came)
+    Raw<T, VEC> held[DEPTH > 0 ? 1 : 3][DEPTH > 0 ? 1 : ROWS][DEPTH > 0 ? 1 : NV];
+    float mean[ROWS], rstd[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      mean[r] = layer && row0 + r < a.rows ? a.mean_dev[row0 + r] : 0.f;
+      rstd[r] = row0 + r < a.rows ? a.rstd_dev[row0 + r] : 0.f;
+    }
+    if constexpr (DEPTH > 0) {
+      fetch(row0 + (DEPTH - 1) * step, slot == 0 ? DEPTH - 1 : slot - 1);
+      copies_wait<DEPTH - 1>();
+    } else {
+#pragma unroll
+      for (int in = 0; in < 3; ++in)
+        if (in < inputs)
+#pragma unroll
+          for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+              const int c = (i * G + t) * VEC;
+              if (c < H && row0 + r < a.rows) held[in][r][i].load(source(in, row0 + r, c));
+            }
+    }
+    auto get = [&](int slot, int in, int r, int i, float* f) {
+      if constexpr (DEPTH > 0) {
+        Raw<T, VEC> v;
+        v.load(reinterpret_cast<const T*>(place(slot, in, r, i)));
+        v.get(f);
+      } else {
+        held[in][r][i].keep();
+        held[in][r][i].get(f);
+      }
+    };
     float s[2 * ROWS];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      s[2 * r] = s[2 * r + 1] = 0.f;
+      mean[r] *= -rstd[r];  // (u = z rstd - mean rstd)
+      constexpr int P = VEC > 1 ? 2 : 1;
+      float s0[P] = {}, s1[P] = {};
 #pragma unroll
       for (int i = 0; i < NV; ++i)
         if ((i * G + t) * VEC < H && row0 + r < a.rows) {
           float u[VEC], g[VEC];
-          x[r][i].get(u);
-          y[r][i].get(g);
+          get(slot, 0, r, i, u);
+          get(slot, 1, r, i, g);
+          vfma1<VEC>(u, u, rstd[r], mean[r]);
+          vfma<VEC>(dg + i * VEC, g, u, dg + i * VEC);
+          vadd<VEC>(db + i * VEC, g, db + i * VEC);
+          vmul<VEC>(g, g, w + i * VEC);
 #pragma unroll
-          for (int j = 0; j < VEC; ++j) {
-            const int k = i * VEC + j;
-            u[j] = (u[j] - mean[r]) * rstd[r];
-            dg[k] = fmaf(g[j], u[j], dg[k]);
-            db[k] += g[j];
-            g[j] *= w[k];
-            s[2 * r] += g[j];
-            s[2 * r + 1] = fmaf(g[j], u[j], s[2 * r + 1]);
+          for (int j = 0; j < VEC; j += P) {
+            vadd<P>(s0, s0, g + j);
+            vfma<P>(s1, g + j, u + j, s1);
           }
         }
+      s[2 * r] = s0[0] + (P > 1 ? s0[P - 1] : 0.f);
+      s[2 * r + 1] = s1[0] + (P > 1 ? s1[P - 1] : 0.f);
     }
+    const int here = slot;
+    if (DEPTH > 0) slot = slot + 1 == DEPTH ? 0 : slot + 1;
     if (!a.dx_dev) continue;
     block_sum(s, sh, turn);
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      const float mg = layer ? s[2 * r] * inv : 0.f, mgu = s[2 * r + 1] * inv;
+      const float mg = layer ? s[2 * r] * inv * -rstd[r] : 0.f, mgu = s[2 * r + 1] * inv * -rstd[r];
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const int c = (i * G + t) * VEC;
         if (c < H && row0 + r < a.rows) {
           float u[VEC], g[VEC], e[VEC];
-          x[r][i].keep();
-          y[r][i].keep();
-          x[r][i].get(u);
-          y[r][i].get(g);
-          if (a.dsum_dev) d[r][i].get(e);
-#pragma unroll
-          for (int j = 0; j < VEC; ++j) {
-            u[j] = (u[j] - mean[r]) * rstd[r];
-            g[j] = (g[j] * w[i * VEC + j] - mg - u[j] * mgu) * rstd[r];
-            if (a.dsum_dev) g[j] += e[j];
+          get(here, 0, r, i, u);
+          get(here, 1, r, i, g);
+          vfma1<VEC>(u, u, rstd[r], mean[r]);
+          vmul<VEC>(g, g, w + i * VEC);
+          vfma1<VEC>(u, u, mgu, mg);
+          vfmas<VEC>(g, g, rstd[r], u);
+          if (more) {
+            get(here, 2, r, i, e);
+            vadd<VEC>(g, g, e);
           }
           put<VEC>(static_cast<T*>(a.dx_dev) + (row0 + r) * a.dx_stride + c, g);
         }
@@ -352,10 +488,11 @@ __global__ void __launch_bounds__(max_threads(VEC * NV, ROWS), min_ctas(VEC * NV
     }
 }
 
-// dgamma and dbeta of 32 columns from `ctas` partial sums: 16 warps take every 16th, then the warps' sums in turn
+// dgamma and dbeta of 32 columns from `ctas` partial sums: 32 warps take every 32nd, eight at once on their way, then the
+// warps' sums in turn
 template <typename W>
-__global__ void __launch_bounds__(512) norm_weights_kernel(const float* sums, W* dgamma, W* dbeta, int ctas, int H) {
-  __shared__ float sh[16][33];
+__global__ void __launch_bounds__(1024) norm_weights_kernel(const float* sums, W* dgamma, W* dbeta, int ctas, int H) {
+  __shared__ float sh[32][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
   W* out = blockIdx.y ? dbeta : dgamma;
   pdl_wait();
@@ -364,39 +501,59 @@ __global__ void __launch_bounds__(512) norm_weights_kernel(const float* sums, W*
   const float* at = sums + (int64_t)blockIdx.y * ctas * H;
   float s = 0.f;
   if (c < H)
-#pragma unroll 8
-    for (int i = warp; i < ctas; i += 16) s += at[(int64_t)i * H + c];
+    for (int i0 = warp; i0 < ctas; i0 += 256) {
+      float v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = i0 + 32 * k < ctas ? at[(int64_t)(i0 + 32 * k) * H + c] : 0.f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s += v[k];
+    }
   sh[warp][lane] = s;
   __syncthreads();
-  if (warp == 0 && c < H) {
-    s = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s += sh[i][lane];
-    out[c] = from_f<W>(s);
-  }
+  s = warp_sum(sh[lane][warp]);  // column `warp`
+  if (lane == 0 && blockIdx.x * 32 + warp < H) out[blockIdx.x * 32 + warp] = from_f<W>(s);
 }
 
 int bwd_ctas(const ra_norm_args& a) { return std::min(a.rows, NORM_MAX_CTAS); }
 
-template <typename T, typename W, int VEC, int NV, int ROWS>
+// CTAs of `threads` with `smem` bytes each that an SM holds, as far as those decide
+int ctas_an_sm(int threads, int smem) { return std::max(1, std::min(2048 / threads, smem ? 227 * 1024 / (smem + 4096) : 32)); }
+
+template <typename T, typename W, int VEC, int NV, int ROWS, int DEPTH = 0>
 cudaError_t launch(const ra_norm_args& a, bool backward, cudaStream_t st) {
   const int vecs = (a.hidden + VEC - 1) / VEC;
   const int threads = ((vecs + NV - 1) / NV + 31) / 32 * 32;
   const int groups = (a.rows + ROWS - 1) / ROWS;
+  const int each = DEPTH * ROWS * NV * threads * 16;  // of the ring, an input
+  constexpr int most_smem = DEPTH * ROWS * NV * max_threads(VEC * NV, ROWS) * 16;
   note_launch(1);
   if (!backward) {
-    const int most = device_sm_count() * std::max(1, std::min(32, 2048 / threads));
-    return launch_pdl(norm_fwd_kernel<T, W, VEC, NV, ROWS>, dim3(std::min(groups, most)), dim3(threads), 0, st, a);
+    auto k = norm_fwd_kernel<T, W, VEC, NV, ROWS, DEPTH>;
+    if (DEPTH > 0) {
+      static const cudaError_t attr = allow_smem(k, std::min(2 * most_smem, MAX_DYNAMIC_SMEM - 4096));
+      if (attr != cudaSuccess) return attr;
+    }
+    const int smem = each * (a.residual_dev ? 2 : 1), most = device_sm_count() * ctas_an_sm(threads, smem);
+    return launch_pdl(k, dim3(std::min(groups, most)), dim3(threads), smem, st, a);
   }
-  const int ctas = std::min(groups, NORM_MAX_CTAS);
+  auto k = norm_bwd_kernel<T, W, VEC, NV, ROWS, DEPTH>;
+  if (DEPTH > 0) {
+    static const cudaError_t attr = allow_smem(k, std::min(3 * most_smem, MAX_DYNAMIC_SMEM - 4096));
+    if (attr != cudaSuccess) return attr;
+  }
+  const int smem = each * (a.dsum_dev && a.dx_dev ? 3 : 2);
+  const int ctas = std::min(std::min(groups, NORM_MAX_CTAS), device_sm_count() * (DEPTH > 0 ? ctas_an_sm(threads, smem) : 4));
   float* sums = reinterpret_cast<float*>(static_cast<char*>(a.workspace_dev) + WS_ZERO);
-  cudaError_t e = launch_pdl(norm_bwd_kernel<T, W, VEC, NV, ROWS>, dim3(ctas), dim3(threads), 0, st, a, sums);
+  cudaError_t e = launch_pdl(k, dim3(ctas), dim3(threads), smem, st, a, sums);
   if (e != cudaSuccess || (!a.dgamma_dev && !a.dbeta_dev)) return e;
   note_launch(1);
-  return launch_pdl(norm_weights_kernel<W>, dim3((a.hidden + 31) / 32, a.dbeta_dev ? 2 : 1), dim3(512), 0, st,
+  return launch_pdl(norm_weights_kernel<W>, dim3((a.hidden + 31) / 32, a.dbeta_dev ? 2 : 1), dim3(1024), 0, st,
                     (const float*)sums, (W*)a.dgamma_dev, (W*)a.dbeta_dev, ctas, (int)a.hidden);
 }
 
+// rows of the ring by their values' size, and its groups (65536 x 1024 and 8192 x 2048 trained: 140 and 54 us; two rows and three
+// groups 154 and 62, three groups 145 and 60; without a ring 173 and 82)
+constexpr int RING_ROWS = 8, RING_DEPTH = 2;
 bool at16(const void* p, int64_t stride, int es) { return !p || (((uintptr_t)p & 15) == 0 && stride * es % 16 == 0); }
 
 template <typename T, typename W>
@@ -412,7 +569,7 @@ cudaError_t dispatch(const ra_norm_args& a, bool backward, cudaStream_t st) {
   // several rows at a time where there are enough of them for every SM
   const bool many = a.rows >= 4 * 608;
   if (wide) {
-    if (a.hidden <= 2048) return many ? launch<T, W, V, 8 / V, 16 / es / 2>(a, backward, st) : launch<T, W, V, 8 / V, 1>(a, backward, st);
+    if (a.hidden <= 2048) return many ? launch<T, W, V, 8 / V, RING_ROWS / es, RING_DEPTH>(a, backward, st) : launch<T, W, V, 8 / V, 1>(a, backward, st);
     if (a.hidden <= 8192) return many ? launch<T, W, V, 16 / V, 4 / es>(a, backward, st) : launch<T, W, V, 8 / V, 1>(a, backward, st);
     return launch<T, W, V, 32 / V, 1>(a, backward, st);
   }
