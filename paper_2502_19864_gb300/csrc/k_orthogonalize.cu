@@ -26,28 +26,44 @@ using prod::Tile;
 using prod::Unit;
 using prod::up;
 
-constexpr int NORM_CTAS = 64;  // parts of a matrix's sum of squares, at most
+constexpr int NORM_CTAS = 512;  // parts of a matrix's sum of squares, at most
 
-template <typename T> __device__ __forceinline__ float value(const void* p, int64_t at) { return to_f(static_cast<const T*>(p)[at]); }
+// VEC elements at c, c + 1, .. of a row (VEC 1: at any place)
+template <typename T, int VEC>
+__device__ __forceinline__ void elements(const T* p, float* v) {
+  if constexpr (VEC == 1) {
+    v[0] = to_f(*p);
+  } else {
+    const uint4 x = *reinterpret_cast<const uint4*>(p);
+    const T* h = reinterpret_cast<const T*>(&x);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) v[i] = to_f(h[i]);
+  }
+}
 
 // Sums of squares of the elements by their size, scaled so that none overflows or vanishes: those above 2^50 by 2^-140, those
-// below 2^-50 by 2^140, and the others.
-template <typename T>
+// below 2^-50 by 2^140, and the others.  A warp a row.
+template <typename T, int VEC>
 __global__ void __launch_bounds__(256) orth_norm_kernel(const ra_orthogonalize_args a, float* norms) {
   pdl_wait();
   pdl_trigger();
   const int m = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   float s[3] = {0.f, 0.f, 0.f};
   for (int r = blockIdx.x * 8 + warp; r < a.rows; r += gridDim.x * 8) {
-    const int64_t base = m * a.x_matrix_stride + r * a.x_stride;
-#pragma unroll 8
-    for (int c = lane; c < a.cols; c += 32) {
-      const float v = value<T>(a.x_dev, base + c), av = fabsf(v);
-      const bool big = av > 0x1p50f, small = av < 0x1p-50f;
-      const float w = v * (big ? 0x1p-70f : small ? 0x1p70f : 1.f), q = w * w;
-      s[0] += big ? q : 0.f;
-      s[1] += big || small ? 0.f : q;
-      s[2] += small ? q : 0.f;
+    const T* row = static_cast<const T*>(a.x_dev) + m * a.x_matrix_stride + r * a.x_stride;
+#pragma unroll 4
+    for (int c = lane * VEC; c < a.cols; c += 32 * VEC) {
+      float v[VEC];
+      elements<T, VEC>(row + c, v);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const float av = fabsf(v[i]);
+        const bool big = av > 0x1p50f, small = av < 0x1p-50f;
+        const float w = v[i] * (big ? 0x1p-70f : small ? 0x1p70f : 1.f), q = w * w;
+        s[0] += big ? q : 0.f;
+        s[1] += big || small ? 0.f : q;
+        s[2] += small ? q : 0.f;
+      }
     }
   }
   __shared__ float sh[8][3];
@@ -67,6 +83,7 @@ __global__ void __launch_bounds__(256) orth_norm_kernel(const ra_orthogonalize_a
 // takes its whole matrix
 struct Scale {
   float p, q, f;
+  __device__ __forceinline__ float power(float v) const { return v * p * q; }
   __device__ __forceinline__ float operator()(float v) const { return v == 0.f && f == f ? 0.f : v * p * f * q; }
 };
 // (by a warp)
@@ -84,54 +101,78 @@ __device__ __forceinline__ Scale scale_of(const float* norms, int parts, float e
   return {ldexpf(1.f, e / 2), ldexpf(1.f, e - e / 2), (float)f};
 }
 
-// The scaled matrices in planes [n][planes][rows][pitch]; or (planes 0) into out
-template <typename T>
-__global__ void __launch_bounds__(256) orth_start_kernel(const ra_orthogonalize_args a, const float* norms, int parts, bf16* x, int planes, int pitch) {
+// The scaled matrices in planes [n][planes][rows][pitch].  One plane (bf16): scaled by the power of two alone, exactly; the
+// factor, which goes to factors[m], is left to the first step's products.  No plane: into out.
+template <typename T, int VEC>
+__global__ void __launch_bounds__(256) orth_start_kernel(const ra_orthogonalize_args a, const float* norms, int parts, float* factors, bf16* x, int planes, int pitch) {
   __shared__ Scale sh;
   pdl_wait();
   pdl_trigger();
   const int m = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (warp == 0) {
     const Scale mine = scale_of(norms + (int64_t)m * parts * 3, parts, a.eps);
-    if (lane == 0) sh = mine;
+    if (lane == 0) {
+      sh = mine;
+      if (blockIdx.x == 0) factors[m] = mine.f;
+    }
   }
   __syncthreads();
   const Scale s = sh;
   const int64_t plane = (int64_t)a.rows * pitch;
   for (int r = blockIdx.x * 8 + warp; r < a.rows; r += gridDim.x * 8) {
-    const int64_t base = m * a.x_matrix_stride + r * a.x_stride;
+    const T* row = static_cast<const T*>(a.x_dev) + m * a.x_matrix_stride + r * a.x_stride;
     if (planes == 0) {
       for (int c = lane; c < a.cols; c += 32)
-        static_cast<T*>(a.out_dev)[m * a.out_matrix_stride + r * a.out_stride + c] = from_f<T>(s(value<T>(a.x_dev, base + c)));
+        static_cast<T*>(a.out_dev)[m * a.out_matrix_stride + r * a.out_stride + c] = from_f<T>(s(to_f(row[c])));
       continue;
     }
     bf16* d = x + ((int64_t)m * planes * a.rows + r) * pitch;
 #pragma unroll 4
-    for (int c = lane; c < pitch; c += 32) {
-      float v = c < a.cols ? s(value<T>(a.x_dev, base + c)) : 0.f;
-      if (planes == 2) {
-        d[c] = __float2bfloat16_rn(prod::plane_round(v));
-        d[plane + c] = __float2bfloat16_rn(v);
+    for (int c = lane * VEC; c < pitch; c += 32 * VEC) {  // (cols is a multiple of VEC)
+      float v[VEC];
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) v[i] = 0.f;
+      if (c < a.cols) elements<T, VEC>(row + c, v);
+      auto store = [&](int k, const bf16* h) {
+        if constexpr (VEC == 1) d[k * plane + c] = h[0];
+        else if constexpr (VEC == 4) *reinterpret_cast<uint2*>(d + k * plane + c) = *reinterpret_cast<const uint2*>(h);
+        else *reinterpret_cast<uint4*>(d + k * plane + c) = *reinterpret_cast<const uint4*>(h);
+      };
+      __align__(16) bf16 h[VEC];
+      if (planes == 1) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) h[i] = __float2bfloat16_rn(s.power(v[i]));
+        store(0, h);
       } else {
 #pragma unroll
-        for (int k = 0; k < 3; ++k) d[k * plane + c] = __float2bfloat16_rn(prod::plane_trunc(v));
+        for (int i = 0; i < VEC; ++i) v[i] = s(v[i]);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) {
+            h[i] = __float2bfloat16_rz(v[i]);
+            prod::plane_trunc(v[i]);
+          }
+          store(k, h);
+        }
       }
     }
   }
 }
 
 struct OrthArgs {
-  CUtensorMap a, b;        // the product's operands
-  CUtensorMap o, o2, out;  // where it goes: planes, T's planes, the result
+  CUtensorMap a, b, out;   // the product's operands; the result
   prod::Shape shape;
   unsigned* err;
+  const float* factors;    // of the first step's matrices: P is scaled by the power'th power of its factor
+  bf16 *o, *o2;            // P + add I and, if wanted, mul2 P + add2 I in planes [n][planes][rows][pitch]
+  int pitch, power;
   void* dst;
   int64_t dst_stride, dst_matrix_stride;
   int rows, cols;          // of the product
-  int k, n, planes, cg, dtype;
-  bool a_mn, b_mn, last, map_out;
-  float add, add2, mul2;   // o = P + add I and, if wanted, o2 = mul2 P + add2 I
-  bool second;
+  int k, n, pa, pb, cg, dtype;
+  bool a_mn, b_mn, sym, last, map_out;
+  float add, add2, mul2;
 };
 #define MAP(m, ...)                                                    \
   do {                                                                 \
@@ -143,12 +184,14 @@ struct OrthArgs {
     if (_e != cudaSuccess) return _e;        \
   } while (0)
 
+template <int PLANES>
 struct Step {
   using Args = OrthArgs;
+  // of a symmetric product (square tiles) those on and above the diagonal, column by column of tiles
   static __host__ __device__ __forceinline__ int tiles(const Args& p, int& mt, int& nt) {
     mt = (p.rows + prod::BM * p.cg - 1) / (prod::BM * p.cg);
     nt = (p.cols + p.shape.bn - 1) / p.shape.bn;
-    return mt * nt;
+    return p.sym ? nt * (nt + 1) / 2 : mt * nt;
   }
   static __device__ __forceinline__ int count(const Args& p) {
     int mt, nt;
@@ -158,24 +201,49 @@ struct Step {
     int m_n, n_n, mt, nt;
     const int each = tiles(p, m_n, n_n);
     w.z = u / each;
-    prod::tile_of(u % each, m_n, n_n, mt, nt);
+    u %= each;
+    if (p.sym) {
+      nt = (int)((sqrtf(8.f * u + 1.f) - 1.f) * 0.5f);
+      while (nt * (nt + 1) / 2 > u) --nt;
+      while ((nt + 1) * (nt + 2) / 2 <= u) ++nt;
+      mt = u - nt * (nt + 1) / 2;
+    } else {
+      prod::tile_of(u, m_n, n_n, mt, nt);
+    }
     w.a = &p.a;
     w.b = &p.b;
     w.m0 = w.ar = mt * prod::BM * p.cg;
     w.n0 = w.br = nt * p.shape.bn;
-    w.ak = w.bk = w.kb0 = w.job = 0;
-    w.az = w.bz = w.z * p.planes;
+    w.ak = w.bk = w.kb0 = 0;
+    w.job = p.sym && mt != nt;  // its mirror image too
+    w.az = w.z * p.pa;
+    w.bz = w.z * p.pb;
     w.kb1 = (p.k + prod::BK - 1) / prod::BK;
     w.a_mn = p.a_mn;
     w.b_mn = p.b_mn;
   }
+  template <typename F>
+  static __device__ __forceinline__ void put(const Args& p, const Unit& w, bf16* to, F f, int row, int col, int lane) {
+    const int64_t plane = (int64_t)p.rows * p.pitch;
+    bf16* base = to + (int64_t)w.z * PLANES * plane;
+    prod::planes_out<PLANES>(base + (int64_t)row * p.pitch + col, plane, f, row < p.rows, p.pitch - col);
+    if (w.job) prod::planes_mirrored<PLANES>(base + (int64_t)col * p.pitch + (row & ~1), plane, f, p.pitch, p.rows - col, row < p.pitch, lane);
+  }
   static __device__ __forceinline__ void finish(const Args& p, const Unit& w, const Tile& t, Store& st, float (&v)[4][32]) {
     const int row0 = w.m0 + t.rank * prod::BM + t.quad * 32, row = row0 + t.lane;
     if (row0 >= p.rows) return;
+    float f = 1.f;
+    if (p.power) {
+      f = p.factors[w.z];
+      if (p.power == 2) f *= f;
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int col = w.n0 + 32 * (t.half + 2 * i);
       if (i >= t.chunks || col >= p.cols) break;
+      if (p.power)
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[i][j] *= f;
       if (p.last) {
         if (p.map_out) {
           if (p.dtype == RA_BF16) st.bf16_row(&p.out, [&](int j) { return v[i][j]; }, col, row0, w.z);
@@ -193,16 +261,15 @@ struct Step {
       }
       // (the identity's part: nothing behind the last row)
       const int diag = row < p.rows ? row - col : -1;
-      st.planes_row(&p.o, [&](int j) { return v[i][j] + (j == diag ? p.add : 0.f); }, col, row0, w.z * p.planes, p.planes);
-      if (p.second)
-        st.planes_row(&p.o2, [&](int j) { return p.mul2 * v[i][j] + (j == diag ? p.add2 : 0.f); }, col, row0, w.z * p.planes, p.planes);
+      put(p, w, p.o, [&](int j) { return v[i][j] + (j == diag ? p.add : 0.f); }, row, col, t.lane);
+      if (p.o2) put(p, w, p.o2, [&](int j) { return p.mul2 * v[i][j] + (j == diag ? p.add2 : 0.f); }, row, col, t.lane);
     }
   }
 };
 
 struct Plan {
   int planes, low, high, pitch, low_pitch, parts;
-  size_t norms, x[2], s, t, q, bytes;
+  size_t norms, factors, x[2], s, t, q, bytes;
 };
 Plan plan(const ra_orthogonalize_args& a) {
   Plan p = {};
@@ -211,7 +278,7 @@ Plan plan(const ra_orthogonalize_args& a) {
   p.high = std::max(a.rows, a.cols);
   p.pitch = up(a.cols, 8);
   p.low_pitch = up(p.low, 8);
-  p.parts = std::min(NORM_CTAS, parts_of(a.rows, 8));
+  p.parts = std::min(std::max(1, NORM_CTAS / a.n_matrices), parts_of(a.rows, 8));
   size_t at = WS_ZERO;
   auto take = [&](size_t n) {
     const size_t r = at;
@@ -220,6 +287,7 @@ Plan plan(const ra_orthogonalize_args& a) {
   };
   const size_t n = (size_t)a.n_matrices * p.planes * 2;
   p.norms = take((size_t)a.n_matrices * p.parts * 3 * 4);
+  p.factors = take((size_t)a.n_matrices * 4);
   for (size_t& x : p.x) x = take(n * a.rows * p.pitch);
   p.s = take(n * p.low * p.low_pitch);
   p.t = take(n * p.low * p.low_pitch);
@@ -228,77 +296,107 @@ Plan plan(const ra_orthogonalize_args& a) {
   return p;
 }
 
+// ... of a symmetric product: square tiles, about half of them
+Pick pick_sym(int rows, int n, int blocks) {
+  auto time = [&](Pick k) {
+    const int64_t t = parts_of(rows, k.bn);
+    return (double)parts_of(n * t * (t + 1) / 2, prod::SMS / k.cg) * (blocks * prod::block_time(k) + 1.5) + (k.cg == 2 ? 1. : 0.);
+  };
+  const Pick one = {1, 128}, two = {2, 256};
+  return rows > 128 && time(two) < time(one) ? two : one;
+}
+
 template <typename T>
 cudaError_t run(const ra_orthogonalize_args& a, cudaStream_t st) {
   const Plan p = plan(a);
   char* ws = static_cast<char*>(a.workspace_dev);
   const int n = a.n_matrices, nz = n * p.planes;
   const bool wide = a.rows <= a.cols;
-  float* norms = reinterpret_cast<float*>(ws + p.norms);
-  note_launch(2);
-  DO(launch_pdl(orth_norm_kernel<T>, dim3(p.parts, n), dim3(256), 0, st, a, norms));
-  DO(launch_pdl(orth_start_kernel<T>, dim3(std::min(parts_of(a.rows, 8), std::max(64, 1216 / n)), n), dim3(256), 0, st, a, (const float*)norms, p.parts,
-                reinterpret_cast<bf16*>(ws + p.x[0]), a.steps ? p.planes : 0, p.pitch));
+  float *norms = reinterpret_cast<float*>(ws + p.norms), *factors = reinterpret_cast<float*>(ws + p.factors);
+  bf16* x[2] = {reinterpret_cast<bf16*>(ws + p.x[0]), reinterpret_cast<bf16*>(ws + p.x[1])};
+  bf16 *s = reinterpret_cast<bf16*>(ws + p.s), *t = reinterpret_cast<bf16*>(ws + p.t), *q = reinterpret_cast<bf16*>(ws + p.q);
+  constexpr int es = sizeof(T), V = 16 / es;
+  // bf16 matrices are one plane as they come
+  const int first = a.steps == 0 ? 0 : es == 2 ? 1 : 3;
+  {
+    const bool vec = ((uintptr_t)a.x_dev & 15) == 0 && a.cols % V == 0 && a.x_stride % V == 0 && (n == 1 || a.x_matrix_stride % V == 0);
+    const dim3 ng(p.parts, n), sg(std::min(parts_of(a.rows, 8), std::max(16, 2432 / n)), n);
+    note_launch(2);
+    DO(launch_pdl(vec ? orth_norm_kernel<T, V> : orth_norm_kernel<T, 1>, ng, dim3(256), 0, st, a, norms));
+    DO(launch_pdl(vec ? orth_start_kernel<T, V> : orth_start_kernel<T, 1>, sg, dim3(256), 0, st, a, (const float*)norms, p.parts, factors, x[0], first,
+                  p.pitch));
+  }
   if (a.steps == 0) return cudaSuccess;
 
-  const int terms = prod::terms_of(p.planes).n, chunk = p.planes == 3 ? 4 : 32;
+  const int chunk = p.planes == 3 ? 4 : 32;
   OrthArgs g = {};
   g.err = a.err_dev;
+  g.factors = factors;
   g.n = n;
-  g.planes = p.planes;
   g.dtype = a.dtype;
-  auto shape = [&](OrthArgs& s, int rows, int cols, int k) {
-    const Pick c = prod::pick(rows, cols, n, parts_of(k, prod::BK) * terms);
+  auto shape = [&](OrthArgs& s, int rows, int cols, int k, int pa, int pb, bool sym) {
+    const prod::Terms terms = prod::terms_of(pa, pb);
+    const int blocks = parts_of(k, prod::BK) * terms.n;
+    const Pick c = sym ? pick_sym(rows, n, blocks) : prod::pick(rows, cols, n, blocks);
     s.rows = rows;
     s.cols = cols;
     s.k = k;
+    s.pa = pa;
+    s.pb = pb;
+    s.sym = sym;
     s.cg = c.cg;
-    s.shape = prod::shape_of(c.bn, c.cg, p.planes, chunk);
+    s.shape = prod::shape_of(c.bn, c.cg, terms, chunk);
   };
   auto go = [&](const OrthArgs& s) {
     int mt, nt;
-    const int64_t units = (int64_t)n * Step::tiles(s, mt, nt);
-    const int u = (int)std::min<int64_t>(units, 1 << 20);
-    return s.cg == 2 ? prod::launch<Step, 2>(s, u, st) : prod::launch<Step, 1>(s, u, st);
+    using S = Step<es == 2 ? 2 : 3>;
+    const int u = (int)std::min<int64_t>((int64_t)n * S::tiles(s, mt, nt), 1 << 20);
+    return s.cg == 2 ? prod::launch<S, 2>(s, u, st) : prod::launch<S, 1>(s, u, st);
   };
-  const int es = a.dtype == RA_BF16 ? 2 : 4;
-  OrthArgs gram = g, square = g, apply = g;
-  shape(gram, p.low, p.low, p.high);
-  gram.a_mn = gram.b_mn = !wide;
-  gram.second = true;
-  gram.add2 = a.b;
-  gram.mul2 = a.c;
-  MAP(gram.o, ws + p.s, DT_BF16, nz, p.low, p.low_pitch, p.low_pitch, 32, 32);
-  MAP(gram.o2, ws + p.t, DT_BF16, nz, p.low, p.low_pitch, p.low_pitch, 32, 32);
-  shape(square, p.low, p.low, p.low);
+  OrthArgs square = g;
+  shape(square, p.low, p.low, p.low, p.planes, p.planes, true);
   square.add = a.a;
-  MAP(square.a, ws + p.s, DT_BF16, nz, p.low, p.low_pitch, p.low_pitch, 64, prod::BM);
-  MAP(square.b, ws + p.t, DT_BF16, nz, p.low, p.low_pitch, p.low_pitch, 64, square.shape.bn / square.cg);
-  MAP(square.o, ws + p.q, DT_BF16, nz, p.low, p.low_pitch, p.low_pitch, 32, 32);
-  shape(apply, a.rows, a.cols, p.low);
-  apply.b_mn = wide;
-  if (wide) MAP(apply.a, ws + p.q, DT_BF16, nz, p.low, p.low_pitch, p.low_pitch, 64, prod::BM);
-  else MAP(apply.b, ws + p.q, DT_BF16, nz, p.low, p.low_pitch, p.low_pitch, 64, apply.shape.bn / apply.cg);
-  apply.dst = a.out_dev;
-  apply.dst_stride = a.out_stride;
-  apply.dst_matrix_stride = a.out_matrix_stride;
-  // the result by TMA where its rows are at 16-byte boundaries and its matrices one after the other
-  apply.map_out = ((uintptr_t)a.out_dev & 15) == 0 && a.out_stride * es % 16 == 0 && (int64_t)a.cols * es % 16 == 0 &&
-                  (n == 1 || a.out_matrix_stride == a.rows * a.out_stride);
-  if (apply.map_out) MAP(apply.out, a.out_dev, a.dtype, n, a.rows, a.cols, a.out_stride, a.dtype == RA_BF16 ? 32 : 16, 32);
+  square.o = q;
+  square.pitch = p.low_pitch;
+  MAP(square.a, s, DT_BF16, nz, p.low, p.low_pitch, p.low_pitch, 64, prod::BM);
+  MAP(square.b, t, DT_BF16, nz, p.low, p.low_pitch, p.low_pitch, 64, square.shape.bn / square.cg);
   for (int i = 0; i < a.steps; ++i) {
-    const char* x = ws + p.x[i & 1];
+    const int px = i == 0 ? first : p.planes;
+    const bf16* from = x[i & 1];
+    OrthArgs gram = g, apply = g;
+    shape(gram, p.low, p.low, p.high, px, px, true);
+    gram.a_mn = gram.b_mn = !wide;
+    gram.power = px == 1 ? 2 : 0;
+    gram.o = s;
+    gram.o2 = t;
+    gram.add2 = a.b;
+    gram.mul2 = a.c;
+    gram.pitch = p.low_pitch;
+    shape(apply, a.rows, a.cols, p.low, wide ? p.planes : px, wide ? px : p.planes, false);
+    apply.b_mn = wide;
+    apply.power = px == 1 ? 1 : 0;
+    apply.o = x[(i + 1) & 1];
+    apply.pitch = p.pitch;
     if (wide) {
-      MAP(gram.a, x, DT_BF16, nz, a.rows, p.pitch, p.pitch, 64, prod::BM);
-      MAP(gram.b, x, DT_BF16, nz, a.rows, p.pitch, p.pitch, 64, gram.shape.bn / gram.cg);
-      MAP(apply.b, x, DT_BF16, nz, a.rows, p.pitch, p.pitch, 64, 64);
+      MAP(gram.a, from, DT_BF16, n * px, a.rows, p.pitch, p.pitch, 64, prod::BM);
+      MAP(gram.b, from, DT_BF16, n * px, a.rows, p.pitch, p.pitch, 64, gram.shape.bn / gram.cg);
+      MAP(apply.a, q, DT_BF16, nz, p.low, p.low_pitch, p.low_pitch, 64, prod::BM);
+      MAP(apply.b, from, DT_BF16, n * px, a.rows, p.pitch, p.pitch, 64, 64);
     } else {
-      MAP(gram.a, x, DT_BF16, nz, a.rows, p.pitch, p.pitch, 64, 64);
+      MAP(gram.a, from, DT_BF16, n * px, a.rows, p.pitch, p.pitch, 64, 64);
       gram.b = gram.a;
-      MAP(apply.a, x, DT_BF16, nz, a.rows, p.pitch, p.pitch, 64, prod::BM);
+      MAP(apply.a, from, DT_BF16, n * px, a.rows, p.pitch, p.pitch, 64, prod::BM);
+      MAP(apply.b, q, DT_BF16, nz, p.low, p.low_pitch, p.low_pitch, 64, apply.shape.bn / apply.cg);
     }
-    MAP(apply.o, ws + p.x[(i + 1) & 1], DT_BF16, nz, a.rows, p.pitch, p.pitch, 32, 32);
-    apply.last = i + 1 == a.steps;
+    if ((apply.last = i + 1 == a.steps)) {
+      apply.dst = a.out_dev;
+      apply.dst_stride = a.out_stride;
+      apply.dst_matrix_stride = a.out_matrix_stride;
+      // by TMA where rows are at 16-byte boundaries and matrices one after the other
+      apply.map_out = ((uintptr_t)a.out_dev & 15) == 0 && a.out_stride * es % 16 == 0 && (int64_t)a.cols * es % 16 == 0 &&
+                      (n == 1 || a.out_matrix_stride == a.rows * a.out_stride);
+      if (apply.map_out) MAP(apply.out, a.out_dev, a.dtype, n, a.rows, a.cols, a.out_stride, es == 2 ? 32 : 16, 32);
+    }
     DO(go(gram));
     DO(go(square));
     DO(go(apply));

@@ -59,17 +59,11 @@ __device__ __forceinline__ void put_row(const Prep& p, const bf16* src, int r, i
     *reinterpret_cast<uint4*>(d + c) = src ? *reinterpret_cast<const uint4*>(src + c) : make_uint4(0, 0, 0, 0);
 }
 __device__ __forceinline__ void split4(float4 v, bf16* d, int64_t plane) {
-  float x[4] = {v.x, v.y, v.z, v.w};
+  uint32_t x[3], y[3];
+  prod::planes_of<3>(v.x, v.y, x);
+  prod::planes_of<3>(v.z, v.w, y);
 #pragma unroll
-  for (int k = 0; k < 3; ++k) {
-    __nv_bfloat162 h[2];
-    float y[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = prod::plane_trunc(x[i]);
-    h[0] = __floats2bfloat162_rn(y[0], y[1]);
-    h[1] = __floats2bfloat162_rn(y[2], y[3]);
-    *reinterpret_cast<uint2*>(d + k * plane) = *reinterpret_cast<uint2*>(h);
-  }
+  for (int k = 0; k < 3; ++k) *reinterpret_cast<uint2*>(d + k * plane) = make_uint2(x[k], y[k]);
 }
 __device__ __forceinline__ void put_row(const Prep& p, const float* src, int r, int H, int lane) {
   bf16* d = static_cast<bf16*>(p.x) + (int64_t)r * p.pitch;
@@ -197,6 +191,8 @@ struct VocabArgs {
   const float *scale, *lse, *ref;
   float2* stats;
   float* zlab;
+  bf16* dzp;                    // fp32: dz's planes
+  int dz_pitch;
   int tokens, hidden, rows, planes;
   int v0, width;                // the piece: words v0 .. v0 + width
   int wrow;                     // where it begins in the map of W
@@ -248,7 +244,7 @@ struct Logits {
         }
         auto at = [&](int j) { return v[i][j]; };
         if (PLANES == 1) st.bf16_row(&p.dz, at, w.n0 + c, row0, 0);
-        else st.planes_row(&p.dz, at, w.n0 + c, row0, 0, 3);
+        else prod::planes_out<3>(p.dzp + (int64_t)row * p.dz_pitch + w.n0 + c, (int64_t)p.rows * p.dz_pitch, at, true, 32);
       }
     } else {
       float m = -INFINITY;
@@ -427,6 +423,7 @@ struct Plan {
 
 constexpr int LOGITS_CHUNK = 16;  // k-blocks of an accumulator of logits, whose error is the loss's: 4e-7 of it
 
+prod::Terms terms_for(int planes) { return prod::terms_of(planes, planes); }
 // (the same whether both gradients are wanted or one)
 Plan plan(const ra_vocab_loss_args& a) {
   Plan p = {};
@@ -442,7 +439,7 @@ Plan plan(const ra_vocab_loss_args& a) {
   p.width = up(parts_of(a.vocab, p.pieces), 256);
   p.pieces = parts_of(a.vocab, p.width);
 
-  const int hb = parts_of(a.hidden, prod::BK), terms = prod::terms_of(p.planes).n;
+  const int hb = parts_of(a.hidden, prod::BK), terms = terms_for(p.planes).n;
   p.logits = prod::pick(a.tokens, p.pieces == 1 || !f32 ? a.vocab : p.width, 1, hb * terms);
   if (p.logits.bn < 128) p.logits.bn = 128;
   p.forward = p.logits;
@@ -532,6 +529,8 @@ VocabArgs args_of(const ra_vocab_loss_args& a, const Plan& p, char* ws) {
   g.ref = r.ref;
   g.stats = reinterpret_cast<float2*>(ws + p.st);
   g.zlab = reinterpret_cast<float*>(ws + p.zlab);
+  g.dzp = reinterpret_cast<bf16*>(ws + p.dz);
+  g.dz_pitch = p.width;
   g.tokens = a.tokens;
   g.hidden = a.hidden;
   g.rows = p.rows;
@@ -584,7 +583,7 @@ cudaError_t forward(const ra_vocab_loss_args& a, cudaStream_t st) {
   DO(prepare(a, r, false, st));
   VocabArgs g = args_of(a, p, ws);
   g.cg = p.forward.cg;
-  g.shape = prod::shape_of(p.forward.bn, p.forward.cg, p.planes, std::min(p.chunk, LOGITS_CHUNK));
+  g.shape = prod::shape_of(p.forward.bn, p.forward.cg, terms_for(p.planes), std::min(p.chunk, LOGITS_CHUNK));
   DO(x_maps(a, p, ws, g.x, g.xc, prod::BM));
   const int step = p.planes == 1 ? a.vocab : p.width;
   for (int v0 = 0; v0 < a.vocab; v0 += step) {
@@ -618,9 +617,9 @@ cudaError_t backward(const ra_vocab_loss_args& a, cudaStream_t st) {
   }
   h = g;
   g.cg = p.logits.cg;
-  g.shape = prod::shape_of(p.logits.bn, p.logits.cg, p.planes, std::min(p.chunk, LOGITS_CHUNK));
+  g.shape = prod::shape_of(p.logits.bn, p.logits.cg, terms_for(p.planes), std::min(p.chunk, LOGITS_CHUNK));
   h.cg = p.grads.cg;
-  h.shape = prod::shape_of(p.grads.bn, p.grads.cg, p.planes, p.chunk);
+  h.shape = prod::shape_of(p.grads.bn, p.grads.cg, terms_for(p.planes), p.chunk);
   for (int v0 = 0; v0 < a.vocab; v0 += p.width) {
     const int width = std::min(p.width, a.vocab - v0);
     DO(piece(a, p, ws, g, v0, width, st));

@@ -37,11 +37,18 @@ struct Terms {
   int n;
   uint32_t a, b;
 };
-__host__ __device__ inline Terms terms_of(int planes) {
-  if (planes == 1) return {1, 0u, 0u};
-  if (planes == 2) return {3, 0u | 1u << 2 | 0u << 4, 1u | 0u << 2 | 0u << 4};
-  // (0, 2) (2, 0) (1, 1) (0, 1) (1, 0) (0, 0): what is left out is below 2^-24 of the whole
-  return {6, 0u | 2u << 2 | 1u << 4 | 0u << 6 | 1u << 8 | 0u << 10, 2u | 0u << 2 | 1u << 4 | 1u << 6 | 0u << 8 | 0u << 10};
+// Of operands of pa and pb planes: all pairs (i, j) with i + j less than the larger number; what is left out is below 2^-8 of
+// the last plane's part (three planes: (0, 2) (1, 1) (2, 0) (0, 1) (1, 0) (0, 0), 2^-24 of the whole)
+inline Terms terms_of(int pa, int pb) {
+  Terms t = {0, 0u, 0u};
+  for (int sum = (pa > pb ? pa : pb) - 1; sum >= 0; --sum)
+    for (int i = 0; i <= sum; ++i)
+      if (i < pa && sum - i < pb) {
+        t.a |= (uint32_t)i << (2 * t.n);
+        t.b |= (uint32_t)(sum - i) << (2 * t.n);
+        ++t.n;
+      }
+  return t;
 }
 
 struct Shape {
@@ -50,13 +57,13 @@ struct Shape {
   int stages, stage_bytes;
   Terms terms;
 };
-inline Shape shape_of(int bn, int cg, int planes, int chunk) {
+inline Shape shape_of(int bn, int cg, Terms terms, int chunk) {
   Shape s;
   s.bn = bn;
   s.chunk = chunk;
   s.stage_bytes = A_BYTES + (bn / cg + 63) / 64 * 64 * BK * 2;
   s.stages = RING / s.stage_bytes < MAX_STAGES ? RING / s.stage_bytes : MAX_STAGES;
-  s.terms = terms_of(planes);
+  s.terms = terms;
   return s;
 }
 
@@ -69,7 +76,7 @@ inline int parts_of(int64_t a, int b) { return (int)((a + b - 1) / b); }
 inline int up(int64_t a, int b) { return (int)((a + b - 1) / b * b); }
 // microseconds of a k-block of a tile (measured on long products; the issue of products and copies paces the narrow ones)
 inline double block_time(Pick k) {
-  if (k.cg == 2) return k.bn == 256 ? 0.345 : 0.25;
+  if (k.cg == 2) return k.bn > 224 ? 0.345 : k.bn > 128 ? 0.31 : 0.25;
   return k.bn <= 64 ? 0.2 : k.bn <= 128 ? 0.222 : k.bn <= 192 ? 0.31 : 0.365;
 }
 // ... of `batch` products m x n of `blocks` k-blocks: rounds of tiles, each with about 1 us for its start and end
@@ -79,7 +86,7 @@ inline double time_of(Pick k, int64_t m, int64_t n, int64_t batch, int blocks) {
 }
 inline Pick pick(int64_t m, int64_t n, int64_t batch, int blocks) {
   Pick best = {1, n <= 64 ? 64 : 128};
-  for (Pick k : {Pick{1, 64}, Pick{1, 256}, Pick{2, 256}})
+  for (Pick k : {Pick{1, 64}, Pick{1, 256}, Pick{2, 224}, Pick{2, 256}})
     if ((k.cg == 1 || m > BM) && n > k.bn / 2 && time_of(k, m, n, batch, blocks) < time_of(best, m, n, batch, blocks)) best = k;
   return best;
 }
@@ -118,22 +125,61 @@ __device__ __forceinline__ void load(const CUtensorMap* tm, uint32_t dst, uint32
 }
 
 // The next 8 bits of x's significand and what is left, exactly (truncated, so that no plane overflows and all have x's sign).
-// What is not finite goes into the first plane whole.
+// What is not finite leaves NaN.
 __device__ __forceinline__ float plane_trunc(float& x) {
   const float h = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
-  if (!isfinite(x)) {
-    const float y = x;
-    x = 0.f;
-    return y;
-  }
   x = __fsub_rn(x, h);
   return h;
 }
-// The same, rounded: of two planes, 17 bits together.  What is not finite is in none of them
-__device__ __forceinline__ float plane_round(float& x) {
-  const float h = __bfloat162float(__float2bfloat16_rn(x));
-  x = __fsub_rn(x, h);
-  return h;
+// Two values' planes, a word of two bf16 each: three truncated ones (exact: the words are the upper halves), or two rounded
+template <int PLANES>
+__device__ __forceinline__ void planes_of(float x, float y, uint32_t (&w)[PLANES]) {
+  if constexpr (PLANES == 3) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      w[k] = __byte_perm(__float_as_uint(x), __float_as_uint(y), 0x7632);
+      plane_trunc(x);
+      plane_trunc(y);
+    }
+    w[2] = __byte_perm(__float_as_uint(x), __float_as_uint(y), 0x7632);
+  } else {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+    w[0] = *reinterpret_cast<const uint32_t*>(&h);
+    const __nv_bfloat162 l = __floats2bfloat162_rn(__fsub_rn(x, __uint_as_float(w[0] << 16)), __fsub_rn(y, __uint_as_float(w[0] & 0xffff0000u)));
+    w[1] = *reinterpret_cast<const uint32_t*>(&l);
+  }
+}
+// 32 columns f(0), f(1), .. of a row to its planes, `plane` values apart, from registers, 16 bytes at a time; `left`: how many of
+// the columns (a multiple of 8) are there
+template <int PLANES, typename F>
+__device__ __forceinline__ void planes_out(bf16* to, int64_t plane, F f, bool row_ok, int left) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    uint32_t w[4][PLANES];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) planes_of<PLANES>(f(8 * q + 2 * i), f(8 * q + 2 * i + 1), w[i]);
+#pragma unroll
+    for (int k = 0; k < PLANES; ++k)
+      if (row_ok && 8 * q < left) *reinterpret_cast<uint4*>(to + k * plane + 8 * q) = make_uint4(w[0][k], w[1][k], w[2][k], w[3][k]);
+  }
+}
+// The same, transposed: to the 32 rows `pitch` apart that are the columns, of which rows_left are there; `to` is the first of them at
+// the column that is this lane's row, rounded down to even.  Two lanes' values of a column meet in one word.
+template <int PLANES, typename F>
+__device__ __forceinline__ void planes_mirrored(bf16* to, int64_t plane, F f, int64_t pitch, int rows_left, bool col_ok, int lane) {
+  const bool odd = lane & 1;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    uint32_t w[PLANES];
+    planes_of<PLANES>(f(2 * i), f(2 * i + 1), w);
+    const int j = 2 * i + odd;
+#pragma unroll
+    for (int k = 0; k < PLANES; ++k) {
+      const uint32_t other = __shfl_xor_sync(0xffffffffu, w[k], 1);
+      const uint32_t v = odd ? __byte_perm(other, w[k], 0x7632) : __byte_perm(w[k], other, 0x5410);
+      if (j < rows_left && col_ok) *reinterpret_cast<uint32_t*>(to + k * plane + j * pitch) = v;
+    }
+  }
 }
 
 // What an epilogue warp stores through: boxes of 32 rows x 64 bytes (32 bf16 or 16 fp32 columns), 64-byte swizzled, by TMA
@@ -176,27 +222,6 @@ struct Store {
       *reinterpret_cast<uint4*>(s + lane * 64 + ((q ^ sw) << 4)) = x;
     }
     send(tm, s, col, row, z, false);
-  }
-  // ... in planes at z, z + 1, ..
-  template <typename F>
-  __device__ __forceinline__ void planes_row(const CUtensorMap* tm, F f, int col, int row, int z, int planes) {
-    if (planes == 2) {
-#pragma unroll 1
-      for (int k = 0; k < 2; ++k)
-        bf16_row(tm, [&](int j) {
-          float x = f(j);
-          const float h = plane_round(x);
-          return k == 0 ? h : x;
-        }, col, row, z + k);
-    } else {
-#pragma unroll 1
-      for (int k = 0; k < 3; ++k)
-        bf16_row(tm, [&](int j) {
-          float x = f(j);
-          const float h = plane_trunc(x), m = plane_trunc(x);
-          return k == 0 ? h : k == 1 ? m : x;
-        }, col, row, z + k);
-    }
   }
   // ... in fp32, stored or added to what is there; columns from `cols` on are not the map's
   __device__ __forceinline__ void f32_row(const CUtensorMap* tm, const float* v, int col, int row, int z, bool add, int cols) {
