@@ -41,8 +41,17 @@ __device__ __forceinline__ void elements(const T* p, float* v) {
   }
 }
 
-// Sums of squares of the elements by their size, scaled so that none overflows or vanishes: those above 2^50 by 2^-140, those
-// below 2^-50 by 2^140, and the others.  A warp a row.
+// Sums of squares by the elements' size, scaled so that none overflows or vanishes: those above 2^50 by 2^-140, those below 2^-50
+// by 2^140 (s[2]), and the others (s[1])
+__device__ __forceinline__ void add_square(float v, float (&s)[3]) {
+  const float av = fabsf(v);
+  const bool big = av > 0x1p50f, small = av < 0x1p-50f;
+  const float w = v * (big ? 0x1p-70f : small ? 0x1p70f : 1.f), q = w * w;
+  s[0] += big ? q : 0.f;
+  s[1] += big || small ? 0.f : q;
+  s[2] += small ? q : 0.f;
+}
+// ... of a matrix's parts.  A warp a row.
 template <typename T, int VEC>
 __global__ void __launch_bounds__(256) orth_norm_kernel(const ra_orthogonalize_args a, float* norms) {
   pdl_wait();
@@ -56,14 +65,7 @@ __global__ void __launch_bounds__(256) orth_norm_kernel(const ra_orthogonalize_a
       float v[VEC];
       elements<T, VEC>(row + c, v);
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        const float av = fabsf(v[i]);
-        const bool big = av > 0x1p50f, small = av < 0x1p-50f;
-        const float w = v[i] * (big ? 0x1p-70f : small ? 0x1p70f : 1.f), q = w * w;
-        s[0] += big ? q : 0.f;
-        s[1] += big || small ? 0.f : q;
-        s[2] += small ? q : 0.f;
-      }
+      for (int i = 0; i < VEC; ++i) add_square(v[i], s);
     }
   }
   __shared__ float sh[8][3];
@@ -101,10 +103,10 @@ __device__ __forceinline__ Scale scale_of(const float* norms, int parts, float e
   return {ldexpf(1.f, e / 2), ldexpf(1.f, e - e / 2), (float)f};
 }
 
-// The scaled matrices in planes [n][planes][rows][pitch].  One plane (bf16): scaled by the power of two alone, exactly; the
+// The scaled matrices in planes [n][planes][rows][pitch], zeros behind cols up to width.  One plane (bf16): scaled by the power of two alone, exactly; the
 // factor, which goes to factors[m], is left to the first step's products.  No plane: into out.
 template <typename T, int VEC>
-__global__ void __launch_bounds__(256) orth_start_kernel(const ra_orthogonalize_args a, const float* norms, int parts, float* factors, bf16* x, int planes, int pitch) {
+__global__ void __launch_bounds__(256) orth_start_kernel(const ra_orthogonalize_args a, const float* norms, int parts, float* factors, bf16* x, int planes, int width, int pitch) {
   __shared__ Scale sh;
   pdl_wait();
   pdl_trigger();
@@ -128,7 +130,7 @@ __global__ void __launch_bounds__(256) orth_start_kernel(const ra_orthogonalize_
     }
     bf16* d = x + ((int64_t)m * planes * a.rows + r) * pitch;
 #pragma unroll 4
-    for (int c = lane * VEC; c < pitch; c += 32 * VEC) {  // (cols is a multiple of VEC)
+    for (int c = lane * VEC; c < width; c += 32 * VEC) {  // (cols is a multiple of VEC)
       float v[VEC];
 #pragma unroll
       for (int i = 0; i < VEC; ++i) v[i] = 0.f;
@@ -166,7 +168,7 @@ struct OrthArgs {
   unsigned* err;
   const float* factors;    // of the first step's matrices: P is scaled by the power'th power of its factor
   bf16 *o, *o2;            // P + add I and, if wanted, mul2 P + add2 I in planes [n][planes][rows][pitch]
-  int pitch, power;
+  int width, pitch, power;  // (width: the columns that are written, to a multiple of 8)
   void* dst;
   int64_t dst_stride, dst_matrix_stride;
   int rows, cols;          // of the product
@@ -226,8 +228,8 @@ struct Step {
   static __device__ __forceinline__ void put(const Args& p, const Unit& w, bf16* to, F f, int row, int col, int lane) {
     const int64_t plane = (int64_t)p.rows * p.pitch;
     bf16* base = to + (int64_t)w.z * PLANES * plane;
-    prod::planes_out<PLANES>(base + (int64_t)row * p.pitch + col, plane, f, row < p.rows, p.pitch - col);
-    if (w.job) prod::planes_mirrored<PLANES>(base + (int64_t)col * p.pitch + (row & ~1), plane, f, p.pitch, p.rows - col, row < p.pitch, lane);
+    prod::planes_out<PLANES>(base + (int64_t)row * p.pitch + col, plane, f, row < p.rows, p.width - col);
+    if (w.job) prod::planes_mirrored<PLANES>(base + (int64_t)col * p.pitch + (row & ~1), plane, f, p.pitch, p.rows - col, row < p.width, lane);
   }
   static __device__ __forceinline__ void finish(const Args& p, const Unit& w, const Tile& t, Store& st, float (&v)[4][32]) {
     const int row0 = w.m0 + t.rank * prod::BM + t.quad * 32, row = row0 + t.lane;
@@ -267,8 +269,429 @@ struct Step {
   }
 };
 
+// ---- matrices whose smaller side is at most 64 --------------------------------------------------
+// An adapter's matrix stays on chip through all steps: a cluster of up to eight CTAs has one matrix, each CTA `blocks` blocks
+// of 64 of the longer side's indexes (rows, say; a wide matrix comes transposed), in planes in shared memory,
+// [block][64 rows][64 of the shorter side], 128-byte swizzled.  S is the sum of the CTAs' products X^T X, which they leave
+// for one another in shared memory and each adds up, in the same order; S T and X Q each CTA does by itself.  The same storage is an
+// MN-major operand of X^T X and a K-major one of X Q.
+// Bound: latency.  A step is three products' issue and read-out and one meeting of the cluster, 7 us, where three
+// launches of the products above take 30 (48 of 1024 x 64).
+constexpr int SMALL = 64, SMALL_THREADS = 256, SMALL_BLOCK = SMALL * 128;  // bytes of a block's plane
+constexpr int PART_PITCH = SMALL + 4;                                      // of S in fp32: rows four banks apart
+constexpr int PART_BYTES = SMALL * PART_PITCH * 4;
+template <int PL>
+constexpr int small_blocks() { return PL == 2 ? 9 : 5; }  // that shared memory holds
+template <int PL>
+constexpr int small_smem() { return PL * (small_blocks<PL>() + 2) * SMALL_BLOCK + 2 * PART_BYTES + 1024; }
+
+struct SmallArgs {
+  ra_orthogonalize_args a;
+  int blocks, ctas;  // of a CTA; of a cluster
+  bool tall, vec_in, vec_out;
+  prod::Terms terms;
+};
+
+template <typename T, int PL>
+__global__ void __launch_bounds__(SMALL_THREADS, 1) orth_small_kernel(const __grid_constant__ SmallArgs p) {
+  using namespace tc;
+  extern __shared__ uint8_t raw[];
+  __shared__ __align__(8) uint64_t bar;
+  __shared__ uint32_t tmem_sh;
+  __shared__ volatile int abort_sh;
+  __shared__ float norm_sh[3], norms_sh[8 * 3], warp_sh[8][3];
+  __shared__ Scale scale_sh;
+  constexpr int V = 16 / (int)sizeof(T);
+  const ra_orthogonalize_args& a = p.a;
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31, quad = warp & 3, half = warp >> 2;
+  const int HB = p.blocks, CS = p.ctas, rank = (int)blockIdx.x % CS, m = (int)blockIdx.x / CS;
+  const int low = p.tall ? a.cols : a.rows, high = p.tall ? a.rows : a.cols, rows = HB * SMALL, first = rank * rows;
+  uint8_t *xs = smem, *ss = xs + PL * HB * SMALL_BLOCK, *ts = ss + PL * SMALL_BLOCK;
+  float* part = reinterpret_cast<float*>(ts + PL * SMALL_BLOCK);
+  const uint32_t xa = smem_u32(xs), sa = smem_u32(ss), ta = smem_u32(ts);
+
+  if (tid == 0) {
+    mbar_init(&bar, 1);
+    abort_sh = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_sh)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_sh;
+  pdl_wait();
+  pdl_trigger();
+
+  // ---- the matrix, in units of eight of a row's elements; where they are 32 bytes or less at a 16-byte boundary, a thread's all
+  // at once on their way, and held until the norm is there; else four at a time, twice
+  const T* x = static_cast<const T*>(a.x_dev) + m * a.x_matrix_stride;
+  const int units = rows * 8;
+  const bool hold = p.tall && p.vec_in;
+  constexpr int HELD = small_blocks<PL>() * 512 / SMALL_THREADS, PIECES = 8 / V;
+  uint4 held[HELD][PIECES];
+  auto place = [&](int u, int& r, int& j) {
+    r = p.tall ? u >> 3 : u % rows;  // (neighbours in memory to neighbouring threads)
+    j = p.tall ? u & 7 : u / rows;
+  };
+  auto scattered = [&](int u, float (&v)[8]) {
+    int r, j;
+    place(u, r, j);
+    const int hi = first + r, lo = 8 * j;
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+      v[c] = u < units && hi < high && lo + c < low ? to_f(x[p.tall ? hi * a.x_stride + lo + c : (lo + c) * a.x_stride + hi]) : 0.f;
+  };
+  float s3[3] = {0.f, 0.f, 0.f};
+  if (hold) {
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+      const int u = tid + i * SMALL_THREADS, hi = first + (u >> 3), lo = 8 * (u & 7);
+#pragma unroll
+      for (int q = 0; q < PIECES; ++q) {
+        held[i][q] = make_uint4(0, 0, 0, 0);
+        if (u < units && hi < high && lo + V * q < low) held[i][q] = *reinterpret_cast<const uint4*>(x + hi * a.x_stride + lo + V * q);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < HELD; ++i)
+#pragma unroll
+      for (int q = 0; q < PIECES; ++q) {
+        const T* h = reinterpret_cast<const T*>(&held[i][q]);
+#pragma unroll
+        for (int c = 0; c < V; ++c) add_square(to_f(h[c]), s3);
+      }
+  } else {
+    for (int u0 = tid; u0 < units; u0 += 4 * SMALL_THREADS) {
+      float v[4][8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) scattered(u0 + i * SMALL_THREADS, v[i]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < 8; ++c) add_square(v[i][c], s3);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 3; ++k) s3[k] = warp_sum(s3[k]);
+  if (lane == 0)
+    for (int k = 0; k < 3; ++k) warp_sh[warp][k] = s3[k];
+  __syncthreads();
+  if (tid < 3) {
+    float t = 0.f;
+    for (int w = 0; w < 8; ++w) t += warp_sh[w][tid];
+    norm_sh[tid] = t;
+  }
+  auto meet = [&]() {  // the cluster's writes to shared memory are seen by all of it
+    if (CS > 1) {
+      cluster_arrive();
+      cluster_wait();
+    } else {
+      __syncthreads();
+    }
+  };
+  auto far = [&](const float* q, int of) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(peer_addr(smem_u32(q), of)) : "memory");
+    return v;
+  };
+  meet();
+  if (tid < 3 * CS) norms_sh[tid] = CS > 1 ? far(norm_sh + tid % 3, tid / 3) : norm_sh[tid];
+  __syncthreads();
+  if (warp == 0) {
+    const Scale mine = scale_of(norms_sh, CS, a.eps);
+    if (lane == 0) scale_sh = mine;
+  }
+  __syncthreads();
+  const Scale scale = scale_sh;
+  // eight values' planes to chunk j of row r of a 64-row block
+  auto planes8 = [&](uint8_t* to, int step, int r, int j, const float* v) {
+    uint32_t w[4][PL];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) prod::planes_of<PL>(v[2 * i], v[2 * i + 1], w[i]);
+#pragma unroll
+    for (int k = 0; k < PL; ++k) *reinterpret_cast<uint4*>(to + k * step + swz(r, j)) = make_uint4(w[0][k], w[1][k], w[2][k], w[3][k]);
+  };
+  auto keep = [&](int u, float (&v)[8]) {
+    int r, j;
+    place(u, r, j);
+    if (u >= units) return;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) v[c] = first + r < high && 8 * j + c < low ? scale(v[c]) : 0.f;
+    planes8(xs + (r >> 6) * SMALL_BLOCK, HB * SMALL_BLOCK, r & 63, j, v);
+  };
+  if (hold) {
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+      float v[8];
+#pragma unroll
+      for (int q = 0; q < PIECES; ++q) {
+        const T* h = reinterpret_cast<const T*>(&held[i][q]);
+#pragma unroll
+        for (int c = 0; c < V; ++c) v[V * q + c] = to_f(h[c]);
+      }
+      keep(tid + i * SMALL_THREADS, v);
+    }
+  } else {
+    for (int u0 = tid; u0 < units; u0 += 4 * SMALL_THREADS) {
+      float v[4][8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) scattered(u0 + i * SMALL_THREADS, v[i]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) keep(u0 + i * SMALL_THREADS, v[i]);
+    }
+  }
+
+  uint32_t phase = 0;
+  // what the threads wrote is an operand now; one thread issues f's products, all wait for them
+  auto terms = [&](auto f) {
+    for (int t = 0; t < p.terms.n; ++t) f(t, (int)(p.terms.a >> (2 * t) & 3u), (int)(p.terms.b >> (2 * t) & 3u));
+  };
+  auto products = [&](auto f) {
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 0 && elect_one()) {
+      tc_fence_after();
+      f();
+      umma_commit(&bar);
+    }
+    __syncwarp();
+    mbar_wait(&bar, phase, &abort_sh, a.err_dev);
+    phase ^= 1u;
+    tc_fence_after();
+  };
+  constexpr uint32_t MN = idesc_bf16_abmn(128, SMALL), KK = idesc_bf16(128, SMALL);
+  constexpr uint32_t C_S = 0, C_Q = PL == 2 ? 128 : 256, C_X = C_Q + 64;  // (C_X + 64 pairs <= 512)
+  const int r = quad * 32 + lane;  // S and Q are with quads 0 and 1
+  const uint32_t at = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(32 * half);
+  float* const parts[2] = {part, part + SMALL * PART_PITCH};
+  const int pairs = (HB + 1) / 2;
+  for (int step = 0; step < a.steps; ++step) {
+    // planes 0 and 1 (64 rows of the product each) by all planes (64 columns each) at once, and plane 2 by plane 0
+    products([&]() {
+      const uint32_t plane = HB * SMALL_BLOCK;
+      for (int b = 0; b < HB; ++b)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t at = xa + b * SMALL_BLOCK + k * 2048;
+          umma_bf16(tmem + C_S, sdesc_mn_sw128_lbo(at, plane), sdesc_mn_sw128_lbo(at, plane), idesc_bf16_abmn(128, 64 * PL), (uint32_t)(b | k));
+          if (PL == 3)
+            umma_bf16(tmem + C_S + 64 * PL, sdesc_mn_sw128_lbo(at + 2 * plane, SMALL_BLOCK), sdesc_mn_sw128(at), MN, (uint32_t)(b | k));
+        }
+    });
+    float v[32];
+    float *mine = parts[step & 1], *low_rows = reinterpret_cast<float*>(ss);  // (Q is done with)
+    {
+      float y[32];
+      tmem_ld32(at + C_S + 64, v);
+      if (PL == 3 && quad < 2) {
+        tmem_ld32(at + C_S + 64 * (PL - 1), y);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] += y[j];
+        tmem_ld32(at + C_S + 64 * PL, y);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] += y[j];
+      }
+      tmem_ld32(at + C_S, y);
+#pragma unroll
+      for (int j = 0; j < 32; ++j) v[j] += y[j];
+    }
+    if (quad >= 2)
+#pragma unroll
+      for (int j = 0; j < 32; j += 4)
+        *reinterpret_cast<float4*>(low_rows + (r - SMALL) * PART_PITCH + 32 * half + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+    __syncthreads();
+    if (quad < 2)
+#pragma unroll
+      for (int j = 0; j < 32; j += 4) {
+        const float4 y = *reinterpret_cast<const float4*>(low_rows + r * PART_PITCH + 32 * half + j);
+        v[j] += y.x;
+        v[j + 1] += y.y;
+        v[j + 2] += y.z;
+        v[j + 3] += y.w;
+        if (CS > 1) *reinterpret_cast<float4*>(mine + r * PART_PITCH + 32 * half + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+      }
+    meet();
+    if (CS > 1) {
+      // the CTAs' sums, neighbouring threads on neighbouring pieces (a row a thread takes 32 lines of another SM's memory an
+      // instruction: 2.5 us a CTA of the cluster), and back through this CTA's memory to the rows' threads
+      for (int i = tid; i < SMALL * PART_PITCH / 4; i += SMALL_THREADS) {
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int c = 0; c < CS; ++c) {
+          float4 y;
+          asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(y.x), "=f"(y.y), "=f"(y.z), "=f"(y.w) : "r"(peer_addr(smem_u32(mine) + 16 * i, c)));
+          sum.x += y.x;
+          sum.y += y.y;
+          sum.z += y.z;
+          sum.w += y.w;
+        }
+        *reinterpret_cast<float4*>(low_rows + 4 * i) = sum;
+      }
+      __syncthreads();
+      if (quad < 2)
+#pragma unroll
+        for (int j = 0; j < 32; j += 4) {
+          const float4 y = *reinterpret_cast<const float4*>(low_rows + r * PART_PITCH + 32 * half + j);
+          v[j] = y.x;
+          v[j + 1] = y.y;
+          v[j + 2] = y.z;
+          v[j + 3] = y.w;
+        }
+      __syncthreads();
+    }
+    const int diag = r < low ? r - 32 * half : -1;
+    if (quad < 2) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) planes8(ss, SMALL_BLOCK, r, 4 * half + q, v + 8 * q);
+#pragma unroll
+      for (int j = 0; j < 32; ++j) v[j] = a.c * v[j] + (j == diag ? a.b : 0.f);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) planes8(ts, SMALL_BLOCK, r, 4 * half + q, v + 8 * q);
+    }
+    products([&]() {  // (S and T are symmetric; rows 64.. of the product are of what lies behind S's plane)
+      terms([&](int t, int pa, int pb) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          umma_bf16(tmem + C_Q, sdesc_mn_sw128_lbo(sa + pa * SMALL_BLOCK + k * 2048, SMALL_BLOCK), sdesc_mn_sw128(ta + pb * SMALL_BLOCK + k * 2048), MN,
+                    (uint32_t)(t | k));
+      });
+    });
+    if (quad < 2) {
+      tmem_ld32(at + C_Q, v);
+#pragma unroll
+      for (int j = 0; j < 32; ++j) v[j] += j == diag ? a.a : 0.f;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) planes8(ss, SMALL_BLOCK, r, 4 * half + q, v + 8 * q);  // Q, where S was
+    }
+    products([&]() {
+      terms([&](int t, int pa, int pb) {
+        for (int b = 0; b < pairs; ++b)
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            umma_bf16(tmem + C_X + 64 * b, sdesc_sw128(xa + (pa * HB + 2 * b) * SMALL_BLOCK + k * 32), sdesc_sw128(sa + pb * SMALL_BLOCK + k * 32), KK,
+                      (uint32_t)(t | k));
+      });
+    });
+    const bool last = step + 1 == a.steps;
+    T* out = static_cast<T*>(a.out_dev) + m * a.out_matrix_stride;
+    for (int b = 0; b < pairs; ++b) {
+      __syncwarp();
+      tmem_ld32(at + C_X + 64 * b, v);
+      const int row = b * 128 + r;
+      if (row >= rows) continue;
+      if (!last) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) planes8(xs + (row >> 6) * SMALL_BLOCK, HB * SMALL_BLOCK, row & 63, 4 * half + q, v + 8 * q);
+        continue;
+      }
+      const int hi = first + row;
+      if (hi >= high) continue;
+      if (p.tall && p.vec_out) {
+        T* o = out + hi * a.out_stride + 32 * half;
+#pragma unroll
+        for (int j = 0; j < 32; j += V)
+          if (32 * half + j < low) {
+            __align__(16) T h[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) h[i] = from_f<T>(v[j + i]);
+            *reinterpret_cast<uint4*>(o + j) = *reinterpret_cast<const uint4*>(h);
+          }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+          const int lo = 32 * half + j;
+          if (lo < low) out[p.tall ? hi * a.out_stride + lo : lo * a.out_stride + hi] = from_f<T>(v[j]);
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  meet();  // (no CTA leaves while another reads its sums)
+  if (warp == 0) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+  }
+}
+
+bool small_fits(const ra_orthogonalize_args& a) {
+  const int most = a.dtype == RA_BF16 ? small_blocks<2>() : small_blocks<3>();
+  return std::min(a.rows, a.cols) <= SMALL && parts_of(std::max(a.rows, a.cols), SMALL) <= 8 * most && a.steps > 0;
+}
+
+template <typename T, int PL>
+cudaError_t run_small(const ra_orthogonalize_args& a, cudaStream_t st) {
+  auto k = orth_small_kernel<T, PL>;
+  // (all of shared memory, whatever the plan: one CTA an SM, whose TMEM no other waits for)
+  constexpr int smem = small_smem<PL>();
+  auto config = [&](cudaLaunchConfig_t& cfg, cudaLaunchAttribute* at, int ctas) {
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = ctas;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.gridDim = dim3((unsigned)a.n_matrices * ctas);
+    cfg.blockDim = dim3(SMALL_THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+  };
+  struct Fit {
+    cudaError_t error;
+    int clusters[9];  // of each size, that run at the same time
+  };
+  static const Fit fit = [&] {
+    Fit f = {allow_smem(k, smem), {}};
+    for (int c = 1; c <= 8 && f.error == cudaSuccess; ++c) {
+      cudaLaunchConfig_t cfg = {};
+      cudaLaunchAttribute at[1];
+      config(cfg, at, c);
+      cfg.gridDim = dim3((unsigned)c);
+      f.error = cudaOccupancyMaxActiveClusters(&f.clusters[c], k, &cfg);
+    }
+    return f;
+  }();
+  if (fit.error != cudaSuccess) return fit.error;
+  // CTAs of a cluster and blocks of a CTA by the measured time: rounds of clusters, each of about 5 us and 1 a block to begin with, and
+  // 3 us, 0.35 a block and 0.5 a CTA a step (1024 x 64 in bf16: two CTAs 7.2 us a step, four 6.2, eight 7.6)
+  int ctas = 0, blocks = 0;
+  double best = 1e30;
+  const int all = parts_of(std::max(a.rows, a.cols), SMALL);
+  for (int c = 1; c <= 8; ++c) {
+    const int b = parts_of(all, c);
+    if (b > small_blocks<PL>() || parts_of(all, b) != c || fit.clusters[c] < 1) continue;
+    const double t = (double)parts_of(a.n_matrices, fit.clusters[c]) * (5. + b + a.steps * (3. + 0.35 * b + 0.5 * c));
+    if (t < best) {
+      best = t;
+      ctas = c;
+      blocks = b;
+    }
+  }
+  if (ctas == 0) return cudaErrorNotSupported;
+  constexpr int V = 16 / (int)sizeof(T);
+  auto aligned = [&](const void* p, int64_t stride, int64_t matrix) {
+    return ((uintptr_t)p & 15) == 0 && stride % V == 0 && (a.n_matrices == 1 || matrix % V == 0) && a.cols % V == 0;
+  };
+  SmallArgs p = {a, blocks, ctas, a.rows > a.cols, aligned(a.x_dev, a.x_stride, a.x_matrix_stride), aligned(a.out_dev, a.out_stride, a.out_matrix_stride),
+                 prod::terms_of(PL, PL)};
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute at[2];
+  config(cfg, at, ctas);
+  at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.numAttrs = 2;
+  note_launch(1);
+  return cudaLaunchKernelEx(&cfg, k, p);
+}
+
 struct Plan {
-  int planes, low, high, pitch, low_pitch, parts;
+  int planes, low, high, parts;
+  // columns to a multiple of 8, what TMA reads of a row; rows at 128 bytes, the boxes' rows (at 16, each would touch two lines)
+  int width, pitch, low_width, low_pitch;
   size_t norms, factors, x[2], s, t, q, bytes;
 };
 Plan plan(const ra_orthogonalize_args& a) {
@@ -276,8 +699,10 @@ Plan plan(const ra_orthogonalize_args& a) {
   p.planes = a.dtype == RA_F32 ? 3 : 2;
   p.low = std::min(a.rows, a.cols);
   p.high = std::max(a.rows, a.cols);
-  p.pitch = up(a.cols, 8);
-  p.low_pitch = up(p.low, 8);
+  p.width = up(a.cols, 8);
+  p.pitch = up(a.cols, 64);
+  p.low_width = up(p.low, 8);
+  p.low_pitch = up(p.low, 64);
   p.parts = std::min(std::max(1, NORM_CTAS / a.n_matrices), parts_of(a.rows, 8));
   size_t at = WS_ZERO;
   auto take = [&](size_t n) {
@@ -296,14 +721,17 @@ Plan plan(const ra_orthogonalize_args& a) {
   return p;
 }
 
-// ... of a symmetric product: square tiles, about half of them
-Pick pick_sym(int rows, int n, int blocks) {
+// A symmetric product: all tiles, or (sym) square ones on and above the diagonal, which takes rounds off and costs a round the
+// mirrored stores: 2048 x 2048 of K = 5632 in two planes 98 -> 73 us, two of 777 x 777 in three planes 49 -> 60
+Pick pick_sym(int rows, int n, int blocks, bool& sym) {
   auto time = [&](Pick k) {
     const int64_t t = parts_of(rows, k.bn);
-    return (double)parts_of(n * t * (t + 1) / 2, prod::SMS / k.cg) * (blocks * prod::block_time(k) + 1.5) + (k.cg == 2 ? 1. : 0.);
+    return (double)parts_of(n * t * (t + 1) / 2, prod::SMS / k.cg) * (blocks * prod::block_time(k) + 6.) + (k.cg == 2 ? 1. : 0.);
   };
-  const Pick one = {1, 128}, two = {2, 256};
-  return rows > 128 && time(two) < time(one) ? two : one;
+  const Pick one = {1, 128}, two = {2, 256}, best = rows > 128 && time(two) < time(one) ? two : one;
+  const Pick all = prod::pick(rows, rows, n, blocks);
+  sym = time(best) < prod::time_of(all, rows, rows, n, blocks);
+  return sym ? best : all;
 }
 
 template <typename T>
@@ -324,7 +752,7 @@ cudaError_t run(const ra_orthogonalize_args& a, cudaStream_t st) {
     note_launch(2);
     DO(launch_pdl(vec ? orth_norm_kernel<T, V> : orth_norm_kernel<T, 1>, ng, dim3(256), 0, st, a, norms));
     DO(launch_pdl(vec ? orth_start_kernel<T, V> : orth_start_kernel<T, 1>, sg, dim3(256), 0, st, a, (const float*)norms, p.parts, factors, x[0], first,
-                  p.pitch));
+                  p.width, p.pitch));
   }
   if (a.steps == 0) return cudaSuccess;
 
@@ -337,7 +765,7 @@ cudaError_t run(const ra_orthogonalize_args& a, cudaStream_t st) {
   auto shape = [&](OrthArgs& s, int rows, int cols, int k, int pa, int pb, bool sym) {
     const prod::Terms terms = prod::terms_of(pa, pb);
     const int blocks = parts_of(k, prod::BK) * terms.n;
-    const Pick c = sym ? pick_sym(rows, n, blocks) : prod::pick(rows, cols, n, blocks);
+    const Pick c = sym ? pick_sym(rows, n, blocks, sym) : prod::pick(rows, cols, n, blocks);
     s.rows = rows;
     s.cols = cols;
     s.k = k;
@@ -357,9 +785,10 @@ cudaError_t run(const ra_orthogonalize_args& a, cudaStream_t st) {
   shape(square, p.low, p.low, p.low, p.planes, p.planes, true);
   square.add = a.a;
   square.o = q;
+  square.width = p.low_width;
   square.pitch = p.low_pitch;
-  MAP(square.a, s, DT_BF16, nz, p.low, p.low_pitch, p.low_pitch, 64, prod::BM);
-  MAP(square.b, t, DT_BF16, nz, p.low, p.low_pitch, p.low_pitch, 64, square.shape.bn / square.cg);
+  MAP(square.a, s, DT_BF16, nz, p.low, p.low_width, p.low_pitch, 64, prod::BM);
+  MAP(square.b, t, DT_BF16, nz, p.low, p.low_width, p.low_pitch, 64, square.shape.bn / square.cg);
   for (int i = 0; i < a.steps; ++i) {
     const int px = i == 0 ? first : p.planes;
     const bf16* from = x[i & 1];
@@ -371,22 +800,24 @@ cudaError_t run(const ra_orthogonalize_args& a, cudaStream_t st) {
     gram.o2 = t;
     gram.add2 = a.b;
     gram.mul2 = a.c;
+    gram.width = p.low_width;
     gram.pitch = p.low_pitch;
     shape(apply, a.rows, a.cols, p.low, wide ? p.planes : px, wide ? px : p.planes, false);
     apply.b_mn = wide;
     apply.power = px == 1 ? 1 : 0;
     apply.o = x[(i + 1) & 1];
+    apply.width = p.width;
     apply.pitch = p.pitch;
     if (wide) {
-      MAP(gram.a, from, DT_BF16, n * px, a.rows, p.pitch, p.pitch, 64, prod::BM);
-      MAP(gram.b, from, DT_BF16, n * px, a.rows, p.pitch, p.pitch, 64, gram.shape.bn / gram.cg);
-      MAP(apply.a, q, DT_BF16, nz, p.low, p.low_pitch, p.low_pitch, 64, prod::BM);
-      MAP(apply.b, from, DT_BF16, n * px, a.rows, p.pitch, p.pitch, 64, 64);
+      MAP(gram.a, from, DT_BF16, n * px, a.rows, p.width, p.pitch, 64, prod::BM);
+      MAP(gram.b, from, DT_BF16, n * px, a.rows, p.width, p.pitch, 64, gram.shape.bn / gram.cg);
+      MAP(apply.a, q, DT_BF16, nz, p.low, p.low_width, p.low_pitch, 64, prod::BM);
+      MAP(apply.b, from, DT_BF16, n * px, a.rows, p.width, p.pitch, 64, 64);
     } else {
-      MAP(gram.a, from, DT_BF16, n * px, a.rows, p.pitch, p.pitch, 64, 64);
+      MAP(gram.a, from, DT_BF16, n * px, a.rows, p.width, p.pitch, 64, 64);
       gram.b = gram.a;
-      MAP(apply.a, from, DT_BF16, n * px, a.rows, p.pitch, p.pitch, 64, prod::BM);
-      MAP(apply.b, q, DT_BF16, nz, p.low, p.low_pitch, p.low_pitch, 64, apply.shape.bn / apply.cg);
+      MAP(apply.a, from, DT_BF16, n * px, a.rows, p.width, p.pitch, 64, prod::BM);
+      MAP(apply.b, q, DT_BF16, nz, p.low, p.low_width, p.low_pitch, 64, apply.shape.bn / apply.cg);
     }
     if ((apply.last = i + 1 == a.steps)) {
       apply.dst = a.out_dev;
@@ -406,8 +837,9 @@ cudaError_t run(const ra_orthogonalize_args& a, cudaStream_t st) {
 
 }  // namespace
 
-size_t orthogonalize_workspace(const ra_orthogonalize_args& a) { return plan(a).bytes; }
+size_t orthogonalize_workspace(const ra_orthogonalize_args& a) { return small_fits(a) ? WS_ZERO : plan(a).bytes; }
 cudaError_t orthogonalize(const ra_orthogonalize_args& a, cudaStream_t st) {
+  if (small_fits(a)) return a.dtype == RA_BF16 ? run_small<bf16, 2>(a, st) : run_small<float, 3>(a, st);
   return a.dtype == RA_BF16 ? run<bf16>(a, st) : run<float>(a, st);
 }
 

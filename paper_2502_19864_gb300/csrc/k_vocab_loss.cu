@@ -34,7 +34,7 @@ struct Prep {
   int *count, *index, *label;  // of the counted tokens: how many; each one's place among all, its label,
   float *scale, *lse, *ref;    // ... dloss over the largest of them, lse, and that largest (backward)
   void* x;                     // ... and hidden states: [planes][rows][pitch]
-  int rows, pitch, planes;
+  int rows, width, pitch, planes;  // (zeros from hidden to width)
 };
 __device__ __forceinline__ bool counted(const ra_vocab_loss_args& a, int label) { return (uint32_t)label < (uint32_t)a.vocab; }
 
@@ -67,7 +67,7 @@ __device__ __forceinline__ void split4(float4 v, bf16* d, int64_t plane) {
 }
 __device__ __forceinline__ void put_row(const Prep& p, const float* src, int r, int H, int lane) {
   bf16* d = static_cast<bf16*>(p.x) + (int64_t)r * p.pitch;
-  for (int c = lane * 4; c < p.pitch; c += 128)
+  for (int c = lane * 4; c < p.width; c += 128)
     split4(src && c < H ? *reinterpret_cast<const float4*>(src + c) : make_float4(0.f, 0.f, 0.f, 0.f), d + c, (int64_t)p.rows * p.pitch);
 }
 
@@ -170,10 +170,10 @@ __global__ void __launch_bounds__(256) vocab_prep_kernel(const ra_vocab_loss_arg
 }
 
 // rows [row0, row0 + rows) of W into planes
-__global__ void __launch_bounds__(256) vocab_split_kernel(const float* w, int64_t stride, bf16* out, int rows, int H, int pitch) {
+__global__ void __launch_bounds__(256) vocab_split_kernel(const float* w, int64_t stride, bf16* out, int rows, int H, int width, int pitch) {
   pdl_wait();
   pdl_trigger();
-  const int per = pitch / 4;
+  const int per = width / 4;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)rows * per; i += (int64_t)gridDim.x * 256) {
     const int r = (int)(i / per), c = (int)(i % per) * 4;
     split4(c < H ? *reinterpret_cast<const float4*>(w + r * stride + c) : make_float4(0.f, 0.f, 0.f, 0.f), out + (int64_t)r * pitch + c, (int64_t)rows * pitch);
@@ -414,7 +414,8 @@ __global__ void __launch_bounds__(128) vocab_sum_kernel(const float* sums, int s
 
 // ---- the plan -----------------------------------------------------------------------------
 struct Plan {
-  int planes, rows, pitch, chunk;
+  int planes, rows, chunk;
+  int wide, pitch;                // of gathered or split rows: columns to a multiple of 8, 128-byte boundaries
   int pieces, width;              // of the vocabulary, backward (and fp32 forward)
   Pick forward, logits, grads;    // (forward: of its logits)
   int splits_x, splits_w, stats;  // parts of the statistics
@@ -431,7 +432,8 @@ Plan plan(const ra_vocab_loss_args& a) {
   p.planes = f32 ? 3 : 1;
   p.chunk = f32 ? 4 : 128;
   p.rows = up(a.tokens > 0 ? a.tokens : 1, ROWS);
-  p.pitch = up(a.hidden, 8);
+  p.wide = up(a.hidden, 8);
+  p.pitch = up(a.hidden, 64);
   // pieces of at most 128 MB of dz
   int64_t most = (128ll << 20) / (2ll * p.planes * p.rows) / 256 * 256;
   most = std::max<int64_t>(most, 256);
@@ -507,6 +509,7 @@ Prep prep_of(const Plan& p, char* ws) {
   r.ref = reinterpret_cast<float*>(ws + p.ref);
   r.x = ws + p.xc;
   r.rows = p.rows;
+  r.width = p.wide;
   r.pitch = p.pitch;
   r.planes = p.planes;
   return r;
@@ -550,12 +553,12 @@ cudaError_t piece(const ra_vocab_loss_args& a, const Plan& p, char* ws, VocabArg
   g.wrow = p.planes == 1 ? v0 : 0;
   if (p.planes == 1) return cudaSuccess;
   note_launch(1);
-  return launch_pdl(vocab_split_kernel, dim3((unsigned)std::min<int64_t>(((int64_t)width * p.pitch / 4 + 255) / 256, 8 * SMS)), dim3(256), 0, st,
-                    static_cast<const float*>(a.w_dev) + v0 * a.w_stride, a.w_stride, reinterpret_cast<bf16*>(ws + p.wc), width, (int)a.hidden, p.pitch);
+  return launch_pdl(vocab_split_kernel, dim3((unsigned)std::min<int64_t>(((int64_t)width * p.wide / 4 + 255) / 256, 8 * SMS)), dim3(256), 0, st,
+                    static_cast<const float*>(a.w_dev) + v0 * a.w_stride, a.w_stride, reinterpret_cast<bf16*>(ws + p.wc), width, (int)a.hidden, p.wide, p.pitch);
 }
 cudaError_t w_map(const ra_vocab_loss_args& a, const Plan& p, char* ws, CUtensorMap& m, int width, int box_rows) {
   if (p.planes == 1) MAP(m, a.w_dev, DT_BF16, 1, a.vocab, a.hidden, a.w_stride, 64, box_rows);
-  else MAP(m, ws + p.wc, DT_BF16, 3, width, p.pitch, p.pitch, 64, box_rows);
+  else MAP(m, ws + p.wc, DT_BF16, 3, width, p.wide, p.pitch, 64, box_rows);
   return cudaSuccess;
 }
 #define DO(x)                                \
@@ -572,7 +575,7 @@ cudaError_t products(const VocabArgs& g, int64_t units, cudaStream_t st) {
 // hidden states as given (bf16) and gathered, in boxes of box_rows rows
 cudaError_t x_maps(const ra_vocab_loss_args& a, const Plan& p, char* ws, CUtensorMap& given, CUtensorMap& gathered, int box_rows) {
   if (p.planes == 1) MAP(given, a.x_dev, DT_BF16, 1, a.tokens, a.hidden, a.x_stride, 64, box_rows);
-  MAP(gathered, ws + p.xc, DT_BF16, p.planes, p.rows, p.pitch, p.pitch, 64, box_rows);
+  MAP(gathered, ws + p.xc, DT_BF16, p.planes, p.rows, p.wide, p.pitch, 64, box_rows);
   return cudaSuccess;
 }
 

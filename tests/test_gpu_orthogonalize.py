@@ -75,7 +75,8 @@ def check(s, dtype, steps=5, coef=COEF, eps=1e-7):
 
 
 SHAPES = [(1, 1, 1), (2, 1, 9), (3, 9, 1), (1, 5, 7), (4, 16, 128), (4, 128, 16), (2, 64, 64), (3, 65, 127), (2, 200, 130), (48, 96, 40),
-          (1, 300, 1000), (1, 513, 257), (2, 128, 128), (1, 777, 640), (1, 31, 4099)]
+          (1, 300, 1000), (1, 513, 257), (2, 128, 128), (1, 777, 640), (1, 31, 4099), (5, 64, 1024), (7, 1024, 64), (3, 321, 33), (1, 2560, 64),
+          (2, 63, 2561), (200, 64, 65), (1, 4608, 17), (40, 520, 48), (1, 1100, 600)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
