@@ -51,6 +51,19 @@ __device__ __forceinline__ void add_square(float v, float (&s)[3]) {
   s[1] += big || small ? 0.f : q;
   s[2] += small ? q : 0.f;
 }
+// N elements' squares, as they are where their sum has room on both sides
+template <int N>
+__device__ __forceinline__ void add_squares(const float* v, float (&s)[3]) {
+  float q = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) q = fmaf(v[i], v[i], q);
+  if (q > 0x1p-60f && q < 0x1p100f) {
+    s[1] += q;
+  } else {
+#pragma unroll 1
+    for (int i = 0; i < N; ++i) add_square(v[i], s);
+  }
+}
 // ... of a matrix's parts.  A warp a row.
 template <typename T, int VEC>
 __global__ void __launch_bounds__(256) orth_norm_kernel(const ra_orthogonalize_args a, float* norms) {
@@ -64,8 +77,7 @@ __global__ void __launch_bounds__(256) orth_norm_kernel(const ra_orthogonalize_a
     for (int c = lane * VEC; c < a.cols; c += 32 * VEC) {
       float v[VEC];
       elements<T, VEC>(row + c, v);
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) add_square(v[i], s);
+      add_squares<VEC>(v, s);
     }
   }
   __shared__ float sh[8][3];
@@ -84,9 +96,9 @@ __global__ void __launch_bounds__(256) orth_norm_kernel(const ra_orthogonalize_a
 // 1 / (|x| + eps) as two powers of two and a factor in [1, 2); NaN where |x| is not finite, so that a value that is not finite
 // takes its whole matrix
 struct Scale {
-  float p, q, f;
+  float p, q, f, fq;  // (the powers, the factor, and the factor times the second power)
   __device__ __forceinline__ float power(float v) const { return v * p * q; }
-  __device__ __forceinline__ float operator()(float v) const { return v == 0.f && f == f ? 0.f : v * p * f * q; }
+  __device__ __forceinline__ float operator()(float v) const { return v * p * fq; }
 };
 // (by a warp)
 __device__ __forceinline__ Scale scale_of(const float* norms, int parts, float eps) {
@@ -94,13 +106,14 @@ __device__ __forceinline__ Scale scale_of(const float* norms, int parts, float e
   for (int i = threadIdx.x & 31; i < parts; i += 32) t += (double)norms[3 * i] * 0x1p140 + (double)norms[3 * i + 1] + (double)norms[3 * i + 2] * 0x1p-140;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
-  if (!isfinite(t)) return {1.f, 1.f, NAN};
+  if (!isfinite(t)) return {1.f, 1.f, NAN, NAN};
   const double s = 1. / (sqrt(t) + (double)eps);
-  if (!isfinite(s)) return {1.f, 1.f, 1.f};  // (all zeros, and eps too)
+  if (!isfinite(s)) return {1.f, 1.f, 1.f, 1.f};  // (all zeros, and eps too)
   int e;
   const double f = 2. * frexp(s, &e);
   --e;
-  return {ldexpf(1.f, e / 2), ldexpf(1.f, e - e / 2), (float)f};
+  const float q = ldexpf(1.f, e - e / 2);
+  return {ldexpf(1.f, e / 2), q, (float)f, (float)f * q};
 }
 
 // The scaled matrices in planes [n][planes][rows][pitch], zeros behind cols up to width.  One plane (bf16): scaled by the power of two alone, exactly; the
@@ -277,7 +290,7 @@ struct Step {
 // MN-major operand of X^T X and a K-major one of X Q.
 // Bound: latency.  A step is three products' issue and read-out and one meeting of the cluster, 7 us, where three
 // launches of the products above take 30 (48 of 1024 x 64).
-constexpr int SMALL = 64, SMALL_THREADS = 256, SMALL_BLOCK = SMALL * 128;  // bytes of a block's plane
+constexpr int SMALL = 64, SMALL_THREADS = 512, SMALL_BLOCK = SMALL * 128;  // bytes of a block's plane
 constexpr int PART_PITCH = SMALL + 4;                                      // of S in fp32: rows four banks apart
 constexpr int PART_BYTES = SMALL * PART_PITCH * 4;
 template <int PL>
@@ -299,12 +312,12 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) orth_small_kernel(const __gr
   __shared__ __align__(8) uint64_t bar;
   __shared__ uint32_t tmem_sh;
   __shared__ volatile int abort_sh;
-  __shared__ float norm_sh[3], norms_sh[8 * 3], warp_sh[8][3];
+  __shared__ float norm_sh[3], norms_sh[8 * 3], warp_sh[16][3];
   __shared__ Scale scale_sh;
   constexpr int V = 16 / (int)sizeof(T);
   const ra_orthogonalize_args& a = p.a;
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31, quad = warp & 3, half = warp >> 2;
+  const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31, quad = warp & 3, grp = warp >> 2;  // (16 of 64 columns)
   const int HB = p.blocks, CS = p.ctas, rank = (int)blockIdx.x % CS, m = (int)blockIdx.x / CS;
   const int low = p.tall ? a.cols : a.rows, high = p.tall ? a.rows : a.cols, rows = HB * SMALL, first = rank * rows;
   uint8_t *xs = smem, *ss = xs + PL * HB * SMALL_BLOCK, *ts = ss + PL * SMALL_BLOCK;
@@ -362,8 +375,10 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) orth_small_kernel(const __gr
 #pragma unroll
       for (int q = 0; q < PIECES; ++q) {
         const T* h = reinterpret_cast<const T*>(&held[i][q]);
+        float v[V];
 #pragma unroll
-        for (int c = 0; c < V; ++c) add_square(to_f(h[c]), s3);
+        for (int c = 0; c < V; ++c) v[c] = to_f(h[c]);
+        if (tid + i * SMALL_THREADS < units) add_squares<V>(v, s3);
       }
   } else {
     for (int u0 = tid; u0 < units; u0 += 4 * SMALL_THREADS) {
@@ -372,8 +387,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) orth_small_kernel(const __gr
       for (int i = 0; i < 4; ++i) scattered(u0 + i * SMALL_THREADS, v[i]);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int c = 0; c < 8; ++c) add_square(v[i][c], s3);
+        if (u0 + i * SMALL_THREADS < units) add_squares<8>(v[i], s3);
     }
   }
 #pragma unroll
@@ -383,7 +397,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) orth_small_kernel(const __gr
   __syncthreads();
   if (tid < 3) {
     float t = 0.f;
-    for (int w = 0; w < 8; ++w) t += warp_sh[w][tid];
+    for (int w = 0; w < SMALL_THREADS / 32; ++w) t += warp_sh[w][tid];
     norm_sh[tid] = t;
   }
   auto meet = [&]() {  // the cluster's writes to shared memory are seen by all of it
@@ -421,7 +435,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) orth_small_kernel(const __gr
     place(u, r, j);
     if (u >= units) return;
 #pragma unroll
-    for (int c = 0; c < 8; ++c) v[c] = first + r < high && 8 * j + c < low ? scale(v[c]) : 0.f;
+    for (int c = 0; c < 8; ++c) v[c] = scale(v[c]);
     planes8(xs + (r >> 6) * SMALL_BLOCK, HB * SMALL_BLOCK, r & 63, j, v);
   };
   if (hold) {
@@ -468,7 +482,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) orth_small_kernel(const __gr
   constexpr uint32_t MN = idesc_bf16_abmn(128, SMALL), KK = idesc_bf16(128, SMALL);
   constexpr uint32_t C_S = 0, C_Q = PL == 2 ? 128 : 256, C_X = C_Q + 64;  // (C_X + 64 pairs <= 512)
   const int r = quad * 32 + lane;  // S and Q are with quads 0 and 1
-  const uint32_t at = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(32 * half);
+  const uint32_t at = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(16 * grp);
   float* const parts[2] = {part, part + SMALL * PART_PITCH};
   const int pairs = (HB + 1) / 2;
   for (int step = 0; step < a.steps; ++step) {
@@ -484,60 +498,68 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) orth_small_kernel(const __gr
             umma_bf16(tmem + C_S + 64 * PL, sdesc_mn_sw128_lbo(at + 2 * plane, SMALL_BLOCK), sdesc_mn_sw128(at), MN, (uint32_t)(b | k));
         }
     });
-    float v[32];
+    float v[16];
     float *mine = parts[step & 1], *low_rows = reinterpret_cast<float*>(ss);  // (Q is done with)
     {
-      float y[32];
-      tmem_ld32(at + C_S + 64, v);
+      float y[16];
+      tmem_ld16(at + C_S + 64, v);
       if (PL == 3 && quad < 2) {
-        tmem_ld32(at + C_S + 64 * (PL - 1), y);
+        tmem_ld16(at + C_S + 64 * (PL - 1), y);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] += y[j];
-        tmem_ld32(at + C_S + 64 * PL, y);
+        for (int j = 0; j < 16; ++j) v[j] += y[j];
+        tmem_ld16(at + C_S + 64 * PL, y);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] += y[j];
+        for (int j = 0; j < 16; ++j) v[j] += y[j];
       }
-      tmem_ld32(at + C_S, y);
+      tmem_ld16(at + C_S, y);
 #pragma unroll
-      for (int j = 0; j < 32; ++j) v[j] += y[j];
+      for (int j = 0; j < 16; ++j) v[j] += y[j];
     }
     if (quad >= 2)
 #pragma unroll
-      for (int j = 0; j < 32; j += 4)
-        *reinterpret_cast<float4*>(low_rows + (r - SMALL) * PART_PITCH + 32 * half + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+      for (int j = 0; j < 16; j += 4)
+        *reinterpret_cast<float4*>(low_rows + (r - SMALL) * PART_PITCH + 16 * grp + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
     __syncthreads();
     if (quad < 2)
 #pragma unroll
-      for (int j = 0; j < 32; j += 4) {
-        const float4 y = *reinterpret_cast<const float4*>(low_rows + r * PART_PITCH + 32 * half + j);
+      for (int j = 0; j < 16; j += 4) {
+        const float4 y = *reinterpret_cast<const float4*>(low_rows + r * PART_PITCH + 16 * grp + j);
         v[j] += y.x;
         v[j + 1] += y.y;
         v[j + 2] += y.z;
         v[j + 3] += y.w;
-        if (CS > 1) *reinterpret_cast<float4*>(mine + r * PART_PITCH + 32 * half + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+        if (CS > 1) *reinterpret_cast<float4*>(mine + r * PART_PITCH + 16 * grp + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
       }
     meet();
     if (CS > 1) {
       // the CTAs' sums, neighbouring threads on neighbouring pieces (a row a thread takes 32 lines of another SM's memory an
       // instruction: 2.5 us a CTA of the cluster), and back through this CTA's memory to the rows' threads
-      for (int i = tid; i < SMALL * PART_PITCH / 4; i += SMALL_THREADS) {
-        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-        for (int c = 0; c < CS; ++c) {
-          float4 y;
-          asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(y.x), "=f"(y.y), "=f"(y.z), "=f"(y.w) : "r"(peer_addr(smem_u32(mine) + 16 * i, c)));
-          sum.x += y.x;
-          sum.y += y.y;
-          sum.z += y.z;
-          sum.w += y.w;
+      constexpr int PIECES4 = SMALL * PART_PITCH / 4, EACH = (PIECES4 + SMALL_THREADS - 1) / SMALL_THREADS;
+      float4 sum[EACH] = {};
+#pragma unroll 2
+      for (int c = 0; c < CS; ++c) {
+        const uint32_t from = peer_addr(smem_u32(mine), c);
+        float4 y[EACH];
+#pragma unroll
+        for (int i = 0; i < EACH; ++i)
+          if (tid + i * SMALL_THREADS < PIECES4)
+            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(y[i].x), "=f"(y[i].y), "=f"(y[i].z), "=f"(y[i].w) : "r"(from + 16 * (tid + i * SMALL_THREADS)));
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+          sum[i].x += y[i].x;
+          sum[i].y += y[i].y;
+          sum[i].z += y[i].z;
+          sum[i].w += y[i].w;
         }
-        *reinterpret_cast<float4*>(low_rows + 4 * i) = sum;
       }
+#pragma unroll
+      for (int i = 0; i < EACH; ++i)
+        if (tid + i * SMALL_THREADS < PIECES4) *reinterpret_cast<float4*>(low_rows + 4 * (tid + i * SMALL_THREADS)) = sum[i];
       __syncthreads();
       if (quad < 2)
 #pragma unroll
-        for (int j = 0; j < 32; j += 4) {
-          const float4 y = *reinterpret_cast<const float4*>(low_rows + r * PART_PITCH + 32 * half + j);
+        for (int j = 0; j < 16; j += 4) {
+          const float4 y = *reinterpret_cast<const float4*>(low_rows + r * PART_PITCH + 16 * grp + j);
           v[j] = y.x;
           v[j + 1] = y.y;
           v[j + 2] = y.z;
@@ -545,14 +567,14 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) orth_small_kernel(const __gr
         }
       __syncthreads();
     }
-    const int diag = r < low ? r - 32 * half : -1;
+    const int diag = r < low ? r - 16 * grp : -1;
     if (quad < 2) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) planes8(ss, SMALL_BLOCK, r, 4 * half + q, v + 8 * q);
+      for (int q = 0; q < 2; ++q) planes8(ss, SMALL_BLOCK, r, 2 * grp + q, v + 8 * q);
 #pragma unroll
-      for (int j = 0; j < 32; ++j) v[j] = a.c * v[j] + (j == diag ? a.b : 0.f);
+      for (int j = 0; j < 16; ++j) v[j] = a.c * v[j] + (j == diag ? a.b : 0.f);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) planes8(ts, SMALL_BLOCK, r, 4 * half + q, v + 8 * q);
+      for (int q = 0; q < 2; ++q) planes8(ts, SMALL_BLOCK, r, 2 * grp + q, v + 8 * q);
     }
     products([&]() {  // (S and T are symmetric; rows 64.. of the product are of what lies behind S's plane)
       terms([&](int t, int pa, int pb) {
@@ -563,11 +585,11 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) orth_small_kernel(const __gr
       });
     });
     if (quad < 2) {
-      tmem_ld32(at + C_Q, v);
+      tmem_ld16(at + C_Q, v);
 #pragma unroll
-      for (int j = 0; j < 32; ++j) v[j] += j == diag ? a.a : 0.f;
+      for (int j = 0; j < 16; ++j) v[j] += j == diag ? a.a : 0.f;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) planes8(ss, SMALL_BLOCK, r, 4 * half + q, v + 8 * q);  // Q, where S was
+      for (int q = 0; q < 2; ++q) planes8(ss, SMALL_BLOCK, r, 2 * grp + q, v + 8 * q);  // Q, where S was
     }
     products([&]() {
       terms([&](int t, int pa, int pb) {
@@ -582,21 +604,21 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) orth_small_kernel(const __gr
     T* out = static_cast<T*>(a.out_dev) + m * a.out_matrix_stride;
     for (int b = 0; b < pairs; ++b) {
       __syncwarp();
-      tmem_ld32(at + C_X + 64 * b, v);
+      tmem_ld16(at + C_X + 64 * b, v);
       const int row = b * 128 + r;
       if (row >= rows) continue;
       if (!last) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) planes8(xs + (row >> 6) * SMALL_BLOCK, HB * SMALL_BLOCK, row & 63, 4 * half + q, v + 8 * q);
+        for (int q = 0; q < 2; ++q) planes8(xs + (row >> 6) * SMALL_BLOCK, HB * SMALL_BLOCK, row & 63, 2 * grp + q, v + 8 * q);
         continue;
       }
       const int hi = first + row;
       if (hi >= high) continue;
       if (p.tall && p.vec_out) {
-        T* o = out + hi * a.out_stride + 32 * half;
+        T* o = out + hi * a.out_stride + 16 * grp;
 #pragma unroll
-        for (int j = 0; j < 32; j += V)
-          if (32 * half + j < low) {
+        for (int j = 0; j < 16; j += V)
+          if (16 * grp + j < low) {
             __align__(16) T h[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) h[i] = from_f<T>(v[j + i]);
@@ -604,8 +626,8 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) orth_small_kernel(const __gr
           }
       } else {
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-          const int lo = 32 * half + j;
+        for (int j = 0; j < 16; ++j) {
+          const int lo = 16 * grp + j;
           if (lo < low) out[p.tall ? hi * a.out_stride + lo : lo * a.out_stride + hi] = from_f<T>(v[j]);
         }
       }
@@ -664,7 +686,7 @@ cudaError_t run_small(const ra_orthogonalize_args& a, cudaStream_t st) {
   for (int c = 1; c <= 8; ++c) {
     const int b = parts_of(all, c);
     if (b > small_blocks<PL>() || parts_of(all, b) != c || fit.clusters[c] < 1) continue;
-    const double t = (double)parts_of(a.n_matrices, fit.clusters[c]) * (5. + b + a.steps * (3. + 0.35 * b + 0.5 * c));
+    const double t = (double)parts_of(a.n_matrices, fit.clusters[c]) * (5. + b + a.steps * (3. + 0.35 * b + 0.5 * c + (c > 1 ? 1. : 0.)));
     if (t < best) {
       best = t;
       ctas = c;

@@ -461,7 +461,7 @@ Plan plan(const ra_vocab_loss_args& a) {
     const int64_t ux = parts_of(a.tokens, prod::BM * k.cg) * nt, uw = parts_of(p.width, prod::BM * k.cg) * nt;
     const double all = (double)ux * kx + (double)uw * kw, workers = SMS / k.cg;
     // a tile's k-blocks are cut so that none has more than about a third of a worker's share of all of them
-    auto cut = [&](int kb) { return std::max(1, std::min(std::min(16, kb / 16), (int)(3. * kb * workers / std::max(all, 1.)))); };
+    auto cut = [&](int kb) { return std::max(1, std::min(std::min(16, kb * terms / 16), (int)(3. * kb * workers / std::max(all, 1.)))); };
     const int sx = cut(kx), sw = p.pieces == 1 && (int64_t)p.width * a.hidden * 4 * cut(kw) <= (128ll << 20) ? cut(kw) : 1;
     const double longest = std::max(parts_of(kx, sx), parts_of(kw, sw));
     const double time = (std::max(all / workers, longest) + 0.3 * longest) * terms * prod::block_time(k) + (double)(ux * sx + uw * sw) / workers * 1.;

@@ -76,7 +76,7 @@ inline int parts_of(int64_t a, int b) { return (int)((a + b - 1) / b); }
 inline int up(int64_t a, int b) { return (int)((a + b - 1) / b * b); }
 // microseconds of a k-block of a tile (measured on long products; the issue of products and copies paces the narrow ones)
 inline double block_time(Pick k) {
-  if (k.cg == 2) return k.bn > 224 ? 0.345 : k.bn > 128 ? 0.31 : 0.25;
+  if (k.cg == 2) return k.bn > 128 ? 0.345 : 0.25;
   return k.bn <= 64 ? 0.2 : k.bn <= 128 ? 0.222 : k.bn <= 192 ? 0.31 : 0.365;
 }
 // ... of `batch` products m x n of `blocks` k-blocks: rounds of tiles, each with about 1 us for its start and end
@@ -86,7 +86,7 @@ inline double time_of(Pick k, int64_t m, int64_t n, int64_t batch, int blocks) {
 }
 inline Pick pick(int64_t m, int64_t n, int64_t batch, int blocks) {
   Pick best = {1, n <= 64 ? 64 : 128};
-  for (Pick k : {Pick{1, 64}, Pick{1, 256}, Pick{2, 224}, Pick{2, 256}})
+  for (Pick k : {Pick{1, 64}, Pick{1, 256}, Pick{2, 256}})
     if ((k.cg == 1 || m > BM) && n > k.bn / 2 && time_of(k, m, n, batch, blocks) < time_of(best, m, n, batch, blocks)) best = k;
   return best;
 }
