@@ -208,6 +208,10 @@ struct Step {
     nt = (p.cols + p.shape.bn - 1) / p.shape.bn;
     return p.sym ? nt * (nt + 1) / 2 : mt * nt;
   }
+  static __device__ __forceinline__ void prefetch(const Args& p) {
+    prod::prefetch_map(&p.a);
+    prod::prefetch_map(&p.b);
+  }
   static __device__ __forceinline__ int count(const Args& p) {
     int mt, nt;
     return p.n * tiles(p, mt, nt);

@@ -71,14 +71,40 @@ __device__ __forceinline__ void put_row(const Prep& p, const float* src, int r, 
     split4(src && c < H ? *reinterpret_cast<const float4*>(src + c) : make_float4(0.f, 0.f, 0.f, 0.f), d + c, (int64_t)p.rows * p.pitch);
 }
 
+// rows of W into planes (fp32)
+struct Split {
+  const float* w;
+  int64_t stride;
+  bf16* out;
+  int rows, hidden, width, pitch;
+};
+__device__ __forceinline__ void split_rows(const Split& s, int cta, int ctas) {
+  const int per = s.width / 4;
+  for (int64_t i = (int64_t)cta * 256 + threadIdx.x; i < (int64_t)s.rows * per; i += (int64_t)ctas * 256) {
+    const int r = (int)(i / per), c = (int)(i % per) * 4;
+    split4(c < s.hidden ? *reinterpret_cast<const float4*>(s.w + r * s.stride + c) : make_float4(0.f, 0.f, 0.f, 0.f), s.out + (int64_t)r * s.pitch + c,
+           (int64_t)s.rows * s.pitch);
+  }
+}
+__global__ void __launch_bounds__(256) vocab_split_kernel(const Split s) {
+  pdl_wait();
+  pdl_trigger();
+  split_rows(s, blockIdx.x, gridDim.x);
+}
+
+// The first `ctas` CTAs number and gather the tokens; those behind them take the vocabulary's first piece apart
 template <typename T>
-__global__ void __launch_bounds__(256) vocab_prep_kernel(const ra_vocab_loss_args a, const Prep p, int backward) {
+__global__ void __launch_bounds__(256) vocab_prep_kernel(const ra_vocab_loss_args a, const Prep p, int backward, int ctas, const Split split) {
   __shared__ int2 sh[8];
   __shared__ int list[256], warp_n[8];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, T_ = a.tokens;
   pdl_wait();
   pdl_trigger();
-  const int per = (T_ + gridDim.x - 1) / gridDim.x;
+  if ((int)blockIdx.x >= ctas) {
+    split_rows(split, blockIdx.x - ctas, gridDim.x - ctas);
+    return;
+  }
+  const int per = (T_ + ctas - 1) / ctas;
   const int start = min(T_, (int)blockIdx.x * per), end = min(T_, start + per);
   int2 n = make_int2(0, 0);
   float top = 0.f;
@@ -158,25 +184,14 @@ __global__ void __launch_bounds__(256) vocab_prep_kernel(const ra_vocab_loss_arg
   // the rows up to whole tiles
   const int up = (total + ROWS - 1) / ROWS * ROWS;
   if (gather)
-    for (int r = total + blockIdx.x * 8 + warp; r < up; r += gridDim.x * 8) put_row(p, (const T*)nullptr, r, a.hidden, lane);
-  for (int r = total + blockIdx.x * 256 + tid; r < up; r += gridDim.x * 256) {
+    for (int r = total + blockIdx.x * 8 + warp; r < up; r += ctas * 8) put_row(p, (const T*)nullptr, r, a.hidden, lane);
+  for (int r = total + blockIdx.x * 256 + tid; r < up; r += ctas * 256) {
     p.label[r] = -1;
     p.scale[r] = p.lse[r] = 0.f;
   }
   if (blockIdx.x == 0 && tid == 0) {
     *p.count = total;
     *p.ref = top;
-  }
-}
-
-// rows [row0, row0 + rows) of W into planes
-__global__ void __launch_bounds__(256) vocab_split_kernel(const float* w, int64_t stride, bf16* out, int rows, int H, int width, int pitch) {
-  pdl_wait();
-  pdl_trigger();
-  const int per = width / 4;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)rows * per; i += (int64_t)gridDim.x * 256) {
-    const int r = (int)(i / per), c = (int)(i % per) * 4;
-    split4(c < H ? *reinterpret_cast<const float4*>(w + r * stride + c) : make_float4(0.f, 0.f, 0.f, 0.f), out + (int64_t)r * pitch + c, (int64_t)rows * pitch);
   }
 }
 
@@ -211,10 +226,16 @@ template <bool BACK, int PLANES = 1>
 struct Logits {
   using Args = VocabArgs;
   static __device__ __forceinline__ int count(const Args& p) {
-    return ceil_div(*p.count, prod::BM * p.cg) * ceil_div(p.width, p.shape.bn);
+    return ceil_div(tokens(p), prod::BM * p.cg) * ceil_div(p.width, p.shape.bn);
   }
+  static __device__ __forceinline__ void prefetch(const Args& p) {
+    prod::prefetch_map(&p.xc);
+    prod::prefetch_map(&p.w);
+  }
+  // (count NULL: all, as they are)
+  static __device__ __forceinline__ int tokens(const Args& p) { return p.count ? *p.count : p.tokens; }
   static __device__ __forceinline__ void unit(const Args& p, int u, Unit& w) {
-    const int n = *p.count, mt_n = ceil_div(n, prod::BM * p.cg), nt_n = ceil_div(p.width, p.shape.bn);
+    const int n = tokens(p), mt_n = ceil_div(n, prod::BM * p.cg), nt_n = ceil_div(p.width, p.shape.bn);
     int mt, nt;
     prod::tile_of(u, mt_n, nt_n, mt, nt);
     w.a = hidden_map(p, n, &p.x, &p.xc);
@@ -230,7 +251,7 @@ struct Logits {
   }
   static __device__ __forceinline__ void finish(const Args& p, const Unit& w, const Tile& t, Store& st, float (&v)[4][32]) {
     const int row0 = w.m0 + t.rank * prod::BM + t.quad * 32, row = row0 + t.lane;
-    const int label = p.label[row] - p.v0 - w.n0;  // its column in this tile
+    const int label = (p.count || row < p.tokens ? p.label[row] : -1) - p.v0 - w.n0;  // its column in this tile
     if (BACK) {
       const float scale = p.scale[row], lse = p.lse[row];
 #pragma unroll
@@ -293,6 +314,12 @@ struct Grads {
       x_first = kx >= kw;
     }
   };
+  static __device__ __forceinline__ void prefetch(const Args& p) {
+    prod::prefetch_map(&p.dzk);
+    prod::prefetch_map(&p.dzm);
+    prod::prefetch_map(&p.wm);
+    prod::prefetch_map(&p.xcm);
+  }
   static __device__ __forceinline__ int count(const Args& p) {
     const Count c(p);
     return c.ux + c.uw;
@@ -348,12 +375,12 @@ struct Grads {
 
 // ---- what is joined at the end ------------------------------------------------------------
 // eight tokens a CTA, 64 threads on each one's parts
-__global__ void __launch_bounds__(512) vocab_join_kernel(const ra_vocab_loss_args a, const Prep p, const float2* stats, const float* zlab, int parts) {
+__global__ void __launch_bounds__(512) vocab_join_kernel(const ra_vocab_loss_args a, const Prep p, const float2* stats, const float* zlab, int parts, int direct) {
   __shared__ float2 sh[16][8];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, k = tid & 7, r = blockIdx.x * 8 + k;
   pdl_wait();
   pdl_trigger();
-  const int n = *p.count;
+  const int n = direct ? a.tokens : *p.count;
   if ((int)blockIdx.x * 8 >= n) return;
   // maximum and sum of two parts (-inf and 0, or NaN, where there is nothing, or nothing but NaN)
   auto join = [](float2 x, float2 y) {
@@ -382,6 +409,13 @@ __global__ void __launch_bounds__(512) vocab_join_kernel(const ra_vocab_loss_arg
 #pragma unroll
   for (int i = 1; i < 16; ++i) s = join(s, sh[i][k]);
   const float lse = s.x + logf(s.y);
+  if (direct) {
+    const int l = a.labels_dev[r];
+    if (l >= a.vocab) set_dev_error(a.err_dev, RA_DEVERR_BOUNDS);
+    a.loss_dev[r] = counted(a, l) ? lse - zlab[r] : 0.f;
+    if (a.lse_dev) a.lse_dev[r] = counted(a, l) ? lse : 0.f;
+    return;
+  }
   const int t = p.index[r];
   a.loss_dev[t] = lse - zlab[r];
   if (a.lse_dev) a.lse_dev[t] = lse;
@@ -514,11 +548,16 @@ Prep prep_of(const Plan& p, char* ws) {
   r.planes = p.planes;
   return r;
 }
-cudaError_t prepare(const ra_vocab_loss_args& a, const Prep& r, bool backward, cudaStream_t st) {
+Split split_of(const ra_vocab_loss_args& a, const Plan& p, char* ws, int v0, int width) {
+  return {static_cast<const float*>(a.w_dev) + v0 * a.w_stride, a.w_stride, reinterpret_cast<bf16*>(ws + p.wc), width, a.hidden, p.wide, p.pitch};
+}
+int split_ctas(const Split& s) { return (int)std::min<int64_t>(((int64_t)s.rows * s.width / 4 + 255) / 256, 8 * SMS); }
+cudaError_t prepare(const ra_vocab_loss_args& a, const Plan& p, char* ws, const Prep& r, bool backward, cudaStream_t st) {
   const int ctas = std::min(parts_of(a.tokens, 32), 2 * SMS);
   note_launch(1);
-  return a.dtype == RA_BF16 ? launch_pdl(vocab_prep_kernel<bf16>, dim3(ctas), dim3(256), 0, st, a, r, (int)backward)
-                            : launch_pdl(vocab_prep_kernel<float>, dim3(ctas), dim3(256), 0, st, a, r, (int)backward);
+  if (a.dtype == RA_BF16) return launch_pdl(vocab_prep_kernel<bf16>, dim3(ctas), dim3(256), 0, st, a, r, (int)backward, ctas, Split{});
+  const Split s = split_of(a, p, ws, 0, std::min(p.width, (int)a.vocab));
+  return launch_pdl(vocab_prep_kernel<float>, dim3(ctas + split_ctas(s)), dim3(256), 0, st, a, r, (int)backward, ctas, s);
 }
 
 VocabArgs args_of(const ra_vocab_loss_args& a, const Plan& p, char* ws) {
@@ -547,14 +586,15 @@ VocabArgs args_of(const ra_vocab_loss_args& a, const Plan& p, char* ws) {
   } while (0)
 
 // the piece's W, K-major boxes of bn rows or MN-major ones of 64; fp32: its planes, made first
+// (the first piece's by the launch that numbers the tokens)
 cudaError_t piece(const ra_vocab_loss_args& a, const Plan& p, char* ws, VocabArgs& g, int v0, int width, cudaStream_t st) {
   g.v0 = v0;
   g.width = width;
   g.wrow = p.planes == 1 ? v0 : 0;
-  if (p.planes == 1) return cudaSuccess;
+  if (p.planes == 1 || v0 == 0) return cudaSuccess;
+  const Split s = split_of(a, p, ws, v0, width);
   note_launch(1);
-  return launch_pdl(vocab_split_kernel, dim3((unsigned)std::min<int64_t>(((int64_t)width * p.wide / 4 + 255) / 256, 8 * SMS)), dim3(256), 0, st,
-                    static_cast<const float*>(a.w_dev) + v0 * a.w_stride, a.w_stride, reinterpret_cast<bf16*>(ws + p.wc), width, (int)a.hidden, p.wide, p.pitch);
+  return launch_pdl(vocab_split_kernel, dim3(split_ctas(s)), dim3(256), 0, st, s);
 }
 cudaError_t w_map(const ra_vocab_loss_args& a, const Plan& p, char* ws, CUtensorMap& m, int width, int box_rows) {
   if (p.planes == 1) MAP(m, a.w_dev, DT_BF16, 1, a.vocab, a.hidden, a.w_stride, 64, box_rows);
@@ -583,8 +623,14 @@ cudaError_t forward(const ra_vocab_loss_args& a, cudaStream_t st) {
   const Plan p = plan(a);
   char* ws = static_cast<char*>(a.workspace_dev);
   const Prep r = prep_of(p, ws);
-  DO(prepare(a, r, false, st));
+  // few tokens in bf16 are one tile's rows, counted or not: their logits need no numbering
+  const bool direct = p.planes == 1 && a.tokens <= prod::BM;
+  if (!direct) DO(prepare(a, p, ws, r, false, st));
   VocabArgs g = args_of(a, p, ws);
+  if (direct) {
+    g.count = nullptr;
+    g.label = a.labels_dev;
+  }
   g.cg = p.forward.cg;
   g.shape = prod::shape_of(p.forward.bn, p.forward.cg, terms_for(p.planes), std::min(p.chunk, LOGITS_CHUNK));
   DO(x_maps(a, p, ws, g.x, g.xc, prod::BM));
@@ -597,7 +643,7 @@ cudaError_t forward(const ra_vocab_loss_args& a, cudaStream_t st) {
     g.stat0 += 2 * parts_of(width, g.shape.bn);
   }
   note_launch(1);
-  return launch_pdl(vocab_join_kernel, dim3(parts_of(a.tokens, 8)), dim3(512), 0, st, a, r, (const float2*)g.stats, (const float*)g.zlab, (int)g.stat0);
+  return launch_pdl(vocab_join_kernel, dim3(parts_of(a.tokens, 8)), dim3(512), 0, st, a, r, (const float2*)g.stats, (const float*)g.zlab, (int)g.stat0, (int)direct);
 }
 
 template <typename T>
@@ -605,7 +651,7 @@ cudaError_t backward(const ra_vocab_loss_args& a, cudaStream_t st) {
   const Plan p = plan(a);
   char* ws = static_cast<char*>(a.workspace_dev);
   const Prep r = prep_of(p, ws);
-  DO(prepare(a, r, true, st));
+  DO(prepare(a, p, ws, r, true, st));
   VocabArgs g = args_of(a, p, ws), h;
   g.want_x = a.dx_dev != nullptr;
   g.want_w = a.dw_dev != nullptr;

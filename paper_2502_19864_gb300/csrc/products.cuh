@@ -245,7 +245,10 @@ struct Tile {
   int chunks;            // of 32 columns that this warp holds
 };
 
-// P: Args (with `Shape shape`, `unsigned* err`), static int count(const Args&), static void unit(const Args&, int, Unit&) and
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* tm) {
+  asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(tm)) : "memory");
+}
+// P: Args (with `Shape shape`, `unsigned* err`), static void prefetch(const Args&) (of the operands' maps), static int count(const Args&), static void unit(const Args&, int, Unit&) and
 // static void finish(const Args&, const Unit&, const Tile&, Store&, float (&v)[4][32]).
 template <class P, int CG>
 __global__ void __launch_bounds__(THREADS, 1) products_kernel(const __grid_constant__ typename P::Args p) {
@@ -274,6 +277,7 @@ __global__ void __launch_bounds__(THREADS, 1) products_kernel(const __grid_const
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
+  if (threadIdx.x == 32) P::prefetch(p);
   if (CG == 2) {  // the barriers of both CTAs are there before either signals the other's
     __syncthreads();
     cluster_arrive();
