@@ -185,7 +185,7 @@ struct OrthArgs {
   void* dst;
   int64_t dst_stride, dst_matrix_stride;
   int rows, cols;          // of the product
-  int k, n, pa, pb, cg, dtype;
+  int k, n, cg, dtype;
   bool a_mn, b_mn, sym, last, map_out;
   float add, add2, mul2;
 };
@@ -199,8 +199,10 @@ struct OrthArgs {
     if (_e != cudaSuccess) return _e;        \
   } while (0)
 
-template <int PLANES>
+// PLANES: of what is kept; A_PLANES, B_PLANES: of the operands
+template <int PLANES, int A_PLANES, int B_PLANES>
 struct Step {
+  static constexpr int PA = A_PLANES, PB = B_PLANES;
   using Args = OrthArgs;
   // of a symmetric product (square tiles) those on and above the diagonal, column by column of tiles
   static __host__ __device__ __forceinline__ int tiles(const Args& p, int& mt, int& nt) {
@@ -235,8 +237,8 @@ struct Step {
     w.n0 = w.br = nt * p.shape.bn;
     w.ak = w.bk = w.kb0 = 0;
     w.job = p.sym && mt != nt;  // its mirror image too
-    w.az = w.z * p.pa;
-    w.bz = w.z * p.pb;
+    w.az = w.z * PA;
+    w.bz = w.z * PB;
     w.kb1 = (p.k + prod::BK - 1) / prod::BK;
     w.a_mn = p.a_mn;
     w.b_mn = p.b_mn;
@@ -749,13 +751,13 @@ Plan plan(const ra_orthogonalize_args& a) {
 
 // A symmetric product: all tiles, or (sym) square ones on and above the diagonal, which takes rounds off and costs a round the
 // mirrored stores: 2048 x 2048 of K = 5632 in two planes 98 -> 73 us, two of 777 x 777 in three planes 49 -> 60
-Pick pick_sym(int rows, int n, int blocks, bool& sym) {
+Pick pick_sym(int rows, int n, int blocks, int planes, bool& sym) {
   auto time = [&](Pick k) {
     const int64_t t = parts_of(rows, k.bn);
     return (double)parts_of(n * t * (t + 1) / 2, prod::SMS / k.cg) * (blocks * prod::block_time(k) + 6.) + (k.cg == 2 ? 1. : 0.);
   };
   const Pick one = {1, 128}, two = {2, 256}, best = rows > 128 && time(two) < time(one) ? two : one;
-  const Pick all = prod::pick(rows, rows, n, blocks);
+  const Pick all = prod::pick(rows, rows, n, blocks, planes, planes);
   sym = time(best) < prod::time_of(all, rows, rows, n, blocks);
   return sym ? best : all;
 }
@@ -789,21 +791,19 @@ cudaError_t run(const ra_orthogonalize_args& a, cudaStream_t st) {
   g.n = n;
   g.dtype = a.dtype;
   auto shape = [&](OrthArgs& s, int rows, int cols, int k, int pa, int pb, bool sym) {
-    const prod::Terms terms = prod::terms_of(pa, pb);
-    const int blocks = parts_of(k, prod::BK) * terms.n;
-    const Pick c = sym ? pick_sym(rows, n, blocks, sym) : prod::pick(rows, cols, n, blocks);
+    const int blocks = parts_of(k, prod::BK) * prod::terms_of(pa, pb).n;
+    const Pick c = sym ? pick_sym(rows, n, blocks, pa, sym) : prod::pick(rows, cols, n, blocks, pa, pb);
     s.rows = rows;
     s.cols = cols;
     s.k = k;
-    s.pa = pa;
-    s.pb = pb;
     s.sym = sym;
     s.cg = c.cg;
-    s.shape = prod::shape_of(c.bn, c.cg, terms, chunk);
+    s.shape = prod::shape_of(c.bn, c.cg, pa, pb, chunk);
   };
-  auto go = [&](const OrthArgs& s) {
+  constexpr int PL = es == 2 ? 2 : 3, ONE = es == 2 ? 1 : 3;  // planes of what is kept, and of the matrices as they come
+  auto go = [&](const OrthArgs& s, auto step) {
+    using S = decltype(step);
     int mt, nt;
-    using S = Step<es == 2 ? 2 : 3>;
     const int u = (int)std::min<int64_t>((int64_t)n * S::tiles(s, mt, nt), 1 << 20);
     return s.cg == 2 ? prod::launch<S, 2>(s, u, st) : prod::launch<S, 1>(s, u, st);
   };
@@ -854,9 +854,10 @@ cudaError_t run(const ra_orthogonalize_args& a, cudaStream_t st) {
                       (n == 1 || a.out_matrix_stride == a.rows * a.out_stride);
       if (apply.map_out) MAP(apply.out, a.out_dev, a.dtype, n, a.rows, a.cols, a.out_stride, es == 2 ? 32 : 16, 32);
     }
-    DO(go(gram));
-    DO(go(square));
-    DO(go(apply));
+    using Full = Step<PL, PL, PL>;
+    DO(px == PL ? go(gram, Full()) : go(gram, Step<PL, ONE, ONE>()));
+    DO(go(square, Full()));
+    DO(px == PL ? go(apply, Full()) : wide ? go(apply, Step<PL, PL, ONE>()) : go(apply, Step<PL, ONE, PL>()));
   }
   return cudaSuccess;
 }

@@ -221,9 +221,10 @@ __device__ __forceinline__ const CUtensorMap* hidden_map(const VocabArgs& p, int
   return p.planes == 1 && count == p.tokens ? given : gathered;
 }
 
-// tiles of logits; BACK: into dz, else into statistics; PLANES: of dz
-template <bool BACK, int PLANES = 1>
+// tiles of logits; BACK: into dz, else into statistics; PLANES: of the operands and of dz
+template <bool BACK, int PLANES>
 struct Logits {
+  static constexpr int PA = PLANES, PB = PLANES;
   using Args = VocabArgs;
   static __device__ __forceinline__ int count(const Args& p) {
     return ceil_div(tokens(p), prod::BM * p.cg) * ceil_div(p.width, p.shape.bn);
@@ -297,7 +298,9 @@ struct Logits {
 };
 
 // dx sums (job 0) and dw (job 1) of a piece, the longer ones first
+template <int PLANES>
 struct Grads {
+  static constexpr int PA = PLANES, PB = PLANES;
   using Args = VocabArgs;
   struct Count {
     int n, mx, mw, nt, kx, kw, ux, uw;
@@ -458,7 +461,6 @@ struct Plan {
 
 constexpr int LOGITS_CHUNK = 16;  // k-blocks of an accumulator of logits, whose error is the loss's: 4e-7 of it
 
-prod::Terms terms_for(int planes) { return prod::terms_of(planes, planes); }
 // (the same whether both gradients are wanted or one)
 Plan plan(const ra_vocab_loss_args& a) {
   Plan p = {};
@@ -475,8 +477,8 @@ Plan plan(const ra_vocab_loss_args& a) {
   p.width = up(parts_of(a.vocab, p.pieces), 256);
   p.pieces = parts_of(a.vocab, p.width);
 
-  const int hb = parts_of(a.hidden, prod::BK), terms = terms_for(p.planes).n;
-  p.logits = prod::pick(a.tokens, p.pieces == 1 || !f32 ? a.vocab : p.width, 1, hb * terms);
+  const int hb = parts_of(a.hidden, prod::BK), terms = prod::terms_of(p.planes, p.planes).n;
+  p.logits = prod::pick(a.tokens, p.pieces == 1 || !f32 ? a.vocab : p.width, 1, hb * terms, p.planes, p.planes);
   if (p.logits.bn < 128) p.logits.bn = 128;
   p.forward = p.logits;
   if (a.tokens <= prod::BM && !f32) {
@@ -491,6 +493,7 @@ Plan plan(const ra_vocab_loss_args& a) {
   for (Pick k : {Pick{1, 64}, Pick{1, 128}, Pick{1, 256}, Pick{2, 256}}) {
     if (k.cg == 2 && (a.tokens <= prod::BM || a.hidden <= 128)) continue;
     if (k.bn > 64 && a.hidden <= k.bn / 2) continue;
+    if (prod::stages_of(k.bn, k.cg, p.planes, p.planes) < 2) continue;
     const int64_t nt = parts_of(a.hidden, k.bn);
     const int64_t ux = parts_of(a.tokens, prod::BM * k.cg) * nt, uw = parts_of(p.width, prod::BM * k.cg) * nt;
     const double all = (double)ux * kx + (double)uw * kw, workers = SMS / k.cg;
@@ -619,6 +622,7 @@ cudaError_t x_maps(const ra_vocab_loss_args& a, const Plan& p, char* ws, CUtenso
   return cudaSuccess;
 }
 
+template <int PLANES>
 cudaError_t forward(const ra_vocab_loss_args& a, cudaStream_t st) {
   const Plan p = plan(a);
   char* ws = static_cast<char*>(a.workspace_dev);
@@ -632,21 +636,22 @@ cudaError_t forward(const ra_vocab_loss_args& a, cudaStream_t st) {
     g.label = a.labels_dev;
   }
   g.cg = p.forward.cg;
-  g.shape = prod::shape_of(p.forward.bn, p.forward.cg, terms_for(p.planes), std::min(p.chunk, LOGITS_CHUNK));
+  g.shape = prod::shape_of(p.forward.bn, p.forward.cg, p.planes, p.planes, std::min(p.chunk, LOGITS_CHUNK));
   DO(x_maps(a, p, ws, g.x, g.xc, prod::BM));
   const int step = p.planes == 1 ? a.vocab : p.width;
   for (int v0 = 0; v0 < a.vocab; v0 += step) {
     const int width = std::min(step, a.vocab - v0);
     DO(piece(a, p, ws, g, v0, width, st));
     DO(w_map(a, p, ws, g.w, width, p.forward.bn / p.forward.cg));
-    DO(products<Logits<false>>(g, (int64_t)parts_of(a.tokens, prod::BM * g.cg) * parts_of(width, g.shape.bn), st));
+    const int64_t tiles = (int64_t)parts_of(a.tokens, prod::BM * g.cg) * parts_of(width, g.shape.bn);
+    DO((products<Logits<false, PLANES>>(g, tiles, st)));
     g.stat0 += 2 * parts_of(width, g.shape.bn);
   }
   note_launch(1);
   return launch_pdl(vocab_join_kernel, dim3(parts_of(a.tokens, 8)), dim3(512), 0, st, a, r, (const float2*)g.stats, (const float*)g.zlab, (int)g.stat0, (int)direct);
 }
 
-template <typename T>
+template <typename T, int PLANES>
 cudaError_t backward(const ra_vocab_loss_args& a, cudaStream_t st) {
   const Plan p = plan(a);
   char* ws = static_cast<char*>(a.workspace_dev);
@@ -666,17 +671,16 @@ cudaError_t backward(const ra_vocab_loss_args& a, cudaStream_t st) {
   }
   h = g;
   g.cg = p.logits.cg;
-  g.shape = prod::shape_of(p.logits.bn, p.logits.cg, terms_for(p.planes), std::min(p.chunk, LOGITS_CHUNK));
+  g.shape = prod::shape_of(p.logits.bn, p.logits.cg, p.planes, p.planes, std::min(p.chunk, LOGITS_CHUNK));
   h.cg = p.grads.cg;
-  h.shape = prod::shape_of(p.grads.bn, p.grads.cg, terms_for(p.planes), p.chunk);
+  h.shape = prod::shape_of(p.grads.bn, p.grads.cg, p.planes, p.planes, p.chunk);
   for (int v0 = 0; v0 < a.vocab; v0 += p.width) {
     const int width = std::min(p.width, a.vocab - v0);
     DO(piece(a, p, ws, g, v0, width, st));
     DO(w_map(a, p, ws, g.w, width, p.logits.bn / p.logits.cg));
     MAP(g.dz, ws + p.dz, DT_BF16, p.planes, p.rows, p.width, p.width, 32, 32);
     const int64_t tiles = (int64_t)parts_of(a.tokens, prod::BM * g.cg) * parts_of(width, g.shape.bn);
-    if (p.planes == 1) DO((products<Logits<true, 1>>(g, tiles, st)));
-    else DO((products<Logits<true, 3>>(g, tiles, st)));
+    DO((products<Logits<true, PLANES>>(g, tiles, st)));
     h.v0 = v0;
     h.width = width;
     h.wrow = g.wrow;
@@ -684,7 +688,7 @@ cudaError_t backward(const ra_vocab_loss_args& a, cudaStream_t st) {
     MAP(h.dzk, ws + p.dz, DT_BF16, p.planes, p.rows, p.width, p.width, 64, prod::BM);
     MAP(h.dzm, ws + p.dz, DT_BF16, p.planes, p.rows, p.width, p.width, 64, 64);
     const int64_t nt = parts_of(a.hidden, h.shape.bn);
-    DO(products<Grads>(h, nt * ((h.want_x ? (int64_t)parts_of(a.tokens, prod::BM * h.cg) * h.splits_x : 0) +
+    DO(products<Grads<PLANES>>(h, nt * ((h.want_x ? (int64_t)parts_of(a.tokens, prod::BM * h.cg) * h.splits_x : 0) +
                                 (h.want_w ? (int64_t)parts_of(width, prod::BM * h.cg) * h.splits_w : 0)), st));
   }
   if (a.dw_dev && p.splits_w > 1) {
@@ -705,13 +709,13 @@ cudaError_t backward(const ra_vocab_loss_args& a, cudaStream_t st) {
 }  // namespace
 
 size_t vocab_loss_workspace(const ra_vocab_loss_args& a) { return plan(a).bytes; }
-cudaError_t vocab_loss_fwd(const ra_vocab_loss_args& a, cudaStream_t st) { return forward(a, st); }
+cudaError_t vocab_loss_fwd(const ra_vocab_loss_args& a, cudaStream_t st) { return a.dtype == RA_BF16 ? forward<1>(a, st) : forward<3>(a, st); }
 cudaError_t vocab_loss_bwd(const ra_vocab_loss_args& a, cudaStream_t st) {
   if (a.tokens == 0) {
     const size_t es = a.dtype == RA_BF16 ? 2 : 4;
     return cudaMemset2DAsync(a.dw_dev, a.dw_stride * es, 0, a.hidden * es, a.vocab, st);
   }
-  return a.dtype == RA_BF16 ? backward<bf16>(a, st) : backward<float>(a, st);
+  return a.dtype == RA_BF16 ? backward<bf16, 1>(a, st) : backward<float, 3>(a, st);
 }
 
 }  // namespace ra

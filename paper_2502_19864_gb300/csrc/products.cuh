@@ -39,7 +39,7 @@ struct Terms {
 };
 // Of operands of pa and pb planes: all pairs (i, j) with i + j less than the larger number; what is left out is below 2^-8 of
 // the last plane's part (three planes: (0, 2) (1, 1) (2, 0) (0, 1) (1, 0) (0, 0), 2^-24 of the whole)
-inline Terms terms_of(int pa, int pb) {
+__host__ __device__ constexpr Terms terms_of(int pa, int pb) {
   Terms t = {0, 0u, 0u};
   for (int sum = (pa > pb ? pa : pb) - 1; sum >= 0; --sum)
     for (int i = 0; i <= sum; ++i)
@@ -51,19 +51,24 @@ inline Terms terms_of(int pa, int pb) {
   return t;
 }
 
+// A stage of the ring has a k-block of all planes of both operands: each comes once, for all the terms it is in (two of 777 x 777
+// of K = 1000 in three planes: 38 us with a stage a term, which loads twice as much)
 struct Shape {
   int bn;       // columns of a tile: a multiple of 32, of 64 CG for an MN-major B
   int chunk;    // k-blocks of an accumulator
-  int stages, stage_bytes;
-  Terms terms;
+  int b_bytes, stages, stage_bytes;
 };
-inline Shape shape_of(int bn, int cg, Terms terms, int chunk) {
+inline int stages_of(int bn, int cg, int pa, int pb) {
+  const int stage = pa * A_BYTES + pb * ((bn / cg + 63) / 64 * 64 * BK * 2);
+  return RING / stage < MAX_STAGES ? RING / stage : MAX_STAGES;
+}
+inline Shape shape_of(int bn, int cg, int pa, int pb, int chunk) {
   Shape s;
   s.bn = bn;
   s.chunk = chunk;
-  s.stage_bytes = A_BYTES + (bn / cg + 63) / 64 * 64 * BK * 2;
-  s.stages = RING / s.stage_bytes < MAX_STAGES ? RING / s.stage_bytes : MAX_STAGES;
-  s.terms = terms;
+  s.b_bytes = (bn / cg + 63) / 64 * 64 * BK * 2;
+  s.stage_bytes = pa * A_BYTES + pb * s.b_bytes;
+  s.stages = stages_of(bn, cg, pa, pb);
   return s;
 }
 
@@ -79,15 +84,18 @@ inline double block_time(Pick k) {
   if (k.cg == 2) return k.bn > 128 ? 0.345 : 0.25;
   return k.bn <= 64 ? 0.2 : k.bn <= 128 ? 0.222 : k.bn <= 192 ? 0.31 : 0.365;
 }
-// ... of `batch` products m x n of `blocks` k-blocks: rounds of tiles, each with about 1 us for its start and end
+// ... of `batch` products m x n of `blocks` k-blocks, terms counted: rounds of tiles, each with about 1 us for its start and end
 inline double time_of(Pick k, int64_t m, int64_t n, int64_t batch, int blocks) {
   const int64_t tiles = batch * parts_of(m, BM * k.cg) * parts_of(n, k.bn);
   return (double)parts_of(tiles, SMS / k.cg) * (blocks * block_time(k) + 1.) + (k.cg == 2 ? 1. : 0.);
 }
-inline Pick pick(int64_t m, int64_t n, int64_t batch, int blocks) {
+// the fastest, of those whose ring has two stages
+inline Pick pick(int64_t m, int64_t n, int64_t batch, int blocks, int pa, int pb) {
   Pick best = {1, n <= 64 ? 64 : 128};
   for (Pick k : {Pick{1, 64}, Pick{1, 256}, Pick{2, 256}})
-    if ((k.cg == 1 || m > BM) && n > k.bn / 2 && time_of(k, m, n, batch, blocks) < time_of(best, m, n, batch, blocks)) best = k;
+    if ((k.cg == 1 || m > BM) && n > k.bn / 2 && stages_of(k.bn, k.cg, pa, pb) >= 2 &&
+        time_of(k, m, n, batch, blocks) < time_of(best, m, n, batch, blocks))
+      best = k;
   return best;
 }
 
@@ -248,7 +256,7 @@ struct Tile {
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* tm) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(tm)) : "memory");
 }
-// P: Args (with `Shape shape`, `unsigned* err`), static void prefetch(const Args&) (of the operands' maps), static int count(const Args&), static void unit(const Args&, int, Unit&) and
+// P: the operands' planes PA and PB, Args (with `Shape shape`, `unsigned* err`), static void prefetch(const Args&) (of the operands' maps), static int count(const Args&), static void unit(const Args&, int, Unit&) and
 // static void finish(const Args&, const Unit&, const Tile&, Store&, float (&v)[4][32]).
 template <class P, int CG>
 __global__ void __launch_bounds__(THREADS, 1) products_kernel(const __grid_constant__ typename P::Args p) {
@@ -299,7 +307,6 @@ __global__ void __launch_bounds__(THREADS, 1) products_kernel(const __grid_const
   pdl_wait();
   pdl_trigger();
   const int units = P::count(p);
-  const Terms terms = p.shape.terms;
   const int chunk = p.shape.chunk;
 
   if (warp == 0) {
@@ -309,36 +316,38 @@ __global__ void __launch_bounds__(THREADS, 1) products_kernel(const __grid_const
       uint32_t phase = 0;
       bool ok = true;
       const int boxes = (bnc + 63) / 64;
-      const uint32_t bytes = CG * (uint32_t)A_BYTES;
       for (int u = worker; ok && u < units; u += workers) {
         Unit w;
         P::unit(p, u, w);
         const int ar = w.ar + rank * BM, br = w.br + rank * bnc;
-        const uint32_t all = bytes + CG * (uint32_t)((w.b_mn ? boxes * 64 : bnc) * BK * 2);
+        const uint32_t all = CG * (uint32_t)(P::PA * A_BYTES + P::PB * (w.b_mn ? boxes * 64 : bnc) * BK * 2);
         for (int c0 = w.kb0; ok && c0 < w.kb1; c0 += chunk) {
           const int c1 = min(c0 + chunk, w.kb1);
-          for (int t = 0; ok && t < terms.n; ++t) {
-            const int az = w.az + (int)(terms.a >> (2 * t) & 3u), bz = w.bz + (int)(terms.b >> (2 * t) & 3u);
-            for (int kb = c0; kb < c1; ++kb) {
-              if (!mbar_wait(&empty_bar[stage], phase ^ 1u, &abort_sh, p.err)) { ok = false; break; }
-              if (rank == 0) mbar_expect_tx(&full_bar[stage], all);
-              const uint32_t sa = smem_base + stage * p.shape.stage_bytes, sb = sa + A_BYTES;
-              const uint32_t full = CG == 2 ? peer_addr(smem_u32(&full_bar[stage]), 0) : smem_u32(&full_bar[stage]);
-              const int ka = w.ak + kb * BK, kbb = w.bk + kb * BK;
+          for (int kb = c0; kb < c1; ++kb) {
+            if (!mbar_wait(&empty_bar[stage], phase ^ 1u, &abort_sh, p.err)) { ok = false; break; }
+            if (rank == 0) mbar_expect_tx(&full_bar[stage], all);
+            const uint32_t full = CG == 2 ? peer_addr(smem_u32(&full_bar[stage]), 0) : smem_u32(&full_bar[stage]);
+            const int ka = w.ak + kb * BK, kbb = w.bk + kb * BK;
+            uint32_t to = smem_base + stage * p.shape.stage_bytes;
+#pragma unroll
+            for (int z = 0; z < P::PA; ++z, to += A_BYTES) {
               if (w.a_mn) {
-                load<CG>(w.a, sa, full, ar, ka, az);
-                load<CG>(w.a, sa + 8192, full, ar + 64, ka, az);
+                load<CG>(w.a, to, full, ar, ka, w.az + z);
+                load<CG>(w.a, to + 8192, full, ar + 64, ka, w.az + z);
               } else {
-                load<CG>(w.a, sa, full, ka, ar, az);
+                load<CG>(w.a, to, full, ka, ar, w.az + z);
               }
-              if (w.b_mn) {
-                for (int x = 0; x < boxes; ++x) load<CG>(w.b, sb + x * 8192, full, br + 64 * x, kbb, bz);
-              } else {
-                load<CG>(w.b, sb, full, kbb, br, bz);
-              }
-              ++issued;
-              if (++stage == stages) { stage = 0; phase ^= 1u; }
             }
+#pragma unroll
+            for (int z = 0; z < P::PB; ++z, to += p.shape.b_bytes) {
+              if (w.b_mn) {
+                for (int x = 0; x < boxes; ++x) load<CG>(w.b, to + x * 8192, full, br + 64 * x, kbb, w.bz + z);
+              } else {
+                load<CG>(w.b, to, full, kbb, br, w.bz + z);
+              }
+            }
+            ++issued;
+            if (++stage == stages) { stage = 0; phase ^= 1u; }
           }
         }
       }
@@ -365,10 +374,11 @@ __global__ void __launch_bounds__(THREADS, 1) products_kernel(const __grid_const
         P::unit(p, u, w);
         const uint32_t idesc = idesc_bf16(CG * BM, bn) | (w.a_mn ? 1u << 15 : 0u) | (w.b_mn ? 1u << 16 : 0u);
         // 16 values of K on: 32 bytes inside the swizzle's atom, or 16 rows of 128 bytes
-        const uint64_t ad = w.a_mn ? mnmaj : kmaj, bd = (w.b_mn ? mnmaj : kmaj) + (uint64_t)(A_BYTES / 16);
+        const uint64_t ad = w.a_mn ? mnmaj : kmaj, bd = (w.b_mn ? mnmaj : kmaj) + (uint64_t)(P::PA * A_BYTES / 16);
+        const uint32_t bplane = (uint32_t)p.shape.b_bytes / 16;
         const uint64_t as = w.a_mn ? 128u : 2u, bs = w.b_mn ? 128u : 2u;
         for (int c0 = w.kb0; ok && c0 < w.kb1; c0 += chunk) {
-          const int steps = (min(c0 + chunk, w.kb1) - c0) * terms.n;
+          const int steps = min(c0 + chunk, w.kb1) - c0;
           if (!mbar_wait(&tempty_bar[acc], acc_phase ^ 1u, &abort_sh, p.err)) { ok = false; break; }
           tc_fence_after();
           const uint32_t d = tmem_base + (uint32_t)(acc * MAX_BN);
@@ -376,11 +386,16 @@ __global__ void __launch_bounds__(THREADS, 1) products_kernel(const __grid_const
             if (!mbar_wait(&full_bar[stage], phase, &abort_sh, p.err)) { ok = false; break; }
             tc_fence_after();
             const uint64_t off = (uint64_t)(stage * (p.shape.stage_bytes / 16));
+            constexpr Terms terms = terms_of(P::PA, P::PB);
 #pragma unroll
-            for (int k = 0; k < BK / 16; ++k) {
-              const uint64_t x = ad + off + as * (uint64_t)k, y = bd + off + bs * (uint64_t)k;
-              if (CG == 2) umma_bf16_pair(d, x, y, idesc, i | k);
-              else umma_bf16(d, x, y, idesc, i | k);
+            for (int t = 0; t < terms.n; ++t) {
+              const uint64_t at = ad + off + (uint64_t)((terms.a >> (2 * t) & 3u) * (A_BYTES / 16)), bt = bd + off + (uint64_t)((terms.b >> (2 * t) & 3u) * bplane);
+#pragma unroll
+              for (int k = 0; k < BK / 16; ++k) {
+                const uint64_t x = at + as * (uint64_t)k, y = bt + bs * (uint64_t)k;
+                if (CG == 2) umma_bf16_pair(d, x, y, idesc, i | t | k);
+                else umma_bf16(d, x, y, idesc, i | t | k);
+              }
             }
             if (CG == 2) umma_commit_pair(&empty_bar[stage]);
             else umma_commit(&empty_bar[stage]);
