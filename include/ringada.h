@@ -627,8 +627,8 @@ size_t ra_vocab_loss_workspace_bytes(const ra_vocab_loss_args* args);
 ra_status ra_vocab_loss_forward(const ra_vocab_loss_args* args, ra_stream_t stream);
 ra_status ra_vocab_loss_backward(const ra_vocab_loss_args* args, ra_stream_t stream);
 
-/* Orthogonalisation of updates by Newton-Schulz products, for n_matrices matrices x [rows, cols] of their own, matrix_stride
- * elements apart: X = x / (|x| + eps) (the root of the sum of squares), then `steps` times
+/* Orthogonalisation of updates by Newton-Schulz products, for n_matrices matrices x [rows, cols], matrix_stride elements
+ * apart (one behind the other, or side by side in wider rows): X = x / (|x| + eps) (the root of the sum of squares), then `steps` times
  *   X <- a X + (b X X^T + c (X X^T)^2) X
  * and out = X in the type.  With a = 3.4445, b = -4.775, c = 2.0315 five steps bring singular values that are not too
  * small to between about 0.7 and 1.2 (what is subtracted from a weight in place of its momentum).  A matrix with an

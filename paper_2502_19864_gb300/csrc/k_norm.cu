@@ -523,7 +523,7 @@ template <typename T, typename W, int VEC, int NV, int ROWS, int DEPTH = 0>
 cudaError_t launch(const ra_norm_args& a, bool backward, cudaStream_t st) {
   const int vecs = (a.hidden + VEC - 1) / VEC;
   const int threads = ((vecs + NV - 1) / NV + 31) / 32 * 32;
-  const int groups = (a.rows + ROWS - 1) / ROWS;
+  const int groups = (int)(((int64_t)a.rows + ROWS - 1) / ROWS);
   const int each = DEPTH * ROWS * NV * threads * 16;  // of the ring, an input
   constexpr int most_smem = DEPTH * ROWS * NV * max_threads(VEC * NV, ROWS) * 16;
   note_launch(1);

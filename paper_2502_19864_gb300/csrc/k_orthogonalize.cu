@@ -756,7 +756,7 @@ Pick pick_sym(int rows, int n, int blocks, int planes, bool& sym) {
     const int64_t t = parts_of(rows, k.bn);
     return (double)parts_of(n * t * (t + 1) / 2, prod::SMS / k.cg) * (blocks * prod::block_time(k) + 6.) + (k.cg == 2 ? 1. : 0.);
   };
-  const Pick one = {1, 128}, two = {2, 256}, best = rows > 128 && time(two) < time(one) ? two : one;
+  const Pick one = {1, 128}, two = {2, 256}, best = rows > 128 && prod::takes(two, planes, planes) && time(two) < time(one) ? two : one;
   const Pick all = prod::pick(rows, rows, n, blocks, planes, planes);
   sym = time(best) < prod::time_of(all, rows, rows, n, blocks);
   return sym ? best : all;

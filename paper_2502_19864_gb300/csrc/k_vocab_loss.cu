@@ -435,9 +435,18 @@ __global__ void __launch_bounds__(128) vocab_sum_kernel(const float* sums, int s
     T* o = out + (index ? index[r] : r) * stride;
     for (int c = threadIdx.x * 4; c < H; c += 512) {
       float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int i = 0; i < splits; ++i) {
-        const float4 v = *reinterpret_cast<const float4*>(sums + i * part + (int64_t)r * pitch + c);
-        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+      for (int i0 = 0; i0 < splits; i0 += 8) {  // eight at once on their way
+        float4 v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          v[i] = i0 + i < splits ? *reinterpret_cast<const float4*>(sums + (i0 + i) * part + (int64_t)r * pitch + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          s.x += v[i].x;
+          s.y += v[i].y;
+          s.z += v[i].z;
+          s.w += v[i].w;
+        }
       }
       if (sizeof(T) == 4) {
         *reinterpret_cast<float4*>(o + c) = s;
@@ -490,16 +499,18 @@ Plan plan(const ra_vocab_loss_args& a) {
 
   const int kx = parts_of(p.width, prod::BK), kw = parts_of(a.tokens > 0 ? a.tokens : 1, prod::BK);
   double best = 1e30;
-  for (Pick k : {Pick{1, 64}, Pick{1, 128}, Pick{1, 256}, Pick{2, 256}}) {
+  for (Pick k : {Pick{1, 64}, Pick{1, 128}, Pick{1, 256}, Pick{2, 128}, Pick{2, 256}}) {
     if (k.cg == 2 && (a.tokens <= prod::BM || a.hidden <= 128)) continue;
     if (k.bn > 64 && a.hidden <= k.bn / 2) continue;
-    if (prod::stages_of(k.bn, k.cg, p.planes, p.planes) < 2) continue;
+    if (!prod::takes(k, p.planes, p.planes)) continue;
     const int64_t nt = parts_of(a.hidden, k.bn);
     const int64_t ux = parts_of(a.tokens, prod::BM * k.cg) * nt, uw = parts_of(p.width, prod::BM * k.cg) * nt;
     const double all = (double)ux * kx + (double)uw * kw, workers = SMS / k.cg;
-    // a tile's k-blocks are cut so that none has more than about a third of a worker's share of all of them
-    auto cut = [&](int kb) { return std::max(1, std::min(std::min(16, kb * terms / 16), (int)(3. * kb * workers / std::max(all, 1.)))); };
-    const int sx = cut(kx), sw = p.pieces == 1 && (int64_t)p.width * a.hidden * 4 * cut(kw) <= (128ll << 20) ? cut(kw) : 1;
+    // A tile's k-blocks are cut so that none has more than about a share of a worker's part of all of them: dx, whose sums are added
+    // up at the end anyway, a sixth, into parts of 16 products at least (4096 tokens, half of them counted, 657 -> 607 us against a
+    // third: fewer tokens than were planned for leave its long tiles to the end), dw a third, into parts of 64
+    auto cut = [&](int kb, int least, double share) { return std::max(1, std::min(std::min(16, kb * terms / least), (int)(share * kb * workers / std::max(all, 1.)))); };
+    const int sx = cut(kx, 16, 6.), cw = cut(kw, 64, 3.), sw = p.pieces == 1 && (int64_t)p.width * a.hidden * 4 * cw <= (128ll << 20) ? cw : 1;
     const double longest = std::max(parts_of(kx, sx), parts_of(kw, sw));
     const double time = (std::max(all / workers, longest) + 0.3 * longest) * terms * prod::block_time(k) + (double)(ux * sx + uw * sw) / workers * 1.;
     if (time < best) {
@@ -627,22 +638,25 @@ cudaError_t forward(const ra_vocab_loss_args& a, cudaStream_t st) {
   const Plan p = plan(a);
   char* ws = static_cast<char*>(a.workspace_dev);
   const Prep r = prep_of(p, ws);
+  VocabArgs g = args_of(a, p, ws);
+  g.cg = p.forward.cg;
+  g.shape = prod::shape_of(p.forward.bn, p.forward.cg, p.planes, p.planes, std::min(p.chunk, LOGITS_CHUNK));
+  // (what may be refused, before anything is enqueued)
+  DO(x_maps(a, p, ws, g.x, g.xc, prod::BM));
+  if (p.planes == 1) DO(w_map(a, p, ws, g.w, a.vocab, p.forward.bn / p.forward.cg));
   // few tokens in bf16 are one tile's rows, counted or not: their logits need no numbering
   const bool direct = p.planes == 1 && a.tokens <= prod::BM;
-  if (!direct) DO(prepare(a, p, ws, r, false, st));
-  VocabArgs g = args_of(a, p, ws);
   if (direct) {
     g.count = nullptr;
     g.label = a.labels_dev;
+  } else {
+    DO(prepare(a, p, ws, r, false, st));
   }
-  g.cg = p.forward.cg;
-  g.shape = prod::shape_of(p.forward.bn, p.forward.cg, p.planes, p.planes, std::min(p.chunk, LOGITS_CHUNK));
-  DO(x_maps(a, p, ws, g.x, g.xc, prod::BM));
   const int step = p.planes == 1 ? a.vocab : p.width;
   for (int v0 = 0; v0 < a.vocab; v0 += step) {
     const int width = std::min(step, a.vocab - v0);
     DO(piece(a, p, ws, g, v0, width, st));
-    DO(w_map(a, p, ws, g.w, width, p.forward.bn / p.forward.cg));
+    if (p.planes > 1) DO(w_map(a, p, ws, g.w, width, p.forward.bn / p.forward.cg));
     const int64_t tiles = (int64_t)parts_of(a.tokens, prod::BM * g.cg) * parts_of(width, g.shape.bn);
     DO((products<Logits<false, PLANES>>(g, tiles, st)));
     g.stat0 += 2 * parts_of(width, g.shape.bn);
@@ -656,7 +670,6 @@ cudaError_t backward(const ra_vocab_loss_args& a, cudaStream_t st) {
   const Plan p = plan(a);
   char* ws = static_cast<char*>(a.workspace_dev);
   const Prep r = prep_of(p, ws);
-  DO(prepare(a, p, ws, r, true, st));
   VocabArgs g = args_of(a, p, ws), h;
   g.want_x = a.dx_dev != nullptr;
   g.want_w = a.dw_dev != nullptr;
@@ -674,17 +687,22 @@ cudaError_t backward(const ra_vocab_loss_args& a, cudaStream_t st) {
   g.shape = prod::shape_of(p.logits.bn, p.logits.cg, p.planes, p.planes, std::min(p.chunk, LOGITS_CHUNK));
   h.cg = p.grads.cg;
   h.shape = prod::shape_of(p.grads.bn, p.grads.cg, p.planes, p.planes, p.chunk);
+  if (p.planes == 1) {
+    DO(w_map(a, p, ws, g.w, a.vocab, p.logits.bn / p.logits.cg));
+    DO(w_map(a, p, ws, h.wm, a.vocab, 64));
+  }
+  DO(prepare(a, p, ws, r, true, st));
   for (int v0 = 0; v0 < a.vocab; v0 += p.width) {
     const int width = std::min(p.width, a.vocab - v0);
     DO(piece(a, p, ws, g, v0, width, st));
-    DO(w_map(a, p, ws, g.w, width, p.logits.bn / p.logits.cg));
+    if (p.planes > 1) DO(w_map(a, p, ws, g.w, width, p.logits.bn / p.logits.cg));
     MAP(g.dz, ws + p.dz, DT_BF16, p.planes, p.rows, p.width, p.width, 32, 32);
     const int64_t tiles = (int64_t)parts_of(a.tokens, prod::BM * g.cg) * parts_of(width, g.shape.bn);
     DO((products<Logits<true, PLANES>>(g, tiles, st)));
     h.v0 = v0;
     h.width = width;
     h.wrow = g.wrow;
-    DO(w_map(a, p, ws, h.wm, width, 64));
+    if (p.planes > 1) DO(w_map(a, p, ws, h.wm, width, 64));
     MAP(h.dzk, ws + p.dz, DT_BF16, p.planes, p.rows, p.width, p.width, 64, prod::BM);
     MAP(h.dzm, ws + p.dz, DT_BF16, p.planes, p.rows, p.width, p.width, 64, 64);
     const int64_t nt = parts_of(a.hidden, h.shape.bn);

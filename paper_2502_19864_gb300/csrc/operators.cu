@@ -153,8 +153,7 @@ ra_status check_norm(const ra_norm_args& a, bool backward) {
   TRY(check_loose(a.dy_dev, a.dy_stride, a.hidden, a.dtype));
   if (a.dsum_dev) TRY(check_loose(a.dsum_dev, a.dsum_stride, a.hidden, a.dtype));
   if (a.dx_dev) TRY(check_loose(a.dx_dev, a.dx_stride, a.hidden, a.dtype));
-  if (!aligned(a.dgamma_dev, wes) || !aligned(a.dbeta_dev, wes)) return RA_ERR_ARG;
-  return check_workspace(a.workspace_dev, a.workspace_bytes, norm_workspace(a));
+  return aligned(a.dgamma_dev, wes) && aligned(a.dbeta_dev, wes) ? RA_OK : RA_ERR_ARG;
 }
 ra_status check_vocab(const ra_vocab_loss_args& a, bool backward) {
   if (a.dtype != RA_F32 && a.dtype != RA_BF16) return RA_ERR_ARG;
@@ -183,10 +182,11 @@ ra_status check_orthogonalize(const ra_orthogonalize_args& a) {
   if (a.rows > 32768 || a.cols > 32768 || a.steps > 64 || a.n_matrices > 65535) return RA_ERR_SHAPE;
   TRY(check_loose(a.x_dev, a.x_stride, a.cols, a.dtype));
   TRY(check_loose(a.out_dev, a.out_stride, a.cols, a.dtype));
-  // matrices of their own (the last row of one ends before the next begins)
-  if (a.n_matrices > 1 && (a.x_matrix_stride < (a.rows - 1) * a.x_stride + a.cols ||
-                           a.out_matrix_stride < (a.rows - 1) * a.out_stride + a.cols))
-    return RA_ERR_SHAPE;
+  // matrices of their own: one behind the other, or side by side
+  auto apart = [&](int64_t stride, int64_t matrix) {
+    return matrix >= (a.rows - 1) * stride + a.cols || (matrix >= a.cols && stride >= (a.n_matrices - 1) * matrix + a.cols);
+  };
+  if (a.n_matrices > 1 && (!apart(a.x_stride, a.x_matrix_stride) || !apart(a.out_stride, a.out_matrix_stride))) return RA_ERR_SHAPE;
   return RA_OK;
 }
 
@@ -258,9 +258,7 @@ ra_status ra_verify_draft(const ra_verify_draft_args* args, ra_stream_t stream) 
 }
 
 size_t ra_norm_workspace_bytes(const ra_norm_args* args) {
-  if (!args) return 0;
-  ra_norm_args a = *args;  // a block for the forward alone has what this needs too
-  return check_norm(a, false) == RA_OK ? norm_workspace(a) : 0;
+  return args && (check_norm(*args, false) == RA_OK || check_norm(*args, true) == RA_OK) ? norm_workspace(*args) : 0;
 }
 ra_status ra_norm_forward(const ra_norm_args* args, ra_stream_t stream) {
   if (!args) return RA_ERR_ARG;
@@ -272,13 +270,14 @@ ra_status ra_norm_forward(const ra_norm_args* args, ra_stream_t stream) {
 ra_status ra_norm_backward(const ra_norm_args* args, ra_stream_t stream) {
   if (!args) return RA_ERR_ARG;
   TRY(check_norm(*args, true));
+  if (args->rows > 0) TRY(check_workspace(args->workspace_dev, args->workspace_bytes, norm_workspace(*args)));
   if (!args->dx_dev && !args->dgamma_dev && !args->dbeta_dev) return RA_OK;
   if (!tc_available()) return RA_ERR_UNSUPPORTED;
   return launched(norm_bwd(*args, (cudaStream_t)stream));
 }
 
 size_t ra_vocab_loss_workspace_bytes(const ra_vocab_loss_args* args) {
-  return args && check_vocab(*args, false) == RA_OK ? vocab_loss_workspace(*args) : 0;
+  return args && (check_vocab(*args, false) == RA_OK || check_vocab(*args, true) == RA_OK) ? vocab_loss_workspace(*args) : 0;
 }
 ra_status ra_vocab_loss_forward(const ra_vocab_loss_args* args, ra_stream_t stream) {
   if (!args) return RA_ERR_ARG;

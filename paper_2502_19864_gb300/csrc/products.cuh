@@ -6,7 +6,9 @@
 // at consecutive z, each holding the next 8 bits: of the planes' products those that matter are added up, the smallest
 // first.  The tensor cores truncate what they add to an accumulator: a sum of K products of one sign loses about 4.3e-10 K of
 // itself (measured: 9e-7 at K = 2048, 3.5e-5 at 32768).  So an accumulator takes `chunk` k-blocks, and the epilogue's threads
-// add up the chunks' accumulators in fp32 registers, rounded to nearest.
+// add up the chunks' accumulators in fp32 registers, rounded to nearest; and of three planes' products all but the largest
+// have an accumulator of their own, so that their five steps a k-block are not truncated at the largest's size (two of 777 x 777 x
+// 1000 orthogonalised: 1.5e-5 from 64 bits with one accumulator, 3e-6 with two).
 //
 // One persistent CTA an SM (or, CG = 2, a pair on two): warp 0 keeps a ring of operand stages filled by TMA, warp 1
 // issues the products into one of two accumulators in TMEM, warps 2..9 take the finished one into registers, 128 values a thread,
@@ -89,11 +91,13 @@ inline double time_of(Pick k, int64_t m, int64_t n, int64_t batch, int blocks) {
   const int64_t tiles = batch * parts_of(m, BM * k.cg) * parts_of(n, k.bn);
   return (double)parts_of(tiles, SMS / k.cg) * (blocks * block_time(k) + 1.) + (k.cg == 2 ? 1. : 0.);
 }
-// the fastest, of those whose ring has two stages
+// whether a tile's ring has two stages, and TMEM room for two accumulators, of three planes twice
+inline bool takes(Pick k, int pa, int pb) { return stages_of(k.bn, k.cg, pa, pb) >= 2 && (pa < 3 && pb < 3 ? k.bn <= MAX_BN : k.bn <= MAX_BN / 2); }
+// the fastest
 inline Pick pick(int64_t m, int64_t n, int64_t batch, int blocks, int pa, int pb) {
   Pick best = {1, n <= 64 ? 64 : 128};
-  for (Pick k : {Pick{1, 64}, Pick{1, 256}, Pick{2, 256}})
-    if ((k.cg == 1 || m > BM) && n > k.bn / 2 && stages_of(k.bn, k.cg, pa, pb) >= 2 &&
+  for (Pick k : {Pick{1, 64}, Pick{1, 256}, Pick{2, 128}, Pick{2, 256}})
+    if ((k.cg == 1 || m > BM) && n > k.bn / 2 && takes(k, pa, pb) &&
         time_of(k, m, n, batch, blocks) < time_of(best, m, n, batch, blocks))
       best = k;
   return best;
@@ -307,6 +311,7 @@ __global__ void __launch_bounds__(THREADS, 1) products_kernel(const __grid_const
   pdl_wait();
   pdl_trigger();
   const int units = P::count(p);
+  constexpr bool TWO = P::PA == 3 && P::PB == 3;  // accumulators: the largest term's, and 128 columns on the others'
   const int chunk = p.shape.chunk;
 
   if (warp == 0) {
@@ -389,12 +394,14 @@ __global__ void __launch_bounds__(THREADS, 1) products_kernel(const __grid_const
             constexpr Terms terms = terms_of(P::PA, P::PB);
 #pragma unroll
             for (int t = 0; t < terms.n; ++t) {
+              const uint32_t dt = TWO && t < terms.n - 1 ? d + MAX_BN / 2 : d;
               const uint64_t at = ad + off + (uint64_t)((terms.a >> (2 * t) & 3u) * (A_BYTES / 16)), bt = bd + off + (uint64_t)((terms.b >> (2 * t) & 3u) * bplane);
 #pragma unroll
               for (int k = 0; k < BK / 16; ++k) {
                 const uint64_t x = at + as * (uint64_t)k, y = bt + bs * (uint64_t)k;
-                if (CG == 2) umma_bf16_pair(d, x, y, idesc, i | t | k);
-                else umma_bf16(d, x, y, idesc, i | t | k);
+                const uint32_t more = TWO && t == terms.n - 1 ? i | k : i | t | k;
+                if (CG == 2) umma_bf16_pair(dt, x, y, idesc, more);
+                else umma_bf16(dt, x, y, idesc, more);
               }
             }
             if (CG == 2) umma_commit_pair(&empty_bar[stage]);
@@ -442,6 +449,15 @@ __global__ void __launch_bounds__(THREADS, 1) products_kernel(const __grid_const
         for (int i = 0; i < 4; ++i)
           if (i < t.chunks) {
             float x[32];
+            if (TWO) {
+              tmem_ld32(at + MAX_BN / 2 + 64 * i, x);
+#pragma unroll
+              for (int j = 0; j < 32; j += 2) {
+                const float2 s = __fadd2_rn(make_float2(v[i][j], v[i][j + 1]), make_float2(x[j], x[j + 1]));
+                v[i][j] = s.x;
+                v[i][j + 1] = s.y;
+              }
+            }
             tmem_ld32(at + 64 * i, x);
 #pragma unroll
             for (int j = 0; j < 32; j += 2) {

@@ -88,6 +88,25 @@ def test_against_64_bits(n, rows, cols, dtype):
     check(s, dtype)
 
 
+@pytest.mark.parametrize("n,rows,cols", [(2, 777, 1000), (8, 128, 16), (1, 300, 2000)])
+def test_fp32_is_no_further_off_than_fp32_products(n, rows, cols):
+    """Three times what plain fp32 products on the CUDA cores leave: each of theirs is off by the roundings of K sums, as the planes'
+    are, whose accumulators are truncated, which is twice a rounding, and whose smallest terms are left out."""
+    a, s = make(n, rows, cols, "f32", seed=3)
+    R.ra_orthogonalize(a)
+    x = s["x"]
+    x = x / (x.square().sum((1, 2), keepdim=True).sqrt() + 1e-7)
+    tall = rows > cols
+    x = x.transpose(1, 2) if tall else x
+    for _ in range(5):
+        S = x @ x.transpose(1, 2)
+        x = COEF[0] * x + (COEF[1] * S + COEF[2] * (S @ S)) @ x
+    x = x.transpose(1, 2) if tall else x
+    eps = float(torch.tensor(1e-7, dtype=torch.float32))
+    want = steps64(s["x"], 5, COEF, eps)
+    assert (s["out"].double() - want).norm() <= 3 * (x.double() - want).norm()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("steps", [0, 1, 2, 6])
 def test_steps(dtype, steps):
@@ -115,6 +134,31 @@ def test_strides(dtype, pad, gap):
     check(s, dtype)
     s["out"].fill_(7.0)
     assert bool((s["whole"] == 7.0).all())  # what lies between rows and matrices is left as it was
+
+
+@pytest.mark.parametrize("dtype,n,rows,cols", [("bf16", 1, 1537, 2050), ("bf16", 1, 2400, 2410), ("f32", 1, 1700, 1701)])
+def test_symmetric_products_by_halves(dtype, n, rows, cols):
+    """Sizes at which one triangle of the symmetric products' tiles is computed and the other mirrored."""
+    a, s = make(n, rows, cols, dtype)
+    s["workspace"][16384:] = 255
+    R.ra_orthogonalize(a)
+    torch.cuda.synchronize()
+    check(s, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(90, 72), (72, 90), (300, 40)])
+def test_matrices_side_by_side(dtype, rows, cols):
+    a, s = make(1, rows, 3 * cols, dtype)
+    for name in ("x", "out"):
+        s[name] = s[name].view(rows, 3, cols).transpose(0, 1)
+    a.n_matrices, a.cols, a.x_matrix_stride, a.out_matrix_stride = 3, cols, cols, cols
+    n = R.ra_orthogonalize_workspace_bytes(a)
+    s["workspace"] = workspace(n)
+    a.workspace_dev, a.workspace_bytes = s["workspace"].data_ptr(), n
+    R.ra_orthogonalize(a)
+    torch.cuda.synchronize()
+    check(s, dtype)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])

@@ -96,3 +96,17 @@ def test_workspaces():
         assert size(block()) >= 16384
         assert size(block(dtype=9)) == 0
         assert size(block(workspace_dev=None, workspace_bytes=0)) == size(block())
+    # blocks of the backward alone, or the forward alone
+    assert R.ra_norm_workspace_bytes(norm(x_dev=None, y_dev=None)) == R.ra_norm_workspace_bytes(norm())
+    assert R.ra_norm_workspace_bytes(norm(dy_dev=None, rstd_dev=None)) == R.ra_norm_workspace_bytes(norm())
+    assert R.ra_vocab_loss_workspace_bytes(loss(loss_dev=None)) == R.ra_vocab_loss_workspace_bytes(loss())
+    assert 0 < R.ra_vocab_loss_workspace_bytes(loss(dloss_dev=None, lse_dev=None, dx_dev=None, dw_dev=None)) <= R.ra_vocab_loss_workspace_bytes(loss())
+    for change in (dict(dx_dev=None), dict(dw_dev=None)):  # (either gradient alone takes no more)
+        assert R.ra_vocab_loss_workspace_bytes(loss(**change)) == R.ra_vocab_loss_workspace_bytes(loss())
+
+
+def test_matrices_side_by_side():
+    side = dict(x_stride=128, x_matrix_stride=64, out_stride=130, out_matrix_stride=65)
+    assert R.ra_orthogonalize_workspace_bytes(orth(**side)) >= 16384
+    for wrong in (dict(x_stride=127), dict(x_matrix_stride=63), dict(out_stride=128), dict(out_matrix_stride=67)):
+        assert R.ra_orthogonalize_workspace_bytes(orth(**{**side, **wrong})) == 0
