@@ -203,6 +203,8 @@ struct OrthArgs {
 template <int PLANES, int A_PLANES, int B_PLANES>
 struct Step {
   static constexpr int PA = A_PLANES, PB = B_PLANES;
+  // (bf16: what an accumulator of 32768 products loses, 3.5e-5 of them, is of the size of what two planes leave out)
+  static constexpr bool PARTS = true, ONE = PLANES == 2;
   using Args = OrthArgs;
   // of a symmetric product (square tiles) those on and above the diagonal, column by column of tiles
   static __host__ __device__ __forceinline__ int tiles(const Args& p, int& mt, int& nt) {
@@ -247,44 +249,38 @@ struct Step {
   static __device__ __forceinline__ void put(const Args& p, const Unit& w, bf16* to, F f, int row, int col, int lane) {
     const int64_t plane = (int64_t)p.rows * p.pitch;
     bf16* base = to + (int64_t)w.z * PLANES * plane;
-    prod::planes_out<PLANES>(base + (int64_t)row * p.pitch + col, plane, f, row < p.rows, p.width - col);
+    const int row0 = row - lane;
+    prod::planes_out<PLANES>(base + (int64_t)row0 * p.pitch + col, plane, p.pitch, f, p.rows - row0, p.width - col, lane);
     if (w.job) prod::planes_mirrored<PLANES>(base + (int64_t)col * p.pitch + (row & ~1), plane, f, p.pitch, p.rows - col, row < p.width, lane);
   }
-  static __device__ __forceinline__ void finish(const Args& p, const Unit& w, const Tile& t, Store& st, float (&v)[4][32]) {
-    const int row0 = w.m0 + t.rank * prod::BM + t.quad * 32, row = row0 + t.lane;
-    if (row0 >= p.rows) return;
-    float f = 1.f;
+  static __device__ __forceinline__ void part(const Args& p, const Unit& w, const Tile& t, Store& st, int i, float (&v)[32]) {
+    const int row0 = w.m0 + t.rank * prod::BM + t.quad * 32, row = row0 + t.lane, col = w.n0 + 32 * (t.half + 2 * i);
+    if (row0 >= p.rows || col >= p.cols) return;
     if (p.power) {
-      f = p.factors[w.z];
+      float f = p.factors[w.z];
       if (p.power == 2) f *= f;
+#pragma unroll
+      for (int j = 0; j < 32; ++j) v[j] *= f;
     }
+    if (p.last) {
+      if (p.map_out) {
+        if (p.dtype == RA_BF16) st.bf16_row(&p.out, [&](int j) { return v[j]; }, col, row0, w.z);
+        else st.f32_row(&p.out, v, col, row0, w.z, false, p.cols);
+      } else if (row < p.rows) {
+        const int64_t at = w.z * p.dst_matrix_stride + row * p.dst_stride + col;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int col = w.n0 + 32 * (t.half + 2 * i);
-      if (i >= t.chunks || col >= p.cols) break;
-      if (p.power)
-#pragma unroll
-        for (int j = 0; j < 32; ++j) v[i][j] *= f;
-      if (p.last) {
-        if (p.map_out) {
-          if (p.dtype == RA_BF16) st.bf16_row(&p.out, [&](int j) { return v[i][j]; }, col, row0, w.z);
-          else st.f32_row(&p.out, v[i], col, row0, w.z, false, p.cols);
-        } else if (row < p.rows) {
-          const int64_t at = w.z * p.dst_matrix_stride + row * p.dst_stride + col;
-#pragma unroll
-          for (int j = 0; j < 32; ++j)
-            if (col + j < p.cols) {
-              if (p.dtype == RA_BF16) static_cast<bf16*>(p.dst)[at + j] = __float2bfloat16_rn(v[i][j]);
-              else static_cast<float*>(p.dst)[at + j] = v[i][j];
-            }
-        }
-        continue;
+        for (int j = 0; j < 32; ++j)
+          if (col + j < p.cols) {
+            if (p.dtype == RA_BF16) static_cast<bf16*>(p.dst)[at + j] = __float2bfloat16_rn(v[j]);
+            else static_cast<float*>(p.dst)[at + j] = v[j];
+          }
       }
-      // (the identity's part: nothing behind the last row)
-      const int diag = row < p.rows ? row - col : -1;
-      put(p, w, p.o, [&](int j) { return v[i][j] + (j == diag ? p.add : 0.f); }, row, col, t.lane);
-      if (p.o2) put(p, w, p.o2, [&](int j) { return p.mul2 * v[i][j] + (j == diag ? p.add2 : 0.f); }, row, col, t.lane);
+      return;
     }
+    // (the identity's part: nothing behind the last row)
+    const int diag = row < p.rows ? row - col : -1;
+    put(p, w, p.o, [&](int j) { return v[j] + (j == diag ? p.add : 0.f); }, row, col, t.lane);
+    if (p.o2) put(p, w, p.o2, [&](int j) { return p.mul2 * v[j] + (j == diag ? p.add2 : 0.f); }, row, col, t.lane);
   }
 };
 
@@ -784,7 +780,7 @@ cudaError_t run(const ra_orthogonalize_args& a, cudaStream_t st) {
   }
   if (a.steps == 0) return cudaSuccess;
 
-  const int chunk = p.planes == 3 ? 4 : 32;
+  const int chunk = p.planes == 3 ? 4 : 512;
   OrthArgs g = {};
   g.err = a.err_dev;
   g.factors = factors;

@@ -225,6 +225,7 @@ __device__ __forceinline__ const CUtensorMap* hidden_map(const VocabArgs& p, int
 template <bool BACK, int PLANES>
 struct Logits {
   static constexpr int PA = PLANES, PB = PLANES;
+  static constexpr bool PARTS = BACK, ONE = false;
   using Args = VocabArgs;
   static __device__ __forceinline__ int count(const Args& p) {
     return ceil_div(tokens(p), prod::BM * p.cg) * ceil_div(p.width, p.shape.bn);
@@ -250,50 +251,53 @@ struct Logits {
     w.job = 0;
     w.z = nt;
   }
-  static __device__ __forceinline__ void finish(const Args& p, const Unit& w, const Tile& t, Store& st, float (&v)[4][32]) {
-    const int row0 = w.m0 + t.rank * prod::BM + t.quad * 32, row = row0 + t.lane;
-    const int label = (p.count || row < p.tokens ? p.label[row] : -1) - p.v0 - w.n0;  // its column in this tile
-    if (BACK) {
-      const float scale = p.scale[row], lse = p.lse[row];
+  // this lane's row of the tile, and where its label is among the tile's columns
+  static __device__ __forceinline__ int row_of(const Unit& w, const Tile& t) { return w.m0 + t.rank * prod::BM + t.quad * 32 + t.lane; }
+  static __device__ __forceinline__ int label_of(const Args& p, const Unit& w, int row) {
+    return (p.count || row < p.tokens ? p.label[row] : -1) - p.v0 - w.n0;
+  }
+  // dz = scale (exp(z - lse) - onehot)
+  static __device__ __forceinline__ void part(const Args& p, const Unit& w, const Tile& t, Store& st, int i, float (&v)[32]) {
+    const int row = row_of(w, t), row0 = row - t.lane, label = label_of(p, w, row);
+    const float scale = p.scale[row], lse = p.lse[row];
+    const int c = 32 * (t.half + 2 * i), left = p.width - w.n0 - c;  // (zeros up to a whole k-block of the sums that follow)
+    if (w.n0 + c >= (p.width + 63) / 64 * 64) return;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int c = 32 * (t.half + 2 * i), left = p.width - w.n0 - c;  // (zeros up to a whole k-block of the sums that follow)
-        if (i >= t.chunks || w.n0 + c >= (p.width + 63) / 64 * 64) break;
-#pragma unroll
-        for (int j = 0; j < 32; ++j) {
-          const float e = ex2_fast(__fmul_rn(__fsub_rn(v[i][j], lse), LOG2E));
-          v[i][j] = j < left ? __fmul_rn(scale, c + j == label ? __fsub_rn(e, 1.f) : e) : 0.f;
-        }
-        auto at = [&](int j) { return v[i][j]; };
-        if (PLANES == 1) st.bf16_row(&p.dz, at, w.n0 + c, row0, 0);
-        else prod::planes_out<3>(p.dzp + (int64_t)row * p.dz_pitch + w.n0 + c, (int64_t)p.rows * p.dz_pitch, at, true, 32);
-      }
-    } else {
-      float m = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int c = 32 * (t.half + 2 * i);
-        if (i >= t.chunks) break;
-        if (w.n0 + c + 32 > p.width)
-#pragma unroll
-          for (int j = 0; j < 32; ++j)
-            if (w.n0 + c + j >= p.width) v[i][j] = -INFINITY;
-        if ((uint32_t)(label - c) < 32u)
-#pragma unroll
-          for (int j = 0; j < 32; ++j)
-            if (c + j == label) p.zlab[row] = v[i][j];
-#pragma unroll
-        for (int j = 0; j < 32; ++j) m = fmaxf(m, v[i][j]);
-      }
-      float l = 0.f;
-      const float from = m > -INFINITY ? m : 0.f;  // (nothing but NaN, or no words at all)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (i < t.chunks)
-#pragma unroll
-          for (int j = 0; j < 32; ++j) l += ex2_fast(__fmul_rn(__fsub_rn(v[i][j], from), LOG2E));
-      p.stats[(int64_t)(p.stat0 + 2 * w.z + t.half) * p.rows + row] = make_float2(m, l);
+    for (int j = 0; j < 32; ++j) {
+      const float e = ex2_fast(__fmul_rn(__fsub_rn(v[j], lse), LOG2E));
+      v[j] = j < left ? __fmul_rn(scale, c + j == label ? __fsub_rn(e, 1.f) : e) : 0.f;
     }
+    auto at = [&](int j) { return v[j]; };
+    if (PLANES == 1) st.bf16_row(&p.dz, at, w.n0 + c, row0, 0);
+    else prod::planes_out<3>(p.dzp + (int64_t)row0 * p.dz_pitch + w.n0 + c, (int64_t)p.rows * p.dz_pitch, p.dz_pitch, at, 32, 32, t.lane);
+  }
+  template <int CH>
+  static __device__ __forceinline__ void finish(const Args& p, const Unit& w, const Tile& t, Store& st, float (&v)[CH][32]) {
+    const int row = row_of(w, t), label = label_of(p, w, row);
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const int c = 32 * (t.half + 2 * i);
+      if (i >= t.chunks) break;
+      if (w.n0 + c + 32 > p.width)
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+          if (w.n0 + c + j >= p.width) v[i][j] = -INFINITY;
+      if ((uint32_t)(label - c) < 32u)
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+          if (c + j == label) p.zlab[row] = v[i][j];
+#pragma unroll
+      for (int j = 0; j < 32; ++j) m = fmaxf(m, v[i][j]);
+    }
+    float l = 0.f;
+    const float from = m > -INFINITY ? m : 0.f;  // (nothing but NaN, or no words at all)
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+      if (i < t.chunks)
+#pragma unroll
+        for (int j = 0; j < 32; ++j) l += ex2_fast(__fmul_rn(__fsub_rn(v[i][j], from), LOG2E));
+    p.stats[(int64_t)(p.stat0 + 2 * w.z + t.half) * p.rows + row] = make_float2(m, l);
   }
 };
 
@@ -301,6 +305,7 @@ struct Logits {
 template <int PLANES>
 struct Grads {
   static constexpr int PA = PLANES, PB = PLANES;
+  static constexpr bool PARTS = true, ONE = false;
   using Args = VocabArgs;
   struct Count {
     int n, mx, mw, nt, kx, kw, ux, uw;
@@ -358,21 +363,16 @@ struct Grads {
       w.kb1 = min(w.kb0 + c.kw, ceil_div(c.n, prod::BK));
     }
   }
-  static __device__ __forceinline__ void finish(const Args& p, const Unit& w, const Tile& t, Store& st, float (&v)[4][32]) {
-    const int row0 = w.m0 + t.rank * prod::BM + t.quad * 32;
-    if (w.job == 1 && row0 >= p.width) return;
+  static __device__ __forceinline__ void part(const Args& p, const Unit& w, const Tile& t, Store& st, int i, float (&v)[32]) {
+    const int row0 = w.m0 + t.rank * prod::BM + t.quad * 32, c = w.n0 + 32 * (t.half + 2 * i);
+    if ((w.job == 1 && row0 >= p.width) || c >= p.hidden) return;
     const float ref = *p.ref;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int c = w.n0 + 32 * (t.half + 2 * i);
-      if (i >= t.chunks || c >= p.hidden) break;
-#pragma unroll
-      for (int j = 0; j < 32; ++j) v[i][j] *= ref;
-      if (w.job == 0) st.f32_row(&p.dxs, v[i], c, row0, w.z, p.v0 > 0, p.hidden);
-      else if (p.splits_w > 1) st.f32_row(&p.dw, v[i], c, row0, w.z, false, p.hidden);
-      else if (p.dtype == RA_BF16) st.bf16_row(&p.dw, [&](int j) { return v[i][j]; }, c, p.v0 + row0, 0);
-      else st.f32_row(&p.dw, v[i], c, p.v0 + row0, 0, false, p.hidden);
-    }
+    for (int j = 0; j < 32; ++j) v[j] *= ref;
+    if (w.job == 0) st.f32_row(&p.dxs, v, c, row0, w.z, p.v0 > 0, p.hidden);
+    else if (p.splits_w > 1) st.f32_row(&p.dw, v, c, row0, w.z, false, p.hidden);
+    else if (p.dtype == RA_BF16) st.bf16_row(&p.dw, [&](int j) { return v[j]; }, c, p.v0 + row0, 0);
+    else st.f32_row(&p.dw, v, c, p.v0 + row0, 0, false, p.hidden);
   }
 };
 

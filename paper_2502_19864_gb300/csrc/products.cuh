@@ -21,6 +21,7 @@
 #include "common.cuh"
 #include "kernels.h"
 #include "tcgen05.cuh"
+#include "window_tc.cuh"
 
 namespace ra {
 namespace prod {
@@ -161,18 +162,30 @@ __device__ __forceinline__ void planes_of(float x, float y, uint32_t (&w)[PLANES
     w[1] = *reinterpret_cast<const uint32_t*>(&l);
   }
 }
-// 32 columns f(0), f(1), .. of a row to its planes, `plane` values apart, from registers, 16 bytes at a time; `left`: how many of
-// the columns (a multiple of 8) are there
-template <int PLANES, typename F>
-__device__ __forceinline__ void planes_out(bf16* to, int64_t plane, F f, bool row_ok, int left) {
+// Plane K of two values, a word
+template <int PLANES, int K>
+__device__ __forceinline__ uint32_t plane_of(float x, float y) {
+  uint32_t w[PLANES];
+  planes_of<PLANES>(x, y, w);
+  return w[K];
+}
+// Plane K, and those after it, of a warp's 32 rows of 32 columns, a lane having f(0), f(1), .. of its row: `to` is the first
+// row's place in plane 0, rows are `pitch` and planes `plane` values apart; `rows` and `cols` (a multiple of 8) of them are there.
+// Four lanes exchange 16-byte pieces, so that a store fills 64 bytes of each of eight rows (a row a lane touches 32 lines an
+// instruction: 13 us of a launch of 98 tiles of 128 x 128 in two times three planes)
+template <int PLANES, int K = 0, typename F>
+__device__ __forceinline__ void planes_out(bf16* to, int64_t plane, int64_t pitch, F f, int rows, int cols, int lane) {
+  if constexpr (K < PLANES) {
+    uint32_t w[16];
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    uint32_t w[4][PLANES];
+    for (int i = 0; i < 16; ++i) w[i] = plane_of<PLANES, K>(f(2 * i), f(2 * i + 1));
+    transpose4(w, lane);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) planes_of<PLANES>(f(8 * q + 2 * i), f(8 * q + 2 * i + 1), w[i]);
-#pragma unroll
-    for (int k = 0; k < PLANES; ++k)
-      if (row_ok && 8 * q < left) *reinterpret_cast<uint4*>(to + k * plane + 8 * q) = make_uint4(w[0][k], w[1][k], w[2][k], w[3][k]);
+    for (int i = 0; i < 4; ++i) {
+      const int r = (lane & ~3) + i, c = 8 * (lane & 3);
+      if (r < rows && c < cols) *reinterpret_cast<uint4*>(to + K * plane + r * pitch + c) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    }
+    planes_out<PLANES, K + 1>(to, plane, pitch, f, rows, cols, lane);
   }
 }
 // The same, transposed: to the 32 rows `pitch` apart that are the columns, of which rows_left are there; `to` is the first of them at
@@ -261,7 +274,8 @@ __device__ __forceinline__ void prefetch_map(const CUtensorMap* tm) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(tm)) : "memory");
 }
 // P: the operands' planes PA and PB, Args (with `Shape shape`, `unsigned* err`), static void prefetch(const Args&) (of the operands' maps), static int count(const Args&), static void unit(const Args&, int, Unit&) and
-// static void finish(const Args&, const Unit&, const Tile&, Store&, float (&v)[4][32]).
+// PARTS (ONE: a unit has k-blocks, and one accumulator takes them all) and static void part(const Args&, const Unit&, const Tile&, Store&, int i, float (&v)[32]) for this warp's i-th 32 columns, or
+// static void finish(const Args&, const Unit&, const Tile&, Store&, float (&v)[CH][32]) for all of them.
 template <class P, int CG>
 __global__ void __launch_bounds__(THREADS, 1) products_kernel(const __grid_constant__ typename P::Args p) {
   extern __shared__ uint8_t smem_raw[];
@@ -436,36 +450,23 @@ __global__ void __launch_bounds__(THREADS, 1) products_kernel(const __grid_const
     for (int u = worker; ok && u < units; u += workers) {
       Unit w;
       P::unit(p, u, w);
-      float v[4][32];
+      constexpr int CH = TWO ? 2 : 4;
+      const uint32_t mine = tmem_base + ((uint32_t)(t.quad * 32) << 16) + (uint32_t)(32 * t.half);
+      // this warp's i-th 32 columns of the accumulator
+      auto read = [&](int i, float* x) {
+        tmem_ld32(mine + (uint32_t)(acc * MAX_BN + 64 * i), x);
+        if (TWO) {
+          float y[32];
+          tmem_ld32(mine + (uint32_t)(acc * MAX_BN + MAX_BN / 2 + 64 * i), y);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 32; ++j) v[i][j] = 0.f;
-      for (int c0 = w.kb0; c0 < w.kb1; c0 += chunk) {
-        if (!mbar_wait_warp(&tfull_bar[acc], acc_phase, &abort_sh, p.err)) { ok = false; break; }
-        tc_fence_after();
-        const uint32_t at = tmem_base + ((uint32_t)(t.quad * 32) << 16) + (uint32_t)(acc * MAX_BN + 32 * t.half);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (i < t.chunks) {
-            float x[32];
-            if (TWO) {
-              tmem_ld32(at + MAX_BN / 2 + 64 * i, x);
-#pragma unroll
-              for (int j = 0; j < 32; j += 2) {
-                const float2 s = __fadd2_rn(make_float2(v[i][j], v[i][j + 1]), make_float2(x[j], x[j + 1]));
-                v[i][j] = s.x;
-                v[i][j + 1] = s.y;
-              }
-            }
-            tmem_ld32(at + 64 * i, x);
-#pragma unroll
-            for (int j = 0; j < 32; j += 2) {
-              const float2 s = __fadd2_rn(make_float2(v[i][j], v[i][j + 1]), make_float2(x[j], x[j + 1]));
-              v[i][j] = s.x;
-              v[i][j + 1] = s.y;
-            }
+          for (int j = 0; j < 32; j += 2) {
+            const float2 s = __fadd2_rn(make_float2(x[j], x[j + 1]), make_float2(y[j], y[j + 1]));
+            x[j] = s.x;
+            x[j + 1] = s.y;
           }
+        }
+      };
+      auto release = [&]() {
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
@@ -473,8 +474,56 @@ __global__ void __launch_bounds__(THREADS, 1) products_kernel(const __grid_const
           else mbar_arrive(&tempty_bar[acc]);
         }
         if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+      };
+      if constexpr (P::PARTS) {
+        // one accumulator has it all: straight from there, 32 columns at a time
+        if (P::ONE || (w.kb0 < w.kb1 && w.kb0 + chunk >= w.kb1)) {
+          if (!mbar_wait_warp(&tfull_bar[acc], acc_phase, &abort_sh, p.err)) break;
+          tc_fence_after();
+#pragma unroll
+          for (int i = 0; i < CH; ++i)
+            if (i < t.chunks) {
+              float x[32];
+              __syncwarp();
+              read(i, x);
+              P::part(p, w, t, st, i, x);
+            }
+          release();
+          continue;
+        }
       }
-      if (ok) P::finish(p, w, t, st, v);
+      if constexpr (!P::ONE) {
+      float v[CH][32];
+#pragma unroll
+      for (int i = 0; i < CH; ++i)
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[i][j] = 0.f;
+      for (int c0 = w.kb0; c0 < w.kb1; c0 += chunk) {
+        if (!mbar_wait_warp(&tfull_bar[acc], acc_phase, &abort_sh, p.err)) { ok = false; break; }
+        tc_fence_after();
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+          if (i < t.chunks) {
+            float x[32];
+            read(i, x);
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) {
+              const float2 s = __fadd2_rn(make_float2(v[i][j], v[i][j + 1]), make_float2(x[j], x[j + 1]));
+              v[i][j] = s.x;
+              v[i][j + 1] = s.y;
+            }
+          }
+        release();
+      }
+      if (!ok) break;
+      if constexpr (P::PARTS) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+          if (i < t.chunks) P::part(p, w, t, st, i, v[i]);
+      } else {
+        P::finish(p, w, t, st, v);
+      }
+      }
     }
     if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");  // this warp's stores are complete
   }
