@@ -458,6 +458,245 @@ __global__ void __launch_bounds__(128) vocab_sum_kernel(const float* sums, int s
   }
 }
 
+// ---- few fp32 tokens ----------------------------------------------------------------------
+// Up to 32 tokens in fp32 are bound by W's bytes, which its planes would be four times over (a word of 100000 x 1024 is read in
+// 61 us in all; 16 tokens through planes 330 us, trained 915; here 128 and 438).  So on the CUDA cores, with the hidden states in
+// shared memory, a warp four words at a time.  W is read once by the forward, and by the backward once for dz and dw and once
+// for dx.  From 16 tokens on the multiply-adds bound, four to a value of shared memory (32 tokens 203 and 708 us).
+constexpr int FEW = 32, FEW_WORDS = 4, FEW_THREADS = 256, FEW_SMEM = 128 * 1024;
+
+// The sums over the warp of N (a multiple of 32) values; lane l is left with the N / 32 from l N / 32 on, in v[0], v[1], ..
+template <int N>
+__device__ __forceinline__ void scatter_sum(float (&v)[N], int lane) {
+  int o = 16;
+#pragma unroll
+  for (int k = N / 2; k >= N / 32; k >>= 1, o >>= 1) {
+    const bool high = lane & o;
+#pragma unroll
+    for (int i = 0; i < k; ++i) {
+      const float give = high ? v[i] : v[i + k], keep = high ? v[i + k] : v[i];
+      v[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+    }
+  }
+}
+
+// Logits of words in fours; forward: each warp's maxima and sums to stats [warps][TT]; BACK: dz [vocab][TT] and dw
+template <int TT, bool BACK>
+__global__ void __launch_bounds__(FEW_THREADS, TT <= 16 ? 2 : 1)
+    vocab_few_kernel(const __grid_constant__ ra_vocab_loss_args a, float2* stats, float* zlab, float* dz) {
+  extern __shared__ __align__(16) float xs[];  // [TT][H]
+  __shared__ float4 dzs[FEW_THREADS / 32][TT];
+  constexpr int EACH = FEW_WORDS * TT / 32;  // logits of a lane: of tokens t0.., of word k of the four
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, H = a.hidden;
+  const float* x = static_cast<const float*>(a.x_dev);
+  const float* w = static_cast<const float*>(a.w_dev);
+  pdl_wait();
+  pdl_trigger();
+  for (int i = tid; i < TT * (H / 4); i += FEW_THREADS) {
+    const int t = i / (H / 4), c = i % (H / 4) * 4;
+    const bool in = t < a.tokens && counted(a, a.labels_dev[t]);
+    *reinterpret_cast<float4*>(xs + t * H + c) = in ? *reinterpret_cast<const float4*>(x + t * a.x_stride + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  __syncthreads();
+  const int k = lane * EACH / TT, t0 = lane * EACH % TT;
+  int label[EACH];
+  float scale[EACH], lse[EACH], m[EACH], l[EACH];
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) {
+    const int t = t0 + e;
+    label[e] = t < a.tokens ? a.labels_dev[t] : -1;
+    if (!counted(a, label[e])) label[e] = -1;
+    scale[e] = BACK && label[e] >= 0 ? a.dloss_dev[t] : 0.f;
+    lse[e] = BACK && label[e] >= 0 ? a.lse_dev[t] : 0.f;
+    m[e] = -INFINITY;
+    l[e] = 0.f;
+  }
+  const int step = (int)gridDim.x * (FEW_THREADS / 32) * FEW_WORDS;
+  for (int v0 = ((int)blockIdx.x * (FEW_THREADS / 32) + warp) * FEW_WORDS; v0 < a.vocab; v0 += step) {
+    float z[FEW_WORDS * TT];
+#pragma unroll
+    for (int i = 0; i < FEW_WORDS * TT; ++i) z[i] = 0.f;
+    auto fetch = [&](int c, float4* y) {
+#pragma unroll
+      for (int i = 0; i < FEW_WORDS; ++i)
+        y[i] = c < H && v0 + i < a.vocab ? *reinterpret_cast<const float4*>(w + (v0 + i) * a.w_stride + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+    };
+    float4 y[FEW_WORDS], next[FEW_WORDS];
+    fetch(lane * 4, y);
+    for (int c = lane * 4; c - lane * 4 < H; c += 128) {
+      fetch(c + 128, next);
+      if (c < H)
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+          const float4 h = *reinterpret_cast<const float4*>(xs + t * H + c);
+#pragma unroll
+          for (int i = 0; i < FEW_WORDS; ++i)
+            z[i * TT + t] = fmaf(y[i].x, h.x, fmaf(y[i].y, h.y, fmaf(y[i].z, h.z, fmaf(y[i].w, h.w, z[i * TT + t]))));
+        }
+#pragma unroll
+      for (int i = 0; i < FEW_WORDS; ++i) y[i] = next[i];
+    }
+    scatter_sum(z, lane);
+    const int v = v0 + k;
+    if (!BACK) {
+#pragma unroll
+      for (int e = 0; e < EACH; ++e)
+        if (v < a.vocab) {
+          if (v == label[e]) zlab[t0 + e] = z[e];
+          const float top = fmaxf(m[e], z[e]), from = top > -INFINITY ? top : 0.f;
+          l[e] = l[e] * ex2_fast(__fmul_rn(__fsub_rn(m[e], from), LOG2E)) + ex2_fast(__fmul_rn(__fsub_rn(z[e], from), LOG2E));
+          m[e] = top;
+        }
+    } else {
+      float* mine = reinterpret_cast<float*>(dzs[warp]);  // [TT][4]
+      __syncwarp();
+#pragma unroll
+      for (int e = 0; e < EACH; ++e) {
+        const float p = ex2_fast(__fmul_rn(__fsub_rn(z[e], lse[e]), LOG2E));
+        const float d = label[e] < 0 ? 0.f : __fmul_rn(scale[e], v == label[e] ? __fsub_rn(p, 1.f) : p);
+        mine[(t0 + e) * 4 + k] = d;
+        if (a.dx_dev && v < a.vocab) dz[(int64_t)v * TT + t0 + e] = d;
+      }
+      __syncwarp();
+      if (a.dw_dev)
+        for (int c = lane * 4; c < H; c += 128) {
+          float4 s[FEW_WORDS] = {};
+#pragma unroll
+          for (int t = 0; t < TT; ++t) {
+            const float4 h = *reinterpret_cast<const float4*>(xs + t * H + c), d = dzs[warp][t];
+            const float ds[4] = {d.x, d.y, d.z, d.w};
+#pragma unroll
+            for (int i = 0; i < FEW_WORDS; ++i) {
+              s[i].x = fmaf(ds[i], h.x, s[i].x);
+              s[i].y = fmaf(ds[i], h.y, s[i].y);
+              s[i].z = fmaf(ds[i], h.z, s[i].z);
+              s[i].w = fmaf(ds[i], h.w, s[i].w);
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < FEW_WORDS; ++i)
+            if (v0 + i < a.vocab) *reinterpret_cast<float4*>(static_cast<float*>(a.dw_dev) + (v0 + i) * a.dw_stride + c) = s[i];
+        }
+    }
+  }
+  if (!BACK) {
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+      // lanes of the same token are those of the other words: 32 / FEW_WORDS lanes apart
+#pragma unroll
+      for (int o = 16; o >= 32 / FEW_WORDS; o >>= 1) {
+        const float m2 = __shfl_xor_sync(0xffffffffu, m[e], o), l2 = __shfl_xor_sync(0xffffffffu, l[e], o);
+        const float top = fmaxf(m[e], m2), from = top > -INFINITY ? top : 0.f;
+        l[e] = l[e] * ex2_fast(__fmul_rn(__fsub_rn(m[e], from), LOG2E)) + l2 * ex2_fast(__fmul_rn(__fsub_rn(m2, from), LOG2E));
+        m[e] = top;
+      }
+      if (k == 0) stats[((int64_t)blockIdx.x * (FEW_THREADS / 32) + warp) * TT + t0 + e] = make_float2(m[e], l[e]);
+    }
+  }
+}
+
+// dx of a part of the vocabulary: sums [parts][TT][pitch] of dz W; a warp 128 columns of every eighth group of words, the next
+// group's rows and dz on their way
+template <int TT>
+__global__ void __launch_bounds__(256, TT <= 16 ? 2 : 1)
+    vocab_few_dx_kernel(const __grid_constant__ ra_vocab_loss_args a, const float* dz, float* sums, int per, int pitch) {
+  constexpr int AT_ONCE = TT <= 16 ? 8 : 4, PIECES = AT_ONCE * TT / 4, EACH = (PIECES + 31) / 32;  // words of a group; its dz, in fours
+  __shared__ float4 sh[4][TT][32];
+  __shared__ float4 dzs[8][PIECES];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 128 + lane * 4;
+  pdl_wait();
+  pdl_trigger();
+  const int v1 = min(a.vocab, ((int)blockIdx.y + 1) * per);
+  const float* w = static_cast<const float*>(a.w_dev);
+  float4 s[TT];
+#pragma unroll
+  for (int t = 0; t < TT; ++t) s[t] = make_float4(0.f, 0.f, 0.f, 0.f);
+  const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto fetch = [&](int v0, float4 (&y)[AT_ONCE], float4 (&d)[EACH]) {
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) y[i] = c < a.hidden && v0 + i < v1 ? *reinterpret_cast<const float4*>(w + (v0 + i) * a.w_stride + c) : none;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+      const int i = e * 32 + lane;
+      d[e] = i < PIECES && v0 + i / (TT / 4) < v1 ? reinterpret_cast<const float4*>(dz + (int64_t)v0 * TT)[i] : none;
+    }
+  };
+  float4 y[AT_ONCE], ny[AT_ONCE], d[EACH];
+  int v0 = (int)blockIdx.y * per + warp * AT_ONCE;
+  fetch(v0, y, d);
+  for (; v0 < v1; v0 += 8 * AT_ONCE) {
+    __syncwarp();
+#pragma unroll
+    for (int e = 0; e < EACH; ++e)
+      if (e * 32 + lane < PIECES) dzs[warp][e * 32 + lane] = d[e];
+    __syncwarp();
+    fetch(v0 + 8 * AT_ONCE, ny, d);
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+#pragma unroll
+      for (int q = 0; q < TT / 4; ++q) {
+        const float4 g = dzs[warp][i * (TT / 4) + q];
+        const float gs[4] = {g.x, g.y, g.z, g.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float4& r = s[4 * q + j];
+          r.x = fmaf(gs[j], y[i].x, r.x);
+          r.y = fmaf(gs[j], y[i].y, r.y);
+          r.z = fmaf(gs[j], y[i].z, r.z);
+          r.w = fmaf(gs[j], y[i].w, r.w);
+        }
+      }
+      y[i] = ny[i];
+    }
+  }
+  // the eight warps' sums, halved three times
+  for (int half = 4; half >= 1; half >>= 1) {
+    if (warp >= half && warp < 2 * half)
+#pragma unroll
+      for (int t = 0; t < TT; ++t) sh[warp - half][t][lane] = s[t];
+    __syncthreads();
+    if (warp < half)
+#pragma unroll
+      for (int t = 0; t < TT; ++t) {
+        const float4 o = sh[warp][t][lane];
+        s[t].x += o.x;
+        s[t].y += o.y;
+        s[t].z += o.z;
+        s[t].w += o.w;
+      }
+    __syncthreads();
+  }
+  if (warp == 0 && c < a.hidden)
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+      if (t < a.tokens) *reinterpret_cast<float4*>(sums + ((int64_t)blockIdx.y * TT + t) * pitch + c) = s[t];
+}
+// the parts' sums, added up; nothing for tokens that are not counted
+__global__ void __launch_bounds__(128) vocab_few_sum_kernel(const __grid_constant__ ra_vocab_loss_args a, const float* sums, int parts, int64_t part, int pitch) {
+  const int t = blockIdx.y, c = (blockIdx.x * 128 + threadIdx.x) * 4;
+  pdl_wait();
+  pdl_trigger();
+  if (c >= a.hidden) return;
+  const int label = a.labels_dev[t];
+  if (label >= a.vocab && c == 0) set_dev_error(a.err_dev, RA_DEVERR_BOUNDS);
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (counted(a, label))
+    for (int i0 = 0; i0 < parts; i0 += 8) {
+      float4 v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        v[i] = i0 + i < parts ? *reinterpret_cast<const float4*>(sums + (i0 + i) * part + (int64_t)t * pitch + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        s.x += v[i].x;
+        s.y += v[i].y;
+        s.z += v[i].z;
+        s.w += v[i].w;
+      }
+    }
+  *reinterpret_cast<float4*>(static_cast<float*>(a.dx_dev) + t * a.dx_stride + c) = s;
+}
+
 // ---- the plan -----------------------------------------------------------------------------
 struct Plan {
   int planes, rows, chunk;
@@ -724,15 +963,83 @@ cudaError_t backward(const ra_vocab_loss_args& a, cudaStream_t st) {
   return cudaSuccess;
 }
 
+// ---- few fp32 tokens: the plan and the launches --------------------------------------------
+struct FewPlan {
+  int tt, ctas, parts, per;  // tokens, CTAs of the logits; parts of the vocabulary for dx, words of one
+  size_t stats, zlab, dz, sums, bytes;
+};
+bool few(const ra_vocab_loss_args& a) {
+  const int tt = a.tokens <= 8 ? 8 : a.tokens <= 16 ? 16 : FEW;
+  return a.dtype == RA_F32 && a.tokens >= 1 && a.tokens <= FEW && (int64_t)tt * a.hidden * 4 <= FEW_SMEM;
+}
+FewPlan few_plan(const ra_vocab_loss_args& a) {
+  FewPlan p;
+  p.tt = a.tokens <= 8 ? 8 : a.tokens <= 16 ? 16 : FEW;
+  const int smem = p.tt * a.hidden * 4, each = p.tt <= 16 && smem <= 96 * 1024 ? 2 : 1;
+  p.ctas = std::min(parts_of(a.vocab, FEW_WORDS * FEW_THREADS / 32), SMS * each);
+  const int blocks = parts_of(a.hidden, 128);
+  p.per = up(parts_of(a.vocab, std::max(1, std::min(2 * SMS / blocks, parts_of(a.vocab, 64)))), 8);
+  p.parts = parts_of(a.vocab, p.per);
+  size_t at = WS_ZERO;
+  auto take = [&](size_t n) {
+    const size_t r = at;
+    at += (n + 255) / 256 * 256;
+    return r;
+  };
+  p.zlab = take((size_t)p.tt * 4);
+  p.stats = take((size_t)p.ctas * (FEW_THREADS / 32) * p.tt * sizeof(float2));
+  const bool train = a.dx_dev || a.dw_dev;
+  p.dz = take(train ? (size_t)a.vocab * p.tt * 4 : 0);
+  p.sums = take(train ? (size_t)p.parts * p.tt * up(a.hidden, 4) * 4 : 0);
+  p.bytes = at;
+  return p;
+}
+template <int TT>
+cudaError_t few_run(const ra_vocab_loss_args& a, bool backward, cudaStream_t st) {
+  const FewPlan p = few_plan(a);
+  char* ws = static_cast<char*>(a.workspace_dev);
+  float2* stats = reinterpret_cast<float2*>(ws + p.stats);
+  float *zlab = reinterpret_cast<float*>(ws + p.zlab), *dz = reinterpret_cast<float*>(ws + p.dz), *sums = reinterpret_cast<float*>(ws + p.sums);
+  static const cudaError_t attr = [] {
+    const cudaError_t e = allow_smem(vocab_few_kernel<TT, false>, FEW_SMEM);
+    return e == cudaSuccess ? allow_smem(vocab_few_kernel<TT, true>, FEW_SMEM) : e;
+  }();
+  if (attr != cudaSuccess) return attr;
+  const size_t smem = (size_t)TT * a.hidden * 4;
+  if (!backward) {
+    note_launch(2);
+    DO(launch_pdl(vocab_few_kernel<TT, false>, dim3(p.ctas), dim3(FEW_THREADS), smem, st, a, stats, zlab, (float*)nullptr));
+    Prep r = {};
+    r.rows = TT;
+    return launch_pdl(vocab_join_kernel, dim3(parts_of(a.tokens, 8)), dim3(512), 0, st, a, r, (const float2*)stats, (const float*)zlab,
+                      p.ctas * (FEW_THREADS / 32), 1);
+  }
+  note_launch(1);
+  DO(launch_pdl(vocab_few_kernel<TT, true>, dim3(p.ctas), dim3(FEW_THREADS), smem, st, a, stats, zlab, dz));
+  if (!a.dx_dev) return cudaSuccess;
+  const int blocks = parts_of(a.hidden, 128), pitch = up(a.hidden, 4);
+  note_launch(2);
+  DO(launch_pdl(vocab_few_dx_kernel<TT>, dim3(blocks, p.parts), dim3(256), 0, st, a, (const float*)dz, sums, p.per, pitch));
+  return launch_pdl(vocab_few_sum_kernel, dim3(parts_of(a.hidden, 512), a.tokens), dim3(128), 0, st, a, (const float*)sums, p.parts,
+                    (int64_t)TT * pitch, pitch);
+}
+cudaError_t few_any(const ra_vocab_loss_args& a, bool backward, cudaStream_t st) {
+  return a.tokens <= 8 ? few_run<8>(a, backward, st) : a.tokens <= 16 ? few_run<16>(a, backward, st) : few_run<FEW>(a, backward, st);
+}
+
 }  // namespace
 
-size_t vocab_loss_workspace(const ra_vocab_loss_args& a) { return plan(a).bytes; }
-cudaError_t vocab_loss_fwd(const ra_vocab_loss_args& a, cudaStream_t st) { return a.dtype == RA_BF16 ? forward<1>(a, st) : forward<3>(a, st); }
+size_t vocab_loss_workspace(const ra_vocab_loss_args& a) { return few(a) ? few_plan(a).bytes : plan(a).bytes; }
+cudaError_t vocab_loss_fwd(const ra_vocab_loss_args& a, cudaStream_t st) {
+  if (few(a)) return few_any(a, false, st);
+  return a.dtype == RA_BF16 ? forward<1>(a, st) : forward<3>(a, st);
+}
 cudaError_t vocab_loss_bwd(const ra_vocab_loss_args& a, cudaStream_t st) {
   if (a.tokens == 0) {
     const size_t es = a.dtype == RA_BF16 ? 2 : 4;
     return cudaMemset2DAsync(a.dw_dev, a.dw_stride * es, 0, a.hidden * es, a.vocab, st);
   }
+  if (few(a)) return few_any(a, true, st);
   return a.dtype == RA_BF16 ? backward<bf16, 1>(a, st) : backward<float, 3>(a, st);
 }
 

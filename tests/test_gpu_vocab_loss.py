@@ -87,7 +87,8 @@ def check(s, dtype, grads=("dx", "dw")):
 
 
 SIZES = [(1, 1, 8), (1, 5, 8), (3, 40, 16), (7, 1000, 64), (64, 64, 64), (65, 257, 72), (130, 513, 128), (300, 5003, 136),
-         (1025, 300, 256), (513, 2050, 512), (257, 30011, 64), (2, 100000, 32), (4100, 97, 24)]
+         (1025, 300, 256), (513, 2050, 512), (257, 30011, 64), (2, 100000, 32), (4100, 97, 24), (8, 3001, 1000), (9, 77, 2048), (16, 500, 200),
+         (17, 1003, 1024), (32, 2000, 136), (33, 2000, 136), (5, 70, 4104), (30, 3, 64)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -102,8 +103,9 @@ def test_against_64_bits(tokens, vocab, hidden, dtype):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("ignored", [0.0, 0.9, 1.1])
-def test_how_many_are_counted(dtype, ignored):
-    a, s = make(300, 700, 64, dtype, ignored=ignored)
+@pytest.mark.parametrize("tokens", [20, 300])
+def test_how_many_are_counted(dtype, ignored, tokens):
+    a, s = make(tokens, 700, 64, dtype, ignored=ignored)
     both(a)
     torch.cuda.synchronize()
     check(s, dtype)
@@ -119,8 +121,9 @@ def test_one_token_is_counted():
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_what_is_not_counted_does_not_matter(dtype):
-    a, s = make(300, 700, 64, dtype, ignored=0.3)
+@pytest.mark.parametrize("tokens", [20, 300])
+def test_what_is_not_counted_does_not_matter(dtype, tokens):
+    a, s = make(tokens, 700, 64, dtype, ignored=0.3)
     both(a)
     torch.cuda.synchronize()
     want = {n: s[n].clone() for n in ("loss", "lse", "dx", "dw")}
@@ -135,23 +138,30 @@ def test_what_is_not_counted_does_not_matter(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_labels_out_of_range(dtype):
-    a, s = make(100, 500, 64, dtype)
-    s["labels"][3], s["labels"][60], s["labels"][61] = 500, 2 ** 31 - 1, -2 ** 31
-    both(a)
-    torch.cuda.synchronize()
-    check(s, dtype)
-    assert int(s["err"]) == R.RA_DEV_BOUNDS
+@pytest.mark.parametrize("tokens", [20, 100, 300])
+def test_labels_out_of_range(dtype, tokens):
+    for call in ("forward", "backward"):
+        a, s = make(tokens, 500, 64, dtype)
+        s["labels"][3], s["labels"][10], s["labels"][11] = 500, 2 ** 31 - 1, -2 ** 31
+        both(a)
+        torch.cuda.synchronize()
+        check(s, dtype)
+        assert int(s["err"]) == R.RA_DEV_BOUNDS
+        s["err"].zero_()
+        (R.ra_vocab_loss_forward if call == "forward" else R.ra_vocab_loss_backward)(a)
+        torch.cuda.synchronize()
+        assert int(s["err"]) == R.RA_DEV_BOUNDS, call
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("pad", [8, 56])
-def test_strides(dtype, pad):
-    a, s = make(150, 333, 64, dtype, pad=pad)
+@pytest.mark.parametrize("tokens", [12, 150])
+def test_strides(dtype, pad, tokens):
+    a, s = make(tokens, 333, 64, dtype, pad=pad)
     both(a)
     torch.cuda.synchronize()
     check(s, dtype)
-    for n, rows in (("dx", 149), ("dw", 332)):
+    for n, rows in (("dx", tokens - 1), ("dw", 332)):
         between = torch.as_strided(s[n], (rows, pad), (64 + pad, 1), s[n].storage_offset() + 64)
         assert bool((between == 7.0).all())
 
@@ -159,10 +169,11 @@ def test_strides(dtype, pad):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_large_logits(dtype):
     """Logits of hundreds: exponentials of all but a few words vanish, and nothing overflows."""
-    a, s = make(200, 900, 64, dtype, scale=150.0)
-    both(a)
-    torch.cuda.synchronize()
-    check(s, dtype)
+    for tokens in (7, 200):
+        a, s = make(tokens, 900, 64, dtype, scale=150.0)
+        both(a)
+        torch.cuda.synchronize()
+        check(s, dtype)
 
 
 def test_words_of_the_label_alone():
@@ -173,19 +184,22 @@ def test_words_of_the_label_alone():
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_a_token_that_is_not_finite_stays_by_itself_in_dx(dtype):
-    a, s = make(300, 700, 64, dtype, ignored=0.0)
-    s["x"][77, 3] = float("nan")
+@pytest.mark.parametrize("tokens,at", [(20, 7), (100, 77), (300, 77)])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_a_token_that_is_not_finite_stays_by_itself_in_dx(dtype, tokens, at, value):
+    a, s = make(tokens, 700, 64, dtype, ignored=0.0)
+    s["x"][at, 3] = value
     both(a)
     torch.cuda.synchronize()
-    ok = torch.arange(300, device="cuda") != 77
-    assert bool(s["loss"][77].isnan()) and bool(s["dx"][77].isnan().all())
+    ok = torch.arange(tokens, device="cuda") != at
+    assert not bool(s["loss"][at].isfinite()) and not bool(s["dx"][at].isfinite().any())
     assert bool(s["loss"][ok].isfinite().all()) and bool(s["dx"][ok].isfinite().all())
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_parts(dtype):
-    a, s = make(200, 700, 64, dtype)
+@pytest.mark.parametrize("tokens", [25, 200])
+def test_parts(dtype, tokens):
+    a, s = make(tokens, 700, 64, dtype)
     both(a)
     torch.cuda.synchronize()
     want = {n: s[n].clone() for n in ("loss", "lse", "dx", "dw")}
@@ -237,9 +251,10 @@ def test_against_differences():
         assert abs(first - float(grads[name].view(-1)[i])) <= third * h * h / 3 + 16 * 32 * U * 4 / h
 
 
-def test_the_same_twice_captured_and_on_two_streams():
-    a, s = make(400, 3000, 128, "bf16")
-    b, t = make(77, 1500, 64, "f32", seed=5)
+@pytest.mark.parametrize("wide", [True, False])
+def test_the_same_twice_captured_and_on_two_streams(wide):
+    a, s = make(400 if wide else 90, 3000, 128, "bf16")
+    b, t = make(77 if wide else 9, 1500, 64, "f32", seed=5)
     names = ("loss", "lse", "dx", "dw")
     for x in (a, b):
         both(x)
@@ -263,7 +278,7 @@ def test_the_same_twice_captured_and_on_two_streams():
 
 
 def test_one_workspace_for_any_shapes():
-    cases = [make(5, 3000, 64, "bf16"), make(700, 90, 128, "f32"), make(130, 1025, 64, "bf16")]
+    cases = [make(5, 3000, 64, "bf16"), make(700, 90, 128, "f32"), make(130, 1025, 64, "bf16"), make(11, 900, 64, "f32")]
     need = max(s["workspace"].numel() for _, s in cases)
     ws = workspace(need)
     ws[16384:] = 255
@@ -273,5 +288,5 @@ def test_one_workspace_for_any_shapes():
             both(a)
     torch.cuda.synchronize()
     assert bool((ws[:16384] == 0).all())
-    for (a, s), dtype in zip(cases, ("bf16", "f32", "bf16")):
+    for (a, s), dtype in zip(cases, ("bf16", "f32", "bf16", "f32")):
         check(s, dtype)
