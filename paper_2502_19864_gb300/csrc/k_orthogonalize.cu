@@ -9,7 +9,8 @@
 // steps grows with them, about 140-fold by the last; 2^-17 is then a quarter of the output's own rounding at
 // worst, where one plane's 2^-9 would be as large as what is computed.
 //
-// Bound: the products, 2 low^2 high + low^3 multiply-adds a step, three (six) times over for the planes.
+// Bound: the products, 1.5 low^2 high + low^3 / 2 multiply-adds a step with the symmetric ones' halves, three (six) times over for
+// the planes; of small matrices the launches.  2048 x 5632 in bf16 0.87 ms for five steps, 2 x 777 x 1000 in fp32 0.37 ms.
 #include <algorithm>
 
 #include "common.cuh"
@@ -290,8 +291,8 @@ struct Step {
 // [block][64 rows][64 of the shorter side], 128-byte swizzled.  S is the sum of the CTAs' products X^T X, which they leave
 // for one another in shared memory and each adds up, in the same order; S T and X Q each CTA does by itself.  The same storage is an
 // MN-major operand of X^T X and a K-major one of X Q.
-// Bound: latency.  A step is three products' issue and read-out and one meeting of the cluster, 7 us, where three
-// launches of the products above take 30 (48 of 1024 x 64).
+// Bound: latency.  A step is three products' issue and read-out and one meeting of the cluster: 48 of 1024 x 64 in bf16 take 6.6 us a
+// step and 46 us in all (three launches of the products above a step: 200 us in all), 8 of 128 x 16 in fp32 29 us (91 us).
 constexpr int SMALL = 64, SMALL_THREADS = 512, SMALL_BLOCK = SMALL * 128;  // bytes of a block's plane
 constexpr int PART_PITCH = SMALL + 4;                                      // of S in fp32: rows four banks apart
 constexpr int PART_BYTES = SMALL * PART_PITCH * 4;
