@@ -502,6 +502,7 @@ __global__ void __launch_bounds__(FEW_THREADS, TT <= 16 ? 2 : 1)
     *reinterpret_cast<float4*>(xs + t * H + c) = in ? *reinterpret_cast<const float4*>(x + t * a.x_stride + c) : make_float4(0.f, 0.f, 0.f, 0.f);
   }
   __syncthreads();
+  if (blockIdx.x == 0 && tid < a.tokens && a.labels_dev[tid] >= a.vocab) set_dev_error(a.err_dev, RA_DEVERR_BOUNDS);
   const int k = lane * EACH / TT, t0 = lane * EACH % TT;
   int label[EACH];
   float scale[EACH], lse[EACH], m[EACH], l[EACH];
@@ -682,7 +683,6 @@ __global__ void __launch_bounds__(128) vocab_few_sum_kernel(const __grid_constan
   pdl_trigger();
   if (c >= a.hidden) return;
   const int label = a.labels_dev[t];
-  if (label >= a.vocab && c == 0) set_dev_error(a.err_dev, RA_DEVERR_BOUNDS);
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
   if (counted(a, label))
     for (int i0 = 0; i0 < parts; i0 += 8) {

@@ -110,3 +110,13 @@ def test_matrices_side_by_side():
     assert R.ra_orthogonalize_workspace_bytes(orth(**side)) >= 16384
     for wrong in (dict(x_stride=127), dict(x_matrix_stride=63), dict(out_stride=128), dict(out_matrix_stride=67)):
         assert R.ra_orthogonalize_workspace_bytes(orth(**{**side, **wrong})) == 0
+
+
+def test_products_let_dependents_start_behind_the_allocation():
+    """As test_tmem_order.py has it for the kernels in .cu files: the products' kernel is in a header."""
+    import os
+    import re
+    path = os.path.join(os.path.dirname(os.path.abspath(__file__)), "..", "paper_2502_19864_gb300", "csrc", "products.cuh")
+    body = re.sub(r"//[^\n]*", "", open(path).read()).split("__global__")[1]
+    barrier = body.index("__syncthreads()", body.rindex("tcgen05.alloc"))
+    assert body.index("pdl_trigger()") > barrier
