@@ -8,7 +8,7 @@
 // a second kernel, in a fixed order.
 //
 // Bound: bytes.  A row is read once, held in registers through the reductions and written once.  A CTA's threads share a
-// row, eight (16, 32) values each, and take ROWS rows at a time, so that enough loads are on their way and a barrier
+// row (up to 256 values: a warp's), eight (16, 32) values each, and take ROWS rows at a time, so that enough loads are on their way and a barrier
 // serves them all; two values an instruction, as the instructions' issue is the next bound (28 a value without: 165 us, with 137).
 // Forward and backward of 65536 x 1024 in bf16 take 137 us (4.9 TB/s), of 8192 x 2048 with its residual 52 us (5.2 TB/s).
 #include <algorithm>
@@ -21,7 +21,7 @@ namespace {
 
 constexpr int NORM_MAX_CTAS = 608;  // four an SM of 152: the backward's partial sums
 
-// VEC values at a 16-byte aligned place (VEC 1: anywhere), as they come from memory.  keep(): what was computed of them before is
+// VEC values at a place that is a multiple of their bytes, as they come from memory.  keep(): what was computed of them before is
 // computed again after, and not held in registers of its own in between
 template <typename T, int VEC> struct Raw;
 template <> struct Raw<float, 4> {
@@ -43,6 +43,27 @@ template <> struct Raw<bf16, 8> {
   }
   __device__ __forceinline__ void keep() { asm volatile("" : "+r"(v.x), "+r"(v.y), "+r"(v.z), "+r"(v.w)); }
 };
+template <> struct Raw<float, 2> {
+  float2 v;
+  __device__ __forceinline__ void load(const float* p) { v = *reinterpret_cast<const float2*>(p); }
+  __device__ __forceinline__ void get(float* f) const { f[0] = v.x; f[1] = v.y; }
+  __device__ __forceinline__ void keep() { asm volatile("" : "+f"(v.x), "+f"(v.y)); }
+};
+template <> struct Raw<bf16, 4> {
+  uint2 v;
+  __device__ __forceinline__ void load(const bf16* p) { v = *reinterpret_cast<const uint2*>(p); }
+  __device__ __forceinline__ void get(float* f) const {
+    f[0] = __uint_as_float(v.x << 16); f[1] = __uint_as_float(v.x & 0xffff0000u);
+    f[2] = __uint_as_float(v.y << 16); f[3] = __uint_as_float(v.y & 0xffff0000u);
+  }
+  __device__ __forceinline__ void keep() { asm volatile("" : "+r"(v.x), "+r"(v.y)); }
+};
+template <> struct Raw<bf16, 2> {
+  uint32_t v;
+  __device__ __forceinline__ void load(const bf16* p) { v = *reinterpret_cast<const uint32_t*>(p); }
+  __device__ __forceinline__ void get(float* f) const { f[0] = __uint_as_float(v << 16); f[1] = __uint_as_float(v & 0xffff0000u); }
+  __device__ __forceinline__ void keep() { asm volatile("" : "+r"(v)); }
+};
 template <> struct Raw<float, 8> {
   float4 a, b;
   __device__ __forceinline__ void load(const float* p) {
@@ -61,18 +82,23 @@ template <typename T> struct Raw<T, 1> {
   __device__ __forceinline__ void keep() {}
 };
 template <int VEC> __device__ __forceinline__ void put(float* p, const float* v) {
-  if (VEC == 1) *p = v[0];
-  else *reinterpret_cast<float4*>(p) = make_float4(v[0], v[VEC > 1 ? 1 : 0], v[VEC > 1 ? 2 : 0], v[VEC > 1 ? 3 : 0]);
+  if constexpr (VEC == 1) *p = v[0];
+  else if constexpr (VEC == 2) *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]);
+  else *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
 }
 template <int VEC> __device__ __forceinline__ void put(bf16* p, const float* v) {
-  if (VEC == 1) {
+  if constexpr (VEC == 1) {
     *p = __float2bfloat16_rn(v[0]);
   } else {
-    uint4 x;
-    __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&x);
+    uint32_t w[VEC / 2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(v[VEC > 1 ? 2 * i : 0], v[VEC > 1 ? 2 * i + 1 : 0]);
-    *reinterpret_cast<uint4*>(p) = x;
+    for (int i = 0; i < VEC / 2; ++i) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    if constexpr (VEC == 2) *reinterpret_cast<uint32_t*>(p) = w[0];
+    else if constexpr (VEC == 4) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+    else *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
 
@@ -134,10 +160,14 @@ __device__ __forceinline__ float inv_sqrt(float v) {
   return y > 0.f && y < INFINITY ? r : y;  // (of 0, infinity and NaN the unit's answer)
 }
 
-// DEPTH groups of ROWS rows in shared memory on their way from `N_IN` inputs, 16 bytes (VEC values) a thread at a place of its own,
-// so that no thread waits for another's copies
-__device__ __forceinline__ void copy16(void* smem, const void* p) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(p) : "memory");
+// DEPTH groups of ROWS rows in shared memory on their way from the inputs, BYTES (VEC values) a thread at a place of its own, so
+// that no thread waits for another's copies
+template <int BYTES>
+__device__ __forceinline__ void copy(void* smem, const void* p) {
+  if constexpr (BYTES == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(p) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(p), "n"(BYTES) : "memory");
 }
 __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -186,7 +216,7 @@ constexpr int min_ctas(int n, int rows, bool backward) { return n == 8 && rows >
 template <typename T, typename W, int VEC, int NV, int ROWS, int DEPTH>
 __global__ void __launch_bounds__(max_threads(VEC * NV, ROWS), min_ctas(VEC * NV, ROWS, false)) norm_fwd_kernel(const __grid_constant__ ra_norm_args a) {
   __shared__ __align__(16) float sh1[2 * 32 * ROWS], sh2[2 * 32 * 2 * ROWS];
-  constexpr int N = VEC * NV;
+  constexpr int N = VEC * NV, PIECE = VEC * (int)sizeof(T);
   const int t = threadIdx.x, G = blockDim.x, H = a.hidden;
   const bool layer = a.kind == RA_NORM_LAYER;
   const float inv = 1.f / (float)H;
@@ -194,10 +224,11 @@ __global__ void __launch_bounds__(max_threads(VEC * NV, ROWS), min_ctas(VEC * NV
   const W* beta = static_cast<const W*>(a.beta_dev);
   pdl_wait();
   pdl_trigger();
-  extern __shared__ __align__(16) uint8_t ring[];  // [DEPTH][inputs][ROWS][NV][G] pieces of 16 bytes
+  extern __shared__ __align__(16) uint8_t ring[];  // [blockDim.y][DEPTH][inputs][ROWS][NV][G] pieces
   const int inputs = a.residual_dev ? 2 : 1;
-  const int64_t step = (int64_t)gridDim.x * ROWS;
-  auto place = [&](int slot, int in, int r, int i) { return ring + ((((slot * inputs + in) * ROWS + r) * NV + i) * G + t) * 16; };
+  const int64_t first = ((int64_t)blockIdx.x * blockDim.y + threadIdx.y) * ROWS, step = (int64_t)gridDim.x * blockDim.y * ROWS;
+  uint8_t* own = ring + threadIdx.y * (DEPTH * inputs * ROWS * NV * G * PIECE);
+  auto place = [&](int slot, int in, int r, int i) { return own + ((((slot * inputs + in) * ROWS + r) * NV + i) * G + t) * PIECE; };
   auto fetch = [&](int64_t row0, int slot) {
     if constexpr (DEPTH > 0) {
 #pragma unroll
@@ -206,8 +237,8 @@ __global__ void __launch_bounds__(max_threads(VEC * NV, ROWS), min_ctas(VEC * NV
         for (int i = 0; i < NV; ++i) {
           const int c = (i * G + t) * VEC;
           if (c < H && row0 + r < a.rows) {
-            copy16(place(slot, 0, r, i), static_cast<const T*>(a.x_dev) + (row0 + r) * a.x_stride + c);
-            if (inputs > 1) copy16(place(slot, 1, r, i), static_cast<const T*>(a.residual_dev) + (row0 + r) * a.residual_stride + c);
+            copy<PIECE>(place(slot, 0, r, i), static_cast<const T*>(a.x_dev) + (row0 + r) * a.x_stride + c);
+            if (inputs > 1) copy<PIECE>(place(slot, 1, r, i), static_cast<const T*>(a.residual_dev) + (row0 + r) * a.residual_stride + c);
           }
         }
       copies_end();
@@ -221,8 +252,8 @@ __global__ void __launch_bounds__(max_threads(VEC * NV, ROWS), min_ctas(VEC * NV
   };
   int turn = 0, slot = 0;
   if constexpr (DEPTH > 0)
-    for (int d = 0; d + 1 < DEPTH; ++d) fetch((int64_t)blockIdx.x * ROWS + d * step, d);
-  for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < a.rows; row0 += step, ++turn) {
+    for (int d = 0; d + 1 < DEPTH; ++d) fetch(first + d * step, d);
+  for (int64_t row0 = first; row0 < a.rows; row0 += step, ++turn) {
     if constexpr (DEPTH > 0) {
       fetch(row0 + (DEPTH - 1) * step, slot == 0 ? DEPTH - 1 : slot - 1);
       copies_wait<DEPTH - 1>();
@@ -341,7 +372,7 @@ __global__ void __launch_bounds__(max_threads(VEC * NV, ROWS), min_ctas(VEC * NV
 template <typename T, typename W, int VEC, int NV, int ROWS, int DEPTH>
 __global__ void __launch_bounds__(max_threads(VEC * NV, ROWS), min_ctas(VEC * NV, ROWS, true)) norm_bwd_kernel(const __grid_constant__ ra_norm_args a, float* sums) {
   __shared__ __align__(16) float sh[2 * 32 * 2 * ROWS];
-  constexpr int N = VEC * NV;
+  constexpr int N = VEC * NV, PIECE = VEC * (int)sizeof(T);
   const int t = threadIdx.x, G = blockDim.x, H = a.hidden;
   const bool layer = a.kind == RA_NORM_LAYER;
   const float inv = 1.f / (float)H;
@@ -363,15 +394,16 @@ __global__ void __launch_bounds__(max_threads(VEC * NV, ROWS), min_ctas(VEC * NV
         v.get(w + i * VEC);
       }
     }
-  extern __shared__ __align__(16) uint8_t ring[];  // [DEPTH][inputs][ROWS][NV][G] pieces of 16 bytes
+  extern __shared__ __align__(16) uint8_t ring[];  // [blockDim.y][DEPTH][inputs][ROWS][NV][G] pieces
   const bool more = a.dsum_dev && a.dx_dev;
   const int inputs = more ? 3 : 2;
-  const int64_t step = (int64_t)gridDim.x * ROWS;
+  const int64_t first = ((int64_t)blockIdx.x * blockDim.y + threadIdx.y) * ROWS, step = (int64_t)gridDim.x * blockDim.y * ROWS;
+  uint8_t* own = ring + threadIdx.y * (DEPTH * inputs * ROWS * NV * G * PIECE);
   auto source = [&](int in, int64_t row, int c) {
     return in == 0 ? zsrc + row * zstride + c
                    : in == 1 ? static_cast<const T*>(a.dy_dev) + row * a.dy_stride + c : static_cast<const T*>(a.dsum_dev) + row * a.dsum_stride + c;
   };
-  auto place = [&](int slot, int in, int r, int i) { return ring + ((((slot * inputs + in) * ROWS + r) * NV + i) * G + t) * 16; };
+  auto place = [&](int slot, int in, int r, int i) { return own + ((((slot * inputs + in) * ROWS + r) * NV + i) * G + t) * PIECE; };
   auto fetch = [&](int64_t row0, int slot) {
     if constexpr (DEPTH > 0) {
 #pragma unroll
@@ -380,9 +412,9 @@ __global__ void __launch_bounds__(max_threads(VEC * NV, ROWS), min_ctas(VEC * NV
         for (int i = 0; i < NV; ++i) {
           const int c = (i * G + t) * VEC;
           if (c < H && row0 + r < a.rows) {
-            copy16(place(slot, 0, r, i), source(0, row0 + r, c));
-            copy16(place(slot, 1, r, i), source(1, row0 + r, c));
-            if (more) copy16(place(slot, 2, r, i), source(2, row0 + r, c));
+            copy<PIECE>(place(slot, 0, r, i), source(0, row0 + r, c));
+            copy<PIECE>(place(slot, 1, r, i), source(1, row0 + r, c));
+            if (more) copy<PIECE>(place(slot, 2, r, i), source(2, row0 + r, c));
           }
         }
       copies_end();
@@ -390,8 +422,8 @@ __global__ void __launch_bounds__(max_threads(VEC * NV, ROWS), min_ctas(VEC * NV
   };
   int turn = 0, slot = 0;
   if constexpr (DEPTH > 0)
-    for (int d = 0; d + 1 < DEPTH; ++d) fetch((int64_t)blockIdx.x * ROWS + d * step, d);
-  for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < a.rows; row0 += step, ++turn) {
+    for (int d = 0; d + 1 < DEPTH; ++d) fetch(first + d * step, d);
+  for (int64_t row0 = first; row0 < a.rows; row0 += step, ++turn) {
     // (without a ring the rows are held as they came)
     Raw<T, VEC> held[DEPTH > 0 ? 1 : 3][DEPTH > 0 ? 1 : ROWS][DEPTH > 0 ? 1 : NV];
     float mean[ROWS], rstd[ROWS];
@@ -477,6 +509,29 @@ __global__ void __launch_bounds__(max_threads(VEC * NV, ROWS), min_ctas(VEC * NV
       }
     }
   }
+  if (blockDim.y > 1) {  // the warps' sums in turn
+    float* part = reinterpret_cast<float*>(ring);
+    const int all = N * G;
+    copies_wait<0>();
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const int c = (i * G + t) * VEC + j;
+        part[2 * threadIdx.y * all + c] = dg[i * VEC + j];
+        part[(2 * threadIdx.y + 1) * all + c] = db[i * VEC + j];
+      }
+    __syncthreads();
+    for (int k = threadIdx.y * G + t; k < 2 * H; k += blockDim.y * G) {
+      const int c = k < H ? k : k - H + all;
+      float v = 0.f;
+      for (int y = 0; y < (int)blockDim.y; ++y) v += part[2 * y * all + c];
+      if (k < H ? a.dgamma_dev != nullptr : a.dbeta_dev != nullptr)
+        sums[k < H ? (int64_t)blockIdx.x * H + k : (int64_t)(gridDim.x + blockIdx.x) * H + (k - H)] = v;
+    }
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -520,73 +575,105 @@ int bwd_ctas(const ra_norm_args& a) { return std::min(a.rows, NORM_MAX_CTAS); }
 // CTAs of `threads` with `smem` bytes each that an SM holds, as far as those decide
 int ctas_an_sm(int threads, int smem) { return std::max(1, std::min(2048 / threads, smem ? 227 * 1024 / (smem + 4096) : 32)); }
 
-template <typename T, typename W, int VEC, int NV, int ROWS, int DEPTH = 0>
-cudaError_t launch(const ra_norm_args& a, bool backward, cudaStream_t st) {
+template <bool BACK, typename T, typename W, int VEC, int NV, int ROWS, int DEPTH = 0>
+cudaError_t launch(const ra_norm_args& a, cudaStream_t st) {
   const int vecs = (a.hidden + VEC - 1) / VEC;
   const int threads = ((vecs + NV - 1) / NV + 31) / 32 * 32;
-  const int groups = (int)(((int64_t)a.rows + ROWS - 1) / ROWS);
-  const int each = DEPTH * ROWS * NV * threads * 16;  // of the ring, an input
-  constexpr int most_smem = DEPTH * ROWS * NV * max_threads(VEC * NV, ROWS) * 16;
-  note_launch(1);
-  if (!backward) {
-    auto k = norm_fwd_kernel<T, W, VEC, NV, ROWS, DEPTH>;
-    if (DEPTH > 0) {
-      static const cudaError_t attr = allow_smem(k, std::min(2 * most_smem, MAX_DYNAMIC_SMEM - 4096));
-      if (attr != cudaSuccess) return attr;
-    }
-    const int smem = each * (a.residual_dev ? 2 : 1), most = device_sm_count() * ctas_an_sm(threads, smem);
-    return launch_pdl(k, dim3(std::min(groups, most)), dim3(threads), smem, st, a);
-  }
-  auto k = norm_bwd_kernel<T, W, VEC, NV, ROWS, DEPTH>;
+  const int groups = (int)(((int64_t)a.rows + ROWS - 1) / ROWS), sms = device_sm_count();
+  // Rows of one warp: up to eight warps a CTA with rows of their own, as far as two CTAs an SM have as many (24071 x 40 in fp32
+  // backward 19 us, with a warp a CTA 33)
+  const int ys = threads == 32 && ROWS > 1 ? std::max(1, std::min(8, groups / (2 * sms))) : 1;
+  const int wide = (groups + ys - 1) / ys;
+  constexpr int each = DEPTH * ROWS * NV * VEC * (int)sizeof(T);  // bytes of the ring a thread and input
+  constexpr int most = std::min((BACK ? 3 : 2) * each * max_threads(VEC * NV, ROWS), MAX_DYNAMIC_SMEM - 4096);
+  auto k = [] {
+    if constexpr (BACK) return norm_bwd_kernel<T, W, VEC, NV, ROWS, DEPTH>;
+    else return norm_fwd_kernel<T, W, VEC, NV, ROWS, DEPTH>;
+  }();
   if (DEPTH > 0) {
-    static const cudaError_t attr = allow_smem(k, std::min(3 * most_smem, MAX_DYNAMIC_SMEM - 4096));
+    static const cudaError_t attr = allow_smem(k, most);
     if (attr != cudaSuccess) return attr;
   }
-  const int smem = each * (a.dsum_dev && a.dx_dev ? 3 : 2);
-  const int ctas = std::min(std::min(groups, NORM_MAX_CTAS), device_sm_count() * (DEPTH > 0 ? ctas_an_sm(threads, smem) : 4));
-  float* sums = reinterpret_cast<float*>(static_cast<char*>(a.workspace_dev) + WS_ZERO);
-  cudaError_t e = launch_pdl(k, dim3(ctas), dim3(threads), smem, st, a, sums);
-  if (e != cudaSuccess || (!a.dgamma_dev && !a.dbeta_dev)) return e;
   note_launch(1);
-  return launch_pdl(norm_weights_kernel<W>, dim3((a.hidden + 31) / 32, a.dbeta_dev ? 2 : 1), dim3(1024), 0, st,
-                    (const float*)sums, (W*)a.dgamma_dev, (W*)a.dbeta_dev, ctas, (int)a.hidden);
+  if constexpr (!BACK) {
+    const int smem = ys * threads * each * (a.residual_dev ? 2 : 1);
+    return launch_pdl(k, dim3(std::min(wide, sms * ctas_an_sm(threads * ys, smem))), dim3(threads, ys), smem, st, a);
+  } else {
+    const int ring = ys * threads * each * (a.dsum_dev && a.dx_dev ? 3 : 2);
+    const int smem = std::max(ring, ys > 1 ? ys * threads * 2 * VEC * NV * (int)sizeof(float) : 0);  // (the warps' sums after it)
+    const int ctas = std::min(std::min(wide, NORM_MAX_CTAS), sms * (DEPTH > 0 ? ctas_an_sm(threads * ys, smem) : 4));
+    float* sums = reinterpret_cast<float*>(static_cast<char*>(a.workspace_dev) + WS_ZERO);
+    const cudaError_t e = launch_pdl(k, dim3(ctas), dim3(threads, ys), smem, st, a, sums);
+    if (e != cudaSuccess || (!a.dgamma_dev && !a.dbeta_dev)) return e;
+    note_launch(1);
+    return launch_pdl(norm_weights_kernel<W>, dim3((a.hidden + 31) / 32, a.dbeta_dev ? 2 : 1), dim3(1024), 0, st,
+                      (const float*)sums, (W*)a.dgamma_dev, (W*)a.dbeta_dev, ctas, (int)a.hidden);
+  }
 }
 
 // rows of the ring by their values' size, and its groups (65536 x 1024 and 8192 x 2048 trained: 140 and 54 us; two rows and three
 // groups 154 and 62, three groups 145 and 60; without a ring 173 and 82)
 constexpr int RING_ROWS = 8, RING_DEPTH = 2;
-bool at16(const void* p, int64_t stride, int es) { return !p || (((uintptr_t)p & 15) == 0 && stride * es % 16 == 0); }
 
-template <typename T, typename W>
-cudaError_t dispatch(const ra_norm_args& a, bool backward, cudaStream_t st) {
-  constexpr int es = sizeof(T), V = 16 / es;
-  bool wide = a.hidden % V == 0 && at16(a.gamma_dev, 0, es) && at16(a.beta_dev, 0, es);
-  if (!backward || !a.residual_dev) wide = wide && at16(a.x_dev, a.x_stride, es);
-  wide = wide && at16(a.sum_dev, a.sum_stride, es);
-  if (backward)
-    wide = wide && at16(a.dy_dev, a.dy_stride, es) && at16(a.dsum_dev, a.dsum_stride, es) && at16(a.dx_dev, a.dx_stride, es);
-  else
-    wide = wide && at16(a.residual_dev, a.residual_stride, es) && at16(a.y_dev, a.y_stride, es);
-  // several rows at a time where there are enough of them for every SM
-  const bool many = a.rows >= 4 * 608;
-  if (wide) {
-    if (a.hidden <= 2048) return many ? launch<T, W, V, 8 / V, RING_ROWS / es, RING_DEPTH>(a, backward, st) : launch<T, W, V, 8 / V, 1>(a, backward, st);
-    if (a.hidden <= 8192) return many ? launch<T, W, V, 16 / V, 4 / es>(a, backward, st) : launch<T, W, V, 8 / V, 1>(a, backward, st);
-    return launch<T, W, V, 32 / V, 1>(a, backward, st);
+// The widest accesses that all rows and weights allow, up to 16 bytes
+template <typename T>
+int widest(const ra_norm_args& a, bool backward) {
+  constexpr int es = sizeof(T);
+  const int wes = a.w_dtype == RA_BF16 ? 2 : 4;
+  int v = 16 / es;
+  auto rows = [&](const void* p, int64_t stride) {
+    while (p && v > 1 && (((uintptr_t)p & (v * es - 1)) || stride % v)) v /= 2;
+  };
+  auto weights = [&](const void* p) {
+    while (p && v > 1 && ((uintptr_t)p & (std::min(16, v * wes) - 1))) v /= 2;
+  };
+  while (a.hidden % v) v /= 2;
+  weights(a.gamma_dev);
+  weights(a.beta_dev);
+  if (!backward || !a.residual_dev) rows(a.x_dev, a.x_stride);
+  rows(a.sum_dev, a.sum_stride);
+  if (backward) {
+    rows(a.dy_dev, a.dy_stride);
+    rows(a.dsum_dev, a.dsum_stride);
+    rows(a.dx_dev, a.dx_stride);
+  } else {
+    rows(a.residual_dev, a.residual_stride);
+    rows(a.y_dev, a.y_stride);
   }
-  if (a.hidden <= 8192) return a.hidden <= 2048 && many ? launch<T, W, 1, 8, 16 / es / 2>(a, backward, st) : launch<T, W, 1, 8, 1>(a, backward, st);
-  return launch<T, W, 1, 32, 1>(a, backward, st);
+  return v;
 }
 
-cudaError_t any(const ra_norm_args& a, bool backward, cudaStream_t st) {
-  if (a.dtype == RA_F32) return dispatch<float, float>(a, backward, st);
-  return a.w_dtype == RA_F32 ? dispatch<bf16, float>(a, backward, st) : dispatch<bf16, bf16>(a, backward, st);
+// VEC values an access; several rows at a time where there are enough of them for every SM, backward through a ring where they are
+// in pieces of 4 bytes at least, forward where they are in 16 (8192 x 8192 with its residual 91 us, without 142; in pieces of 4
+// 11793 x 2302 takes 70 us with it and 54 without).  Backward by single 2-byte values, rows longer than 2048 go one by one, as two
+// have no room in the registers (11793 x 2299: 139 us, 300 so)
+template <bool BACK, typename T, typename W, int VEC>
+cudaError_t by_size(const ra_norm_args& a, cudaStream_t st) {
+  constexpr int piece = VEC * (int)sizeof(T), NV = 8 / VEC, DEPTH = piece >= (BACK ? 4 : 16) ? RING_DEPTH : 0;
+  const bool many = a.rows >= 4 * 608;
+  if (a.hidden <= 2048 && many) return launch<BACK, T, W, VEC, NV, RING_ROWS / (int)sizeof(T), DEPTH>(a, st);
+  if constexpr (!BACK || DEPTH > 0)
+    if (a.hidden <= 8192 && many) return launch<BACK, T, W, VEC, 2 * NV, RING_ROWS / 2 / (int)sizeof(T), DEPTH>(a, st);
+  if (a.hidden <= 8192) return launch<BACK, T, W, VEC, NV, 1>(a, st);
+  return launch<BACK, T, W, VEC, 4 * NV, 1>(a, st);
+}
+template <bool BACK, typename T, typename W>
+cudaError_t dispatch(const ra_norm_args& a, cudaStream_t st) {
+  const int vec = widest<T>(a, BACK);
+  if constexpr (sizeof(T) == 2)
+    if (vec == 8) return by_size<BACK, T, W, 8>(a, st);
+  return vec == 4 ? by_size<BACK, T, W, 4>(a, st) : vec == 2 ? by_size<BACK, T, W, 2>(a, st) : by_size<BACK, T, W, 1>(a, st);
+}
+template <bool BACK>
+cudaError_t any(const ra_norm_args& a, cudaStream_t st) {
+  if (a.dtype == RA_F32) return dispatch<BACK, float, float>(a, st);
+  return a.w_dtype == RA_F32 ? dispatch<BACK, bf16, float>(a, st) : dispatch<BACK, bf16, bf16>(a, st);
 }
 
 }  // namespace
 
 size_t norm_workspace(const ra_norm_args& a) { return WS_ZERO + (size_t)bwd_ctas(a) * 2 * a.hidden * sizeof(float); }
-cudaError_t norm_fwd(const ra_norm_args& a, cudaStream_t st) { return any(a, false, st); }
+cudaError_t norm_fwd(const ra_norm_args& a, cudaStream_t st) { return any<false>(a, st); }
 cudaError_t norm_bwd(const ra_norm_args& a, cudaStream_t st) {
   if (a.rows == 0) {
     const size_t n = (size_t)a.hidden * (a.w_dtype == RA_BF16 ? 2 : 4);
@@ -594,7 +681,7 @@ cudaError_t norm_bwd(const ra_norm_args& a, cudaStream_t st) {
     if (e == cudaSuccess && a.dbeta_dev) e = cudaMemsetAsync(a.dbeta_dev, 0, n, st);
     return e;
   }
-  return any(a, true, st);
+  return any<true>(a, st);
 }
 
 }  // namespace ra

@@ -124,6 +124,21 @@ def test_strides(dtype, pad):
         assert bool((whole == 7.0).all())
 
 
+@pytest.mark.parametrize("dtype,wdtype", [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("kind,residual", [("layer", False), ("rms", True)])
+@pytest.mark.parametrize("rows,hidden,pad", [(70, 386, 0), (2501, 386, 0), (2501, 1340, 0), (2501, 392, 2), (2501, 392, 4), (2501, 77, 0),
+                                             (2501, 2302, 0), (2501, 2300, 4), (2501, 2299, 0), (70, 8198, 0)])
+def test_accesses_of_each_width(rows, hidden, pad, kind, residual, dtype, wdtype):
+    a, s = make(rows, hidden, kind, dtype, wdtype, residual, seed=rows + hidden, pad=pad)
+    R.ra_norm_forward(a)
+    R.ra_norm_backward(a)
+    torch.cuda.synchronize()
+    check(a, s, kind, dtype, wdtype, residual)
+    if pad:
+        for n in ("y", "dx") + (("sum",) if residual else ()):
+            assert bool((torch.as_strided(s[n], (rows - 1, pad), (hidden + pad, 1), s[n].storage_offset() + hidden) == 7.0).all()), n
+
+
 def test_a_place_that_is_not_aligned():
     a, s = make(20, 256, "layer", "bf16", "bf16", False)
     buf = torch.zeros(20 * 256 + 1, dtype=torch.bfloat16, device="cuda")
