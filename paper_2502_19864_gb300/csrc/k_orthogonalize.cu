@@ -189,6 +189,9 @@ struct OrthArgs {
   int k, n, cg, dtype;
   bool a_mn, b_mn, sym, last, map_out;
   float add, add2, mul2;
+  // S of few tiles and a long K: K in `splits` ranges of `blocks` k-blocks, whose sums go to sums [splits][n][rows][sums_pitch]
+  int splits, blocks, sums_pitch;
+  float* sums;
 };
 #define MAP(m, ...)                                                    \
   do {                                                                 \
@@ -219,11 +222,12 @@ struct Step {
   }
   static __device__ __forceinline__ int count(const Args& p) {
     int mt, nt;
-    return p.n * tiles(p, mt, nt);
+    return p.n * tiles(p, mt, nt) * p.splits;
   }
   static __device__ __forceinline__ void unit(const Args& p, int u, Unit& w) {
     int m_n, n_n, mt, nt;
-    const int each = tiles(p, m_n, n_n);
+    const int each = tiles(p, m_n, n_n), range = u % p.splits;
+    u /= p.splits;
     w.z = u / each;
     u %= each;
     if (p.sym) {
@@ -238,11 +242,12 @@ struct Step {
     w.b = &p.b;
     w.m0 = w.ar = mt * prod::BM * p.cg;
     w.n0 = w.br = nt * p.shape.bn;
-    w.ak = w.bk = w.kb0 = 0;
-    w.job = p.sym && mt != nt;  // its mirror image too
+    w.kb0 = range * p.blocks;
+    w.ak = w.bk = 0;
+    w.job = p.splits > 1 ? range : p.sym && mt != nt;  // the range; or: its mirror image too
     w.az = w.z * PA;
     w.bz = w.z * PB;
-    w.kb1 = (p.k + prod::BK - 1) / prod::BK;
+    w.kb1 = min(w.kb0 + p.blocks, (p.k + prod::BK - 1) / prod::BK);
     w.a_mn = p.a_mn;
     w.b_mn = p.b_mn;
   }
@@ -262,6 +267,14 @@ struct Step {
       if (p.power == 2) f *= f;
 #pragma unroll
       for (int j = 0; j < 32; ++j) v[j] *= f;
+    }
+    if (p.splits > 1) {
+      if (row < p.rows) {
+        float* to = p.sums + (((int64_t)w.job * p.n + w.z) * p.rows + row) * p.sums_pitch + col;
+#pragma unroll
+        for (int j = 0; j < 32; j += 4) *reinterpret_cast<float4*>(to + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+      }
+      return;
     }
     if (p.last) {
       if (p.map_out) {
@@ -284,6 +297,53 @@ struct Step {
     if (p.o2) put(p, w, p.o2, [&](int j) { return p.mul2 * v[j] + (j == diag ? p.add2 : 0.f); }, row, col, t.lane);
   }
 };
+
+// S and T from the ranges' sums, in order: a CTA a 32 x 32 block on or above the diagonal, and its mirror image
+template <int PLANES>
+__global__ void __launch_bounds__(256) orth_join_kernel(const OrthArgs p) {
+  __shared__ float tile[32][33];
+  pdl_wait();
+  pdl_trigger();
+  int bj = (int)((sqrtf(8.f * blockIdx.x + 1.f) - 1.f) * 0.5f);
+  while (bj * (bj + 1) / 2 > (int)blockIdx.x) --bj;
+  while ((bj + 1) * (bj + 2) / 2 <= (int)blockIdx.x) ++bj;
+  const int bi = (int)blockIdx.x - bj * (bj + 1) / 2, z = blockIdx.y, r = threadIdx.x >> 3, c = 4 * (threadIdx.x & 7);
+  const int64_t plane = (int64_t)p.rows * p.pitch, range = (int64_t)p.n * p.rows * p.sums_pitch;
+  auto put = [&](const float* v, int row, int col) {
+    if (row >= p.rows || col >= p.width) return;
+    uint32_t lo[PLANES], hi[PLANES], lo2[PLANES], hi2[PLANES];
+    float t[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) t[j] = p.mul2 * v[j] + (row == col + j ? p.add2 : 0.f);
+    prod::planes_of<PLANES>(v[0], v[1], lo);
+    prod::planes_of<PLANES>(v[2], v[3], hi);
+    prod::planes_of<PLANES>(t[0], t[1], lo2);
+    prod::planes_of<PLANES>(t[2], t[3], hi2);
+    const int64_t at = (int64_t)z * PLANES * plane + (int64_t)row * p.pitch + col;
+#pragma unroll
+    for (int k = 0; k < PLANES; ++k) {
+      *reinterpret_cast<uint2*>(p.o + at + k * plane) = make_uint2(lo[k], hi[k]);
+      *reinterpret_cast<uint2*>(p.o2 + at + k * plane) = make_uint2(lo2[k], hi2[k]);
+    }
+  };
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+  if (32 * bi + r < p.rows) {
+    const float* from = p.sums + ((int64_t)z * p.rows + 32 * bi + r) * p.sums_pitch + 32 * bj + c;
+#pragma unroll 4
+    for (int s = 0; s < p.splits; ++s) {
+      const float4 x = *reinterpret_cast<const float4*>(from + s * range);
+      v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
+    }
+  }
+  put(v, 32 * bi + r, 32 * bj + c);
+  if (bi == bj) return;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) tile[r][c + j] = v[j];
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] = tile[c + j][r];
+  put(v, 32 * bj + r, 32 * bi + c);
+}
 
 // ---- matrices whose smaller side is at most 64 --------------------------------------------------
 // An adapter's matrix stays on chip through all steps: a cluster of up to eight CTAs has one matrix, each CTA `blocks` blocks
@@ -713,12 +773,58 @@ cudaError_t run_small(const ra_orthogonalize_args& a, cudaStream_t st) {
   return cudaLaunchKernelEx(&cfg, k, p);
 }
 
+// A symmetric product: all tiles, or (sym) square ones on and above the diagonal, which takes rounds off and costs a round the
+// mirrored stores: 2048 x 2048 of K = 5632 in two planes 98 -> 73 us, two of 777 x 777 in three planes 49 -> 60
+double time_sym(Pick k, int rows, int n, int blocks) {
+  const int64_t t = parts_of(rows, k.bn);
+  return (double)parts_of(n * t * (t + 1) / 2, prod::SMS / k.cg) * (blocks * prod::block_time(k) + 6.) + (k.cg == 2 ? 1. : 0.);
+}
+Pick pick_sym(int rows, int n, int blocks, int planes, bool& sym) {
+  auto time = [&](Pick k) { return time_sym(k, rows, n, blocks); };
+  const Pick one = {1, 128}, two = {2, 256}, best = rows > 128 && prod::takes(two, planes, planes) && time(two) < time(one) ? two : one;
+  const Pick all = prod::pick(rows, rows, n, blocks, planes, planes);
+  sym = time(best) < prod::time_of(all, rows, rows, n, blocks);
+  return sym ? best : all;
+}
+
 struct Plan {
   int planes, low, high, parts;
   // columns to a multiple of 8, what TMA reads of a row; rows at 128 bytes, the boxes' rows (at 16, each would touch two lines)
   int width, pitch, low_width, low_pitch;
-  size_t norms, factors, x[2], s, t, q, bytes;
+  size_t norms, factors, x[2], s, t, q, sums, bytes;
 };
+// S's K in ranges where its tiles leave SMs idle: k-blocks of a range, by the time of rounds of tiles and 4 us for the join (3892 x 390
+// in fp32: 81 us a step in one range); all of them where that is slower than PICK's tiles with whole K
+int range_of(int rows, int n, int kbs, int planes, Pick pick, bool sym) {
+  const int terms = prod::terms_of(planes, planes).n;
+  const int64_t side = parts_of(rows, prod::BM), tiles = n * side * (side + 1) / 2;
+  double best = sym ? time_sym(pick, rows, n, kbs * terms) : prod::time_of(pick, rows, rows, n, kbs * terms);
+  int range = kbs;
+  for (int splits = 2; splits <= 16 && splits <= kbs; ++splits) {
+    const int each = parts_of(kbs, splits);
+    const double t = (double)parts_of(tiles * parts_of(kbs, each), prod::SMS) * (each * terms * prod::block_time({1, prod::BM}) + 1.) + 4.;
+    if (t < best) {
+      best = t;
+      range = each;
+    }
+  }
+  return range;
+}
+// The tiles and ranges of S, of matrices in `planes`
+struct Gram {
+  Pick pick;
+  bool sym;
+  int range, splits;
+};
+Gram gram_of(int low, int high, int n, int planes) {
+  Gram g;
+  const int kbs = parts_of(high, prod::BK);
+  g.pick = pick_sym(low, n, kbs * prod::terms_of(planes, planes).n, planes, g.sym);
+  g.range = range_of(low, n, kbs, planes, g.pick, g.sym);
+  g.splits = parts_of(kbs, g.range);
+  if (g.splits > 1) g.pick = {1, prod::BM}, g.sym = true;
+  return g;
+}
 Plan plan(const ra_orthogonalize_args& a) {
   Plan p = {};
   p.planes = a.dtype == RA_F32 ? 3 : 2;
@@ -742,21 +848,11 @@ Plan plan(const ra_orthogonalize_args& a) {
   p.s = take(n * p.low * p.low_pitch);
   p.t = take(n * p.low * p.low_pitch);
   p.q = take(n * p.low * p.low_pitch);
+  int splits = 1;  // (matrices of bf16 are one plane in the first step)
+  for (int planes : {p.planes, p.planes == 3 ? 3 : 1}) splits = std::max(splits, gram_of(p.low, p.high, a.n_matrices, planes).splits);
+  p.sums = take(splits > 1 ? (size_t)splits * a.n_matrices * p.low * up(p.low, 32) * 4 : 0);
   p.bytes = at;
   return p;
-}
-
-// A symmetric product: all tiles, or (sym) square ones on and above the diagonal, which takes rounds off and costs a round the
-// mirrored stores: 2048 x 2048 of K = 5632 in two planes 98 -> 73 us, two of 777 x 777 in three planes 49 -> 60
-Pick pick_sym(int rows, int n, int blocks, int planes, bool& sym) {
-  auto time = [&](Pick k) {
-    const int64_t t = parts_of(rows, k.bn);
-    return (double)parts_of(n * t * (t + 1) / 2, prod::SMS / k.cg) * (blocks * prod::block_time(k) + 6.) + (k.cg == 2 ? 1. : 0.);
-  };
-  const Pick one = {1, 128}, two = {2, 256}, best = rows > 128 && prod::takes(two, planes, planes) && time(two) < time(one) ? two : one;
-  const Pick all = prod::pick(rows, rows, n, blocks, planes, planes);
-  sym = time(best) < prod::time_of(all, rows, rows, n, blocks);
-  return sym ? best : all;
 }
 
 template <typename T>
@@ -787,13 +883,13 @@ cudaError_t run(const ra_orthogonalize_args& a, cudaStream_t st) {
   g.factors = factors;
   g.n = n;
   g.dtype = a.dtype;
-  auto shape = [&](OrthArgs& s, int rows, int cols, int k, int pa, int pb, bool sym) {
-    const int blocks = parts_of(k, prod::BK) * prod::terms_of(pa, pb).n;
-    const Pick c = sym ? pick_sym(rows, n, blocks, pa, sym) : prod::pick(rows, cols, n, blocks, pa, pb);
+  g.splits = 1;
+  auto shape = [&](OrthArgs& s, int rows, int cols, int k, int pa, int pb, Pick c, bool sym) {
     s.rows = rows;
     s.cols = cols;
     s.k = k;
     s.sym = sym;
+    s.blocks = parts_of(k, prod::BK);
     s.cg = c.cg;
     s.shape = prod::shape_of(c.bn, c.cg, pa, pb, chunk);
   };
@@ -801,11 +897,13 @@ cudaError_t run(const ra_orthogonalize_args& a, cudaStream_t st) {
   auto go = [&](const OrthArgs& s, auto step) {
     using S = decltype(step);
     int mt, nt;
-    const int u = (int)std::min<int64_t>((int64_t)n * S::tiles(s, mt, nt), 1 << 20);
+    const int u = (int)std::min<int64_t>((int64_t)n * S::tiles(s, mt, nt) * s.splits, 1 << 20);
     return s.cg == 2 ? prod::launch<S, 2>(s, u, st) : prod::launch<S, 1>(s, u, st);
   };
   OrthArgs square = g;
-  shape(square, p.low, p.low, p.low, p.planes, p.planes, true);
+  bool sym;
+  const Pick half = pick_sym(p.low, n, parts_of(p.low, prod::BK) * prod::terms_of(p.planes, p.planes).n, p.planes, sym);
+  shape(square, p.low, p.low, p.low, p.planes, p.planes, half, sym);
   square.add = a.a;
   square.o = q;
   square.width = p.low_width;
@@ -816,7 +914,12 @@ cudaError_t run(const ra_orthogonalize_args& a, cudaStream_t st) {
     const int px = i == 0 ? first : p.planes;
     const bf16* from = x[i & 1];
     OrthArgs gram = g, apply = g;
-    shape(gram, p.low, p.low, p.high, px, px, true);
+    const Gram how = gram_of(p.low, p.high, n, px);
+    shape(gram, p.low, p.low, p.high, px, px, how.pick, how.sym);
+    gram.splits = how.splits;
+    gram.blocks = how.range;
+    gram.sums = reinterpret_cast<float*>(ws + p.sums);
+    gram.sums_pitch = up(p.low, 32);
     gram.a_mn = gram.b_mn = !wide;
     gram.power = px == 1 ? 2 : 0;
     gram.o = s;
@@ -825,7 +928,8 @@ cudaError_t run(const ra_orthogonalize_args& a, cudaStream_t st) {
     gram.mul2 = a.c;
     gram.width = p.low_width;
     gram.pitch = p.low_pitch;
-    shape(apply, a.rows, a.cols, p.low, wide ? p.planes : px, wide ? px : p.planes, false);
+    const int pa = wide ? p.planes : px, pb = wide ? px : p.planes;
+    shape(apply, a.rows, a.cols, p.low, pa, pb, prod::pick(a.rows, a.cols, n, parts_of(p.low, prod::BK) * prod::terms_of(pa, pb).n, pa, pb), false);
     apply.b_mn = wide;
     apply.power = px == 1 ? 1 : 0;
     apply.o = x[(i + 1) & 1];
@@ -853,6 +957,11 @@ cudaError_t run(const ra_orthogonalize_args& a, cudaStream_t st) {
     }
     using Full = Step<PL, PL, PL>;
     DO(px == PL ? go(gram, Full()) : go(gram, Step<PL, ONE, ONE>()));
+    if (gram.splits > 1) {
+      const int side = parts_of(p.low, 32);
+      note_launch(1);
+      DO(launch_pdl(orth_join_kernel<PL>, dim3(side * (side + 1) / 2, n), dim3(256), 0, st, gram));
+    }
     DO(go(square, Full()));
     DO(px == PL ? go(apply, Full()) : wide ? go(apply, Step<PL, PL, ONE>()) : go(apply, Step<PL, ONE, PL>()));
   }

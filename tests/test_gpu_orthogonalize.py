@@ -147,6 +147,16 @@ def test_symmetric_products_by_halves(dtype, n, rows, cols):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,rows,cols", [(1, 3892, 390), (3, 70, 4001), (2, 2050, 129), (1, 20, 30000), (1, 2500, 256), (1, 32768, 65)])
+def test_long_sides_in_ranges(n, rows, cols, dtype):
+    """Sizes at which S has few tiles and a K that is cut in ranges."""
+    a, s = make(n, rows, cols, dtype)
+    R.ra_orthogonalize(a)
+    torch.cuda.synchronize()
+    check(s, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows,cols", [(90, 72), (72, 90), (300, 40)])
 def test_matrices_side_by_side(dtype, rows, cols):
     a, s = make(1, rows, 3 * cols, dtype)
