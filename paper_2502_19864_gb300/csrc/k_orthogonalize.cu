@@ -2,7 +2,7 @@
 //
 // X = x / (|x| + eps); then `steps` times X <- (a I + S (b I + c S)) X with S = X X^T (rows <= cols), or, which is the same
 // polynomial of X, X <- X (a I + S (b I + c S)) with S = X^T X: S has the smaller of the two sides.  A step is three
-// products on the tensor cores: S, of which S and T = b I + c S are kept; Q = a I + S T; and X.
+// products on the tensor cores: S; Q = a I + b S + c S S; and X.
 //
 // Operands are planes of bf16 (products.cuh).  For fp32 three, the significand whole.  For bf16 matrices two, 17 bits: a
 // step raises what lies along small singular values by up to 3.4445 while the large ones stay, so that an error of the first
@@ -177,21 +177,22 @@ __global__ void __launch_bounds__(256) orth_start_kernel(const ra_orthogonalize_
 }
 
 struct OrthArgs {
-  CUtensorMap a, b, out;   // the product's operands; the result
+  CUtensorMap a, b, out;   // the product's operands; the result, or its planes [n][planes][rows][pitch]
   prod::Shape shape;
   unsigned* err;
   const float* factors;    // of the first step's matrices: P is scaled by the power'th power of its factor
-  bf16 *o, *o2;            // P + add I and, if wanted, mul2 P + add2 I in planes [n][planes][rows][pitch]
+  const bf16* with;        // not NULL: the result is mul P + mul_with W + add I, W in planes like its own; else P
+  bf16* o;                 // (the ranges' sums': its planes)
   int width, pitch, power;  // (width: the columns that are written, to a multiple of 8)
   void* dst;
   int64_t dst_stride, dst_matrix_stride;
   int rows, cols;          // of the product
   int k, n, cg, dtype;
   bool a_mn, b_mn, sym, last, map_out;
-  float add, add2, mul2;
+  float add, mul, mul_with;
   // S of few tiles and a long K: K in `splits` ranges of `blocks` k-blocks, whose sums go to sums [splits][n][rows][sums_pitch]
   int splits, blocks, sums_pitch;
-  float* sums;
+  const float* sums;
 };
 #define MAP(m, ...)                                                    \
   do {                                                                 \
@@ -251,14 +252,6 @@ struct Step {
     w.a_mn = p.a_mn;
     w.b_mn = p.b_mn;
   }
-  template <typename F>
-  static __device__ __forceinline__ void put(const Args& p, const Unit& w, bf16* to, F f, int row, int col, int lane) {
-    const int64_t plane = (int64_t)p.rows * p.pitch;
-    bf16* base = to + (int64_t)w.z * PLANES * plane;
-    const int row0 = row - lane;
-    prod::planes_out<PLANES>(base + (int64_t)row0 * p.pitch + col, plane, p.pitch, f, p.rows - row0, p.width - col, lane);
-    if (w.job) prod::planes_mirrored<PLANES>(base + (int64_t)col * p.pitch + (row & ~1), plane, f, p.pitch, p.rows - col, row < p.width, lane);
-  }
   static __device__ __forceinline__ void part(const Args& p, const Unit& w, const Tile& t, Store& st, int i, float (&v)[32]) {
     const int row0 = w.m0 + t.rank * prod::BM + t.quad * 32, row = row0 + t.lane, col = w.n0 + 32 * (t.half + 2 * i);
     if (row0 >= p.rows || col >= p.cols) return;
@@ -269,36 +262,57 @@ struct Step {
       for (int j = 0; j < 32; ++j) v[j] *= f;
     }
     if (p.splits > 1) {
-      if (row < p.rows) {
-        float* to = p.sums + (((int64_t)w.job * p.n + w.z) * p.rows + row) * p.sums_pitch + col;
-#pragma unroll
-        for (int j = 0; j < 32; j += 4) *reinterpret_cast<float4*>(to + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-      }
+      st.f32_row(&p.out, v, col, row0, w.job * p.n + w.z, false, p.sums_pitch);
       return;
     }
     if (p.last) {
       if (p.map_out) {
         if (p.dtype == RA_BF16) st.bf16_row(&p.out, [&](int j) { return v[j]; }, col, row0, w.z);
         else st.f32_row(&p.out, v, col, row0, w.z, false, p.cols);
-      } else if (row < p.rows) {
-        const int64_t at = w.z * p.dst_matrix_stride + row * p.dst_stride + col;
-#pragma unroll
-        for (int j = 0; j < 32; ++j)
-          if (col + j < p.cols) {
-            if (p.dtype == RA_BF16) static_cast<bf16*>(p.dst)[at + j] = __float2bfloat16_rn(v[j]);
-            else static_cast<float*>(p.dst)[at + j] = v[j];
-          }
+      } else {
+        const int64_t at = w.z * p.dst_matrix_stride + row0 * p.dst_stride + col + t.lane;
+        st.by_columns(v, [&](int r, float x) {
+          if (row0 + r >= p.rows || col + t.lane >= p.cols) return;
+          if (p.dtype == RA_BF16) static_cast<bf16*>(p.dst)[at + r * p.dst_stride] = __float2bfloat16_rn(x);
+          else static_cast<float*>(p.dst)[at + r * p.dst_stride] = x;
+        });
       }
       return;
     }
-    // (the identity's part: nothing behind the last row)
-    const int diag = row < p.rows ? row - col : -1;
-    put(p, w, p.o, [&](int j) { return v[j] + (j == diag ? p.add : 0.f); }, row, col, t.lane);
-    if (p.o2) put(p, w, p.o2, [&](int j) { return p.mul2 * v[j] + (j == diag ? p.add2 : 0.f); }, row, col, t.lane);
+    if (p.with) {
+      const bf16* from = p.with + (int64_t)w.z * PLANES * p.rows * p.pitch + (int64_t)row0 * p.pitch + col;
+      uint32_t h[PLANES][16];
+#pragma unroll
+      for (int k = 0; k < PLANES; ++k)  // (a warp's load: 64 bytes of eight rows)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int r = (t.lane & ~3) + q, c = 8 * (t.lane & 3);
+          uint4 u = make_uint4(0, 0, 0, 0);
+          if (row0 + r < p.rows && col + c < p.width) u = *reinterpret_cast<const uint4*>(from + ((int64_t)k * p.rows + r) * p.pitch + c);
+          h[k][4 * q] = u.x, h[k][4 * q + 1] = u.y, h[k][4 * q + 2] = u.z, h[k][4 * q + 3] = u.w;
+        }
+      float x[32];
+#pragma unroll
+      for (int k = PLANES - 1; k >= 0; --k) {
+        tc::transpose4(h[k], t.lane);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const float lo = __uint_as_float(h[k][j] << 16), hi = __uint_as_float(h[k][j] & 0xffff0000u);
+          x[2 * j] = k + 1 < PLANES ? x[2 * j] + lo : lo;
+          x[2 * j + 1] = k + 1 < PLANES ? x[2 * j + 1] + hi : hi;
+        }
+      }
+      const int diag = row < p.rows ? row - col : -1;  // (nothing behind the last row)
+#pragma unroll
+      for (int j = 0; j < 32; ++j) v[j] = fmaf(p.mul, v[j], fmaf(p.mul_with, x[j], j == diag ? p.add : 0.f));
+    }
+    auto at = [&](int j) { return v[j]; };
+    st.planes<PLANES, false>(&p.out, at, col, row0, w.z * PLANES);
+    if (w.job) st.planes<PLANES, true>(&p.out, at, row0, col, w.z * PLANES);
   }
 };
 
-// S and T from the ranges' sums, in order: a CTA a 32 x 32 block on or above the diagonal, and its mirror image
+// S from the ranges' sums, in order: a CTA a 32 x 32 block on or above the diagonal, and its mirror image
 template <int PLANES>
 __global__ void __launch_bounds__(256) orth_join_kernel(const OrthArgs p) {
   __shared__ float tile[32][33];
@@ -311,20 +325,12 @@ __global__ void __launch_bounds__(256) orth_join_kernel(const OrthArgs p) {
   const int64_t plane = (int64_t)p.rows * p.pitch, range = (int64_t)p.n * p.rows * p.sums_pitch;
   auto put = [&](const float* v, int row, int col) {
     if (row >= p.rows || col >= p.width) return;
-    uint32_t lo[PLANES], hi[PLANES], lo2[PLANES], hi2[PLANES];
-    float t[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) t[j] = p.mul2 * v[j] + (row == col + j ? p.add2 : 0.f);
+    uint32_t lo[PLANES], hi[PLANES];
     prod::planes_of<PLANES>(v[0], v[1], lo);
     prod::planes_of<PLANES>(v[2], v[3], hi);
-    prod::planes_of<PLANES>(t[0], t[1], lo2);
-    prod::planes_of<PLANES>(t[2], t[3], hi2);
-    const int64_t at = (int64_t)z * PLANES * plane + (int64_t)row * p.pitch + col;
+    bf16* to = p.o + (int64_t)z * PLANES * plane + (int64_t)row * p.pitch + col;
 #pragma unroll
-    for (int k = 0; k < PLANES; ++k) {
-      *reinterpret_cast<uint2*>(p.o + at + k * plane) = make_uint2(lo[k], hi[k]);
-      *reinterpret_cast<uint2*>(p.o2 + at + k * plane) = make_uint2(lo2[k], hi2[k]);
-    }
+    for (int k = 0; k < PLANES; ++k) *reinterpret_cast<uint2*>(to + k * plane) = make_uint2(lo[k], hi[k]);
   };
   float v[4] = {0.f, 0.f, 0.f, 0.f};
   if (32 * bi + r < p.rows) {
@@ -773,56 +779,50 @@ cudaError_t run_small(const ra_orthogonalize_args& a, cudaStream_t st) {
   return cudaLaunchKernelEx(&cfg, k, p);
 }
 
-// A symmetric product: all tiles, or (sym) square ones on and above the diagonal, which takes rounds off and costs a round the
-// mirrored stores: 2048 x 2048 of K = 5632 in two planes 98 -> 73 us, two of 777 x 777 in three planes 49 -> 60
-double time_sym(Pick k, int rows, int n, int blocks) {
+// What an epilogue takes for 128 x 128, in microseconds a plane of it, of two or three: stored (with its mirror image twice that), read as much
+constexpr double plane_time(int kept) { return kept == 2 ? 0.8 : 1.9; }
+// A symmetric product: all tiles, or (sym) square ones on and above the diagonal, which takes rounds off and costs the
+// mirrored stores: 2048 x 2048 of K = 5632 in two planes 98 -> 73 us, two of 777 x 777 in three planes 49 -> 60.  `reads`: planes are read too
+double time_sym(Pick k, int rows, int n, int blocks, double out) {
   const int64_t t = parts_of(rows, k.bn);
-  return (double)parts_of(n * t * (t + 1) / 2, prod::SMS / k.cg) * (blocks * prod::block_time(k) + 6.) + (k.cg == 2 ? 1. : 0.);
+  return prod::time_of_tiles(k, n * t * (t + 1) / 2, blocks, t > 1 ? 2. * out : out);
 }
-Pick pick_sym(int rows, int n, int blocks, int planes, bool& sym) {
-  auto time = [&](Pick k) { return time_sym(k, rows, n, blocks); };
+struct Square {
+  Pick pick;
+  bool sym;
+  double time;
+};
+Square pick_sym(int rows, int n, int blocks, int planes, int kept, bool reads) {
+  const double write = kept * plane_time(kept), read = reads ? write : 0.;
+  auto time = [&](Pick k) { return time_sym(k, rows, n, blocks, write) + read * k.bn / 128.; };
   const Pick one = {1, 128}, two = {2, 256}, best = rows > 128 && prod::takes(two, planes, planes) && time(two) < time(one) ? two : one;
-  const Pick all = prod::pick(rows, rows, n, blocks, planes, planes);
-  sym = time(best) < prod::time_of(all, rows, rows, n, blocks);
-  return sym ? best : all;
+  const Pick all = prod::pick(rows, rows, n, blocks, planes, planes, write + read);
+  const double half = time(best), whole = prod::time_of(all, rows, rows, n, blocks, write + read);
+  return half < whole ? Square{best, true, half} : Square{all, false, whole};
 }
 
 struct Plan {
   int planes, low, high, parts;
   // columns to a multiple of 8, what TMA reads of a row; rows at 128 bytes, the boxes' rows (at 16, each would touch two lines)
   int width, pitch, low_width, low_pitch;
-  size_t norms, factors, x[2], s, t, q, sums, bytes;
+  size_t norms, factors, x[2], s, q, sums, bytes;
 };
-// S's K in ranges where its tiles leave SMs idle: k-blocks of a range, by the time of rounds of tiles and 4 us for the join (3892 x 390
-// in fp32: 81 us a step in one range); all of them where that is slower than PICK's tiles with whole K
-int range_of(int rows, int n, int kbs, int planes, Pick pick, bool sym) {
-  const int terms = prod::terms_of(planes, planes).n;
-  const int64_t side = parts_of(rows, prod::BM), tiles = n * side * (side + 1) / 2;
-  double best = sym ? time_sym(pick, rows, n, kbs * terms) : prod::time_of(pick, rows, rows, n, kbs * terms);
-  int range = kbs;
-  for (int splits = 2; splits <= 16 && splits <= kbs; ++splits) {
-    const int each = parts_of(kbs, splits);
-    const double t = (double)parts_of(tiles * parts_of(kbs, each), prod::SMS) * (each * terms * prod::block_time({1, prod::BM}) + 1.) + 4.;
-    if (t < best) {
-      best = t;
-      range = each;
-    }
-  }
-  return range;
-}
-// The tiles and ranges of S, of matrices in `planes`
+// The tiles of S and the k-blocks of a range, of matrices in `planes`, kept in `kept`.  K in ranges where S's tiles leave SMs idle
+// (3892 x 390 in fp32: 81 us a step in one range, 20 in ten and their join)
 struct Gram {
-  Pick pick;
-  bool sym;
+  Square how;
   int range, splits;
 };
-Gram gram_of(int low, int high, int n, int planes) {
-  Gram g;
-  const int kbs = parts_of(high, prod::BK);
-  g.pick = pick_sym(low, n, kbs * prod::terms_of(planes, planes).n, planes, g.sym);
-  g.range = range_of(low, n, kbs, planes, g.pick, g.sym);
-  g.splits = parts_of(kbs, g.range);
-  if (g.splits > 1) g.pick = {1, prod::BM}, g.sym = true;
+Gram gram_of(int low, int high, int n, int planes, int kept) {
+  const int kbs = parts_of(high, prod::BK), terms = prod::terms_of(planes, planes).n;
+  const int64_t side = parts_of(low, prod::BM), tiles = n * side * (side + 1) / 2;
+  Gram g = {pick_sym(low, n, kbs * terms, planes, kept, false), kbs, 1};
+  for (int splits = 2; splits <= 16 && splits <= kbs; ++splits) {
+    const int each = parts_of(kbs, splits), ranges = parts_of(kbs, each);
+    const Pick tile = {1, prod::BM};
+    const double t = prod::time_of_tiles(tile, tiles * ranges, each * terms, 1.5) + 5.;  // (stored as they are; the join)
+    if (t < g.how.time) g = {{tile, true, t}, each, ranges};
+  }
   return g;
 }
 Plan plan(const ra_orthogonalize_args& a) {
@@ -846,10 +846,9 @@ Plan plan(const ra_orthogonalize_args& a) {
   p.factors = take((size_t)a.n_matrices * 4);
   for (size_t& x : p.x) x = take(n * a.rows * p.pitch);
   p.s = take(n * p.low * p.low_pitch);
-  p.t = take(n * p.low * p.low_pitch);
   p.q = take(n * p.low * p.low_pitch);
   int splits = 1;  // (matrices of bf16 are one plane in the first step)
-  for (int planes : {p.planes, p.planes == 3 ? 3 : 1}) splits = std::max(splits, gram_of(p.low, p.high, a.n_matrices, planes).splits);
+  for (int planes : {p.planes, p.planes == 3 ? 3 : 1}) splits = std::max(splits, gram_of(p.low, p.high, a.n_matrices, planes, p.planes).splits);
   p.sums = take(splits > 1 ? (size_t)splits * a.n_matrices * p.low * up(p.low, 32) * 4 : 0);
   p.bytes = at;
   return p;
@@ -863,7 +862,7 @@ cudaError_t run(const ra_orthogonalize_args& a, cudaStream_t st) {
   const bool wide = a.rows <= a.cols;
   float *norms = reinterpret_cast<float*>(ws + p.norms), *factors = reinterpret_cast<float*>(ws + p.factors);
   bf16* x[2] = {reinterpret_cast<bf16*>(ws + p.x[0]), reinterpret_cast<bf16*>(ws + p.x[1])};
-  bf16 *s = reinterpret_cast<bf16*>(ws + p.s), *t = reinterpret_cast<bf16*>(ws + p.t), *q = reinterpret_cast<bf16*>(ws + p.q);
+  bf16 *s = reinterpret_cast<bf16*>(ws + p.s), *q = reinterpret_cast<bf16*>(ws + p.q);
   constexpr int es = sizeof(T), V = 16 / es;
   // bf16 matrices are one plane as they come
   const int first = a.steps == 0 ? 0 : es == 2 ? 1 : 3;
@@ -901,38 +900,39 @@ cudaError_t run(const ra_orthogonalize_args& a, cudaStream_t st) {
     return s.cg == 2 ? prod::launch<S, 2>(s, u, st) : prod::launch<S, 1>(s, u, st);
   };
   OrthArgs square = g;
-  bool sym;
-  const Pick half = pick_sym(p.low, n, parts_of(p.low, prod::BK) * prod::terms_of(p.planes, p.planes).n, p.planes, sym);
-  shape(square, p.low, p.low, p.low, p.planes, p.planes, half, sym);
+  const Square half = pick_sym(p.low, n, parts_of(p.low, prod::BK) * prod::terms_of(p.planes, p.planes).n, p.planes, p.planes, true);
+  shape(square, p.low, p.low, p.low, p.planes, p.planes, half.pick, half.sym);
   square.add = a.a;
-  square.o = q;
+  square.mul = a.c;
+  square.mul_with = a.b;
+  square.with = s;
   square.width = p.low_width;
   square.pitch = p.low_pitch;
+  MAP(square.out, q, DT_BF16, nz, p.low, p.low_width, p.low_pitch, 32, 32);
   MAP(square.a, s, DT_BF16, nz, p.low, p.low_width, p.low_pitch, 64, prod::BM);
-  MAP(square.b, t, DT_BF16, nz, p.low, p.low_width, p.low_pitch, 64, square.shape.bn / square.cg);
+  MAP(square.b, s, DT_BF16, nz, p.low, p.low_width, p.low_pitch, 64, square.shape.bn / square.cg);
   for (int i = 0; i < a.steps; ++i) {
     const int px = i == 0 ? first : p.planes;
     const bf16* from = x[i & 1];
     OrthArgs gram = g, apply = g;
-    const Gram how = gram_of(p.low, p.high, n, px);
-    shape(gram, p.low, p.low, p.high, px, px, how.pick, how.sym);
+    const Gram how = gram_of(p.low, p.high, n, px, p.planes);
+    shape(gram, p.low, p.low, p.high, px, px, how.how.pick, how.how.sym);
     gram.splits = how.splits;
     gram.blocks = how.range;
-    gram.sums = reinterpret_cast<float*>(ws + p.sums);
+    gram.sums = reinterpret_cast<const float*>(ws + p.sums);
     gram.sums_pitch = up(p.low, 32);
+    if (gram.splits > 1) MAP(gram.out, gram.sums, RA_F32, n * gram.splits, p.low, gram.sums_pitch, gram.sums_pitch, 16, 32);
+    else MAP(gram.out, s, DT_BF16, nz, p.low, p.low_width, p.low_pitch, 32, 32);
     gram.a_mn = gram.b_mn = !wide;
     gram.power = px == 1 ? 2 : 0;
     gram.o = s;
-    gram.o2 = t;
-    gram.add2 = a.b;
-    gram.mul2 = a.c;
     gram.width = p.low_width;
     gram.pitch = p.low_pitch;
     const int pa = wide ? p.planes : px, pb = wide ? px : p.planes;
-    shape(apply, a.rows, a.cols, p.low, pa, pb, prod::pick(a.rows, a.cols, n, parts_of(p.low, prod::BK) * prod::terms_of(pa, pb).n, pa, pb), false);
+    shape(apply, a.rows, a.cols, p.low, pa, pb, prod::pick(a.rows, a.cols, n, parts_of(p.low, prod::BK) * prod::terms_of(pa, pb).n, pa, pb, p.planes * plane_time(p.planes)), false);
+    MAP(apply.out, x[(i + 1) & 1], DT_BF16, nz, a.rows, p.width, p.pitch, 32, 32);
     apply.b_mn = wide;
     apply.power = px == 1 ? 1 : 0;
-    apply.o = x[(i + 1) & 1];
     apply.width = p.width;
     apply.pitch = p.pitch;
     if (wide) {

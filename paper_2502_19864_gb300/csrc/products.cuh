@@ -82,24 +82,30 @@ struct Pick {
 constexpr int SMS = 152;  // a plan is the same on every device
 inline int parts_of(int64_t a, int b) { return (int)((a + b - 1) / b); }
 inline int up(int64_t a, int b) { return (int)((a + b - 1) / b * b); }
-// microseconds of a k-block of a tile (measured on long products; the issue of products and copies paces the narrow ones)
-inline double block_time(Pick k) {
-  if (k.cg == 2) return k.bn > 128 ? 0.345 : 0.25;
+// microseconds of a k-block of a tile (measured on long products; the issue of products and copies paces the narrow ones, power the widest:
+// by the share of SMs that have one)
+inline double block_time(Pick k, double share = 1.) {
+  if (k.cg == 2) return k.bn > 128 ? 0.24 + 0.105 * (share < 1. ? share : 1.) : 0.25;
   return k.bn <= 64 ? 0.2 : k.bn <= 128 ? 0.222 : k.bn <= 192 ? 0.31 : 0.365;
 }
-// ... of `batch` products m x n of `blocks` k-blocks, terms counted: rounds of tiles, each with about 1 us for its start and end
-inline double time_of(Pick k, int64_t m, int64_t n, int64_t batch, int blocks) {
-  const int64_t tiles = batch * parts_of(m, BM * k.cg) * parts_of(n, k.bn);
-  return (double)parts_of(tiles, SMS / k.cg) * (blocks * block_time(k) + 1.) + (k.cg == 2 ? 1. : 0.);
+// ... of `tiles` tiles of `blocks` k-blocks, terms counted, in rounds, each with about 1 us for its start and end, and a tile's epilogue,
+// `out` microseconds for 128 columns, beside the next one's products
+inline double time_of_tiles(Pick k, int64_t tiles, int blocks, double out) {
+  const double in = blocks * block_time(k, (double)tiles * k.cg / SMS) + 1., end = out * k.bn / 128.;
+  return in + (parts_of(tiles, SMS / k.cg) - 1) * (in > end ? in : end) + end + (k.cg == 2 ? 1. : 0.);
+}
+// ... of `batch` products m x n
+inline double time_of(Pick k, int64_t m, int64_t n, int64_t batch, int blocks, double out = 0.) {
+  return time_of_tiles(k, batch * parts_of(m, BM * k.cg) * parts_of(n, k.bn), blocks, out);
 }
 // whether a tile's ring has two stages, and TMEM room for two accumulators, of three planes twice
 inline bool takes(Pick k, int pa, int pb) { return stages_of(k.bn, k.cg, pa, pb) >= 2 && (pa < 3 && pb < 3 ? k.bn <= MAX_BN : k.bn <= MAX_BN / 2); }
 // the fastest
-inline Pick pick(int64_t m, int64_t n, int64_t batch, int blocks, int pa, int pb) {
+inline Pick pick(int64_t m, int64_t n, int64_t batch, int blocks, int pa, int pb, double out = 0.) {
   Pick best = {1, n <= 64 ? 64 : 128};
   for (Pick k : {Pick{1, 64}, Pick{1, 256}, Pick{2, 128}, Pick{2, 256}})
     if ((k.cg == 1 || m > BM) && n > k.bn / 2 && takes(k, pa, pb) &&
-        time_of(k, m, n, batch, blocks) < time_of(best, m, n, batch, blocks))
+        time_of(k, m, n, batch, blocks, out) < time_of(best, m, n, batch, blocks, out))
       best = k;
   return best;
 }
@@ -188,25 +194,6 @@ __device__ __forceinline__ void planes_out(bf16* to, int64_t plane, int64_t pitc
     planes_out<PLANES, K + 1>(to, plane, pitch, f, rows, cols, lane);
   }
 }
-// The same, transposed: to the 32 rows `pitch` apart that are the columns, of which rows_left are there; `to` is the first of them at
-// the column that is this lane's row, rounded down to even.  Two lanes' values of a column meet in one word.
-template <int PLANES, typename F>
-__device__ __forceinline__ void planes_mirrored(bf16* to, int64_t plane, F f, int64_t pitch, int rows_left, bool col_ok, int lane) {
-  const bool odd = lane & 1;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    uint32_t w[PLANES];
-    planes_of<PLANES>(f(2 * i), f(2 * i + 1), w);
-    const int j = 2 * i + odd;
-#pragma unroll
-    for (int k = 0; k < PLANES; ++k) {
-      const uint32_t other = __shfl_xor_sync(0xffffffffu, w[k], 1);
-      const uint32_t v = odd ? __byte_perm(other, w[k], 0x7632) : __byte_perm(w[k], other, 0x5410);
-      if (j < rows_left && col_ok) *reinterpret_cast<uint32_t*>(to + k * plane + j * pitch) = v;
-    }
-  }
-}
-
 // What an epilogue warp stores through: boxes of 32 rows x 64 bytes (32 bf16 or 16 fp32 columns), 64-byte swizzled, by TMA
 struct Store {
   uint8_t* staging;
@@ -247,6 +234,39 @@ struct Store {
       *reinterpret_cast<uint4*>(s + lane * 64 + ((q ^ sw) << 4)) = x;
     }
     send(tm, s, col, row, z, false);
+  }
+  // ... its planes, which are z0, z0 + 1, .. of the map.  TURNED: the warp's 32 x 32 transposed, with `row` and `col` as they are then
+  template <int PLANES, bool TURNED, int K = 0, typename F>
+  __device__ __forceinline__ void planes(const CUtensorMap* tm, F f, int col, int row, int z0) {
+    if constexpr (K < PLANES) {
+      uint32_t w[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) w[i] = plane_of<PLANES, K>(f(2 * i), f(2 * i + 1));
+      uint8_t* s = slot();
+      if (TURNED) {  // this lane's values are a column: two bytes of each row
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+          *reinterpret_cast<uint16_t*>(s + j * 64 + ((((lane >> 3) ^ (j >> 1)) & 3) << 4) + (lane & 7) * 2) = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+      } else {
+        const int sw = (lane >> 1) & 3;
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *reinterpret_cast<uint4*>(s + lane * 64 + ((q ^ sw) << 4)) = make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
+      }
+      send(tm, s, col, row, z0 + K, false);
+      planes<PLANES, TURNED, K + 1>(tm, f, col, row, z0);
+    }
+  }
+  // ... not by TMA: g(r, value) for this lane's column of the warp's rows r, so that a row's 32 values leave side by side
+  template <typename G>
+  __device__ __forceinline__ void by_columns(const float (&v)[32], G g) {
+    float* s = reinterpret_cast<float*>(staging);
+#pragma unroll
+    for (int j = 0; j < 32; ++j) s[lane * 32 + (j ^ lane)] = v[j];
+    __syncwarp();
+#pragma unroll 8
+    for (int r = 0; r < 32; ++r) g(r, s[r * 32 + (lane ^ r)]);
+    __syncwarp();
   }
   // ... in fp32, stored or added to what is there; columns from `cols` on are not the map's
   __device__ __forceinline__ void f32_row(const CUtensorMap* tm, const float* v, int col, int row, int z, bool add, int cols) {
@@ -476,18 +496,18 @@ __global__ void __launch_bounds__(THREADS, 1) products_kernel(const __grid_const
         if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
       };
       if constexpr (P::PARTS) {
-        // one accumulator has it all: straight from there, 32 columns at a time
+        // one accumulator has it all: straight from there, 32 columns at a time (the operator's code once: where it runs once or twice
+        // a launch, it takes the time in which its instructions come; 2048 x 2048 in bf16 orthogonalised 475 us unrolled, 428 so)
         if (P::ONE || (w.kb0 < w.kb1 && w.kb0 + chunk >= w.kb1)) {
           if (!mbar_wait_warp(&tfull_bar[acc], acc_phase, &abort_sh, p.err)) break;
           tc_fence_after();
-#pragma unroll
-          for (int i = 0; i < CH; ++i)
-            if (i < t.chunks) {
-              float x[32];
-              __syncwarp();
-              read(i, x);
-              P::part(p, w, t, st, i, x);
-            }
+#pragma unroll 1
+          for (int i = 0; i < t.chunks; ++i) {
+            float x[32];
+            __syncwarp();
+            read(i, x);
+            P::part(p, w, t, st, i, x);
+          }
           release();
           continue;
         }
