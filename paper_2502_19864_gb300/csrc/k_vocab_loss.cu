@@ -210,8 +210,6 @@ struct VocabArgs {
   const float *scale, *lse, *ref;
   float2* stats;
   float* zlab;
-  bf16* dzp;                    // fp32: dz's planes
-  int dz_pitch;
   int tokens, hidden, rows, planes;
   int v0, width;                // the piece: words v0 .. v0 + width
   int wrow;                     // where it begins in the map of W
@@ -273,7 +271,7 @@ struct Logits {
     }
     auto at = [&](int j) { return v[j]; };
     if (PLANES == 1) st.bf16_row(&p.dz, at, w.n0 + c, row0, 0);
-    else prod::planes_out<3>(p.dzp + (int64_t)row0 * p.dz_pitch + w.n0 + c, (int64_t)p.rows * p.dz_pitch, p.dz_pitch, at, 32, 32, t.lane);
+    else st.planes<3, false>(&p.dz, at, w.n0 + c, row0, 0);
   }
   template <int CH>
   static __device__ __forceinline__ void finish(const Args& p, const Unit& w, const Tile& t, Store& st, float (&v)[CH][32]) {
@@ -828,8 +826,6 @@ VocabArgs args_of(const ra_vocab_loss_args& a, const Plan& p, char* ws) {
   g.ref = r.ref;
   g.stats = reinterpret_cast<float2*>(ws + p.st);
   g.zlab = reinterpret_cast<float*>(ws + p.zlab);
-  g.dzp = reinterpret_cast<bf16*>(ws + p.dz);
-  g.dz_pitch = p.width;
   g.tokens = a.tokens;
   g.hidden = a.hidden;
   g.rows = p.rows;

@@ -175,25 +175,6 @@ __device__ __forceinline__ uint32_t plane_of(float x, float y) {
   planes_of<PLANES>(x, y, w);
   return w[K];
 }
-// Plane K, and those after it, of a warp's 32 rows of 32 columns, a lane having f(0), f(1), .. of its row: `to` is the first
-// row's place in plane 0, rows are `pitch` and planes `plane` values apart; `rows` and `cols` (a multiple of 8) of them are there.
-// Four lanes exchange 16-byte pieces, so that a store fills 64 bytes of each of eight rows (a row a lane touches 32 lines an
-// instruction: 13 us of a launch of 98 tiles of 128 x 128 in two times three planes)
-template <int PLANES, int K = 0, typename F>
-__device__ __forceinline__ void planes_out(bf16* to, int64_t plane, int64_t pitch, F f, int rows, int cols, int lane) {
-  if constexpr (K < PLANES) {
-    uint32_t w[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) w[i] = plane_of<PLANES, K>(f(2 * i), f(2 * i + 1));
-    transpose4(w, lane);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = (lane & ~3) + i, c = 8 * (lane & 3);
-      if (r < rows && c < cols) *reinterpret_cast<uint4*>(to + K * plane + r * pitch + c) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
-    }
-    planes_out<PLANES, K + 1>(to, plane, pitch, f, rows, cols, lane);
-  }
-}
 // What an epilogue warp stores through: boxes of 32 rows x 64 bytes (32 bf16 or 16 fp32 columns), 64-byte swizzled, by TMA
 struct Store {
   uint8_t* staging;
@@ -235,7 +216,8 @@ struct Store {
     }
     send(tm, s, col, row, z, false);
   }
-  // ... its planes, which are z0, z0 + 1, .. of the map.  TURNED: the warp's 32 x 32 transposed, with `row` and `col` as they are then
+  // ... its planes, which are z0, z0 + 1, .. of the map (straight from registers, 64 bytes of eight rows a store, 2 x 777 x 1000 in fp32
+  // orthogonalised takes 370 us, so 352).  TURNED: the warp's 32 x 32 transposed, with `row` and `col` as they are then
   template <int PLANES, bool TURNED, int K = 0, typename F>
   __device__ __forceinline__ void planes(const CUtensorMap* tm, F f, int col, int row, int z0) {
     if constexpr (K < PLANES) {
