@@ -10,7 +10,7 @@
 // worst, where one plane's 2^-9 would be as large as what is computed.
 //
 // Bound: the products, 1.5 low^2 high + low^3 / 2 multiply-adds a step with the symmetric ones' halves, three (six) times over for
-// the planes; of small matrices the launches.  2048 x 5632 in bf16 0.87 ms for five steps, 2 x 777 x 1000 in fp32 0.37 ms.
+// the planes; of small matrices the launches.  2048 x 5632 in bf16 0.80 ms for five steps, 2 x 777 x 1000 in fp32 0.31 ms.
 #include <algorithm>
 
 #include "common.cuh"
@@ -190,7 +190,7 @@ struct OrthArgs {
   int k, n, cg, dtype;
   bool a_mn, b_mn, sym, last, map_out;
   float add, mul, mul_with;
-  // S of few tiles and a long K: K in `splits` ranges of `blocks` k-blocks, whose sums go to sums [splits][n][rows][sums_pitch]
+  // a symmetric product of few tiles: K in `splits` ranges of `blocks` k-blocks, whose sums go to sums [splits][n][rows][sums_pitch]
   int splits, blocks, sums_pitch;
   const float* sums;
 };
@@ -312,7 +312,7 @@ struct Step {
   }
 };
 
-// S from the ranges' sums, in order: a CTA a 32 x 32 block on or above the diagonal, and its mirror image
+// The symmetric product from the ranges' sums, in order: a CTA a 32 x 32 block on or above the diagonal, and its mirror image
 template <int PLANES>
 __global__ void __launch_bounds__(256) orth_join_kernel(const OrthArgs p) {
   __shared__ float tile[32][33];
@@ -325,10 +325,23 @@ __global__ void __launch_bounds__(256) orth_join_kernel(const OrthArgs p) {
   const int64_t plane = (int64_t)p.rows * p.pitch, range = (int64_t)p.n * p.rows * p.sums_pitch;
   auto put = [&](const float* v, int row, int col) {
     if (row >= p.rows || col >= p.width) return;
+    const int64_t at = (int64_t)z * PLANES * plane + (int64_t)row * p.pitch + col;
+    float x[4] = {v[0], v[1], v[2], v[3]};
+    if (p.with) {
+      float w[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = PLANES - 1; k >= 0; --k) {
+        const uint2 h = *reinterpret_cast<const uint2*>(p.with + at + k * plane);
+        w[0] += __uint_as_float(h.x << 16), w[1] += __uint_as_float(h.x & 0xffff0000u);
+        w[2] += __uint_as_float(h.y << 16), w[3] += __uint_as_float(h.y & 0xffff0000u);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = fmaf(p.mul, x[j], fmaf(p.mul_with, w[j], row == col + j ? p.add : 0.f));
+    }
     uint32_t lo[PLANES], hi[PLANES];
-    prod::planes_of<PLANES>(v[0], v[1], lo);
-    prod::planes_of<PLANES>(v[2], v[3], hi);
-    bf16* to = p.o + (int64_t)z * PLANES * plane + (int64_t)row * p.pitch + col;
+    prod::planes_of<PLANES>(x[0], x[1], lo);
+    prod::planes_of<PLANES>(x[2], x[3], hi);
+    bf16* to = p.o + at;
 #pragma unroll
     for (int k = 0; k < PLANES; ++k) *reinterpret_cast<uint2*>(to + k * plane) = make_uint2(lo[k], hi[k]);
   };
@@ -779,8 +792,8 @@ cudaError_t run_small(const ra_orthogonalize_args& a, cudaStream_t st) {
   return cudaLaunchKernelEx(&cfg, k, p);
 }
 
-// What an epilogue takes for 128 x 128, in microseconds a plane of it, of two or three: stored (with its mirror image twice that), read as much
-constexpr double plane_time(int kept) { return kept == 2 ? 0.8 : 1.9; }
+// What an epilogue takes for 128 x 128, in microseconds a plane of it, of two or three: stored (with its mirror image twice that), read as much (of the part of a tile that is there)
+constexpr double plane_time(int kept) { return kept == 2 ? 0.8 : 1.5; }
 // A symmetric product: all tiles, or (sym) square ones on and above the diagonal, which takes rounds off and costs the
 // mirrored stores: 2048 x 2048 of K = 5632 in two planes 98 -> 73 us, two of 777 x 777 in three planes 49 -> 60.  `reads`: planes are read too
 double time_sym(Pick k, int rows, int n, int blocks, double out) {
@@ -793,7 +806,7 @@ struct Square {
   double time;
 };
 Square pick_sym(int rows, int n, int blocks, int planes, int kept, bool reads) {
-  const double write = kept * plane_time(kept), read = reads ? write : 0.;
+  const double part = (double)rows / up(rows, prod::BM), write = kept * plane_time(kept) * part * part, read = reads ? write : 0.;
   auto time = [&](Pick k) { return time_sym(k, rows, n, blocks, write) + read * k.bn / 128.; };
   const Pick one = {1, 128}, two = {2, 256}, best = rows > 128 && prod::takes(two, planes, planes) && time(two) < time(one) ? two : one;
   const Pick all = prod::pick(rows, rows, n, blocks, planes, planes, write + read);
@@ -807,20 +820,20 @@ struct Plan {
   int width, pitch, low_width, low_pitch;
   size_t norms, factors, x[2], s, q, sums, bytes;
 };
-// The tiles of S and the k-blocks of a range, of matrices in `planes`, kept in `kept`.  K in ranges where S's tiles leave SMs idle
-// (3892 x 390 in fp32: 81 us a step in one range, 20 in ten and their join)
-struct Gram {
+// The tiles of a symmetric product and the k-blocks of a range, of operands in `planes`, kept in `kept`.  K in ranges where its tiles
+// leave SMs idle (S of 3892 x 390 in fp32: 81 us a step in one range, 20 in ten and their join)
+struct Ranges {
   Square how;
   int range, splits;
 };
-Gram gram_of(int low, int high, int n, int planes, int kept) {
-  const int kbs = parts_of(high, prod::BK), terms = prod::terms_of(planes, planes).n;
-  const int64_t side = parts_of(low, prod::BM), tiles = n * side * (side + 1) / 2;
-  Gram g = {pick_sym(low, n, kbs * terms, planes, kept, false), kbs, 1};
+Ranges ranges_of(int rows, int k, int n, int planes, int kept, bool reads) {
+  const int kbs = parts_of(k, prod::BK), terms = prod::terms_of(planes, planes).n;
+  const int64_t side = parts_of(rows, prod::BM), tiles = n * side * (side + 1) / 2;
+  Ranges g = {pick_sym(rows, n, kbs * terms, planes, kept, reads), kbs, 1};
   for (int splits = 2; splits <= 16 && splits <= kbs; ++splits) {
     const int each = parts_of(kbs, splits), ranges = parts_of(kbs, each);
     const Pick tile = {1, prod::BM};
-    const double t = prod::time_of_tiles(tile, tiles * ranges, each * terms, 1.5) + 5.;  // (stored as they are; the join)
+    const double t = prod::time_of_tiles(tile, tiles * ranges, each * terms, 1.5) + (reads ? 8. : 6.);  // (stored as they are; the join)
     if (t < g.how.time) g = {{tile, true, t}, each, ranges};
   }
   return g;
@@ -847,8 +860,8 @@ Plan plan(const ra_orthogonalize_args& a) {
   for (size_t& x : p.x) x = take(n * a.rows * p.pitch);
   p.s = take(n * p.low * p.low_pitch);
   p.q = take(n * p.low * p.low_pitch);
-  int splits = 1;  // (matrices of bf16 are one plane in the first step)
-  for (int planes : {p.planes, p.planes == 3 ? 3 : 1}) splits = std::max(splits, gram_of(p.low, p.high, a.n_matrices, planes, p.planes).splits);
+  int splits = ranges_of(p.low, p.low, a.n_matrices, p.planes, p.planes, true).splits;  // Q's; S's (matrices of bf16 are one plane in the first step)
+  for (int planes : {p.planes, p.planes == 3 ? 3 : 1}) splits = std::max(splits, ranges_of(p.low, p.high, a.n_matrices, planes, p.planes, false).splits);
   p.sums = take(splits > 1 ? (size_t)splits * a.n_matrices * p.low * up(p.low, 32) * 4 : 0);
   p.bytes = at;
   return p;
@@ -900,34 +913,41 @@ cudaError_t run(const ra_orthogonalize_args& a, cudaStream_t st) {
     return s.cg == 2 ? prod::launch<S, 2>(s, u, st) : prod::launch<S, 1>(s, u, st);
   };
   OrthArgs square = g;
-  const Square half = pick_sym(p.low, n, parts_of(p.low, prod::BK) * prod::terms_of(p.planes, p.planes).n, p.planes, p.planes, true);
-  shape(square, p.low, p.low, p.low, p.planes, p.planes, half.pick, half.sym);
+  // a symmetric product into `to`
+  auto symmetric = [&](OrthArgs& s, int k, int planes, bf16* to, bool reads) {
+    const Ranges r = ranges_of(p.low, k, n, planes, p.planes, reads);
+    shape(s, p.low, p.low, k, planes, planes, r.how.pick, r.how.sym);
+    s.splits = r.splits;
+    s.blocks = r.range;
+    s.sums = reinterpret_cast<const float*>(ws + p.sums);
+    s.sums_pitch = up(p.low, 32);
+    s.o = to;
+    s.width = p.low_width;
+    s.pitch = p.low_pitch;
+    if (s.splits > 1) MAP(s.out, s.sums, RA_F32, n * s.splits, p.low, s.sums_pitch, s.sums_pitch, 16, 32);
+    else MAP(s.out, to, DT_BF16, nz, p.low, p.low_width, p.low_pitch, 32, 32);
+    return cudaSuccess;
+  };
+  auto join = [&](const OrthArgs& s) {
+    if (s.splits == 1) return cudaSuccess;
+    const int side = parts_of(p.low, 32);
+    note_launch(1);
+    return launch_pdl(orth_join_kernel<PL>, dim3(side * (side + 1) / 2, n), dim3(256), 0, st, s);
+  };
+  DO(symmetric(square, p.low, p.planes, q, true));
   square.add = a.a;
   square.mul = a.c;
   square.mul_with = a.b;
   square.with = s;
-  square.width = p.low_width;
-  square.pitch = p.low_pitch;
-  MAP(square.out, q, DT_BF16, nz, p.low, p.low_width, p.low_pitch, 32, 32);
   MAP(square.a, s, DT_BF16, nz, p.low, p.low_width, p.low_pitch, 64, prod::BM);
   MAP(square.b, s, DT_BF16, nz, p.low, p.low_width, p.low_pitch, 64, square.shape.bn / square.cg);
   for (int i = 0; i < a.steps; ++i) {
     const int px = i == 0 ? first : p.planes;
     const bf16* from = x[i & 1];
     OrthArgs gram = g, apply = g;
-    const Gram how = gram_of(p.low, p.high, n, px, p.planes);
-    shape(gram, p.low, p.low, p.high, px, px, how.how.pick, how.how.sym);
-    gram.splits = how.splits;
-    gram.blocks = how.range;
-    gram.sums = reinterpret_cast<const float*>(ws + p.sums);
-    gram.sums_pitch = up(p.low, 32);
-    if (gram.splits > 1) MAP(gram.out, gram.sums, RA_F32, n * gram.splits, p.low, gram.sums_pitch, gram.sums_pitch, 16, 32);
-    else MAP(gram.out, s, DT_BF16, nz, p.low, p.low_width, p.low_pitch, 32, 32);
+    DO(symmetric(gram, p.high, px, s, false));
     gram.a_mn = gram.b_mn = !wide;
     gram.power = px == 1 ? 2 : 0;
-    gram.o = s;
-    gram.width = p.low_width;
-    gram.pitch = p.low_pitch;
     const int pa = wide ? p.planes : px, pb = wide ? px : p.planes;
     shape(apply, a.rows, a.cols, p.low, pa, pb, prod::pick(a.rows, a.cols, n, parts_of(p.low, prod::BK) * prod::terms_of(pa, pb).n, pa, pb, p.planes * plane_time(p.planes)), false);
     MAP(apply.out, x[(i + 1) & 1], DT_BF16, nz, a.rows, p.width, p.pitch, 32, 32);
@@ -957,12 +977,9 @@ cudaError_t run(const ra_orthogonalize_args& a, cudaStream_t st) {
     }
     using Full = Step<PL, PL, PL>;
     DO(px == PL ? go(gram, Full()) : go(gram, Step<PL, ONE, ONE>()));
-    if (gram.splits > 1) {
-      const int side = parts_of(p.low, 32);
-      note_launch(1);
-      DO(launch_pdl(orth_join_kernel<PL>, dim3(side * (side + 1) / 2, n), dim3(256), 0, st, gram));
-    }
+    DO(join(gram));
     DO(go(square, Full()));
+    DO(join(square));
     DO(px == PL ? go(apply, Full()) : wide ? go(apply, Step<PL, PL, ONE>()) : go(apply, Step<PL, ONE, PL>()));
   }
   return cudaSuccess;
