@@ -286,3 +286,33 @@ def test_a_captured_step_and_two_streams():
     for q, w in zip((s, t), want):
         for n in w:
             assert torch.equal(q[n], w[n]), n
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hidden", [40, 77, 250])
+def test_many_short_rows_some_outputs_and_in_place(hidden, dtype):
+    """Rows of a warp each, eight warps a CTA: any of the outputs may be left out, and dx may take dy's place.  (Without dx a CTA reads
+    fewer inputs and more CTAs have room, which add up the weights' sums in another order: within the bounds, not bit for bit.)"""
+    a, s = make(5003, hidden, "layer", dtype, "f32", True)
+    R.ra_norm_forward(a)
+    R.ra_norm_backward(a)
+    torch.cuda.synchronize()
+    check(a, s, "layer", dtype, "f32", True)
+    names = ("dx", "dgamma", "dbeta")
+    want = {n: s[n].clone() for n in names}
+    for left in names:
+        for n in names:
+            s[n].fill_(7.0)
+        kept = getattr(a, left + "_dev")
+        setattr(a, left + "_dev", None)
+        R.ra_norm_backward(a)
+        setattr(a, left + "_dev", kept)
+        assert bool((s[left] == 7.0).all()), left
+        for n in names:
+            assert n == left or left == "dx" or torch.equal(s[n], want[n]), (left, n)
+        s[left].copy_(want[left])
+        check(a, s, "layer", dtype, "f32", True)
+    dy = s["dy"].clone()
+    a.dx_dev = a.dy_dev
+    R.ra_norm_backward(a)
+    assert torch.equal(s["dy"], want["dx"]) and torch.equal(s["dbeta"], want["dbeta"]) and not torch.equal(s["dy"], dy)

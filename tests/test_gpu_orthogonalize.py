@@ -237,3 +237,15 @@ def test_a_workspace_of_anything_behind_its_zeros():
     torch.cuda.synchronize()
     check(s, "bf16")
     assert bool((s["workspace"][:16384] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_ranges_keep_matrices_apart(dtype):
+    a, s = make(3, 70, 4001, dtype)
+    R.ra_orthogonalize(a)
+    want = s["out"].clone()
+    s["x"][1, 69, 4000] = float("nan")
+    s["out"].fill_(7.0)
+    R.ra_orthogonalize(a)
+    torch.cuda.synchronize()
+    assert torch.equal(s["out"][0], want[0]) and torch.equal(s["out"][2], want[2]) and bool(s["out"][1].isnan().all())
