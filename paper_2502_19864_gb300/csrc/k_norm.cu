@@ -7,10 +7,12 @@
 // dgamma = sum dy u, dbeta = sum dy, which each CTA keeps in registers over its rows; the CTAs' partial sums are added in
 // a second kernel, in a fixed order.
 //
-// Bound: bytes.  A row is read once, held in registers through the reductions and written once.  A CTA's threads share a
-// row (up to 256 values: a warp's), eight (16, 32) values each, and take ROWS rows at a time, so that enough loads are on their way and a barrier
-// serves them all; two values an instruction, as the instructions' issue is the next bound (28 a value without: 165 us, with 137).
-// Forward and backward of 65536 x 1024 in bf16 take 137 us (4.9 TB/s), of 8192 x 2048 with its residual 52 us (5.2 TB/s).
+// Bound: bytes.  A row is read once, held in registers through the reductions and written once.  A CTA's threads share a row (one
+// of up to 256 values: a warp's, eight warps a CTA), eight (16, 32) values each, and take ROWS rows at a time, so that enough
+// loads are on their way and a barrier serves them all; two values an instruction, as the instructions' issue is the next bound (28
+// a value without: 165 us, with 137).
+// Forward and backward of 65536 x 1024 in bf16 take 137 us (4.9 TB/s), of 8192 x 2048 with its residual 52 us (5.2 TB/s), of
+// 16271 x 1334, in pieces of 4 bytes, 135 us (2.5 TB/s).
 #include <algorithm>
 
 #include "common.cuh"

@@ -275,8 +275,10 @@ struct Tile {
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* tm) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(tm)) : "memory");
 }
-// P: the operands' planes PA and PB, Args (with `Shape shape`, `unsigned* err`), static void prefetch(const Args&) (of the operands' maps), static int count(const Args&), static void unit(const Args&, int, Unit&) and
-// PARTS (ONE: a unit has k-blocks, and one accumulator takes them all) and static void part(const Args&, const Unit&, const Tile&, Store&, int i, float (&v)[32]) for this warp's i-th 32 columns, or
+// P: the operands' planes PA and PB, Args (with `Shape shape`, `unsigned* err`), static void prefetch(const Args&) (of the operands'
+// maps), static int count(const Args&), static void unit(const Args&, int, Unit&) and
+// PARTS (ONE: a unit has k-blocks, and one accumulator takes them all) and static void part(const Args&, const Unit&, const Tile&,
+// Store&, int i, float (&v)[32]) for this warp's i-th 32 columns, or
 // static void finish(const Args&, const Unit&, const Tile&, Store&, float (&v)[CH][32]) for all of them.
 template <class P, int CG>
 __global__ void __launch_bounds__(THREADS, 1) products_kernel(const __grid_constant__ typename P::Args p) {
