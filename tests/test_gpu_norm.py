@@ -316,3 +316,39 @@ def test_many_short_rows_some_outputs_and_in_place(hidden, dtype):
     a.dx_dev = a.dy_dev
     R.ra_norm_backward(a)
     assert torch.equal(s["dy"], want["dx"]) and torch.equal(s["dbeta"], want["dbeta"]) and not torch.equal(s["dy"], dy)
+
+
+@pytest.mark.parametrize("dtype,wdtype", [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("kind,residual", [("layer", False), ("layer", True), ("rms", True)])
+@pytest.mark.parametrize("rows,hidden", [(2501, 264), (2433, 520), (5003, 1024), (2501, 2048), (2501, 2056), (2501, 4096), (2433, 8192)])
+def test_many_rows_of_several_warps(rows, hidden, kind, residual, dtype, wdtype):
+    """Rows in 16-byte pieces, several at a time through the ring, whose sums meet at barriers: from 2432 on."""
+    a, s = make(rows, hidden, kind, dtype, wdtype, residual, seed=rows + hidden)
+    s["workspace"][16384:] = 255
+    R.ra_norm_forward(a)
+    R.ra_norm_backward(a)
+    torch.cuda.synchronize()
+    check(a, s, kind, dtype, wdtype, residual)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hidden", [1024, 2304, 2302])
+def test_many_rows_of_several_warps_in_place(hidden, dtype):
+    a, s = make(2501, hidden, "layer", dtype, "f32", True)
+    b, t = make(2501, hidden, "layer", dtype, "f32", True)
+    R.ra_norm_forward(a)
+    R.ra_norm_backward(a)
+    b.sum_dev, t["sum"] = b.residual_dev, t["residual"]
+    b.y_dev, t["y"] = b.x_dev, t["x"]
+    R.ra_norm_forward(b)
+    for place in ("dsum", "dy"):
+        kept = t[place].clone()
+        b.dx_dev = t[place].data_ptr()
+        for n in ("dgamma", "dbeta"):
+            t[n].fill_(7.0)
+        R.ra_norm_backward(b)
+        torch.cuda.synchronize()
+        for n in ("y", "sum", "dgamma", "dbeta"):
+            assert torch.equal(s[n], t[n]), n
+        assert torch.equal(s["dx"], t[place]), place
+        t[place].copy_(kept)
