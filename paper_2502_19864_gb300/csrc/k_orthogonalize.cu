@@ -838,6 +838,10 @@ Ranges ranges_of(int rows, int k, int n, int planes, int kept, bool reads) {
   }
   return g;
 }
+// The planes of the matrices in a step, as they come (bf16 ones are one plane) or as they are kept
+int planes_in(const Plan& p, bool first) { return first && p.planes == 2 ? 1 : p.planes; }
+Ranges gram_of(const ra_orthogonalize_args& a, const Plan& p, bool first) { return ranges_of(p.low, p.high, a.n_matrices, planes_in(p, first), p.planes, false); }
+Ranges square_of(const ra_orthogonalize_args& a, const Plan& p) { return ranges_of(p.low, p.low, a.n_matrices, p.planes, p.planes, true); }
 Plan plan(const ra_orthogonalize_args& a) {
   Plan p = {};
   p.planes = a.dtype == RA_F32 ? 3 : 2;
@@ -860,11 +864,16 @@ Plan plan(const ra_orthogonalize_args& a) {
   for (size_t& x : p.x) x = take(n * a.rows * p.pitch);
   p.s = take(n * p.low * p.low_pitch);
   p.q = take(n * p.low * p.low_pitch);
-  int splits = ranges_of(p.low, p.low, a.n_matrices, p.planes, p.planes, true).splits;  // Q's; S's (matrices of bf16 are one plane in the first step)
-  for (int planes : {p.planes, p.planes == 3 ? 3 : 1}) splits = std::max(splits, ranges_of(p.low, p.high, a.n_matrices, planes, p.planes, false).splits);
+  int splits = square_of(a, p).splits;
+  for (bool first : {true, false}) splits = std::max(splits, gram_of(a, p, first).splits);
   p.sums = take(splits > 1 ? (size_t)splits * a.n_matrices * p.low * up(p.low, 32) * 4 : 0);
   p.bytes = at;
   return p;
+}
+
+Pick apply_of(const ra_orthogonalize_args& a, const Plan& p, bool first) {
+  const int px = planes_in(p, first), pa = a.rows <= a.cols ? p.planes : px, pb = a.rows <= a.cols ? px : p.planes;
+  return prod::pick(a.rows, a.cols, a.n_matrices, parts_of(p.low, prod::BK) * prod::terms_of(pa, pb).n, pa, pb, p.planes * plane_time(p.planes));
 }
 
 template <typename T>
@@ -914,8 +923,7 @@ cudaError_t run(const ra_orthogonalize_args& a, cudaStream_t st) {
   };
   OrthArgs square = g;
   // a symmetric product into `to`
-  auto symmetric = [&](OrthArgs& s, int k, int planes, bf16* to, bool reads) {
-    const Ranges r = ranges_of(p.low, k, n, planes, p.planes, reads);
+  auto symmetric = [&](OrthArgs& s, int k, int planes, bf16* to, const Ranges& r) {
     shape(s, p.low, p.low, k, planes, planes, r.how.pick, r.how.sym);
     s.splits = r.splits;
     s.blocks = r.range;
@@ -934,7 +942,7 @@ cudaError_t run(const ra_orthogonalize_args& a, cudaStream_t st) {
     note_launch(1);
     return launch_pdl(orth_join_kernel<PL>, dim3(side * (side + 1) / 2, n), dim3(256), 0, st, s);
   };
-  DO(symmetric(square, p.low, p.planes, q, true));
+  DO(symmetric(square, p.low, p.planes, q, square_of(a, p)));
   square.add = a.a;
   square.mul = a.c;
   square.mul_with = a.b;
@@ -945,11 +953,11 @@ cudaError_t run(const ra_orthogonalize_args& a, cudaStream_t st) {
     const int px = i == 0 ? first : p.planes;
     const bf16* from = x[i & 1];
     OrthArgs gram = g, apply = g;
-    DO(symmetric(gram, p.high, px, s, false));
+    DO(symmetric(gram, p.high, px, s, gram_of(a, p, i == 0)));
     gram.a_mn = gram.b_mn = !wide;
     gram.power = px == 1 ? 2 : 0;
     const int pa = wide ? p.planes : px, pb = wide ? px : p.planes;
-    shape(apply, a.rows, a.cols, p.low, pa, pb, prod::pick(a.rows, a.cols, n, parts_of(p.low, prod::BK) * prod::terms_of(pa, pb).n, pa, pb, p.planes * plane_time(p.planes)), false);
+    shape(apply, a.rows, a.cols, p.low, pa, pb, apply_of(a, p, i == 0), false);
     MAP(apply.out, x[(i + 1) & 1], DT_BF16, nz, a.rows, p.width, p.pitch, 32, 32);
     apply.b_mn = wide;
     apply.power = px == 1 ? 1 : 0;
@@ -987,6 +995,17 @@ cudaError_t run(const ra_orthogonalize_args& a, cudaStream_t st) {
 
 }  // namespace
 
+void orthogonalize_plan(const ra_orthogonalize_args& a, int32_t (&out)[17]) {
+  const Plan p = plan(a);
+  const Ranges s0 = gram_of(a, p, true), s = gram_of(a, p, false), q = square_of(a, p);
+  const Pick x0 = apply_of(a, p, true), x = apply_of(a, p, false);
+  int32_t* at = out;
+  *at++ = small_fits(a);
+  for (const Ranges* r : {&s0, &s, &q})
+    for (int v : {r->how.pick.cg, r->how.pick.bn, (int)r->how.sym, r->splits}) *at++ = v;
+  for (const Pick* k : {&x0, &x})
+    for (int v : {k->cg, k->bn}) *at++ = v;
+}
 size_t orthogonalize_workspace(const ra_orthogonalize_args& a) { return small_fits(a) ? WS_ZERO : plan(a).bytes; }
 cudaError_t orthogonalize(const ra_orthogonalize_args& a, cudaStream_t st) {
   if (small_fits(a)) return a.dtype == RA_BF16 ? run_small<bf16, 2>(a, st) : run_small<float, 3>(a, st);

@@ -1029,6 +1029,13 @@ cudaError_t few_any(const ra_vocab_loss_args& a, bool backward, cudaStream_t st)
 
 }  // namespace
 
+void vocab_loss_plan(const ra_vocab_loss_args& a, int32_t (&out)[12]) {
+  const Plan p = plan(a);
+  int32_t* at = out;
+  for (int v : {(int)few(a), p.planes, p.pieces, p.width, p.forward.cg, p.forward.bn, p.logits.cg, p.logits.bn, p.grads.cg, p.grads.bn, p.splits_x,
+                p.splits_w})
+    *at++ = v;
+}
 size_t vocab_loss_workspace(const ra_vocab_loss_args& a) { return few(a) ? few_plan(a).bytes : plan(a).bytes; }
 cudaError_t vocab_loss_fwd(const ra_vocab_loss_args& a, cudaStream_t st) {
   if (few(a)) return few_any(a, false, st);

@@ -43,4 +43,12 @@ cudaError_t vocab_loss_bwd(const ra_vocab_loss_args& a, cudaStream_t st);
 size_t orthogonalize_workspace(const ra_orthogonalize_args& a);
 cudaError_t orthogonalize(const ra_orthogonalize_args& a, cudaStream_t st);
 
+// What the launchers choose for a block's sizes, for tests that ask which form a size runs:
+//   loss: few fp32 tokens; planes; pieces of the vocabulary, words of one; CTAs and columns of a tile of the forward's logits, the
+//   backward's, the gradients; ranges of K of dx and of dW
+//   orthogonalisation: smaller side up to 64; CTAs, columns, halves and ranges of S in the first step and in the others, and of Q; CTAs
+//   and columns of X in the first step and in the others
+void vocab_loss_plan(const ra_vocab_loss_args& a, int32_t (&out)[12]);
+void orthogonalize_plan(const ra_orthogonalize_args& a, int32_t (&out)[17]);
+
 }  // namespace ra

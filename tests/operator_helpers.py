@@ -9,6 +9,7 @@ n products, off by n u more.  With A = sum_j p_j |v_j| the bound of an fp32 outp
   A bf16 kernel that rounds its weights to bf16 before the product with v adds e A, and e |o| for its output.
   The decode kernel's weights enter the product in two bf16 terms, off by e^2: the output's rounding is left, and
   e |o| <= e / 2 (A + |o|), as |o| <= A."""
+import ctypes as C
 import math
 
 import torch
@@ -63,3 +64,21 @@ def slots(pages, table, b, n):
 
 def workspace(n, device="cuda"):
     return torch.zeros(max(n, 256), dtype=torch.uint8, device=device)
+
+
+# ---- which form a size runs -----------------------------------------------------------------
+
+def vocab_loss_plan(a):
+    """{name: number} of the form that a vocabulary loss's block takes: its pieces, and the tiles as (CTAs, columns)."""
+    v = (C.c_int32 * 12)()
+    assert R.lib().ra_internal_vocab_loss_plan(C.byref(a), v) == 0
+    few, planes, pieces, width, *t, splits_x, splits_w = v
+    return {"few": few, "planes": planes, "pieces": pieces, "width": width, "forward": tuple(t[:2]), "logits": tuple(t[2:4]),
+            "grads": tuple(t[4:]), "splits_x": splits_x, "splits_w": splits_w}
+
+
+def orthogonalize_plan(a):
+    """{product: (CTAs, columns, halves, ranges)} of an orthogonalisation, S and X in the first step with a 0."""
+    v = (C.c_int32 * 17)()
+    assert R.lib().ra_internal_orthogonalize_plan(C.byref(a), v) == 0
+    return {"small": v[0], "S0": tuple(v[1:5]), "S": tuple(v[5:9]), "Q": tuple(v[9:13]), "X0": tuple(v[13:15]), "X": tuple(v[15:17])}

@@ -11,7 +11,7 @@ import pytest
 import torch
 
 from paper_2502_19864_gb300 import ringada as R
-from tests.operator_helpers import DT, E, RA, U, workspace
+from tests.operator_helpers import DT, E, RA, U, orthogonalize_plan, workspace
 
 pytestmark = pytest.mark.gpu
 COEF = (3.4445, -4.775, 2.0315)
@@ -249,3 +249,57 @@ def test_ranges_keep_matrices_apart(dtype):
     R.ra_orthogonalize(a)
     torch.cuda.synchronize()
     assert torch.equal(s["out"][0], want[0]) and torch.equal(s["out"][2], want[2]) and bool(s["out"][1].isnan().all())
+
+
+# Sizes and the forms that they run, as orthogonalize_plan has them ("ranges": more than one): tiles' CTAs and columns, and for S and Q
+# whether half of the tiles is computed and mirrored.  Between them all the forms of S, Q and X in both directions.
+FORMS = [
+    ("bf16", 40, 141, 135, {"S0": (1, 128, 1, 1), "S": (1, 128, 1, 1), "Q": (1, 128, 1, 1)}),
+    ("bf16", 40, 138, 143, {"S0": (1, 128, 1, 1), "S": (1, 128, 1, 1), "Q": (1, 128, 1, 1)}),
+    ("bf16", 16, 280, 259, {"S0": (1, 128, 0, 1), "S": (1, 128, 0, 1), "Q": (1, 128, 0, 1)}),
+    ("bf16", 16, 266, 282, {"S0": (1, 128, 0, 1), "S": (1, 128, 0, 1), "Q": (1, 128, 0, 1)}),
+    ("bf16", 16, 405, 391, {"S0": (1, 256, 0, 1), "S": (1, 256, 0, 1), "Q": (1, 256, 0, 1)}),
+    ("bf16", 16, 385, 386, {"S0": (1, 256, 0, 1), "S": (1, 256, 0, 1), "Q": (1, 256, 0, 1)}),
+    ("bf16", 16, 388, 1765, {"S0": (2, 256, 0, 1), "S": (2, 256, 1, 1)}),
+    ("bf16", 16, 1736, 405, {"S0": (2, 256, 0, 1), "X": (2, 256)}),
+    ("bf16", 16, 2103, 392, {"S": (2, 256, 1, 1), "X": (2, 256)}),
+    ("bf16", 3, 1214, 1203, {"Q": (2, 256, 0, 1)}),
+    ("bf16", 4, 1405, 1040, {"S0": (2, 256, 1, 1), "S": (2, 256, 1, 1), "Q": (2, 256, 1, 1)}),
+    ("bf16", 4, 1057, 1490, {"S0": (2, 256, 1, 1), "S": (2, 256, 1, 1), "Q": (2, 256, 1, 1)}),
+    ("bf16", 1, 1038, 1028, {"Q": (1, 128, 1, "ranges")}),
+    ("bf16", 1, 1026, 1087, {"Q": (1, 128, 1, "ranges")}),
+    ("bf16", 1, 2523, 65, {"S0": (1, 128, 1, "ranges"), "S": (1, 128, 1, "ranges")}),
+    ("bf16", 1, 65, 2782, {"S0": (1, 128, 1, "ranges"), "S": (1, 128, 1, "ranges")}),
+    ("bf16", 40, 270, 129, {"X": (1, 256)}),
+    ("bf16", 40, 66, 1420, {"X0": (1, 256), "X": (1, 256)}),
+    ("bf16", 2, 454, 2445, {"X0": (2, 256), "X": (2, 256)}),
+    ("bf16", 4, 1198, 450, {"X0": (2, 256)}),
+    ("f32", 40, 143, 129, {"S": (1, 128, 1, 1), "Q": (1, 128, 1, 1)}),
+    ("f32", 40, 133, 160, {"S": (1, 128, 1, 1), "Q": (1, 128, 1, 1)}),
+    ("f32", 16, 280, 258, {"S": (1, 128, 0, 1), "Q": (1, 128, 0, 1), "X": (1, 128)}),
+    ("f32", 16, 257, 300, {"S": (1, 128, 0, 1), "Q": (1, 128, 0, 1), "X": (1, 128)}),
+    ("f32", 1, 360, 348, {"S": (1, 128, 1, "ranges"), "Q": (1, 128, 1, "ranges")}),
+    ("f32", 1, 349, 357, {"S": (1, 128, 1, "ranges"), "Q": (1, 128, 1, "ranges")}),
+    ("f32", 1, 67, 65, {"S": (1, 64, 0, 1), "Q": (1, 64, 0, 1), "X": (1, 64)}),
+    ("f32", 1, 65, 68, {"S": (1, 64, 0, 1), "Q": (1, 64, 0, 1), "X": (1, 64)}),
+]
+
+
+@pytest.mark.parametrize("dtype,n,rows,cols,forms", FORMS)
+def test_each_form(dtype, n, rows, cols, forms):
+    a, s = make(n, rows, cols, dtype, seed=cols)
+    check_forms(orthogonalize_plan(a), forms)
+    s["workspace"][16384:] = 255
+    R.ra_orthogonalize(a)
+    torch.cuda.synchronize()
+    check(s, dtype)
+
+
+def check_forms(plan, forms):
+    for name, want in forms.items():
+        got = plan[name]
+        if want[-1] == "ranges":
+            assert got[-1] > 1, (name, got)
+            got, want = got[:-1], want[:-1]
+        assert got == want, (name, got, want)
+    assert not plan["small"]

@@ -9,7 +9,7 @@ import pytest
 import torch
 
 from paper_2502_19864_gb300 import ringada as R
-from tests.operator_helpers import DT, E, RA, U, workspace
+from tests.operator_helpers import DT, E, RA, U, vocab_loss_plan, workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -290,3 +290,104 @@ def test_one_workspace_for_any_shapes():
     assert bool((ws[:16384] == 0).all())
     for (a, s), dtype in zip(cases, ("bf16", "f32", "bf16", "f32")):
         check(s, dtype)
+
+
+# Sizes and the forms that they run, as vocab_loss_plan has them: pieces of the vocabulary; tiles' CTAs and columns of the logits
+# and of the gradients; whether the gradients' sums are cut ("cut": dx's, dW's).  Between them all the tiles of both types.
+FORMS = [
+    ("bf16", 150, 9923, 960, {"pieces": 1, "forward": (2, 256), "logits": (2, 256)}),
+    ("bf16", 38, 36972, 8, {"pieces": 1, "forward": (1, 256), "logits": (1, 256)}),
+    ("bf16", 36, 19979, 8, {"pieces": 1, "forward": (1, 160)}),
+    ("bf16", 34, 11159, 1264, {"pieces": 1, "forward": (1, 96), "grads": (1, 256), "cut": (True, False)}),
+    ("bf16", 999, 839, 1992, {"pieces": 1, "grads": (2, 256), "cut": (False, False)}),
+    ("bf16", 134, 4886, 1376, {"pieces": 1, "grads": (2, 256), "cut": (True, False)}),
+    ("bf16", 8200, 97, 24, {"pieces": 1, "grads": (1, 64), "cut": (False, True)}),
+    ("bf16", 1303, 43550, 8, {"pieces": 2, "grads": (1, 64)}),
+    ("bf16", 2100, 40001, 64, {"pieces": 2, "grads": (1, 64)}),
+    ("bf16", 1548, 37661, 88, {"pieces": 2, "grads": (1, 128)}),
+    ("bf16", 1025, 58697, 528, {"pieces": 2, "grads": (1, 256)}),
+    ("bf16", 2060, 40001, 520, {"pieces": 2, "grads": (2, 256)}),
+    ("bf16", 3300, 60001, 136, {"pieces": 4}),
+    ("f32", 1370, 66, 1296, {"pieces": 1, "grads": (1, 128), "cut": (False, True)}),
+    ("f32", 4890, 262, 152, {"pieces": 1, "cut": (True, True)}),
+    ("f32", 300, 50003, 64, {"pieces": 2, "grads": (1, 64)}),
+    ("f32", 277, 44441, 88, {"pieces": 2, "grads": (1, 128)}),
+    ("f32", 4134, 5255, 824, {"pieces": 2, "grads": (1, 128), "cut": (False, False)}),
+    ("f32", 2100, 30011, 264, {"pieces": 4, "grads": (1, 128)}),
+]
+
+
+def check_forms(plan, forms):
+    for name, want in forms.items():
+        got = (plan["splits_x"] > 1, plan["splits_w"] > 1) if name == "cut" else plan[name]
+        assert got == want, (name, got, want)
+    assert not plan["few"]
+
+
+@pytest.mark.parametrize("ignored", [0.0, 0.3])
+@pytest.mark.parametrize("dtype,tokens,vocab,hidden,forms", FORMS)
+def test_each_form(dtype, tokens, vocab, hidden, forms, ignored):
+    """With the labels of some tokens at the pieces' borders, a workspace of anything behind its zeros, and each gradient alone."""
+    a, s = make(tokens, vocab, hidden, dtype, ignored=ignored, seed=vocab)
+    p = vocab_loss_plan(a)
+    check_forms(p, forms)
+    at = sorted({w for q in range(p["pieces"]) for w in (q * p["width"], q * p["width"] - 1, q * p["width"] + 1)} & set(range(vocab)) | {vocab - 1})
+    s["labels"][5:5 + len(at)] = torch.tensor(at, dtype=torch.int32, device="cuda")
+    s["workspace"][16384:] = 255
+    n = R.ra_kernel_launches()
+    R.ra_vocab_loss_forward(a)
+    n, n0 = R.ra_kernel_launches(), n
+    R.ra_vocab_loss_backward(a)
+    launched = n - n0, R.ra_kernel_launches() - n
+    torch.cuda.synchronize()
+    pieces, cut_w = p["pieces"], p["splits_w"] > 1
+    if dtype == "bf16":  # numbering, all logits, join; numbering, dz and gradients a piece, sums
+        direct = tokens <= 128
+        assert launched == (2 if direct else 3, 2 + 2 * pieces + cut_w)
+    else:                # and each piece's logits, the later ones' planes of W
+        assert launched == (1 + 2 * pieces, 1 + 3 * pieces + cut_w)
+    check(s, dtype)
+    assert int(s["err"]) == 0
+    want = {g: s[g].clone() for g in ("dx", "dw")}
+    for keep in ("dx", "dw"):
+        for g in ("dx", "dw"):
+            s[g].fill_(7.0)
+            setattr(a, g + "_dev", s[g].data_ptr() if g == keep else None)
+        s["workspace"][16384:] = 255
+        R.ra_vocab_loss_backward(a)
+        torch.cuda.synchronize()
+        for g in ("dx", "dw"):
+            assert torch.equal(s[g], want[g]) if g == keep else bool((s[g] == 7.0).all()), (keep, g)
+
+
+@pytest.mark.parametrize("dtype,tokens,vocab", [("bf16", 2100, 40001), ("f32", 300, 50003)])
+@pytest.mark.parametrize("which", ["none", "first piece", "last word"])
+def test_pieces_that_no_label_is_in(dtype, tokens, vocab, which):
+    a, s = make(tokens, vocab, 64, dtype, ignored=0.2)
+    width = vocab_loss_plan(a)["width"]
+    assert width < vocab
+    on = s["labels"] >= 0
+    s["labels"][on] = {"none": -1, "last word": vocab - 1}.get(which, 0) if which != "first piece" else s["labels"][on] % width
+    s["workspace"][16384:] = 255
+    both(a)
+    torch.cuda.synchronize()
+    check(s, dtype)
+
+
+@pytest.mark.parametrize("dtype,tokens,vocab", [("bf16", 2100, 40001), ("f32", 300, 50003)])
+def test_pieces_captured(dtype, tokens, vocab):
+    a, s = make(tokens, vocab, 64, dtype)
+    assert vocab_loss_plan(a)["pieces"] > 1
+    both(a)
+    torch.cuda.synchronize()
+    want = {n: s[n].clone() for n in ("loss", "lse", "dx", "dw")}
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both(a, torch.cuda.current_stream())
+    for n in want:
+        s[n].fill_(7.0)
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    for n in want:
+        assert torch.equal(s[n], want[n]), n

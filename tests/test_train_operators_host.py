@@ -120,3 +120,16 @@ def test_products_let_dependents_start_behind_the_allocation():
     body = re.sub(r"//[^\n]*", "", open(path).read()).split("__global__")[1]
     barrier = body.index("__syncthreads()", body.rindex("tcgen05.alloc"))
     assert body.index("pdl_trigger()") > barrier
+
+
+def test_forms_of_the_tested_sizes():
+    """The sizes at which the GPU tests run each form of the products do take it: the forms come from times that may be fitted anew."""
+    from tests import test_gpu_orthogonalize as O
+    from tests import test_gpu_vocab_loss as V
+    from tests.operator_helpers import RA, orthogonalize_plan, vocab_loss_plan
+    for dtype, tokens, vocab, hidden, forms in V.FORMS:
+        V.check_forms(vocab_loss_plan(loss(tokens=tokens, vocab=vocab, hidden=hidden, x_stride=hidden, w_stride=hidden, dx_stride=hidden,
+                                           dw_stride=hidden, dtype=RA[dtype])), forms)
+    for dtype, n, rows, cols, forms in O.FORMS:
+        O.check_forms(orthogonalize_plan(orth(n_matrices=n, rows=rows, cols=cols, x_stride=cols, out_stride=cols, x_matrix_stride=rows * cols,
+                                              out_matrix_stride=rows * cols, dtype=RA[dtype])), forms)
