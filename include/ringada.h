@@ -608,7 +608,7 @@ ra_status ra_norm_backward(const ra_norm_args* args, ra_stream_t stream);
  * the mean over n counted ones), and writes dx [tokens, hidden] (zero for those not counted) and dw [vocab, hidden],
  * either of them where it is not NULL, in fixed orders.
  * bf16: products of bf16 values summed in float32; dz = dloss (softmax - onehot) enters its two products over the largest |dloss|,
- * rounded to bf16.
+ * rounded to bf16 (of up to 128 tokens: to the sum of two bf16 values, 16 bits).
  * hidden is a multiple of 8 (bf16) or 4 (f32), rows at 16-byte boundaries. */
 typedef struct {
   const void* x_dev; int64_t x_stride;

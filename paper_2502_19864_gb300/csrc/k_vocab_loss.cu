@@ -5,7 +5,7 @@
 // Forward: tiles of logits z = x W^T; of each tile's rows the maximum and the sum of exp(z - maximum) go to the workspace,
 // with the label's logit; a second kernel joins them: lse = m + log(sum), loss = lse - z[label].
 // Backward, piece by piece of the vocabulary: the piece's logits again and dz = dloss (exp(z - lse) - onehot) into the
-// workspace (rounded, in bf16, relative to the largest |dloss|); then, in one launch, dw of the piece = dz^T x and the sums of dx += dz W, the latter in fp32 and, where its tiles are
+// workspace (rounded, in bf16, relative to the largest |dloss|; of up to 128 tokens in two terms); then, in one launch, dw of the piece = dz^T x and the sums of dx += dz W, the latter in fp32 and, where its tiles are
 // few, in parts of the vocabulary, which a last kernel adds up and puts where the tokens were.
 // fp32 operands are cut into three planes of bf16 (products.cuh), dz too; bf16 ones are read where they are.
 //
@@ -223,8 +223,8 @@ __device__ __forceinline__ const CUtensorMap* hidden_map(const VocabArgs& p, int
   return p.planes == 1 && count == p.tokens ? given : gathered;
 }
 
-// tiles of logits; BACK: into dz, else into statistics; PLANES: of the operands and of dz
-template <bool BACK, int PLANES>
+// tiles of logits; BACK: into dz, else into statistics; PLANES: of the operands; DZ: of dz
+template <bool BACK, int PLANES, int DZ>
 struct Logits {
   static constexpr int PA = PLANES, PB = PLANES;
   static constexpr bool PARTS = BACK, ONE = false;
@@ -270,8 +270,8 @@ struct Logits {
       v[j] = j < left ? __fmul_rn(scale, c + j == label ? __fsub_rn(e, 1.f) : e) : 0.f;
     }
     auto at = [&](int j) { return v[j]; };
-    if (PLANES == 1) st.bf16_row(&p.dz, at, w.n0 + c, row0, 0);
-    else st.planes<3, false>(&p.dz, at, w.n0 + c, row0, 0);
+    if constexpr (DZ == 1) st.bf16_row(&p.dz, at, w.n0 + c, row0, 0);
+    else st.planes<DZ, false>(&p.dz, at, w.n0 + c, row0, 0);
   }
   template <int CH>
   static __device__ __forceinline__ void finish(const Args& p, const Unit& w, const Tile& t, Store& st, float (&v)[CH][32]) {
@@ -304,9 +304,9 @@ struct Logits {
 };
 
 // dx sums (job 0) and dw (job 1) of a piece, the longer ones first
-template <int PLANES>
+template <int PLANES, int DZ>
 struct Grads {
-  static constexpr int PA = PLANES, PB = PLANES;
+  static constexpr int PA = DZ, PB = PLANES;
   static constexpr bool PARTS = true, ONE = false;
   using Args = VocabArgs;
   struct Count {
@@ -701,7 +701,7 @@ __global__ void __launch_bounds__(128) vocab_few_sum_kernel(const __grid_constan
 
 // ---- the plan -----------------------------------------------------------------------------
 struct Plan {
-  int planes, rows, chunk;
+  int planes, dz_planes, rows, chunk;
   int wide, pitch;                // of gathered or split rows: columns to a multiple of 8, 128-byte boundaries
   int pieces, width;              // of the vocabulary, backward (and fp32 forward)
   Pick forward, logits, grads;    // (forward: of its logits)
@@ -716,19 +716,23 @@ Plan plan(const ra_vocab_loss_args& a) {
   Plan p = {};
   const bool f32 = a.dtype == RA_F32;
   p.planes = f32 ? 3 : 1;
+  // bf16: of one row of tiles, where W's bytes and the launches bound and not the products, dz keeps 16 bits: 107 x 359 x 664 trained
+  // 29.3 -> 30.5 us, 16 x 32000 x 2048 154 -> 162, and gradients as far from 64 bits as their own rounding (0.0017; with 8 bits 0.0019 at
+  // the former).  Of more tokens the second plane's products are paid for: 1024 x 32000 x 256 94 -> 129 us, 4096 x 4096 x 1024 128 -> 167
+  p.dz_planes = f32 ? 3 : a.tokens <= prod::BM ? 2 : 1;
   p.chunk = f32 ? 4 : 128;
   p.rows = up(a.tokens > 0 ? a.tokens : 1, ROWS);
   p.wide = up(a.hidden, 8);
   p.pitch = up(a.hidden, 64);
   // pieces of at most 128 MB of dz
-  int64_t most = (128ll << 20) / (2ll * p.planes * p.rows) / 256 * 256;
+  int64_t most = (128ll << 20) / (2ll * p.dz_planes * p.rows) / 256 * 256;
   most = std::max<int64_t>(most, 256);
   p.pieces = parts_of(a.vocab, (int)std::min<int64_t>(most, 1 << 24));
   p.width = up(parts_of(a.vocab, p.pieces), 256);
   p.pieces = parts_of(a.vocab, p.width);
 
-  const int hb = parts_of(a.hidden, prod::BK), terms = prod::terms_of(p.planes, p.planes).n;
-  p.logits = prod::pick(a.tokens, p.pieces == 1 || !f32 ? a.vocab : p.width, 1, hb * terms, p.planes, p.planes);
+  const int hb = parts_of(a.hidden, prod::BK), terms = prod::terms_of(p.dz_planes, p.planes).n;
+  p.logits = prod::pick(a.tokens, p.pieces == 1 || !f32 ? a.vocab : p.width, 1, hb * prod::terms_of(p.planes, p.planes).n, p.planes, p.planes);
   if (p.logits.bn < 128) p.logits.bn = 128;
   p.forward = p.logits;
   if (a.tokens <= prod::BM && !f32) {
@@ -743,7 +747,7 @@ Plan plan(const ra_vocab_loss_args& a) {
   for (Pick k : {Pick{1, 64}, Pick{1, 128}, Pick{1, 256}, Pick{2, 128}, Pick{2, 256}}) {
     if (k.cg == 2 && (a.tokens <= prod::BM || a.hidden <= 128)) continue;
     if (k.bn > 64 && a.hidden <= k.bn / 2) continue;
-    if (!prod::takes(k, p.planes, p.planes)) continue;
+    if (!prod::takes(k, p.dz_planes, p.planes)) continue;
     const int64_t nt = parts_of(a.hidden, k.bn);
     const int64_t ux = parts_of(a.tokens, prod::BM * k.cg) * nt, uw = parts_of(p.width, prod::BM * k.cg) * nt;
     const double all = (double)ux * kx + (double)uw * kw, workers = SMS / k.cg;
@@ -781,7 +785,7 @@ Plan plan(const ra_vocab_loss_args& a) {
   p.st = take((size_t)p.stats * p.rows * sizeof(float2));
   const size_t forward = at;
   at = shared;
-  p.dz = take((size_t)p.planes * p.rows * p.width * 2);
+  p.dz = take((size_t)p.dz_planes * p.rows * p.width * 2);
   p.dxs = take((size_t)p.splits_x * p.rows * p.pitch * 4);
   p.dws = take(p.splits_w > 1 ? (size_t)p.splits_w * p.width * p.pitch * 4 : 0);
   p.bytes = a.dx_dev || a.dw_dev ? std::max(at, forward) : forward;
@@ -897,14 +901,14 @@ cudaError_t forward(const ra_vocab_loss_args& a, cudaStream_t st) {
     DO(piece(a, p, ws, g, v0, width, st));
     if (p.planes > 1) DO(w_map(a, p, ws, g.w, width, p.forward.bn / p.forward.cg));
     const int64_t tiles = (int64_t)parts_of(a.tokens, prod::BM * g.cg) * parts_of(width, g.shape.bn);
-    DO((products<Logits<false, PLANES>>(g, tiles, st)));
+    DO((products<Logits<false, PLANES, PLANES>>(g, tiles, st)));
     g.stat0 += 2 * parts_of(width, g.shape.bn);
   }
   note_launch(1);
   return launch_pdl(vocab_join_kernel, dim3(parts_of(a.tokens, 8)), dim3(512), 0, st, a, r, (const float2*)g.stats, (const float*)g.zlab, (int)g.stat0, (int)direct);
 }
 
-template <typename T, int PLANES>
+template <typename T, int PLANES, int DZ>
 cudaError_t backward(const ra_vocab_loss_args& a, cudaStream_t st) {
   const Plan p = plan(a);
   char* ws = static_cast<char*>(a.workspace_dev);
@@ -925,7 +929,7 @@ cudaError_t backward(const ra_vocab_loss_args& a, cudaStream_t st) {
   g.cg = p.logits.cg;
   g.shape = prod::shape_of(p.logits.bn, p.logits.cg, p.planes, p.planes, std::min(p.chunk, LOGITS_CHUNK));
   h.cg = p.grads.cg;
-  h.shape = prod::shape_of(p.grads.bn, p.grads.cg, p.planes, p.planes, p.chunk);
+  h.shape = prod::shape_of(p.grads.bn, p.grads.cg, DZ, p.planes, p.chunk);
   if (p.planes == 1) {
     DO(w_map(a, p, ws, g.w, a.vocab, p.logits.bn / p.logits.cg));
     DO(w_map(a, p, ws, h.wm, a.vocab, 64));
@@ -935,18 +939,18 @@ cudaError_t backward(const ra_vocab_loss_args& a, cudaStream_t st) {
     const int width = std::min(p.width, a.vocab - v0);
     DO(piece(a, p, ws, g, v0, width, st));
     if (p.planes > 1) DO(w_map(a, p, ws, g.w, width, p.logits.bn / p.logits.cg));
-    MAP(g.dz, ws + p.dz, DT_BF16, p.planes, p.rows, p.width, p.width, 32, 32);
+    MAP(g.dz, ws + p.dz, DT_BF16, DZ, p.rows, p.width, p.width, 32, 32);
     const int64_t tiles = (int64_t)parts_of(a.tokens, prod::BM * g.cg) * parts_of(width, g.shape.bn);
-    DO((products<Logits<true, PLANES>>(g, tiles, st)));
+    DO((products<Logits<true, PLANES, DZ>>(g, tiles, st)));
     h.v0 = v0;
     h.width = width;
     h.wrow = g.wrow;
     if (p.planes > 1) DO(w_map(a, p, ws, h.wm, width, 64));
-    MAP(h.dzk, ws + p.dz, DT_BF16, p.planes, p.rows, p.width, p.width, 64, prod::BM);
-    MAP(h.dzm, ws + p.dz, DT_BF16, p.planes, p.rows, p.width, p.width, 64, 64);
+    MAP(h.dzk, ws + p.dz, DT_BF16, DZ, p.rows, p.width, p.width, 64, prod::BM);
+    MAP(h.dzm, ws + p.dz, DT_BF16, DZ, p.rows, p.width, p.width, 64, 64);
     const int64_t nt = parts_of(a.hidden, h.shape.bn);
-    DO(products<Grads<PLANES>>(h, nt * ((h.want_x ? (int64_t)parts_of(a.tokens, prod::BM * h.cg) * h.splits_x : 0) +
-                                (h.want_w ? (int64_t)parts_of(width, prod::BM * h.cg) * h.splits_w : 0)), st));
+    DO((products<Grads<PLANES, DZ>>(h, nt * ((h.want_x ? (int64_t)parts_of(a.tokens, prod::BM * h.cg) * h.splits_x : 0) +
+                                (h.want_w ? (int64_t)parts_of(width, prod::BM * h.cg) * h.splits_w : 0)), st)));
   }
   if (a.dw_dev && p.splits_w > 1) {
     note_launch(1);
@@ -1047,7 +1051,8 @@ cudaError_t vocab_loss_bwd(const ra_vocab_loss_args& a, cudaStream_t st) {
     return cudaMemset2DAsync(a.dw_dev, a.dw_stride * es, 0, a.hidden * es, a.vocab, st);
   }
   if (few(a)) return few_any(a, true, st);
-  return a.dtype == RA_BF16 ? backward<bf16, 1>(a, st) : backward<float, 3>(a, st);
+  if (a.dtype == RA_F32) return backward<float, 3, 3>(a, st);
+  return plan(a).dz_planes == 2 ? backward<bf16, 1, 2>(a, st) : backward<bf16, 1, 1>(a, st);
 }
 
 }  // namespace ra

@@ -391,3 +391,28 @@ def test_pieces_captured(dtype, tokens, vocab):
     torch.cuda.synchronize()
     for n in want:
         assert torch.equal(s[n], want[n]), n
+
+
+@pytest.mark.parametrize("tokens,vocab,hidden", [(1, 200, 64), (2, 332, 1104), (20, 700, 64), (107, 359, 664), (128, 1003, 256), (100, 140001, 64)])
+def test_few_bf16_tokens_keep_16_bits_of_dz(tokens, vocab, hidden):
+    """Of up to 128 tokens dz enters its products as two bf16 terms: e^2 |dz| stands in the bounds where e |dz| does for more tokens."""
+    a, s = make(tokens, vocab, hidden, "bf16", ignored=0.0, seed=hidden)
+    s["workspace"][16384:] = 255
+    both(a)
+    torch.cuda.synchronize()
+    check(s, "bf16")
+    x, w, lab = s["x"].double(), s["w"].double(), s["labels"].long()
+    row = torch.arange(tokens, device="cuda")
+    z = x @ w.T
+    top = (hidden + 8) * U * (x.abs() @ w.abs().T).amax(1)
+    lse = torch.logsumexp(z, 1)
+    p = torch.exp(z - lse[:, None])
+    dp = 2 * top + 2 * U * (z - lse[:, None]).abs().amax(1) + 8 * U + (128 + vocab / 64) * U
+    d = p.clone()
+    d[row, lab] -= 1
+    scale = s["dloss"].double()[:, None]
+    G = d * scale
+    dG = scale * (p * dp[:, None] + 2 * U * d.abs()) + E * E * G.abs()
+    for name, want, bound in (("dx", G @ w, dG @ w.abs() + (vocab + 8) * U * (G.abs() @ w.abs())),
+                              ("dw", G.T @ x, dG.T @ x.abs() + (tokens + 8) * U * (G.abs().T @ x.abs()))):
+        near(s[name], want, bound + (E + U) * want.abs(), name)
