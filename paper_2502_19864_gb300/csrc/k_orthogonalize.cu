@@ -919,7 +919,7 @@ cudaError_t run(const ra_orthogonalize_args& a, cudaStream_t st) {
     using S = decltype(step);
     int mt, nt;
     const int u = (int)std::min<int64_t>((int64_t)n * S::tiles(s, mt, nt) * s.splits, 1 << 20);
-    return s.cg == 2 ? prod::launch<S, 2>(s, u, st) : prod::launch<S, 1>(s, u, st);
+    return prod::launch<S>(s, s.cg, u, st);
   };
   OrthArgs square = g;
   // a symmetric product into `to`

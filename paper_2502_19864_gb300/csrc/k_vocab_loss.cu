@@ -744,7 +744,7 @@ Plan plan(const ra_vocab_loss_args& a) {
 
   const int kx = parts_of(p.width, prod::BK), kw = parts_of(a.tokens > 0 ? a.tokens : 1, prod::BK);
   double best = 1e30;
-  for (Pick k : {Pick{1, 64}, Pick{1, 128}, Pick{1, 256}, Pick{2, 128}, Pick{2, 256}}) {
+  for (Pick k : {Pick{1, 64}, Pick{1, 128}, Pick{1, 256}, Pick{2, 256}}) {
     if (k.cg == 2 && (a.tokens <= prod::BM || a.hidden <= 128)) continue;
     if (k.bn > 64 && a.hidden <= k.bn / 2) continue;
     if (!prod::takes(k, p.dz_planes, p.planes)) continue;
@@ -867,7 +867,7 @@ cudaError_t w_map(const ra_vocab_loss_args& a, const Plan& p, char* ws, CUtensor
 template <class P>
 cudaError_t products(const VocabArgs& g, int64_t units, cudaStream_t st) {
   const int n = (int)std::min<int64_t>(units, 1 << 20);
-  return g.cg == 2 ? prod::launch<P, 2>(g, n, st) : prod::launch<P, 1>(g, n, st);
+  return prod::launch<P>(g, g.cg, n, st);
 }
 // hidden states as given (bf16) and gathered, in boxes of box_rows rows
 cudaError_t x_maps(const ra_vocab_loss_args& a, const Plan& p, char* ws, CUtensorMap& given, CUtensorMap& gathered, int box_rows) {

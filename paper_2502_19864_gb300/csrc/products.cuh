@@ -85,7 +85,7 @@ inline int up(int64_t a, int b) { return (int)((a + b - 1) / b * b); }
 // microseconds of a k-block of a tile (measured on long products; the issue of products and copies paces the narrow ones, power the widest:
 // by the share of SMs that have one)
 inline double block_time(Pick k, double share = 1.) {
-  if (k.cg == 2) return k.bn > 128 ? 0.24 + 0.105 * (share < 1. ? share : 1.) : 0.25;
+  if (k.cg == 2) return 0.24 + 0.105 * (share < 1. ? share : 1.);  // (256 columns: of 128 a pair takes longer than its CTAs apart, 0.25)
   return k.bn <= 64 ? 0.2 : k.bn <= 128 ? 0.222 : k.bn <= 192 ? 0.31 : 0.365;
 }
 // ... of `tiles` tiles of `blocks` k-blocks, terms counted, in rounds, each with about 1 us for its start and end, and a tile's epilogue,
@@ -103,7 +103,7 @@ inline bool takes(Pick k, int pa, int pb) { return stages_of(k.bn, k.cg, pa, pb)
 // the fastest
 inline Pick pick(int64_t m, int64_t n, int64_t batch, int blocks, int pa, int pb, double out = 0.) {
   Pick best = {1, n <= 64 ? 64 : 128};
-  for (Pick k : {Pick{1, 64}, Pick{1, 256}, Pick{2, 128}, Pick{2, 256}})
+  for (Pick k : {Pick{1, 64}, Pick{1, 256}, Pick{2, 256}})
     if ((k.cg == 1 || m > BM) && n > k.bn / 2 && takes(k, pa, pb) &&
         time_of(k, m, n, batch, blocks, out) < time_of(best, m, n, batch, blocks, out))
       best = k;
@@ -545,6 +545,10 @@ __global__ void __launch_bounds__(THREADS, 1) products_kernel(const __grid_const
   }
 }
 
+// (tiles of three planes have at most 128 columns, and are one CTA's)
+template <class P>
+constexpr bool has_pairs() { return P::PA < 3 && P::PB < 3; }
+
 template <class P, int CG>
 cudaError_t launch(const typename P::Args& p, int units, cudaStream_t st) {
   auto k = products_kernel<P, CG>;
@@ -566,6 +570,12 @@ cudaError_t launch(const typename P::Args& p, int units, cudaStream_t st) {
   cfg.numAttrs = CG == 2 ? 2 : 1;
   note_launch(1);
   return cudaLaunchKernelEx(&cfg, k, p);
+}
+template <class P>
+cudaError_t launch(const typename P::Args& p, int cg, int units, cudaStream_t st) {
+  if constexpr (has_pairs<P>())
+    if (cg == 2) return launch<P, 2>(p, units, st);
+  return launch<P, 1>(p, units, st);
 }
 
 }  // namespace prod
