@@ -632,7 +632,7 @@ ra_status ra_vocab_loss_backward(const ra_vocab_loss_args* args, ra_stream_t str
  *   X <- a X + (b X X^T + c (X X^T)^2) X
  * and out = X in the type.  With a = 3.4445, b = -4.775, c = 2.0315 five steps bring singular values that are not too
  * small to between about 0.7 and 1.2 (what is subtracted from a weight in place of its momentum).  A matrix with an
- * element that is not finite gives no finite value.  rows and cols of 1 to 32768, any strides; out may be x. */
+ * element that is not finite gives no finite value, one of zeros gives zeros (with eps = 0 too).  rows and cols of 1 to 32768, any strides; out may be x. */
 typedef struct {
   const void* x_dev; int64_t x_stride, x_matrix_stride;
   void* out_dev; int64_t out_stride, out_matrix_stride;

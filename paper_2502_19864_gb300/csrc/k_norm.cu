@@ -7,12 +7,15 @@
 // dgamma = sum dy u, dbeta = sum dy, which each CTA keeps in registers over its rows; the CTAs' partial sums are added in
 // a second kernel, in a fixed order.
 //
-// Bound: bytes.  A row is read once, held in registers through the reductions and written once.  A CTA's threads share a row (one
-// of up to 256 values: a warp's, eight warps a CTA), eight (16, 32) values each, and take ROWS rows at a time, so that enough
-// loads are on their way and a barrier serves them all; two values an instruction, as the instructions' issue is the next bound (28
-// a value without: 165 us, with 137).
+// Bound: bytes.  A row is read once, held in registers (or, on its way through a ring, in shared memory) through the reductions
+// and written once.  A CTA's threads share a row (one of up to 256 values: a warp's, eight warps a CTA), eight (16, 32) values each, and
+// take ROWS rows at a time, so that enough loads are on their way and a barrier serves them all; two values an instruction, as the
+// instructions' issue is the next bound (28 a value without: 165 us, with 137).
 // Forward and backward of 65536 x 1024 in bf16 take 137 us (4.9 TB/s), of 8192 x 2048 with its residual 52 us (5.2 TB/s), of
 // 16271 x 1334, in pieces of 4 bytes, 135 us (2.5 TB/s).
+// Rows over 8192 values have 32 a thread and the 64 registers of 1024 threads.  The forward has room: 4096 x 8200 in bf16 with its
+// residual 64 us (4.2 TB/s), 2048 x 32768 117 us (4.6).  The backward, which holds the weights, their sums and three inputs, spills 1.0 to
+// 1.9 KB a thread: 200 us (1.3 TB/s, where 4096 x 8192 takes 52) and 449; in fp32 440 and 790.
 #include <algorithm>
 
 #include "common.cuh"
@@ -613,8 +616,8 @@ cudaError_t launch(const ra_norm_args& a, cudaStream_t st) {
   }
 }
 
-// rows of the ring by their values' size, and its groups (65536 x 1024 and 8192 x 2048 trained: 140 and 54 us; two rows and three
-// groups 154 and 62, three groups 145 and 60; without a ring 173 and 82)
+// rows of the ring by their values' size, and its groups (65536 x 1024 and 8192 x 2048 trained: 140 and 54 us when these were measured, 137
+// and 52 now; two rows and three groups 154 and 62, three groups 145 and 60; without a ring 173 and 82)
 constexpr int RING_ROWS = 8, RING_DEPTH = 2;
 
 // The widest accesses that all rows and weights allow, up to 16 bytes

@@ -1,7 +1,8 @@
 // k_vocab_loss.cu -- cross-entropy over a vocabulary from hidden states, without keeping logits.
 //
 // First the tokens that are counted are found and numbered (a CTA counts those before its own), and where not all are, their
-// hidden states are gathered, so that what is not counted costs nothing and is never read.
+// hidden states are gathered, so that what is not counted costs nothing and is never read.  (But for the forward of up to 128 bf16 tokens,
+// which are one row of tiles in any case: it takes them as they are, reads all of W, and drops the results of those that are not counted.)
 // Forward: tiles of logits z = x W^T; of each tile's rows the maximum and the sum of exp(z - maximum) go to the workspace,
 // with the label's logit; a second kernel joins them: lse = m + log(sum), loss = lse - z[label].
 // Backward, piece by piece of the vocabulary: the piece's logits again and dz = dloss (exp(z - lse) - onehot) into the
@@ -10,8 +11,9 @@
 // fp32 operands are cut into three planes of bf16 (products.cuh), dz too; bf16 ones are read where they are.
 //
 // Bound: the products, four of tokens x vocab x hidden with the logits computed again (keeping them would be three, and 2 tokens x
-// vocab bytes).  8192 x 32000 x 2048 in bf16: forward 0.53 ms (2.0 PFLOP/s), backward 0.58 ms of logits again and 1.16 ms of
-// gradients (1.85 PFLOP/s), 2.69 ms in all.  Few tokens: W's bytes; 16 of 32000 x 2048 in 33 us (3.9 TB/s).
+// vocab bytes).  8192 x 32000 x 2048 in bf16, one pass after the other: forward 0.55 ms (2.0 PFLOP/s), backward 2.0 ms (1.6 PFLOP/s), 2.65 ms
+// in all, at the clock that the power leaves.  One launch at a time, with pauses, the logits take 0.53 ms, the backward's 0.59 and its
+// gradients 1.18 (1.8 PFLOP/s).  Few tokens: W's bytes; 16 of 32000 x 2048 in 33 us (3.9 TB/s).
 #include <algorithm>
 
 #include "common.cuh"
