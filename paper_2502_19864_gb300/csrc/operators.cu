@@ -312,11 +312,13 @@ ra_status ra_orthogonalize(const ra_orthogonalize_args* args, ra_stream_t stream
 
 // (not in the header: what the launchers choose, for tests)
 ra_status ra_internal_vocab_loss_plan(const ra_vocab_loss_args* args, int32_t (&out)[12]) {
+  if (!args || args->tokens == 0) return RA_ERR_ARG;
   TRY(check_vocab(*args, false));
   vocab_loss_plan(*args, out);
   return RA_OK;
 }
 ra_status ra_internal_orthogonalize_plan(const ra_orthogonalize_args* args, int32_t (&out)[17]) {
+  if (!args || args->n_matrices == 0) return RA_ERR_ARG;
   TRY(check_orthogonalize(*args));
   orthogonalize_plan(*args, out);
   return RA_OK;

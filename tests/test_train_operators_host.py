@@ -133,3 +133,13 @@ def test_forms_of_the_tested_sizes():
     for dtype, n, rows, cols, forms in O.FORMS:
         O.check_forms(orthogonalize_plan(orth(n_matrices=n, rows=rows, cols=cols, x_stride=cols, out_stride=cols, x_matrix_stride=rows * cols,
                                               out_matrix_stride=rows * cols, dtype=RA[dtype])), forms)
+
+
+def test_no_form_of_no_work():
+    import ctypes as C
+    out = (C.c_int32 * 17)()
+    for plan, blocks in ((R.lib().ra_internal_vocab_loss_plan, (loss(tokens=0), loss(tokens=-1), loss(x_dev=None))),
+                         (R.lib().ra_internal_orthogonalize_plan, (orth(n_matrices=0), orth(n_matrices=-1), orth(x_dev=None)))):
+        assert plan(None, out) == ARG
+        for block in blocks:
+            assert plan(C.byref(block), out) == ARG
